@@ -616,6 +616,119 @@ int oilbird_query_static(const oilbird_static_pool* pool, const void* q_bf16 /* 
                          const oilbird_query_out* out, void* cuda_stream);
 const char* oilbird_query_static_error(void);   /* why the last call was rejected        */
 
+/*
+ * The verifier's key/value cache in 4 bits (not in the paper, whose verifier is a given; the
+ * Limitations section asks for bounded memory).  One forward pass of the verifier over a
+ * request's draft tree is, per layer: attend() from every node to the request's cached context
+ * and to the nodes it sees (the mask oilbird_merge_chains writes); once the accepted path is
+ * known, weigh() adds the attention weight its nodes gave to every cached slot; append()
+ * stores the path's keys and values; evict() cuts a cache that has outgrown its budget to the
+ * slots that received most weight.  read() gives stored rows back in 16 bits.  A decoding step
+ * without a tree is a tree of one node.
+ *
+ * All arrays are the caller's; the struct only names them (one per layer; copy it, pass it by
+ * pointer).  Positions are already in the keys (rotated before they are stored).
+ *   pages       [n_pages, n_kv_heads] blocks of oilbird_kv_block_bytes(head_dim, page_size)
+ *   weight      fp32 accumulated attention weight of each slot;  pos: its position
+ *   page_table  pages of each sequence in order; an entry that names no page (negative, or
+ *               n_pages and above) is a page without content: nothing is read or stored there
+ *   seq_len     slots each sequence holds;  n_pos: positions it has seen (append and evict
+ *               update them in stream order)
+ *   workspace   zeroed once by the caller; one stream at a time
+ * Block layout, for `page` slots, groups g of 64 channels: K codes [g][slot][32 bytes], K meta
+ * [slot][g] (32-bit word: scale in the low half, lo in the high half, both of the cache's
+ * 16-bit type), then V codes and V meta likewise.  Channel 8w+2n of a group is bits 4n..4n+3 of
+ * its little-endian word w, channel 8w+2n+1 bits 16+4n..19+4n (n = 0..3).  An element stands for
+ * scale * code + lo, with lo = the group's minimum, scale = rn16((maximum - lo) / 15) and
+ * code = rint((x - lo) / scale) in 0..15 (scale 0: code 0).  A group holding a NaN or an
+ * infinity reads as NaN.
+ *
+ * head_dim 64 or 128; page_size 16, 32 or 64; bf16 or f16; up to OILBIRD_KV_MAX_SEQ sequences,
+ * up to OILBIRD_TREE_MAX_NODES nodes each.  Refusals return OILBIRD_EINVAL and leave the
+ * reason in oilbird_kv_last_error().  Nothing synchronises (but status()) or allocates; the
+ * calls can be captured in a CUDA graph after the first call on the device.
+ */
+#define OILBIRD_KV_BF16          0
+#define OILBIRD_KV_F16           1
+#define OILBIRD_KV_MAX_SEQ    1024
+#define OILBIRD_KV_MAX_GROUP    64   /* query heads per key/value head                    */
+#define OILBIRD_KV_MAX_EVICT_SLOTS 851968  /* slots per sequence that evict() can handle  */
+typedef struct {
+  void*          pages;        /* dev, 16-byte aligned                                    */
+  float*         weight;       /* dev [n_pages, n_kv_heads, page_size]                    */
+  int32_t*       pos;          /* dev [n_pages, n_kv_heads, page_size]                    */
+  const int32_t* page_table;   /* dev [n_seq, max_pages]                                  */
+  int32_t*       seq_len;      /* dev [n_seq]                                             */
+  int32_t*       n_pos;        /* dev [n_seq]                                             */
+  void*          workspace;    /* dev, 16-byte aligned                                    */
+  size_t         workspace_bytes;
+  int64_t        n_pages;
+  int32_t        n_seq, max_pages, page_size, n_kv_heads, head_dim;
+  int32_t        dtype;        /* OILBIRD_KV_BF16 or OILBIRD_KV_F16                       */
+  int32_t        device;       /* CUDA ordinal                                            */
+} oilbird_kv_cache;
+/* 16-bit elements [sequence, row, head, channel]; strides in elements, multiples of 8; channels
+ * are contiguous; data 16-byte aligned. */
+typedef struct {
+  const void* data;
+  int64_t seq_stride, row_stride, head_stride;
+} oilbird_kv_rows;
+int64_t oilbird_kv_block_bytes(int32_t head_dim, int32_t page_size);   /* 0: not offered    */
+size_t  oilbird_kv_workspace_bytes(int32_t head_dim);
+/*
+ * Append: of the m rows per sequence in k and v, the rows select[s, 0..n) (dev [n_seq, rows];
+ * NULL: rows 0..n) are stored at slots seq_len[s].. with positions n_pos[s].., n = n_new[s] (dev;
+ * NULL: `rows`).  weight: dev [n_seq, n_kv_heads, m] the rows' first weights, NULL: 0.  A row
+ * that finds no page, or a select entry outside 0..m-1, is not stored (its slot counts) and is
+ * counted in status().
+ */
+int oilbird_kv_append(const oilbird_kv_cache* cache, const oilbird_kv_rows* k,
+                      const oilbird_kv_rows* v, int32_t m, int32_t rows, const int32_t* n_new,
+                      const int32_t* select, const float* weight, void* cuda_stream);
+/* Slots start[s].. (dev [n_seq]; NULL: 0) as 16-bit rows: k, v dev [n_seq, n, n_kv_heads,
+ * head_dim]; zeros where there is no slot. */
+int oilbird_kv_read(const oilbird_kv_cache* cache, int32_t n, const int32_t* start, void* k,
+                    void* v, void* cuda_stream);
+/*
+ * Attention of m nodes per sequence: q [n_seq, m, n_q_heads, head_dim] (head h reads key/value
+ * head h / (n_q_heads / n_kv_heads)), scores scale * q.k over every slot of the sequence and,
+ * with k_new and v_new ([n_seq, m, n_kv_heads, head_dim], in 16 bits), over the nodes j whose
+ * bit is set in the node's mask word (dev, mask_stride words per sequence; NULL: nodes 0..i).
+ * n_new: nodes of each sequence (dev; NULL: m); what lies behind them gets out = 0, lse = -inf,
+ * and so does a row that sees nothing.  out: like q, written; lse: dev fp32 [n_seq, m, n_q_heads],
+ * natural logarithm of the sum of exponentials, may be NULL; lse_strides (host): its strides in
+ * elements for sequence, node and head, NULL: contiguous.
+ */
+int oilbird_kv_attend(const oilbird_kv_cache* cache, int32_t n_q_heads, int32_t m,
+                      const oilbird_kv_rows* q, const oilbird_kv_rows* k_new,
+                      const oilbird_kv_rows* v_new, const uint64_t* mask, int64_t mask_stride,
+                      const int32_t* n_new, float scale, const oilbird_kv_rows* out, float* lse,
+                      const int64_t* lse_strides, void* cuda_stream);
+/*
+ * Accumulate: weight[slot, head] += sum over nodes i and the head's query heads of
+ * row_weight[s, i] * exp(scale * q.k - lse), with the same arguments as attend and its lse.
+ * row_weight: dev fp32 [n_seq, m], NULL: 1; nodes with weight 0 cost nothing.  node_weight: dev
+ * fp32 [n_seq, n_kv_heads, m], the same sums for the nodes themselves (append()'s `weight`),
+ * written; given with k_new or not at all.
+ */
+int oilbird_kv_weigh(const oilbird_kv_cache* cache, int32_t n_q_heads, int32_t m,
+                     const oilbird_kv_rows* q, const float* lse, const int64_t* lse_strides,
+                     const oilbird_kv_rows* k_new, const uint64_t* mask, int64_t mask_stride,
+                     const int32_t* n_new, const float* row_weight, float scale, float* node_weight, void* cuda_stream);
+/*
+ * Evict: every sequence with more than `budget` slots keeps, for each head by itself, the slots
+ * with position < sink or >= n_pos - recent, then the others by (weight descending, position
+ * ascending; a NaN weight counts as the lowest) up to `budget`.  Slots are not put in order:
+ * the i-th slot below budget that was not kept takes the i-th kept slot from budget on.
+ * sink + recent <= budget.
+ */
+int oilbird_kv_evict(const oilbird_kv_cache* cache, int32_t budget, int32_t sink, int32_t recent,
+                     void* cuda_stream);
+/* Synchronises cuda_stream; *dropped (may be NULL) = rows that append() could not store since
+ * the workspace was zeroed.  OILBIRD_ESTALL if a bounded device-side wait gave up. */
+int oilbird_kv_status(const oilbird_kv_cache* cache, int64_t* dropped, void* cuda_stream);
+const char* oilbird_kv_last_error(void);
+
 const char* oilbird_strerror(int code);
 const char* oilbird_last_cuda_error(void);    /* text of the last failing CUDA call      */
 

@@ -79,6 +79,22 @@ class MergeParams(ctypes.Structure):
                 ("min_len", ctypes.c_int32), ("root_attached", ctypes.c_int32)]
 
 
+class CKVCache(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("pos", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("seq_len", ctypes.c_void_p),
+                ("n_pos", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t), ("n_pages", ctypes.c_int64),
+                ("n_seq", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("device", ctypes.c_int32)]
+
+
+class CKVRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("seq_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
 class PoolStats(ctypes.Structure):
     _fields_ = [("degenerate_rows", ctypes.c_int64), ("nonfinite_queries", ctypes.c_int64),
                 ("stalled", ctypes.c_int32), ("reserved", ctypes.c_int32)]
@@ -156,6 +172,18 @@ SYMBOLS = {
     "oilbird_index_rows": (_i64, [_vp]),
     "oilbird_index_read": (ctypes.c_int, [_vp, _vp, _vp, _vp]),
     "oilbird_index_last_error": (ctypes.c_char_p, []),
+    "oilbird_kv_block_bytes": (_i64, [_i32, _i32]),
+    "oilbird_kv_workspace_bytes": (ctypes.c_size_t, [_i32]),
+    "oilbird_kv_append": (ctypes.c_int, [ctypes.POINTER(CKVCache), _vp, _vp, _i32, _i32, _vp, _vp,
+                                         _vp, _vp]),
+    "oilbird_kv_read": (ctypes.c_int, [ctypes.POINTER(CKVCache), _i32, _vp, _vp, _vp, _vp]),
+    "oilbird_kv_attend": (ctypes.c_int, [ctypes.POINTER(CKVCache), _i32, _i32, _vp, _vp, _vp, _vp,
+                                         _i64, _vp, ctypes.c_float, _vp, _vp, _vp, _vp]),
+    "oilbird_kv_weigh": (ctypes.c_int, [ctypes.POINTER(CKVCache), _i32, _i32, _vp, _vp, _vp, _vp, _vp,
+                                        _i64, _vp, _vp, ctypes.c_float, _vp, _vp]),
+    "oilbird_kv_evict": (ctypes.c_int, [ctypes.POINTER(CKVCache), _i32, _i32, _i32, _vp]),
+    "oilbird_kv_status": (ctypes.c_int, [ctypes.POINTER(CKVCache), ctypes.POINTER(_i64), _vp]),
+    "oilbird_kv_last_error": (ctypes.c_char_p, []),
     "oilbird_query_static": (ctypes.c_int, [ctypes.POINTER(StaticPool), _vp, _i32,
                                             ctypes.POINTER(CQueryParams),
                                             ctypes.POINTER(CQueryOut), _vp]),
@@ -851,3 +879,201 @@ def merge_chains(tree_tok: torch.Tensor, tree_parent: torch.Tensor, n_nodes: tor
                                       walked.data_ptr(), ctypes.byref(mp), dev.index or 0,
                                       _stream_ptr(stream)), "oilbird_merge_chains")
     return MergeOut(tree_tok, tree_parent, n_nodes, depth, mask, status, bought, walked)
+
+
+# ------------------------------------------------- the verifier's 4-bit key/value cache ----
+KV_BF16, KV_F16 = 0, 1
+KV_MAX_SEQ, KV_MAX_GROUP, KV_MAX_EVICT_SLOTS = 1024, 64, 851968
+_KV_DTYPES = {torch.bfloat16: KV_BF16, torch.float16: KV_F16}
+
+
+def _kv_check(rc: int, where: str) -> None:
+    if rc != OK:
+        err = OilbirdError(rc, where)
+        err.args = (err.args[0] + ": " + lib().oilbird_kv_last_error().decode(),)
+        raise err
+
+
+class KVCache:
+    """Keys and values of n_seq requests (one layer) in 4 bits, in pages, with the attention
+    weight each slot has received (oilbird_kv_* of the C-ABI; see include/oilbird.h for the
+    format and the semantics of every call).
+
+    KVCache(...) allocates everything, max_len slots for each sequence.  KVCache.over(...) works
+    on tensors the caller holds: pages (uint8, the blocks of all pages), weight (fp32) and pos
+    (int32) [n_pages, n_kv_heads, page_size], page_table (int32 [n_seq, max_pages]), seq_len and
+    n_pos (int32 [n_seq]).  The workspace may be shared by caches that are used on one stream.
+    """
+
+    def __init__(self, n_seq: int, n_kv_heads: int, head_dim: int, max_len: int, *,
+                 page_size: int = 64, dtype=torch.bfloat16, device: int = 0):
+        if not torch.cuda.is_available():
+            raise RuntimeError("the key/value cache needs a CUDA device; there is no CPU fallback")
+        dev = torch.device(f"cuda:{device}")
+        block = lib().oilbird_kv_block_bytes(int(head_dim), int(page_size))
+        if block == 0:
+            raise ValueError("head_dim: 64 or 128; page_size: 16, 32 or 64")
+        per = max(1, -(-int(max_len) // page_size))
+        n_pages = n_seq * per
+        self._setup(torch.zeros(n_pages * n_kv_heads * block, dtype=torch.uint8, device=dev),
+                    torch.zeros(n_pages, n_kv_heads, page_size, device=dev),
+                    torch.zeros(n_pages, n_kv_heads, page_size, dtype=torch.int32, device=dev),
+                    torch.arange(n_pages, dtype=torch.int32, device=dev).view(n_seq, per),
+                    torch.zeros(n_seq, dtype=torch.int32, device=dev),
+                    torch.zeros(n_seq, dtype=torch.int32, device=dev), dtype, head_dim, None)
+
+    @classmethod
+    def over(cls, pages: torch.Tensor, weight: torch.Tensor, pos: torch.Tensor,
+             page_table: torch.Tensor, seq_len: torch.Tensor, n_pos: torch.Tensor, *,
+             dtype=torch.bfloat16, workspace: torch.Tensor | None = None) -> "KVCache":
+        self = cls.__new__(cls)
+        L = lib()
+        page_size = int(weight.shape[2])
+        cells = max(1, weight.shape[0] * weight.shape[1])
+        head_dim = [d for d in (64, 128) if L.oilbird_kv_block_bytes(d, page_size) * cells == pages.numel()]
+        if not head_dim:
+            raise ValueError("pages: n_pages * n_kv_heads blocks of oilbird_kv_block_bytes() bytes")
+        self._setup(pages, weight, pos, page_table, seq_len, n_pos, dtype, head_dim[0], workspace)
+        return self
+
+    def _setup(self, pages, weight, pos, page_table, seq_len, n_pos, dtype, head_dim, workspace):
+        self._L = lib()
+        dev = pages.device
+        if dtype not in _KV_DTYPES:
+            raise ValueError("dtype: torch.bfloat16 or torch.float16")
+        n_seq, max_pages = page_table.shape
+        for t, dt, shape in ((pages, torch.uint8, None), (weight, torch.float32, None),
+                             (pos, torch.int32, weight.shape), (page_table, torch.int32, None),
+                             (seq_len, torch.int32, (n_seq,)), (n_pos, torch.int32, (n_seq,))):
+            if not t.is_cuda or t.device != dev or t.dtype != dt or not t.is_contiguous() or \
+                    (shape is not None and tuple(t.shape) != tuple(shape)):
+                raise ValueError("the cache's tensors: contiguous, on one CUDA device, of the documented "
+                                 "types and shapes")
+        need = self._L.oilbird_kv_workspace_bytes(int(head_dim))
+        if workspace is None:
+            workspace = torch.zeros(need, dtype=torch.uint8, device=dev)
+        self.pages, self.weight, self.pos, self.page_table = pages, weight, pos, page_table
+        self.seq_len, self.n_pos, self.workspace = seq_len, n_pos, workspace
+        self.dtype, self.head_dim, self.n_kv_heads = dtype, int(head_dim), int(weight.shape[1])
+        self.n_seq, self.page_size = int(n_seq), int(weight.shape[2])
+        self._dev = dev
+        self._c = CKVCache(pages.data_ptr(), weight.data_ptr(), pos.data_ptr(),
+                           page_table.data_ptr(), seq_len.data_ptr(), n_pos.data_ptr(),
+                           workspace.data_ptr(), workspace.numel(), weight.shape[0], n_seq,
+                           max_pages, self.page_size, self.n_kv_heads, self.head_dim,
+                           _KV_DTYPES[dtype], dev.index or 0)
+        self._ref = ctypes.byref(self._c)
+
+    def _rows(self, t: torch.Tensor, heads: int, m: int | None = None):
+        """The C view of a [n_seq, m, heads, head_dim] tensor (any strides but the last)."""
+        shape, stride = t.shape, t.stride()
+        assert t.is_cuda and t.dtype == self.dtype and len(shape) == 4
+        assert shape[0] == self.n_seq and shape[2] == heads and shape[3] == self.head_dim
+        assert (m is None or shape[1] == m) and stride[3] == 1
+        return ctypes.byref(CKVRows(t.data_ptr(), stride[0], stride[1], stride[2]))
+
+    def _vec(self, t, dtype, *shape):
+        """Pointer of an optional contiguous tensor of that type and shape."""
+        if t is None:
+            return None
+        assert t.is_cuda and t.dtype == dtype and t.shape == shape and t.is_contiguous()
+        return t.data_ptr()
+
+    def _lse(self, t, m, heads):
+        """Pointer and strides of a [n_seq, m, heads] fp32 tensor."""
+        assert t.is_cuda and t.dtype == torch.float32 and t.shape == (self.n_seq, m, heads)
+        return t.data_ptr(), None if t.is_contiguous() else (ctypes.c_int64 * 3)(*t.stride())
+
+    def _mask(self, mask, m):
+        if mask is None:
+            return None, 0
+        assert mask.is_cuda and mask.dtype in (torch.int64, torch.uint64)
+        assert mask.shape[0] == self.n_seq and mask.shape[1] >= m and mask.stride(1) == 1
+        return mask.data_ptr(), mask.stride(0)
+
+    def append(self, k: torch.Tensor, v: torch.Tensor, n_new: torch.Tensor | None = None,
+               select: torch.Tensor | None = None, weight: torch.Tensor | None = None,
+               stream=None) -> None:
+        """Store rows of k and v [n_seq, m, n_kv_heads, head_dim]: rows select[s, :n_new[s]]
+        (int32 [n_seq, rows]; None: the first n_new[s], None: all).  weight: fp32
+        [n_seq, n_kv_heads, m], the rows' first weights (None: 0)."""
+        m = k.shape[1]
+        if m == 0:
+            return
+        rows = m if select is None else select.shape[1]
+        _kv_check(self._L.oilbird_kv_append(
+            self._ref, self._rows(k, self.n_kv_heads), self._rows(v, self.n_kv_heads, m), m, rows,
+            self._vec(n_new, torch.int32, self.n_seq),
+            self._vec(select, torch.int32, self.n_seq, rows),
+            self._vec(weight, torch.float32, self.n_seq, self.n_kv_heads, m),
+            _stream_ptr(stream)), "oilbird_kv_append")
+
+    def read(self, n: int, start: torch.Tensor | None = None, stream=None):
+        """Slots start[s] .. start[s] + n - 1 (int32 [n_seq]; None: from 0) in 16 bits: (k, v), each
+        [n_seq, n, n_kv_heads, head_dim]; zeros where a sequence has no slot."""
+        shape = (self.n_seq, n, self.n_kv_heads, self.head_dim)
+        k, v = ALLOC(shape, self.dtype, self._dev), ALLOC(shape, self.dtype, self._dev)
+        _kv_check(self._L.oilbird_kv_read(self._ref, n, self._vec(start, torch.int32, self.n_seq),
+                                          k.data_ptr(), v.data_ptr(), _stream_ptr(stream)),
+                  "oilbird_kv_read")
+        return k, v
+
+    def attend(self, q: torch.Tensor, k_new: torch.Tensor | None = None,
+               v_new: torch.Tensor | None = None, mask: torch.Tensor | None = None,
+               n_new: torch.Tensor | None = None, scale: float | None = None,
+               out: torch.Tensor | None = None, lse: torch.Tensor | None = None, stream=None):
+        """Attention of q [n_seq, m, n_q_heads, head_dim] over the cached slots and, with k_new and
+        v_new [n_seq, m, n_kv_heads, head_dim], over the nodes that mask (int64 [n_seq, >= m], bit j:
+        sees node j; None: nodes 0..i) names.  n_new: int32 [n_seq] nodes of each sequence (None: m).
+        Returns (out, lse): out like q, lse fp32 [n_seq, m, n_q_heads] (natural logarithm)."""
+        m, heads = q.shape[1], q.shape[2]
+        if out is None:
+            out = ALLOC((self.n_seq, m, heads, self.head_dim), self.dtype, self._dev)
+        if lse is None:
+            lse = ALLOC((self.n_seq, m, heads), torch.float32, self._dev)
+        mp, ms = self._mask(mask, m)
+        _kv_check(self._L.oilbird_kv_attend(
+            self._ref, heads, m, self._rows(q, heads),
+            None if k_new is None else self._rows(k_new, self.n_kv_heads, m),
+            None if v_new is None else self._rows(v_new, self.n_kv_heads, m), mp, ms,
+            self._vec(n_new, torch.int32, self.n_seq),
+            self.head_dim ** -0.5 if scale is None else scale, self._rows(out, heads, m),
+            *self._lse(lse, m, heads), _stream_ptr(stream)), "oilbird_kv_attend")
+        return out, lse
+
+    def weigh(self, q: torch.Tensor, lse: torch.Tensor, k_new: torch.Tensor | None = None,
+              mask: torch.Tensor | None = None, n_new: torch.Tensor | None = None,
+              row_weight: torch.Tensor | None = None, scale: float | None = None, stream=None):
+        """Add to every slot's weight what the nodes with row_weight (fp32 [n_seq, m]; None: 1) gave
+        it in attend (same arguments, and its lse).  Returns the same sums for the new nodes,
+        fp32 [n_seq, n_kv_heads, m] (None without k_new): append()'s weight."""
+        m, heads = q.shape[1], q.shape[2]
+        nodes = None
+        if k_new is not None:
+            nodes = ALLOC((self.n_seq, self.n_kv_heads, m), torch.float32, self._dev)
+        mp, ms = self._mask(mask, m)
+        _kv_check(self._L.oilbird_kv_weigh(
+            self._ref, heads, m, self._rows(q, heads),
+            *self._lse(lse, m, heads),
+            None if k_new is None else self._rows(k_new, self.n_kv_heads, m), mp, ms,
+            self._vec(n_new, torch.int32, self.n_seq),
+            self._vec(row_weight, torch.float32, self.n_seq, m),
+            self.head_dim ** -0.5 if scale is None else scale,
+            None if nodes is None else nodes.data_ptr(), _stream_ptr(stream)), "oilbird_kv_weigh")
+        return nodes
+
+    def evict(self, budget: int, sink: int = 4, recent: int | None = None, stream=None) -> None:
+        """Cut every sequence to `budget` slots per head: positions below sink and the newest
+        `recent` (None: half the budget, as far as sink leaves room) stay, then the slots of
+        greatest weight."""
+        if recent is None:
+            recent = max(0, min(budget // 2, budget - sink))
+        _kv_check(self._L.oilbird_kv_evict(self._ref, int(budget), int(sink), int(recent),
+                                           _stream_ptr(stream)), "oilbird_kv_evict")
+
+    def dropped(self, stream=None) -> int:
+        """Rows append() could not store so far (synchronises)."""
+        n = ctypes.c_int64()
+        _kv_check(self._L.oilbird_kv_status(self._ref, ctypes.byref(n), _stream_ptr(stream)),
+                  "oilbird_kv_status")
+        return int(n.value)

@@ -71,6 +71,10 @@ inline cudaError_t preload_kernel(K kernel, bool dynamic_smem = false) {
 cudaError_t preload_append_kernels();
 cudaError_t preload_evict_kernels();
 cudaError_t preload_index_kernels();
+cudaError_t preload_kv_attend_kernels();
+cudaError_t preload_kv_evict_kernels();
+cudaError_t preload_kv_store_kernels();
+cudaError_t preload_kv_weigh_kernels();
 cudaError_t preload_merge_kernels();
 cudaError_t preload_merge_tree_kernels();
 cudaError_t preload_quant8_kernels();

@@ -50,6 +50,10 @@ cudaError_t preload_all_kernels() {
   if ((e = preload_append_kernels()) != cudaSuccess) return e;
   if ((e = preload_evict_kernels()) != cudaSuccess) return e;
   if ((e = preload_index_kernels()) != cudaSuccess) return e;
+  if ((e = preload_kv_attend_kernels()) != cudaSuccess) return e;
+  if ((e = preload_kv_evict_kernels()) != cudaSuccess) return e;
+  if ((e = preload_kv_store_kernels()) != cudaSuccess) return e;
+  if ((e = preload_kv_weigh_kernels()) != cudaSuccess) return e;
   if ((e = preload_merge_kernels()) != cudaSuccess) return e;
   if ((e = preload_merge_tree_kernels()) != cudaSuccess) return e;
   if ((e = preload_quant8_kernels()) != cudaSuccess) return e;
