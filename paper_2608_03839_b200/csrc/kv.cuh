@@ -211,17 +211,22 @@ __device__ __forceinline__ long long block_exclusive_scan(long long v, long long
 }
 
 // ---- tiles ----
-// The slots of all (sequence, key head, row block) items, 32 to a tile, are one list: sequence
-// by sequence, its items in turn, its tiles in turn (cached slots first, new nodes behind
-// them).  Items whose rows do not exist have one empty tile.
-constexpr int kKvTile = 32;
+// The slots of all (sequence, key head, row block) items, 64 to a tile, are one list: sequence
+// by sequence, its items in turn, its tiles in turn.  An item begins with a round of kKvFront
+// tiles, one for each warp of a block: the new nodes (32 each) in the first of them, nothing in
+// the others.  Nodes come first because their loads depend on nothing, and the round stands for
+// what an item costs besides its slots (operands, joining), so that a block that gets many
+// short items gets fewer slots.  Items whose rows do not exist have one empty tile.
+constexpr int kKvTile = 64, kKvNodeTile = 32, kKvFront = 8;
 
 struct TileCursor {
   int s;                // sequence
   int len, nodes;       // its slots and new nodes
   int tiles;            // tiles of each of its items that have rows ...
   int live;             // ... and how many items those are
-  int item, tile;
+  int item, head, tile; // head: item modulo the key heads
+  __device__ __forceinline__ int slot0() const { return (tile - kKvFront) * kKvTile; }
+  __device__ __forceinline__ bool cached() const { return item < live && tile >= kKvFront; }
 };
 
 struct TileList {
@@ -231,18 +236,14 @@ struct TileList {
   long long total;
   int n_seq, n_kv, items;      // items of every sequence
   int group, rows;             // query heads per key head, rows per block (0: all items live)
-  int node_tiles;              // per item; -1: as many as the sequence's nodes need
 
   __device__ __forceinline__ int live_items(int n) const {
     return rows == 0 ? items : n_kv * ((n * group + rows - 1) / rows);
   }
-  __device__ __forceinline__ int tiles_of(int l, int n) const {
-    const int t = (l + kKvTile - 1) / kKvTile + (node_tiles < 0 ? (n + kKvTile - 1) / kKvTile : node_tiles);
-    return t > 0 ? t : 1;
-  }
+  __device__ __forceinline__ int tiles_of(int l) const { return (l + kKvTile - 1) / kKvTile + kKvFront; }
   __device__ __forceinline__ long long tiles_in(int l, int n) const {
     const int live = live_items(n);
-    return (long long)live * tiles_of(l, n) + (items - live);
+    return (long long)live * tiles_of(l) + (items - live);
   }
   // Every thread calls; scratch: a word per warp.
   template <int kThreads>
@@ -277,7 +278,7 @@ struct TileList {
     k.s = s;
     k.len = len[s];
     k.nodes = nodes[s];
-    k.tiles = tiles_of(k.len, k.nodes);
+    k.tiles = tiles_of(k.len);
     k.live = live_items(k.nodes);
   }
   __device__ __forceinline__ void seek(TileCursor& k, long long u) const {   // to list position u
@@ -290,71 +291,96 @@ struct TileList {
     const long long r = u - cum[lo], full = (long long)k.live * k.tiles;
     if (r < full) { k.item = (int)(r / k.tiles); k.tile = (int)(r - (long long)k.item * k.tiles); }
     else { k.item = k.live + (int)(r - full); k.tile = 0; }
+    k.head = k.item % n_kv;
   }
   __device__ __forceinline__ void advance(TileCursor& k, int n) const {      // n tiles on, inside the list
     for (k.tile += n;;) {
       const int here = k.item < k.live ? k.tiles : 1;
       if (k.tile < here) return;
       k.tile -= here;
-      if (++k.item == items) { load(k, k.s + 1); k.item = 0; }
+      if (++k.head == n_kv) k.head = 0;
+      if (++k.item == items) { load(k, k.s + 1); k.item = k.head = 0; }
     }
   }
 };
 
-// The two pages that hold a tile's halves (one page if it holds 32 slots or more); -1 where
-// the table names none or the half has no slot.  Lane 0 gets the first, lane 1 the second.
+// The pages that hold a tile's quarters of 16 slots, lane q the q-th's; -1 where the table names
+// none or the quarter has no slot.
 __device__ __forceinline__ int tile_pages(const KvView& c, const TileCursor& k, int lane) {
-  const int slot = k.tile * kKvTile + lane * 16;
   int p = -1;
-  if (k.item < k.live && lane < 2 && slot < k.len) {
-    p = c.table[(size_t)k.s * c.max_pages + (slot >> c.page_shift)];
-    p = (p >= 0 && p < c.n_pages) ? p : -1;
+  if (k.cached() && lane < 4) {
+    const int slot = k.slot0() + lane * 16;
+    if (slot < k.len) {
+      p = c.table[(size_t)k.s * c.max_pages + (slot >> c.page_shift)];
+      p = (uint32_t)p < (uint32_t)c.n_pages ? p : -1;
+    }
   }
   return p;
 }
 // Starts the copies of a tile (a whole warp): codes [group][slot][32 B] and meta [slot][group]
-// of the keys and, with kValues, of the values behind them.  Halves without a page are zeroed.
+// of the keys and, with kValues, of the values behind them.  Quarters without a page are zeroed.
 template <int D, bool kValues>
-__device__ __forceinline__ void copy_tile(const KvView& c, int head, int slot0, int p0, int p1,
+__device__ __forceinline__ void copy_tile(const KvView& c, const TileCursor& k, int pages,
                                           unsigned char* dst_ptr, int lane) {
-  constexpr int G = D / kKvGroup;
+  constexpr int G = D / kKvGroup, kParts = kValues ? 2 : 1;
+  constexpr int kTilePart = G * kKvTile * 36;
+  const uint32_t dst = kv_smem(dst_ptr) + lane * 16;
   const int page = 1 << c.page_shift;
   const size_t block = 2 * (size_t)kv_part_bytes(D, page);
-  const unsigned char* base0 = c.pages + ((size_t)(p0 < 0 ? 0 : p0) * c.n_kv + head) * block;
-  const unsigned char* base1 = c.pages + ((size_t)(p1 < 0 ? 0 : p1) * c.n_kv + head) * block;
-  const uint32_t n0 = p0 < 0 ? 0 : 16, n1 = p1 < 0 ? 0 : 16;
-  const int in0 = slot0 & (page - 1), in1 = (slot0 + 16) & (page - 1);
-  const uint32_t dst = kv_smem(dst_ptr);
-  const int part = G * page * 36, tile_part = G * kKvTile * 36;
+  if (c.page_shift == 6) {                               // the tile is a page
+    const int p = __shfl_sync(0xffffffffu, pages, 0);
+    const uint32_t n = p < 0 ? 0 : 16;
+    const unsigned char* b = c.pages + ((size_t)(uint32_t)max(p, 0) * c.n_kv + k.head) * block + lane * 16;
+    constexpr int kChunks = kTilePart / 16;              // and lies in memory as it will here
 #pragma unroll
-  for (int kv = 0; kv < (kValues ? 2 : 1); ++kv) {
+    for (int i = 0; i < kParts * kChunks; i += 32)
+      if (i + 32 <= kParts * kChunks || i + lane < kParts * kChunks) cp_async16(dst + i * 16, b + i * 16, n);
+    return;
+  }
+  const int part = G * page * 36;
 #pragma unroll
-    for (int i = 0; i < 2 * G; ++i) {                    // 16 slots of a group: 32 chunks
-      const unsigned char* b = (i & 1 ? base1 : base0) + kv * part +
-                               ((i >> 1) * page + (i & 1 ? in1 : in0)) * 32 + lane * 16;
-      cp_async16(dst + kv * tile_part + i * 512 + lane * 16, b, i & 1 ? n1 : n0);
-    }
-    if (lane < 8 * G) {
-      const bool second = lane >= 4 * G;
-      const unsigned char* b = (second ? base1 : base0) + kv * part + G * page * 32 +
-                               (second ? in1 : in0) * 4 * G + (second ? lane - 4 * G : lane) * 16;
-      cp_async16(dst + kv * tile_part + G * kKvTile * 32 + lane * 16, b, second ? n1 : n0);
+  for (int q = 0; q < 4; ++q) {
+    const int p = __shfl_sync(0xffffffffu, pages, q), in = (k.slot0() + q * 16) & (page - 1);
+    const unsigned char* b = c.pages + ((size_t)(uint32_t)max(p, 0) * c.n_kv + k.head) * block;
+    const uint32_t n = p < 0 ? 0 : 16;
+#pragma unroll
+    for (int kv = 0; kv < kParts; ++kv) {
+#pragma unroll
+      for (int i = 0; i < G; ++i)
+        cp_async16(dst + kv * kTilePart + i * 2048 + q * 512, b + kv * part + (i * page + in) * 32 + lane * 16, n);
+      if (lane < 4 * G)
+        cp_async16(dst + kv * kTilePart + G * 2048 + q * 64 * G, b + kv * part + (G * page * 8 + in * G) * 4 + lane * 16, n);
     }
   }
 }
 // bit i: slot i of the tile exists and has a page
-__device__ __forceinline__ uint32_t tile_valid(int left, int p0, int p1) {
-  uint32_t v = left >= 32 ? 0xffffffffu : (1u << left) - 1u;
-  if (p0 < 0) v &= 0xffff0000u;
-  if (p1 < 0) v &= 0x0000ffffu;
+__device__ __forceinline__ unsigned long long tile_valid(const TileCursor& k, int pages) {
+  const int left = k.len - k.slot0();
+  unsigned long long v = left >= 64 ? ~0ull : (1ull << left) - 1ull;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (__shfl_sync(0xffffffffu, pages, q) < 0) v &= ~(0xffffull << (16 * q));
   return v;
+}
+// Zeroes the meta of a tile's slots that are not valid, so that whatever lay there is finite.
+template <int G>
+__device__ __forceinline__ void clear_meta(unsigned char* meta, unsigned long long valid, int lane) {
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int sl = lane + 32 * e;
+    if (!(valid >> sl & 1ull)) {
+#pragma unroll
+      for (int i = 0; i < G; ++i) reinterpret_cast<uint32_t*>(meta)[sl * G + i] = 0u;
+    }
+  }
 }
 
 // One query row as matrix operands: what lane (row g, t4) of a warp holds of it.  b[step] are
 // the pairs of a product step; sum[group] the row's sums (all lanes of the row); returns the
-// row's factor exponent.  have == false: zeros.
+// row's factor exponent.  have == false: zeros.  negate: for a negative scale, so that factors
+// are positive and the largest product is the largest score.
 template <int D, bool kBf16>
-__device__ __forceinline__ int row_operands(const uint16_t* qp, bool have, int t4,
+__device__ __forceinline__ int row_operands(const uint16_t* qp, bool have, int t4, bool negate,
                                             uint32_t (&b)[D / 16][2], float (&sum)[D / kKvGroup]) {
   constexpr int G = D / kKvGroup;
   float x[G][16], top = 0.f;
@@ -378,7 +404,7 @@ __device__ __forceinline__ int row_operands(const uint16_t* qp, bool have, int t
   top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
   top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
   const int e0 = row_exponent(top);
-  const float up = pow2(kRowTop - e0);
+  const float up = negate ? -pow2(kRowTop - e0) : pow2(kRowTop - e0);
 #pragma unroll
   for (int i = 0; i < G; ++i) {
     sum[i] = 0.f;
@@ -396,7 +422,17 @@ __device__ __forceinline__ int row_operands(const uint16_t* qp, bool have, int t
 }
 // What a score in the products' units is multiplied by to become an exponent of two.
 __device__ __forceinline__ float row_factor(float scale, int e0) {
-  return scale * kLog2e * (0x1p24f / (float)(1 << kRowTop)) * pow2(e0);
+  return fmaxf(fabsf(scale) * kLog2e * (0x1p24f / (float)(1 << kRowTop)) * pow2(e0), 1e-37f);
+}
+// The scales and offsets of one slot.
+template <int G> __device__ __forceinline__ void load_meta(const unsigned char* p, uint32_t (&m)[G]) {
+  if (G == 2) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    m[0] = v.x;
+    m[G - 1] = v.y;
+  } else {
+    m[0] = *reinterpret_cast<const uint32_t*>(p);
+  }
 }
 
 }  // namespace oilbird

@@ -17,7 +17,7 @@
 // 2t+1 is slot t+4: then both the K loads (8 bytes a lane) and the V loads (4 bytes a lane)
 // take 256 and 128 contiguous bytes of shared memory.
 //
-// Work.  The tiles (32 slots) of all (sequence, head, row block) items are one list, cut into
+// Work.  The tiles (64 slots) of all (sequence, head, row block) items are one list, cut into
 // equal runs, one per block; a block's eight warps take the run's tiles in turn, each
 // through a ring of its own (asynchronous 16-byte copies, no block-wide waits), which runs on
 // across items.  At the end of an item's share the warps' results are joined in
@@ -27,30 +27,44 @@
 
 namespace oilbird {
 
-constexpr int kAtThreads = 256, kAtWarps = 8, kAtTile = kKvTile, kAtStages = 4;
-
+// Rows per block are 8 NT.  The ring holds 147 KB at D = 128, about three times what an SM must
+// have in flight for its share of the memory rate.
+constexpr int kAtWarps = 8, kAtThreads = 256, kAtStages = 2;
 template <int D>
-struct AttendShared {
-  static constexpr int kStage = kAtTile * (D / kKvGroup) * 72;       // K codes, K meta, V codes, V meta
+struct Attend {
+  static constexpr int kStage = kKvTile * (D / kKvGroup) * 72;       // K codes, K meta, V codes, V meta
   static constexpr int kRing = kAtWarps * kAtStages * kStage;
-  static constexpr int kObuf = kAtWarps * 8 * (D + 4) * 4;
-  static constexpr int kMl = kAtWarps * 8 * 8;
-  static constexpr int kValid = kAtWarps * kAtStages * 4;
+  static constexpr int kObuf = kAtWarps * 8 * (D + 4) * 4;           // twice
+  static constexpr int kMl = kAtWarps * 8 * 8;                       // twice
+  static constexpr int kValid = kAtWarps * kAtStages * 8;
   static constexpr int kCum = (kKvMaxSeq + 1) * 8;
-  static constexpr int kBytes = kRing + kObuf + kMl + kValid + kCum + kKvMaxSeq * 5 + kAtWarps * 8 + 16;
+  static constexpr int kBytes = kRing + 2 * (kObuf + kMl) + kValid + kCum + kAtWarps * 8 + kKvMaxSeq * 5 + 16;
 };
+
+template <int N> __device__ __forceinline__ void load_floats(const float* p, float (&v)[N]) {
+  if (N == 4) { const float4 x = *reinterpret_cast<const float4*>(p); v[0] = x.x; v[1] = x.y; v[N - 2] = x.z; v[N - 1] = x.w; }
+  else { const float2 x = *reinterpret_cast<const float2*>(p); v[0] = x.x; v[1] = x.y; }
+}
+template <int N> __device__ __forceinline__ void load_floats_cg(const float* p, float (&v)[N]) {
+  if (N == 4) { const float4 x = __ldcg(reinterpret_cast<const float4*>(p)); v[0] = x.x; v[1] = x.y; v[N - 2] = x.z; v[N - 1] = x.w; }
+  else { const float2 x = __ldcg(reinterpret_cast<const float2*>(p)); v[0] = x.x; v[1] = x.y; }
+}
+template <int N> __device__ __forceinline__ void store_floats(float* p, const float (&v)[N]) {
+  if (N == 4) __stcg(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[N - 2], v[N - 1]));
+  else __stcg(reinterpret_cast<float2*>(p), make_float2(v[0], v[1]));
+}
 
 template <int D, int NT, bool kBf16>
 __global__ void __launch_bounds__(kAtThreads, 1)
 kv_attend_kernel(const KvView c, const KvAttendArgs a) {
-  using Sh = AttendShared<D>;
+  using Sh = Attend<D>;
   constexpr int G = D / kKvGroup, kRows = NT * 8, kSteps = D / 16;
   extern __shared__ __align__(16) unsigned char smem[];
   unsigned char* ring = smem;
   float* obuf = reinterpret_cast<float*>(smem + Sh::kRing);
-  float2* ml = reinterpret_cast<float2*>(smem + Sh::kRing + Sh::kObuf);
-  uint32_t* valid_s = reinterpret_cast<uint32_t*>(smem + Sh::kRing + Sh::kObuf + Sh::kMl);
-  long long* cum = reinterpret_cast<long long*>(smem + Sh::kRing + Sh::kObuf + Sh::kMl + Sh::kValid);
+  float2* ml = reinterpret_cast<float2*>(smem + Sh::kRing + 2 * Sh::kObuf);
+  unsigned long long* valid_s = reinterpret_cast<unsigned long long*>(smem + Sh::kRing + 2 * (Sh::kObuf + Sh::kMl));
+  long long* cum = reinterpret_cast<long long*>(valid_s + kAtWarps * kAtStages);
   long long* scratch = cum + kKvMaxSeq + 1;
   int* len_s = reinterpret_cast<int*>(scratch + kAtWarps);
   unsigned char* nodes_s = reinterpret_cast<unsigned char*>(len_s + kKvMaxSeq);
@@ -67,7 +81,6 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
   list.items = c.n_kv * rblocks;
   list.group = a.group;
   list.rows = kRows;
-  list.node_tiles = a.k.p ? -1 : 0;
   list.build<kAtThreads>(c, a.n_new, a.m, scratch);
   const long long total = list.total;
   // blocks share the list evenly; no block gets less than a tile for each of its warps
@@ -79,18 +92,17 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
 
   // ---- the warp's ring of tiles ----
   unsigned char* my_ring = ring + warp * (kAtStages * Sh::kStage);
-  uint32_t* my_valid = valid_s + warp * kAtStages;
+  unsigned long long* my_valid = valid_s + warp * kAtStages;
   TileCursor pc;
   long long pu = u0 + warp;                              // the next tile to copy, its pages
   int ahead = -1;
   if (pu < u1) { list.seek(pc, pu); ahead = tile_pages(c, pc, lane); }
   auto issue = [&](int stage) {
     if (pu < u1) {
-      const int slot0 = pc.tile * kAtTile;
-      if (pc.item < pc.live && slot0 < pc.len) {
-        const int p0 = __shfl_sync(0xffffffffu, ahead, 0), p1 = __shfl_sync(0xffffffffu, ahead, 1);
-        copy_tile<D, true>(c, pc.item % c.n_kv, slot0, p0, p1, my_ring + stage * Sh::kStage, lane);
-        if (lane == 0) my_valid[stage] = tile_valid(pc.len - slot0, p0, p1);
+      if (pc.cached()) {
+        copy_tile<D, true>(c, pc, ahead, my_ring + stage * Sh::kStage, lane);
+        const unsigned long long v = tile_valid(pc, ahead);
+        if (lane == 0) my_valid[stage] = v;
       }
       pu += kAtWarps;
       if (pu < u1) { list.advance(pc, kAtWarps); ahead = tile_pages(c, pc, lane); }
@@ -98,8 +110,8 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
     cp_async_commit();
   };
 #pragma unroll
-  for (int i = 0; i < kAtStages - 1; ++i) issue(i);
-  int stage = 0;
+  for (int i = 0; i < kAtStages; ++i) issue(i);
+  int stage = 0, buf = 0;
 
   // ---- item by item ----
   TileCursor bc;
@@ -111,14 +123,14 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
     const int piece = (int)min((long long)(n_tiles - tile0), u1 - at);
     const long long item_u0 = at - tile0;
     // live items: head fastest, then row block; the others follow in the same order
-    const int head = item % c.n_kv;
-    const int rb = item / c.n_kv, row0 = rb * kRows;
+    const int head = bc.head, row0 = item / c.n_kv * kRows;
     const int n_rows = bc.nodes * a.group;               // rows of the sequence that exist
     const int s = bc.s;
 
     float o[NT][4 * G][4];                               // channel tiles x rows, in units of 2^(eref + 24)
     float olo[NT][G][2], l[NT][2], m[NT][2];
     int eref = -120;
+    bool fresh = true, had = false;                      // eref is free to fall; the warp took a tile
 #pragma unroll
     for (int r = 0; r < NT; ++r) {
 #pragma unroll
@@ -134,350 +146,346 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
       }
     }
 
-    if (mu < at + piece && item < bc.live) {
-      // ---- query rows as operands ----
-      uint32_t qf[NT][kSteps][2];
-      float f[NT][2], qsum[NT][G][2];
+    if (item < bc.live && mu < at + piece && mu < item_u0 + kKvFront) {
+      // ---- the item's first round: new nodes, 16-bit keys and values, with the tree's mask ----
+      const int node0 = (int)(mu - item_u0) * kKvNodeTile;
+      if (a.k.p && node0 < bc.nodes) {
+        had = true;
+        float sc[NT][2][4];
 #pragma unroll
-      for (int r = 0; r < NT; ++r) {
-        const int row = row0 + r * 8 + g;
-        const bool have = row < n_rows;
-        const int node = have ? row / a.group : 0;
-        float sum[G];
-        const int e0 = row_operands<D, kBf16>(a.q.at(s, node, head * a.group + (have ? row % a.group : 0)), have, t4,
-                                              qf[r], sum);
+        for (int r = 0; r < NT; ++r)
 #pragma unroll
-        for (int i = 0; i < G; ++i) {                    // accumulators hold rows 2t and 2t+1
-          qsum[r][i][0] = __shfl_sync(0xffffffffu, sum[i], 8 * t4) * 0x1p-24f;
-          qsum[r][i][1] = __shfl_sync(0xffffffffu, sum[i], 8 * t4 + 4) * 0x1p-24f;
+          for (int ch = 0; ch < 2; ++ch)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc[r][ch][e] = 0.f;
+        const bool both = node0 + 16 < bc.nodes;         // the second sixteen exist
+        uint4 qw[NT][G][2];
+#pragma unroll
+        for (int r = 0; r < NT; ++r) {
+          const int row = row0 + r * 8 + g;
+          const int node = row < n_rows ? row / a.group : 0, sub = row < n_rows ? row % a.group : 0;
+          const uint16_t* qp = a.q.at(s, node, head * a.group + sub) + t4 * 16;
+#pragma unroll
+          for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              qw[r][i][half] = make_uint4(0, 0, 0, 0);
+              if (row < n_rows) qw[r][i][half] = *reinterpret_cast<const uint4*>(qp + i * kKvGroup + half * 8);
+            }
         }
-        const float ff = row_factor(a.scale, e0);
-        f[r][0] = __shfl_sync(0xffffffffu, ff, 8 * t4);
-        f[r][1] = __shfl_sync(0xffffffffu, ff, 8 * t4 + 4);
-      }
-
-      for (; mu < at + piece; mu += kAtWarps) {
-        const int tile = (int)(mu - item_u0);
-        cp_async_wait<kAtStages - 2>();
-        __syncwarp();
-        const unsigned char* st = my_ring + stage * Sh::kStage;
-        const int slot0 = tile * kAtTile;
-        if (slot0 < bc.len) {
-          const uint32_t valid = my_valid[stage];
-          const uint32_t* kmeta = reinterpret_cast<const uint32_t*>(st + G * kAtTile * 32);
-          const unsigned char* vst = st + G * kAtTile * 36;
-          const uint32_t* vmeta = reinterpret_cast<const uint32_t*>(vst + G * kAtTile * 32);
-          float sc[NT][2][4];
-          const int slot_g = (g >> 1) + 4 * (g & 1);     // logical row g of a chunk
-          // ---- scores ----
 #pragma unroll
-          for (int ch = 0; ch < 2; ++ch) {
-            const int sl = ch * 16 + slot_g;
-            const bool ok0 = valid >> sl & 1, ok1 = valid >> (sl + 8) & 1;
+        for (int ch = 0; ch < 2; ++ch) {
+          if (ch && !both) break;
+          uint4 kw[2][G][2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int node = node0 + ch * 16 + g + 8 * k;
+            const uint16_t* kp = a.k.at(s, node < bc.nodes ? node : 0, head) + t4 * 16;
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+#pragma unroll
+              for (int half = 0; half < 2; ++half) {
+                kw[k][i][half] = make_uint4(0, 0, 0, 0);
+                if (node < bc.nodes) kw[k][i][half] = *reinterpret_cast<const uint4*>(kp + i * kKvGroup + half * 8);
+              }
+          }
+#pragma unroll
+          for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+              for (int r = 0; r < NT; ++r) {
+                const uint4 &x = kw[0][i][half], &y = kw[1][i][half], &z = qw[r][i][half];
+                mma16816<kBf16>(sc[r][ch], x.x, y.x, x.y, y.y, z.x, z.y);
+                mma16816<kBf16>(sc[r][ch], x.z, y.z, x.w, y.w, z.z, z.w);
+              }
+        }
+        const float fs = a.scale * kLog2e;
+#pragma unroll
+        for (int r = 0; r < NT; ++r)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int row = row0 + r * 8 + 2 * t4 + e;
+            unsigned long long sees = 0;
+            if (row < n_rows) {
+              const int node = row / a.group;
+              sees = a.mask ? a.mask[s * a.mask_stride + node] : (2ull << node) - 1ull;
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int ch = 0; ch < 2; ++ch)
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const int node = node0 + ch * 16 + g + 8 * k;
+                const bool ok = node < bc.nodes && (sees >> node & 1ull);
+                float& x = sc[r][ch][e + 2 * k];
+                x = ok ? x * fs : -INFINITY;
+                mx = fmaxf(mx, x);
+              }
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+            m[r][e] = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+          }
+        // these products need no units: eref = 0 after them, where no finite value overflows;
+        // the first cached tile chooses anew
+        eref = 0;
+#pragma unroll
+        for (int ch = 0; ch < 2; ++ch) {
+          if (ch && !both) break;
+          // p as the sum of two 16-bit numbers: with bf16 one alone would be as coarse as the
+          // result's own rounding
+          uint32_t hi[NT][2], lo[NT][2];
+#pragma unroll
+          for (int r = 0; r < NT; ++r)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              float p[2];
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                p[e] = exp2_approx(sc[r][ch][e + 2 * k] - (m[r][e] == -INFINITY ? 0.f : m[r][e]));
+                l[r][e] += p[e];
+              }
+              const uint32_t h = pack16<kBf16>(p[0], p[1]);
+              hi[r][k] = transpose8x8(h);
+              lo[r][k] = transpose8x8(pack16<kBf16>(p[0] - half_lo<kBf16>(h), p[1] - half_hi<kBf16>(h)));
+            }
+          uint4 w[G][4];                                 // nodes 2t, 2t+1, 2t+8, 2t+9; 8 channels
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int node = node0 + ch * 16 + 2 * t4 + (k & 1) + 8 * (k >> 1);
+            const uint16_t* vp = a.v.at(s, node < bc.nodes ? node : 0, head) + g * 8;
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+              w[i][k] = make_uint4(0, 0, 0, 0);
+              if (node < bc.nodes) w[i][k] = *reinterpret_cast<const uint4*>(vp + i * kKvGroup);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+              const uint32_t x0 = (&w[i][0].x)[n], x1 = (&w[i][1].x)[n], x2 = (&w[i][2].x)[n], x3 = (&w[i][3].x)[n];
+              const uint32_t ea = __byte_perm(x0, x1, 0x5410), oa = __byte_perm(x0, x1, 0x7632);
+              const uint32_t eb = __byte_perm(x2, x3, 0x5410), ob = __byte_perm(x2, x3, 0x7632);
+#pragma unroll
+              for (int r = 0; r < NT; ++r) {
+                mma16816<kBf16>(o[r][i * 4 + n], ea, oa, eb, ob, hi[r][0], hi[r][1]);
+                mma16816<kBf16>(o[r][i * 4 + n], ea, oa, eb, ob, lo[r][0], lo[r][1]);
+              }
+            }
+        }
+        // (the cached codes of odd pairs carry 16 times their value)
+#pragma unroll
+        for (int r = 0; r < NT; ++r)
+#pragma unroll
+          for (int i = 0; i < 4 * G; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[r][i][e] *= i & 1 ? 0x1p-20f : 0x1p-24f;
+      }
+    }
+
+    // ---- cached tiles ----
+    uint32_t qf[NT][kSteps][2];
+    float f[NT][2], qsum[NT][G][2];
+    bool loaded = false;
+    for (; mu < at + piece; mu += kAtWarps) {
+      const int tile = (int)(mu - item_u0);
+      if (item < bc.live && tile >= kKvFront) {
+        if (!loaded) {                                   // query rows as operands
+          loaded = had = true;
+#pragma unroll
+          for (int r = 0; r < NT; ++r) {
+            const int row = row0 + r * 8 + g;
+            const bool have = row < n_rows;
+            const int node = have ? row / a.group : 0;
+            float sum[G];
+            const int e0 = row_operands<D, kBf16>(a.q.at(s, node, head * a.group + (have ? row % a.group : 0)), have, t4,
+                                                  a.scale < 0.f, qf[r], sum);
+#pragma unroll
+            for (int i = 0; i < G; ++i) {                // accumulators hold rows 2t and 2t+1
+              qsum[r][i][0] = __shfl_sync(0xffffffffu, sum[i], 8 * t4) * 0x1p-24f;
+              qsum[r][i][1] = __shfl_sync(0xffffffffu, sum[i], 8 * t4 + 4) * 0x1p-24f;
+            }
+            const float ff = row_factor(a.scale, e0);
+            f[r][0] = __shfl_sync(0xffffffffu, ff, 8 * t4);
+            f[r][1] = __shfl_sync(0xffffffffu, ff, 8 * t4 + 4);
+          }
+        }
+        cp_async_wait<kAtStages - 1>();
+        __syncwarp();
+        unsigned char* st = my_ring + stage * Sh::kStage;
+        unsigned char* kmeta = st + G * kKvTile * 32;
+        const unsigned char* vst = st + G * kKvTile * 36;
+        unsigned char* vmeta = st + G * kKvTile * 68;
+        const unsigned long long valid = my_valid[stage];
+        const bool partial = valid != ~0ull;             // the sequence's end, or a page that is none
+        if (partial) {
+          clear_meta<G>(kmeta, valid, lane);
+          clear_meta<G>(vmeta, valid, lane);
+          __syncwarp();
+        }
+        const int slot_g = (g >> 1) + 4 * (g & 1);       // logical row g of a chunk
+        // ---- scores ----
+        float sc[NT][4][4];
+#pragma unroll
+        for (int ch = 0; ch < 4; ++ch) {
+          const int sl = ch * 16 + slot_g;
+          uint32_t km[2][G];
+          load_meta<G>(kmeta + sl * 4 * G, km[0]);
+          load_meta<G>(kmeta + (sl + 8) * 4 * G, km[1]);
+#pragma unroll
+          for (int i = 0; i < G; ++i) {
+            const uint2 w0 = *reinterpret_cast<const uint2*>(st + (i * kKvTile + sl) * 32 + t4 * 8);
+            const uint2 w1 = *reinterpret_cast<const uint2*>(st + (i * kKvTile + sl + 8) * 32 + t4 * 8);
+            float acc[NT][4];
 #pragma unroll
             for (int r = 0; r < NT; ++r)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) sc[r][ch][e] = 0.f;
+              for (int e = 0; e < 4; ++e) acc[r][e] = 0.f;
 #pragma unroll
-            for (int i = 0; i < G; ++i) {
-              const uint2 w0 = *reinterpret_cast<const uint2*>(st + (i * kAtTile + sl) * 32 + t4 * 8);
-              const uint2 w1 = *reinterpret_cast<const uint2*>(st + (i * kAtTile + sl + 8) * 32 + t4 * 8);
-              uint32_t meta0 = kmeta[sl * G + i], meta1 = kmeta[(sl + 8) * G + i];
-              meta0 = ok0 ? meta0 : 0u;
-              meta1 = ok1 ? meta1 : 0u;
-              float acc[NT][4];
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t x0 = (j & 2 ? w0.y : w0.x) >> (8 * (j & 1));
+              const uint32_t x1 = (j & 2 ? w1.y : w1.x) >> (8 * (j & 1));
 #pragma unroll
               for (int r = 0; r < NT; ++r)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[r][e] = 0.f;
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const uint32_t x0 = (j & 2 ? w0.y : w0.x) >> (8 * (j & 1));
-                const uint32_t x1 = (j & 2 ? w1.y : w1.x) >> (8 * (j & 1));
-#pragma unroll
-                for (int r = 0; r < NT; ++r)
-                  mma16816<false>(acc[r], x0 & 0x000f000fu, x1 & 0x000f000fu, x0 & 0x00f000f0u,
-                                  x1 & 0x00f000f0u, qf[r][i * 4 + j][0], qf[r][i * 4 + j][1]);
-              }
-              const float s0 = half_lo<kBf16>(meta0), l0 = half_hi<kBf16>(meta0);
-              const float s1 = half_lo<kBf16>(meta1), l1 = half_hi<kBf16>(meta1);
-#pragma unroll
-              for (int r = 0; r < NT; ++r) {
-                sc[r][ch][0] = fmaf(s0, acc[r][0], fmaf(l0, qsum[r][i][0], sc[r][ch][0]));
-                sc[r][ch][1] = fmaf(s0, acc[r][1], fmaf(l0, qsum[r][i][1], sc[r][ch][1]));
-                sc[r][ch][2] = fmaf(s1, acc[r][2], fmaf(l1, qsum[r][i][0], sc[r][ch][2]));
-                sc[r][ch][3] = fmaf(s1, acc[r][3], fmaf(l1, qsum[r][i][1], sc[r][ch][3]));
-              }
+                mma16816<false>(acc[r], x0 & 0x000f000fu, x1 & 0x000f000fu, x0 & 0x00f000f0u,
+                                x1 & 0x00f000f0u, qf[r][i * 4 + j][0], qf[r][i * 4 + j][1]);
             }
+            const float s0 = half_lo<kBf16>(km[0][i]), l0 = half_hi<kBf16>(km[0][i]);
+            const float s1 = half_lo<kBf16>(km[1][i]), l1 = half_hi<kBf16>(km[1][i]);
 #pragma unroll
             for (int r = 0; r < NT; ++r) {
-              sc[r][ch][0] = ok0 ? sc[r][ch][0] * f[r][0] : -INFINITY;
-              sc[r][ch][1] = ok0 ? sc[r][ch][1] * f[r][1] : -INFINITY;
-              sc[r][ch][2] = ok1 ? sc[r][ch][2] * f[r][0] : -INFINITY;
-              sc[r][ch][3] = ok1 ? sc[r][ch][3] * f[r][1] : -INFINITY;
+              float (&x)[4] = sc[r][ch];
+              x[0] = fmaf(s0, acc[r][0], i ? fmaf(l0, qsum[r][i][0], x[0]) : l0 * qsum[r][i][0]);
+              x[1] = fmaf(s0, acc[r][1], i ? fmaf(l0, qsum[r][i][1], x[1]) : l0 * qsum[r][i][1]);
+              x[2] = fmaf(s1, acc[r][2], i ? fmaf(l1, qsum[r][i][0], x[2]) : l1 * qsum[r][i][0]);
+              x[3] = fmaf(s1, acc[r][3], i ? fmaf(l1, qsum[r][i][1], x[3]) : l1 * qsum[r][i][1]);
             }
           }
-          // ---- running maximum; the value scales' power of two ----
-          uint32_t vm[2][2][G];
-          uint32_t vtop = 0;
+        }
+        if (partial) {
 #pragma unroll
-          for (int ch = 0; ch < 2; ++ch) {
-            const int sl = ch * 16 + slot_g;
+          for (int ch = 0; ch < 4; ++ch)
 #pragma unroll
-            for (int i = 0; i < G; ++i) {
-              vm[ch][0][i] = (valid >> sl & 1) ? vmeta[sl * G + i] : 0u;
-              vm[ch][1][i] = (valid >> (sl + 8) & 1) ? vmeta[(sl + 8) * G + i] : 0u;
-              const uint32_t b0 = vm[ch][0][i] & 0xffffu, b1 = vm[ch][1][i] & 0xffffu;
-              const uint32_t inf = kBf16 ? 0x7f80u : 0x7c00u;
-              vtop = max(vtop, b0 < inf ? b0 : 0u);
-              vtop = max(vtop, b1 < inf ? b1 : 0u);
-            }
+            for (int k = 0; k < 2; ++k)
+              if (!(valid >> (ch * 16 + slot_g + 8 * k) & 1)) {
+#pragma unroll
+                for (int r = 0; r < NT; ++r) sc[r][ch][2 * k] = sc[r][ch][2 * k + 1] = -INFINITY;
+              }
+        }
+        // ---- running maximum; the value scales' power of two ----
+        constexpr uint32_t kInf = kBf16 ? 0x7f80u : 0x7c00u;
+        uint32_t vtop;
+        {
+          const uint2 x = *reinterpret_cast<const uint2*>(vmeta + lane * 8);
+          vtop = __vmaxu2(x.x, x.y);
+          uint2 y = make_uint2(0, 0);
+          if (G == 2) {
+            y = *reinterpret_cast<const uint2*>(vmeta + 256 + lane * 8);
+            vtop = __vmaxu2(vtop, __vmaxu2(y.x, y.y));
           }
-          vtop = __reduce_max_sync(0xffffffffu, vtop);
-          const int etile = kBf16 ? min(max((int)(vtop >> 7) - 126, -120), 100) : (int)(vtop >> 10) - 14;
-          float mx[NT][2];
-          bool grow = etile > eref;
+          vtop = __reduce_max_sync(0xffffffffu, vtop & 0xffffu);
+          if (vtop >= kInf) {                            // a group that reads as NaN says nothing
+            vtop = 0;
+            for (const uint32_t w : {x.x, x.y, y.x, y.y}) vtop = max(vtop, (w & 0xffffu) < kInf ? w & 0xffffu : 0u);
+            vtop = __reduce_max_sync(0xffffffffu, vtop);
+          }
+        }
+        const int etile = kBf16 ? min(max((int)(vtop >> 7) - 126, -120), 100) : (int)(vtop >> 10) - 14;
+        float mx[NT][2];
+        bool grow = etile > eref || fresh;
+#pragma unroll
+        for (int r = 0; r < NT; ++r)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float x = fmaxf(sc[r][0][e], sc[r][0][e + 2]);
+#pragma unroll
+            for (int ch = 1; ch < 4; ++ch) x = fmaxf(x, fmaxf(sc[r][ch][e], sc[r][ch][e + 2]));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+            mx[r][e] = x * f[r][e];
+            // p may grow to 2^8 before the accumulators are brought to a new maximum
+            grow |= mx[r][e] > m[r][e] + 8.f;
+          }
+        if (__any_sync(0xffffffffu, grow)) {
+          // (behind new nodes, which leave eref at 0, it falls no further than their sums allow)
+          const int enew = fresh ? (eref == 0 ? max(etile, -60) : etile) : max(eref, etile);
+          const float ve = pow2(min(max(eref - enew, -126), 126));
+          eref = enew;
+          fresh = false;
 #pragma unroll
           for (int r = 0; r < NT; ++r)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              float x = fmaxf(fmaxf(sc[r][0][e], sc[r][0][e + 2]), fmaxf(sc[r][1][e], sc[r][1][e + 2]));
-              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-              mx[r][e] = x;
-              // p may grow to 2^8 before the accumulators are brought to a new maximum
-              grow |= x > m[r][e] + 8.f;
+              const float mn = fmaxf(m[r][e], mx[r][e]);
+              const float down = mn == -INFINITY ? 1.f : exp2_approx(m[r][e] - mn);
+              m[r][e] = mn;
+              l[r][e] *= down;
+#pragma unroll
+              for (int i = 0; i < G; ++i) olo[r][i][e] *= down;
+#pragma unroll
+              for (int i = 0; i < 4 * G; ++i) { o[r][i][e] *= down * ve; o[r][i][e + 2] *= down * ve; }
             }
-          if (__any_sync(0xffffffffu, grow)) {
-            const int enew = max(eref, etile);
-            const float ve = pow2(max(eref - enew, -126));
-            eref = enew;
+        }
+        const float vdown = pow2(-eref);
+        float neg[NT][2];
 #pragma unroll
-            for (int r = 0; r < NT; ++r)
+        for (int r = 0; r < NT; ++r)
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const float mn = fmaxf(m[r][e], mx[r][e]);
-                const float down = mn == -INFINITY ? 1.f : exp2_approx(m[r][e] - mn);
-                m[r][e] = mn;
-                l[r][e] *= down;
+          for (int e = 0; e < 2; ++e) neg[r][e] = m[r][e] == -INFINITY ? 0.f : -m[r][e];
+        // ---- probabilities, and the products with the values ----
 #pragma unroll
-                for (int i = 0; i < G; ++i) olo[r][i][e] *= down;
+        for (int ch = 0; ch < 4; ++ch) {
+          const int sl = ch * 16 + slot_g;
+          uint32_t vm[2][G], pb[NT][G][2];
+          load_meta<G>(vmeta + sl * 4 * G, vm[0]);
+          load_meta<G>(vmeta + (sl + 8) * 4 * G, vm[1]);
 #pragma unroll
-                for (int i = 0; i < 4 * G; ++i) { o[r][i][e] *= down * ve; o[r][i][e + 2] *= down * ve; }
-              }
-          }
-          const float vdown = pow2(-eref);
-          // ---- probabilities, and the products with the values ----
+          for (int r = 0; r < NT; ++r) {
+            float p[4];
 #pragma unroll
-          for (int ch = 0; ch < 2; ++ch) {
-            float vs[2][G], vl[2][G];
-#pragma unroll
-            for (int i = 0; i < G; ++i)
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                vs[k][i] = half_lo<kBf16>(vm[ch][k][i]) * vdown;
-                vl[k][i] = half_hi<kBf16>(vm[ch][k][i]);
-              }
-            uint32_t pb[NT][G][2];
-#pragma unroll
-            for (int r = 0; r < NT; ++r) {
-              float p[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float mm = m[r][e & 1] == -INFINITY ? 0.f : m[r][e & 1];
-                p[e] = exp2_approx(sc[r][ch][e] - mm);
-              }
-              l[r][0] += p[0] + p[2];
-              l[r][1] += p[1] + p[3];
-#pragma unroll
-              for (int i = 0; i < G; ++i) {
-                olo[r][i][0] = fmaf(p[0], vl[0][i], fmaf(p[2], vl[1][i], olo[r][i][0]));
-                olo[r][i][1] = fmaf(p[1], vl[0][i], fmaf(p[3], vl[1][i], olo[r][i][1]));
-                pb[r][i][0] = transpose8x8(pack16<false>(p[0] * vs[0][i], p[1] * vs[0][i]));
-                pb[r][i][1] = transpose8x8(pack16<false>(p[2] * vs[1][i], p[3] * vs[1][i]));
-              }
-            }
-            // operand column 2t is slot t, 2t+1 slot t+4 (and +8): as the scores' rows
+            for (int e = 0; e < 4; ++e) p[e] = exp2_approx(fmaf(sc[r][ch][e], f[r][e & 1], neg[r][e & 1]));
+            l[r][0] += p[0] + p[2];
+            l[r][1] += p[1] + p[3];
 #pragma unroll
             for (int i = 0; i < G; ++i) {
-              const unsigned char* vp = vst + (i * kAtTile + ch * 16 + t4) * 32 + g * 4;
-              const uint32_t w0 = *reinterpret_cast<const uint32_t*>(vp);
-              const uint32_t w1 = *reinterpret_cast<const uint32_t*>(vp + 4 * 32);
-              const uint32_t w2 = *reinterpret_cast<const uint32_t*>(vp + 8 * 32);
-              const uint32_t w3 = *reinterpret_cast<const uint32_t*>(vp + 12 * 32);
-              // even channels of both slots, odd channels of both slots
-              const uint32_t ea = __byte_perm(w0, w1, 0x5410), oa = __byte_perm(w0, w1, 0x7632);
-              const uint32_t eb = __byte_perm(w2, w3, 0x5410), ob = __byte_perm(w2, w3, 0x7632);
-#pragma unroll
-              for (int n = 0; n < 4; ++n) {
-                const uint32_t mask = n & 1 ? 0x00f000f0u : 0x000f000fu;
-                const int sh = n & 2 ? 8 : 0;
-#pragma unroll
-                for (int r = 0; r < NT; ++r)
-                  mma16816<false>(o[r][i * 4 + n], (ea >> sh) & mask, (oa >> sh) & mask, (eb >> sh) & mask,
-                                  (ob >> sh) & mask, pb[r][i][0], pb[r][i][1]);
-              }
+              const float v0 = half_lo<kBf16>(vm[0][i]) * vdown, l0 = half_hi<kBf16>(vm[0][i]);
+              const float v1 = half_lo<kBf16>(vm[1][i]) * vdown, l1 = half_hi<kBf16>(vm[1][i]);
+              olo[r][i][0] = fmaf(p[0], l0, fmaf(p[2], l1, olo[r][i][0]));
+              olo[r][i][1] = fmaf(p[1], l0, fmaf(p[3], l1, olo[r][i][1]));
+              pb[r][i][0] = transpose8x8(pack16<false>(p[0] * v0, p[1] * v0));
+              pb[r][i][1] = transpose8x8(pack16<false>(p[2] * v1, p[3] * v1));
             }
           }
-        } else {
-          // ---- new nodes: 16-bit keys and values, with the tree's mask ----
-          const int cached_tiles = (bc.len + kAtTile - 1) / kAtTile;
-          const int node0 = (tile - cached_tiles) * kAtTile;
-          if (a.k.p && node0 < bc.nodes) {
-            float sc[NT][2][4];
+          // operand column 2t is slot t, 2t+1 slot t+4 (and +8): as the scores' rows
 #pragma unroll
-            for (int r = 0; r < NT; ++r)
+          for (int i = 0; i < G; ++i) {
+            const unsigned char* vp = vst + (i * kKvTile + ch * 16 + t4) * 32 + g * 4;
+            const uint32_t w0 = *reinterpret_cast<const uint32_t*>(vp);
+            const uint32_t w1 = *reinterpret_cast<const uint32_t*>(vp + 4 * 32);
+            const uint32_t w2 = *reinterpret_cast<const uint32_t*>(vp + 8 * 32);
+            const uint32_t w3 = *reinterpret_cast<const uint32_t*>(vp + 12 * 32);
+            // even channels of both slots, odd channels of both slots
+            const uint32_t ea = __byte_perm(w0, w1, 0x5410), oa = __byte_perm(w0, w1, 0x7632);
+            const uint32_t eb = __byte_perm(w2, w3, 0x5410), ob = __byte_perm(w2, w3, 0x7632);
 #pragma unroll
-              for (int ch = 0; ch < 2; ++ch)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sc[r][ch][e] = 0.f;
-#pragma unroll
-            for (int i = 0; i < G; ++i)
-#pragma unroll
-              for (int half = 0; half < 2; ++half) {     // 8 channels at a time
-                uint4 kw[2][2];
-#pragma unroll
-                for (int ch = 0; ch < 2; ++ch)
-#pragma unroll
-                  for (int k = 0; k < 2; ++k) {
-                    const int node = node0 + ch * 16 + g + 8 * k;
-                    kw[ch][k] = make_uint4(0, 0, 0, 0);
-                    if (node < bc.nodes)
-                      kw[ch][k] = *reinterpret_cast<const uint4*>(a.k.at(s, node, head) + i * kKvGroup + t4 * 16 + half * 8);
-                  }
-#pragma unroll
-                for (int r = 0; r < NT; ++r) {
-                  const int row = row0 + r * 8 + g;
-                  uint4 qw = make_uint4(0, 0, 0, 0);
-                  if (row < n_rows)
-                    qw = *reinterpret_cast<const uint4*>(a.q.at(s, row / a.group, head * a.group + row % a.group) +
-                                                         i * kKvGroup + t4 * 16 + half * 8);
-#pragma unroll
-                  for (int ch = 0; ch < 2; ++ch) {
-                    mma16816<kBf16>(sc[r][ch], kw[ch][0].x, kw[ch][1].x, kw[ch][0].y, kw[ch][1].y, qw.x, qw.y);
-                    mma16816<kBf16>(sc[r][ch], kw[ch][0].z, kw[ch][1].z, kw[ch][0].w, kw[ch][1].w, qw.z, qw.w);
-                  }
-                }
-              }
-            const float fs = a.scale * kLog2e;
-            float mx[NT][2];
-#pragma unroll
-            for (int r = 0; r < NT; ++r)
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const int row = row0 + r * 8 + 2 * t4 + e;
-                unsigned long long sees = 0;
-                if (row < n_rows) {
-                  const int node = row / a.group;
-                  sees = a.mask ? a.mask[s * a.mask_stride + node] : (2ull << node) - 1ull;
-                }
-                mx[r][e] = -INFINITY;
-#pragma unroll
-                for (int ch = 0; ch < 2; ++ch)
-#pragma unroll
-                  for (int k = 0; k < 2; ++k) {
-                    const int node = node0 + ch * 16 + g + 8 * k;
-                    const bool ok = node < bc.nodes && (sees >> node & 1ull);
-                    float& x = sc[r][ch][e + 2 * k];
-                    x = ok ? x * fs : -INFINITY;
-                    mx[r][e] = fmaxf(mx[r][e], x);
-                  }
-                mx[r][e] = fmaxf(mx[r][e], __shfl_xor_sync(0xffffffffu, mx[r][e], 4));
-                mx[r][e] = fmaxf(mx[r][e], __shfl_xor_sync(0xffffffffu, mx[r][e], 8));
-                mx[r][e] = fmaxf(mx[r][e], __shfl_xor_sync(0xffffffffu, mx[r][e], 16));
-              }
-            // These products need no units: the accumulators are brought to 1 and, as the last
-            // tiles of the item, left at eref >= 0, where no finite value overflows.
-            const float there = pow2(min(eref + 24, 127));
-            eref = max(eref, 0);
-            const float back = pow2(-(eref + 24));
-#pragma unroll
-            for (int r = 0; r < NT; ++r)
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const float mn = fmaxf(m[r][e], mx[r][e]);
-                const float down = mn == -INFINITY ? 1.f : exp2_approx(m[r][e] - mn);
-                m[r][e] = mn;
-                l[r][e] *= down;
-#pragma unroll
-                for (int i = 0; i < G; ++i) olo[r][i][e] *= down;
-#pragma unroll
-                for (int i = 0; i < 4 * G; ++i) { o[r][i][e] *= down * there; o[r][i][e + 2] *= down * there; }
-              }
-#pragma unroll
-            for (int ch = 0; ch < 2; ++ch) {
-              // p as the sum of two 16-bit numbers: with bf16 one alone would be as coarse as
-              // the result's own rounding
-              uint32_t hi[NT][2], lo[NT][2];
+            for (int n = 0; n < 4; ++n) {
+              const uint32_t mask = n & 1 ? 0x00f000f0u : 0x000f000fu;
+              const int sh = n & 2 ? 8 : 0;
 #pragma unroll
               for (int r = 0; r < NT; ++r)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                  float p[2], q[2];
-#pragma unroll
-                  for (int e = 0; e < 2; ++e) {
-                    const float mm = m[r][e] == -INFINITY ? 0.f : m[r][e];
-                    p[e] = exp2_approx(sc[r][ch][e + 2 * k] - mm);
-                    l[r][e] += p[e];
-                  }
-                  const uint32_t h = pack16<kBf16>(p[0], p[1]);
-                  q[0] = p[0] - half_lo<kBf16>(h);
-                  q[1] = p[1] - half_hi<kBf16>(h);
-                  hi[r][k] = transpose8x8(h);
-                  lo[r][k] = transpose8x8(pack16<kBf16>(q[0], q[1]));
-                }
-#pragma unroll
-              for (int i = 0; i < G; ++i) {
-                uint4 w[4];                              // nodes 2t, 2t+1, 2t+8, 2t+9; 8 channels
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                  const int node = node0 + ch * 16 + 2 * t4 + (k & 1) + 8 * (k >> 1);
-                  w[k] = make_uint4(0, 0, 0, 0);
-                  if (node < bc.nodes)
-                    w[k] = *reinterpret_cast<const uint4*>(a.v.at(s, node, head) + i * kKvGroup + g * 8);
-                }
-#pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                  const uint32_t x0 = (&w[0].x)[n], x1 = (&w[1].x)[n], x2 = (&w[2].x)[n], x3 = (&w[3].x)[n];
-                  const uint32_t ea = __byte_perm(x0, x1, 0x5410), oa = __byte_perm(x0, x1, 0x7632);
-                  const uint32_t eb = __byte_perm(x2, x3, 0x5410), ob = __byte_perm(x2, x3, 0x7632);
-#pragma unroll
-                  for (int r = 0; r < NT; ++r) {
-                    // channel pair 2n: the cached codes of odd n carry 16 times their value
-                    float (&d)[4] = o[r][i * 4 + n];
-                    if (n & 1) {
-#pragma unroll
-                      for (int e = 0; e < 4; ++e) d[e] *= 0.0625f;
-                    }
-                    mma16816<kBf16>(d, ea, oa, eb, ob, hi[r][0], hi[r][1]);
-                    mma16816<kBf16>(d, ea, oa, eb, ob, lo[r][0], lo[r][1]);
-                    if (n & 1) {
-#pragma unroll
-                      for (int e = 0; e < 4; ++e) d[e] *= 16.f;
-                    }
-                  }
-                }
-              }
+                mma16816<false>(o[r][i * 4 + n], (ea >> sh) & mask, (oa >> sh) & mask, (eb >> sh) & mask,
+                                (ob >> sh) & mask, pb[r][i][0], pb[r][i][1]);
             }
-#pragma unroll
-            for (int r = 0; r < NT; ++r)
-#pragma unroll
-              for (int i = 0; i < 4 * G; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[r][i][e] *= back;
           }
         }
-        __syncwarp();
-        issue(stage == 0 ? kAtStages - 1 : stage - 1);
-        stage = stage == kAtStages - 1 ? 0 : stage + 1;
+      } else {
+        cp_async_wait<kAtStages - 1>();                  // an empty tile: nothing was copied
       }
-    } else {
-      for (; mu < at + piece; mu += kAtWarps) {          // items without rows: nothing was copied
-        cp_async_wait<kAtStages - 2>();
-        issue(stage == 0 ? kAtStages - 1 : stage - 1);
-        stage = stage == kAtStages - 1 ? 0 : stage + 1;
-      }
+      __syncwarp();
+      issue(stage);
+      stage = stage == kAtStages - 1 ? 0 : stage + 1;
     }
 
     // ---- the warps' results joined; the item's share written ----
@@ -511,6 +519,10 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
 
 #pragma unroll
     for (int r = 0; r < NT; ++r) {
+      // (two buffers in turn: the barrier of the next one is behind every read of this one)
+      float* ob = obuf + buf * (Sh::kObuf / 4);
+      float2* mb = ml + buf * (Sh::kMl / 8);
+      buf ^= 1;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
 #pragma unroll
@@ -519,7 +531,8 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
 #pragma unroll
           for (int i = 0; i < G; ++i) olo[r][i][e] += __shfl_xor_sync(0xffffffffu, olo[r][i][e], x);
         }
-        float* dst = obuf + (warp * 8 + 2 * t4 + e) * kOs + g * 8;
+        float* dst = ob + (warp * 8 + 2 * t4 + e) * kOs + g * 8;
+        if (had)
 #pragma unroll
         for (int i = 0; i < G; ++i) {
           // channels 8g + 2n (accumulator e) and 8g + 2n + 1 (e + 2); odd n carry 16 times
@@ -533,7 +546,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
           *reinterpret_cast<float4*>(dst + i * kKvGroup) = make_float4(v[0], v[1], v[2], v[3]);
           *reinterpret_cast<float4*>(dst + i * kKvGroup + 4) = make_float4(v[4], v[5], v[6], v[7]);
         }
-        if (g == 0) ml[warp * 8 + 2 * t4 + e] = make_float2(m[r][e], l[r][e]);
+        if (g == 0) mb[warp * 8 + 2 * t4 + e] = make_float2(m[r][e], l[r][e]);
       }
       __syncthreads();
       {
@@ -541,29 +554,27 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
 #pragma unroll
         for (int e = 0; e < kPer; ++e) v[e] = 0.f;
 #pragma unroll
-        for (int w = 0; w < kAtWarps; ++w) big = fmaxf(big, ml[w * 8 + row_w].x);
+        for (int w = 0; w < kAtWarps; ++w) big = fmaxf(big, mb[w * 8 + row_w].x);
 #pragma unroll
         for (int w = 0; w < kAtWarps; ++w) {
-          const float2 x = ml[w * 8 + row_w];
+          const float2 x = mb[w * 8 + row_w];
           const float k = x.x == -INFINITY ? (x.y == 0.f ? 0.f : 1.f) : exp2_approx(x.x - big);
           sum = fmaf(k, x.y, sum);
           if (k != 0.f) {
-            const float* src = obuf + (w * 8 + row_w) * kOs + lane * kPer;
+            float x2[kPer];
+            load_floats<kPer>(ob + (w * 8 + row_w) * kOs + lane * kPer, x2);
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) v[e] = fmaf(k, src[e], v[e]);
+            for (int e = 0; e < kPer; ++e) v[e] = fmaf(k, x2[e], v[e]);
           }
         }
         if (whole) {
           finish(r, big, sum, v);
         } else {
-          float* dst = my_part + (size_t)(r * 8 + row_w) * D + lane * kPer;
-#pragma unroll
-          for (int e = 0; e < kPer; ++e) __stcg(dst + e, v[e]);
+          store_floats<kPer>(my_part + (size_t)(r * 8 + row_w) * D + lane * kPer, v);
           if (lane == 0)
             __stcg(reinterpret_cast<float2*>(my_part + (size_t)kRows * D) + r * 8 + row_w, make_float2(big, sum));
         }
       }
-      __syncthreads();
     }
     if (!whole) {
       unsigned* ticket = reinterpret_cast<unsigned*>(c.work + kKvTicketOff) + b0;
@@ -603,18 +614,15 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
               const float ki = __shfl_sync(0xffffffffu, k, i);
               const float li = __shfl_sync(0xffffffffu, x.y, i);
               sum = fmaf(ki, li, sum);
-              const float* src = part_of(p0 + i) + (size_t)(r * 8 + row_w) * D + lane * kPer;
+              float y[kPer];
+              load_floats_cg<kPer>(part_of(p0 + i) + (size_t)(r * 8 + row_w) * D + lane * kPer, y);
 #pragma unroll
-              for (int e = 0; e < kPer; ++e) {
-                const float y = __ldcg(src + e);
-                v[e] = ki != 0.f ? fmaf(ki, y, v[e]) : v[e];
-              }
+              for (int e = 0; e < kPer; ++e) v[e] = ki != 0.f ? fmaf(ki, y[e], v[e]) : v[e];
             }
           }
           finish(r, big, sum, v);
         }
       }
-      __syncthreads();
     }
     at += piece;
     if (at < u1) list.advance(bc, piece);
@@ -623,14 +631,12 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
 
 template <int D, int NT, bool kBf16>
 static cudaError_t attend_launch(const KvView& c, const KvAttendArgs& a, int sms, cudaStream_t st) {
-  return launch_pdl(kv_attend_kernel<D, NT, kBf16>, dim3(sms), dim3(kAtThreads), AttendShared<D>::kBytes, st, c, a);
+  return launch_pdl(kv_attend_kernel<D, NT, kBf16>, dim3(sms), dim3(kAtThreads), Attend<D>::kBytes, st, c, a);
 }
 template <int D, bool kBf16>
 static cudaError_t attend_rows(const KvView& c, const KvAttendArgs& a, int sms, cudaStream_t st) {
-  const int rows = a.m * a.group;
-  if (rows <= 8) return attend_launch<D, 1, kBf16>(c, a, sms, st);
-  if (rows <= 16) return attend_launch<D, 2, kBf16>(c, a, sms, st);
-  return attend_launch<D, 4, kBf16>(c, a, sms, st);
+  if (a.m * a.group <= 8) return attend_launch<D, 1, kBf16>(c, a, sms, st);
+  return attend_launch<D, 2, kBf16>(c, a, sms, st);
 }
 
 cudaError_t launch_kv_attend(const KvView& c, const KvAttendArgs& a, int head_dim, bool bf16, int sms,
@@ -642,10 +648,8 @@ cudaError_t launch_kv_attend(const KvView& c, const KvAttendArgs& a, int head_di
 
 template <int D, bool kBf16>
 static cudaError_t preload_rows() {
-  cudaError_t e;
-  if ((e = preload_kernel(kv_attend_kernel<D, 1, kBf16>, true)) != cudaSuccess) return e;
-  if ((e = preload_kernel(kv_attend_kernel<D, 2, kBf16>, true)) != cudaSuccess) return e;
-  return preload_kernel(kv_attend_kernel<D, 4, kBf16>, true);
+  const cudaError_t e = preload_kernel(kv_attend_kernel<D, 1, kBf16>, true);
+  return e != cudaSuccess ? e : preload_kernel(kv_attend_kernel<D, 2, kBf16>, true);
 }
 cudaError_t preload_kv_attend_kernels() {
   cudaError_t e;

@@ -13,7 +13,7 @@
 
 namespace oilbird {
 
-constexpr int kWgThreads = 256, kWgWarps = 8, kWgStages = 4;
+constexpr int kWgThreads = 256, kWgWarps = 8, kWgStages = 2;
 constexpr int kWgMaxRows = 256;                          // rows of one launch
 
 template <int D>
@@ -23,7 +23,7 @@ struct WeighShared {
   static constexpr int kRowTile = 32 * (D / 16) * 8;                 // operands of 8 rows
   // behind the ring: cum, scratch, len, per row: sum per group, factor, lse, weight, index
   static constexpr int kFixed = kRing + (kKvMaxSeq + 1) * 8 + kWgWarps * 8 + kKvMaxSeq * 5 +
-                                kWgWarps * kWgStages * 4 + 64;
+                                kWgWarps * kWgStages * 8 + 64;
   static int bytes(int row_tiles) { return kFixed + row_tiles * (kRowTile + 8 * 4 * (D / kKvGroup + 4)); }
 };
 
@@ -35,14 +35,14 @@ kv_weigh_kernel(const KvView c, const KvWeighArgs a, int row_tiles) {
   extern __shared__ __align__(16) unsigned char smem[];
   unsigned char* ring = smem;
   uint2* qs = reinterpret_cast<uint2*>(smem + Sh::kRing);            // [row tile][step][lane]
-  float* row_sum = reinterpret_cast<float*>(smem + Sh::kRing + row_tiles * Sh::kRowTile);   // [row][G]
+  float* row_sum = reinterpret_cast<float*>(smem + Sh::kRing + row_tiles * Sh::kRowTile);   // [G][row]
   float* row_f = row_sum + row_tiles * 8 * G;
   float* row_lse = row_f + row_tiles * 8;                            // in exponents of two
   float* row_w = row_lse + row_tiles * 8;
   int* row_id = reinterpret_cast<int*>(row_w + row_tiles * 8);
   long long* cum = reinterpret_cast<long long*>(row_id + row_tiles * 8);
   long long* scratch = cum + kKvMaxSeq + 1;
-  uint32_t* valid_s = reinterpret_cast<uint32_t*>(scratch + kWgWarps);
+  unsigned long long* valid_s = reinterpret_cast<unsigned long long*>(scratch + kWgWarps);
   int* len_s = reinterpret_cast<int*>(valid_s + kWgWarps * kWgStages);
   int* count_s = len_s + kKvMaxSeq;                                  // [kWgWarps + 1]
   unsigned char* nodes_s = reinterpret_cast<unsigned char*>(count_s + kWgWarps + 1);
@@ -57,7 +57,6 @@ kv_weigh_kernel(const KvView c, const KvWeighArgs a, int row_tiles) {
   list.items = c.n_kv;
   list.group = a.group;
   list.rows = 0;
-  list.node_tiles = a.node_weight ? (a.m + kKvTile - 1) / kKvTile : 0;
   list.build<kWgThreads>(c, a.n_new, a.m, scratch);
   const long long total = list.total;
   const long long n_cta = min((long long)gridDim.x, (total + kWgWarps - 1) / kWgWarps);
@@ -65,18 +64,17 @@ kv_weigh_kernel(const KvView c, const KvWeighArgs a, int row_tiles) {
   const long long u0 = total * blockIdx.x / n_cta, u1 = total * (blockIdx.x + 1) / n_cta;
 
   unsigned char* my_ring = ring + warp * (kWgStages * Sh::kStage);
-  uint32_t* my_valid = valid_s + warp * kWgStages;
+  unsigned long long* my_valid = valid_s + warp * kWgStages;
   TileCursor pc;
   long long pu = u0 + warp;
   int ahead = -1;
   if (pu < u1) { list.seek(pc, pu); ahead = tile_pages(c, pc, lane); }
   auto issue = [&](int stage) {
     if (pu < u1) {
-      const int slot0 = pc.tile * kKvTile;
-      if (slot0 < pc.len) {
-        const int p0 = __shfl_sync(0xffffffffu, ahead, 0), p1 = __shfl_sync(0xffffffffu, ahead, 1);
-        copy_tile<D, false>(c, pc.item, slot0, p0, p1, my_ring + stage * Sh::kStage, lane);
-        if (lane == 0) my_valid[stage] = tile_valid(pc.len - slot0, p0, p1);
+      if (pc.cached()) {
+        copy_tile<D, false>(c, pc, ahead, my_ring + stage * Sh::kStage, lane);
+        const unsigned long long v = tile_valid(pc, ahead);
+        if (lane == 0) my_valid[stage] = v;
       }
       pu += kWgWarps;
       if (pu < u1) { list.advance(pc, kWgWarps); ahead = tile_pages(c, pc, lane); }
@@ -84,7 +82,7 @@ kv_weigh_kernel(const KvView c, const KvWeighArgs a, int row_tiles) {
     cp_async_commit();
   };
 #pragma unroll
-  for (int i = 0; i < kWgStages - 1; ++i) issue(i);
+  for (int i = 0; i < kWgStages; ++i) issue(i);
   int stage = 0;
 
   TileCursor bc;
@@ -129,110 +127,115 @@ kv_weigh_kernel(const KvView c, const KvWeighArgs a, int row_tiles) {
       uint32_t b[kSteps][2];
       float sum[G];
       const int e0 = row_operands<D, kBf16>(a.q.at(s, have ? id / a.group : 0, head * a.group + (have ? id % a.group : 0)),
-                                            have, t4, b, sum);
+                                            have, t4, a.scale < 0.f, b, sum);
 #pragma unroll
       for (int j = 0; j < kSteps; ++j) qs[(r * kSteps + j) * 32 + lane] = make_uint2(b[j][0], b[j][1]);
       if (t4 == 0) {
         row_f[r * 8 + g] = have ? row_factor(a.scale, e0) : 0.f;
 #pragma unroll
-        for (int i = 0; i < G; ++i) row_sum[(r * 8 + g) * G + i] = sum[i] * 0x1p-24f;
+        for (int i = 0; i < G; ++i) row_sum[i * row_tiles * 8 + r * 8 + g] = sum[i] * 0x1p-24f;
       }
     }
     __syncthreads();
 
     for (; mu < at + piece; mu += kWgWarps) {
-      const int tile = (int)(mu - item_u0), slot0 = tile * kKvTile;
-      cp_async_wait<kWgStages - 2>();
+      const int tile = (int)(mu - item_u0), slot0 = (tile - kKvFront) * kKvTile;
+      cp_async_wait<kWgStages - 1>();
       __syncwarp();
-      float got[2][2] = {{0.f, 0.f}, {0.f, 0.f}};        // chunk, logical rows g and g + 8
-      if (slot0 < bc.len) {
-        const unsigned char* st = my_ring + stage * Sh::kStage;
-        const uint32_t* kmeta = reinterpret_cast<const uint32_t*>(st + G * kKvTile * 32);
-        const uint32_t valid = my_valid[stage];
+      if (tile >= kKvFront) {
+        unsigned char* st = my_ring + stage * Sh::kStage;
+        unsigned char* kmeta = st + G * kKvTile * 32;
+        const unsigned long long valid = my_valid[stage];
+        if (valid != ~0ull) {
+          clear_meta<G>(kmeta, valid, lane);
+          __syncwarp();
+        }
         const int slot_g = (g >> 1) + 4 * (g & 1);
-        uint2 w[2][2][G];
-        float sc[2][2][G], lo[2][2][G];
 #pragma unroll
-        for (int ch = 0; ch < 2; ++ch)
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const int sl = ch * 16 + slot_g + 8 * k;
-#pragma unroll
-            for (int i = 0; i < G; ++i) {
-              w[ch][k][i] = *reinterpret_cast<const uint2*>(st + (i * kKvTile + sl) * 32 + t4 * 8);
-              const uint32_t meta = kmeta[sl * G + i];
-              sc[ch][k][i] = half_lo<kBf16>(meta);
-              lo[ch][k][i] = half_hi<kBf16>(meta);
-            }
-          }
-        for (int r = 0; r < n_tiles; ++r) {
-          float f[2], ls[2], rwt[2], qsum[G][2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int i = r * 8 + 2 * t4 + e;
-            f[e] = row_f[i];
-            ls[e] = row_lse[i];
-            rwt[e] = row_w[i];
-#pragma unroll
-            for (int k = 0; k < G; ++k) qsum[k][e] = row_sum[i * G + k];
-          }
-          float x[2][4];
+        for (int pair = 0; pair < 2; ++pair) {           // 32 slots: two chunks
+          float got[2][2] = {{0.f, 0.f}, {0.f, 0.f}};    // chunk, logical rows g and g + 8
+          uint2 w[2][2][G];
+          float sc[2][2][G], lo[2][2][G];
 #pragma unroll
           for (int ch = 0; ch < 2; ++ch)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[ch][e] = 0.f;
+            for (int k = 0; k < 2; ++k) {
+              const int sl = pair * 32 + ch * 16 + slot_g + 8 * k;
+              uint32_t meta[G];
+              load_meta<G>(kmeta + sl * 4 * G, meta);
 #pragma unroll
-          for (int i = 0; i < G; ++i) {
-            float acc[2][4];
-#pragma unroll
-            for (int ch = 0; ch < 2; ++ch)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) acc[ch][e] = 0.f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint2 b = qs[(r * kSteps + i * 4 + j) * 32 + lane];
-#pragma unroll
-              for (int ch = 0; ch < 2; ++ch) {
-                const uint32_t x0 = (j & 2 ? w[ch][0][i].y : w[ch][0][i].x) >> (8 * (j & 1));
-                const uint32_t x1 = (j & 2 ? w[ch][1][i].y : w[ch][1][i].x) >> (8 * (j & 1));
-                mma16816<false>(acc[ch], x0 & 0x000f000fu, x1 & 0x000f000fu, x0 & 0x00f000f0u, x1 & 0x00f000f0u,
-                                b.x, b.y);
+              for (int i = 0; i < G; ++i) {
+                w[ch][k][i] = *reinterpret_cast<const uint2*>(st + (i * kKvTile + sl) * 32 + t4 * 8);
+                sc[ch][k][i] = half_lo<kBf16>(meta[i]);
+                lo[ch][k][i] = half_hi<kBf16>(meta[i]);
               }
+            }
+          for (int r = 0; r < n_tiles; ++r) {
+            float f[2], ls[2], rwt[2], qsum[G][2];
+            const int i2 = r * 8 + 2 * t4;               // the lane's two rows
+            *reinterpret_cast<float2*>(f) = *reinterpret_cast<const float2*>(row_f + i2);
+            *reinterpret_cast<float2*>(ls) = *reinterpret_cast<const float2*>(row_lse + i2);
+            *reinterpret_cast<float2*>(rwt) = *reinterpret_cast<const float2*>(row_w + i2);
+#pragma unroll
+            for (int k = 0; k < G; ++k)
+              *reinterpret_cast<float2*>(qsum[k]) = *reinterpret_cast<const float2*>(row_sum + k * row_tiles * 8 + i2);
+            float x[2][4];
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+              float acc[2][4];
+#pragma unroll
+              for (int ch = 0; ch < 2; ++ch)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[ch][e] = 0.f;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const uint2 b = qs[(r * kSteps + i * 4 + j) * 32 + lane];
+#pragma unroll
+                for (int ch = 0; ch < 2; ++ch) {
+                  const uint32_t x0 = (j & 2 ? w[ch][0][i].y : w[ch][0][i].x) >> (8 * (j & 1));
+                  const uint32_t x1 = (j & 2 ? w[ch][1][i].y : w[ch][1][i].x) >> (8 * (j & 1));
+                  mma16816<false>(acc[ch], x0 & 0x000f000fu, x1 & 0x000f000fu, x0 & 0x00f000f0u, x1 & 0x00f000f0u,
+                                  b.x, b.y);
+                }
+              }
+#pragma unroll
+              for (int ch = 0; ch < 2; ++ch)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const float y = lo[ch][e >> 1][i] * qsum[i][e & 1];
+                  x[ch][e] = fmaf(sc[ch][e >> 1][i], acc[ch][e], i ? x[ch][e] + y : y);
+                }
             }
 #pragma unroll
             for (int ch = 0; ch < 2; ++ch)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                x[ch][e] = fmaf(sc[ch][e >> 1][i], acc[ch][e], fmaf(lo[ch][e >> 1][i], qsum[i][e & 1], x[ch][e]));
+                got[ch][e >> 1] = fmaf(rwt[e & 1], exp2_approx(fmaf(x[ch][e], f[e & 1], -ls[e & 1])), got[ch][e >> 1]);
           }
+          // the four lanes of a slot hold two rows each; then lane t4 adds slot (t4 & 1) * 8 of
+          // chunk t4 / 2
+          float mine = 0.f;
 #pragma unroll
           for (int ch = 0; ch < 2; ++ch)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              got[ch][e >> 1] = fmaf(rwt[e & 1], exp2_approx(fmaf(x[ch][e], f[e & 1], -ls[e & 1])), got[ch][e >> 1]);
-        }
-        // the four lanes of a slot hold two rows each; then lane t4 adds slot (t4 & 1) * 8 of chunk t4 / 2
-        float mine = 0.f;
-#pragma unroll
-        for (int ch = 0; ch < 2; ++ch)
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            float v = got[ch][k];
-            v += __shfl_xor_sync(0xffffffffu, v, 1);
-            v += __shfl_xor_sync(0xffffffffu, v, 2);
-            if (t4 == ch * 2 + k) mine = v;
+            for (int k = 0; k < 2; ++k) {
+              float v = got[ch][k];
+              v += __shfl_xor_sync(0xffffffffu, v, 1);
+              v += __shfl_xor_sync(0xffffffffu, v, 2);
+              if (t4 == ch * 2 + k) mine = v;
+            }
+          const int sl = pair * 32 + (t4 >> 1) * 16 + (t4 & 1) * 8 + slot_g;
+          if (n_tiles && (valid >> sl & 1)) {
+            const int slot = slot0 + sl, page = 1 << c.page_shift;
+            const int p = c.table[(size_t)s * c.max_pages + (slot >> c.page_shift)];
+            // nobody else adds to this slot in this launch: the result has no order to depend on
+            atomicAdd(c.weight + ((size_t)p * c.n_kv + head) * page + (slot & (page - 1)), mine);
           }
-        const int sl = (t4 >> 1) * 16 + (t4 & 1) * 8 + slot_g;
-        if (n_tiles && (valid >> sl & 1)) {
-          const int slot = slot0 + sl;
-          const int p = c.table[(size_t)s * c.max_pages + (slot >> c.page_shift)];
-          const int page = 1 << c.page_shift;
-          // nobody else adds to this slot in this launch: the result has no order to depend on
-          atomicAdd(c.weight + ((size_t)p * c.n_kv + head) * page + (slot & (page - 1)), mine);
         }
-      } else {
+      } else if (a.node_weight && tile * kKvNodeTile < a.m) {
         // ---- new nodes ----
-        const int node0 = (tile - (bc.len + kKvTile - 1) / kKvTile) * kKvTile;
+        const int node0 = tile * kKvNodeTile;
+        float got[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
         for (int r = 0; r < n_tiles; ++r) {
           const int id = row_id[r * 8 + g];
           float x[2][4];
@@ -284,14 +287,14 @@ kv_weigh_kernel(const KvView c, const KvWeighArgs a, int row_tiles) {
             v += __shfl_xor_sync(0xffffffffu, v, 1);
             v += __shfl_xor_sync(0xffffffffu, v, 2);
             const int node = node0 + ch * 16 + g + 8 * k;
-            if (a.node_weight && t4 == ch * 2 + k && node < a.m) {
+            if (t4 == ch * 2 + k && node < a.m) {
               float* p = a.node_weight + ((size_t)s * c.n_kv + head) * a.m + node;
               *p = a.node0 == 0 ? v : *p + v;            // a later launch of the same call adds
             }
           }
       }
       __syncwarp();
-      issue(stage == 0 ? kWgStages - 1 : stage - 1);
+      issue(stage);
       stage = stage == kWgStages - 1 ? 0 : stage + 1;
     }
     __syncthreads();
