@@ -317,49 +317,45 @@ __device__ __forceinline__ int tile_pages(const KvView& c, const TileCursor& k, 
   }
   return p;
 }
-// Starts the copies of a tile (a whole warp): codes [group][slot][32 B] and meta [slot][group]
-// of the keys and, with kValues, of the values behind them.  Quarters without a page are zeroed.
-template <int D, bool kValues>
+// Starts the copies of a tile's keys (kValue 0) or values (1), a whole warp: codes
+// [group][slot][32 B] and meta [slot][group].  Quarters without a page are zeroed.
+template <int D, int kValue>
 __device__ __forceinline__ void copy_tile(const KvView& c, const TileCursor& k, int pages,
                                           unsigned char* dst_ptr, int lane) {
-  constexpr int G = D / kKvGroup, kParts = kValues ? 2 : 1;
-  constexpr int kTilePart = G * kKvTile * 36;
+  constexpr int G = D / kKvGroup;
   const uint32_t dst = kv_smem(dst_ptr) + lane * 16;
   const int page = 1 << c.page_shift;
   const size_t block = 2 * (size_t)kv_part_bytes(D, page);
   if (c.page_shift == 6) {                               // the tile is a page
+    constexpr int kPart = G * kKvTile * 36, kChunks = kPart / 16;    // as it lies in memory
     const int p = __shfl_sync(0xffffffffu, pages, 0);
     const uint32_t n = p < 0 ? 0 : 16;
-    const unsigned char* b = c.pages + ((size_t)(uint32_t)max(p, 0) * c.n_kv + k.head) * block + lane * 16;
-    constexpr int kChunks = kTilePart / 16;              // and lies in memory as it will here
+    const unsigned char* b = c.pages + ((size_t)(uint32_t)max(p, 0) * c.n_kv + k.head) * block + kValue * kPart + lane * 16;
 #pragma unroll
-    for (int i = 0; i < kParts * kChunks; i += 32)
-      if (i + 32 <= kParts * kChunks || i + lane < kParts * kChunks) cp_async16(dst + i * 16, b + i * 16, n);
+    for (int i = 0; i < kChunks; i += 32)
+      if (i + 32 <= kChunks || i + lane < kChunks) cp_async16(dst + i * 16, b + i * 16, n);
     return;
   }
   const int part = G * page * 36;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const int p = __shfl_sync(0xffffffffu, pages, q), in = (k.slot0() + q * 16) & (page - 1);
-    const unsigned char* b = c.pages + ((size_t)(uint32_t)max(p, 0) * c.n_kv + k.head) * block;
+    const unsigned char* b = c.pages + ((size_t)(uint32_t)max(p, 0) * c.n_kv + k.head) * block + kValue * part;
     const uint32_t n = p < 0 ? 0 : 16;
 #pragma unroll
-    for (int kv = 0; kv < kParts; ++kv) {
-#pragma unroll
-      for (int i = 0; i < G; ++i)
-        cp_async16(dst + kv * kTilePart + i * 2048 + q * 512, b + kv * part + (i * page + in) * 32 + lane * 16, n);
-      if (lane < 4 * G)
-        cp_async16(dst + kv * kTilePart + G * 2048 + q * 64 * G, b + kv * part + (G * page * 8 + in * G) * 4 + lane * 16, n);
-    }
+    for (int i = 0; i < G; ++i) cp_async16(dst + i * 2048 + q * 512, b + (i * page + in) * 32 + lane * 16, n);
+    if (lane < 4 * G) cp_async16(dst + G * 2048 + q * 64 * G, b + (G * page * 8 + in * G) * 4 + lane * 16, n);
   }
 }
 // bit i: slot i of the tile exists and has a page
 __device__ __forceinline__ unsigned long long tile_valid(const TileCursor& k, int pages) {
   const int left = k.len - k.slot0();
+  const uint32_t have = __ballot_sync(0xffffffffu, pages >= 0);
+  if (left >= 64 && (have & 15u) == 15u) return ~0ull;
   unsigned long long v = left >= 64 ? ~0ull : (1ull << left) - 1ull;
 #pragma unroll
   for (int q = 0; q < 4; ++q)
-    if (__shfl_sync(0xffffffffu, pages, q) < 0) v &= ~(0xffffull << (16 * q));
+    if (!(have >> q & 1u)) v &= ~(0xffffull << (16 * q));
   return v;
 }
 // Zeroes the meta of a tile's slots that are not valid, so that whatever lay there is finite.

@@ -18,7 +18,7 @@
 // take 256 and 128 contiguous bytes of shared memory.
 //
 // Work.  The tiles (64 slots) of all (sequence, head, row block) items are one list, cut into
-// equal runs, one per block; a block's eight warps take the run's tiles in turn, each
+// equal runs, one per block; a block's warps take the run's tiles in turn, each
 // through a ring of its own (asynchronous 16-byte copies, no block-wide waits), which runs on
 // across items.  At the end of an item's share the warps' results are joined in
 // shared memory; items cut between blocks go through the workspace, and the block that
@@ -27,18 +27,20 @@
 
 namespace oilbird {
 
-// Rows per block are 8 NT.  The ring holds 147 KB at D = 128, about three times what an SM must
-// have in flight for its share of the memory rate.
-constexpr int kAtWarps = 8, kAtThreads = 256, kAtStages = 2;
-template <int D>
+// Rows per block are 8 NT.  A warp's ring holds its tile's keys and values in buffers of their
+// own: the next tile's keys are asked for as soon as the scores are taken, its values after the
+// products with them, so that a single buffer of each keeps half a tile per warp in flight.
+// Eight rows leave registers for twelve warps an SM.
+template <int D, int NT>
 struct Attend {
-  static constexpr int kStage = kKvTile * (D / kKvGroup) * 72;       // K codes, K meta, V codes, V meta
-  static constexpr int kRing = kAtWarps * kAtStages * kStage;
-  static constexpr int kObuf = kAtWarps * 8 * (D + 4) * 4;           // twice
-  static constexpr int kMl = kAtWarps * 8 * 8;                       // twice
-  static constexpr int kValid = kAtWarps * kAtStages * 8;
+  static constexpr int kWarps = NT == 1 ? 12 : 8, kThreads = 32 * kWarps, kStages = NT == 1 ? 1 : 2;
+  static constexpr int kPart = kKvTile * (D / kKvGroup) * 36;        // codes, meta of K or of V
+  static constexpr int kRing = kWarps * kStages * 2 * kPart;
+  static constexpr int kObuf = kWarps * 8 * (D + 4) * 4;             // twice
+  static constexpr int kMl = kWarps * 8 * 8;                         // twice
+  static constexpr int kValid = kWarps * kStages * 8;
   static constexpr int kCum = (kKvMaxSeq + 1) * 8;
-  static constexpr int kBytes = kRing + 2 * (kObuf + kMl) + kValid + kCum + kAtWarps * 8 + kKvMaxSeq * 5 + 16;
+  static constexpr int kBytes = kRing + 2 * (kObuf + kMl) + kValid + kCum + kWarps * 8 + kKvMaxSeq * 5 + 16;
 };
 
 template <int N> __device__ __forceinline__ void load_floats(const float* p, float (&v)[N]) {
@@ -55,9 +57,10 @@ template <int N> __device__ __forceinline__ void store_floats(float* p, const fl
 }
 
 template <int D, int NT, bool kBf16>
-__global__ void __launch_bounds__(kAtThreads, 1)
+__global__ void __launch_bounds__(Attend<D, NT>::kThreads, 1)
 kv_attend_kernel(const KvView c, const KvAttendArgs a) {
-  using Sh = Attend<D>;
+  using Sh = Attend<D, NT>;
+  constexpr int kAtThreads = Sh::kThreads, kAtWarps = Sh::kWarps, kAtStages = Sh::kStages;
   constexpr int G = D / kKvGroup, kRows = NT * 8, kSteps = D / 16;
   extern __shared__ __align__(16) unsigned char smem[];
   unsigned char* ring = smem;
@@ -91,26 +94,30 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
   const long long u0 = share_at(blockIdx.x), u1 = share_at(blockIdx.x + 1);
 
   // ---- the warp's ring of tiles ----
-  unsigned char* my_ring = ring + warp * (kAtStages * Sh::kStage);
+  unsigned char* my_ring = ring + warp * (kAtStages * 2 * Sh::kPart);
   unsigned long long* my_valid = valid_s + warp * kAtStages;
   TileCursor pc;
   long long pu = u0 + warp;                              // the next tile to copy, its pages
   int ahead = -1;
   if (pu < u1) { list.seek(pc, pu); ahead = tile_pages(c, pc, lane); }
-  auto issue = [&](int stage) {
+  auto issue_keys = [&](int stage) {
+    if (pu < u1 && pc.cached()) {
+      copy_tile<D, 0>(c, pc, ahead, my_ring + stage * 2 * Sh::kPart, lane);
+      const unsigned long long v = tile_valid(pc, ahead);
+      if (lane == 0) my_valid[stage] = v;
+    }
+    cp_async_commit();
+  };
+  auto issue_values = [&](int stage) {                   // and on to the next tile
     if (pu < u1) {
-      if (pc.cached()) {
-        copy_tile<D, true>(c, pc, ahead, my_ring + stage * Sh::kStage, lane);
-        const unsigned long long v = tile_valid(pc, ahead);
-        if (lane == 0) my_valid[stage] = v;
-      }
+      if (pc.cached()) copy_tile<D, 1>(c, pc, ahead, my_ring + stage * 2 * Sh::kPart + Sh::kPart, lane);
       pu += kAtWarps;
       if (pu < u1) { list.advance(pc, kAtWarps); ahead = tile_pages(c, pc, lane); }
     }
     cp_async_commit();
   };
 #pragma unroll
-  for (int i = 0; i < kAtStages; ++i) issue(i);
+  for (int i = 0; i < kAtStages; ++i) { issue_keys(i); issue_values(i); }
   int stage = 0, buf = 0;
 
   // ---- item by item ----
@@ -311,17 +318,14 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
             f[r][1] = __shfl_sync(0xffffffffu, ff, 8 * t4 + 4);
           }
         }
-        cp_async_wait<kAtStages - 1>();
+        cp_async_wait<2 * kAtStages - 1>();
         __syncwarp();
-        unsigned char* st = my_ring + stage * Sh::kStage;
+        unsigned char* st = my_ring + stage * 2 * Sh::kPart;
         unsigned char* kmeta = st + G * kKvTile * 32;
-        const unsigned char* vst = st + G * kKvTile * 36;
-        unsigned char* vmeta = st + G * kKvTile * 68;
         const unsigned long long valid = my_valid[stage];
         const bool partial = valid != ~0ull;             // the sequence's end, or a page that is none
         if (partial) {
           clear_meta<G>(kmeta, valid, lane);
-          clear_meta<G>(vmeta, valid, lane);
           __syncwarp();
         }
         const int slot_g = (g >> 1) + 4 * (g & 1);       // logical row g of a chunk
@@ -373,7 +377,17 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
                 for (int r = 0; r < NT; ++r) sc[r][ch][2 * k] = sc[r][ch][2 * k + 1] = -INFINITY;
               }
         }
+        __syncwarp();
+        issue_keys(stage);
         // ---- running maximum; the value scales' power of two ----
+        const unsigned char* vst = st + Sh::kPart;
+        unsigned char* vmeta = st + Sh::kPart + G * kKvTile * 32;
+        cp_async_wait<2 * kAtStages - 1>();
+        __syncwarp();
+        if (partial) {
+          clear_meta<G>(vmeta, valid, lane);
+          __syncwarp();
+        }
         constexpr uint32_t kInf = kBf16 ? 0x7f80u : 0x7c00u;
         uint32_t vtop;
         {
@@ -481,10 +495,12 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
           }
         }
       } else {
-        cp_async_wait<kAtStages - 1>();                  // an empty tile: nothing was copied
+        cp_async_wait<2 * kAtStages - 1>();              // an empty tile: nothing was copied
+        __syncwarp();
+        issue_keys(stage);
       }
       __syncwarp();
-      issue(stage);
+      issue_values(stage);
       stage = stage == kAtStages - 1 ? 0 : stage + 1;
     }
 
@@ -549,7 +565,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
         if (g == 0) mb[warp * 8 + 2 * t4 + e] = make_float2(m[r][e], l[r][e]);
       }
       __syncthreads();
-      {
+      if (warp < 8) {
         float big = -INFINITY, sum = 0.f, v[kPer];
 #pragma unroll
         for (int e = 0; e < kPer; ++e) v[e] = 0.f;
@@ -586,7 +602,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
         if (*flag) *ticket = 0u;                         // for the next call
       }
       __syncthreads();
-      if (*flag) {
+      if (*flag && warp < 8) {
         __threadfence();
 #pragma unroll 1
         for (int r = 0; r < NT; ++r) {
@@ -609,7 +625,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
             big = nb;
             const float k = x.x == -INFINITY ? (x.y == 0.f ? 0.f : 1.f) : exp2_approx(x.x - nb);
             const int n = min(32, b1 - p0 + 1);
-#pragma unroll 4
+#pragma unroll 8
             for (int i = 0; i < n; ++i) {
               const float ki = __shfl_sync(0xffffffffu, k, i);
               const float li = __shfl_sync(0xffffffffu, x.y, i);
@@ -631,7 +647,8 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
 
 template <int D, int NT, bool kBf16>
 static cudaError_t attend_launch(const KvView& c, const KvAttendArgs& a, int sms, cudaStream_t st) {
-  return launch_pdl(kv_attend_kernel<D, NT, kBf16>, dim3(sms), dim3(kAtThreads), Attend<D>::kBytes, st, c, a);
+  return launch_pdl(kv_attend_kernel<D, NT, kBf16>, dim3(sms), dim3(Attend<D, NT>::kThreads), Attend<D, NT>::kBytes,
+                    st, c, a);
 }
 template <int D, bool kBf16>
 static cudaError_t attend_rows(const KvView& c, const KvAttendArgs& a, int sms, cudaStream_t st) {

@@ -72,7 +72,7 @@ kv_weigh_kernel(const KvView c, const KvWeighArgs a, int row_tiles) {
   auto issue = [&](int stage) {
     if (pu < u1) {
       if (pc.cached()) {
-        copy_tile<D, false>(c, pc, ahead, my_ring + stage * Sh::kStage, lane);
+        copy_tile<D, 0>(c, pc, ahead, my_ring + stage * Sh::kStage, lane);
         const unsigned long long v = tile_valid(pc, ahead);
         if (lane == 0) my_valid[stage] = v;
       }
