@@ -29,7 +29,7 @@ namespace oilbird {
 
 constexpr int kKvGroup = 64;              // channels that share a scale and an offset
 constexpr int kKvMaxSeq = OILBIRD_KV_MAX_SEQ;   // their lengths sit in shared memory
-constexpr int kKvMaxCtas = 256;
+constexpr int kKvMaxCtas = 512;
 constexpr float kLog2e = 1.4426950408889634f;
 
 __host__ __device__ inline int kv_part_bytes(int head_dim, int page) {   // K or V of one block
@@ -45,7 +45,7 @@ struct KvWork {
 };
 constexpr size_t kKvTicketOff = 256;                                  // unsigned [kKvMaxCtas]
 constexpr size_t kKvPartOff = kKvTicketOff + 4 * kKvMaxCtas;          // partial results
-constexpr int kKvPartRows = 2 * kKvMaxCtas * 32;                      // rows of D + 2 floats
+constexpr int kKvPartRows = 2 * kKvMaxCtas * 16;                      // rows of D + 2 floats
 
 struct KvView {
   unsigned char* pages;      // [n_pages, n_kv, block]
@@ -274,10 +274,12 @@ struct TileList {
     }
     __syncthreads();
   }
+  // Cursors are the same in every lane; the shuffles say so, which moves their arithmetic out of
+  // the lanes' registers.
   __device__ __forceinline__ void load(TileCursor& k, int s) const {
     k.s = s;
-    k.len = len[s];
-    k.nodes = nodes[s];
+    k.len = __shfl_sync(0xffffffffu, len[s], 0);
+    k.nodes = __shfl_sync(0xffffffffu, (int)nodes[s], 0);
     k.tiles = tiles_of(k.len);
     k.live = live_items(k.nodes);
   }
@@ -287,11 +289,50 @@ struct TileList {
       const int mid = (lo + hi + 1) >> 1;
       if (cum[mid] <= u) lo = mid; else hi = mid - 1;
     }
+    lo = __shfl_sync(0xffffffffu, lo, 0);
     load(k, lo);
     const long long r = u - cum[lo], full = (long long)k.live * k.tiles;
-    if (r < full) { k.item = (int)(r / k.tiles); k.tile = (int)(r - (long long)k.item * k.tiles); }
-    else { k.item = k.live + (int)(r - full); k.tile = 0; }
+    int item, tile = 0;
+    if (r < full) {
+      item = full <= 0x7fffffffLL ? (int)((uint32_t)r / (uint32_t)k.tiles) : (int)(r / k.tiles);
+      tile = (int)(r - (long long)item * k.tiles);
+    } else {
+      item = k.live + (int)(r - full);
+    }
+    k.item = __shfl_sync(0xffffffffu, item, 0);
+    k.tile = __shfl_sync(0xffffffffu, tile, 0);
     k.head = k.item % n_kv;
+  }
+  // The list is cut at raw(b) = total b / n_cta, but not where that would leave a piece of
+  // hardly more than an item's first round, or the last few tiles of one: such a cut moves to the item's
+  // edge.  (Every block finds the same cuts.)
+  static constexpr int kNearStart = kKvFront + 4, kNearEnd = 4;
+  __device__ __forceinline__ long long cut(TileCursor& k, int b, int n_cta) const {
+    // (32-bit division wherever the numbers allow: the 64-bit one is a long routine)
+    const long long u = total * n_cta <= 0xffffffffLL ? (long long)((uint32_t)total * (uint32_t)b / (uint32_t)n_cta)
+                                                      : total * b / n_cta;
+    if (u >= total) return total;
+    seek(k, u);
+    const int tiles = k.item < k.live ? k.tiles : 1;
+    if (k.tile <= kNearStart) { const long long at = u - k.tile; k.tile = 0; return at; }
+    if (tiles - k.tile > kNearEnd) return u;
+    const int on = tiles - k.tile;
+    if (u + on < total) advance(k, on);
+    return u + on;
+  }
+  // Blocks that share the item [i0, i0 + tiles): b0..b1.
+  __device__ __forceinline__ void owners(long long i0, int tiles, int n_cta, int& b0, int& b1) const {
+    const long long lo = i0 + kNearStart + 1, hi = i0 + tiles - kNearEnd;
+    // in front of the first cut behind the start; the last cut before the end
+    if ((total + kNearStart + 2) * (n_cta + 1) <= 0xffffffffLL) {
+      const uint32_t t = (uint32_t)total, n = (uint32_t)n_cta;
+      b0 = (int)(((uint32_t)lo * n + t - 1) / t) - 1;
+      b1 = (int)(((uint32_t)hi * n + t - 1) / t) - 1;
+    } else {
+      b0 = (int)((lo * n_cta + total - 1) / total) - 1;
+      b1 = (int)((hi * n_cta + total - 1) / total) - 1;
+    }
+    if (b1 < b0) b1 = b0;
   }
   __device__ __forceinline__ void advance(TileCursor& k, int n) const {      // n tiles on, inside the list
     for (k.tile += n;;) {

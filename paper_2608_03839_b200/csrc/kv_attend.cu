@@ -33,14 +33,13 @@ namespace oilbird {
 // Eight rows leave registers for twelve warps an SM.
 template <int D, int NT>
 struct Attend {
-  static constexpr int kWarps = NT == 1 ? 12 : 8, kThreads = 32 * kWarps, kStages = NT == 1 ? 1 : 2;
+  static constexpr int kWarps = NT == 1 ? 6 : 4, kThreads = 32 * kWarps, kCtas = 2;
   static constexpr int kPart = kKvTile * (D / kKvGroup) * 36;        // codes, meta of K or of V
-  static constexpr int kRing = kWarps * kStages * 2 * kPart;
-  static constexpr int kObuf = kWarps * 8 * (D + 4) * 4;             // twice
-  static constexpr int kMl = kWarps * 8 * 8;                         // twice
-  static constexpr int kValid = kWarps * kStages * 8;
+  static constexpr int kRing = kWarps * 2 * kPart;
+  static constexpr int kObuf = kWarps * 8 * (D + 4) * 4;
+  static constexpr int kMl = kWarps * 8 * 8;
   static constexpr int kCum = (kKvMaxSeq + 1) * 8;
-  static constexpr int kBytes = kRing + 2 * (kObuf + kMl) + kValid + kCum + kWarps * 8 + kKvMaxSeq * 5 + 16;
+  static constexpr int kBytes = kRing + kObuf + kMl + kCum + kWarps * 8 + kKvMaxSeq * 5 + 16;
 };
 
 template <int N> __device__ __forceinline__ void load_floats(const float* p, float (&v)[N]) {
@@ -57,23 +56,22 @@ template <int N> __device__ __forceinline__ void store_floats(float* p, const fl
 }
 
 template <int D, int NT, bool kBf16>
-__global__ void __launch_bounds__(Attend<D, NT>::kThreads, 1)
+__global__ void __launch_bounds__(Attend<D, NT>::kThreads, Attend<D, NT>::kCtas)
 kv_attend_kernel(const KvView c, const KvAttendArgs a) {
   using Sh = Attend<D, NT>;
-  constexpr int kAtThreads = Sh::kThreads, kAtWarps = Sh::kWarps, kAtStages = Sh::kStages;
+  constexpr int kAtThreads = Sh::kThreads, kAtWarps = Sh::kWarps;
   constexpr int G = D / kKvGroup, kRows = NT * 8, kSteps = D / 16;
   extern __shared__ __align__(16) unsigned char smem[];
   unsigned char* ring = smem;
   float* obuf = reinterpret_cast<float*>(smem + Sh::kRing);
-  float2* ml = reinterpret_cast<float2*>(smem + Sh::kRing + 2 * Sh::kObuf);
-  unsigned long long* valid_s = reinterpret_cast<unsigned long long*>(smem + Sh::kRing + 2 * (Sh::kObuf + Sh::kMl));
-  long long* cum = reinterpret_cast<long long*>(valid_s + kAtWarps * kAtStages);
+  float2* ml = reinterpret_cast<float2*>(smem + Sh::kRing + Sh::kObuf);
+  long long* cum = reinterpret_cast<long long*>(smem + Sh::kRing + Sh::kObuf + Sh::kMl);
   long long* scratch = cum + kKvMaxSeq + 1;
   int* len_s = reinterpret_cast<int*>(scratch + kAtWarps);
   unsigned char* nodes_s = reinterpret_cast<unsigned char*>(len_s + kKvMaxSeq);
   int* flag = reinterpret_cast<int*>(nodes_s + kKvMaxSeq);
 
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, g = lane >> 2, t4 = lane & 3;
   const int rblocks = (a.m * a.group + kRows - 1) / kRows;
   pdl_enter();
 
@@ -87,48 +85,43 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
   list.build<kAtThreads>(c, a.n_new, a.m, scratch);
   const long long total = list.total;
   // blocks share the list evenly; no block gets less than a tile for each of its warps
-  const long long n_cta = min((long long)gridDim.x, (total + kAtWarps - 1) / kAtWarps);
+  const int n_cta = (int)min((long long)gridDim.x, (total + kAtWarps - 1) / kAtWarps);
   if (blockIdx.x >= n_cta) return;
-  auto share_at = [&](long long b) { return total * b / n_cta; };
-  auto owner = [&](long long u) { return (int)(((u + 1) * n_cta - 1) / total); };
-  const long long u0 = share_at(blockIdx.x), u1 = share_at(blockIdx.x + 1);
+  TileCursor bc, pc;                                     // the block's item; the warp's next tile to copy
+  const long long u1_all = list.cut(pc, blockIdx.x + 1, n_cta), u0 = list.cut(bc, blockIdx.x, n_cta);
+  const int u1 = (int)(u1_all - u0);                     // positions from here on count from u0
+  if (u1 <= 0) return;
 
   // ---- the warp's ring of tiles ----
-  unsigned char* my_ring = ring + warp * (kAtStages * 2 * Sh::kPart);
-  unsigned long long* my_valid = valid_s + warp * kAtStages;
-  TileCursor pc;
-  long long pu = u0 + warp;                              // the next tile to copy, its pages
-  int ahead = -1;
-  if (pu < u1) { list.seek(pc, pu); ahead = tile_pages(c, pc, lane); }
-  auto issue_keys = [&](int stage) {
+  unsigned char* st = ring + warp * (2 * Sh::kPart);
+  int pu = warp, ahead = -1;                             // the next tile to copy; its pages
+  unsigned long long valid_next = 0;
+  pc = bc;
+  if (pu < u1) { list.advance(pc, warp); ahead = tile_pages(c, pc, lane); }
+  auto issue_keys = [&]() {
     if (pu < u1 && pc.cached()) {
-      copy_tile<D, 0>(c, pc, ahead, my_ring + stage * 2 * Sh::kPart, lane);
-      const unsigned long long v = tile_valid(pc, ahead);
-      if (lane == 0) my_valid[stage] = v;
+      copy_tile<D, 0>(c, pc, ahead, st, lane);
+      valid_next = tile_valid(pc, ahead);
     }
     cp_async_commit();
   };
-  auto issue_values = [&](int stage) {                   // and on to the next tile
+  auto issue_values = [&]() {                            // and on to the next tile
     if (pu < u1) {
-      if (pc.cached()) copy_tile<D, 1>(c, pc, ahead, my_ring + stage * 2 * Sh::kPart + Sh::kPart, lane);
+      if (pc.cached()) copy_tile<D, 1>(c, pc, ahead, st + Sh::kPart, lane);
       pu += kAtWarps;
       if (pu < u1) { list.advance(pc, kAtWarps); ahead = tile_pages(c, pc, lane); }
     }
     cp_async_commit();
   };
-#pragma unroll
-  for (int i = 0; i < kAtStages; ++i) { issue_keys(i); issue_values(i); }
-  int stage = 0, buf = 0;
+  issue_keys();
+  issue_values();
 
   // ---- item by item ----
-  TileCursor bc;
-  list.seek(bc, u0);
-  long long mu = u0 + warp;                              // the warp's next tile to compute
-  for (long long at = u0; at < u1;) {
+  int mu = warp;                                         // the warp's next tile to compute
+  for (int at = 0; at < u1;) {
     const int item = bc.item, tile0 = bc.tile;
     const int n_tiles = item < bc.live ? bc.tiles : 1;
-    const int piece = (int)min((long long)(n_tiles - tile0), u1 - at);
-    const long long item_u0 = at - tile0;
+    const int piece = min(n_tiles - tile0, u1 - at), item_u0 = at - tile0;
     // live items: head fastest, then row block; the others follow in the same order
     const int head = bc.head, row0 = item / c.n_kv * kRows;
     const int n_rows = bc.nodes * a.group;               // rows of the sequence that exist
@@ -155,7 +148,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
 
     if (item < bc.live && mu < at + piece && mu < item_u0 + kKvFront) {
       // ---- the item's first round: new nodes, 16-bit keys and values, with the tree's mask ----
-      const int node0 = (int)(mu - item_u0) * kKvNodeTile;
+      const int node0 = (mu - item_u0) * kKvNodeTile;
       if (a.k.p && node0 < bc.nodes) {
         had = true;
         float sc[NT][2][4];
@@ -296,7 +289,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
     float f[NT][2], qsum[NT][G][2];
     bool loaded = false;
     for (; mu < at + piece; mu += kAtWarps) {
-      const int tile = (int)(mu - item_u0);
+      const int tile = mu - item_u0;
       if (item < bc.live && tile >= kKvFront) {
         if (!loaded) {                                   // query rows as operands
           loaded = had = true;
@@ -318,11 +311,10 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
             f[r][1] = __shfl_sync(0xffffffffu, ff, 8 * t4 + 4);
           }
         }
-        cp_async_wait<2 * kAtStages - 1>();
+        cp_async_wait<1>();
         __syncwarp();
-        unsigned char* st = my_ring + stage * 2 * Sh::kPart;
         unsigned char* kmeta = st + G * kKvTile * 32;
-        const unsigned long long valid = my_valid[stage];
+        const unsigned long long valid = valid_next;
         const bool partial = valid != ~0ull;             // the sequence's end, or a page that is none
         if (partial) {
           clear_meta<G>(kmeta, valid, lane);
@@ -378,11 +370,11 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
               }
         }
         __syncwarp();
-        issue_keys(stage);
+        issue_keys();
         // ---- running maximum; the value scales' power of two ----
         const unsigned char* vst = st + Sh::kPart;
         unsigned char* vmeta = st + Sh::kPart + G * kKvTile * 32;
-        cp_async_wait<2 * kAtStages - 1>();
+        cp_async_wait<1>();
         __syncwarp();
         if (partial) {
           clear_meta<G>(vmeta, valid, lane);
@@ -495,27 +487,26 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
           }
         }
       } else {
-        cp_async_wait<2 * kAtStages - 1>();              // an empty tile: nothing was copied
+        cp_async_wait<1>();              // an empty tile: nothing was copied
         __syncwarp();
-        issue_keys(stage);
+        issue_keys();
       }
       __syncwarp();
-      issue_values(stage);
-      stage = stage == kAtStages - 1 ? 0 : stage + 1;
+      issue_values();
     }
 
     // ---- the warps' results joined; the item's share written ----
-    const int b0 = owner(item_u0), b1 = owner(item_u0 + n_tiles - 1);
+    int b0, b1;
+    list.owners(u0 + item_u0, n_tiles, n_cta, b0, b1);
     const bool whole = b0 == b1;
     float* parts = reinterpret_cast<float*>(c.work + kKvPartOff);
     const size_t part_floats = (size_t)kRows * (D + 2);
     float* my_part = parts + (size_t)(2 * blockIdx.x + (blockIdx.x == b0 ? 1 : 0)) * part_floats;
     const float unit = pow2(min(eref + 24, 127));
     constexpr int kOs = D + 4, kPer = D / 32;            // floats a thread handles of its row
-    const int row_w = warp;                              // joining: warp w takes row w
 
     auto finish = [&](int r, float big, float sum, const float (&v)[kPer]) {
-      const int row = row0 + r * 8 + row_w;
+      const int row = row0 + r;
       if (row < a.m * a.group) {
         const int node = row / a.group, hq = head * a.group + row % a.group;
         if (row >= n_rows) sum = 0.f;                    // behind the sequence's nodes
@@ -535,10 +526,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
 
 #pragma unroll
     for (int r = 0; r < NT; ++r) {
-      // (two buffers in turn: the barrier of the next one is behind every read of this one)
-      float* ob = obuf + buf * (Sh::kObuf / 4);
-      float2* mb = ml + buf * (Sh::kMl / 8);
-      buf ^= 1;
+      if (r) __syncthreads();
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
 #pragma unroll
@@ -547,7 +535,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
 #pragma unroll
           for (int i = 0; i < G; ++i) olo[r][i][e] += __shfl_xor_sync(0xffffffffu, olo[r][i][e], x);
         }
-        float* dst = ob + (warp * 8 + 2 * t4 + e) * kOs + g * 8;
+        float* dst = obuf + (warp * 8 + 2 * t4 + e) * kOs + g * 8;
         if (had)
 #pragma unroll
         for (int i = 0; i < G; ++i) {
@@ -562,61 +550,67 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
           *reinterpret_cast<float4*>(dst + i * kKvGroup) = make_float4(v[0], v[1], v[2], v[3]);
           *reinterpret_cast<float4*>(dst + i * kKvGroup + 4) = make_float4(v[4], v[5], v[6], v[7]);
         }
-        if (g == 0) mb[warp * 8 + 2 * t4 + e] = make_float2(m[r][e], l[r][e]);
+        if (g == 0) ml[warp * 8 + 2 * t4 + e] = make_float2(m[r][e], l[r][e]);
       }
       __syncthreads();
-      if (warp < 8) {
+      for (int rr = warp; rr < 8; rr += kAtWarps) {
+        float2 x[kAtWarps];
         float big = -INFINITY, sum = 0.f, v[kPer];
 #pragma unroll
         for (int e = 0; e < kPer; ++e) v[e] = 0.f;
 #pragma unroll
-        for (int w = 0; w < kAtWarps; ++w) big = fmaxf(big, mb[w * 8 + row_w].x);
+        for (int w = 0; w < kAtWarps; ++w) { x[w] = ml[w * 8 + rr]; big = fmaxf(big, x[w].x); }
 #pragma unroll
         for (int w = 0; w < kAtWarps; ++w) {
-          const float2 x = mb[w * 8 + row_w];
-          const float k = x.x == -INFINITY ? (x.y == 0.f ? 0.f : 1.f) : exp2_approx(x.x - big);
-          sum = fmaf(k, x.y, sum);
-          if (k != 0.f) {
-            float x2[kPer];
-            load_floats<kPer>(ob + (w * 8 + row_w) * kOs + lane * kPer, x2);
+          const float k = x[w].x == -INFINITY ? (x[w].y == 0.f ? 0.f : 1.f) : exp2_approx(x[w].x - big);
+          sum = fmaf(k, x[w].y, sum);
+          if (k != 0.f) {                                // (a warp without tiles left nothing)
+            float y[kPer];
+            load_floats<kPer>(obuf + (w * 8 + rr) * kOs + lane * kPer, y);
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) v[e] = fmaf(k, x2[e], v[e]);
+            for (int e = 0; e < kPer; ++e) v[e] = fmaf(k, y[e], v[e]);
           }
         }
         if (whole) {
-          finish(r, big, sum, v);
+          finish(r * 8 + rr, big, sum, v);
         } else {
-          store_floats<kPer>(my_part + (size_t)(r * 8 + row_w) * D + lane * kPer, v);
+          store_floats<kPer>(my_part + (size_t)(r * 8 + rr) * D + lane * kPer, v);
           if (lane == 0)
-            __stcg(reinterpret_cast<float2*>(my_part + (size_t)kRows * D) + r * 8 + row_w, make_float2(big, sum));
+            __stcg(reinterpret_cast<float2*>(my_part + (size_t)kRows * D) + r * 8 + rr, make_float2(big, sum));
         }
       }
     }
     if (!whole) {
       unsigned* ticket = reinterpret_cast<unsigned*>(c.work + kKvTicketOff) + b0;
-      __threadfence();
       __syncthreads();
       if (tid == 0) {
+        __threadfence();                                 // (after the barrier: for all that the block wrote)
         const unsigned n = atomicAdd(ticket, 1u);
+        __threadfence();
         *flag = n == (unsigned)(b1 - b0);
         if (*flag) *ticket = 0u;                         // for the next call
       }
       __syncthreads();
-      if (*flag && warp < 8) {
-        __threadfence();
+      if (*flag) {
+        auto part_of = [&](int b) { return parts + (size_t)(2 * b + (b == b0 ? 1 : 0)) * part_floats; };
 #pragma unroll 1
-        for (int r = 0; r < NT; ++r) {
+        for (int r = warp; r < kRows; r += kAtWarps) {
           float big = -INFINITY, sum = 0.f, v[kPer];
 #pragma unroll
           for (int e = 0; e < kPer; ++e) v[e] = 0.f;
-          auto part_of = [&](int b) { return parts + (size_t)(2 * b + (b == b0 ? 1 : 0)) * part_floats; };
-          for (int p0 = b0; p0 <= b1; p0 += 32) {
+          constexpr int kBatch = 8;                      // pieces asked for at once
+          for (int p0 = b0; p0 <= b1; p0 += kBatch) {
+            const int n = min(kBatch, b1 - p0 + 1);
             float2 x = make_float2(-INFINITY, 0.f);
-            if (p0 + lane <= b1)
-              x = __ldcg(reinterpret_cast<const float2*>(part_of(p0 + lane) + (size_t)kRows * D) + r * 8 + row_w);
-            float top = fmaxf(x.x, __shfl_xor_sync(0xffffffffu, x.x, 16));
+            if (lane < n) x = __ldcg(reinterpret_cast<const float2*>(part_of(p0 + lane) + (size_t)kRows * D) + r);
+            float y[kBatch][kPer];
 #pragma unroll
-            for (int sft = 8; sft; sft >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, sft));
+            for (int i = 0; i < kBatch; ++i)
+              if (i < n) load_floats_cg<kPer>(part_of(p0 + i) + (size_t)r * D + lane * kPer, y[i]);
+            float top = x.x;
+#pragma unroll
+            for (int sft = kBatch / 2; sft; sft >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, sft));
+            top = __shfl_sync(0xffffffffu, top, 0);
             const float nb = fmaxf(big, top);
             const float down = big == -INFINITY ? (sum == 0.f ? 0.f : 1.f) : exp2_approx(big - nb);
             sum *= down;
@@ -624,22 +618,21 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
             for (int e = 0; e < kPer; ++e) v[e] *= down;
             big = nb;
             const float k = x.x == -INFINITY ? (x.y == 0.f ? 0.f : 1.f) : exp2_approx(x.x - nb);
-            const int n = min(32, b1 - p0 + 1);
-#pragma unroll 8
-            for (int i = 0; i < n; ++i) {
-              const float ki = __shfl_sync(0xffffffffu, k, i);
-              const float li = __shfl_sync(0xffffffffu, x.y, i);
-              sum = fmaf(ki, li, sum);
-              float y[kPer];
-              load_floats_cg<kPer>(part_of(p0 + i) + (size_t)(r * 8 + row_w) * D + lane * kPer, y);
 #pragma unroll
-              for (int e = 0; e < kPer; ++e) v[e] = ki != 0.f ? fmaf(ki, y[e], v[e]) : v[e];
+            for (int i = 0; i < kBatch; ++i) {
+              const float ki = __shfl_sync(0xffffffffu, k, i), li = __shfl_sync(0xffffffffu, x.y, i);
+              if (i < n) {
+                sum = fmaf(ki, li, sum);
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) v[e] = ki != 0.f ? fmaf(ki, y[i][e], v[e]) : v[e];
+              }
             }
           }
           finish(r, big, sum, v);
         }
       }
     }
+    __syncthreads();
     at += piece;
     if (at < u1) list.advance(bc, piece);
   }
@@ -647,7 +640,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
 
 template <int D, int NT, bool kBf16>
 static cudaError_t attend_launch(const KvView& c, const KvAttendArgs& a, int sms, cudaStream_t st) {
-  return launch_pdl(kv_attend_kernel<D, NT, kBf16>, dim3(sms), dim3(Attend<D, NT>::kThreads), Attend<D, NT>::kBytes,
+  return launch_pdl(kv_attend_kernel<D, NT, kBf16>, dim3(Attend<D, NT>::kCtas * sms), dim3(Attend<D, NT>::kThreads), Attend<D, NT>::kBytes,
                     st, c, a);
 }
 template <int D, bool kBf16>
@@ -658,7 +651,7 @@ static cudaError_t attend_rows(const KvView& c, const KvAttendArgs& a, int sms, 
 
 cudaError_t launch_kv_attend(const KvView& c, const KvAttendArgs& a, int head_dim, bool bf16, int sms,
                              cudaStream_t st) {
-  if (sms > kKvMaxCtas) sms = kKvMaxCtas;
+  if (2 * sms > kKvMaxCtas) sms = kKvMaxCtas / 2;
   if (head_dim == 64) return bf16 ? attend_rows<64, true>(c, a, sms, st) : attend_rows<64, false>(c, a, sms, st);
   return bf16 ? attend_rows<128, true>(c, a, sms, st) : attend_rows<128, false>(c, a, sms, st);
 }

@@ -47,7 +47,7 @@ kv_weigh_kernel(const KvView c, const KvWeighArgs a, int row_tiles) {
   int* count_s = len_s + kKvMaxSeq;                                  // [kWgWarps + 1]
   unsigned char* nodes_s = reinterpret_cast<unsigned char*>(count_s + kWgWarps + 1);
 
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, g = lane >> 2, t4 = lane & 3;
   pdl_enter();
 
   TileList list;
@@ -59,16 +59,18 @@ kv_weigh_kernel(const KvView c, const KvWeighArgs a, int row_tiles) {
   list.rows = 0;
   list.build<kWgThreads>(c, a.n_new, a.m, scratch);
   const long long total = list.total;
-  const long long n_cta = min((long long)gridDim.x, (total + kWgWarps - 1) / kWgWarps);
+  const int n_cta = (int)min((long long)gridDim.x, (total + kWgWarps - 1) / kWgWarps);
   if (blockIdx.x >= n_cta) return;
-  const long long u0 = total * blockIdx.x / n_cta, u1 = total * (blockIdx.x + 1) / n_cta;
+  TileCursor bc, pc;                                     // the block's item; the warp's next tile to copy
+  const long long u1_all = list.cut(pc, blockIdx.x + 1, n_cta), u0 = list.cut(bc, blockIdx.x, n_cta);
+  const int u1 = (int)(u1_all - u0);                     // positions from here on count from u0
+  if (u1 <= 0) return;
 
   unsigned char* my_ring = ring + warp * (kWgStages * Sh::kStage);
   unsigned long long* my_valid = valid_s + warp * kWgStages;
-  TileCursor pc;
-  long long pu = u0 + warp;
-  int ahead = -1;
-  if (pu < u1) { list.seek(pc, pu); ahead = tile_pages(c, pc, lane); }
+  int pu = warp, ahead = -1;
+  pc = bc;
+  if (pu < u1) { list.advance(pc, warp); ahead = tile_pages(c, pc, lane); }
   auto issue = [&](int stage) {
     if (pu < u1) {
       if (pc.cached()) {
@@ -85,13 +87,10 @@ kv_weigh_kernel(const KvView c, const KvWeighArgs a, int row_tiles) {
   for (int i = 0; i < kWgStages; ++i) issue(i);
   int stage = 0;
 
-  TileCursor bc;
-  list.seek(bc, u0);
-  long long mu = u0 + warp;
-  for (long long at = u0; at < u1;) {
+  int mu = warp;
+  for (int at = 0; at < u1;) {
     const int head = bc.item, s = bc.s;
-    const int piece = (int)min((long long)(bc.tiles - bc.tile), u1 - at);
-    const long long item_u0 = at - bc.tile;
+    const int piece = min(bc.tiles - bc.tile, u1 - at), item_u0 = at - bc.tile;
 
     // ---- the rows that take part, in order ----
     const int first = a.node0 * a.group, last = min(a.node1, bc.nodes) * a.group;
@@ -139,14 +138,14 @@ kv_weigh_kernel(const KvView c, const KvWeighArgs a, int row_tiles) {
     __syncthreads();
 
     for (; mu < at + piece; mu += kWgWarps) {
-      const int tile = (int)(mu - item_u0), slot0 = (tile - kKvFront) * kKvTile;
+      const int tile = mu - item_u0, slot0 = (tile - kKvFront) * kKvTile;
       cp_async_wait<kWgStages - 1>();
       __syncwarp();
       if (tile >= kKvFront) {
         unsigned char* st = my_ring + stage * Sh::kStage;
         unsigned char* kmeta = st + G * kKvTile * 32;
         const unsigned long long valid = my_valid[stage];
-        if (valid != ~0ull) {
+        if (__any_sync(0xffffffffu, valid != ~0ull)) {
           clear_meta<G>(kmeta, valid, lane);
           __syncwarp();
         }
@@ -312,7 +311,7 @@ static cudaError_t weigh_launch(const KvView& c, KvWeighArgs a, int sms, cudaStr
     a.node0 = n;
     a.node1 = n + per < a.m ? n + per : a.m;
     const int row_tiles = ((a.node1 - a.node0) * a.group + 7) / 8;
-    const cudaError_t e = launch_pdl(kv_weigh_kernel<D, kBf16>, dim3(2 * sms < kKvMaxCtas ? 2 * sms : kKvMaxCtas),
+    const cudaError_t e = launch_pdl(kv_weigh_kernel<D, kBf16>, dim3(2 * sms),
                                      dim3(kWgThreads), WeighShared<D>::bytes(row_tiles), st, c, a, row_tiles);
     if (e != cudaSuccess) return e;
   }
