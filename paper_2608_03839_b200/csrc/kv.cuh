@@ -306,7 +306,9 @@ struct TileList {
   // The list is cut at raw(b) = total b / n_cta, but not where that would leave a piece of
   // hardly more than an item's first round, or the last few tiles of one: such a cut moves to the item's
   // edge.  (Every block finds the same cuts.)
-  static constexpr int kNearStart = kKvFront + 4, kNearEnd = 4;
+  // (Where blocks get little, more so: an item's few tiles are better left together.)
+  __device__ __forceinline__ int near_end(int n_cta) const { return total < 64LL * n_cta ? 4 : 1; }
+  __device__ __forceinline__ int near_start(int n_cta) const { return kKvFront + near_end(n_cta); }
   __device__ __forceinline__ long long cut(TileCursor& k, int b, int n_cta) const {
     // (32-bit division wherever the numbers allow: the 64-bit one is a long routine)
     const long long u = total * n_cta <= 0xffffffffLL ? (long long)((uint32_t)total * (uint32_t)b / (uint32_t)n_cta)
@@ -314,17 +316,17 @@ struct TileList {
     if (u >= total) return total;
     seek(k, u);
     const int tiles = k.item < k.live ? k.tiles : 1;
-    if (k.tile <= kNearStart) { const long long at = u - k.tile; k.tile = 0; return at; }
-    if (tiles - k.tile > kNearEnd) return u;
+    if (k.tile <= near_start(n_cta)) { const long long at = u - k.tile; k.tile = 0; return at; }
+    if (tiles - k.tile > near_end(n_cta)) return u;
     const int on = tiles - k.tile;
     if (u + on < total) advance(k, on);
     return u + on;
   }
   // Blocks that share the item [i0, i0 + tiles): b0..b1.
   __device__ __forceinline__ void owners(long long i0, int tiles, int n_cta, int& b0, int& b1) const {
-    const long long lo = i0 + kNearStart + 1, hi = i0 + tiles - kNearEnd;
+    const long long lo = i0 + near_start(n_cta) + 1, hi = i0 + tiles - near_end(n_cta);
     // in front of the first cut behind the start; the last cut before the end
-    if ((total + kNearStart + 2) * (n_cta + 1) <= 0xffffffffLL) {
+    if ((total + 64) * (n_cta + 1) <= 0xffffffffLL) {
       const uint32_t t = (uint32_t)total, n = (uint32_t)n_cta;
       b0 = (int)(((uint32_t)lo * n + t - 1) / t) - 1;
       b1 = (int)(((uint32_t)hi * n + t - 1) / t) - 1;

@@ -39,8 +39,9 @@ struct Attend {
   static constexpr int kObuf = kWarps * 8 * (D + 4) * 4;
   static constexpr int kMl = kWarps * 8 * 8;
   static constexpr int kCum = (kKvMaxSeq + 1) * 8;
-  static constexpr int kBytes = kRing + kObuf + kMl + kCum + kWarps * 8 + kKvMaxSeq * 5 + 16;
+  static constexpr int kBytes = kRing + kObuf + kMl + kCum + kWarps * 8 + kKvMaxSeq * 5 + 64;
 };
+struct OpenItem { int b0, b1, s, head, row0, n_rows; };  // an item whose pieces are all there
 
 template <int N> __device__ __forceinline__ void load_floats(const float* p, float (&v)[N]) {
   if (N == 4) { const float4 x = *reinterpret_cast<const float4*>(p); v[0] = x.x; v[1] = x.y; v[N - 2] = x.z; v[N - 1] = x.w; }
@@ -69,10 +70,12 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
   long long* scratch = cum + kKvMaxSeq + 1;
   int* len_s = reinterpret_cast<int*>(scratch + kAtWarps);
   unsigned char* nodes_s = reinterpret_cast<unsigned char*>(len_s + kKvMaxSeq);
-  int* flag = reinterpret_cast<int*>(nodes_s + kKvMaxSeq);
+  int* n_open = reinterpret_cast<int*>(nodes_s + kKvMaxSeq);
+  OpenItem* open = reinterpret_cast<OpenItem*>(n_open + 1);
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, g = lane >> 2, t4 = lane & 3;
   const int rblocks = (a.m * a.group + kRows - 1) / kRows;
+  if (tid == 0) *n_open = 0;                             // (barriers follow)
   pdl_enter();
 
   TileList list;
@@ -115,6 +118,26 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
   };
   issue_keys();
   issue_values();
+
+  constexpr int kOs = D + 4, kPer = D / 32;              // floats a lane handles of a row in a join
+  constexpr size_t kPartFloats = (size_t)kRows * (D + 2);
+  float* parts = reinterpret_cast<float*>(c.work + kKvPartOff);
+  // row `row` of (s, head) is complete: v relative to 2^big, with the sum of its weights
+  auto finish = [&](int s, int head, int row, int n_rows, float big, float sum, const float (&v)[kPer]) {
+    if (row >= a.m * a.group) return;
+    const int node = row / a.group, hq = head * a.group + row % a.group;
+    if (row >= n_rows) sum = 0.f;                        // behind the sequence's nodes
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    uint16_t* op = a.out + s * a.out_seq + node * a.out_row + hq * a.out_head + lane * kPer;
+    uint32_t w[kPer / 2];
+#pragma unroll
+    for (int e = 0; e < kPer / 2; ++e) w[e] = sum == 0.f ? 0u : pack16<kBf16>(v[2 * e] * inv, v[2 * e + 1] * inv);
+    if (kPer == 4) *reinterpret_cast<uint2*>(op) = make_uint2(w[0], w[kPer / 2 - 1]);
+    else *reinterpret_cast<uint32_t*>(op) = w[0];
+    if (a.lse && lane == 0)
+      a.lse[s * a.lse_seq + node * a.lse_row + hq * a.lse_head] =
+          sum == 0.f ? -INFINITY : (big + log2f(sum)) * 0.6931471805599453f;
+  };
 
   // ---- item by item ----
   int mu = warp;                                         // the warp's next tile to compute
@@ -324,38 +347,53 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
         // ---- scores ----
         float sc[NT][4][4];
 #pragma unroll
-        for (int ch = 0; ch < 4; ++ch) {
-          const int sl = ch * 16 + slot_g;
-          uint32_t km[2][G];
-          load_meta<G>(kmeta + sl * 4 * G, km[0]);
-          load_meta<G>(kmeta + (sl + 8) * 4 * G, km[1]);
+        for (int c0 = 0; c0 < 4; c0 += 4) {       // independent sums side by side
+          uint2 w[4][2][G];
+          float acc[4][G][NT][4];
 #pragma unroll
-          for (int i = 0; i < G; ++i) {
-            const uint2 w0 = *reinterpret_cast<const uint2*>(st + (i * kKvTile + sl) * 32 + t4 * 8);
-            const uint2 w1 = *reinterpret_cast<const uint2*>(st + (i * kKvTile + sl + 8) * 32 + t4 * 8);
-            float acc[NT][4];
+          for (int ch = 0; ch < 4; ++ch)
 #pragma unroll
-            for (int r = 0; r < NT; ++r)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) acc[r][e] = 0.f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint32_t x0 = (j & 2 ? w0.y : w0.x) >> (8 * (j & 1));
-              const uint32_t x1 = (j & 2 ? w1.y : w1.x) >> (8 * (j & 1));
+            for (int i = 0; i < G; ++i) {
+              const int sl = (c0 + ch) * 16 + slot_g;
+              w[ch][0][i] = *reinterpret_cast<const uint2*>(st + (i * kKvTile + sl) * 32 + t4 * 8);
+              w[ch][1][i] = *reinterpret_cast<const uint2*>(st + (i * kKvTile + sl + 8) * 32 + t4 * 8);
 #pragma unroll
               for (int r = 0; r < NT; ++r)
-                mma16816<false>(acc[r], x0 & 0x000f000fu, x1 & 0x000f000fu, x0 & 0x00f000f0u,
-                                x1 & 0x00f000f0u, qf[r][i * 4 + j][0], qf[r][i * 4 + j][1]);
-            }
-            const float s0 = half_lo<kBf16>(km[0][i]), l0 = half_hi<kBf16>(km[0][i]);
-            const float s1 = half_lo<kBf16>(km[1][i]), l1 = half_hi<kBf16>(km[1][i]);
 #pragma unroll
-            for (int r = 0; r < NT; ++r) {
-              float (&x)[4] = sc[r][ch];
-              x[0] = fmaf(s0, acc[r][0], i ? fmaf(l0, qsum[r][i][0], x[0]) : l0 * qsum[r][i][0]);
-              x[1] = fmaf(s0, acc[r][1], i ? fmaf(l0, qsum[r][i][1], x[1]) : l0 * qsum[r][i][1]);
-              x[2] = fmaf(s1, acc[r][2], i ? fmaf(l1, qsum[r][i][0], x[2]) : l1 * qsum[r][i][0]);
-              x[3] = fmaf(s1, acc[r][3], i ? fmaf(l1, qsum[r][i][1], x[3]) : l1 * qsum[r][i][1]);
+                for (int e = 0; e < 4; ++e) acc[ch][i][r][e] = 0.f;
+            }
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int ch = 0; ch < 4; ++ch)
+#pragma unroll
+              for (int i = 0; i < G; ++i) {
+                const uint32_t x0 = (j & 2 ? w[ch][0][i].y : w[ch][0][i].x) >> (8 * (j & 1));
+                const uint32_t x1 = (j & 2 ? w[ch][1][i].y : w[ch][1][i].x) >> (8 * (j & 1));
+#pragma unroll
+                for (int r = 0; r < NT; ++r)
+                  mma16816<false>(acc[ch][i][r], x0 & 0x000f000fu, x1 & 0x000f000fu, x0 & 0x00f000f0u,
+                                  x1 & 0x00f000f0u, qf[r][i * 4 + j][0], qf[r][i * 4 + j][1]);
+              }
+#pragma unroll
+          for (int ch = 0; ch < 4; ++ch) {
+            const int sl = (c0 + ch) * 16 + slot_g;
+            uint32_t km[2][G];
+            load_meta<G>(kmeta + sl * 4 * G, km[0]);
+            load_meta<G>(kmeta + (sl + 8) * 4 * G, km[1]);
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+              const float s0 = half_lo<kBf16>(km[0][i]), l0 = half_hi<kBf16>(km[0][i]);
+              const float s1 = half_lo<kBf16>(km[1][i]), l1 = half_hi<kBf16>(km[1][i]);
+#pragma unroll
+              for (int r = 0; r < NT; ++r) {
+                float (&x)[4] = sc[r][c0 + ch];
+                const float (&y)[4] = acc[ch][i][r];
+                x[0] = fmaf(s0, y[0], i ? fmaf(l0, qsum[r][i][0], x[0]) : l0 * qsum[r][i][0]);
+                x[1] = fmaf(s0, y[1], i ? fmaf(l0, qsum[r][i][1], x[1]) : l0 * qsum[r][i][1]);
+                x[2] = fmaf(s1, y[2], i ? fmaf(l1, qsum[r][i][0], x[2]) : l1 * qsum[r][i][0]);
+                x[3] = fmaf(s1, y[3], i ? fmaf(l1, qsum[r][i][1], x[3]) : l1 * qsum[r][i][1]);
+              }
             }
           }
         }
@@ -499,30 +537,8 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
     int b0, b1;
     list.owners(u0 + item_u0, n_tiles, n_cta, b0, b1);
     const bool whole = b0 == b1;
-    float* parts = reinterpret_cast<float*>(c.work + kKvPartOff);
-    const size_t part_floats = (size_t)kRows * (D + 2);
-    float* my_part = parts + (size_t)(2 * blockIdx.x + (blockIdx.x == b0 ? 1 : 0)) * part_floats;
+    float* my_part = parts + (size_t)(2 * blockIdx.x + (blockIdx.x == b0 ? 1 : 0)) * kPartFloats;
     const float unit = pow2(min(eref + 24, 127));
-    constexpr int kOs = D + 4, kPer = D / 32;            // floats a thread handles of its row
-
-    auto finish = [&](int r, float big, float sum, const float (&v)[kPer]) {
-      const int row = row0 + r;
-      if (row < a.m * a.group) {
-        const int node = row / a.group, hq = head * a.group + row % a.group;
-        if (row >= n_rows) sum = 0.f;                    // behind the sequence's nodes
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        uint16_t* op = a.out + s * a.out_seq + node * a.out_row + hq * a.out_head + lane * kPer;
-        uint32_t w[kPer / 2];
-#pragma unroll
-        for (int e = 0; e < kPer / 2; ++e)
-          w[e] = sum == 0.f ? 0u : pack16<kBf16>(v[2 * e] * inv, v[2 * e + 1] * inv);
-        if (kPer == 4) *reinterpret_cast<uint2*>(op) = make_uint2(w[0], w[kPer / 2 - 1]);
-        else *reinterpret_cast<uint32_t*>(op) = w[0];
-        if (a.lse && lane == 0)
-          a.lse[s * a.lse_seq + node * a.lse_row + hq * a.lse_head] =
-              sum == 0.f ? -INFINITY : (big + log2f(sum)) * 0.6931471805599453f;
-      }
-    };
 
 #pragma unroll
     for (int r = 0; r < NT; ++r) {
@@ -572,7 +588,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
           }
         }
         if (whole) {
-          finish(r * 8 + rr, big, sum, v);
+          finish(s, head, row0 + r * 8 + rr, n_rows, big, sum, v);
         } else {
           store_floats<kPer>(my_part + (size_t)(r * 8 + rr) * D + lane * kPer, v);
           if (lane == 0)
@@ -580,61 +596,62 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
         }
       }
     }
-    if (!whole) {
+    __syncthreads();
+    if (!whole && tid == 0) {                            // the block that brings the last piece joins them
       unsigned* ticket = reinterpret_cast<unsigned*>(c.work + kKvTicketOff) + b0;
-      __syncthreads();
-      if (tid == 0) {
-        __threadfence();                                 // (after the barrier: for all that the block wrote)
-        const unsigned n = atomicAdd(ticket, 1u);
-        __threadfence();
-        *flag = n == (unsigned)(b1 - b0);
-        if (*flag) *ticket = 0u;                         // for the next call
-      }
-      __syncthreads();
-      if (*flag) {
-        auto part_of = [&](int b) { return parts + (size_t)(2 * b + (b == b0 ? 1 : 0)) * part_floats; };
-#pragma unroll 1
-        for (int r = warp; r < kRows; r += kAtWarps) {
-          float big = -INFINITY, sum = 0.f, v[kPer];
-#pragma unroll
-          for (int e = 0; e < kPer; ++e) v[e] = 0.f;
-          constexpr int kBatch = 8;                      // pieces asked for at once
-          for (int p0 = b0; p0 <= b1; p0 += kBatch) {
-            const int n = min(kBatch, b1 - p0 + 1);
-            float2 x = make_float2(-INFINITY, 0.f);
-            if (lane < n) x = __ldcg(reinterpret_cast<const float2*>(part_of(p0 + lane) + (size_t)kRows * D) + r);
-            float y[kBatch][kPer];
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i)
-              if (i < n) load_floats_cg<kPer>(part_of(p0 + i) + (size_t)r * D + lane * kPer, y[i]);
-            float top = x.x;
-#pragma unroll
-            for (int sft = kBatch / 2; sft; sft >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, sft));
-            top = __shfl_sync(0xffffffffu, top, 0);
-            const float nb = fmaxf(big, top);
-            const float down = big == -INFINITY ? (sum == 0.f ? 0.f : 1.f) : exp2_approx(big - nb);
-            sum *= down;
-#pragma unroll
-            for (int e = 0; e < kPer; ++e) v[e] *= down;
-            big = nb;
-            const float k = x.x == -INFINITY ? (x.y == 0.f ? 0.f : 1.f) : exp2_approx(x.x - nb);
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-              const float ki = __shfl_sync(0xffffffffu, k, i), li = __shfl_sync(0xffffffffu, x.y, i);
-              if (i < n) {
-                sum = fmaf(ki, li, sum);
-#pragma unroll
-                for (int e = 0; e < kPer; ++e) v[e] = ki != 0.f ? fmaf(ki, y[i][e], v[e]) : v[e];
-              }
-            }
-          }
-          finish(r, big, sum, v);
-        }
+      __threadfence();                                   // (after the barrier: for all that the block wrote)
+      const unsigned n = atomicAdd(ticket, 1u);
+      __threadfence();
+      if (n == (unsigned)(b1 - b0)) {
+        *ticket = 0u;                                    // for the next call
+        open[*n_open] = OpenItem{b0, b1, s, head, row0, n_rows};
+        ++*n_open;                                       // its first and its last item, at most
       }
     }
-    __syncthreads();
     at += piece;
     if (at < u1) list.advance(bc, piece);
+  }
+
+  // ---- items whose last piece came from here: the pieces joined, in their order ----
+  __syncthreads();
+  for (int q = 0; q < *n_open; ++q) {
+    const OpenItem it = open[q];
+    auto part_of = [&](int b) { return parts + (size_t)(2 * b + (b == it.b0 ? 1 : 0)) * kPartFloats; };
+    for (int r = warp; r < kRows; r += kAtWarps) {
+      float big = -INFINITY, sum = 0.f, v[kPer];
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) v[e] = 0.f;
+      constexpr int kBatch = 20;                         // pieces asked for at once
+      for (int p0 = it.b0; p0 <= it.b1; p0 += kBatch) {
+        const int n = min(kBatch, it.b1 - p0 + 1);
+        float2 x = make_float2(-INFINITY, 0.f);
+        if (lane < n) x = __ldcg(reinterpret_cast<const float2*>(part_of(p0 + lane) + (size_t)kRows * D) + r);
+        float y[kBatch][kPer];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+          if (i < n) load_floats_cg<kPer>(part_of(p0 + i) + (size_t)r * D + lane * kPer, y[i]);
+        float top = x.x;
+#pragma unroll
+        for (int sft = 16; sft; sft >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, sft));
+        const float nb = fmaxf(big, top);
+        const float down = big == -INFINITY ? (sum == 0.f ? 0.f : 1.f) : exp2_approx(big - nb);
+        sum *= down;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) v[e] *= down;
+        big = nb;
+        const float k = x.x == -INFINITY ? (x.y == 0.f ? 0.f : 1.f) : exp2_approx(x.x - nb);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const float ki = __shfl_sync(0xffffffffu, k, i), li = __shfl_sync(0xffffffffu, x.y, i);
+          if (i < n) {
+            sum = fmaf(ki, li, sum);
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) v[e] = ki != 0.f ? fmaf(ki, y[i][e], v[e]) : v[e];
+          }
+        }
+      }
+      finish(it.s, it.head, it.row0 + r, it.n_rows, big, sum, v);
+    }
   }
 }
 
