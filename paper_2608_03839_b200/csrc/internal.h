@@ -74,6 +74,7 @@ cudaError_t preload_index_kernels();
 cudaError_t preload_kv_attend_kernels();
 cudaError_t preload_kv_evict_kernels();
 cudaError_t preload_kv_store_kernels();
+cudaError_t preload_kv_tree_kernels();
 cudaError_t preload_kv_weigh_kernels();
 cudaError_t preload_merge_kernels();
 cudaError_t preload_merge_tree_kernels();

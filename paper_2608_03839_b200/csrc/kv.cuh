@@ -45,7 +45,8 @@ struct KvWork {
 };
 constexpr size_t kKvTicketOff = 256;                                  // unsigned [kKvMaxCtas]
 constexpr size_t kKvPartOff = kKvTicketOff + 4 * kKvMaxCtas;          // partial results
-constexpr int kKvPartRows = 2 * kKvMaxCtas * 16;                      // rows of D + 2 floats
+constexpr int kKvTreeMaxCtas = 160;                                   // of the kernel for many rows
+constexpr int kKvPartRows = 2 * kKvTreeMaxCtas * 256;                       // rows of D + 2 floats
 
 struct KvView {
   unsigned char* pages;      // [n_pages, n_kv, block]
@@ -115,6 +116,7 @@ struct KvAttendArgs {
 cudaError_t launch_kv_append(const KvView& c, const KvAppendArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st);
 cudaError_t launch_kv_read(const KvView& c, const KvReadArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st);
 cudaError_t launch_kv_attend(const KvView& c, const KvAttendArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st);
+cudaError_t launch_kv_tree(const KvView& c, const KvAttendArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st);
 cudaError_t launch_kv_weigh(const KvView& c, const KvWeighArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st);
 cudaError_t launch_kv_evict(const KvView& c, KvEvictArgs a, int head_dim, cudaStream_t st);
 
@@ -211,25 +213,24 @@ __device__ __forceinline__ long long block_exclusive_scan(long long v, long long
 }
 
 // ---- tiles ----
-// The slots of all (sequence, key head, row block) items, 64 to a tile, are one list: sequence
-// by sequence, its items in turn, its tiles in turn.  An item begins with a round of kKvFront
-// tiles, one for each warp of a block: the new nodes (32 each) in the first of them, nothing in
-// the others.  Nodes come first because their loads depend on nothing, and the round stands for
-// what an item costs besides its slots (operands, joining), so that a block that gets many
-// short items gets fewer slots.  Items whose rows do not exist have one empty tile.
-constexpr int kKvTile = 64, kKvNodeTile = 32, kKvFront = 8;
+// The slots of all (sequence, key head, row block) items, kTile to a tile, are one list: sequence
+// by sequence, its items in turn, its tiles in turn.  An item begins with kFront tiles: the new
+// nodes in the first of them, nothing in the others.  Nodes come first because their loads
+// depend on nothing, and the front stands for what an item costs besides its slots (operands,
+// joining), so that a block that gets many short items gets fewer slots.  Items whose rows do
+// not exist have one empty tile.
+template <int kTile, int kFront>
+struct TileListOf {
+  struct Cursor {
+    int s;                // sequence
+    int len, nodes;       // its slots and new nodes
+    int tiles;            // tiles of each of its items that have rows ...
+    int live;             // ... and how many items those are
+    int item, head, tile; // head: item modulo the key heads
+    __device__ __forceinline__ int slot0() const { return (tile - kFront) * kTile; }
+    __device__ __forceinline__ bool cached() const { return item < live && tile >= kFront; }
+  };
 
-struct TileCursor {
-  int s;                // sequence
-  int len, nodes;       // its slots and new nodes
-  int tiles;            // tiles of each of its items that have rows ...
-  int live;             // ... and how many items those are
-  int item, head, tile; // head: item modulo the key heads
-  __device__ __forceinline__ int slot0() const { return (tile - kKvFront) * kKvTile; }
-  __device__ __forceinline__ bool cached() const { return item < live && tile >= kKvFront; }
-};
-
-struct TileList {
   long long* cum;       // shared memory: [n_seq + 1] tiles in front of each sequence
   int* len;             // [n_seq], within the table's room
   unsigned char* nodes; // [n_seq], 0..m
@@ -240,7 +241,7 @@ struct TileList {
   __device__ __forceinline__ int live_items(int n) const {
     return rows == 0 ? items : n_kv * ((n * group + rows - 1) / rows);
   }
-  __device__ __forceinline__ int tiles_of(int l) const { return (l + kKvTile - 1) / kKvTile + kKvFront; }
+  __device__ __forceinline__ int tiles_of(int l) const { return (l + kTile - 1) / kTile + kFront; }
   __device__ __forceinline__ long long tiles_in(int l, int n) const {
     const int live = live_items(n);
     return (long long)live * tiles_of(l) + (items - live);
@@ -276,14 +277,14 @@ struct TileList {
   }
   // Cursors are the same in every lane; the shuffles say so, which moves their arithmetic out of
   // the lanes' registers.
-  __device__ __forceinline__ void load(TileCursor& k, int s) const {
+  __device__ __forceinline__ void load(Cursor& k, int s) const {
     k.s = s;
     k.len = __shfl_sync(0xffffffffu, len[s], 0);
     k.nodes = __shfl_sync(0xffffffffu, (int)nodes[s], 0);
     k.tiles = tiles_of(k.len);
     k.live = live_items(k.nodes);
   }
-  __device__ __forceinline__ void seek(TileCursor& k, long long u) const {   // to list position u
+  __device__ __forceinline__ void seek(Cursor& k, long long u) const {   // to list position u
     int lo = 0, hi = n_seq - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -307,9 +308,9 @@ struct TileList {
   // hardly more than an item's first round, or the last few tiles of one: such a cut moves to the item's
   // edge.  (Every block finds the same cuts.)
   // (Where blocks get little, more so: an item's few tiles are better left together.)
-  __device__ __forceinline__ int near_end(int n_cta) const { return total < 64LL * n_cta ? 4 : 1; }
-  __device__ __forceinline__ int near_start(int n_cta) const { return kKvFront + near_end(n_cta); }
-  __device__ __forceinline__ long long cut(TileCursor& k, int b, int n_cta) const {
+  __device__ __forceinline__ int near_end(int n_cta) const { return total < (long long)kFront * kFront * n_cta ? 4 : 1; }
+  __device__ __forceinline__ int near_start(int n_cta) const { return kFront + near_end(n_cta); }
+  __device__ __forceinline__ long long cut(Cursor& k, int b, int n_cta) const {
     // (32-bit division wherever the numbers allow: the 64-bit one is a long routine)
     const long long u = total * n_cta <= 0xffffffffLL ? (long long)((uint32_t)total * (uint32_t)b / (uint32_t)n_cta)
                                                       : total * b / n_cta;
@@ -336,7 +337,7 @@ struct TileList {
     }
     if (b1 < b0) b1 = b0;
   }
-  __device__ __forceinline__ void advance(TileCursor& k, int n) const {      // n tiles on, inside the list
+  __device__ __forceinline__ void advance(Cursor& k, int n) const {      // n tiles on, inside the list
     for (k.tile += n;;) {
       const int here = k.item < k.live ? k.tiles : 1;
       if (k.tile < here) return;
@@ -346,6 +347,10 @@ struct TileList {
     }
   }
 };
+
+constexpr int kKvTile = 64, kKvNodeTile = 32, kKvFront = 8;
+using TileList = TileListOf<kKvTile, kKvFront>;
+using TileCursor = TileList::Cursor;
 
 // The pages that hold a tile's quarters of 16 slots, lane q the q-th's; -1 where the table names
 // none or the quarter has no slot.

@@ -31,6 +31,7 @@ namespace oilbird {
 // own: the next tile's keys are asked for as soon as the scores are taken, its values after the
 // products with them, so that a single buffer of each keeps half a tile per warp in flight.
 // Eight rows leave registers for twelve warps an SM.
+constexpr int kFewRows = 16;                             // more go to kv_tree.cu
 template <int D, int NT>
 struct Attend {
   static constexpr int kWarps = NT == 1 ? 6 : 4, kThreads = 32 * kWarps, kCtas = 2;
@@ -252,6 +253,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
         // these products need no units: eref = 0 after them, where no finite value overflows;
         // the first cached tile chooses anew
         eref = 0;
+        bool odd = false;
 #pragma unroll
         for (int ch = 0; ch < 2; ++ch) {
           if (ch && !both) break;
@@ -281,6 +283,13 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
             for (int i = 0; i < G; ++i) {
               w[i][k] = make_uint4(0, 0, 0, 0);
               if (node < bc.nodes) w[i][k] = *reinterpret_cast<const uint4*>(vp + i * kKvGroup);
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {              // infinities and NaN: see below
+                uint32_t& v = (&w[i][k].x)[x];
+                constexpr uint32_t kInf = kBf16 ? 0x7f80u : 0x7c00u;
+                if ((v & kInf) == kInf) { odd = true; v &= 0xffff0000u; }
+                if ((v >> 16 & kInf) == kInf) { odd = true; v &= 0x0000ffffu; }
+              }
             }
           }
 #pragma unroll
@@ -295,6 +304,32 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
                 mma16816<kBf16>(o[r][i * 4 + n], ea, oa, eb, ob, hi[r][0], hi[r][1]);
                 mma16816<kBf16>(o[r][i * 4 + n], ea, oa, eb, ob, lo[r][0], lo[r][1]);
               }
+            }
+        }
+        if (__any_sync(0xffffffffu, odd)) {
+          // values that are not finite stayed out of the products (0 times a hidden node's
+          // would have reached every row): they are added to the rows that see them
+#pragma unroll
+          for (int r = 0; r < NT; ++r)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int row = row0 + r * 8 + 2 * t4 + e;
+              if (row >= n_rows) continue;
+              const int node = row / a.group;
+              const unsigned long long sees = a.mask ? a.mask[s * a.mask_stride + node] : (2ull << node) - 1ull;
+              for (int j = node0; j < min(node0 + kKvNodeTile, bc.nodes); ++j)
+                if (sees >> j & 1ull) {
+                  const uint16_t* vp = a.v.at(s, j, head) + g * 8;
+#pragma unroll
+                  for (int i = 0; i < G; ++i)
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) {
+                      const uint32_t w = *reinterpret_cast<const uint32_t*>(vp + i * kKvGroup + 2 * n);
+                      const float v0 = half_lo<kBf16>(w), v1 = half_hi<kBf16>(w);
+                      if (!(fabsf(v0) < INFINITY)) o[r][i * 4 + n][e] += v0;
+                      if (!(fabsf(v1) < INFINITY)) o[r][i * 4 + n][e + 2] += v1;
+                    }
+                }
             }
         }
         // (the cached codes of odd pairs carry 16 times their value)
@@ -663,7 +698,8 @@ static cudaError_t attend_launch(const KvView& c, const KvAttendArgs& a, int sms
 template <int D, bool kBf16>
 static cudaError_t attend_rows(const KvView& c, const KvAttendArgs& a, int sms, cudaStream_t st) {
   if (a.m * a.group <= 8) return attend_launch<D, 1, kBf16>(c, a, sms, st);
-  return attend_launch<D, 2, kBf16>(c, a, sms, st);
+  if (a.m * a.group <= kFewRows) return attend_launch<D, 2, kBf16>(c, a, sms, st);
+  return launch_kv_tree(c, a, D, kBf16, sms, st);
 }
 
 cudaError_t launch_kv_attend(const KvView& c, const KvAttendArgs& a, int head_dim, bool bf16, int sms,

@@ -1,0 +1,905 @@
+// Attention over the 4-bit cache for many query rows per key/value head (whole draft trees,
+// prompt chunks): tensor cores with accumulators in TMEM.
+//
+// The formulas are those of kv_attend.cu.  With 128 or 256 rows on a tile of 128 slots the
+// products decide (4 D flops for each row and slot), so keys and values are turned into f16 once per tile
+// and every row of the block uses them.  One block an SM:
+//   warps 0-3, 4-7   softmax: one row per thread.  Two groups of 128 rows A and B, or, where the
+//                    block has 128 rows or fewer, the same rows twice: A takes the even tiles
+//                    and B the odd ones, each with sums of its own.
+//   warps 8-15       decode: codes, scales and offsets from global memory, a tile ahead in
+//                    registers, to f16 in the 128-byte-swizzled layout the products read
+//   warp 16          issues the products: S = Q K^T (A and Q from shared memory) and O += P V
+//                    (P from TMEM, where the softmax warps put it over the scores)
+// While A's scores go through the exponentials the tensor core works on B's tile and the other
+// way round.  Keys are the product's N operand as they lie (channels contiguous), values the N operand with
+// channels contiguous as well (transposed operand), so both have the same layout and neither
+// is transposed by hand.
+//
+// Numbers.  A decoded element is rounded to f16 once (scale * code + lo as one fused
+// multiply-add, 2^-11 of it).  Rows are multiplied by a power of two that brings their largest
+// element to [1, 2); a tile's keys and values likewise by 2^-Ek and 2^-Ev (below 1).  Ek joins the row's factor,
+// Ev the exponent: p = exp2(s + Ev - m) with m the running maximum of s + Ev, so that
+// O = sum p (2^-Ev v) and l = sum 2^-Ev p carry no unit of their own and m alone keeps every
+// operand in range.  m is brought up to date only when a row passes it by 2^8 (the
+// accumulators are rescaled in TMEM then, once a row's maximum has settled never again).
+//
+// Work.  The list of tiles of kv.cuh with 128 slots a tile, one run per block.  An item that a
+// block has to itself is written out by it; the pieces of the others go to the workspace (sums,
+// maxima, fp32 accumulators, rows contiguous so that both sides are coalesced) and a second
+// kernel joins them in their order: with 256 rows a piece is 133 KB, which all SMs together
+// read back in microseconds and one block would not.
+// Every wait is bounded (two seconds): a wait that runs out raises the workspace's flag, all roles
+// leave, TMEM is freed.
+#include "kv.cuh"
+
+namespace oilbird {
+
+namespace {
+
+constexpr int kTrTile = 128, kTrFront = 4;               // slots a tile; see TileListOf
+constexpr int kTrSoftThreads = 256, kTrDecWarps = 8, kTrThreads = kTrSoftThreads + 32 * kTrDecWarps + 32;
+using TreeList = TileListOf<kTrTile, kTrFront>;
+constexpr float kTrLn2 = 0.6931471805599453f;
+
+// ------------------------------------------------------------------ PTX wrappers ---
+__device__ __forceinline__ void bar_init(uint64_t* b, uint32_t n) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(kv_smem(b)), "r"(n));
+}
+__device__ __forceinline__ void bar_arrive(uint64_t* b) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(kv_smem(b)) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(kv_smem(b)), "r"(parity) : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ unsigned long long now_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  return t;
+}
+// Bounded wait; false if it gave up or another role did.
+__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* gave_up, DeviceStats* stats) {
+  if (bar_try(b, parity)) return true;
+  const unsigned long long t0 = now_ns(), limit = wait_limit_ns(stats);
+  for (uint32_t spin = 0;; ++spin) {
+    if (bar_try(b, parity)) return true;
+    if ((spin & 63u) == 63u) {
+      if (*gave_up) return false;
+      if (now_ns() - t0 > limit) {
+        *gave_up = 1;
+        atomicExch(&stats->stalled, 1);
+        return false;
+      }
+    }
+  }
+}
+// the same by a converged warp, one outcome for all lanes
+__device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, volatile int* gave_up, DeviceStats* stats) {
+  return __all_sync(0xffffffffu, bar_wait(b, parity, gave_up, stats));
+}
+__device__ __forceinline__ bool one_lane() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void commit(uint64_t* b) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(kv_smem(b)) : "memory");
+}
+// D[tmem] (+)= A[smem] B[smem], f16 operands, fp32 accumulators, M = 128, K = 16
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+// the same with A from TMEM (two elements a column)
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&v)[32]) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+      ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Matrix in shared memory, rows of 64 f16 (128 bytes), 128-byte swizzle: descriptor of the
+// operand that begins at addr.  Rows are the operand's M or N and the row's channels its K: 8-row
+// groups 1024 bytes apart.  Rows are its K and channels its N (transposed): the same groups
+// along K, and blocks of 64 channels `block` bytes apart.
+__device__ __forceinline__ uint64_t desc128(uint32_t addr, uint32_t block) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(block >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
+         (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// fp32 accumulators, f16 operands, M = 128, N = n; transposed: B's N is contiguous
+__device__ __forceinline__ constexpr uint32_t idesc_f16(int n, bool transposed) {
+  return (1u << 4) | ((uint32_t)transposed << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+struct TileInfo {                    // what the softmax warps need to know of a tile
+  uint32_t valid[4];                 // slots that exist (cached tiles)
+  float key_scale, value_exp, value_scale;   // 2^Ek, Ev, 2^-Ev
+  int flags;                         // 1: new nodes, 2: some slot is not valid, 4: a value is not finite
+};
+struct TreeShared {
+  uint64_t kfull[2], kfree[2], vfull[2], vfree[2], sfull[2], pfull[2], pvdone[2], info_full[4], qfull;
+  uint64_t meet, peaks[2];           // the softmax warps; the decoding warps, by tile parity
+  TileInfo info[4];
+  uint32_t peak[2][kTrDecWarps][2];  // largest key and value bound each decoding warp saw
+  uint32_t tmem;
+  int gave_up;
+  float2 ml[128];                    // group B's sums on their way to A
+};
+
+template <int D>
+struct Tree {
+  static constexpr int kBlocks = D / 64, kMat = kBlocks * kTrTile * 128;     // one tile of K or V in f16
+  static constexpr int kQMat = kBlocks * 256 * 128;
+  static constexpr int kCum = (kKvMaxSeq + 1) * 8 + 32 * 8 + kKvMaxSeq * 5;
+  static constexpr int kBytes = 1024 + 4 * kMat + kQMat + (int)sizeof(TreeShared) + 64 + kCum;
+  // a piece in the workspace: accumulators [group][D / 4][128 rows][4], then (m, l) [group][128 rows]
+  static constexpr size_t kPiece = (size_t)2 * 128 * (D + 2);
+};
+
+// One piece of an item, as every role sees it.
+struct Piece {
+  int s, head, row0, n_rows;         // n_rows: the sequence's
+  bool two;                          // more than 128 rows: groups A and B have rows of their own
+  bool whole;                        // all of the item
+  bool nodes;                        // begins with the new nodes' tile
+  int c0, n;                         // first cached tile; tiles in all
+};
+__device__ __forceinline__ Piece piece_at(const TreeList::Cursor& k, int count, const KvView& c, const KvAttendArgs& a) {
+  Piece p;
+  p.s = k.s;
+  p.head = k.head;
+  p.row0 = k.item / c.n_kv * 256;
+  p.n_rows = k.nodes * a.group;
+  p.two = p.n_rows - p.row0 > 128;
+  p.whole = k.tile == 0 && count == (k.item < k.live ? k.tiles : 1);
+  const bool live = k.item < k.live;
+  p.nodes = live && k.tile == 0 && a.k.p && k.nodes > 0;
+  const int first = max(k.tile, kTrFront), last = k.tile + count;
+  p.c0 = first - kTrFront;
+  p.n = (live && last > first ? last - first : 0) + (p.nodes ? 1 : 0);
+  return p;
+}
+
+// (largest |element| of a group) as float bits; what reads as NaN says nothing
+template <bool kBf16> __device__ __forceinline__ uint32_t meta_peak(uint32_t meta) {
+  const float sc = half_lo<kBf16>(meta), lo = half_hi<kBf16>(meta);
+  const float x = fmaxf(fabsf(lo), fabsf(fmaf(15.f, sc, lo)));
+  return x < INFINITY ? __float_as_uint(x) : 0u;
+}
+// exponent E with peak < 2^E, as far as sums over long sequences times 2^-E stay in range
+__device__ __forceinline__ int peak_exp(uint32_t peak) {
+  return min(max((int)(peak >> 23) - 126, -90), 100);
+}
+__device__ __forceinline__ __half2 as_half2(uint32_t w) { return *reinterpret_cast<__half2*>(&w); }
+__device__ __forceinline__ uint32_t as_word(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
+
+// Eight codes (one word, channels in order) -> eight f16 numbers scale * code + lo.
+// code + 1024 (or 16 code + 1024) is an f16 number by its bits; both ways back to the code are exact.
+__device__ __forceinline__ uint4 decode8(uint32_t w, __half2 sc, __half2 lo) {
+  const uint32_t magic = 0x64006400u;
+  const __half2 m1024 = __half2half2(__ushort_as_half(0xE400)), r16 = __half2half2(__ushort_as_half(0x2C00)),
+                m64 = __half2half2(__ushort_as_half(0xD400));
+  const uint32_t v = w >> 8;
+  uint4 r;
+  r.x = as_word(__hfma2(__hadd2(as_half2((w & 0x000f000fu) | magic), m1024), sc, lo));
+  r.y = as_word(__hfma2(__hfma2(as_half2((w & 0x00f000f0u) | magic), r16, m64), sc, lo));
+  r.z = as_word(__hfma2(__hadd2(as_half2((v & 0x000f000fu) | magic), m1024), sc, lo));
+  r.w = as_word(__hfma2(__hfma2(as_half2((v & 0x00f000f0u) | magic), r16, m64), sc, lo));
+  return r;
+}
+
+}  // namespace
+
+template <int D, bool kBf16>
+__global__ void __launch_bounds__(kTrThreads, 1)
+kv_tree_kernel(const KvView c, const KvAttendArgs a) {
+  using T = Tree<D>;
+  constexpr int G = T::kBlocks;
+  extern __shared__ unsigned char raw_smem[];
+  unsigned char* smem = raw_smem + ((1024 - (kv_smem(raw_smem) & 1023)) & 1023);
+  unsigned char *vmat = smem, *kmat = smem + 2 * T::kMat, *qmat = smem + 4 * T::kMat;
+  TreeShared& sh = *reinterpret_cast<TreeShared*>(qmat + T::kQMat);
+  long long* cum = reinterpret_cast<long long*>(qmat + T::kQMat + (sizeof(TreeShared) + 15) / 16 * 16);
+  long long* scratch = cum + kKvMaxSeq + 1;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  DeviceStats* stats = &reinterpret_cast<KvWork*>(c.work)->stats;
+  volatile int* gave_up = &sh.gave_up;
+
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      bar_init(&sh.kfull[i], kTrDecWarps);
+      bar_init(&sh.kfree[i], 1);
+      bar_init(&sh.vfull[i], kTrDecWarps);
+      bar_init(&sh.vfree[i], 1);
+      bar_init(&sh.sfull[i], 1);
+      bar_init(&sh.pfull[i], 4);
+      bar_init(&sh.pvdone[i], 1);
+      bar_init(&sh.peaks[i], kTrDecWarps);
+    }
+    for (int i = 0; i < 4; ++i) bar_init(&sh.info_full[i], kTrDecWarps);
+    bar_init(&sh.qfull, 8);
+    bar_init(&sh.meet, 8);
+    sh.gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 16) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(kv_smem(&sh.tmem)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = sh.tmem;
+  pdl_enter();
+
+  TreeList list;
+  list.cum = cum;
+  list.len = reinterpret_cast<int*>(scratch + 32);
+  list.nodes = reinterpret_cast<unsigned char*>(list.len + kKvMaxSeq);
+  list.items = c.n_kv * ((a.m * a.group + 255) / 256);
+  list.group = a.group;
+  list.rows = 256;
+  list.build<kTrThreads>(c, a.n_new, a.m, scratch);
+  const int n_cta = (int)min((long long)gridDim.x, list.total);
+  TreeList::Cursor bc, scrap;
+  int u1 = 0;
+  if ((int)blockIdx.x < n_cta) {
+    const long long end = list.cut(scrap, blockIdx.x + 1, n_cta), begin = list.cut(bc, blockIdx.x, n_cta);
+    u1 = (int)(end - begin);
+  }
+  const int block_bytes = 2 * kv_part_bytes(D, 1 << c.page_shift);
+  const int page = 1 << c.page_shift;
+
+  if (warp < 8) {
+    // ============================================================ softmax ========
+    const int wg = warp >> 2, row = tid & 127;           // row of the group
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;   // TMEM lanes of this warp
+    const uint32_t s_tm = tmem + lanes + wg * 256, o_tm = s_tm + 128;
+    uint32_t kt = 0, su = 0, met = 0;                    // tiles, score tiles of the group, meetings so far
+    bool ok = true;
+    auto meet = [&]() {                                  // of both groups
+      __syncwarp();
+      if (lane == 0) bar_arrive(&sh.meet);
+      ok = ok && warp_wait(&sh.meet, met++ & 1, gave_up, stats);
+      return ok;
+    };
+    for (int at = 0; at < u1 && ok;) {
+      const int n_tiles = bc.item < bc.live ? bc.tiles : 1, count = min(n_tiles - bc.tile, u1 - at);
+      const Piece p = piece_at(bc, count, c, a);
+      float m = -INFINITY, l = 0.f;
+      bool odd_values = false;                           // new nodes' values that are not finite
+      const int my_row = p.row0 + (p.two ? wg * 128 : 0) + row;
+      const bool have = my_row < p.n_rows;
+      const int node = have ? my_row / a.group : 0, hq = p.head * a.group + (have ? my_row % a.group : 0);
+      // (both groups have left the piece before: its scores, its accumulators and its Q are free)
+      if (!meet()) break;
+      if (p.n > 0) {
+        // ---- the row as an operand ----
+        const uint16_t* qp = a.q.at(p.s, node, hq);
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+          uint4 w = make_uint4(0, 0, 0, 0);
+          if (have) w = *reinterpret_cast<const uint4*>(qp + i * 8);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t x = (&w.x)[e];
+            top = abs_max(abs_max(top, half_lo<kBf16>(x)), half_hi<kBf16>(x));
+          }
+        }
+        const int e0 = top < INFINITY ? min(row_exponent(top), 126) : 0;
+        const float up = a.scale < 0.f ? -pow2(-e0) : pow2(-e0);
+        const float f = fmaxf(fabsf(a.scale) * kLog2e * pow2(e0), 1e-37f);
+        if (p.two || wg == 0) {
+          unsigned char* qm = qmat + (wg * 128 + row) * 128;
+#pragma unroll
+          for (int i = 0; i < D / 8; ++i) {
+            uint4 w = make_uint4(0, 0, 0, 0);
+            if (have) w = *reinterpret_cast<const uint4*>(qp + i * 8);
+            uint4 h;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t x = (&w.x)[e];
+              (&h.x)[e] = pack16<false>(half_lo<kBf16>(x) * up, half_hi<kBf16>(x) * up);
+            }
+            *reinterpret_cast<uint4*>(qm + (i >> 3) * (256 * 128) + (((i & 7) ^ (row & 7)) << 4)) = h;
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) bar_arrive(&sh.qfull);
+        const unsigned long long sees =
+            !have ? 0ull : a.mask ? a.mask[p.s * a.mask_stride + node] : (2ull << node) - 1ull;
+
+        // ---- tile by tile ----
+        const int mine = p.two ? p.n : (p.n + 1 - wg) / 2;
+        for (int i = 0; i < mine; ++i, ++su) {
+          const uint32_t t = kt + (p.two ? i : 2 * i + wg);
+          if (!warp_wait(&sh.info_full[t & 3], (t >> 2) & 1, gave_up, stats) ||
+              !warp_wait(&sh.sfull[wg], su & 1, gave_up, stats)) { ok = false; break; }
+          fence_after();
+          const TileInfo& info = sh.info[t & 3];
+          const int flags = info.flags;
+          const float g = f * info.key_scale, ev = info.value_exp;
+          // which slots count for this row
+          uint32_t see[4];
+          if (flags & 1) {
+            see[0] = (uint32_t)sees & info.valid[0];
+            see[1] = (uint32_t)(sees >> 32) & info.valid[1];
+            see[2] = see[3] = 0u;
+            odd_values |= (flags & 4) != 0;
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) see[k] = info.valid[k];
+          }
+          const bool masked = flags & 3;
+          float mx = -INFINITY;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            float x[32];
+            tmem_ld32(s_tm + k * 32, x);
+            if (masked) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) mx = fmaxf(mx, see[k] >> e & 1 ? x[e] : -INFINITY);
+            } else {
+              float y[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+              for (int e = 4; e < 32; ++e) y[e & 3] = fmaxf(y[e & 3], x[e]);
+              mx = fmaxf(mx, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
+            }
+          }
+          mx = fmaf(mx, g, ev);
+          if (__any_sync(0xffffffffu, mx > m + 8.f)) {
+            const float mn = fmaxf(m, mx), down = mn == -INFINITY ? 1.f : exp2_approx(m - mn);
+            m = mn;
+            l *= down;
+            if (i > 0) {
+              if (!warp_wait(&sh.pvdone[wg], (su - 1) & 1, gave_up, stats)) { ok = false; break; }
+              fence_after();
+#pragma unroll 1
+              for (int k = 0; k < D; k += 32) {
+                float x[32];
+                tmem_ld32(o_tm + k, x);
+                uint32_t y[16];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                  for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(x[h * 16 + e] * down);
+                  tmem_st16(o_tm + k + h * 16, y);
+                }
+              }
+            }
+          }
+          const float shift = ev - (m == -INFINITY ? 0.f : m);
+          float sum[2] = {0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            float x[32];
+            tmem_ld32(s_tm + k * 32, x);
+            uint32_t y[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              float p0 = exp2_approx(fmaf(x[2 * e], g, shift)), p1 = exp2_approx(fmaf(x[2 * e + 1], g, shift));
+              if (masked) {
+                p0 = see[k] >> (2 * e) & 1 ? p0 : 0.f;
+                p1 = see[k] >> (2 * e + 1) & 1 ? p1 : 0.f;
+              }
+              sum[0] += p0;
+              sum[1] += p1;
+              y[e] = pack16<false>(p0, p1);
+            }
+            tmem_st16(s_tm + k * 16, y);                 // over scores already read
+          }
+          l = fmaf(sum[0] + sum[1], info.value_scale, l);
+          tmem_wait_st();
+          fence_before();
+          __syncwarp();
+          if (lane == 0) bar_arrive(&sh.pfull[wg]);
+        }
+        if (!ok) break;
+        kt += p.n;
+        if (mine > 0) {
+          if (!warp_wait(&sh.pvdone[wg], (su - 1) & 1, gave_up, stats)) { ok = false; break; }
+          fence_after();
+        }
+        if (mine == 0) { m = -INFINITY; l = 0.f; }
+      }
+      // A thread's 32 accumulators from column k on.  Infinities and NaN of new nodes' values
+      // stayed out of the products (0 times a hidden node's would have reached every row): they
+      // are added to the rows that see them.
+      const bool any = p.n > (p.two ? 0 : wg);           // the group has accumulators
+      auto accumulators = [&](int k, float (&x)[32]) {
+        tmem_ld32(o_tm + k, x);
+        if (odd_values && have) {
+          const unsigned long long sees = a.mask ? a.mask[p.s * a.mask_stride + node] : (2ull << node) - 1ull;
+          for (int j = 0; j < bc.nodes; ++j)
+            if (sees >> j & 1ull) {
+              const uint16_t* vp = a.v.at(p.s, j, p.head) + k;
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(vp + 2 * e);
+                const float v0 = half_lo<kBf16>(w), v1 = half_hi<kBf16>(w);
+                if (!(fabsf(v0) < INFINITY)) x[2 * e] += v0;
+                if (!(fabsf(v1) < INFINITY)) x[2 * e + 1] += v1;
+              }
+            }
+        }
+      };
+      if (!p.whole) {
+        // ---- to the workspace ----
+        float* part = reinterpret_cast<float*>(c.work + kKvPartOff) + (size_t)(2 * blockIdx.x + (bc.tile == 0 ? 1 : 0)) * T::kPiece;
+        __stcg(reinterpret_cast<float2*>(part + (size_t)2 * 128 * D) + wg * 128 + row, make_float2(m, l));
+        if (any) {
+#pragma unroll 1
+          for (int k = 0; k < D; k += 32) {
+            float x[32];
+            accumulators(k, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              __stcg(reinterpret_cast<float4*>(part) + ((size_t)wg * (D / 4) + k / 4 + e) * 128 + row,
+                     make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]));
+          }
+        }
+      } else {
+        // ---- to the output; where both groups had the same rows, B's sums by way of Q's place ----
+        float4* swap = reinterpret_cast<float4*>(qmat);
+        if (!p.two) {
+          if (!meet()) break;                            // all scores are taken
+          if (wg == 1) {
+            sh.ml[row] = make_float2(m, l);
+            if (any) {
+#pragma unroll 1
+              for (int k = 0; k < D; k += 32) {
+                float x[32];
+                accumulators(k, x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) swap[(k / 4 + e) * 128 + row] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+              }
+            }
+          }
+          if (!meet()) break;
+        }
+        // group B has the rows behind the 128 in that case: they do not exist
+        const int out_row = p.row0 + wg * 128 + row;
+        float ka = 1.f, kb = 0.f;
+        if (!p.two && wg == 0 && p.n > 1) {
+          const float2 y = sh.ml[row];
+          const float big = fmaxf(m, y.x);
+          ka = m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : exp2_approx(m - big);
+          kb = y.x == -INFINITY ? (y.y == 0.f ? 0.f : 1.f) : exp2_approx(y.x - big);
+          l = fmaf(ka, l, kb * y.y);
+          m = big;
+        }
+        if (!have || (!p.two && wg == 1)) l = 0.f;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const bool exists = out_row < a.m * a.group;
+        const int onode = exists ? out_row / a.group : 0, ohq = p.head * a.group + (exists ? out_row % a.group : 0);
+        uint16_t* op = a.out + p.s * a.out_seq + onode * a.out_row + ohq * a.out_head;
+#pragma unroll 1
+        for (int k = 0; k < D; k += 32) {
+          float x[32];
+          if (any && (p.two || wg == 0)) {
+            accumulators(k, x);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) x[e] *= ka;
+            if (kb != 0.f) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const float4 y = swap[(k / 4 + e) * 128 + row];
+                x[4 * e] = fmaf(kb, y.x, x[4 * e]);
+                x[4 * e + 1] = fmaf(kb, y.y, x[4 * e + 1]);
+                x[4 * e + 2] = fmaf(kb, y.z, x[4 * e + 2]);
+                x[4 * e + 3] = fmaf(kb, y.w, x[4 * e + 3]);
+              }
+            }
+          }
+          if (exists) {
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+              uint32_t w[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) w[e] = l == 0.f ? 0u : pack16<kBf16>(x[8 * h + 2 * e] * inv, x[8 * h + 2 * e + 1] * inv);
+              *reinterpret_cast<uint4*>(op + k + 8 * h) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          }
+        }
+        if (exists && a.lse)
+          a.lse[p.s * a.lse_seq + onode * a.lse_row + ohq * a.lse_head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kTrLn2;
+      }
+      fence_before();
+      at += count;
+      if (at < u1) list.advance(bc, count);
+    }
+  } else if (warp < 16) {
+    // ============================================================ decode =========
+    const int dw = warp - 8, sl = dw * 16 + (lane & 15), half = lane >> 4;   // slot, half of its 32 bytes
+    uint32_t kt = 0;
+    bool ok = true;
+    for (int at = 0; at < u1 && ok;) {
+      const int n_tiles = bc.item < bc.live ? bc.tiles : 1, count = min(n_tiles - bc.tile, u1 - at);
+      const Piece p = piece_at(bc, count, c, a);
+      const int32_t* table = c.table + (size_t)p.s * c.max_pages;
+      // what a thread holds of a tile: 16 bytes of codes and the meta of its slot, for K and V
+      // and each group; the next tile's are asked for before this one's are worked on
+      struct Held {
+        uint4 code[2][G];
+        uint32_t meta[2][G];
+        bool valid;
+      };
+      Held cur, next;
+      cur.valid = next.valid = false;
+      const int first = p.nodes ? -1 : 0, cached = p.n + first;   // tile -1: the new nodes
+      auto page_for = [&](int i) {
+        const int slot = (p.c0 + i) * kTrTile + sl;
+        int q = -1;
+        if (i < cached && slot < bc.len) {
+          q = table[slot >> c.page_shift];
+          q = (uint32_t)q < (uint32_t)c.n_pages ? q : -1;
+        }
+        return q;
+      };
+      auto load = [&](Held& h, int q, int i) {
+        h.valid = q >= 0;
+        const unsigned char* b = c.pages + ((size_t)max(q, 0) * c.n_kv + p.head) * block_bytes;
+        const int in = ((p.c0 + i) * kTrTile + sl) & (page - 1);
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            h.code[kv][g] = make_uint4(0, 0, 0, 0);
+            h.meta[kv][g] = 0u;
+            if (h.valid) {
+              const unsigned char* x = b + kv * (block_bytes / 2);
+              h.code[kv][g] = __ldcg(reinterpret_cast<const uint4*>(x + (g * page + in) * 32 + half * 16));
+              h.meta[kv][g] = __ldcg(reinterpret_cast<const uint32_t*>(x + (G * page * 8 + in * G + g) * 4));
+            }
+          }
+      };
+      int next_page = -1;
+      if (cached > 0) { load(cur, page_for(0), 0); next_page = page_for(1); }
+      for (int i = first; i < cached; ++i, ++kt) {
+        const int st = kt & 1;
+        const uint32_t ph = (kt >> 1) & 1;
+        TileInfo& info = sh.info[kt & 3];
+        unsigned char *km = kmat + st * T::kMat, *vm = vmat + st * T::kMat;
+        if (i >= 0) {
+          load(next, next_page, i + 1);                  // (zeros behind the last)
+          next_page = page_for(i + 2);
+          uint32_t pk = 0, pv = 0;
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            pk = max(pk, meta_peak<kBf16>(cur.meta[0][g]));
+            pv = max(pv, meta_peak<kBf16>(cur.meta[1][g]));
+          }
+          pk = __reduce_max_sync(0xffffffffu, pk);
+          pv = __reduce_max_sync(0xffffffffu, pv);
+          const uint32_t ballot = __ballot_sync(0xffffffffu, cur.valid) & 0xffffu;
+          if (lane == 0) { sh.peak[st][dw][0] = pk; sh.peak[st][dw][1] = pv; }
+          // (the tile before the one before last is done with: its peaks and, four tiles back,
+          // its info may be overwritten)
+          if (!warp_wait(&sh.kfree[st], ph ^ 1, gave_up, stats)) { ok = false; break; }
+          if (lane == 0) {
+            reinterpret_cast<uint16_t*>(info.valid)[dw] = (uint16_t)ballot;
+            if (dw == 0) info.flags = 0;
+          }
+          __syncwarp();
+          if (lane == 0) bar_arrive(&sh.peaks[st]);
+          if (!warp_wait(&sh.peaks[st], ph, gave_up, stats)) { ok = false; break; }
+#pragma unroll
+          for (int w = 0; w < kTrDecWarps; ++w) { pk = max(pk, sh.peak[st][w][0]); pv = max(pv, sh.peak[st][w][1]); }
+          const int ek = peak_exp(pk), ev = peak_exp(pv);
+          if (ballot != 0xffffu && lane == 0) atomicOr(&info.flags, 2);
+          if (dw == 0 && lane == 0) {
+            info.key_scale = pow2(ek);
+            info.value_exp = (float)ev;
+            info.value_scale = pow2(-ev);
+          }
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv) {
+            if (kv == 1 && !warp_wait(&sh.vfree[st], ph ^ 1, gave_up, stats)) { ok = false; break; }
+            const float down = pow2(-(kv ? ev : ek));
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+              const uint32_t m2 = cur.meta[kv][g];
+              const float fs = half_lo<kBf16>(m2) * down, fl = half_hi<kBf16>(m2) * down;
+              const __half2 sc = as_half2(pack16<false>(fs, fs)), lo = as_half2(pack16<false>(fl, fl));
+              unsigned char* dst = (kv ? vm : km) + g * (kTrTile * 128) + sl * 128;
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                *reinterpret_cast<uint4*>(dst + (((half * 4 + k) ^ (sl & 7)) << 4)) = decode8((&cur.code[kv][g].x)[k], sc, lo);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+              bar_arrive(kv ? &sh.vfull[st] : &sh.kfull[st]);
+              if (kv == 0) bar_arrive(&sh.info_full[kt & 3]);
+            }
+          }
+          if (!ok) break;
+          cur = next;
+        } else {
+          // ---- new nodes: 16-bit elements, slots 0..63 of the tile; the rest is zero ----
+          const bool node = sl < bc.nodes;
+          const uint16_t* src[2] = {a.k.at(p.s, node ? sl : 0, p.head), a.v.at(p.s, node ? sl : 0, p.head)};
+          uint32_t peak[2] = {0u, 0u};
+          bool odd = false;
+          for (int kv = 0; kv < 2; ++kv)
+            for (int k = 0; k < D / 16; ++k) {           // the thread's half of the channels, 8 at a time
+              const int ch = (k >> 2) * 64 + half * 32 + (k & 3) * 8;
+              uint4 w = make_uint4(0, 0, 0, 0);
+              if (node) w = *reinterpret_cast<const uint4*>(src[kv] + ch);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const uint32_t x = (&w.x)[e >> 1];
+                const float v = fabsf(e & 1 ? half_hi<kBf16>(x) : half_lo<kBf16>(x));
+                if (v < INFINITY) peak[kv] = max(peak[kv], __float_as_uint(v));
+                else odd |= kv == 1;
+              }
+            }
+          peak[0] = __reduce_max_sync(0xffffffffu, peak[0]);
+          peak[1] = __reduce_max_sync(0xffffffffu, peak[1]);
+          odd = __any_sync(0xffffffffu, odd);
+          const uint32_t ballot = __ballot_sync(0xffffffffu, node) & 0xffffu;
+          if (lane == 0) { sh.peak[st][dw][0] = peak[0]; sh.peak[st][dw][1] = peak[1]; }
+          if (!warp_wait(&sh.kfree[st], ph ^ 1, gave_up, stats) || !warp_wait(&sh.vfree[st], ph ^ 1, gave_up, stats)) {
+            ok = false;
+            break;
+          }
+          if (lane == 0) {
+            reinterpret_cast<uint16_t*>(info.valid)[dw] = (uint16_t)ballot;
+            if (dw == 0) info.flags = 1;
+          }
+          __syncwarp();
+          if (lane == 0) bar_arrive(&sh.peaks[st]);
+          if (!warp_wait(&sh.peaks[st], ph, gave_up, stats)) { ok = false; break; }
+#pragma unroll
+          for (int w = 0; w < kTrDecWarps; ++w) {
+            peak[0] = max(peak[0], sh.peak[st][w][0]);
+            peak[1] = max(peak[1], sh.peak[st][w][1]);
+          }
+          const int ek = peak_exp(peak[0]), ev = peak_exp(peak[1]);
+          if (odd && lane == 0) atomicOr(&info.flags, 4);
+          if (dw == 0 && lane == 0) {
+            info.key_scale = pow2(ek);
+            info.value_exp = (float)ev;
+            info.value_scale = pow2(-ev);
+          }
+          for (int kv = 0; kv < 2; ++kv) {
+            const float down = pow2(-(kv ? ev : ek));
+            for (int k = 0; k < D / 16; ++k) {
+              const int ch = (k >> 2) * 64 + half * 32 + (k & 3) * 8;
+              uint4 w = make_uint4(0, 0, 0, 0), h;
+              if (node) w = *reinterpret_cast<const uint4*>(src[kv] + ch);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                float v0 = half_lo<kBf16>((&w.x)[e]) * down, v1 = half_hi<kBf16>((&w.x)[e]) * down;
+                if (kv) {
+                  v0 = fabsf(v0) < INFINITY ? v0 : 0.f;
+                  v1 = fabsf(v1) < INFINITY ? v1 : 0.f;
+                }
+                (&h.x)[e] = pack16<false>(v0, v1);
+              }
+              *reinterpret_cast<uint4*>((kv ? vm : km) + (k >> 2) * (kTrTile * 128) + sl * 128 +
+                                        (((half * 4 + (k & 3)) ^ (sl & 7)) << 4)) = h;
+            }
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) {
+            bar_arrive(&sh.kfull[st]);
+            bar_arrive(&sh.vfull[st]);
+            bar_arrive(&sh.info_full[kt & 3]);
+          }
+        }
+      }
+      at += count;
+      if (at < u1) list.advance(bc, count);
+    }
+  } else {
+    // ============================================================ products =======
+    uint32_t kt = 0, np = 0, pu[2] = {0, 0};
+    bool ok = true;
+    constexpr uint32_t s_idesc = idesc_f16(kTrTile, false), o_idesc = idesc_f16(D, true);
+    for (int at = 0; at < u1 && ok;) {
+      const int n_tiles = bc.item < bc.live ? bc.tiles : 1, count = min(n_tiles - bc.tile, u1 - at);
+      const Piece p = piece_at(bc, count, c, a);
+      if (p.n > 0) {
+        const int steps = p.two ? 2 * p.n : p.n;
+        ok = warp_wait(&sh.qfull, np & 1, gave_up, stats);
+        ++np;
+        auto scores = [&](int u) {
+          const uint32_t t = kt + (p.two ? u >> 1 : u);
+          const int st = t & 1, wg = u & 1;
+          if (!p.two || wg == 0) ok = ok && warp_wait(&sh.kfull[st], (t >> 1) & 1, gave_up, stats);
+          if (!ok) return;
+          fence_after();
+          const uint32_t qa = kv_smem(qmat) + (p.two ? wg * 128 * 128 : 0), ka = kv_smem(kmat + st * T::kMat);
+          if (one_lane()) {
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+              mma_ss(tmem + wg * 256, desc128(qa + (k >> 2) * (256 * 128) + (k & 3) * 32, 16),
+                     desc128(ka + (k >> 2) * (kTrTile * 128) + (k & 3) * 32, 16), s_idesc, k > 0);
+            commit(&sh.sfull[wg]);
+            if (!p.two || wg == 1) commit(&sh.kfree[st]);
+          }
+          __syncwarp();
+        };
+        scores(0);
+        if (steps > 1) scores(1);
+        for (int u = 0; u < steps && ok; ++u) {
+          const uint32_t t = kt + (p.two ? u >> 1 : u);
+          const int st = t & 1, wg = u & 1;
+          if (!p.two || wg == 0) ok = warp_wait(&sh.vfull[st], (t >> 1) & 1, gave_up, stats);
+          ok = ok && warp_wait(&sh.pfull[wg], pu[wg] & 1, gave_up, stats);
+          if (!ok) break;
+          ++pu[wg];
+          fence_after();
+          const uint32_t va = kv_smem(vmat + st * T::kMat);
+          if (one_lane()) {
+#pragma unroll
+            for (int k = 0; k < kTrTile / 16; ++k)
+              mma_ts(tmem + wg * 256 + 128, tmem + wg * 256 + k * 8, desc128(va + k * 2048, kTrTile * 128), o_idesc,
+                     u > 1 || k > 0);
+            commit(&sh.pvdone[wg]);
+            if (!p.two || wg == 1) commit(&sh.vfree[st]);
+          }
+          __syncwarp();
+          if (u + 2 < steps) scores(u + 2);
+        }
+        kt += p.n;
+      }
+      at += count;
+      if (at < u1) list.advance(bc, count);
+    }
+    // what was issued is done before the memory goes away: the softmax warps waited for the last
+    // products, unless somebody gave up
+    if (*gave_up) {
+      const unsigned long long t0 = now_ns();
+      while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
+    }
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  if (warp == 16)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+// The pieces of every item joined, in their order.  A block: 128 rows of an item, 32 channels;
+// a thread: a row, 16 channels.
+template <int D, bool kBf16>
+__global__ void __launch_bounds__(256)
+kv_tree_join_kernel(const KvView c, const KvAttendArgs a, int tree_ctas) {
+  using T = Tree<D>;
+  extern __shared__ __align__(16) unsigned char smem[];
+  long long* cum = reinterpret_cast<long long*>(smem);
+  long long* scratch = cum + kKvMaxSeq + 1;
+  pdl_enter();
+  TreeList list;
+  list.cum = cum;
+  list.len = reinterpret_cast<int*>(scratch + 32);
+  list.nodes = reinterpret_cast<unsigned char*>(list.len + kKvMaxSeq);
+  list.items = c.n_kv * ((a.m * a.group + 255) / 256);
+  list.group = a.group;
+  list.rows = 256;
+  list.build<256>(c, a.n_new, a.m, scratch);
+  const int n_cta = (int)min((long long)tree_ctas, list.total);
+  const int s = blockIdx.x / list.items, item = blockIdx.x % list.items;
+  const int head = item % c.n_kv, row0 = item / c.n_kv * 256;
+  const int halfb = blockIdx.y & 1, ch0 = (blockIdx.y >> 1) * 32 + (threadIdx.x >> 7) * 16, row = threadIdx.x & 127;
+  const int my_row = row0 + halfb * 128 + row;
+  if (my_row >= a.m * a.group) return;
+  const int node = my_row / a.group, hq = head * a.group + my_row % a.group;
+  const int n_rows = list.nodes[s] * a.group;
+  if (item >= list.live_items(list.nodes[s])) return;    // its block wrote it, as all items it had whole
+  const int tiles = list.tiles_of(list.len[s]);
+  int b0, b1;
+  list.owners(cum[s] + (long long)item * tiles, tiles, n_cta, b0, b1);
+  if (b0 == b1) return;
+  float big = -INFINITY, sum = 0.f, v[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) v[e] = 0.f;
+  if (my_row < n_rows) {
+    const bool two = n_rows - row0 > 128;
+    const float* parts = reinterpret_cast<const float*>(c.work + kKvPartOff);
+    const int groups = two ? 1 : 2, n_src = (b1 - b0 + 1) * groups;
+    auto piece = [&](int i) {
+      const int b = b0 + i / groups;
+      return parts + (size_t)(2 * b + (b == b0 ? 1 : 0)) * T::kPiece;
+    };
+    auto group_of = [&](int i) { return two ? halfb : i % groups; };
+    auto ml = [&](int i) {
+      return __ldcg(reinterpret_cast<const float2*>(piece(i) + (size_t)2 * 128 * D) + group_of(i) * 128 + row);
+    };
+#pragma unroll 4
+    for (int i = 0; i < n_src; ++i) big = fmaxf(big, ml(i).x);
+#pragma unroll 4
+    for (int i = 0; i < n_src; ++i) {
+      const float2 x = ml(i);
+      const float k = x.x == -INFINITY ? (x.y == 0.f ? 0.f : 1.f) : exp2_approx(x.x - big);
+      sum = fmaf(k, x.y, sum);
+      if (k != 0.f) {
+        const float4* src = reinterpret_cast<const float4*>(piece(i)) + ((size_t)group_of(i) * (D / 4) + ch0 / 4) * 128 + row;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float4 y = __ldcg(src + e * 128);
+          v[4 * e] = fmaf(k, y.x, v[4 * e]);
+          v[4 * e + 1] = fmaf(k, y.y, v[4 * e + 1]);
+          v[4 * e + 2] = fmaf(k, y.z, v[4 * e + 2]);
+          v[4 * e + 3] = fmaf(k, y.w, v[4 * e + 3]);
+        }
+      }
+    }
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  uint32_t w[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) w[e] = sum == 0.f ? 0u : pack16<kBf16>(v[2 * e] * inv, v[2 * e + 1] * inv);
+  uint4* op = reinterpret_cast<uint4*>(a.out + s * a.out_seq + node * a.out_row + hq * a.out_head + ch0);
+  op[0] = make_uint4(w[0], w[1], w[2], w[3]);
+  op[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  if (a.lse && ch0 == 0)
+    a.lse[s * a.lse_seq + node * a.lse_row + hq * a.lse_head] = sum == 0.f ? -INFINITY : (big + log2f(sum)) * kTrLn2;
+}
+
+template <int D, bool kBf16>
+static cudaError_t tree_launch(const KvView& c, const KvAttendArgs& a, int sms, cudaStream_t st) {
+  const int grid = sms < kKvTreeMaxCtas ? sms : kKvTreeMaxCtas;
+  const cudaError_t e = launch_pdl(kv_tree_kernel<D, kBf16>, dim3(grid), dim3(kTrThreads), Tree<D>::kBytes, st, c, a);
+  if (e != cudaSuccess) return e;
+  const int items = c.n_seq * c.n_kv * ((a.m * a.group + 255) / 256);
+  return launch_pdl(kv_tree_join_kernel<D, kBf16>, dim3(items, 2 * (D / 32)), dim3(256), Tree<D>::kCum, st, c, a, grid);
+}
+
+cudaError_t launch_kv_tree(const KvView& c, const KvAttendArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st) {
+  if (head_dim == 64) return bf16 ? tree_launch<64, true>(c, a, sms, st) : tree_launch<64, false>(c, a, sms, st);
+  return bf16 ? tree_launch<128, true>(c, a, sms, st) : tree_launch<128, false>(c, a, sms, st);
+}
+
+template <int D, bool kBf16>
+static cudaError_t preload_tree() {
+  const cudaError_t e = preload_kernel(kv_tree_kernel<D, kBf16>, true);
+  return e != cudaSuccess ? e : preload_kernel(kv_tree_join_kernel<D, kBf16>, true);
+}
+cudaError_t preload_kv_tree_kernels() {
+  cudaError_t e;
+  if ((e = preload_tree<64, true>()) != cudaSuccess) return e;
+  if ((e = preload_tree<64, false>()) != cudaSuccess) return e;
+  if ((e = preload_tree<128, true>()) != cudaSuccess) return e;
+  return preload_tree<128, false>();
+}
+
+}  // namespace oilbird

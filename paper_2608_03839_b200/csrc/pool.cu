@@ -53,6 +53,7 @@ cudaError_t preload_all_kernels() {
   if ((e = preload_kv_attend_kernels()) != cudaSuccess) return e;
   if ((e = preload_kv_evict_kernels()) != cudaSuccess) return e;
   if ((e = preload_kv_store_kernels()) != cudaSuccess) return e;
+  if ((e = preload_kv_tree_kernels()) != cudaSuccess) return e;
   if ((e = preload_kv_weigh_kernels()) != cudaSuccess) return e;
   if ((e = preload_merge_kernels()) != cudaSuccess) return e;
   if ((e = preload_merge_tree_kernels()) != cudaSuccess) return e;

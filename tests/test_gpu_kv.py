@@ -613,3 +613,35 @@ def test_owned_cache():
     assert cache.seq_len.tolist() == [100] * 3 and cache.dropped() == 0
     cache.append(k, k)                                           # 128 slots a sequence: 28 more fit
     assert cache.seq_len.tolist() == [128] * 3 and cache.dropped() == 3 * 72
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("m,hq", [(3, 4), (40, 4)])
+def test_attend_what_a_row_does_not_see_does_not_reach_it(dtype, m, hq):
+    """Infinities and NaN in hidden nodes stay there; in a node's values they reach the rows that
+    see it, in their channels."""
+    c = Made([70, 0], 1, 128, 64, dtype)
+    q, kn, vn = (c.rand(2, m, h, 128).to(KIND[dtype]) for h in (hq, 1, 1))
+    mask = torch.ones(2, m, dtype=torch.int64, device="cuda") << torch.arange(m, device="cuda")
+    mask[:, m - 1] |= 1 << 1                                     # the last row also sees node 1
+    want, wl = c.cache.attend(q, kn, vn, mask=mask)
+    kn[:, 0], vn[:, 0] = float("nan"), float("inf")              # row 0 alone sees node 0
+    vn[:, 1, 0, 5] = float("-inf")
+    got, gl = c.cache.attend(q, kn, vn, mask=mask)
+    assert torch.isnan(got[:, 0]).all() and torch.isnan(gl[:, 0]).all()
+    for row in (1, m - 1):
+        assert torch.all(got[:, row, :, 5] == float("-inf"))
+        keep = [ch for ch in range(128) if ch != 5]
+        # (the values' common scale may have changed with the odd element taken out)
+        assert torch.allclose(got[:, row][..., keep].float(), want[:, row][..., keep].float(), rtol=2 * UNIT[dtype], atol=2.0 ** -11)
+    if m > 3:
+        assert torch.equal(gl[:, 2:m - 1], wl[:, 2:m - 1])
+        assert torch.allclose(got[:, 2:m - 1].float(), want[:, 2:m - 1].float(), rtol=2 * UNIT[dtype], atol=2.0 ** -11)
+
+
+@pytest.mark.parametrize("m,hq,hkv,lens", [(64, 16, 1, [900, 130]), (33, 8, 2, [4000]), (17, 8, 1, [5, 129, 0, 127, 128, 1000]),
+                                            (64, 4, 4, [300]), (32, 4, 1, [2000, 90]), (33, 4, 1, [2000, 90])])
+@pytest.mark.parametrize("d,dtype", [(128, "bf16"), (64, "f16")])
+def test_attend_many_rows(m, hq, hkv, lens, d, dtype):
+    """Row blocks of 256, of 128 and fewer (both groups on the same rows), items whole and cut."""
+    attend_case(lens, m, hq, hkv, d, 32, dtype, ragged=len(lens) > 2)
