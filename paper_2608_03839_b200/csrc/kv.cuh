@@ -219,7 +219,7 @@ __device__ __forceinline__ long long block_exclusive_scan(long long v, long long
 // depend on nothing, and the front stands for what an item costs besides its slots (operands,
 // joining), so that a block that gets many short items gets fewer slots.  Items whose rows do
 // not exist have one empty tile.
-template <int kTile, int kFront>
+template <int kTile, int kFront, int kFew>
 struct TileListOf {
   struct Cursor {
     int s;                // sequence
@@ -308,7 +308,7 @@ struct TileListOf {
   // hardly more than an item's first round, or the last few tiles of one: such a cut moves to the item's
   // edge.  (Every block finds the same cuts.)
   // (Where blocks get little, more so: an item's few tiles are better left together.)
-  __device__ __forceinline__ int near_end(int n_cta) const { return total < (long long)kFront * kFront * n_cta ? 4 : 1; }
+  __device__ __forceinline__ int near_end(int n_cta) const { return total < kFew * n_cta ? 4 : 1; }
   __device__ __forceinline__ int near_start(int n_cta) const { return kFront + near_end(n_cta); }
   __device__ __forceinline__ long long cut(Cursor& k, int b, int n_cta) const {
     // (32-bit division wherever the numbers allow: the 64-bit one is a long routine)
@@ -349,7 +349,7 @@ struct TileListOf {
 };
 
 constexpr int kKvTile = 64, kKvNodeTile = 32, kKvFront = 8;
-using TileList = TileListOf<kKvTile, kKvFront>;
+using TileList = TileListOf<kKvTile, kKvFront, 64>;
 using TileCursor = TileList::Cursor;
 
 // The pages that hold a tile's quarters of 16 slots, lane q the q-th's; -1 where the table names

@@ -39,7 +39,7 @@ namespace {
 
 constexpr int kTrTile = 128, kTrFront = 4;               // slots a tile; see TileListOf
 constexpr int kTrSoftThreads = 256, kTrDecWarps = 8, kTrThreads = kTrSoftThreads + 32 * kTrDecWarps + 32;
-using TreeList = TileListOf<kTrTile, kTrFront>;
+using TreeList = TileListOf<kTrTile, kTrFront, 0>;
 constexpr float kTrLn2 = 0.6931471805599453f;
 
 // ------------------------------------------------------------------ PTX wrappers ---
@@ -129,6 +129,27 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]
       ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
         "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
+}
+// pairs of fp32 numbers in one instruction, and the largest of three
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z, w;\n\t"
+      "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "add.rn.f32x2 w, x, y;\n\tmov.b64 {%0, %1}, w;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -365,21 +386,27 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) see[k] = info.valid[k];
           }
-          const bool masked = flags & 3;
+          const bool masked = __any_sync(0xffffffffu, flags & 3);
           float mx = -INFINITY;
+          if (masked) {
+#pragma unroll 1
+            for (int k = 0; k < 4; ++k) {
+              float x[32];
+              tmem_ld32(s_tm + k * 32, x);
+              const uint32_t b = k == 0 ? see[0] : k == 1 ? see[1] : k == 2 ? see[2] : see[3];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            float x[32];
-            tmem_ld32(s_tm + k * 32, x);
-            if (masked) {
-#pragma unroll
-              for (int e = 0; e < 32; ++e) mx = fmaxf(mx, see[k] >> e & 1 ? x[e] : -INFINITY);
-            } else {
-              float y[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-              for (int e = 4; e < 32; ++e) y[e & 3] = fmaxf(y[e & 3], x[e]);
-              mx = fmaxf(mx, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
+              for (int e = 0; e < 32; ++e) mx = fmaxf(mx, b >> e & 1 ? x[e] : -INFINITY);
             }
+          } else {
+            float y[4] = {mx, mx, mx, mx};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              float x[32];
+              tmem_ld32(s_tm + k * 32, x);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) y[e & 3] = max3(y[e & 3], x[2 * e], x[2 * e + 1]);
+            }
+            mx = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
           }
           mx = fmaf(mx, g, ev);
           if (__any_sync(0xffffffffu, mx > m + 8.f)) {
@@ -404,26 +431,43 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
             }
           }
           const float shift = ev - (m == -INFINITY ? 0.f : m);
-          float sum[2] = {0.f, 0.f};
+          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+          const float2 g2 = make_float2(g, g), shift2 = make_float2(shift, shift);
+          if (masked) {
+#pragma unroll 1
+            for (int k = 0; k < 4; ++k) {
+              float x[32];
+              tmem_ld32(s_tm + k * 32, x);
+              const uint32_t b = k == 0 ? see[0] : k == 1 ? see[1] : k == 2 ? see[2] : see[3];
+              uint32_t y[16];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            float x[32];
-            tmem_ld32(s_tm + k * 32, x);
-            uint32_t y[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              float p0 = exp2_approx(fmaf(x[2 * e], g, shift)), p1 = exp2_approx(fmaf(x[2 * e + 1], g, shift));
-              if (masked) {
-                p0 = see[k] >> (2 * e) & 1 ? p0 : 0.f;
-                p1 = see[k] >> (2 * e + 1) & 1 ? p1 : 0.f;
+              for (int e = 0; e < 16; ++e) {
+                const float2 z = fma2(make_float2(x[2 * e], x[2 * e + 1]), g2, shift2);
+                const float2 p = make_float2(b >> (2 * e) & 1 ? exp2_approx(z.x) : 0.f,
+                                             b >> (2 * e + 1) & 1 ? exp2_approx(z.y) : 0.f);
+                sum[e & 1] = add2(sum[e & 1], p);
+                y[e] = pack16<false>(p.x, p.y);
               }
-              sum[0] += p0;
-              sum[1] += p1;
-              y[e] = pack16<false>(p0, p1);
+              tmem_st16(s_tm + k * 16, y);               // over scores already read
             }
-            tmem_st16(s_tm + k * 16, y);                 // over scores already read
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              float x[32];
+              tmem_ld32(s_tm + k * 32, x);
+              uint32_t y[16];
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const float2 z = fma2(make_float2(x[2 * e], x[2 * e + 1]), g2, shift2);
+                const float2 p = make_float2(exp2_approx(z.x), exp2_approx(z.y));
+                sum[e & 1] = add2(sum[e & 1], p);
+                y[e] = pack16<false>(p.x, p.y);
+              }
+              tmem_st16(s_tm + k * 16, y);
+            }
           }
-          l = fmaf(sum[0] + sum[1], info.value_scale, l);
+          sum[0] = add2(sum[0], sum[1]);
+          l = fmaf(sum[0].x + sum[0].y, info.value_scale, l);
           tmem_wait_st();
           fence_before();
           __syncwarp();
@@ -798,10 +842,10 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
-// The pieces of every item joined, in their order.  A block: 128 rows of an item, 32 channels;
-// a thread: a row, 16 channels.
+// The pieces of every item joined, in their order.  A block: 128 rows of an item, 16 channels;
+// a thread: a row, 4 channels.
 template <int D, bool kBf16>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(512)
 kv_tree_join_kernel(const KvView c, const KvAttendArgs a, int tree_ctas) {
   using T = Tree<D>;
   extern __shared__ __align__(16) unsigned char smem[];
@@ -815,11 +859,11 @@ kv_tree_join_kernel(const KvView c, const KvAttendArgs a, int tree_ctas) {
   list.items = c.n_kv * ((a.m * a.group + 255) / 256);
   list.group = a.group;
   list.rows = 256;
-  list.build<256>(c, a.n_new, a.m, scratch);
+  list.build<512>(c, a.n_new, a.m, scratch);
   const int n_cta = (int)min((long long)tree_ctas, list.total);
   const int s = blockIdx.x / list.items, item = blockIdx.x % list.items;
   const int head = item % c.n_kv, row0 = item / c.n_kv * 256;
-  const int halfb = blockIdx.y & 1, ch0 = (blockIdx.y >> 1) * 32 + (threadIdx.x >> 7) * 16, row = threadIdx.x & 127;
+  const int halfb = blockIdx.y & 1, ch0 = (blockIdx.y >> 1) * 16 + (threadIdx.x >> 7) * 4, row = threadIdx.x & 127;
   const int my_row = row0 + halfb * 128 + row;
   if (my_row >= a.m * a.group) return;
   const int node = my_row / a.group, hq = head * a.group + my_row % a.group;
@@ -829,48 +873,50 @@ kv_tree_join_kernel(const KvView c, const KvAttendArgs a, int tree_ctas) {
   int b0, b1;
   list.owners(cum[s] + (long long)item * tiles, tiles, n_cta, b0, b1);
   if (b0 == b1) return;
-  float big = -INFINITY, sum = 0.f, v[16];
-#pragma unroll
-  for (int e = 0; e < 16; ++e) v[e] = 0.f;
+  float big = -INFINITY, sum = 0.f;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
   if (my_row < n_rows) {
     const bool two = n_rows - row0 > 128;
     const float* parts = reinterpret_cast<const float*>(c.work + kKvPartOff);
     const int groups = two ? 1 : 2, n_src = (b1 - b0 + 1) * groups;
-    auto piece = [&](int i) {
-      const int b = b0 + i / groups;
-      return parts + (size_t)(2 * b + (b == b0 ? 1 : 0)) * T::kPiece;
-    };
-    auto group_of = [&](int i) { return two ? halfb : i % groups; };
-    auto ml = [&](int i) {
-      return __ldcg(reinterpret_cast<const float2*>(piece(i) + (size_t)2 * 128 * D) + group_of(i) * 128 + row);
-    };
-#pragma unroll 4
-    for (int i = 0; i < n_src; ++i) big = fmaxf(big, ml(i).x);
-#pragma unroll 4
-    for (int i = 0; i < n_src; ++i) {
-      const float2 x = ml(i);
-      const float k = x.x == -INFINITY ? (x.y == 0.f ? 0.f : 1.f) : exp2_approx(x.x - big);
-      sum = fmaf(k, x.y, sum);
-      if (k != 0.f) {
-        const float4* src = reinterpret_cast<const float4*>(piece(i)) + ((size_t)group_of(i) * (D / 4) + ch0 / 4) * 128 + row;
+    constexpr int kBatch = 8;                            // pieces asked for at once
+    for (int i0 = 0; i0 < n_src; i0 += kBatch) {
+      float2 x[kBatch];
+      float4 y[kBatch];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float4 y = __ldcg(src + e * 128);
-          v[4 * e] = fmaf(k, y.x, v[4 * e]);
-          v[4 * e + 1] = fmaf(k, y.y, v[4 * e + 1]);
-          v[4 * e + 2] = fmaf(k, y.z, v[4 * e + 2]);
-          v[4 * e + 3] = fmaf(k, y.w, v[4 * e + 3]);
+      for (int i = 0; i < kBatch; ++i) {
+        x[i] = make_float2(-INFINITY, 0.f);
+        if (i0 + i < n_src) {
+          const int b = b0 + (i0 + i) / groups, g = two ? halfb : (i0 + i) % groups;
+          const float* part = parts + (size_t)(2 * b + (b == b0 ? 1 : 0)) * T::kPiece;
+          x[i] = __ldcg(reinterpret_cast<const float2*>(part + (size_t)2 * 128 * D) + g * 128 + row);
+          y[i] = __ldcg(reinterpret_cast<const float4*>(part) + ((size_t)g * (D / 4) + ch0 / 4) * 128 + row);
+        }
+      }
+      float top = big;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) top = fmaxf(top, x[i].x);
+      const float down = big == -INFINITY ? (sum == 0.f ? 0.f : 1.f) : exp2_approx(big - top);
+      big = top;
+      sum *= down;
+      v.x *= down; v.y *= down; v.z *= down; v.w *= down;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const float k = x[i].x == -INFINITY ? (x[i].y == 0.f ? 0.f : 1.f) : exp2_approx(x[i].x - big);
+        sum = fmaf(k, x[i].y, sum);
+        if (k != 0.f) {                                  // (a group without tiles left nothing)
+          v.x = fmaf(k, y[i].x, v.x);
+          v.y = fmaf(k, y[i].y, v.y);
+          v.z = fmaf(k, y[i].z, v.z);
+          v.w = fmaf(k, y[i].w, v.w);
         }
       }
     }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  uint32_t w[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) w[e] = sum == 0.f ? 0u : pack16<kBf16>(v[2 * e] * inv, v[2 * e + 1] * inv);
-  uint4* op = reinterpret_cast<uint4*>(a.out + s * a.out_seq + node * a.out_row + hq * a.out_head + ch0);
-  op[0] = make_uint4(w[0], w[1], w[2], w[3]);
-  op[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  *reinterpret_cast<uint2*>(a.out + s * a.out_seq + node * a.out_row + hq * a.out_head + ch0) =
+      sum == 0.f ? make_uint2(0u, 0u)
+                 : make_uint2(pack16<kBf16>(v.x * inv, v.y * inv), pack16<kBf16>(v.z * inv, v.w * inv));
   if (a.lse && ch0 == 0)
     a.lse[s * a.lse_seq + node * a.lse_row + hq * a.lse_head] = sum == 0.f ? -INFINITY : (big + log2f(sum)) * kTrLn2;
 }
@@ -881,7 +927,7 @@ static cudaError_t tree_launch(const KvView& c, const KvAttendArgs& a, int sms, 
   const cudaError_t e = launch_pdl(kv_tree_kernel<D, kBf16>, dim3(grid), dim3(kTrThreads), Tree<D>::kBytes, st, c, a);
   if (e != cudaSuccess) return e;
   const int items = c.n_seq * c.n_kv * ((a.m * a.group + 255) / 256);
-  return launch_pdl(kv_tree_join_kernel<D, kBf16>, dim3(items, 2 * (D / 32)), dim3(256), Tree<D>::kCum, st, c, a, grid);
+  return launch_pdl(kv_tree_join_kernel<D, kBf16>, dim3(items, 2 * (D / 16)), dim3(512), Tree<D>::kCum, st, c, a, grid);
 }
 
 cudaError_t launch_kv_tree(const KvView& c, const KvAttendArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st) {
