@@ -7,10 +7,14 @@
 //   warps 0-3, 4-7   softmax: one row per thread.  Two groups of 128 rows A and B, or, where the
 //                    block has 128 rows or fewer, the same rows twice: A takes the even tiles
 //                    and B the odd ones, each with sums of its own.
-//   warps 8-15       decode: codes, scales and offsets from global memory, a tile ahead in
-//                    registers, to f16 in the 128-byte-swizzled layout the products read
-//   warp 16          issues the products: S = Q K^T (A and Q from shared memory) and O += P V
-//                    (P from TMEM, where the softmax warps put it over the scores)
+//   warps 8-11       decode, a slot per thread: codes from global memory (a tile ahead, each
+//                    thread's in a place of its own in shared memory), scales and offsets (two
+//                    tiles ahead), to f16 in the 128-byte-swizzled layout the products read
+//   warp 12          issues the products: S = Q K^T (from shared memory) and O += P V (P from
+//                    TMEM, where the softmax warps put it over the scores); warps 13-15 only
+//                    complete its group, which gives the softmax warps its registers: 192 each,
+//                    so that a thread holds its row's 128 scores between the maximum and the
+//                    exponentials instead of reading them twice
 // While A's scores go through the exponentials the tensor core works on B's tile and the other
 // way round.  Keys are the product's N operand as they lie (channels contiguous), values the N operand with
 // channels contiguous as well (transposed operand), so both have the same layout and neither
@@ -38,7 +42,10 @@ namespace oilbird {
 namespace {
 
 constexpr int kTrTile = 128, kTrFront = 4;               // slots a tile; see TileListOf
-constexpr int kTrSoftThreads = 256, kTrDecWarps = 8, kTrThreads = kTrSoftThreads + 32 * kTrDecWarps + 32;
+constexpr int kTrDecWarps = 4, kTrIssuer = 12, kTrThreads = 512;
+// registers a thread: launched with 128; the four warpgroups' shares add up to 4 x 128
+constexpr int kTrSoftRegs = 192, kTrDecRegs = 96, kTrIssueRegs = 32;
+static_assert(2 * kTrSoftRegs + kTrDecRegs + kTrIssueRegs == 4 * 128, "more registers than the block was launched with");
 using TreeList = TileListOf<kTrTile, kTrFront, 0>;
 constexpr float kTrLn2 = 0.6931471805599453f;
 
@@ -107,20 +114,33 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
       ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
 }
-__device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&v)[32]) {
-  uint32_t r[32];
+// 32 columns of the warp's lanes; the values are there after tmem_wait32 on them
+__device__ __forceinline__ void tmem_ask32(uint32_t addr, uint32_t* r) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
       "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
       "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(addr));
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_wait32(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :: "memory");
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&v)[32]) {
+  uint32_t r[32];
+  tmem_ask32(addr, r);
+  tmem_wait32(r);
 #pragma unroll
   for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]) {
   asm volatile(
@@ -168,13 +188,13 @@ __device__ __forceinline__ constexpr uint32_t idesc_f16(int n, bool transposed) 
 struct TileInfo {                    // what the softmax warps need to know of a tile
   uint32_t valid[4];                 // slots that exist (cached tiles)
   float key_scale, value_exp, value_scale;   // 2^Ek, Ev, 2^-Ev
-  int flags;                         // 1: new nodes, 2: some slot is not valid, 4: a value is not finite
+  uint8_t flags[4];                  // by decoding warp; 1: new nodes, 2: some slot is not valid, 4: a value is not finite
 };
 struct TreeShared {
   uint64_t kfull[2], kfree[2], vfull[2], vfree[2], sfull[2], pfull[2], pvdone[2], info_full[4], qfull;
   uint64_t meet, peaks[2];           // the softmax warps; the decoding warps, by tile parity
   TileInfo info[4];
-  uint32_t peak[2][kTrDecWarps][2];  // largest key and value bound each decoding warp saw
+  uint32_t peak[4][kTrDecWarps][2];  // by tile: largest key and value bound each decoding warp saw
   uint32_t tmem;
   int gave_up;
   float2 ml[128];                    // group B's sums on their way to A
@@ -184,8 +204,10 @@ template <int D>
 struct Tree {
   static constexpr int kBlocks = D / 64, kMat = kBlocks * kTrTile * 128;     // one tile of K or V in f16
   static constexpr int kQMat = kBlocks * 256 * 128;
-  static constexpr int kCum = (kKvMaxSeq + 1) * 8 + 32 * 8 + kKvMaxSeq * 5;
-  static constexpr int kBytes = 1024 + 4 * kMat + kQMat + (int)sizeof(TreeShared) + 64 + kCum;
+  static constexpr int kCum = (kKvMaxSeq + 1) * 8 + 16 * 8 + kKvMaxSeq * 5;
+  static constexpr int kCodes = kBlocks * 64 + 16;                           // a slot's codes; spread over the banks
+  static constexpr int kBytes = 1024 + 4 * kMat + kQMat + kTrTile * kCodes + (int)sizeof(TreeShared) + 16 + kCum;
+  static_assert(kBytes <= 227 * 1024, "shared memory");
   // a piece in the workspace: accumulators [group][D / 4][128 rows][4], then (m, l) [group][128 rows]
   static constexpr size_t kPiece = (size_t)2 * 128 * (D + 2);
 };
@@ -252,8 +274,9 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
   extern __shared__ unsigned char raw_smem[];
   unsigned char* smem = raw_smem + ((1024 - (kv_smem(raw_smem) & 1023)) & 1023);
   unsigned char *vmat = smem, *kmat = smem + 2 * T::kMat, *qmat = smem + 4 * T::kMat;
-  TreeShared& sh = *reinterpret_cast<TreeShared*>(qmat + T::kQMat);
-  long long* cum = reinterpret_cast<long long*>(qmat + T::kQMat + (sizeof(TreeShared) + 15) / 16 * 16);
+  unsigned char* codes = qmat + T::kQMat;
+  TreeShared& sh = *reinterpret_cast<TreeShared*>(codes + kTrTile * T::kCodes);
+  long long* cum = reinterpret_cast<long long*>(codes + kTrTile * T::kCodes + (sizeof(TreeShared) + 15) / 16 * 16);
   long long* scratch = cum + kKvMaxSeq + 1;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   DeviceStats* stats = &reinterpret_cast<KvWork*>(c.work)->stats;
@@ -276,7 +299,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
     sh.gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 16) {
+  if (warp == kTrIssuer) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(kv_smem(&sh.tmem)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -288,7 +311,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
 
   TreeList list;
   list.cum = cum;
-  list.len = reinterpret_cast<int*>(scratch + 32);
+  list.len = reinterpret_cast<int*>(scratch + 16);
   list.nodes = reinterpret_cast<unsigned char*>(list.len + kKvMaxSeq);
   list.items = c.n_kv * ((a.m * a.group + 255) / 256);
   list.group = a.group;
@@ -306,6 +329,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
 
   if (warp < 8) {
     // ============================================================ softmax ========
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kTrSoftRegs));
     const int wg = warp >> 2, row = tid & 127;           // row of the group
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;   // TMEM lanes of this warp
     const uint32_t s_tm = tmem + lanes + wg * 256, o_tm = s_tm + 128;
@@ -330,16 +354,17 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
       if (p.n > 0) {
         // ---- the row as an operand ----
         const uint16_t* qp = a.q.at(p.s, node, hq);
-        float top = 0.f;
+        uint4 qw[D / 8];
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) {
-          uint4 w = make_uint4(0, 0, 0, 0);
-          if (have) w = *reinterpret_cast<const uint4*>(qp + i * 8);
+          qw[i] = make_uint4(0, 0, 0, 0);
+          if (have) qw[i] = *reinterpret_cast<const uint4*>(qp + i * 8);
+        }
+        float top = 0.f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t x = (&w.x)[e];
-            top = abs_max(abs_max(top, half_lo<kBf16>(x)), half_hi<kBf16>(x));
-          }
+        for (int i = 0; i < D / 2; ++i) {
+          const uint32_t x = (&qw[i >> 2].x)[i & 3];
+          top = abs_max(abs_max(top, half_lo<kBf16>(x)), half_hi<kBf16>(x));
         }
         const int e0 = top < INFINITY ? min(row_exponent(top), 126) : 0;
         const float up = a.scale < 0.f ? -pow2(-e0) : pow2(-e0);
@@ -348,12 +373,10 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
           unsigned char* qm = qmat + (wg * 128 + row) * 128;
 #pragma unroll
           for (int i = 0; i < D / 8; ++i) {
-            uint4 w = make_uint4(0, 0, 0, 0);
-            if (have) w = *reinterpret_cast<const uint4*>(qp + i * 8);
             uint4 h;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const uint32_t x = (&w.x)[e];
+              const uint32_t x = (&qw[i].x)[e];
               (&h.x)[e] = pack16<false>(half_lo<kBf16>(x) * up, half_hi<kBf16>(x) * up);
             }
             *reinterpret_cast<uint4*>(qm + (i >> 3) * (256 * 128) + (((i & 7) ^ (row & 7)) << 4)) = h;
@@ -373,7 +396,9 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
               !warp_wait(&sh.sfull[wg], su & 1, gave_up, stats)) { ok = false; break; }
           fence_after();
           const TileInfo& info = sh.info[t & 3];
-          const int flags = info.flags;
+          uint32_t flags = *reinterpret_cast<const uint32_t*>(info.flags);
+          flags |= flags >> 16;
+          flags |= flags >> 8;
           const float g = f * info.key_scale, ev = info.value_exp;
           // which slots count for this row
           uint32_t see[4];
@@ -387,27 +412,19 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
             for (int k = 0; k < 4; ++k) see[k] = info.valid[k];
           }
           const bool masked = __any_sync(0xffffffffu, flags & 3);
-          float mx = -INFINITY;
+          uint32_t x[128];                               // the row's scores
+#pragma unroll
+          for (int k = 0; k < 4; ++k) tmem_ask32(s_tm + k * 32, x + k * 32);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) tmem_wait32(x + k * 32);
           if (masked) {
-#pragma unroll 1
-            for (int k = 0; k < 4; ++k) {
-              float x[32];
-              tmem_ld32(s_tm + k * 32, x);
-              const uint32_t b = k == 0 ? see[0] : k == 1 ? see[1] : k == 2 ? see[2] : see[3];
 #pragma unroll
-              for (int e = 0; e < 32; ++e) mx = fmaxf(mx, b >> e & 1 ? x[e] : -INFINITY);
-            }
-          } else {
-            float y[4] = {mx, mx, mx, mx};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              float x[32];
-              tmem_ld32(s_tm + k * 32, x);
-#pragma unroll
-              for (int e = 0; e < 16; ++e) y[e & 3] = max3(y[e & 3], x[2 * e], x[2 * e + 1]);
-            }
-            mx = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
+            for (int e = 0; e < 128; ++e) x[e] = see[e >> 5] >> (e & 31) & 1 ? x[e] : 0xff800000u;
           }
+          float y[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int e = 0; e < 64; ++e) y[e & 3] = max3(y[e & 3], __uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1]));
+          float mx = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
           mx = fmaf(mx, g, ev);
           if (__any_sync(0xffffffffu, mx > m + 8.f)) {
             const float mn = fmaxf(m, mx), down = mn == -INFINITY ? 1.f : exp2_approx(m - mn);
@@ -417,54 +434,30 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
               if (!warp_wait(&sh.pvdone[wg], (su - 1) & 1, gave_up, stats)) { ok = false; break; }
               fence_after();
 #pragma unroll 1
-              for (int k = 0; k < D; k += 32) {
-                float x[32];
-                tmem_ld32(o_tm + k, x);
-                uint32_t y[16];
+              for (int k = 0; k < D; k += 16) {
+                uint32_t r[16];
+                tmem_ld16(o_tm + k, r);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                  for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(x[h * 16 + e] * down);
-                  tmem_st16(o_tm + k + h * 16, y);
-                }
+                for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * down);
+                tmem_st16(o_tm + k, r);
               }
             }
           }
           const float shift = ev - (m == -INFINITY ? 0.f : m);
           float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
           const float2 g2 = make_float2(g, g), shift2 = make_float2(shift, shift);
-          if (masked) {
-#pragma unroll 1
-            for (int k = 0; k < 4; ++k) {
-              float x[32];
-              tmem_ld32(s_tm + k * 32, x);
-              const uint32_t b = k == 0 ? see[0] : k == 1 ? see[1] : k == 2 ? see[2] : see[3];
-              uint32_t y[16];
 #pragma unroll
-              for (int e = 0; e < 16; ++e) {
-                const float2 z = fma2(make_float2(x[2 * e], x[2 * e + 1]), g2, shift2);
-                const float2 p = make_float2(b >> (2 * e) & 1 ? exp2_approx(z.x) : 0.f,
-                                             b >> (2 * e + 1) & 1 ? exp2_approx(z.y) : 0.f);
-                sum[e & 1] = add2(sum[e & 1], p);
-                y[e] = pack16<false>(p.x, p.y);
-              }
-              tmem_st16(s_tm + k * 16, y);               // over scores already read
+          for (int k = 0; k < 4; ++k) {
+            uint32_t w[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int i2 = k * 32 + 2 * e;
+              const float2 z = fma2(make_float2(__uint_as_float(x[i2]), __uint_as_float(x[i2 + 1])), g2, shift2);
+              const float2 pr = make_float2(exp2_approx(z.x), exp2_approx(z.y));
+              sum[e & 1] = add2(sum[e & 1], pr);
+              w[e] = pack16<false>(pr.x, pr.y);
             }
-          } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              float x[32];
-              tmem_ld32(s_tm + k * 32, x);
-              uint32_t y[16];
-#pragma unroll
-              for (int e = 0; e < 16; ++e) {
-                const float2 z = fma2(make_float2(x[2 * e], x[2 * e + 1]), g2, shift2);
-                const float2 p = make_float2(exp2_approx(z.x), exp2_approx(z.y));
-                sum[e & 1] = add2(sum[e & 1], p);
-                y[e] = pack16<false>(p.x, p.y);
-              }
-              tmem_st16(s_tm + k * 16, y);
-            }
+            tmem_st16(s_tm + k * 16, w);                 // over the scores
           }
           sum[0] = add2(sum[0], sum[1]);
           l = fmaf(sum[0].x + sum[0].y, info.value_scale, l);
@@ -587,24 +580,17 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
       at += count;
       if (at < u1) list.advance(bc, count);
     }
-  } else if (warp < 16) {
+  } else if (warp < 8 + kTrDecWarps) {
     // ============================================================ decode =========
-    const int dw = warp - 8, sl = dw * 16 + (lane & 15), half = lane >> 4;   // slot, half of its 32 bytes
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTrDecRegs));
+    const int dw = warp - 8, sl = dw * 32 + lane;        // the thread's slot of every tile
+    const uint32_t my_codes = kv_smem(codes + sl * T::kCodes);
     uint32_t kt = 0;
     bool ok = true;
     for (int at = 0; at < u1 && ok;) {
       const int n_tiles = bc.item < bc.live ? bc.tiles : 1, count = min(n_tiles - bc.tile, u1 - at);
       const Piece p = piece_at(bc, count, c, a);
       const int32_t* table = c.table + (size_t)p.s * c.max_pages;
-      // what a thread holds of a tile: 16 bytes of codes and the meta of its slot, for K and V
-      // and each group; the next tile's are asked for before this one's are worked on
-      struct Held {
-        uint4 code[2][G];
-        uint32_t meta[2][G];
-        bool valid;
-      };
-      Held cur, next;
-      cur.valid = next.valid = false;
       const int first = p.nodes ? -1 : 0, cached = p.n + first;   // tile -1: the new nodes
       auto page_for = [&](int i) {
         const int slot = (p.c0 + i) * kTrTile + sl;
@@ -615,61 +601,104 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
         }
         return q;
       };
-      auto load = [&](Held& h, int q, int i) {
-        h.valid = q >= 0;
-        const unsigned char* b = c.pages + ((size_t)max(q, 0) * c.n_kv + p.head) * block_bytes;
-        const int in = ((p.c0 + i) * kTrTile + sl) & (page - 1);
+      auto block_of = [&](int q) { return c.pages + ((size_t)max(q, 0) * c.n_kv + p.head) * block_bytes; };
+      auto slot_in = [&](int i) { return ((p.c0 + i) * kTrTile + sl) & (page - 1); };
+      auto copy_codes = [&](int q, int i) {
+        const unsigned char* b = block_of(q) + slot_in(i) * 32;
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv)
 #pragma unroll
-          for (int g = 0; g < G; ++g) {
-            h.code[kv][g] = make_uint4(0, 0, 0, 0);
-            h.meta[kv][g] = 0u;
-            if (h.valid) {
-              const unsigned char* x = b + kv * (block_bytes / 2);
-              h.code[kv][g] = __ldcg(reinterpret_cast<const uint4*>(x + (g * page + in) * 32 + half * 16));
-              h.meta[kv][g] = __ldcg(reinterpret_cast<const uint32_t*>(x + (G * page * 8 + in * G + g) * 4));
-            }
-          }
+          for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              cp_async16(my_codes + (kv * G + g) * 32 + h * 16, b + kv * (block_bytes / 2) + g * page * 32 + h * 16, q < 0 ? 0 : 16);
+        cp_async_commit();
       };
-      int next_page = -1;
-      if (cached > 0) { load(cur, page_for(0), 0); next_page = page_for(1); }
+      auto load_meta_of = [&](uint32_t (&m)[2][G], int q, int i) {
+        const unsigned char* b = block_of(q) + (G * page * 8 + slot_in(i) * G) * 4;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          uint32_t w[G];
+#pragma unroll
+          for (int g = 0; g < G; ++g) w[g] = 0u;
+          if (q >= 0) load_meta<G>(b + kv * (block_bytes / 2), w);
+#pragma unroll
+          for (int g = 0; g < G; ++g) m[kv][g] = w[g];
+        }
+      };
+      // the warp's largest key and value of tile t (counted over pieces) for the other warps
+      auto post = [&](uint32_t t, uint32_t pk, uint32_t pv) {
+        pk = __reduce_max_sync(0xffffffffu, pk);
+        pv = __reduce_max_sync(0xffffffffu, pv);
+        if (lane == 0) {
+          sh.peak[t & 3][dw][0] = pk;
+          sh.peak[t & 3][dw][1] = pv;
+          bar_arrive(&sh.peaks[t & 1]);
+        }
+        __syncwarp();
+      };
+      auto post_meta = [&](uint32_t t, const uint32_t (&m)[2][G]) {
+        uint32_t pk = 0, pv = 0;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          pk = max(pk, meta_peak<kBf16>(m[0][g]));
+          pv = max(pv, meta_peak<kBf16>(m[1][g]));
+        }
+        post(t, pk, pv);
+      };
+      auto peaks_of = [&](uint32_t t, int& ek, int& ev) {
+        uint32_t pk = 0, pv = 0;
+#pragma unroll
+        for (int w = 0; w < kTrDecWarps; ++w) { pk = max(pk, sh.peak[t & 3][w][0]); pv = max(pv, sh.peak[t & 3][w][1]); }
+        ek = peak_exp(pk);
+        ev = peak_exp(pv);
+      };
+      // Ahead of tile i: the codes of i + 1, scales and offsets (and posted peaks) of i + 1 and
+      // i + 2, the page of i + 3.
+      uint32_t mc[2][G], mn[2][G];
+      int page_c = -1, page_n = -1, page_2 = -1;
+      if (cached > 0) {
+        page_c = page_for(0);
+        page_n = page_for(1);
+        page_2 = page_for(2);
+        copy_codes(page_c, 0);
+        load_meta_of(mc, page_c, 0);
+        load_meta_of(mn, page_n, 1);
+        if (!p.nodes) post_meta(kt, mc);
+      }
       for (int i = first; i < cached; ++i, ++kt) {
         const int st = kt & 1;
         const uint32_t ph = (kt >> 1) & 1;
         TileInfo& info = sh.info[kt & 3];
         unsigned char *km = kmat + st * T::kMat, *vm = vmat + st * T::kMat;
         if (i >= 0) {
-          load(next, next_page, i + 1);                  // (zeros behind the last)
-          next_page = page_for(i + 2);
-          uint32_t pk = 0, pv = 0;
+          if (i + 1 < cached) post_meta(kt + 1, mn);
+          uint32_t m2[2][G];
+          load_meta_of(m2, page_2, i + 2);
+          const int page_3 = page_for(i + 3);
+          cp_async_wait<0>();                            // (a thread reads its own copies alone)
+          uint4 code[2][G][2];
 #pragma unroll
-          for (int g = 0; g < G; ++g) {
-            pk = max(pk, meta_peak<kBf16>(cur.meta[0][g]));
-            pv = max(pv, meta_peak<kBf16>(cur.meta[1][g]));
-          }
-          pk = __reduce_max_sync(0xffffffffu, pk);
-          pv = __reduce_max_sync(0xffffffffu, pv);
-          const uint32_t ballot = __ballot_sync(0xffffffffu, cur.valid) & 0xffffu;
-          if (lane == 0) { sh.peak[st][dw][0] = pk; sh.peak[st][dw][1] = pv; }
-          // (the tile before the one before last is done with: its peaks and, four tiles back,
-          // its info may be overwritten)
-          if (!warp_wait(&sh.kfree[st], ph ^ 1, gave_up, stats)) { ok = false; break; }
+          for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+                code[kv][g][h] = *reinterpret_cast<const uint4*>(codes + sl * T::kCodes + (kv * G + g) * 32 + h * 16);
+          if (i + 1 < cached) copy_codes(page_n, i + 1);
+          const uint32_t ballot = __ballot_sync(0xffffffffu, page_c >= 0);
+          // (free: so is, four tiles back, the place of the tile's info)
+          if (!warp_wait(&sh.kfree[st], ph ^ 1, gave_up, stats) || !warp_wait(&sh.peaks[st], ph, gave_up, stats)) { ok = false; break; }
+          int ek, ev;
+          peaks_of(kt, ek, ev);
           if (lane == 0) {
-            reinterpret_cast<uint16_t*>(info.valid)[dw] = (uint16_t)ballot;
-            if (dw == 0) info.flags = 0;
-          }
-          __syncwarp();
-          if (lane == 0) bar_arrive(&sh.peaks[st]);
-          if (!warp_wait(&sh.peaks[st], ph, gave_up, stats)) { ok = false; break; }
-#pragma unroll
-          for (int w = 0; w < kTrDecWarps; ++w) { pk = max(pk, sh.peak[st][w][0]); pv = max(pv, sh.peak[st][w][1]); }
-          const int ek = peak_exp(pk), ev = peak_exp(pv);
-          if (ballot != 0xffffu && lane == 0) atomicOr(&info.flags, 2);
-          if (dw == 0 && lane == 0) {
-            info.key_scale = pow2(ek);
-            info.value_exp = (float)ev;
-            info.value_scale = pow2(-ev);
+            info.valid[dw] = ballot;
+            info.flags[dw] = ballot != 0xffffffffu ? 2 : 0;
+            if (dw == 0) {
+              info.key_scale = pow2(ek);
+              info.value_exp = (float)ev;
+              info.value_scale = pow2(-ev);
+            }
           }
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv) {
@@ -677,13 +706,13 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
             const float down = pow2(-(kv ? ev : ek));
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-              const uint32_t m2 = cur.meta[kv][g];
-              const float fs = half_lo<kBf16>(m2) * down, fl = half_hi<kBf16>(m2) * down;
+              const uint32_t m1 = mc[kv][g];
+              const float fs = half_lo<kBf16>(m1) * down, fl = half_hi<kBf16>(m1) * down;
               const __half2 sc = as_half2(pack16<false>(fs, fs)), lo = as_half2(pack16<false>(fl, fl));
               unsigned char* dst = (kv ? vm : km) + g * (kTrTile * 128) + sl * 128;
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                *reinterpret_cast<uint4*>(dst + (((half * 4 + k) ^ (sl & 7)) << 4)) = decode8((&cur.code[kv][g].x)[k], sc, lo);
+              for (int k = 0; k < 8; ++k)
+                *reinterpret_cast<uint4*>(dst + ((k ^ (sl & 7)) << 4)) = decode8((&code[kv][g][k >> 2].x)[k & 3], sc, lo);
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
@@ -693,71 +722,79 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
             }
           }
           if (!ok) break;
-          cur = next;
+          page_c = page_n;
+          page_n = page_2;
+          page_2 = page_3;
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+            for (int g = 0; g < G; ++g) { mc[kv][g] = mn[kv][g]; mn[kv][g] = m2[kv][g]; }
         } else {
           // ---- new nodes: 16-bit elements, slots 0..63 of the tile; the rest is zero ----
           const bool node = sl < bc.nodes;
           const uint16_t* src[2] = {a.k.at(p.s, node ? sl : 0, p.head), a.v.at(p.s, node ? sl : 0, p.head)};
           uint32_t peak[2] = {0u, 0u};
           bool odd = false;
-          for (int kv = 0; kv < 2; ++kv)
-            for (int k = 0; k < D / 16; ++k) {           // the thread's half of the channels, 8 at a time
-              const int ch = (k >> 2) * 64 + half * 32 + (k & 3) * 8;
-              uint4 w = make_uint4(0, 0, 0, 0);
-              if (node) w = *reinterpret_cast<const uint4*>(src[kv] + ch);
 #pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const uint32_t x = (&w.x)[e >> 1];
-                const float v = fabsf(e & 1 ? half_hi<kBf16>(x) : half_lo<kBf16>(x));
-                if (v < INFINITY) peak[kv] = max(peak[kv], __float_as_uint(v));
-                else odd |= kv == 1;
-              }
+          for (int b = 0; b < D / 32; ++b) {             // 8 x 16 bytes at a time: half a row of K, then of V
+            const int kv = b / (D / 64), c0 = b % (D / 64) * 64;
+            uint4 w[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              w[k] = make_uint4(0, 0, 0, 0);
+              if (node) w[k] = *reinterpret_cast<const uint4*>(src[kv] + c0 + k * 8);
             }
-          peak[0] = __reduce_max_sync(0xffffffffu, peak[0]);
-          peak[1] = __reduce_max_sync(0xffffffffu, peak[1]);
+#pragma unroll
+            for (int e = 0; e < 64; ++e) {
+              const uint32_t x = (&w[e >> 3].x)[e >> 1 & 3];
+              const float v = fabsf(e & 1 ? half_hi<kBf16>(x) : half_lo<kBf16>(x));
+              if (v < INFINITY) peak[kv] = max(peak[kv], __float_as_uint(v));
+              else odd |= kv == 1;
+            }
+          }
           odd = __any_sync(0xffffffffu, odd);
-          const uint32_t ballot = __ballot_sync(0xffffffffu, node) & 0xffffu;
-          if (lane == 0) { sh.peak[st][dw][0] = peak[0]; sh.peak[st][dw][1] = peak[1]; }
-          if (!warp_wait(&sh.kfree[st], ph ^ 1, gave_up, stats) || !warp_wait(&sh.vfree[st], ph ^ 1, gave_up, stats)) {
+          const uint32_t ballot = __ballot_sync(0xffffffffu, node);
+          post(kt, peak[0], peak[1]);
+          if (cached > 0) post_meta(kt + 1, mc);
+          if (!warp_wait(&sh.kfree[st], ph ^ 1, gave_up, stats) || !warp_wait(&sh.vfree[st], ph ^ 1, gave_up, stats) ||
+              !warp_wait(&sh.peaks[st], ph, gave_up, stats)) {
             ok = false;
             break;
           }
+          int ek, ev;
+          peaks_of(kt, ek, ev);
           if (lane == 0) {
-            reinterpret_cast<uint16_t*>(info.valid)[dw] = (uint16_t)ballot;
-            if (dw == 0) info.flags = 1;
+            info.valid[dw] = ballot;
+            info.flags[dw] = 1 | (odd ? 4 : 0);
+            if (dw == 0) {
+              info.key_scale = pow2(ek);
+              info.value_exp = (float)ev;
+              info.value_scale = pow2(-ev);
+            }
           }
-          __syncwarp();
-          if (lane == 0) bar_arrive(&sh.peaks[st]);
-          if (!warp_wait(&sh.peaks[st], ph, gave_up, stats)) { ok = false; break; }
 #pragma unroll
-          for (int w = 0; w < kTrDecWarps; ++w) {
-            peak[0] = max(peak[0], sh.peak[st][w][0]);
-            peak[1] = max(peak[1], sh.peak[st][w][1]);
-          }
-          const int ek = peak_exp(peak[0]), ev = peak_exp(peak[1]);
-          if (odd && lane == 0) atomicOr(&info.flags, 4);
-          if (dw == 0 && lane == 0) {
-            info.key_scale = pow2(ek);
-            info.value_exp = (float)ev;
-            info.value_scale = pow2(-ev);
-          }
-          for (int kv = 0; kv < 2; ++kv) {
+          for (int b = 0; b < D / 32; ++b) {
+            const int kv = b / (D / 64), blk = b % (D / 64);
             const float down = pow2(-(kv ? ev : ek));
-            for (int k = 0; k < D / 16; ++k) {
-              const int ch = (k >> 2) * 64 + half * 32 + (k & 3) * 8;
-              uint4 w = make_uint4(0, 0, 0, 0), h;
-              if (node) w = *reinterpret_cast<const uint4*>(src[kv] + ch);
+            uint4 w[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              w[k] = make_uint4(0, 0, 0, 0);
+              if (node) w[k] = *reinterpret_cast<const uint4*>(src[kv] + blk * 64 + k * 8);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              uint4 h;
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                float v0 = half_lo<kBf16>((&w.x)[e]) * down, v1 = half_hi<kBf16>((&w.x)[e]) * down;
+                float v0 = half_lo<kBf16>((&w[k].x)[e]) * down, v1 = half_hi<kBf16>((&w[k].x)[e]) * down;
                 if (kv) {
                   v0 = fabsf(v0) < INFINITY ? v0 : 0.f;
                   v1 = fabsf(v1) < INFINITY ? v1 : 0.f;
                 }
                 (&h.x)[e] = pack16<false>(v0, v1);
               }
-              *reinterpret_cast<uint4*>((kv ? vm : km) + (k >> 2) * (kTrTile * 128) + sl * 128 +
-                                        (((half * 4 + (k & 3)) ^ (sl & 7)) << 4)) = h;
+              *reinterpret_cast<uint4*>((kv ? vm : km) + blk * (kTrTile * 128) + sl * 128 + ((k ^ (sl & 7)) << 4)) = h;
             }
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -772,10 +809,12 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
       at += count;
       if (at < u1) list.advance(bc, count);
     }
+    cp_async_wait<0>();
   } else {
     // ============================================================ products =======
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTrIssueRegs));
     uint32_t kt = 0, np = 0, pu[2] = {0, 0};
-    bool ok = true;
+    bool ok = warp == kTrIssuer;
     constexpr uint32_t s_idesc = idesc_f16(kTrTile, false), o_idesc = idesc_f16(D, true);
     for (int at = 0; at < u1 && ok;) {
       const int n_tiles = bc.item < bc.live ? bc.tiles : 1, count = min(n_tiles - bc.tile, u1 - at);
@@ -830,7 +869,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
     }
     // what was issued is done before the memory goes away: the softmax warps waited for the last
     // products, unless somebody gave up
-    if (*gave_up) {
+    if (warp == kTrIssuer && *gave_up) {
       const unsigned long long t0 = now_ns();
       while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
     }
@@ -838,7 +877,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
   fence_before();
   __syncthreads();
   fence_after();
-  if (warp == 16)
+  if (warp == kTrIssuer)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
@@ -854,7 +893,7 @@ kv_tree_join_kernel(const KvView c, const KvAttendArgs a, int tree_ctas) {
   pdl_enter();
   TreeList list;
   list.cum = cum;
-  list.len = reinterpret_cast<int*>(scratch + 32);
+  list.len = reinterpret_cast<int*>(scratch + 16);
   list.nodes = reinterpret_cast<unsigned char*>(list.len + kKvMaxSeq);
   list.items = c.n_kv * ((a.m * a.group + 255) / 256);
   list.group = a.group;
