@@ -306,7 +306,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
   fence_before();
   __syncthreads();
   fence_after();
-  const uint32_t tmem = sh.tmem;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
   pdl_enter();
 
   TreeList list;
@@ -816,6 +816,13 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
     uint32_t kt = 0, np = 0, pu[2] = {0, 0};
     bool ok = warp == kTrIssuer;
     constexpr uint32_t s_idesc = idesc_f16(kTrTile, false), o_idesc = idesc_f16(D, true);
+    // Descriptors are formed here, the same in every lane, and only a constant is added where
+    // one lane issues: what that lane computed for itself would have to be moved to uniform
+    // registers for every product.
+    const uint64_t q_desc = desc128(kv_smem(qmat), 16), k_desc = desc128(kv_smem(kmat), 16),
+                   v_desc = desc128(kv_smem(vmat), kTrTile * 128);
+    constexpr uint64_t kStage = T::kMat >> 4;
+    const bool issuer = one_lane();
     for (int at = 0; at < u1 && ok;) {
       const int n_tiles = bc.item < bc.live ? bc.tiles : 1, count = min(n_tiles - bc.tile, u1 - at);
       const Piece p = piece_at(bc, count, c, a);
@@ -829,12 +836,13 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
           if (!p.two || wg == 0) ok = ok && warp_wait(&sh.kfull[st], (t >> 1) & 1, gave_up, stats);
           if (!ok) return;
           fence_after();
-          const uint32_t qa = kv_smem(qmat) + (p.two ? wg * 128 * 128 : 0), ka = kv_smem(kmat + st * T::kMat);
-          if (one_lane()) {
+          const uint64_t qd = q_desc + (p.two && wg ? (uint64_t)(128 * 128 >> 4) : 0), kd = k_desc + (st ? kStage : 0);
+          const uint32_t to = tmem + wg * 256;
+          if (issuer) {
 #pragma unroll
             for (int k = 0; k < D / 16; ++k)
-              mma_ss(tmem + wg * 256, desc128(qa + (k >> 2) * (256 * 128) + (k & 3) * 32, 16),
-                     desc128(ka + (k >> 2) * (kTrTile * 128) + (k & 3) * 32, 16), s_idesc, k > 0);
+              mma_ss(to, qd + (uint64_t)((k >> 2) * (256 * 128 >> 4) + (k & 3) * 2),
+                     kd + (uint64_t)((k >> 2) * (kTrTile * 128 >> 4) + (k & 3) * 2), s_idesc, k > 0);
             commit(&sh.sfull[wg]);
             if (!p.two || wg == 1) commit(&sh.kfree[st]);
           }
@@ -850,12 +858,12 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
           if (!ok) break;
           ++pu[wg];
           fence_after();
-          const uint32_t va = kv_smem(vmat + st * T::kMat);
-          if (one_lane()) {
+          const uint64_t vd = v_desc + (st ? kStage : 0);
+          const uint32_t to = tmem + wg * 256 + 128, from = tmem + wg * 256, add = u > 1;
+          if (issuer) {
 #pragma unroll
             for (int k = 0; k < kTrTile / 16; ++k)
-              mma_ts(tmem + wg * 256 + 128, tmem + wg * 256 + k * 8, desc128(va + k * 2048, kTrTile * 128), o_idesc,
-                     u > 1 || k > 0);
+              mma_ts(to, from + k * 8, vd + (uint64_t)(k * (2048 >> 4)), o_idesc, k > 0 ? 1u : add);
             commit(&sh.pvdone[wg]);
             if (!p.two || wg == 1) commit(&sh.vfree[st]);
           }
