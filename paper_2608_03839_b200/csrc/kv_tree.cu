@@ -348,39 +348,49 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
       bool odd_values = false;                           // new nodes' values that are not finite
       const int my_row = p.row0 + (p.two ? wg * 128 : 0) + row;
       const bool have = my_row < p.n_rows;
-      const int node = have ? my_row / a.group : 0, hq = p.head * a.group + (have ? my_row % a.group : 0);
+      const int node = have ? my_row / a.group : 0;
       // (both groups have left the piece before: its scores, its accumulators and its Q are free)
       if (!meet()) break;
       if (p.n > 0) {
         // ---- the row as an operand ----
-        const uint16_t* qp = a.q.at(p.s, node, hq);
-        uint4 qw[D / 8];
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-          qw[i] = make_uint4(0, 0, 0, 0);
-          if (have) qw[i] = *reinterpret_cast<const uint4*>(qp + i * 8);
+        // Raw rows are copied to where their f16 will lie (16 bits either way), whole lines at a
+        // time, and turned into f16 in place.  Short loops throughout: this code runs once a
+        // piece, and fetching straight-line code took longer than the work.  (Group B copies
+        // the rows for itself even where A's are the operand: it needs their exponents.)
+        unsigned char* my_q = qmat + (wg * 128 + row) * 128;
+#pragma unroll 2
+        for (int i = lane; i < 32 * (D / 8); i += 32) {
+          const int r = (warp & 3) * 32 + i / (D / 8), chunk = i % (D / 8), gr = p.row0 + (p.two ? wg * 128 : 0) + r;
+          const bool in = gr < p.n_rows;
+          const uint16_t* src = a.q.at(p.s, in ? gr / a.group : 0, p.head * a.group + (in ? gr % a.group : 0)) + chunk * 8;
+          cp_async16(kv_smem(qmat + (chunk >> 3) * (256 * 128) + (wg * 128 + r) * 128 + (((chunk & 7) ^ (r & 7)) << 4)), src, in ? 16 : 0);
         }
+        cp_async_commit();
+        cp_async_wait<0>();
+        __syncwarp();
         float top = 0.f;
+#pragma unroll 2
+        for (int i = 0; i < D / 8; ++i) {
+          const uint4 w = *reinterpret_cast<const uint4*>(my_q + (i >> 3) * (256 * 128) + (((i & 7) ^ (row & 7)) << 4));
 #pragma unroll
-        for (int i = 0; i < D / 2; ++i) {
-          const uint32_t x = (&qw[i >> 2].x)[i & 3];
-          top = abs_max(abs_max(top, half_lo<kBf16>(x)), half_hi<kBf16>(x));
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t x = (&w.x)[e];
+            top = abs_max(abs_max(top, half_lo<kBf16>(x)), half_hi<kBf16>(x));
+          }
         }
         const int e0 = top < INFINITY ? min(row_exponent(top), 126) : 0;
         const float up = a.scale < 0.f ? -pow2(-e0) : pow2(-e0);
         const float f = fmaxf(fabsf(a.scale) * kLog2e * pow2(e0), 1e-37f);
-        if (p.two || wg == 0) {
-          unsigned char* qm = qmat + (wg * 128 + row) * 128;
+#pragma unroll 2
+        for (int i = 0; i < D / 8; ++i) {
+          uint4* at_chunk = reinterpret_cast<uint4*>(my_q + (i >> 3) * (256 * 128) + (((i & 7) ^ (row & 7)) << 4));
+          uint4 w = *at_chunk;
 #pragma unroll
-          for (int i = 0; i < D / 8; ++i) {
-            uint4 h;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t x = (&qw[i].x)[e];
-              (&h.x)[e] = pack16<false>(half_lo<kBf16>(x) * up, half_hi<kBf16>(x) * up);
-            }
-            *reinterpret_cast<uint4*>(qm + (i >> 3) * (256 * 128) + (((i & 7) ^ (row & 7)) << 4)) = h;
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t x = (&w.x)[e];
+            (&w.x)[e] = pack16<false>(half_lo<kBf16>(x) * up, half_hi<kBf16>(x) * up);
           }
+          *at_chunk = w;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
@@ -412,15 +422,23 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
             for (int k = 0; k < 4; ++k) see[k] = info.valid[k];
           }
           const bool masked = __any_sync(0xffffffffu, flags & 3);
+          if (masked) {                                  // -inf where the row does not look
+#pragma unroll 1
+            for (int k = 0; k < 8; ++k) {
+              uint32_t r[16];
+              tmem_ld16(s_tm + k * 16, r);
+              const uint32_t b = (k < 2 ? see[0] : k < 4 ? see[1] : k < 6 ? see[2] : see[3]) >> (k & 1 ? 16 : 0);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) r[e] = b >> e & 1 ? r[e] : 0xff800000u;
+              tmem_st16(s_tm + k * 16, r);
+            }
+            tmem_wait_st();
+          }
           uint32_t x[128];                               // the row's scores
 #pragma unroll
           for (int k = 0; k < 4; ++k) tmem_ask32(s_tm + k * 32, x + k * 32);
 #pragma unroll
           for (int k = 0; k < 4; ++k) tmem_wait32(x + k * 32);
-          if (masked) {
-#pragma unroll
-            for (int e = 0; e < 128; ++e) x[e] = see[e >> 5] >> (e & 31) & 1 ? x[e] : 0xff800000u;
-          }
           float y[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
           for (int e = 0; e < 64; ++e) y[e & 3] = max3(y[e & 3], __uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1]));
@@ -731,40 +749,45 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
             for (int g = 0; g < G; ++g) { mc[kv][g] = mn[kv][g]; mn[kv][g] = m2[kv][g]; }
         } else {
           // ---- new nodes: 16-bit elements, slots 0..63 of the tile; the rest is zero ----
-          const bool node = sl < bc.nodes;
-          const uint16_t* src[2] = {a.k.at(p.s, node ? sl : 0, p.head), a.v.at(p.s, node ? sl : 0, p.head)};
-          uint32_t peak[2] = {0u, 0u};
-          bool odd = false;
-#pragma unroll
-          for (int b = 0; b < D / 32; ++b) {             // 8 x 16 bytes at a time: half a row of K, then of V
-            const int kv = b / (D / 64), c0 = b % (D / 64) * 64;
-            uint4 w[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              w[k] = make_uint4(0, 0, 0, 0);
-              if (node) w[k] = *reinterpret_cast<const uint4*>(src[kv] + c0 + k * 8);
-            }
-#pragma unroll
-            for (int e = 0; e < 64; ++e) {
-              const uint32_t x = (&w[e >> 3].x)[e >> 1 & 3];
-              const float v = fabsf(e & 1 ? half_hi<kBf16>(x) : half_lo<kBf16>(x));
-              if (v < INFINITY) peak[kv] = max(peak[kv], __float_as_uint(v));
-              else odd |= kv == 1;
-            }
-          }
-          odd = __any_sync(0xffffffffu, odd);
-          const uint32_t ballot = __ballot_sync(0xffffffffu, node);
-          post(kt, peak[0], peak[1]);
-          if (cached > 0) post_meta(kt + 1, mc);
-          if (!warp_wait(&sh.kfree[st], ph ^ 1, gave_up, stats) || !warp_wait(&sh.vfree[st], ph ^ 1, gave_up, stats) ||
-              !warp_wait(&sh.peaks[st], ph, gave_up, stats)) {
+          // raw rows copied to where their f16 will lie and turned into f16 in place, as Q's: a
+          // thread has one node's key or value
+          if (!warp_wait(&sh.kfree[st], ph ^ 1, gave_up, stats) || !warp_wait(&sh.vfree[st], ph ^ 1, gave_up, stats)) {
             ok = false;
             break;
           }
+          unsigned char* mat = dw < 2 ? km : vm;
+          const int r0 = (dw & 1) * 32, j = r0 + lane;
+#pragma unroll 2
+          for (int x = lane; x < 32 * (D / 8); x += 32) {
+            const int r = r0 + x / (D / 8), chunk = x % (D / 8);
+            const bool in = r < bc.nodes;
+            cp_async16(kv_smem(mat + (chunk >> 3) * (kTrTile * 128) + r * 128 + (((chunk & 7) ^ (r & 7)) << 4)),
+                       (dw < 2 ? a.k : a.v).at(p.s, in ? r : 0, p.head) + chunk * 8, in ? 16 : 0);
+          }
+          cp_async_commit();
+          cp_async_wait<0>();
+          __syncwarp();
+          uint32_t peak = 0;
+          bool odd = false;
+#pragma unroll 2
+          for (int x = 0; x < D / 8; ++x) {
+            const uint4 w = *reinterpret_cast<const uint4*>(mat + (x >> 3) * (kTrTile * 128) + j * 128 + (((x & 7) ^ (j & 7)) << 4));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const uint32_t y = (&w.x)[e >> 1];
+              const float v = fabsf(e & 1 ? half_hi<kBf16>(y) : half_lo<kBf16>(y));
+              if (v < INFINITY) peak = max(peak, __float_as_uint(v));
+              else odd = dw >= 2;
+            }
+          }
+          odd = __any_sync(0xffffffffu, odd);
+          post(kt, dw < 2 ? peak : 0u, dw < 2 ? 0u : peak);
+          if (cached > 0) post_meta(kt + 1, mc);
+          if (!warp_wait(&sh.peaks[st], ph, gave_up, stats)) { ok = false; break; }
           int ek, ev;
           peaks_of(kt, ek, ev);
           if (lane == 0) {
-            info.valid[dw] = ballot;
+            info.valid[dw] = dw > 1 ? 0u : (uint32_t)(((bc.nodes >= 64 ? 0ull : 1ull << bc.nodes) - 1ull) >> (32 * dw));
             info.flags[dw] = 1 | (odd ? 4 : 0);
             if (dw == 0) {
               info.key_scale = pow2(ek);
@@ -772,30 +795,22 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
               info.value_scale = pow2(-ev);
             }
           }
+          const float down = pow2(-(dw < 2 ? ek : ev));
+#pragma unroll 2
+          for (int x = 0; x < D / 8; ++x) {
+            uint4* at_chunk = reinterpret_cast<uint4*>(mat + (x >> 3) * (kTrTile * 128) + j * 128 + (((x & 7) ^ (j & 7)) << 4));
+            uint4 w = *at_chunk;
 #pragma unroll
-          for (int b = 0; b < D / 32; ++b) {
-            const int kv = b / (D / 64), blk = b % (D / 64);
-            const float down = pow2(-(kv ? ev : ek));
-            uint4 w[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              w[k] = make_uint4(0, 0, 0, 0);
-              if (node) w[k] = *reinterpret_cast<const uint4*>(src[kv] + blk * 64 + k * 8);
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              uint4 h;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                float v0 = half_lo<kBf16>((&w[k].x)[e]) * down, v1 = half_hi<kBf16>((&w[k].x)[e]) * down;
-                if (kv) {
-                  v0 = fabsf(v0) < INFINITY ? v0 : 0.f;
-                  v1 = fabsf(v1) < INFINITY ? v1 : 0.f;
-                }
-                (&h.x)[e] = pack16<false>(v0, v1);
+            for (int e = 0; e < 4; ++e) {
+              float v0 = half_lo<kBf16>((&w.x)[e]) * down, v1 = half_hi<kBf16>((&w.x)[e]) * down;
+              if (dw >= 2) {                             // values that are not finite: see `accumulators`
+                v0 = fabsf(v0) < INFINITY ? v0 : 0.f;
+                v1 = fabsf(v1) < INFINITY ? v1 : 0.f;
               }
-              *reinterpret_cast<uint4*>((kv ? vm : km) + blk * (kTrTile * 128) + sl * 128 + ((k ^ (sl & 7)) << 4)) = h;
+              (&w.x)[e] = pack16<false>(v0, v1);
             }
+            *at_chunk = w;
+            at_chunk[64 * 128 / 16] = make_uint4(0, 0, 0, 0);   // slots 64..127 of the tile
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
