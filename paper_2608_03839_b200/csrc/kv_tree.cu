@@ -358,12 +358,21 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
         // piece, and fetching straight-line code took longer than the work.  (Group B copies
         // the rows for itself even where A's are the operand: it needs their exponents.)
         unsigned char* my_q = qmat + (wg * 128 + row) * 128;
+        {
+          // rows are walked by steps: a division for each would take longer than its copy
+          constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
+          const int chunk = lane % kLanes, first = (warp & 3) * 32 + lane / kLanes;
+          int gr = p.row0 + (p.two ? wg * 128 : 0) + first, nd = gr / a.group, sb = gr - nd * a.group;
+          unsigned char* dst = qmat + (chunk >> 3) * (256 * 128) + (wg * 128 + first) * 128;
+          const uint16_t* src = a.q.at(p.s, 0, p.head * a.group) + chunk * 8;
 #pragma unroll 2
-        for (int i = lane; i < 32 * (D / 8); i += 32) {
-          const int r = (warp & 3) * 32 + i / (D / 8), chunk = i % (D / 8), gr = p.row0 + (p.two ? wg * 128 : 0) + r;
-          const bool in = gr < p.n_rows;
-          const uint16_t* src = a.q.at(p.s, in ? gr / a.group : 0, p.head * a.group + (in ? gr % a.group : 0)) + chunk * 8;
-          cp_async16(kv_smem(qmat + (chunk >> 3) * (256 * 128) + (wg * 128 + r) * 128 + (((chunk & 7) ^ (r & 7)) << 4)), src, in ? 16 : 0);
+          for (int i = 0; i < 32 / kAtOnce; ++i) {
+            const bool in = gr < p.n_rows;
+            cp_async16(kv_smem(dst + i * kAtOnce * 128 + (((chunk & 7) ^ ((first + i * kAtOnce) & 7)) << 4)),
+                       in ? src + nd * a.q.row + sb * a.q.head : src, in ? 16 : 0);
+            gr += kAtOnce;
+            for (sb += kAtOnce; sb >= a.group; sb -= a.group) ++nd;
+          }
         }
         cp_async_commit();
         cp_async_wait<0>();
