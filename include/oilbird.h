@@ -680,7 +680,7 @@ size_t  oilbird_kv_workspace_bytes(int32_t head_dim);
  * NULL: rows 0..n) are stored at slots seq_len[s].. with positions n_pos[s].., n = n_new[s] (dev;
  * NULL: `rows`).  weight: dev [n_seq, n_kv_heads, m] the rows' first weights, NULL: 0.  A row
  * that finds no page, or a select entry outside 0..m-1, is not stored (its slot counts) and is
- * counted in status().
+ * counted in status().  rows at most 2^24, as is read()'s n.
  */
 int oilbird_kv_append(const oilbird_kv_cache* cache, const oilbird_kv_rows* k,
                       const oilbird_kv_rows* v, int32_t m, int32_t rows, const int32_t* n_new,

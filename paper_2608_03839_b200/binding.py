@@ -885,6 +885,18 @@ def merge_chains(tree_tok: torch.Tensor, tree_parent: torch.Tensor, n_nodes: tor
 KV_BF16, KV_F16 = 0, 1
 KV_MAX_SEQ, KV_MAX_GROUP, KV_MAX_EVICT_SLOTS = 1024, 64, 851968
 _KV_DTYPES = {torch.bfloat16: KV_BF16, torch.float16: KV_F16}
+_KV_MASKS = (torch.int64, torch.uint64)
+_KV_ROWS = ctypes.c_int64 * 4          # the layout of CKVRows
+_KV_STRIDES = ctypes.c_int64 * 3
+
+
+def _raw_stream(index: int) -> int:
+    """Handle of the device's current stream."""
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+# the same without the Stream object (six microseconds), where torch offers it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream)
 
 
 def _kv_check(rc: int, where: str) -> None:
@@ -956,7 +968,8 @@ class KVCache:
         self.seq_len, self.n_pos, self.workspace = seq_len, n_pos, workspace
         self.dtype, self.head_dim, self.n_kv_heads = dtype, int(head_dim), int(weight.shape[1])
         self.n_seq, self.page_size = int(n_seq), int(weight.shape[2])
-        self._dev = dev
+        self._dev, self._index = dev, dev.index or 0
+        self._seqs, self._scale = (self.n_seq,), self.head_dim ** -0.5
         self._c = CKVCache(pages.data_ptr(), weight.data_ptr(), pos.data_ptr(),
                            page_table.data_ptr(), seq_len.data_ptr(), n_pos.data_ptr(),
                            workspace.data_ptr(), workspace.numel(), weight.shape[0], n_seq,
@@ -964,32 +977,48 @@ class KVCache:
                            _KV_DTYPES[dtype], dev.index or 0)
         self._ref = ctypes.byref(self._c)
 
-    def _rows(self, t: torch.Tensor, heads: int, m: int | None = None):
+    # (These run for every argument of every call, on the path that bounds small calls: one
+    # comparison for each property, and four integers in place of the struct of the same layout.)
+    def _rows(self, t: torch.Tensor, heads: int, m: int):
         """The C view of a [n_seq, m, heads, head_dim] tensor (any strides but the last)."""
-        shape, stride = t.shape, t.stride()
-        assert t.is_cuda and t.dtype == self.dtype and len(shape) == 4
-        assert shape[0] == self.n_seq and shape[2] == heads and shape[3] == self.head_dim
-        assert (m is None or shape[1] == m) and stride[3] == 1
-        return ctypes.byref(CKVRows(t.data_ptr(), stride[0], stride[1], stride[2]))
+        if t.dtype is self.dtype and t.shape == (self.n_seq, m, heads, self.head_dim) and t.is_cuda:
+            s0, s1, s2, s3 = t.stride()
+            if s3 == 1:
+                return _KV_ROWS(t.data_ptr(), s0, s1, s2)
+        raise AssertionError(f"a CUDA {self.dtype} tensor [{self.n_seq}, {m}, {heads}, {self.head_dim}] "
+                             "with contiguous channels")
 
-    def _vec(self, t, dtype, *shape):
+    def _vec(self, t, dtype, shape):
         """Pointer of an optional contiguous tensor of that type and shape."""
         if t is None:
             return None
-        assert t.is_cuda and t.dtype == dtype and t.shape == shape and t.is_contiguous()
+        if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+            raise AssertionError(f"a contiguous CUDA {dtype} tensor {list(shape)}")
         return t.data_ptr()
 
     def _lse(self, t, m, heads):
         """Pointer and strides of a [n_seq, m, heads] fp32 tensor."""
-        assert t.is_cuda and t.dtype == torch.float32 and t.shape == (self.n_seq, m, heads)
-        return t.data_ptr(), None if t.is_contiguous() else (ctypes.c_int64 * 3)(*t.stride())
+        if t.dtype is not torch.float32 or t.shape != (self.n_seq, m, heads) or not t.is_cuda:
+            raise AssertionError(f"a CUDA fp32 tensor [{self.n_seq}, {m}, {heads}]")
+        return t.data_ptr(), None if t.is_contiguous() else _KV_STRIDES(*t.stride())
 
     def _mask(self, mask, m):
         if mask is None:
             return None, 0
-        assert mask.is_cuda and mask.dtype in (torch.int64, torch.uint64)
-        assert mask.shape[0] == self.n_seq and mask.shape[1] >= m and mask.stride(1) == 1
+        shape = mask.shape
+        if mask.dtype not in _KV_MASKS or len(shape) != 2 or shape[0] != self.n_seq or shape[1] < m or \
+                not mask.is_cuda or mask.stride(1) != 1:
+            raise AssertionError(f"a CUDA int64 tensor [{self.n_seq}, {m} or more]")
         return mask.data_ptr(), mask.stride(0)
+
+    def _new(self, like: torch.Tensor, shape) -> torch.Tensor:
+        # (new_empty takes half the time of torch.empty with a type and a device)
+        return like.new_empty(shape) if ALLOC is _torch_empty else ALLOC(shape, like.dtype, self._dev)
+
+    def _stream(self, stream) -> int:
+        if stream is not None:
+            return stream.cuda_stream
+        return _raw_stream(self._index)
 
     def append(self, k: torch.Tensor, v: torch.Tensor, n_new: torch.Tensor | None = None,
                select: torch.Tensor | None = None, weight: torch.Tensor | None = None,
@@ -1002,19 +1031,19 @@ class KVCache:
             return
         rows = m if select is None else select.shape[1]
         _kv_check(self._L.oilbird_kv_append(
-            self._ref, self._rows(k, self.n_kv_heads), self._rows(v, self.n_kv_heads, m), m, rows,
-            self._vec(n_new, torch.int32, self.n_seq),
-            self._vec(select, torch.int32, self.n_seq, rows),
-            self._vec(weight, torch.float32, self.n_seq, self.n_kv_heads, m),
-            _stream_ptr(stream)), "oilbird_kv_append")
+            self._ref, self._rows(k, self.n_kv_heads, m), self._rows(v, self.n_kv_heads, m), m, rows,
+            self._vec(n_new, torch.int32, self._seqs),
+            self._vec(select, torch.int32, (self.n_seq, rows)),
+            self._vec(weight, torch.float32, (self.n_seq, self.n_kv_heads, m)),
+            self._stream(stream)), "oilbird_kv_append")
 
     def read(self, n: int, start: torch.Tensor | None = None, stream=None):
         """Slots start[s] .. start[s] + n - 1 (int32 [n_seq]; None: from 0) in 16 bits: (k, v), each
         [n_seq, n, n_kv_heads, head_dim]; zeros where a sequence has no slot."""
         shape = (self.n_seq, n, self.n_kv_heads, self.head_dim)
         k, v = ALLOC(shape, self.dtype, self._dev), ALLOC(shape, self.dtype, self._dev)
-        _kv_check(self._L.oilbird_kv_read(self._ref, n, self._vec(start, torch.int32, self.n_seq),
-                                          k.data_ptr(), v.data_ptr(), _stream_ptr(stream)),
+        _kv_check(self._L.oilbird_kv_read(self._ref, n, self._vec(start, torch.int32, self._seqs),
+                                          k.data_ptr(), v.data_ptr(), self._stream(stream)),
                   "oilbird_kv_read")
         return k, v
 
@@ -1026,19 +1055,19 @@ class KVCache:
         v_new [n_seq, m, n_kv_heads, head_dim], over the nodes that mask (int64 [n_seq, >= m], bit j:
         sees node j; None: nodes 0..i) names.  n_new: int32 [n_seq] nodes of each sequence (None: m).
         Returns (out, lse): out like q, lse fp32 [n_seq, m, n_q_heads] (natural logarithm)."""
-        m, heads = q.shape[1], q.shape[2]
+        _, m, heads, _ = q.shape
         if out is None:
-            out = ALLOC((self.n_seq, m, heads, self.head_dim), self.dtype, self._dev)
+            out = self._new(q, (self.n_seq, m, heads, self.head_dim))
         if lse is None:
-            lse = ALLOC((self.n_seq, m, heads), torch.float32, self._dev)
+            lse = self._new(self.weight, (self.n_seq, m, heads))
         mp, ms = self._mask(mask, m)
         _kv_check(self._L.oilbird_kv_attend(
-            self._ref, heads, m, self._rows(q, heads),
+            self._ref, heads, m, self._rows(q, heads, m),
             None if k_new is None else self._rows(k_new, self.n_kv_heads, m),
             None if v_new is None else self._rows(v_new, self.n_kv_heads, m), mp, ms,
-            self._vec(n_new, torch.int32, self.n_seq),
-            self.head_dim ** -0.5 if scale is None else scale, self._rows(out, heads, m),
-            *self._lse(lse, m, heads), _stream_ptr(stream)), "oilbird_kv_attend")
+            self._vec(n_new, torch.int32, self._seqs),
+            self._scale if scale is None else scale, self._rows(out, heads, m),
+            *self._lse(lse, m, heads), self._stream(stream)), "oilbird_kv_attend")
         return out, lse
 
     def weigh(self, q: torch.Tensor, lse: torch.Tensor, k_new: torch.Tensor | None = None,
@@ -1047,19 +1076,19 @@ class KVCache:
         """Add to every slot's weight what the nodes with row_weight (fp32 [n_seq, m]; None: 1) gave
         it in attend (same arguments, and its lse).  Returns the same sums for the new nodes,
         fp32 [n_seq, n_kv_heads, m] (None without k_new): append()'s weight."""
-        m, heads = q.shape[1], q.shape[2]
+        _, m, heads, _ = q.shape
         nodes = None
         if k_new is not None:
-            nodes = ALLOC((self.n_seq, self.n_kv_heads, m), torch.float32, self._dev)
+            nodes = self._new(self.weight, (self.n_seq, self.n_kv_heads, m))
         mp, ms = self._mask(mask, m)
         _kv_check(self._L.oilbird_kv_weigh(
-            self._ref, heads, m, self._rows(q, heads),
+            self._ref, heads, m, self._rows(q, heads, m),
             *self._lse(lse, m, heads),
             None if k_new is None else self._rows(k_new, self.n_kv_heads, m), mp, ms,
-            self._vec(n_new, torch.int32, self.n_seq),
-            self._vec(row_weight, torch.float32, self.n_seq, m),
-            self.head_dim ** -0.5 if scale is None else scale,
-            None if nodes is None else nodes.data_ptr(), _stream_ptr(stream)), "oilbird_kv_weigh")
+            self._vec(n_new, torch.int32, self._seqs),
+            self._vec(row_weight, torch.float32, (self.n_seq, m)),
+            self._scale if scale is None else scale,
+            None if nodes is None else nodes.data_ptr(), self._stream(stream)), "oilbird_kv_weigh")
         return nodes
 
     def evict(self, budget: int, sink: int = 4, recent: int | None = None, stream=None) -> None:
@@ -1069,11 +1098,11 @@ class KVCache:
         if recent is None:
             recent = max(0, min(budget // 2, budget - sink))
         _kv_check(self._L.oilbird_kv_evict(self._ref, int(budget), int(sink), int(recent),
-                                           _stream_ptr(stream)), "oilbird_kv_evict")
+                                           self._stream(stream)), "oilbird_kv_evict")
 
     def dropped(self, stream=None) -> int:
         """Rows append() could not store so far (synchronises)."""
         n = ctypes.c_int64()
-        _kv_check(self._L.oilbird_kv_status(self._ref, ctypes.byref(n), _stream_ptr(stream)),
+        _kv_check(self._L.oilbird_kv_status(self._ref, ctypes.byref(n), self._stream(stream)),
                   "oilbird_kv_status")
         return int(n.value)

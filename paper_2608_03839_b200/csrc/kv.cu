@@ -75,7 +75,8 @@ static int on_device(int device, int* sms) {
   static std::atomic<int> count[64];
   int n = 0;
   if (device < 0 || device >= 64) return kv_refuse("device");
-  KCU(cudaSetDevice(device));
+  int current = -1;                      // (asking is cheaper than setting)
+  if (cudaGetDevice(&current) != cudaSuccess || current != device) KCU(cudaSetDevice(device));
   n = count[device].load(std::memory_order_relaxed);
   if (n == 0) {
     KCU(preload_all_kernels());
@@ -120,7 +121,7 @@ int oilbird_kv_append(const oilbird_kv_cache* cache, const oilbird_kv_rows* k, c
   KvAppendArgs a;
   memset(&a, 0, sizeof a);
   KTRY(check_cache(cache, &c));
-  if (m < 0 || rows < 0) return kv_refuse("m and rows: not negative");
+  if (m < 0 || rows < 0 || rows > (1 << 24)) return kv_refuse("m and rows: not negative, rows at most 2^24");
   if (m == 0 || rows == 0) return OILBIRD_OK;
   if (!select && rows > m) return kv_refuse("rows: m at most without select");
   KTRY(check_rows(k, "k", &a.k));
@@ -132,7 +133,7 @@ int oilbird_kv_append(const oilbird_kv_cache* cache, const oilbird_kv_rows* k, c
   a.rows = rows;
   int sms;
   KTRY(on_device(cache->device, &sms));
-  KCU(launch_kv_append(c, a, cache->head_dim, cache->dtype == OILBIRD_KV_BF16, sms, (cudaStream_t)cuda_stream));
+  KCU(launch_kv_append(c, a, cache->head_dim, cache->dtype == OILBIRD_KV_BF16, (cudaStream_t)cuda_stream));
   return OILBIRD_OK;
 }
 
@@ -140,13 +141,13 @@ int oilbird_kv_read(const oilbird_kv_cache* cache, int32_t n, const int32_t* sta
                     void* cuda_stream) {
   KvView c;
   KTRY(check_cache(cache, &c));
-  if (n < 0) return kv_refuse("n: not negative");
+  if (n < 0 || n > (1 << 24)) return kv_refuse("n: 0 to 2^24");
   if (n == 0) return OILBIRD_OK;
   if (!k || !v || !aligned(k, 16) || !aligned(v, 16)) return kv_refuse("k and v: 16-byte aligned");
   const KvReadArgs a = {(uint16_t*)k, (uint16_t*)v, start, n};
   int sms;
   KTRY(on_device(cache->device, &sms));
-  KCU(launch_kv_read(c, a, cache->head_dim, cache->dtype == OILBIRD_KV_BF16, sms, (cudaStream_t)cuda_stream));
+  KCU(launch_kv_read(c, a, cache->head_dim, cache->dtype == OILBIRD_KV_BF16, (cudaStream_t)cuda_stream));
   return OILBIRD_OK;
 }
 

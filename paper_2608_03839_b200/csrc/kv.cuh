@@ -113,8 +113,8 @@ struct KvAttendArgs {
   int m, group;              // nodes per sequence, query heads per key/value head
 };
 
-cudaError_t launch_kv_append(const KvView& c, const KvAppendArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st);
-cudaError_t launch_kv_read(const KvView& c, const KvReadArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st);
+cudaError_t launch_kv_append(const KvView& c, const KvAppendArgs& a, int head_dim, bool bf16, cudaStream_t st);
+cudaError_t launch_kv_read(const KvView& c, const KvReadArgs& a, int head_dim, bool bf16, cudaStream_t st);
 cudaError_t launch_kv_attend(const KvView& c, const KvAttendArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st);
 cudaError_t launch_kv_tree(const KvView& c, const KvAttendArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st);
 cudaError_t launch_kv_weigh(const KvView& c, const KvWeighArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st);

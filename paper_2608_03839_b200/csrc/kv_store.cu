@@ -1,9 +1,14 @@
 // Storing into the 4-bit cache and reading it back.
 //
-// append: eight lanes take the 64 channels of one group (16 bytes each), agree on its minimum
-// and maximum with three shuffles, and write one word of codes each and one word of scale and
-// offset; a token's group costs 128 bytes in and 36 out.  read: the same lanes, the other way.
-// Both are bound by memory on long inputs and by the launch on a decoding step's few rows.
+// append: a warp takes one row's four key/value heads of a block (or fewer), 16 bytes a lane: eight lanes
+// share the 64 channels of a group, agree on its minimum and maximum (as packed 16-bit
+// numbers, three shuffles for both), and write one word of codes each and one word of scale and
+// offset; a token's group costs 128 bytes in and 36 out.  read: the same lanes, the other way,
+// four slots at a time.  All loads of a warp are on their way before the first is used.  Both
+// are bound by memory on long inputs and by latency on a decoding step's few rows.
+//
+// The quotient (x - lo) / scale is IEEE division's, by Markstein's correction of a product with
+// the reciprocal (one division a group): q = x r, q += (x - q scale) r.
 //
 // The lengths are device memory that every block reads and the call must advance: the block
 // that finishes last does it, when nobody reads them any more.
@@ -33,145 +38,185 @@ __device__ __forceinline__ bool last_block(unsigned* arrivals, unsigned blocks) 
   return last;
 }
 
+// packed 16-bit minimum and maximum; a NaN loses to a number
+template <bool kBf16> __device__ __forceinline__ uint32_t min16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if (kBf16) asm("min.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("min.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+template <bool kBf16> __device__ __forceinline__ uint32_t max16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if (kBf16) asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// Eight lanes' 64 elements (eight each) -> the lane's word of codes, the group's meta.
+template <bool kBf16>
+__device__ __forceinline__ uint32_t quantise64(const uint4& v, uint32_t& meta) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t lo2 = min16x2<kBf16>(min16x2<kBf16>(w[0], w[1]), min16x2<kBf16>(w[2], w[3]));
+  uint32_t hi2 = max16x2<kBf16>(max16x2<kBf16>(w[0], w[1]), max16x2<kBf16>(w[2], w[3]));
+  const uint32_t big = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+  constexpr uint32_t kInf = kBf16 ? 0x7f80u : 0x7c00u;
+  const bool odd = (big & 0xffffu) >= kInf || (big >> 16) >= kInf;
+  // both halves' minimum in the low half, maximum in the high half
+  uint32_t mm = __byte_perm(min16x2<kBf16>(lo2, lo2 >> 16), max16x2<kBf16>(hi2, hi2 << 16), 0x7610);
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) {
+    const uint32_t y = __shfl_xor_sync(0xffffffffu, mm, o);
+    mm = __byte_perm(min16x2<kBf16>(mm, y), max16x2<kBf16>(mm, y), 0x7610);
+  }
+  const bool bad = (__ballot_sync(0xffffffffu, odd) >> (threadIdx.x & 24) & 0xffu) != 0;
+  const float lo = half_lo<kBf16>(mm), hi = half_hi<kBf16>(mm);
+  // halves: the difference of two finite elements cannot overflow
+  meta = pack16<kBf16>((hi * 0.5f - lo * 0.5f) / 7.5f, lo);
+  const float half = half_lo<kBf16>(meta) * 0.5f, base = lo * 0.5f;
+  const float r = 1.f / half;
+  uint32_t codes = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float x = fmaf(e & 1 ? half_hi<kBf16>(w[e >> 1]) : half_lo<kBf16>(w[e >> 1]), 0.5f, -base);
+    float q = x * r;
+    q = fmaf(fmaf(-q, half, x), r, q);
+    // 1.5 * 2^23: the sum's low bits are the integer, rounded to nearest, ties to even
+    const uint32_t c = __float_as_uint(fminf(q, 15.f) + 12582912.f) & 15u;
+    codes |= c << (4 * (e >> 1) + 16 * (e & 1));
+  }
+  if (!(half >= 0x1p-120f)) {                            // no scale, or one whose reciprocal is none
+    codes = 0;
+    if (half > 0.f) {
+#pragma unroll 1
+      for (int e = 0; e < 8; ++e) {
+        const float x = fmaf(e & 1 ? half_hi<kBf16>(w[e >> 1]) : half_lo<kBf16>(w[e >> 1]), 0.5f, -base);
+        codes |= (uint32_t)(int)fminf(rintf(x / half), 15.f) << (4 * (e >> 1) + 16 * (e & 1));
+      }
+    }
+  }
+  if (bad) { codes = 0; meta = kBf16 ? 0x7fc07fc0u : 0x7e007e00u; }
+  return codes;
+}
+
+// grid.y: sequences; a warp: one row, kStHeads heads for D = 128 (twice as many for 64)
+constexpr int kStTurns = 4;
 template <int D, bool kBf16>
 __global__ void __launch_bounds__(kStThreads)
 kv_append_kernel(const KvView c, const KvAppendArgs a) {
   constexpr int G = D / kKvGroup, kUnits = 2 * G;        // units of eight lanes per (token, head)
+  constexpr int kHeadsATurn = 4 / kUnits, kHeads = kStTurns * kHeadsATurn;
   pdl_enter();
   KvWork* work = reinterpret_cast<KvWork*>(c.work);
-  const int lane8 = threadIdx.x & 7;
+  const int lane = threadIdx.x & 31, lane8 = lane & 7, unit = lane >> 3;
   const int page = 1 << c.page_shift;
   const size_t block = 2 * (size_t)kv_part_bytes(D, page);
-  const long long total = (long long)c.n_seq * a.rows * c.n_kv * kUnits;
-  const long long step = (long long)gridDim.x * (kStThreads / 8);
-  // (a warp's four units take part in the shuffles together: the loop bound is the warp's)
-  for (long long u0 = (long long)blockIdx.x * (kStThreads / 8) + (threadIdx.x >> 5) * 4; u0 < total; u0 += step) {
-    const long long u = u0 + ((threadIdx.x & 31) >> 3);
-    bool live = u < total;
-    const long long row = live ? u / kUnits : 0;         // (sequence, row, head)
-    const int part = (int)(live ? u - row * kUnits : 0), kv = part / G, grp = part % G;
-    const int head = (int)(row % c.n_kv);
-    const long long sr = row / c.n_kv;
-    const int s = (int)(sr / a.rows), j = (int)(sr - (long long)s * a.rows);
-    const int n = a.n_new ? a.n_new[s] : a.rows;
-    live = live && j < n;
-    int src = j;
-    if (live && a.select) src = a.select[(size_t)s * a.rows + j];
-    const int before = c.seq_len[s];
-    const long long slot = (long long)(before < 0 ? 0 : before) + j;
-    const int p = live ? page_of(c, s, slot) : -1;
-    const bool store = live && p >= 0 && src >= 0 && src < a.m;
-    if (live && !store && part == 0 && head == 0 && lane8 == 0) atomicAdd(&work->dropped, 1ull);
-    uint32_t w[4] = {0, 0, 0, 0};
-    if (store) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>((kv ? a.v : a.k).at(s, src, head) + grp * kKvGroup + lane8 * 8);
-    float x[8];
-    bool bad = false;
+  const int s = blockIdx.y;
+  const int n = a.n_new ? a.n_new[s] : a.rows;
+  const int before = max(c.seq_len[s], 0), pos0 = c.n_pos[s];
+  const int head_groups = (c.n_kv + kHeads - 1) / kHeads;
+  const int task = blockIdx.x * (kStThreads / 32) + (threadIdx.x >> 5);
+  const int j = task / head_groups, head0 = (task - j * head_groups) * kHeads;
+  if (j < a.rows && j < n) {
+    const int src = a.select ? a.select[(size_t)s * a.rows + j] : j;
+    const long long slot = (long long)before + j;
+    const int p = page_of(c, s, slot);
+    const bool store = p >= 0 && src >= 0 && src < a.m;
+    if (!store) {
+      if (head0 == 0 && lane == 0) atomicAdd(&work->dropped, 1ull);
+    } else {
+      const int kv = unit % kUnits / G, grp = unit % G, in = (int)(slot & (page - 1));
+      const KvRows& rows = kv ? a.v : a.k;
+      uint4 v[kStTurns];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x[2 * e] = half_lo<kBf16>(w[e]);
-      x[2 * e + 1] = half_hi<kBf16>(w[e]);
-    }
-    float lo = x[0], hi = x[0];
+      for (int t = 0; t < kStTurns; ++t) {
+        const int head = head0 + t * kHeadsATurn + unit / kUnits;
+        v[t] = make_uint4(0, 0, 0, 0);
+        if (head < c.n_kv) v[t] = *reinterpret_cast<const uint4*>(rows.at(s, src, head) + grp * kKvGroup + lane8 * 8);
+      }
+      const float w = a.weight && lane < kHeads && head0 + lane < c.n_kv
+                          ? a.weight[((size_t)s * c.n_kv + head0 + lane) * a.m + src] : 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      lo = fminf(lo, x[e]);
-      hi = fmaxf(hi, x[e]);
-      bad |= !(fabsf(x[e]) < INFINITY);
-    }
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
-      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    }
-    bad = (__ballot_sync(0xffffffffu, bad) >> (threadIdx.x & 24) & 0xffu) != 0;
-    // halves: the difference of two finite elements cannot overflow
-    uint32_t meta = pack16<kBf16>((hi * 0.5f - lo * 0.5f) / 7.5f, lo);
-    const float half = half_lo<kBf16>(meta) * 0.5f, base = lo * 0.5f;
-    uint32_t codes = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float q = rintf((x[e] * 0.5f - base) / half);
-      q = half > 0.f ? fminf(fmaxf(q, 0.f), 15.f) : 0.f;
-      codes |= (uint32_t)(int)q << (4 * (e >> 1) + 16 * (e & 1));
-    }
-    if (bad) { codes = 0; meta = kBf16 ? 0x7fc07fc0u : 0x7e007e00u; }
-    if (store) {
-      const int in = (int)(slot & (page - 1));
-      unsigned char* b = c.pages + ((size_t)p * c.n_kv + head) * block + kv * (block / 2);
-      *reinterpret_cast<uint32_t*>(b + ((size_t)grp * page + in) * 32 + lane8 * 4) = codes;
-      if (lane8 == 0) *reinterpret_cast<uint32_t*>(b + (size_t)G * page * 32 + ((size_t)in * G + grp) * 4) = meta;
-      if (part == 0 && lane8 == 1) {
-        const size_t at = ((size_t)p * c.n_kv + head) * page + in;
-        c.weight[at] = a.weight ? a.weight[((size_t)s * c.n_kv + head) * a.m + src] : 0.f;
-        c.pos[at] = c.n_pos[s] + j;
+      for (int t = 0; t < kStTurns; ++t) {
+        const int head = head0 + t * kHeadsATurn + unit / kUnits;
+        uint32_t meta;
+        const uint32_t codes = quantise64<kBf16>(v[t], meta);
+        if (head < c.n_kv) {
+          unsigned char* b = c.pages + ((size_t)p * c.n_kv + head) * block + kv * (block / 2);
+          *reinterpret_cast<uint32_t*>(b + ((size_t)grp * page + in) * 32 + lane8 * 4) = codes;
+          if (lane8 == 0) *reinterpret_cast<uint32_t*>(b + (size_t)G * page * 32 + ((size_t)in * G + grp) * 4) = meta;
+        }
+      }
+      if (lane < kHeads && head0 + lane < c.n_kv) {
+        const size_t at = ((size_t)p * c.n_kv + head0 + lane) * page + in;
+        c.weight[at] = w;
+        c.pos[at] = pos0 + j;
       }
     }
   }
-  if (last_block(&work->arrivals, gridDim.x)) {
+  if (last_block(&work->arrivals, gridDim.x * gridDim.y)) {
     const long long room = (long long)c.max_pages << c.page_shift;
-    for (int s = threadIdx.x; s < c.n_seq; s += kStThreads) {
-      int n = a.n_new ? a.n_new[s] : a.rows;
-      n = n < 0 ? 0 : (n > a.rows ? a.rows : n);
-      const int before = c.seq_len[s];
-      const long long after = (long long)(before < 0 ? 0 : before) + n;
-      c.seq_len[s] = (int)(after > room ? room : after);
-      c.n_pos[s] += n;
+    for (int i = threadIdx.x; i < c.n_seq; i += kStThreads) {
+      int m = a.n_new ? a.n_new[i] : a.rows;
+      m = m < 0 ? 0 : (m > a.rows ? a.rows : m);
+      const long long after = (long long)max(c.seq_len[i], 0) + m;
+      c.seq_len[i] = (int)(after > room ? room : after);
+      c.n_pos[i] += m;
     }
   }
 }
 
+// grid.y: sequences; a warp: four slots of one head, K and V, every group
 template <int D, bool kBf16>
 __global__ void __launch_bounds__(kStThreads)
 kv_read_kernel(const KvView c, const KvReadArgs a) {
   constexpr int G = D / kKvGroup;
   pdl_enter();
-  const int lane8 = threadIdx.x & 7;
+  const int lane = threadIdx.x & 31, lane8 = lane & 7;
   const int page = 1 << c.page_shift;
   const size_t block = 2 * (size_t)kv_part_bytes(D, page);
-  // units of eight lanes: (sequence, head, K or V, group, row), rows fastest, so that a warp's
-  // loads are contiguous
-  const long long total = (long long)c.n_seq * c.n_kv * 2 * G * a.n;
-  for (long long u = (long long)blockIdx.x * (kStThreads / 8) + (threadIdx.x >> 3); u < total;
-       u += (long long)gridDim.x * (kStThreads / 8)) {
-    const long long part = u / a.n;
-    const int j = (int)(u - part * a.n);
-    const int grp = (int)(part % G), kv = (int)(part / G % 2);
-    const long long sh = part / (2 * G);
-    const int head = (int)(sh % c.n_kv), s = (int)(sh / c.n_kv);
-    const long long slot = (a.start ? (long long)a.start[s] : 0) + j;
-    uint32_t out[4] = {0, 0, 0, 0};
-    if (slot >= 0 && slot < c.seq_len[s]) {
-      const int p = page_of(c, s, slot);
-      if (p >= 0) {
-        const int in = (int)(slot & (page - 1));
-        const unsigned char* b = c.pages + ((size_t)p * c.n_kv + head) * block + kv * (block / 2);
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(b + ((size_t)grp * page + in) * 32 + lane8 * 4);
-        const uint32_t meta = *reinterpret_cast<const uint32_t*>(b + (size_t)G * page * 32 + ((size_t)in * G + grp) * 4);
-        const float sc = half_lo<kBf16>(meta), lo = half_hi<kBf16>(meta);
+  const int s = blockIdx.y, task = blockIdx.x * (kStThreads / 32) + (threadIdx.x >> 5);
+  const int j4 = task / c.n_kv, head = task - j4 * c.n_kv, j = j4 * 4 + (lane >> 3);
+  if (j >= a.n) return;
+  const long long slot = (a.start ? (long long)a.start[s] : 0) + j;
+  const int p = slot >= 0 && slot < c.seq_len[s] ? page_of(c, s, slot) : -1;
+  uint32_t w[2][G], meta[2][G];
+  const int in = (int)(slot & (page - 1));
+  const unsigned char* b = c.pages + ((size_t)max(p, 0) * c.n_kv + head) * block;
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
-          out[n] = pack16<kBf16>(fmaf((float)(w >> (4 * n) & 15u), sc, lo), fmaf((float)(w >> (16 + 4 * n) & 15u), sc, lo));
-      }
+  for (int kv = 0; kv < 2; ++kv) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      w[kv][g] = meta[kv][g] = 0;
+      if (p >= 0) w[kv][g] = *reinterpret_cast<const uint32_t*>(b + kv * (block / 2) + (g * page + in) * 32 + lane8 * 4);
     }
-    uint16_t* dst = (kv ? a.v : a.k) + (((size_t)s * a.n + j) * c.n_kv + head) * D + grp * kKvGroup + lane8 * 8;
-    *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(out);
+    if (p >= 0) load_meta<G>(b + kv * (block / 2) + (G * page * 8 + in * G) * 4, meta[kv]);
   }
+  const size_t at = (((size_t)s * a.n + j) * c.n_kv + head) * D + lane8 * 8;
+#pragma unroll
+  for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const float sc = half_lo<kBf16>(meta[kv][g]), lo = half_hi<kBf16>(meta[kv][g]);
+      uint32_t out[4];
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+        out[n] = pack16<kBf16>(fmaf((float)(w[kv][g] >> (4 * n) & 15u), sc, lo), fmaf((float)(w[kv][g] >> (16 + 4 * n) & 15u), sc, lo));
+      __stcs(reinterpret_cast<uint4*>((kv ? a.v : a.k) + at + g * kKvGroup), make_uint4(out[0], out[1], out[2], out[3]));
+    }
 }
 
-static int grid_for(long long units, int sms) {          // eight blocks an SM, enough for every unit
-  const long long want = (units + kStThreads / 8 - 1) / (kStThreads / 8);
-  return (int)(want < 8LL * sms ? (want < 1 ? 1 : want) : 8LL * sms);
-}
-
-cudaError_t launch_kv_append(const KvView& c, const KvAppendArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st) {
-  const int grid = grid_for((long long)c.n_seq * a.rows * c.n_kv * 2 * (head_dim / kKvGroup), sms);
-  auto go = [&](auto kernel) { return launch_pdl(kernel, dim3(grid), dim3(kStThreads), 0, st, c, a); };
+cudaError_t launch_kv_append(const KvView& c, const KvAppendArgs& a, int head_dim, bool bf16, cudaStream_t st) {
+  const int heads = kStTurns * 4 / (2 * (head_dim / kKvGroup));
+  const long long tasks = (long long)a.rows * ((c.n_kv + heads - 1) / heads);
+  const dim3 grid((unsigned)((tasks + kStThreads / 32 - 1) / (kStThreads / 32)), c.n_seq);
+  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(kStThreads), 0, st, c, a); };
   if (head_dim == 64) return bf16 ? go(kv_append_kernel<64, true>) : go(kv_append_kernel<64, false>);
   return bf16 ? go(kv_append_kernel<128, true>) : go(kv_append_kernel<128, false>);
 }
-cudaError_t launch_kv_read(const KvView& c, const KvReadArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st) {
-  const int grid = grid_for((long long)c.n_seq * c.n_kv * 2 * (head_dim / kKvGroup) * a.n, sms);
-  auto go = [&](auto kernel) { return launch_pdl(kernel, dim3(grid), dim3(kStThreads), 0, st, c, a); };
+cudaError_t launch_kv_read(const KvView& c, const KvReadArgs& a, int head_dim, bool bf16, cudaStream_t st) {
+  const long long tasks = ((long long)a.n + 3) / 4 * c.n_kv;
+  const dim3 grid((unsigned)((tasks + kStThreads / 32 - 1) / (kStThreads / 32)), c.n_seq);
+  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(kStThreads), 0, st, c, a); };
   if (head_dim == 64) return bf16 ? go(kv_read_kernel<64, true>) : go(kv_read_kernel<64, false>);
   return bf16 ? go(kv_read_kernel<128, true>) : go(kv_read_kernel<128, false>);
 }
