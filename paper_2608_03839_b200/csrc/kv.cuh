@@ -97,7 +97,7 @@ struct KvReadArgs {
 };
 struct KvEvictArgs {
   int budget, sink, recent;
-  int max_words;             // set by the launch
+  int max_words, held;       // set by the launch
 };
 
 struct KvAttendArgs {

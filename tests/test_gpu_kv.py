@@ -529,6 +529,14 @@ def test_evict_ties_and_odd_weights(weights, shuffled):
     evict_case([70, 500, 64], 64, 3, 9, weights, pos=pos)
 
 
+@pytest.mark.parametrize("most,budget", [(5000, 700), (9000, 8999), (17000, 33), (40000, 4096)])
+def test_evict_sequences_shared_by_several_blocks(most, budget):
+    """Long sequences are handled by two to eight blocks; ties and moves cross between them."""
+    evict_case([most, most // 3, budget, budget + 1], budget, 3, budget // 3,
+               lambda c, s: (torch.rand(s, generator=c.g, device="cuda") < 0.3) * torch.randint(0, 50, s, generator=c.g, device="cuda").float(),
+               d=64, page=64, hkv=1)
+
+
 def test_evict_equal_positions_too():
     """Positions a caller has repeated: the lowest slots stay."""
     evict_case([200], 50, 0, 0, lambda c, s: torch.ones(s, device="cuda"), pos=lambda c, s: torch.full(s, 7, dtype=torch.int32, device="cuda"))
