@@ -133,7 +133,7 @@ int oilbird_kv_append(const oilbird_kv_cache* cache, const oilbird_kv_rows* k, c
   a.rows = rows;
   int sms;
   KTRY(on_device(cache->device, &sms));
-  KCU(launch_kv_append(c, a, cache->head_dim, cache->dtype == OILBIRD_KV_BF16, (cudaStream_t)cuda_stream));
+  KCU(launch_kv_append(c, a, cache->head_dim, cache->dtype == OILBIRD_KV_BF16, sms, (cudaStream_t)cuda_stream));
   return OILBIRD_OK;
 }
 
@@ -230,10 +230,10 @@ int oilbird_kv_evict(const oilbird_kv_cache* cache, int32_t budget, int32_t sink
     return kv_refuse("budget: at least 1, and at least sink + recent");
   if (((int64_t)c.max_pages << c.page_shift) > OILBIRD_KV_MAX_EVICT_SLOTS)
     return kv_refuse("max_pages * page_size: OILBIRD_KV_MAX_EVICT_SLOTS at most");
-  const KvEvictArgs a = {budget, sink, recent, 0};
+  const KvEvictArgs a = {budget, sink, recent, 0, 0, 0};
   int sms;
   KTRY(on_device(cache->device, &sms));
-  KCU(launch_kv_evict(c, a, cache->head_dim, (cudaStream_t)cuda_stream));
+  KCU(launch_kv_evict(c, a, cache->head_dim, sms, (cudaStream_t)cuda_stream));
   return OILBIRD_OK;
 }
 

@@ -32,11 +32,12 @@ __device__ __forceinline__ uint32_t weight_order(float w) {
 
 struct EvictShared {
   uint32_t hist[kEvBins];
-  uint2 moves[kEvThreads];           // source and destination slots
+  int4 moves[kEvThreads];            // pages and slots in them: source, destination
   uint32_t warp_sum[kEvWarps];
   uint32_t digit, below, count;
   // what the other blocks of the cluster read: safe slots; kept for sure, ties; holes, movers
   uint32_t safe, sure, ties, holes, movers;
+  uint32_t all_holes[kEvMaxCluster], all_movers[kEvMaxCluster];    // every block's
 };
 
 // Finds the digit d with  sum of hist[> d] < want <= sum of hist[>= d]  (descending = true), or
@@ -46,10 +47,13 @@ __device__ __forceinline__ void find_digit(EvictShared& sh, cg::cluster_group& c
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   uint4 c = make_uint4(0, 0, 0, 0);                      // four bins, in the order of counting
   const int b = descending ? kEvBins - 4 - 4 * tid : 4 * tid;
-  for (int r = 0; r < n_blocks; ++r) {
-    const uint4 x = *reinterpret_cast<const uint4*>(cl.map_shared_rank(sh.hist, r) + b);
-    c.x += x.x; c.y += x.y; c.z += x.z; c.w += x.w;
-  }
+  uint4 x4[kEvMaxCluster];
+#pragma unroll
+  for (int r = 0; r < kEvMaxCluster; ++r)
+    if (r < n_blocks) x4[r] = *reinterpret_cast<const uint4*>(cl.map_shared_rank(sh.hist, r) + b);
+#pragma unroll
+  for (int r = 0; r < kEvMaxCluster; ++r)
+    if (r < n_blocks) { c.x += x4[r].x; c.y += x4[r].y; c.z += x4[r].z; c.w += x4[r].w; }
   if (descending) { uint32_t t = c.x; c.x = c.w; c.w = t; t = c.y; c.y = c.z; c.z = t; }
   const uint32_t mine = c.x + c.y + c.z + c.w;
   uint32_t x = mine;
@@ -118,18 +122,17 @@ kv_evict_kernel(const KvView c, const KvEvictArgs a, int groups) {
     const int32_t* table = c.table + (size_t)s * c.max_pages;
     auto fetch = [&](int i) {                            // order and position of the run's slot i
       const int slot = first + i, p = table[slot >> c.page_shift];
-      uint2 r = make_uint2(0u, 2147483647u);             // (no page: below everything)
-      if ((uint32_t)p < (uint32_t)c.n_pages) {
-        const size_t at = ((size_t)p * c.n_kv + head) * page + (slot & (page - 1));
-        r = make_uint2(weight_order(c.weight[at]), (uint32_t)c.pos[at]);
-      }
-      return r;
+      const bool have = (uint32_t)p < (uint32_t)c.n_pages;
+      const size_t at = ((size_t)(have ? p : 0) * c.n_kv + head) * page + (slot & (page - 1));
+      const float w = c.weight[at];
+      const int32_t x = c.pos[at];                       // (no page: below everything)
+      return have ? make_uint2(weight_order(w), (uint32_t)x) : make_uint2(0u, 2147483647u);
     };
     if (tid == 0) sh.safe = 0;
     __syncthreads();
     uint32_t n_safe = 0;
     if (a.held) {
-#pragma unroll 4
+#pragma unroll 8
       for (int i = tid; i < n; i += kEvThreads) held[i] = fetch(i);
     }
     auto slot_at = [&](int i) { return a.held ? held[i] : fetch(i); };
@@ -240,57 +243,88 @@ kv_evict_kernel(const KvView c, const KvEvictArgs a, int groups) {
     }
     cl.sync();
     // ---- the moves ----
+    if (tid < n_blocks) {
+      sh.all_holes[tid] = *cl.map_shared_rank(&sh.holes, tid);
+      sh.all_movers[tid] = *cl.map_shared_rank(&sh.movers, tid);
+    }
+    // every block's bits and ranks, where they fit beside one another
+    const int all_words = (len + 31) / 32;
+    uint32_t* every = reinterpret_cast<uint32_t*>(held + (a.held ? a.max_words * 32 : 0));
+    if (a.gather)
+      for (int w = tid; w < all_words; w += kEvThreads) {
+        const int r = w / per, i = w - r * per;
+        every[w] = cl.map_shared_rank(keep, r)[i];
+        every[a.gather + w] = cl.map_shared_rank(rank_h, r)[i];
+        every[2 * a.gather + w] = cl.map_shared_rank(rank_m, r)[i];
+      }
+    __syncthreads();
     uint32_t n_moves = 0;
-    for (int r = 0; r < n_blocks; ++r) n_moves += *cl.map_shared_rank(&sh.holes, r);
+    for (int r = 0; r < n_blocks; ++r) n_moves += sh.all_holes[r];
     const size_t block = 2 * (size_t)kv_part_bytes(groups * kKvGroup, page);
     const int lane8 = tid & 7;
     // the slot with rank i among the holes or the movers
     auto find = [&](uint32_t i, bool hole) {
       int r = 0;
       for (;; ++r) {
-        const uint32_t here = hole ? *cl.map_shared_rank(&sh.holes, r) : *cl.map_shared_rank(&sh.movers, r);
+        const uint32_t here = hole ? sh.all_holes[r] : sh.all_movers[r];
         if (i < here || r == n_blocks - 1) break;
         i -= here;
       }
-      const uint32_t* rk = cl.map_shared_rank(hole ? rank_h : rank_m, r);
-      const int base = r * per, nw = min(per, (len + 31) / 32 - base);
+      const int base = r * per, nw = min(per, all_words - base);
+      const uint32_t* rk = a.gather ? every + (hole ? a.gather : 2 * a.gather) + base : cl.map_shared_rank(hole ? rank_h : rank_m, r);
       int lo = 0, hi = nw - 1;
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (rk[mid] <= i) lo = mid; else hi = mid - 1;
       }
-      const uint32_t k = cl.map_shared_rank(keep, r)[lo];
+      const uint32_t k = a.gather ? every[base + lo] : cl.map_shared_rank(keep, r)[lo];
       const int at = (base + lo) * 32;
       const uint32_t low = at + 32 <= budget ? 0xffffffffu : at >= budget ? 0u : (1u << (budget - at)) - 1u;
       return at + nth_bit(hole ? ~k & low : k & ~low, (int)(i - rk[lo]));
     };
     for (uint32_t m0 = me; m0 < n_moves; m0 += n_blocks * kEvThreads) {
       const uint32_t i = m0 + (uint32_t)tid * n_blocks;
-      if (i < n_moves) sh.moves[tid] = make_uint2(find(i, false), find(i, true));
+      if (i < n_moves) {
+        const int src = find(i, false), dst = find(i, true);
+        const int ps = table[src >> c.page_shift], pd = table[dst >> c.page_shift];
+        const bool ok = (uint32_t)ps < (uint32_t)c.n_pages && (uint32_t)pd < (uint32_t)c.n_pages;
+        sh.moves[tid] = make_int4(ok ? ps : -1, src & (page - 1), pd, dst & (page - 1));
+      }
       __syncthreads();
       const int count = (int)min((n_moves - m0 + n_blocks - 1) / n_blocks, (uint32_t)kEvThreads);
-#pragma unroll 2
-      for (int k = tid >> 3; k < count; k += kEvThreads / 8) {
-        const int src = (int)sh.moves[k].x, dst = (int)sh.moves[k].y;
-        const int ps = table[src >> c.page_shift], pd = table[dst >> c.page_shift];
-        if ((uint32_t)ps >= (uint32_t)c.n_pages || (uint32_t)pd >= (uint32_t)c.n_pages) continue;
-        const int is = src & (page - 1), id = dst & (page - 1);
-        const unsigned char* bs = c.pages + ((size_t)ps * c.n_kv + head) * block;
-        unsigned char* bd = c.pages + ((size_t)pd * c.n_kv + head) * block;
-        // codes: 2 halves of 32 bytes for each of K, V and each group
-        if (lane8 < 4 * groups) {
-          const int kv = lane8 / (2 * groups), grp = lane8 / 2 % groups, half = (lane8 & 1) * 16;
-          const size_t off = kv * (block / 2) + (size_t)grp * page * 32 + half;
-          *reinterpret_cast<uint4*>(bd + off + id * 32) = *reinterpret_cast<const uint4*>(bs + off + is * 32);
+      // lanes 0..7: 16 bytes of codes (two for each 32 of K, V and each group), a word of meta, the
+      // weight and the position; four moves' loads on their way together
+      const int part = groups * page * 36;
+      const int kv = lane8 / (2 * groups), c_off = kv * part + (lane8 / 2 % groups) * page * 32 + (lane8 & 1) * 16;
+      const int m_off = lane8 / groups * part + groups * page * 32 + lane8 % groups * 4;
+      constexpr int kAtOnce = 4;
+      for (int k0 = tid >> 3; k0 < count; k0 += kAtOnce * (kEvThreads / 8)) {
+        int4 mv[kAtOnce];
+        uint4 code[kAtOnce];
+        uint32_t meta[kAtOnce], side[kAtOnce];
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) {
+          const int k = k0 + q * (kEvThreads / 8);
+          mv[q] = k < count ? sh.moves[k] : make_int4(-1, 0, 0, 0);
+          if (mv[q].x >= 0) {
+            const size_t at = (size_t)mv[q].x * c.n_kv + head;
+            const unsigned char* bs = c.pages + at * block;
+            if (lane8 < 4 * groups) code[q] = *reinterpret_cast<const uint4*>(bs + c_off + mv[q].y * 32);
+            if (lane8 < 2 * groups) meta[q] = *reinterpret_cast<const uint32_t*>(bs + m_off + mv[q].y * groups * 4);
+            if (lane8 == 6) side[q] = reinterpret_cast<const uint32_t*>(c.weight)[at * page + mv[q].y];
+            if (lane8 == 7) side[q] = reinterpret_cast<const uint32_t*>(c.pos)[at * page + mv[q].y];
+          }
         }
-        if (lane8 < 2 * groups) {
-          const int kv = lane8 / groups, grp = lane8 % groups;
-          const size_t off = kv * (block / 2) + (size_t)groups * page * 32 + grp * 4;
-          *reinterpret_cast<uint32_t*>(bd + off + id * groups * 4) = *reinterpret_cast<const uint32_t*>(bs + off + is * groups * 4);
-        }
-        const size_t as = ((size_t)ps * c.n_kv + head) * page + is, ad = ((size_t)pd * c.n_kv + head) * page + id;
-        if (lane8 == 6) c.weight[ad] = c.weight[as];
-        if (lane8 == 7) c.pos[ad] = c.pos[as];
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q)
+          if (mv[q].x >= 0) {
+            const size_t at = (size_t)mv[q].z * c.n_kv + head;
+            unsigned char* bd = c.pages + at * block;
+            if (lane8 < 4 * groups) *reinterpret_cast<uint4*>(bd + c_off + mv[q].w * 32) = code[q];
+            if (lane8 < 2 * groups) *reinterpret_cast<uint32_t*>(bd + m_off + mv[q].w * groups * 4) = meta[q];
+            if (lane8 == 6) reinterpret_cast<uint32_t*>(c.weight)[at * page + mv[q].w] = side[q];
+            if (lane8 == 7) reinterpret_cast<uint32_t*>(c.pos)[at * page + mv[q].w] = side[q];
+          }
       }
       __syncthreads();
     }
@@ -310,25 +344,29 @@ kv_evict_kernel(const KvView c, const KvEvictArgs a, int groups) {
       if (c.seq_len[i] > budget) c.seq_len[i] = budget;
 }
 
-// Blocks a cluster: runs of 2048 to 4096 slots are scanned in a few microseconds, and shorter
-// ones do not pay for the cluster's barriers.
-static int evict_cluster(long long slots) { return slots <= 4096 ? 1 : slots <= 8192 ? 2 : slots <= 16384 ? 4 : kEvMaxCluster; }
 static constexpr long long run_words(long long slots, int blocks) { return ((slots + 31) / 32 + blocks - 1) / blocks; }
-static constexpr size_t evict_smem(long long words, bool held) {
-  return sizeof(EvictShared) + (size_t)(words + 3) / 4 * 4 * (12 + (held ? 32 * 8 : 0));
+static constexpr size_t evict_smem(long long words, bool held, long long gather) {
+  return sizeof(EvictShared) + (size_t)(words + 3) / 4 * 4 * (12 + (held ? 32 * 8 : 0)) + (size_t)gather * 12;
 }
-static_assert(evict_smem(run_words(OILBIRD_KV_MAX_EVICT_SLOTS, kEvMaxCluster), false) <= 224 * 1024, "does not fit a block's shared memory");
+static_assert(evict_smem(run_words(OILBIRD_KV_MAX_EVICT_SLOTS, kEvMaxCluster), false, 0) <= 224 * 1024, "does not fit a block's shared memory");
 
-cudaError_t launch_kv_evict(const KvView& c, KvEvictArgs a, int head_dim, cudaStream_t st) {
-  const long long slots = (long long)c.max_pages << c.page_shift;
-  const int blocks = evict_cluster(slots);
-  const long long words = run_words(slots, blocks);
-  a.held = evict_smem(words, true) <= 100 * 1024;        // two blocks an SM
+cudaError_t launch_kv_evict(const KvView& c, KvEvictArgs a, int head_dim, int sms, cudaStream_t st) {
+  const long long slots = (long long)c.max_pages << c.page_shift, items = (long long)c.n_seq * c.n_kv;
+  // Blocks a cluster: as many as let every cluster be on the GPU at once (two blocks an SM), but
+  // runs of at least 2048 slots (shorter ones do not pay for the cluster's barriers) and at
+  // most what a block's shared memory takes.
+  int blocks = 1;
+  while (blocks < kEvMaxCluster && ((slots > 2048LL * blocks && 2 * blocks * items <= 2 * sms) ||
+                                    evict_smem(run_words(slots, blocks), false, 0) > 100 * 1024))
+    blocks *= 2;
+  const long long words = run_words(slots, blocks), all = (slots + 31) / 32;
+  a.held = evict_smem(words, true, 0) <= 100 * 1024;     // two blocks an SM
+  a.gather = blocks > 1 && evict_smem(words, a.held, all) <= 110 * 1024 ? (int)all : 0;
   a.max_words = (int)((words + 3) / 4 * 4);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(c.n_seq * c.n_kv * blocks));
   cfg.blockDim = dim3(kEvThreads);
-  cfg.dynamicSmemBytes = evict_smem(words, a.held);
+  cfg.dynamicSmemBytes = evict_smem(words, a.held, a.gather);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;

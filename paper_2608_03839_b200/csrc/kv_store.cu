@@ -38,29 +38,26 @@ __device__ __forceinline__ bool last_block(unsigned* arrivals, unsigned blocks) 
   return last;
 }
 
-// packed 16-bit minimum and maximum; a NaN loses to a number
+// packed 16-bit minimum and maximum; a NaN wins
 template <bool kBf16> __device__ __forceinline__ uint32_t min16x2(uint32_t a, uint32_t b) {
   uint32_t r;
-  if (kBf16) asm("min.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  else asm("min.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  if (kBf16) asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
 template <bool kBf16> __device__ __forceinline__ uint32_t max16x2(uint32_t a, uint32_t b) {
   uint32_t r;
-  if (kBf16) asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  else asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  if (kBf16) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
 
-// Eight lanes' 64 elements (eight each) -> the lane's word of codes, the group's meta.
+// Eight lanes' 64 elements (eight each) -> the lane's word of codes, the group's meta.  Two
+// elements an instruction wherever there is one for pairs: this is what bounds long appends.
 template <bool kBf16>
 __device__ __forceinline__ uint32_t quantise64(const uint4& v, uint32_t& meta) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  uint32_t lo2 = min16x2<kBf16>(min16x2<kBf16>(w[0], w[1]), min16x2<kBf16>(w[2], w[3]));
-  uint32_t hi2 = max16x2<kBf16>(max16x2<kBf16>(w[0], w[1]), max16x2<kBf16>(w[2], w[3]));
-  const uint32_t big = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
-  constexpr uint32_t kInf = kBf16 ? 0x7f80u : 0x7c00u;
-  const bool odd = (big & 0xffffu) >= kInf || (big >> 16) >= kInf;
+  const uint32_t lo2 = min16x2<kBf16>(min16x2<kBf16>(v.x, v.y), min16x2<kBf16>(v.z, v.w));
+  const uint32_t hi2 = max16x2<kBf16>(max16x2<kBf16>(v.x, v.y), max16x2<kBf16>(v.z, v.w));
   // both halves' minimum in the low half, maximum in the high half
   uint32_t mm = __byte_perm(min16x2<kBf16>(lo2, lo2 >> 16), max16x2<kBf16>(hi2, hi2 << 16), 0x7610);
 #pragma unroll
@@ -68,90 +65,114 @@ __device__ __forceinline__ uint32_t quantise64(const uint4& v, uint32_t& meta) {
     const uint32_t y = __shfl_xor_sync(0xffffffffu, mm, o);
     mm = __byte_perm(min16x2<kBf16>(mm, y), max16x2<kBf16>(mm, y), 0x7610);
   }
-  const bool bad = (__ballot_sync(0xffffffffu, odd) >> (threadIdx.x & 24) & 0xffu) != 0;
   const float lo = half_lo<kBf16>(mm), hi = half_hi<kBf16>(mm);
   // halves: the difference of two finite elements cannot overflow
-  meta = pack16<kBf16>((hi * 0.5f - lo * 0.5f) / 7.5f, lo);
-  const float half = half_lo<kBf16>(meta) * 0.5f, base = lo * 0.5f;
-  const float r = 1.f / half;
+  const float spread = hi * 0.5f - lo * 0.5f;
+  constexpr float kInv = 1.f / 7.5f;
+  float step = spread * kInv;
+  step = fmaf(fmaf(-step, 7.5f, spread), kInv, step);
+  meta = pack16<kBf16>(step, lo);
+  const float half = half_lo<kBf16>(meta) * 0.5f, base = lo * -0.5f, r = 1.f / half;
+  const float2 r2 = make_float2(r, r), h2 = make_float2(-half, -half), b2 = make_float2(base, base),
+               two = make_float2(0.5f, 0.5f), one = make_float2(1.f, 1.f), magic = make_float2(12582912.f, 12582912.f);
   uint32_t codes = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float x = fmaf(e & 1 ? half_hi<kBf16>(w[e >> 1]) : half_lo<kBf16>(w[e >> 1]), 0.5f, -base);
-    float q = x * r;
-    q = fmaf(fmaf(-q, half, x), r, q);
-    // 1.5 * 2^23: the sum's low bits are the integer, rounded to nearest, ties to even
-    const uint32_t c = __float_as_uint(fminf(q, 15.f) + 12582912.f) & 15u;
-    codes |= c << (4 * (e >> 1) + 16 * (e & 1));
+  for (int n = 0; n < 4; ++n) {
+    const uint32_t w = (&v.x)[n];
+    const float2 x = fma2(make_float2(half_lo<kBf16>(w), half_hi<kBf16>(w)), two, b2);
+    float2 q = mul2(x, r2);
+    q = fma2(fma2(q, h2, x), r2, q);
+    // + 1.5 * 2^23: the sum's low bits are the integer, rounded to nearest, ties to even
+    q = fma2(q, one, magic);
+    const uint32_t t = __vminu2(__byte_perm(__float_as_uint(q.x), __float_as_uint(q.y), 0x5410), 0x000f000fu);
+    codes |= t << (4 * n);
   }
   if (!(half >= 0x1p-120f)) {                            // no scale, or one whose reciprocal is none
     codes = 0;
     if (half > 0.f) {
-#pragma unroll 1
+#pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float x = fmaf(e & 1 ? half_hi<kBf16>(w[e >> 1]) : half_lo<kBf16>(w[e >> 1]), 0.5f, -base);
+        const uint32_t w = (&v.x)[e >> 1];
+        const float x = fmaf(e & 1 ? half_hi<kBf16>(w) : half_lo<kBf16>(w), 0.5f, base);
         codes |= (uint32_t)(int)fminf(rintf(x / half), 15.f) << (4 * (e >> 1) + 16 * (e & 1));
       }
     }
   }
-  if (bad) { codes = 0; meta = kBf16 ? 0x7fc07fc0u : 0x7e007e00u; }
+  if (!(fabsf(lo) < INFINITY) || !(fabsf(hi) < INFINITY)) { codes = 0; meta = kBf16 ? 0x7fc07fc0u : 0x7e007e00u; }
   return codes;
 }
 
-// grid.y: sequences; a warp: one row, kStHeads heads for D = 128 (twice as many for 64)
+// grid.y: sequences; a warp: one row's kHeads heads after another, the next one's elements asked
+// for before this one's are worked on
 constexpr int kStTurns = 4;
 template <int D, bool kBf16>
-__global__ void __launch_bounds__(kStThreads)
+__global__ void __launch_bounds__(kStThreads, 3)
 kv_append_kernel(const KvView c, const KvAppendArgs a) {
   constexpr int G = D / kKvGroup, kUnits = 2 * G;        // units of eight lanes per (token, head)
   constexpr int kHeadsATurn = 4 / kUnits, kHeads = kStTurns * kHeadsATurn;
   pdl_enter();
   KvWork* work = reinterpret_cast<KvWork*>(c.work);
   const int lane = threadIdx.x & 31, lane8 = lane & 7, unit = lane >> 3;
+  const int kv = unit % kUnits / G, grp = unit % G;
   const int page = 1 << c.page_shift;
   const size_t block = 2 * (size_t)kv_part_bytes(D, page);
   const int s = blockIdx.y;
-  const int n = a.n_new ? a.n_new[s] : a.rows;
+  int n = a.n_new ? a.n_new[s] : a.rows;
+  n = min(n, a.rows);
   const int before = max(c.seq_len[s], 0), pos0 = c.n_pos[s];
-  const int head_groups = (c.n_kv + kHeads - 1) / kHeads;
-  const int task = blockIdx.x * (kStThreads / 32) + (threadIdx.x >> 5);
-  const int j = task / head_groups, head0 = (task - j * head_groups) * kHeads;
-  if (j < a.rows && j < n) {
-    const int src = a.select ? a.select[(size_t)s * a.rows + j] : j;
-    const long long slot = (long long)before + j;
-    const int p = page_of(c, s, slot);
-    const bool store = p >= 0 && src >= 0 && src < a.m;
-    if (!store) {
-      if (head0 == 0 && lane == 0) atomicAdd(&work->dropped, 1ull);
-    } else {
-      const int kv = unit % kUnits / G, grp = unit % G, in = (int)(slot & (page - 1));
-      const KvRows& rows = kv ? a.v : a.k;
-      uint4 v[kStTurns];
+  const int head_groups = (c.n_kv + kHeads - 1) / kHeads, stride = gridDim.x * (kStThreads / 32);
+  const KvRows& rows = kv ? a.v : a.k;
+  struct Row {
+    uint4 v[kStTurns];
+    float w;
+    int j, head0, p;                                     // p: the page; -1: not stored
+  };
+  auto ask = [&](Row& r, int task) {
+    r.j = task / head_groups;
+    r.head0 = (task - r.j * head_groups) * kHeads;
+    r.p = -1;
+    if (r.j < n) {
+      const int src = a.select ? a.select[(size_t)s * a.rows + r.j] : r.j;
+      if (src >= 0 && src < a.m) {
+        r.p = page_of(c, s, (long long)before + r.j);
 #pragma unroll
-      for (int t = 0; t < kStTurns; ++t) {
-        const int head = head0 + t * kHeadsATurn + unit / kUnits;
-        v[t] = make_uint4(0, 0, 0, 0);
-        if (head < c.n_kv) v[t] = *reinterpret_cast<const uint4*>(rows.at(s, src, head) + grp * kKvGroup + lane8 * 8);
-      }
-      const float w = a.weight && lane < kHeads && head0 + lane < c.n_kv
-                          ? a.weight[((size_t)s * c.n_kv + head0 + lane) * a.m + src] : 0.f;
-#pragma unroll
-      for (int t = 0; t < kStTurns; ++t) {
-        const int head = head0 + t * kHeadsATurn + unit / kUnits;
-        uint32_t meta;
-        const uint32_t codes = quantise64<kBf16>(v[t], meta);
-        if (head < c.n_kv) {
-          unsigned char* b = c.pages + ((size_t)p * c.n_kv + head) * block + kv * (block / 2);
-          *reinterpret_cast<uint32_t*>(b + ((size_t)grp * page + in) * 32 + lane8 * 4) = codes;
-          if (lane8 == 0) *reinterpret_cast<uint32_t*>(b + (size_t)G * page * 32 + ((size_t)in * G + grp) * 4) = meta;
+        for (int t = 0; t < kStTurns; ++t) {
+          const int head = r.head0 + t * kHeadsATurn + unit / kUnits;
+          r.v[t] = make_uint4(0, 0, 0, 0);
+          if (head < c.n_kv) r.v[t] = *reinterpret_cast<const uint4*>(rows.at(s, src, head) + grp * kKvGroup + lane8 * 8);
         }
-      }
-      if (lane < kHeads && head0 + lane < c.n_kv) {
-        const size_t at = ((size_t)p * c.n_kv + head0 + lane) * page + in;
-        c.weight[at] = w;
-        c.pos[at] = pos0 + j;
+        r.w = a.weight && lane < kHeads && r.head0 + lane < c.n_kv
+                  ? a.weight[((size_t)s * c.n_kv + r.head0 + lane) * a.m + src] : 0.f;
       }
     }
+  };
+  int task = blockIdx.x * (kStThreads / 32) + (threadIdx.x >> 5);
+  Row cur, next;
+  ask(cur, task);
+  while (cur.j < n) {
+    ask(next, task += stride);
+    if (cur.p < 0) {
+      if (cur.head0 == 0 && lane == 0) atomicAdd(&work->dropped, 1ull);
+    } else {
+      const int in = (before + cur.j) & (page - 1);
+#pragma unroll
+      for (int t = 0; t < kStTurns; ++t) {
+        const int head = cur.head0 + t * kHeadsATurn + unit / kUnits;
+        uint32_t meta;
+        const uint32_t codes = quantise64<kBf16>(cur.v[t], meta);
+        if (head < c.n_kv) {
+          unsigned char* b = c.pages + ((size_t)cur.p * c.n_kv + head) * block + kv * (block / 2);
+          *reinterpret_cast<uint32_t*>(b + (grp * page + in) * 32 + lane8 * 4) = codes;
+          if (lane8 == 0) *reinterpret_cast<uint32_t*>(b + (G * page * 8 + in * G + grp) * 4) = meta;
+        }
+      }
+      if (lane < kHeads && cur.head0 + lane < c.n_kv) {
+        const size_t at = ((size_t)cur.p * c.n_kv + cur.head0 + lane) * page + in;
+        c.weight[at] = cur.w;
+        c.pos[at] = pos0 + cur.j;
+      }
+    }
+    cur = next;
   }
   if (last_block(&work->arrivals, gridDim.x * gridDim.y)) {
     const long long room = (long long)c.max_pages << c.page_shift;
@@ -205,10 +226,11 @@ kv_read_kernel(const KvView c, const KvReadArgs a) {
     }
 }
 
-cudaError_t launch_kv_append(const KvView& c, const KvAppendArgs& a, int head_dim, bool bf16, cudaStream_t st) {
+cudaError_t launch_kv_append(const KvView& c, const KvAppendArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st) {
   const int heads = kStTurns * 4 / (2 * (head_dim / kKvGroup));
   const long long tasks = (long long)a.rows * ((c.n_kv + heads - 1) / heads);
-  const dim3 grid((unsigned)((tasks + kStThreads / 32 - 1) / (kStThreads / 32)), c.n_seq);
+  const long long want = (tasks + kStThreads / 32 - 1) / (kStThreads / 32), most = (3LL * sms + c.n_seq - 1) / c.n_seq;
+  const dim3 grid((unsigned)(want < most ? want : most), c.n_seq);       // three blocks an SM
   auto go = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(kStThreads), 0, st, c, a); };
   if (head_dim == 64) return bf16 ? go(kv_append_kernel<64, true>) : go(kv_append_kernel<64, false>);
   return bf16 ? go(kv_append_kernel<128, true>) : go(kv_append_kernel<128, false>);
