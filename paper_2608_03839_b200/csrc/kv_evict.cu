@@ -40,6 +40,15 @@ struct EvictShared {
   uint32_t all_holes[kEvMaxCluster], all_movers[kEvMaxCluster];    // every block's
 };
 
+// A block alone takes its own memory and its own barrier.
+template <typename T> __device__ __forceinline__ T* of_block(cg::cluster_group& cl, int n_blocks, T* p, int r) {
+  return n_blocks == 1 ? p : cl.map_shared_rank(p, r);
+}
+__device__ __forceinline__ void sync_blocks(cg::cluster_group& cl, int n_blocks) {
+  if (n_blocks == 1) __syncthreads();
+  else cl.sync();
+}
+
 // Finds the digit d with  sum of hist[> d] < want <= sum of hist[>= d]  (descending = true), or
 // the same counted from the low end, over all blocks' counts; sh.below = the sum strictly in
 // front of d, sh.count that of d.  All threads.
@@ -50,7 +59,7 @@ __device__ __forceinline__ void find_digit(EvictShared& sh, cg::cluster_group& c
   uint4 x4[kEvMaxCluster];
 #pragma unroll
   for (int r = 0; r < kEvMaxCluster; ++r)
-    if (r < n_blocks) x4[r] = *reinterpret_cast<const uint4*>(cl.map_shared_rank(sh.hist, r) + b);
+    if (r < n_blocks) x4[r] = *reinterpret_cast<const uint4*>(of_block(cl, n_blocks, sh.hist, r) + b);
 #pragma unroll
   for (int r = 0; r < kEvMaxCluster; ++r)
     if (r < n_blocks) { c.x += x4[r].x; c.y += x4[r].y; c.z += x4[r].z; c.w += x4[r].w; }
@@ -96,7 +105,7 @@ __device__ __forceinline__ uint32_t warp_inclusive(uint32_t x, int lane) {
   return x;
 }
 
-__global__ void __launch_bounds__(kEvThreads)
+__global__ void __launch_bounds__(kEvThreads, 2)
 kv_evict_kernel(const KvView c, const KvEvictArgs a, int groups) {
   extern __shared__ __align__(16) unsigned char smem[];
   cg::cluster_group cl = cg::this_cluster();
@@ -164,12 +173,12 @@ kv_evict_kernel(const KvView c, const KvEvictArgs a, int groups) {
         n_safe = __reduce_add_sync(0xffffffffu, n_safe);
         if (lane == 0 && n_safe) atomicAdd(&sh.safe, n_safe);
       }
-      cl.sync();
+      sync_blocks(cl, n_blocks);
       if (pass == 0) {
         // positions are distinct, so at most sink + recent <= budget slots are safe; should a
         // caller's be not, the first ones in slot order stay
         uint32_t all = 0;
-        for (int r = 0; r < n_blocks; ++r) all += *cl.map_shared_rank(&sh.safe, r);
+        for (int r = 0; r < n_blocks; ++r) all += *of_block(cl, n_blocks, &sh.safe, r);
         want = all >= (uint32_t)budget ? 0u : (uint32_t)budget - all;
         if (want == 0) break;
       }
@@ -177,7 +186,7 @@ kv_evict_kernel(const KvView c, const KvEvictArgs a, int groups) {
       want -= sh.below;
       if (by_pos) { ppre |= sh.digit << shift; pmask |= dmask << shift; }
       else { prefix |= sh.digit << shift; mask |= dmask << shift; }
-      cl.sync();                                         // the counts may be cleared
+      sync_blocks(cl, n_blocks);                                         // the counts may be cleared
     }
     // kept: safe, or order > prefix, or order == prefix and (position below ppre, or equal to it
     // and among the first `want`); without by_pos every tie is kept
@@ -207,14 +216,14 @@ kv_evict_kernel(const KvView c, const KvEvictArgs a, int groups) {
       }
     }
     if (lane == 0) { atomicAdd(&sh.sure, n_sure); atomicAdd(&sh.ties, n_ties); }
-    cl.sync();
+    sync_blocks(cl, n_blocks);
     // exact ties (equal weight and position) and an excess of safe slots: the first in slot order
     if (warp == 0) {
       uint32_t left = by_pos ? want : 0u, kept = 0;
       for (int r = 0; r < me; ++r) {
-        const uint32_t t = min(left, *cl.map_shared_rank(&sh.ties, r));
+        const uint32_t t = min(left, *of_block(cl, n_blocks, &sh.ties, r));
         left -= t;
-        kept += t + *cl.map_shared_rank(&sh.sure, r);
+        kept += t + *of_block(cl, n_blocks, &sh.sure, r);
       }
       uint32_t holes = 0, movers = 0;
       for (int b0 = 0; b0 < words; b0 += 32) {
@@ -241,11 +250,11 @@ kv_evict_kernel(const KvView c, const KvEvictArgs a, int groups) {
       }
       if (lane == 0) { sh.holes = holes; sh.movers = movers; }
     }
-    cl.sync();
+    sync_blocks(cl, n_blocks);
     // ---- the moves ----
     if (tid < n_blocks) {
-      sh.all_holes[tid] = *cl.map_shared_rank(&sh.holes, tid);
-      sh.all_movers[tid] = *cl.map_shared_rank(&sh.movers, tid);
+      sh.all_holes[tid] = *of_block(cl, n_blocks, &sh.holes, tid);
+      sh.all_movers[tid] = *of_block(cl, n_blocks, &sh.movers, tid);
     }
     // every block's bits and ranks, where they fit beside one another
     const int all_words = (len + 31) / 32;
@@ -253,9 +262,9 @@ kv_evict_kernel(const KvView c, const KvEvictArgs a, int groups) {
     if (a.gather)
       for (int w = tid; w < all_words; w += kEvThreads) {
         const int r = w / per, i = w - r * per;
-        every[w] = cl.map_shared_rank(keep, r)[i];
-        every[a.gather + w] = cl.map_shared_rank(rank_h, r)[i];
-        every[2 * a.gather + w] = cl.map_shared_rank(rank_m, r)[i];
+        every[w] = of_block(cl, n_blocks, keep, r)[i];
+        every[a.gather + w] = of_block(cl, n_blocks, rank_h, r)[i];
+        every[2 * a.gather + w] = of_block(cl, n_blocks, rank_m, r)[i];
       }
     __syncthreads();
     uint32_t n_moves = 0;
@@ -271,13 +280,13 @@ kv_evict_kernel(const KvView c, const KvEvictArgs a, int groups) {
         i -= here;
       }
       const int base = r * per, nw = min(per, all_words - base);
-      const uint32_t* rk = a.gather ? every + (hole ? a.gather : 2 * a.gather) + base : cl.map_shared_rank(hole ? rank_h : rank_m, r);
+      const uint32_t* rk = a.gather ? every + (hole ? a.gather : 2 * a.gather) + base : of_block(cl, n_blocks, hole ? rank_h : rank_m, r);
       int lo = 0, hi = nw - 1;
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (rk[mid] <= i) lo = mid; else hi = mid - 1;
       }
-      const uint32_t k = a.gather ? every[base + lo] : cl.map_shared_rank(keep, r)[lo];
+      const uint32_t k = a.gather ? every[base + lo] : of_block(cl, n_blocks, keep, r)[lo];
       const int at = (base + lo) * 32;
       const uint32_t low = at + 32 <= budget ? 0xffffffffu : at >= budget ? 0u : (1u << (budget - at)) - 1u;
       return at + nth_bit(hole ? ~k & low : k & ~low, (int)(i - rk[lo]));
@@ -293,11 +302,11 @@ kv_evict_kernel(const KvView c, const KvEvictArgs a, int groups) {
       __syncthreads();
       const int count = (int)min((n_moves - m0 + n_blocks - 1) / n_blocks, (uint32_t)kEvThreads);
       // lanes 0..7: 16 bytes of codes (two for each 32 of K, V and each group), a word of meta, the
-      // weight and the position; four moves' loads on their way together
+      // weight and the position; three moves' loads on their way together
       const int part = groups * page * 36;
       const int kv = lane8 / (2 * groups), c_off = kv * part + (lane8 / 2 % groups) * page * 32 + (lane8 & 1) * 16;
       const int m_off = lane8 / groups * part + groups * page * 32 + lane8 % groups * 4;
-      constexpr int kAtOnce = 4;
+      constexpr int kAtOnce = 3;
       for (int k0 = tid >> 3; k0 < count; k0 += kAtOnce * (kEvThreads / 8)) {
         int4 mv[kAtOnce];
         uint4 code[kAtOnce];
@@ -328,7 +337,7 @@ kv_evict_kernel(const KvView c, const KvEvictArgs a, int groups) {
       }
       __syncthreads();
     }
-    cl.sync();                                           // (others may still read this block's bits)
+    sync_blocks(cl, n_blocks);                                           // (others may still read this block's bits)
   }
   // ---- the lengths, once nobody reads them any more ----
   __syncthreads();
