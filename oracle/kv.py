@@ -95,7 +95,7 @@ def evict(weight, pos, n_pos, budget, sink, recent):
     n = len(weight)
     w = np.where(np.isnan(weight), -np.inf, weight).astype(np.float64)
     safe = (pos < sink) | (pos >= n_pos - recent)
-    order = sorted(range(n), key=lambda i: (not safe[i], 0.0 if safe[i] else -w[i], 0 if safe[i] else pos[i], i))
+    order = sorted(range(n), key=lambda i: (not safe[i], 0.0 if safe[i] else -w[i], pos[i], i))
     keep = np.zeros(n, bool)
     keep[order[:budget]] = True
     src = np.arange(min(n, budget))

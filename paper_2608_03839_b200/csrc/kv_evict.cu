@@ -22,6 +22,7 @@ namespace cg = cooperative_groups;
 namespace oilbird {
 
 constexpr int kEvThreads = 512, kEvWarps = 16, kEvBins = 2048, kEvMaxCluster = 8;
+constexpr int kEvFew = 16;                               // slots dropped one by one at most
 
 // Order-preserving integer of a weight; NaN below everything, -0 as +0.
 __device__ __forceinline__ uint32_t weight_order(float w) {
@@ -30,13 +31,17 @@ __device__ __forceinline__ uint32_t weight_order(float w) {
   return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
 
+// The order of a slot that has to stay: above every weight's.
+constexpr uint32_t kEvStays = 0xfffffffeu, kEvGone = 0xffffffffu;
+
 struct EvictShared {
   uint32_t hist[kEvBins];
   int4 moves[kEvThreads];            // pages and slots in them: source, destination
   uint32_t warp_sum[kEvWarps];
+  uint4 last[2][kEvWarps];           // the slot each warp would drop next
   uint32_t digit, below, count;
-  // what the other blocks of the cluster read: safe slots; kept for sure, ties; holes, movers
-  uint32_t safe, sure, ties, holes, movers;
+  // what the other blocks of the cluster read: slots that tie with the last one kept; holes, movers
+  uint32_t ties, holes, movers;
   uint32_t all_holes[kEvMaxCluster], all_movers[kEvMaxCluster];    // every block's
 };
 
@@ -82,6 +87,13 @@ __device__ __forceinline__ void find_digit(EvictShared& sh, cg::cluster_group& c
     before += n;
   }
   __syncthreads();
+}
+
+// The least (x, y, z) of the warp's, in lexical order.
+__device__ __forceinline__ uint4 warp_least(const uint4& v) {
+  const uint32_t x = __reduce_min_sync(0xffffffffu, v.x);
+  const uint32_t y = __reduce_min_sync(0xffffffffu, v.x == x ? v.y : 0xffffffffu);
+  return make_uint4(x, y, __reduce_min_sync(0xffffffffu, v.x == x && v.y == y ? v.z : 0xffffffffu), 0u);
 }
 
 // Position of the n-th set bit (from 0) of w.
@@ -135,121 +147,143 @@ kv_evict_kernel(const KvView c, const KvEvictArgs a, int groups) {
       const size_t at = ((size_t)(have ? p : 0) * c.n_kv + head) * page + (slot & (page - 1));
       const float w = c.weight[at];
       const int32_t x = c.pos[at];                       // (no page: below everything)
-      return have ? make_uint2(weight_order(w), (uint32_t)x) : make_uint2(0u, 2147483647u);
+      return have ? make_uint2(x < a.sink || x >= newest ? kEvStays : weight_order(w), (uint32_t)x) : make_uint2(0u, 2147483647u);
     };
-    if (tid == 0) sh.safe = 0;
-    __syncthreads();
-    uint32_t n_safe = 0;
     if (a.held) {
 #pragma unroll 8
       for (int i = tid; i < n; i += kEvThreads) held[i] = fetch(i);
     }
     auto slot_at = [&](int i) { return a.held ? held[i] : fetch(i); };
-    auto safe_at = [&](const uint2& x) { return x.y != 2147483647u && ((int)x.y < a.sink || (int)x.y >= newest); };
-    // ---- radix selection ----
-    uint32_t prefix = 0, mask = 0, want = 0;             // of the weights' order
+    uint32_t prefix = 0, mask = 0, want = budget;        // of the order; how many of it are kept
     uint32_t ppre = 0, pmask = 0;                        // of the positions, among ties
     bool by_pos = false;
-    for (int pass = 0; pass < 6; ++pass) {
-      if (pass == 3) {
-        // ties with the last kept weight: all of them, or the lowest positions
-        if (sh.count == want) break;
-        by_pos = true;
+    if (tid == 0) sh.ties = 0;
+    if (n_blocks == 1 && a.held && len - budget <= kEvFew) {
+      // ---- few over the budget: the last in order go one by one ----
+      auto last_of = [&]() {
+        uint4 v = make_uint4(kEvGone, 0u, 0u, 0u);
+        for (int i = tid; i < n; i += kEvThreads) {
+          const uint2 x = held[i];
+          const uint32_t y = ~(x.y ^ 0x80000000u), z = ~(uint32_t)i;
+          if (x.x < v.x || (x.x == v.x && (y < v.y || (y == v.y && z < v.z)))) v = make_uint4(x.x, y, z, 0u);
+        }
+        return v;
+      };
+      for (int w = tid; w < words; w += kEvThreads) {
+        keep[w] = w * 32 + 32 <= n ? 0xffffffffu : (1u << (n - w * 32)) - 1u;
+        rank_h[w] = 0u;
       }
-      const int shift = pass % 3 == 0 ? 21 : pass % 3 == 1 ? 10 : 0;
-      const uint32_t dmask = pass % 3 == 2 ? 1023u : 2047u;
-      for (int i = tid; i < kEvBins; i += kEvThreads) sh.hist[i] = 0;
-      __syncthreads();
-      for (int i = tid; i < n; i += kEvThreads) {
-        const uint2 x = slot_at(i);
-        const bool safe = safe_at(x);
-        n_safe += safe;
-        if (!safe && (x.x & mask) == prefix) {
-          const uint32_t key = by_pos ? x.y ^ 0x80000000u : x.x;
-          if (!by_pos || (key & pmask) == ppre) atomicAdd(&sh.hist[key >> shift & dmask], 1u);
+      uint4 mine = last_of();
+      for (int gone = 0; gone < len - budget; ++gone) {
+        const uint4 v = warp_least(mine);
+        if (lane == 0) sh.last[gone & 1][warp] = v;
+        __syncthreads();
+        const int i = (int)~warp_least(sh.last[gone & 1][lane & (kEvWarps - 1)]).z;
+        if (i % kEvThreads == tid) {
+          keep[i / 32] &= ~(1u << (i & 31));
+          held[i].x = kEvGone;
+          mine = last_of();
         }
       }
-      if (pass == 0) {
-        n_safe = __reduce_add_sync(0xffffffffu, n_safe);
-        if (lane == 0 && n_safe) atomicAdd(&sh.safe, n_safe);
+    } else {
+      // ---- radix selection ----
+      for (int pass = 0; pass < 6; ++pass) {
+        if (pass == 3) {
+          // ties with the last one kept: all of them, or the lowest positions
+          if (sh.count == want) break;
+          by_pos = true;
+        }
+        const int shift = pass % 3 == 0 ? 21 : pass % 3 == 1 ? 10 : 0;
+        const uint32_t dmask = pass % 3 == 2 ? 1023u : 2047u;
+        for (int i = tid; i < kEvBins; i += kEvThreads) sh.hist[i] = 0;
+        __syncthreads();
+        uint32_t n_stay = 0;                             // (many in one bin: not one by one)
+        for (int i = tid; i < n; i += kEvThreads) {
+          const uint2 x = slot_at(i);
+          if (pass == 0 && x.x == kEvStays) ++n_stay;
+          else if ((x.x & mask) == prefix) {
+            const uint32_t key = by_pos ? x.y ^ 0x80000000u : x.x;
+            if (!by_pos || (key & pmask) == ppre) atomicAdd(&sh.hist[key >> shift & dmask], 1u);
+          }
+        }
+        if (pass == 0) {
+          n_stay = __reduce_add_sync(0xffffffffu, n_stay);
+          if (lane == 0 && n_stay) atomicAdd(&sh.hist[kEvStays >> 21], n_stay);
+        }
+        sync_blocks(cl, n_blocks);
+        find_digit(sh, cl, n_blocks, want, !by_pos);
+        want -= sh.below;
+        if (by_pos) { ppre |= sh.digit << shift; pmask |= dmask << shift; }
+        else { prefix |= sh.digit << shift; mask |= dmask << shift; }
+        sync_blocks(cl, n_blocks);                       // the counts may be cleared
       }
-      sync_blocks(cl, n_blocks);
-      if (pass == 0) {
-        // positions are distinct, so at most sink + recent <= budget slots are safe; should a
-        // caller's be not, the first ones in slot order stay
-        uint32_t all = 0;
-        for (int r = 0; r < n_blocks; ++r) all += *of_block(cl, n_blocks, &sh.safe, r);
-        want = all >= (uint32_t)budget ? 0u : (uint32_t)budget - all;
-        if (want == 0) break;
-      }
-      find_digit(sh, cl, n_blocks, want, !by_pos);
-      want -= sh.below;
-      if (by_pos) { ppre |= sh.digit << shift; pmask |= dmask << shift; }
-      else { prefix |= sh.digit << shift; mask |= dmask << shift; }
-      sync_blocks(cl, n_blocks);                                         // the counts may be cleared
-    }
-    // kept: safe, or order > prefix, or order == prefix and (position below ppre, or equal to it
-    // and among the first `want`); without by_pos every tie is kept
-    const bool none = mask == 0;                         // nothing but safe slots
-    // ---- a bit per slot, in slot order ----
-    if (tid == 0) { sh.sure = sh.ties = sh.holes = sh.movers = 0; }
-    __syncthreads();
-    uint32_t n_sure = 0, n_ties = 0;
-    for (int i0 = 0; i0 < words * 32; i0 += kEvThreads) {
-      const int i = i0 + tid;
-      bool in = false, tie = false;
-      if (i < n) {
-        const uint2 x = slot_at(i);
-        in = safe_at(x);
-        if (!in && !none) {
+      // kept: order > prefix, or order == prefix and (position below ppre, or equal to it and among
+      // the first `want`); without by_pos every tie is kept
+      // ---- a bit per slot, in slot order ----
+      uint32_t n_ties = 0;
+      for (int i0 = 0; i0 < words * 32; i0 += kEvThreads) {
+        const int i = i0 + tid;
+        bool in = false, tie = false;
+        if (i < n) {
+          const uint2 x = slot_at(i);
           const uint32_t key = x.y ^ 0x80000000u;
           in = x.x > prefix || (x.x == prefix && (!by_pos || key < ppre));
           tie = by_pos && x.x == prefix && key == ppre;
         }
+        const uint32_t b = __ballot_sync(0xffffffffu, in), t = __ballot_sync(0xffffffffu, tie);
+        if (lane == 0 && i / 32 < words) {
+          keep[i / 32] = b;
+          rank_h[i / 32] = t;
+          n_ties += __popc(t);
+        }
       }
-      const uint32_t b = __ballot_sync(0xffffffffu, in), t = __ballot_sync(0xffffffffu, tie);
-      if (lane == 0 && i / 32 < words) {
-        keep[i / 32] = b;
-        rank_h[i / 32] = t;
-        n_sure += __popc(b);
-        n_ties += __popc(t);
-      }
+      if (lane == 0 && n_ties) atomicAdd(&sh.ties, n_ties);
     }
-    if (lane == 0) { atomicAdd(&sh.sure, n_sure); atomicAdd(&sh.ties, n_ties); }
     sync_blocks(cl, n_blocks);
-    // exact ties (equal weight and position) and an excess of safe slots: the first in slot order
-    if (warp == 0) {
-      uint32_t left = by_pos ? want : 0u, kept = 0;
-      for (int r = 0; r < me; ++r) {
-        const uint32_t t = min(left, *of_block(cl, n_blocks, &sh.ties, r));
-        left -= t;
-        kept += t + *of_block(cl, n_blocks, &sh.sure, r);
-      }
-      uint32_t holes = 0, movers = 0;
+    uint32_t ties = 0, left = want;                      // ties of all blocks; what is left for this one's
+    for (int r = 0; r < n_blocks; ++r) {
+      const uint32_t t = *of_block(cl, n_blocks, &sh.ties, r);
+      ties += t;
+      if (r < me) left -= min(left, t);
+    }
+    if (warp == 0 && by_pos && ties > want)
+      // equal in order and position, which a cache's slots are not: the first in slot order stay
       for (int b0 = 0; b0 < words; b0 += 32) {
         const int w = b0 + lane;
-        const uint32_t t = w < words && by_pos ? rank_h[w] : 0u, nt = __popc(t);
-        const uint32_t xt = warp_inclusive(nt, lane), before = xt - nt;
-        uint32_t k = (w < words ? keep[w] : 0u) | first_bits(t, before >= left ? 0u : left - before);
-        left -= min(left, __shfl_sync(0xffffffffu, xt, 31));
-        const uint32_t nk = __popc(k), xk = warp_inclusive(nk, lane), have = kept + xk - nk;
-        k = first_bits(k, have >= (uint32_t)budget ? 0u : (uint32_t)budget - have);
-        kept += __shfl_sync(0xffffffffu, xk, 31);
-        // slots of the word below the budget, and below the length
-        const int at = (w0 + w) * 32;
-        const uint32_t low = at + 32 <= budget ? 0xffffffffu : at >= budget ? 0u : (1u << (budget - at)) - 1u;
-        const uint32_t h = w < words ? ~k & low : 0u, m = w < words ? k & ~low : 0u;
-        const uint32_t xh = warp_inclusive(__popc(h), lane), xm = warp_inclusive(__popc(m), lane);
-        if (w < words) {
-          keep[w] = k;
-          rank_h[w] = holes + xh - __popc(h);
-          rank_m[w] = movers + xm - __popc(m);
-        }
-        holes += __shfl_sync(0xffffffffu, xh, 31);
-        movers += __shfl_sync(0xffffffffu, xm, 31);
+        const uint32_t t = w < words ? rank_h[w] : 0u;
+        const uint32_t x = warp_inclusive(__popc(t), lane), before = x - __popc(t);
+        if (w < words) rank_h[w] = first_bits(t, before >= left ? 0u : left - before);
+        left -= min(left, __shfl_sync(0xffffffffu, x, 31));
       }
-      if (lane == 0) { sh.holes = holes; sh.movers = movers; }
+    __syncthreads();
+    // the ranks: a word a thread, holes in the low and movers in the high half of what the warps
+    // add up (512 words of 32 slots at a time: below 2^15 each)
+    uint32_t holes = 0, movers = 0;
+    for (int b0 = 0; b0 < words; b0 += kEvThreads) {
+      const int w = b0 + tid, at = (w0 + w) * 32;
+      const uint32_t low = at + 32 <= budget ? 0xffffffffu : at >= budget ? 0u : (1u << (budget - at)) - 1u;
+      const uint32_t k = w < words ? keep[w] | rank_h[w] : 0u;
+      const uint32_t mine = w < words ? __popc(~k & low) + (__popc(k & ~low) << 16) : 0u;
+      const uint32_t x = warp_inclusive(mine, lane);
+      if (lane == 31) sh.warp_sum[warp] = x;
+      __syncthreads();
+      uint32_t before = x - mine, all = 0;
+#pragma unroll
+      for (int v = 0; v < kEvWarps; ++v) {
+        const uint32_t y = sh.warp_sum[v];
+        if (v < warp) before += y;
+        all += y;
+      }
+      if (w < words) {
+        keep[w] = k;
+        rank_h[w] = holes + (before & 0xffffu);
+        rank_m[w] = movers + (before >> 16);
+      }
+      holes += all & 0xffffu;
+      movers += all >> 16;
+      __syncthreads();
     }
+    if (tid == 0) { sh.holes = holes; sh.movers = movers; }
     sync_blocks(cl, n_blocks);
     // ---- the moves ----
     if (tid < n_blocks) {

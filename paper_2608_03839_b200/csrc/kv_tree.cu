@@ -176,7 +176,7 @@ struct TileInfo {                    // what the softmax warps need to know of a
   uint8_t flags[4];                  // by decoding warp; 1: new nodes, 2: some slot is not valid, 4: a value is not finite
 };
 struct TreeShared {
-  uint64_t kfull[2], kfree[2], vfull[2], vfree[2], sfull[2], pfull[2], pvdone[2], info_full[4], qfull;
+  uint64_t kfull, kfree, vfull[2], vfree[2], sfull[2], pfull[2], pvdone[2], info_full[4], qfull;
   uint64_t meet, peaks[2];           // the softmax warps; the decoding warps, by tile parity
   TileInfo info[4];
   uint32_t peak[4][kTrDecWarps][2];  // by tile: largest key and value bound each decoding warp saw
@@ -249,6 +249,39 @@ __device__ __forceinline__ uint4 decode8(uint32_t w, __half2 sc, __half2 lo) {
   return r;
 }
 
+// The same as the sum of two f16 numbers.  With mid = scale * 8 + lo an element is
+// scale (code - 8) + mid.  The scale's five leading bits sh and mid to the last of their places,
+// mh, make `hi` = sh (code - 8) + mh, which f16 holds exactly while |mid| < 58 scale (a group whose
+// middle lies within four times its range); what both left over makes `rest`, below scale / 2
+// and off by 2^-13 scale at most.  (Wider off centre, hi is rounded as one f16 number would be.)
+struct KeyParts { __half2 sh, sl, mh, ml; };
+__device__ __forceinline__ KeyParts key_parts(float scale, float lo) {
+  const uint32_t bits = __float_as_uint(scale);
+  const float sh = __uint_as_float(bits & 0xfff80000u), sl = scale - sh, mid = fmaf(8.f, scale, lo);
+  const float grid = __uint_as_float((bits & 0x7f800000u) + (19u << 23) | 0x400000u);     // sums with it end at sh's last place
+  const float m = __fsub_rn(__fadd_rn(mid, grid), grid);
+  KeyParts k;
+  k.sh = as_half2(pack16<false>(sh, sh));
+  k.sl = as_half2(pack16<false>(sl, sl));
+  k.mh = as_half2(pack16<false>(m, m));
+  const float ml = mid - __low2float(k.mh);
+  k.ml = as_half2(pack16<false>(ml, ml));
+  return k;
+}
+__device__ __forceinline__ void decode8_parts(uint32_t w, const KeyParts& k, uint4& hi, uint4& rest) {
+  const uint32_t magic = 0x64006400u;
+  const __half2 m1032 = __half2half2(__ushort_as_half(0xE408)), r16 = __half2half2(__ushort_as_half(0x2C00)),
+                m72 = __half2half2(__ushort_as_half(0xD480));
+  const uint32_t v = w >> 8;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t x = i < 2 ? w : v;
+    const __half2 c = i & 1 ? __hfma2(as_half2((x & 0x00f000f0u) | magic), r16, m72) : __hadd2(as_half2((x & 0x000f000fu) | magic), m1032);
+    (&hi.x)[i] = as_word(__hfma2(c, k.sh, k.mh));
+    (&rest.x)[i] = as_word(__hfma2(c, k.sl, k.ml));
+  }
+}
+
 }  // namespace
 
 template <int D, bool kBf16>
@@ -269,8 +302,6 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
 
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
-      bar_init(&sh.kfull[i], kTrDecWarps);
-      bar_init(&sh.kfree[i], 1);
       bar_init(&sh.vfull[i], kTrDecWarps);
       bar_init(&sh.vfree[i], 1);
       bar_init(&sh.sfull[i], 1);
@@ -279,6 +310,8 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
       bar_init(&sh.peaks[i], kTrDecWarps);
     }
     for (int i = 0; i < 4; ++i) bar_init(&sh.info_full[i], kTrDecWarps);
+    bar_init(&sh.kfull, kTrDecWarps);
+    bar_init(&sh.kfree, 1);
     bar_init(&sh.qfull, 8);
     bar_init(&sh.meet, 8);
     sh.gave_up = 0;
@@ -615,15 +648,14 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
       };
       auto block_of = [&](int q) { return c.pages + ((size_t)max(q, 0) * c.n_kv + p.head) * block_bytes; };
       auto slot_in = [&](int i) { return ((p.c0 + i) * kTrTile + sl) & (page - 1); };
-      auto copy_codes = [&](int q, int i) {
-        const unsigned char* b = block_of(q) + slot_in(i) * 32;
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv)
+      auto copy_codes = [&](int kv, int q, int i) {
+        const unsigned char* b = block_of(q) + slot_in(i) * 32 + kv * (block_bytes / 2);
+        if (i < cached)
 #pragma unroll
           for (int g = 0; g < G; ++g)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-              cp_async16(my_codes + (kv * G + g) * 32 + h * 16, b + kv * (block_bytes / 2) + g * page * 32 + h * 16, q < 0 ? 0 : 16);
+              cp_async16(my_codes + (kv * G + g) * 32 + h * 16, b + g * page * 32 + h * 16, q < 0 ? 0 : 16);
         cp_async_commit();
       };
       auto load_meta_of = [&](uint32_t (&m)[2][G], int q, int i) {
@@ -673,7 +705,8 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
         page_c = page_for(0);
         page_n = page_for(1);
         page_2 = page_for(2);
-        copy_codes(page_c, 0);
+        copy_codes(p.two, page_c, 0);                    // in the order of their use below
+        copy_codes(!p.two, page_c, 0);
         load_meta_of(mc, page_c, 0);
         load_meta_of(mn, page_n, 1);
         if (!p.nodes) post_meta(kt, mc);
@@ -682,55 +715,77 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
         const int st = kt & 1;
         const uint32_t ph = (kt >> 1) & 1;
         TileInfo& info = sh.info[kt & 3];
-        unsigned char *km = kmat + st * T::kMat, *vm = vmat + st * T::kMat;
+        unsigned char *km = kmat, *vm = vmat + st * T::kMat;
         if (i >= 0) {
           if (i + 1 < cached) post_meta(kt + 1, mn);
           uint32_t m2[2][G];
           load_meta_of(m2, page_2, i + 2);
           const int page_3 = page_for(i + 3);
-          cp_async_wait<0>();                            // (a thread reads its own copies alone)
-          uint4 code[2][G][2];
-#pragma unroll
-          for (int kv = 0; kv < 2; ++kv)
+          const uint32_t ballot = __ballot_sync(0xffffffffu, page_c >= 0);
+          // The keys' place is free only once this tile's scores could be next: with 256 rows the
+          // values are turned first.  With 128 it is free early, the values' only when the other
+          // group's are done: then the keys.  (Four tiles back, the place of the tile's info is
+          // free with either.)
+          int ek = 0, ev = 0;
+#pragma unroll 1
+          for (int part = 0; part < 2 && ok; ++part) {
+            const bool values = (part == 0) == p.two;
+            ok = warp_wait(values ? &sh.vfree[st] : &sh.kfree, (values ? ph : kt & 1) ^ 1, gave_up, stats);
+            if (ok && part == 0) {
+              ok = warp_wait(&sh.peaks[st], ph, gave_up, stats);
+              peaks_of(kt, ek, ev);
+              if (lane == 0) {
+                info.valid[dw] = ballot;
+                info.flags[dw] = ballot != 0xffffffffu ? 2 : 0;
+                if (dw == 0) {
+                  info.key_scale = pow2(ek);
+                  info.value_exp = (float)ev;
+                  info.value_scale = pow2(-ev);
+                }
+              }
+            }
+            if (!ok) break;
+            // the codes of this tile, and on to the next one's (a thread reads its own copies alone)
+            uint4 code[G][2];
+            cp_async_wait<1>();
 #pragma unroll
             for (int g = 0; g < G; ++g)
 #pragma unroll
               for (int h = 0; h < 2; ++h)
-                code[kv][g][h] = *reinterpret_cast<const uint4*>(codes + sl * T::kCodes + (kv * G + g) * 32 + h * 16);
-          if (i + 1 < cached) copy_codes(page_n, i + 1);
-          const uint32_t ballot = __ballot_sync(0xffffffffu, page_c >= 0);
-          // (free: so is, four tiles back, the place of the tile's info)
-          if (!warp_wait(&sh.kfree[st], ph ^ 1, gave_up, stats) || !warp_wait(&sh.peaks[st], ph, gave_up, stats)) { ok = false; break; }
-          int ek, ev;
-          peaks_of(kt, ek, ev);
-          if (lane == 0) {
-            info.valid[dw] = ballot;
-            info.flags[dw] = ballot != 0xffffffffu ? 2 : 0;
-            if (dw == 0) {
-              info.key_scale = pow2(ek);
-              info.value_exp = (float)ev;
-              info.value_scale = pow2(-ev);
-            }
-          }
+                code[g][h] = *reinterpret_cast<const uint4*>(codes + sl * T::kCodes + ((values ? G : 0) + g) * 32 + h * 16);
+            copy_codes(values, page_n, i + 1);
+            const float down = pow2(-(values ? ev : ek));
+            if (values) {
 #pragma unroll
-          for (int kv = 0; kv < 2; ++kv) {
-            if (kv == 1 && !warp_wait(&sh.vfree[st], ph ^ 1, gave_up, stats)) { ok = false; break; }
-            const float down = pow2(-(kv ? ev : ek));
+              for (int g = 0; g < G; ++g) {
+                const uint32_t m1 = mc[1][g];
+                const float fs = half_lo<kBf16>(m1) * down, fl = half_hi<kBf16>(m1) * down;
+                const __half2 sc = as_half2(pack16<false>(fs, fs)), lo = as_half2(pack16<false>(fl, fl));
+                unsigned char* dst = vm + g * (kTrTile * 128) + sl * 128;
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-              const uint32_t m1 = mc[kv][g];
-              const float fs = half_lo<kBf16>(m1) * down, fl = half_hi<kBf16>(m1) * down;
-              const __half2 sc = as_half2(pack16<false>(fs, fs)), lo = as_half2(pack16<false>(fl, fl));
-              unsigned char* dst = (kv ? vm : km) + g * (kTrTile * 128) + sl * 128;
+                for (int k = 0; k < 8; ++k)
+                  *reinterpret_cast<uint4*>(dst + ((k ^ (sl & 7)) << 4)) = decode8((&code[g][k >> 2].x)[k & 3], sc, lo);
+              }
+            } else {
 #pragma unroll
-              for (int k = 0; k < 8; ++k)
-                *reinterpret_cast<uint4*>(dst + ((k ^ (sl & 7)) << 4)) = decode8((&code[kv][g][k >> 2].x)[k & 3], sc, lo);
+              for (int g = 0; g < G; ++g) {
+                const uint32_t m1 = mc[0][g];
+                const KeyParts parts = key_parts(half_lo<kBf16>(m1) * down, half_hi<kBf16>(m1) * down);
+                unsigned char* dst = km + g * (kTrTile * 128) + sl * 128;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                  uint4 hi, rest;
+                  decode8_parts((&code[g][k >> 2].x)[k & 3], parts, hi, rest);
+                  *reinterpret_cast<uint4*>(dst + ((k ^ (sl & 7)) << 4)) = hi;
+                  *reinterpret_cast<uint4*>(dst + T::kMat + ((k ^ (sl & 7)) << 4)) = rest;
+                }
+              }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
-              bar_arrive(kv ? &sh.vfull[st] : &sh.kfull[st]);
-              if (kv == 0) bar_arrive(&sh.info_full[kt & 3]);
+              bar_arrive(values ? &sh.vfull[st] : &sh.kfull);
+              if (!values) bar_arrive(&sh.info_full[kt & 3]);
             }
           }
           if (!ok) break;
@@ -745,7 +800,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
           // ---- new nodes: 16-bit elements, slots 0..63 of the tile; the rest is zero ----
           // raw rows copied to where their f16 will lie and turned into f16 in place, as Q's: a
           // thread has one node's key or value
-          if (!warp_wait(&sh.kfree[st], ph ^ 1, gave_up, stats) || !warp_wait(&sh.vfree[st], ph ^ 1, gave_up, stats)) {
+          if (!warp_wait(&sh.kfree, (kt & 1) ^ 1, gave_up, stats) || !warp_wait(&sh.vfree[st], ph ^ 1, gave_up, stats)) {
             ok = false;
             break;
           }
@@ -805,11 +860,13 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
             }
             *at_chunk = w;
             at_chunk[64 * 128 / 16] = make_uint4(0, 0, 0, 0);   // slots 64..127 of the tile
+            if (dw < 2)                                  // (f16 holds the keys whole)
+              at_chunk[T::kMat / 16] = at_chunk[T::kMat / 16 + 64 * 128 / 16] = make_uint4(0, 0, 0, 0);
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) {
-            bar_arrive(&sh.kfull[st]);
+            bar_arrive(&sh.kfull);
             bar_arrive(&sh.vfull[st]);
             bar_arrive(&sh.info_full[kt & 3]);
           }
@@ -841,19 +898,22 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
         ++np;
         auto scores = [&](int u) {
           const uint32_t t = kt + (p.two ? u >> 1 : u);
-          const int st = t & 1, wg = u & 1;
-          if (!p.two || wg == 0) ok = ok && warp_wait(&sh.kfull[st], (t >> 1) & 1, gave_up, stats);
+          const int wg = u & 1;
+          if (!p.two || wg == 0) ok = ok && warp_wait(&sh.kfull, t & 1, gave_up, stats);
           if (!ok) return;
           fence_after();
-          const uint64_t qd = q_desc + (p.two && wg ? (uint64_t)(128 * 128 >> 4) : 0), kd = k_desc + (st ? kStage : 0);
+          const uint64_t qd = q_desc + (p.two && wg ? (uint64_t)(128 * 128 >> 4) : 0);
           const uint32_t to = tmem + wg * 256;
           if (issuer) {
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-              mma_ss(to, qd + (uint64_t)((k >> 2) * (256 * 128 >> 4) + (k & 3) * 2),
-                     kd + (uint64_t)((k >> 2) * (kTrTile * 128 >> 4) + (k & 3) * 2), s_idesc, k > 0);
+            for (int k = 0; k < D / 16; ++k) {           // the keys' leading parts and their rests
+              const uint64_t qk = qd + (uint64_t)((k >> 2) * (256 * 128 >> 4) + (k & 3) * 2);
+              const uint64_t kk = k_desc + (uint64_t)((k >> 2) * (kTrTile * 128 >> 4) + (k & 3) * 2);
+              mma_ss(to, qk, kk, s_idesc, k > 0);
+              mma_ss(to, qk, kk + kStage, s_idesc, 1u);
+            }
             commit(&sh.sfull[wg]);
-            if (!p.two || wg == 1) commit(&sh.kfree[st]);
+            if (!p.two || wg == 1) commit(&sh.kfree);
           }
           __syncwarp();
         };

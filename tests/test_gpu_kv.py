@@ -537,6 +537,19 @@ def test_evict_sequences_shared_by_several_blocks(most, budget):
                d=64, page=64, hkv=1)
 
 
+@pytest.mark.parametrize("over", [1, 2, 15, 16, 17, 18])
+@pytest.mark.parametrize("kind", ["weights", "ties", "all stay", "equal"])
+def test_evict_a_few_over_the_budget(over, kind):
+    """Up to 16 slots over go one by one, more by selection: the same slots either way."""
+    weights = heavy if kind == "weights" else lambda c, s: torch.randint(0, 2, s, generator=c.g, device="cuda").float()
+    pos = {"weights": None,
+           "ties": lambda c, s: torch.randperm(int(np.prod(s)), generator=c.g, device="cuda").int().view(s) % 700,
+           "all stay": lambda c, s: torch.randint(0, 20, s, generator=c.g, device="cuda").int() + 5000,
+           "equal": lambda c, s: torch.full(s, 7, dtype=torch.int32, device="cuda")}[kind]
+    for budget in (3, 33, 600):
+        evict_case([budget + over, budget + 1, budget + over // 2, over], budget, 1, budget // 4, weights, pos=pos)
+
+
 def test_evict_equal_positions_too():
     """Positions a caller has repeated: the lowest slots stay."""
     evict_case([200], 50, 0, 0, lambda c, s: torch.ones(s, device="cuda"), pos=lambda c, s: torch.full(s, 7, dtype=torch.int32, device="cuda"))
