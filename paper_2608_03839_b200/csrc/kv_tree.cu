@@ -44,7 +44,7 @@ namespace {
 constexpr int kTrTile = 128, kTrFront = 4;               // slots a tile; see TileListOf
 constexpr int kTrDecWarps = 4, kTrIssuer = 12, kTrThreads = 512;
 // registers a thread: launched with 128; the four warpgroups' shares add up to 4 x 128
-constexpr int kTrSoftRegs = 192, kTrDecRegs = 96, kTrIssueRegs = 32;
+constexpr int kTrSoftRegs = 192, kTrDecRegs = 104, kTrIssueRegs = 24;
 static_assert(2 * kTrSoftRegs + kTrDecRegs + kTrIssueRegs == 4 * 128, "more registers than the block was launched with");
 using TreeList = TileListOf<kTrTile, kTrFront, 0>;
 constexpr float kTrLn2 = 0.6931471805599453f;
@@ -705,8 +705,8 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
         page_c = page_for(0);
         page_n = page_for(1);
         page_2 = page_for(2);
-        copy_codes(p.two, page_c, 0);                    // in the order of their use below
-        copy_codes(!p.two, page_c, 0);
+        copy_codes(0, page_c, 0);                        // in the order of their use below
+        copy_codes(1, page_c, 0);
         load_meta_of(mc, page_c, 0);
         load_meta_of(mn, page_n, 1);
         if (!p.nodes) post_meta(kt, mc);
@@ -722,16 +722,14 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
           load_meta_of(m2, page_2, i + 2);
           const int page_3 = page_for(i + 3);
           const uint32_t ballot = __ballot_sync(0xffffffffu, page_c >= 0);
-          // The keys' place is free only once this tile's scores could be next: with 256 rows the
-          // values are turned first.  With 128 it is free early, the values' only when the other
-          // group's are done: then the keys.  (Four tiles back, the place of the tile's info is
-          // free with either.)
+          // The keys, whose one place is free once the last tile's scores are there, then the values.
+          // (With the keys' place, four tiles back, the place of the tile's info is free.)
           int ek = 0, ev = 0;
 #pragma unroll 1
           for (int part = 0; part < 2 && ok; ++part) {
-            const bool values = (part == 0) == p.two;
+            const bool values = part == 1;
             ok = warp_wait(values ? &sh.vfree[st] : &sh.kfree, (values ? ph : kt & 1) ^ 1, gave_up, stats);
-            if (ok && part == 0) {
+            if (ok && !values) {
               ok = warp_wait(&sh.peaks[st], ph, gave_up, stats);
               peaks_of(kt, ek, ev);
               if (lane == 0) {
