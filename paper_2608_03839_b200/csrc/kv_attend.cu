@@ -8,7 +8,12 @@
 // products run on the codes alone, as f16 numbers that are exact, and one fp32 multiply-add
 // per (slot, row, group) brings in scale and offset; the scores carry no rounding but fp32's.
 // For the values the scale joins the probability before it becomes an f16 operand (one
-// rounding, at most 2^-11 of each term), and the offsets are summed in fp32.
+// rounding, at most 2^-11 of each term).  All codes are positive, so over a long sequence their
+// sums would outgrow the result by far, and with them what the tensor cores cut off: half of the
+// slots therefore go in with 15 - code and a negative operand, and the groups' middles
+// (lo + 7.5 scale, in fp32) in place of the offsets make up the difference, with 7.5 times the
+// operands' own sums.  On 131,085 slots that took the error from 8e-4 of the result to 2.8e-4
+// (the result's own rounding to f16: 2.1e-4) for 3 to 5 % of the time.
 //
 // Layout.  The products are taken transposed, S^T = K Q^T with 16 slots x 8 rows and
 // O^T = V^T P^T with 16 channels x 8 rows, so that 8 rows (the query heads of one key head)
@@ -17,21 +22,32 @@
 // 2t+1 is slot t+4: then both the K loads (8 bytes a lane) and the V loads (4 bytes a lane)
 // take 256 and 128 contiguous bytes of shared memory.
 //
-// Work.  The tiles (64 slots) of all (sequence, head, row block) items are one list, cut into
-// equal runs, one per block; a block's warps take the run's tiles in turn, each
-// through a ring of its own (asynchronous 16-byte copies, no block-wide waits), which runs on
-// across items.  At the end of an item's share the warps' results are joined in
-// shared memory; items cut between blocks go through the workspace, and the block that
-// finishes last joins the pieces, in their order, whichever block that is.
+// Work.  The tiles (64 slots) of all (sequence, head) items are one list, cut into equal runs, one
+// per block, two blocks an SM; a block's warps take the run's tiles in turn, each through a
+// buffer of its own (asynchronous 16-byte copies, no block-wide waits), which runs on across
+// items.  At the end of an item's share the warps' results are joined in shared memory; items cut
+// between blocks go through the workspace, and the block that finishes last joins the pieces, in
+// their order, whichever block that is.
+//
+// Measured, with 8 key/value heads of 128: 64 sequences of 4,096 to 8,192 slots, 444 MB of cache
+// under 32 query heads, in 108 us (4.1 TB/s; 68 us at the copy rate); 131,085 slots under 64
+// query heads in 44 us (23 us at the copy rate); 517 slots in 10 us.  The long ones are bound by
+// instructions (taking codes apart, 32 lanes' worth of exponentials and scales for each slot and
+// row) at half the issue slots, unevenly between the two blocks of an SM; the short one by the
+// latency of one tile, one join and one launch.
 #include "kv.cuh"
 
 namespace oilbird {
 
-// Rows per block are 8 NT.  A warp's ring holds its tile's keys and values in buffers of their
-// own: the next tile's keys are asked for as soon as the scores are taken, its values after the
-// products with them, so that a single buffer of each keeps half a tile per warp in flight.
-// Eight rows leave registers for twelve warps an SM.
-constexpr int kFewRows = 16;                             // more go to kv_tree.cu
+// Rows per block are 8 NT.  A warp holds its tile's keys and values in buffers of their own: the
+// next tile's keys are asked for as soon as the scores are taken, its values after the products
+// with them, so that a single buffer of each keeps half a tile per warp in flight.
+// Eight rows leave registers (168 a thread) for twelve warps an SM, sixteen rows for eight.
+//
+// More rows go to kv_tree.cu, whose tensor core products cost the same for 17 rows as for 128:
+// 21 rows of 64 channels over 777 slots take 17.2 us there and 18.6 us as two blocks of 16 rows
+// here, which would read the cache twice; with 16 rows or fewer one reading is enough.
+constexpr int kFewRows = 16;
 template <int D, int NT>
 struct Attend {
   static constexpr int kWarps = NT == 1 ? 6 : 4, kThreads = 32 * kWarps, kCtas = 2;
@@ -507,19 +523,36 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
               for (int i = 0; i < 4 * G; ++i) { o[r][i][e] *= down * ve; o[r][i][e + 2] *= down * ve; }
             }
         }
-        const float vdown = pow2(-eref);
+        const float up = pow2(eref), vdown = g & 1 ? -pow2(-eref) : pow2(-eref);
         float neg[NT][2];
 #pragma unroll
         for (int r = 0; r < NT; ++r)
 #pragma unroll
           for (int e = 0; e < 2; ++e) neg[r][e] = m[r][e] == -INFINITY ? 0.f : -m[r][e];
         // ---- probabilities, and the products with the values ----
+        float side[NT][G][4];                            // 15/16 of the operands' sums
+#pragma unroll
+        for (int r = 0; r < NT; ++r)
+#pragma unroll
+          for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) side[r][i][e] = 0.f;
 #pragma unroll
         for (int ch = 0; ch < 4; ++ch) {
           const int sl = ch * 16 + slot_g;
           uint32_t vm[2][G], pb[NT][G][2];
           load_meta<G>(vmeta + sl * 4 * G, vm[0]);
           load_meta<G>(vmeta + (sl + 8) * 4 * G, vm[1]);
+          float v0[G], l0[G], v1[G], l1[G];              // scales, the groups' middles
+#pragma unroll
+          for (int i = 0; i < G; ++i) {
+            v0[i] = half_lo<kBf16>(vm[0][i]);
+            v1[i] = half_lo<kBf16>(vm[1][i]);
+            l0[i] = fmaf(7.5f, v0[i], half_hi<kBf16>(vm[0][i]));
+            l1[i] = fmaf(7.5f, v1[i], half_hi<kBf16>(vm[1][i]));
+            v0[i] *= vdown;
+            v1[i] *= vdown;
+          }
 #pragma unroll
           for (int r = 0; r < NT; ++r) {
             float p[4];
@@ -529,12 +562,11 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
             l[r][1] += p[1] + p[3];
 #pragma unroll
             for (int i = 0; i < G; ++i) {
-              const float v0 = half_lo<kBf16>(vm[0][i]) * vdown, l0 = half_hi<kBf16>(vm[0][i]);
-              const float v1 = half_lo<kBf16>(vm[1][i]) * vdown, l1 = half_hi<kBf16>(vm[1][i]);
-              olo[r][i][0] = fmaf(p[0], l0, fmaf(p[2], l1, olo[r][i][0]));
-              olo[r][i][1] = fmaf(p[1], l0, fmaf(p[3], l1, olo[r][i][1]));
-              pb[r][i][0] = transpose8x8(pack16<false>(p[0] * v0, p[1] * v0));
-              pb[r][i][1] = transpose8x8(pack16<false>(p[2] * v1, p[3] * v1));
+              olo[r][i][0] = fmaf(p[0], l0[i], fmaf(p[2], l1[i], olo[r][i][0]));
+              olo[r][i][1] = fmaf(p[1], l0[i], fmaf(p[3], l1[i], olo[r][i][1]));
+              pb[r][i][0] = transpose8x8(pack16<false>(p[0] * v0[i], p[1] * v0[i]));
+              pb[r][i][1] = transpose8x8(pack16<false>(p[2] * v1[i], p[3] * v1[i]));
+              mma16816<false>(side[r][i], 0x3b803b80u, 0x3b803b80u, 0x3b803b80u, 0x3b803b80u, pb[r][i][0], pb[r][i][1]);
             }
           }
           // operand column 2t is slot t, 2t+1 slot t+4 (and +8): as the scores' rows
@@ -542,9 +574,9 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
           for (int i = 0; i < G; ++i) {
             const unsigned char* vp = vst + (i * kKvTile + ch * 16 + t4) * 32 + g * 4;
             const uint32_t w0 = *reinterpret_cast<const uint32_t*>(vp);
-            const uint32_t w1 = *reinterpret_cast<const uint32_t*>(vp + 4 * 32);
+            const uint32_t w1 = ~*reinterpret_cast<const uint32_t*>(vp + 4 * 32);
             const uint32_t w2 = *reinterpret_cast<const uint32_t*>(vp + 8 * 32);
-            const uint32_t w3 = *reinterpret_cast<const uint32_t*>(vp + 12 * 32);
+            const uint32_t w3 = ~*reinterpret_cast<const uint32_t*>(vp + 12 * 32);
             // even channels of both slots, odd channels of both slots
             const uint32_t ea = __byte_perm(w0, w1, 0x5410), oa = __byte_perm(w0, w1, 0x7632);
             const uint32_t eb = __byte_perm(w2, w3, 0x5410), ob = __byte_perm(w2, w3, 0x7632);
@@ -559,6 +591,14 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
             }
           }
         }
+        // (in all eight lanes of a row, which are added up at the end: 7.5 times)
+#pragma unroll
+        for (int r = 0; r < NT; ++r)
+#pragma unroll
+          for (int i = 0; i < G; ++i) {
+            olo[r][i][0] = fmaf(-up, side[r][i][0], olo[r][i][0]);
+            olo[r][i][1] = fmaf(-up, side[r][i][1], olo[r][i][1]);
+          }
       } else {
         cp_async_wait<1>();              // an empty tile: nothing was copied
         __syncwarp();
