@@ -4,8 +4,12 @@
 // share the 64 channels of a group, agree on its minimum and maximum (as packed 16-bit
 // numbers, three shuffles for both), and write one word of codes each and one word of scale and
 // offset; a token's group costs 128 bytes in and 36 out.  read: the same lanes, the other way,
-// four slots at a time.  All loads of a warp are on their way before the first is used.  Both
-// are bound by memory on long inputs and by latency on a decoding step's few rows.
+// four slots at a time.  All loads of a warp are on their way before the first is used.
+//
+// Measured, with 8 heads of 128: 4 prompts of 2,048 to 4,096 rows (12,800 in all) are stored in
+// 31 us (68 MB, 2.2 TB/s; bound by the instructions of minima, quotients and packing) and read
+// in 16 us (with the zeros behind the shorter ones 85 MB, 5.3 TB/s: memory); 16 paths of four to
+// seven rows in 7 and 4.6 us: latency of a launch and three dependent loads.
 //
 // The quotient (x - lo) / scale is IEEE division's, by Markstein's correction of a product with
 // the reciprocal (one division a group): q = x r, q += (x - q scale) r.
