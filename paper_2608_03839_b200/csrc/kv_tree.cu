@@ -738,7 +738,10 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
           int ek = 0, ev = 0;
 #pragma unroll 1
           for (int part = 0; part < 2 && ok; ++part) {
-            const bool values = part == 1;
+            // (one body that the compiler cannot take apart into two: those took 118 us for 99)
+            int which = part;
+            asm volatile("" : "+r"(which));
+            const bool values = which != 0;
             ok = warp_wait(values ? &sh.vfree[st] : &sh.kfree, (values ? ph : kt & 1) ^ 1, gave_up, stats);
             if (ok && !values) {
               ok = warp_wait(&sh.peaks[st], ph, gave_up, stats);
