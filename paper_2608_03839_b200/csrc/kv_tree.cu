@@ -447,7 +447,9 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
           uint32_t flags = *reinterpret_cast<const uint32_t*>(info.flags);
           flags |= flags >> 16;
           flags |= flags >> 8;
-          const float g = f * info.key_scale, ev = info.value_exp;
+          // (never zero, as f is not: zero times the -inf of what the row does not see is NaN; rows and
+          // keys this small have scores of zero either way)
+          const float g = fmaxf(f * info.key_scale, 1e-37f), ev = info.value_exp;
           // which slots count for this row
           uint32_t see[4];
           if (flags & 1) {
