@@ -25,11 +25,15 @@
 // 2^-11 of it).  Keys are the sum of two f16 numbers (see key_parts), each multiplied with
 // the rows: rounded once they left the logarithms off by 2e-5 of themselves over short
 // sequences, in fp32 outputs; now it is 2e-7, for 16 % more time on long ones.  Rows are multiplied by a power of two that brings their largest
-// element to [1, 2); a tile's keys and values likewise by 2^-Ek and 2^-Ev (below 1).  Ek joins the row's factor,
+// element to [1, 2); a cached tile's keys and values likewise by 2^-Ek and 2^-Ev (below 1).  Ek joins the row's factor,
 // Ev the exponent: p = exp2(s + Ev - m) with m the running maximum of s + Ev, so that
 // O = sum p (2^-Ev v) and l = sum 2^-Ev p carry no unit of their own and m alone keeps every
 // operand in range.  m is brought up to date only when a row passes it by 2^8 (the
-// accumulators are rescaled in TMEM then, once a row's maximum has settled never again).
+// accumulators are rescaled in TMEM then, once a row's maximum has settled never again).  New
+// nodes, which not every row sees, share no scale: each key has a power of two of its own, joined to
+// its scores where the mask is applied, and their values are multiplied as they lie, in the
+// cache's type, with probabilities as the sum of two numbers of that type (two copies of 64 nodes
+// are a tile of 128 slots).
 //
 // Work.  The list of tiles of kv.cuh with 128 slots a tile, one run per block.  An item that a
 // block has to itself is written out by it; the pieces of the others go to the workspace (sums,
@@ -111,7 +115,7 @@ __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::aft
 __device__ __forceinline__ void commit(uint64_t* b) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(kv_smem(b)) : "memory");
 }
-// D[tmem] (+)= A[smem] B[smem], f16 operands, fp32 accumulators, M = 128, K = 16
+// D[tmem] (+)= A[smem] B[smem], 16-bit operands of one type, fp32 accumulators, M = 128, K = 16
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
   asm volatile(
       "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
@@ -177,14 +181,16 @@ __device__ __forceinline__ uint64_t desc128(uint32_t addr, uint32_t block) {
   return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(block >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
          (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
-// fp32 accumulators, f16 operands, M = 128, N = n; transposed: B's N is contiguous
-__device__ __forceinline__ constexpr uint32_t idesc_f16(int n, bool transposed) {
-  return (1u << 4) | ((uint32_t)transposed << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+// fp32 accumulators, f16 (or bf16) operands, M = 128, N = n; transposed: B's N is contiguous
+__device__ __forceinline__ constexpr uint32_t idesc_16(int n, bool transposed, bool bf16) {
+  return (1u << 4) | ((uint32_t)bf16 << 7) | ((uint32_t)bf16 << 10) | ((uint32_t)transposed << 16) |
+         ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
 struct TileInfo {                    // what the softmax warps need to know of a tile
   uint32_t valid[4];                 // slots that exist (cached tiles)
   float key_scale, value_exp, value_scale;   // 2^Ek, Ev, 2^-Ev
   uint8_t flags[4];                  // by decoding warp; 1: new nodes, 2: some slot is not valid, 4: a value is not finite
+  alignas(16) int8_t node_exp[64];   // new nodes: the powers of two their keys were divided by
 };
 struct TreeShared {
   uint64_t kfull, kfree, vfull[2], vfree[2], sfull[2], pfull[2], pvdone[2], info_full[4], qfull;
@@ -462,14 +468,20 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
             for (int k = 0; k < 4; ++k) see[k] = info.valid[k];
           }
           const bool masked = __any_sync(0xffffffffu, flags & 3);
+          const bool nodes = __any_sync(0xffffffffu, flags & 1);
           if (masked) {                                  // -inf where the row does not look
 #pragma unroll 1
             for (int k = 0; k < 8; ++k) {
               uint32_t r[16];
               tmem_ld16(s_tm + k * 16, r);
               const uint32_t b = (k < 2 ? see[0] : k < 4 ? see[1] : k < 6 ? see[2] : see[3]) >> (k & 1 ? 16 : 0);
+              uint4 ex = make_uint4(0, 0, 0, 0);
+              if (nodes && k < 4) ex = *reinterpret_cast<const uint4*>(info.node_exp + k * 16);
 #pragma unroll
-              for (int e = 0; e < 16; ++e) r[e] = b >> e & 1 ? r[e] : 0xff800000u;
+              for (int e = 0; e < 16; ++e) {
+                const float up = pow2((int)(int8_t)((&ex.x)[e >> 2] >> (8 * (e & 3))));
+                r[e] = b >> e & 1 ? __float_as_uint(__uint_as_float(r[e]) * up) : 0xff800000u;
+              }
               tmem_st16(s_tm + k * 16, r);
             }
             tmem_wait_st();
@@ -504,18 +516,38 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
           const float shift = ev - (m == -INFINITY ? 0.f : m);
           float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
           const float2 g2 = make_float2(g, g), shift2 = make_float2(shift, shift);
+          if (nodes) {
+            // the cache's own type, as the nodes' values are: leading parts, then their rests, which
+            // meet the values' second copy
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            uint32_t w[16];
+            for (int k = 0; k < 2; ++k) {
+              uint32_t w[16], rest[16];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int i2 = k * 32 + 2 * e;
-              const float2 z = fma2(make_float2(__uint_as_float(x[i2]), __uint_as_float(x[i2 + 1])), g2, shift2);
-              const float2 pr = make_float2(exp2_approx(z.x), exp2_approx(z.y));
-              sum[e & 1] = add2(sum[e & 1], pr);
-              w[e] = pack16<false>(pr.x, pr.y);
+              for (int e = 0; e < 16; ++e) {
+                const int i2 = k * 32 + 2 * e;
+                const float2 z = fma2(make_float2(__uint_as_float(x[i2]), __uint_as_float(x[i2 + 1])), g2, shift2);
+                const float2 pr = make_float2(exp2_approx(z.x), exp2_approx(z.y));
+                sum[e & 1] = add2(sum[e & 1], pr);
+                w[e] = pack16<kBf16>(pr.x, pr.y);
+                rest[e] = pack16<kBf16>(pr.x - half_lo<kBf16>(w[e]), pr.y - half_hi<kBf16>(w[e]));
+              }
+              tmem_st16(s_tm + k * 16, w);               // over the scores
+              tmem_st16(s_tm + 32 + k * 16, rest);
             }
-            tmem_st16(s_tm + k * 16, w);                 // over the scores
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              uint32_t w[16];
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const int i2 = k * 32 + 2 * e;
+                const float2 z = fma2(make_float2(__uint_as_float(x[i2]), __uint_as_float(x[i2 + 1])), g2, shift2);
+                const float2 pr = make_float2(exp2_approx(z.x), exp2_approx(z.y));
+                sum[e & 1] = add2(sum[e & 1], pr);
+                w[e] = pack16<false>(pr.x, pr.y);
+              }
+              tmem_st16(s_tm + k * 16, w);               // over the scores
+            }
           }
           sum[0] = add2(sum[0], sum[1]);
           l = fmaf(sum[0].x + sum[0].y, info.value_scale, l);
@@ -812,8 +844,10 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
             for (int g = 0; g < G; ++g) { mc[kv][g] = mn[kv][g]; mn[kv][g] = m2[kv][g]; }
         } else {
           // ---- new nodes: 16-bit elements, slots 0..63 of the tile; the rest is zero ----
-          // raw rows copied to where their f16 will lie and turned into f16 in place, as Q's: a
-          // thread has one node's key or value
+          // raw rows copied to where they will lie; a thread has one node's key or value.  Keys are
+          // turned into f16 in place, each by a power of two of its own, values stay as they are
+          // (their products take the cache's type): a hidden node's numbers, however large, take no
+          // bits from what the others hold.
           if (!warp_wait(&sh.kfree, (kt & 1) ^ 1, gave_up, stats) || !warp_wait(&sh.vfree[st], ph ^ 1, gave_up, stats)) {
             ok = false;
             break;
@@ -830,52 +864,62 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
           cp_async_commit();
           cp_async_wait<0>();
           __syncwarp();
-          uint32_t peak = 0;
+          // (nothing to agree on, but the count of tiles goes on)
+          post(kt, 0u, 0u);
+          if (cached > 0) post_meta(kt + 1, mc);
+          if (!warp_wait(&sh.peaks[st], ph, gave_up, stats)) { ok = false; break; }
+          auto my_chunk = [&](int x) {
+            return reinterpret_cast<uint4*>(mat + (x >> 3) * (kTrTile * 128) + j * 128 + (((x & 7) ^ (j & 7)) << 4));
+          };
           bool odd = false;
+          if (dw < 2) {
+            float top = 0.f;
 #pragma unroll 2
-          for (int x = 0; x < D / 8; ++x) {
-            const uint4 w = *reinterpret_cast<const uint4*>(mat + (x >> 3) * (kTrTile * 128) + j * 128 + (((x & 7) ^ (j & 7)) << 4));
+            for (int x = 0; x < D / 8; ++x) {
+              const uint4 w = *my_chunk(x);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const uint32_t y = (&w.x)[e >> 1];
-              const float v = fabsf(e & 1 ? half_hi<kBf16>(y) : half_lo<kBf16>(y));
-              if (v < INFINITY) peak = max(peak, __float_as_uint(v));
-              else odd = dw >= 2;
+              for (int e = 0; e < 8; ++e) {
+                const uint32_t y = (&w.x)[e >> 1];
+                const float v = fabsf(e & 1 ? half_hi<kBf16>(y) : half_lo<kBf16>(y));
+                if (v < INFINITY) top = fmaxf(top, v);
+              }
+            }
+            const int ek = peak_exp(__float_as_uint(top));
+            const float down = pow2(-ek);
+            info.node_exp[j] = (int8_t)ek;
+#pragma unroll 2
+            for (int x = 0; x < D / 8; ++x) {
+              uint4* at_chunk = my_chunk(x);
+              uint4 w = *at_chunk;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) (&w.x)[e] = pack16<false>(half_lo<kBf16>((&w.x)[e]) * down, half_hi<kBf16>((&w.x)[e]) * down);
+              *at_chunk = w;
+              at_chunk[64 * 128 / 16] = make_uint4(0, 0, 0, 0);   // slots 64..127 of the tile
+              // (f16 holds the keys whole)
+              at_chunk[T::kMat / 16] = at_chunk[T::kMat / 16 + 64 * 128 / 16] = make_uint4(0, 0, 0, 0);
+            }
+          } else {
+#pragma unroll 2
+            for (int x = 0; x < D / 8; ++x) {            // values that are not finite: see `accumulators`
+              uint4 w = *my_chunk(x);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                uint32_t& v = (&w.x)[e];
+                constexpr uint32_t kInf = kBf16 ? 0x7f80u : 0x7c00u;
+                if ((v & kInf) == kInf) { odd = true; v &= 0xffff0000u; }
+                if ((v >> 16 & kInf) == kInf) { odd = true; v &= 0x0000ffffu; }
+              }
+              my_chunk(x)[0] = my_chunk(x)[64 * 128 / 16] = w;      // (once for each part of the probabilities)
             }
           }
           odd = __any_sync(0xffffffffu, odd);
-          post(kt, dw < 2 ? peak : 0u, dw < 2 ? 0u : peak);
-          if (cached > 0) post_meta(kt + 1, mc);
-          if (!warp_wait(&sh.peaks[st], ph, gave_up, stats)) { ok = false; break; }
-          int ek, ev;
-          peaks_of(kt, ek, ev);
           if (lane == 0) {
             info.valid[dw] = dw > 1 ? 0u : (uint32_t)(((bc.nodes >= 64 ? 0ull : 1ull << bc.nodes) - 1ull) >> (32 * dw));
             info.flags[dw] = 1 | (odd ? 4 : 0);
             if (dw == 0) {
-              info.key_scale = pow2(ek);
-              info.value_exp = (float)ev;
-              info.value_scale = pow2(-ev);
+              info.key_scale = info.value_scale = 1.f;
+              info.value_exp = 0.f;
             }
-          }
-          const float down = pow2(-(dw < 2 ? ek : ev));
-#pragma unroll 2
-          for (int x = 0; x < D / 8; ++x) {
-            uint4* at_chunk = reinterpret_cast<uint4*>(mat + (x >> 3) * (kTrTile * 128) + j * 128 + (((x & 7) ^ (j & 7)) << 4));
-            uint4 w = *at_chunk;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float v0 = half_lo<kBf16>((&w.x)[e]) * down, v1 = half_hi<kBf16>((&w.x)[e]) * down;
-              if (dw >= 2) {                             // values that are not finite: see `accumulators`
-                v0 = fabsf(v0) < INFINITY ? v0 : 0.f;
-                v1 = fabsf(v1) < INFINITY ? v1 : 0.f;
-              }
-              (&w.x)[e] = pack16<false>(v0, v1);
-            }
-            *at_chunk = w;
-            at_chunk[64 * 128 / 16] = make_uint4(0, 0, 0, 0);   // slots 64..127 of the tile
-            if (dw < 2)                                  // (f16 holds the keys whole)
-              at_chunk[T::kMat / 16] = at_chunk[T::kMat / 16 + 64 * 128 / 16] = make_uint4(0, 0, 0, 0);
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
@@ -895,7 +939,8 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTrIssueRegs));
     uint32_t kt = 0, np = 0, pu[2] = {0, 0};
     bool ok = warp == kTrIssuer;
-    constexpr uint32_t s_idesc = idesc_f16(kTrTile, false), o_idesc = idesc_f16(D, true);
+    constexpr uint32_t s_idesc = idesc_16(kTrTile, false, false), o_idesc = idesc_16(D, true, false);
+    constexpr uint32_t n_idesc = idesc_16(D, true, kBf16);           // new nodes' values
     // Descriptors are formed here, the same in every lane, and only a constant is added where
     // one lane issues: what that lane computed for itself would have to be moved to uniform
     // registers for every product.
@@ -939,6 +984,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
           if (!p.two || wg == 0) ok = warp_wait(&sh.vfull[st], (t >> 1) & 1, gave_up, stats);
           ok = ok && warp_wait(&sh.pfull[wg], pu[wg] & 1, gave_up, stats);
           if (!ok) break;
+          const uint32_t pv_idesc = __shfl_sync(0xffffffffu, p.nodes && t == kt ? n_idesc : o_idesc, 0);
           ++pu[wg];
           fence_after();
           const uint64_t vd = v_desc + (st ? kStage : 0);
@@ -946,7 +992,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
           if (issuer) {
 #pragma unroll
             for (int k = 0; k < kTrTile / 16; ++k)
-              mma_ts(to, from + k * 8, vd + (uint64_t)(k * (2048 >> 4)), o_idesc, k > 0 ? 1u : add);
+              mma_ts(to, from + k * 8, vd + (uint64_t)(k * (2048 >> 4)), pv_idesc, k > 0 ? 1u : add);
             commit(&sh.pvdone[wg]);
             if (!p.two || wg == 1) commit(&sh.vfree[st]);
           }

@@ -67,3 +67,21 @@ def test_scale_of_zero_and_below(m, hq, dtype, scale):
     q, kn = q * 0, kn * 0
     out, lse = c.cache.attend(q, kn, vn, mask=mask, scale=scale)
     check_attend(c, q, kn, vn, mask, None, out, lse, abs(scale))
+
+
+# ---------------------------------------------------------- what a row does not see ----
+
+@pytest.mark.parametrize("dtype,big", [("bf16", 3e38), ("f16", 6e4)])
+@pytest.mark.parametrize("m,hq", [(3, 4), (40, 4), (40, 8)])
+@pytest.mark.parametrize("held", [0, 70])
+def test_large_hidden_nodes_change_nothing(m, hq, held, dtype, big):
+    """Rows are bit for bit the same whatever finite keys and values the nodes they do not see hold."""
+    c = Made([held, held // 2], 1, 128, 64, dtype)
+    q, kn, vn = (c.rand(2, m, h, 128).to(KIND[dtype]) for h in (hq, 1, 1))
+    mask = torch.ones(2, m, dtype=torch.int64, device="cuda") << torch.arange(m, device="cuda")
+    mask[:, 2:] |= 2                                             # most rows also see node 1
+    want, wl = c.cache.attend(q, kn, vn, mask=mask)
+    check_attend(c, q, kn, vn, mask, None, want, wl, 128 ** -0.5)
+    kn[:, 0], vn[:, 0] = big, -big                               # row 0 alone sees node 0
+    got, gl = c.cache.attend(q, kn, vn, mask=mask)
+    assert torch.equal(gl[:, 1:], wl[:, 1:]) and torch.equal(got[:, 1:], want[:, 1:])
