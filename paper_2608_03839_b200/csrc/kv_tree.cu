@@ -26,13 +26,13 @@
 // the rows: rounded once they left the logarithms off by 2e-5 of themselves over short
 // sequences, in fp32 outputs; now it is 2e-7, for 16 % more time on long ones.  Rows are multiplied by a power of two that brings their largest
 // element to [1, 2); a cached tile's keys and values likewise by 2^-Ek and 2^-Ev (below 1).  Ek joins the row's factor,
-// Ev the exponent: p = exp2(s + Ev - m) with m the running maximum of s + Ev, so that
+// Ev the exponent: p = exp2(s + Ev - m + 7) with m the running maximum of s + Ev, so that
 // O = sum p (2^-Ev v) and l = sum 2^-Ev p carry no unit of their own and m alone keeps every
-// operand in range.  m is brought up to date only when a row passes it by 2^8 (the
+// operand in range.  (Without the 7, which f16 has room for, 32,768 slots 17.5 below one other
+// in exp's units came out as nothing.)  m is brought up to date only when a row passes it by 2^8 (the
 // accumulators are rescaled in TMEM then, once a row's maximum has settled never again).  New
 // nodes, which not every row sees, share no scale: each key has a power of two of its own, joined to
-// its scores where the mask is applied, and their values are multiplied as they lie, in the
-// cache's type, with probabilities as the sum of two numbers of that type (two copies of 64 nodes
+// its scores where the mask is applied, and their values are multiplied in the cache's type with probabilities as the sum of two numbers of that type (two copies of 64 nodes
 // are a tile of 128 slots).
 //
 // Work.  The list of tiles of kv.cuh with 128 slots a tile, one run per block.  An item that a
@@ -63,6 +63,9 @@ constexpr int kTrSoftRegs = 192, kTrDecRegs = 104, kTrIssueRegs = 24;
 static_assert(2 * kTrSoftRegs + kTrDecRegs + kTrIssueRegs == 4 * 128, "more registers than the block was launched with");
 using TreeList = TileListOf<kTrTile, kTrFront, 0>;
 constexpr float kTrLn2 = 0.6931471805599453f;
+// Probabilities are f16 operands in units in which a row's largest lies between 2^7 and 2^15: f16
+// ends above that, and what is 2^-21 of the largest still has all its bits, 2^-31 one.
+constexpr int kTrRoom = 7, kTrSlack = 8;
 
 // ------------------------------------------------------------------ PTX wrappers ---
 __device__ __forceinline__ void bar_init(uint64_t* b, uint32_t n) {
@@ -496,8 +499,9 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
           for (int e = 0; e < 64; ++e) y[e & 3] = max3(y[e & 3], __uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1]));
           float mx = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
           mx = fmaf(mx, g, ev);
-          if (__any_sync(0xffffffffu, mx > m + 8.f)) {
-            const float mn = fmaxf(m, mx), down = mn == -INFINITY ? 1.f : exp2_approx(m - mn);
+          if (__any_sync(0xffffffffu, mx > m + kTrSlack)) {
+            // (each row for itself: what its warp's other rows look at changes nothing)
+            const float mn = mx > m + kTrSlack ? mx : m, down = mn == -INFINITY ? 1.f : exp2_approx(m - mn);
             m = mn;
             l *= down;
             if (i > 0) {
@@ -513,7 +517,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
               }
             }
           }
-          const float shift = ev - (m == -INFINITY ? 0.f : m);
+          const float shift = ev + kTrRoom - (m == -INFINITY ? 0.f : m);
           float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
           const float2 g2 = make_float2(g, g), shift2 = make_float2(shift, shift);
           if (nodes) {
@@ -563,6 +567,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
           fence_after();
         }
         if (mine == 0) { m = -INFINITY; l = 0.f; }
+        m -= kTrRoom;                                    // what l and the accumulators are relative to
       }
       // A thread's 32 accumulators from column k on.  Infinities and NaN of new nodes' values
       // stayed out of the products (0 times a hidden node's would have reached every row): they
@@ -872,6 +877,8 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
             return reinterpret_cast<uint4*>(mat + (x >> 3) * (kTrTile * 128) + j * 128 + (((x & 7) ^ (j & 7)) << 4));
           };
           bool odd = false;
+          // (bf16 values leave fp32 the room that the probabilities take; f16 ends far below)
+          constexpr int kNodeExp = kBf16 ? kTrRoom : 0;
           if (dw < 2) {
             float top = 0.f;
 #pragma unroll 2
@@ -908,6 +915,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
                 constexpr uint32_t kInf = kBf16 ? 0x7f80u : 0x7c00u;
                 if ((v & kInf) == kInf) { odd = true; v &= 0xffff0000u; }
                 if ((v >> 16 & kInf) == kInf) { odd = true; v &= 0x0000ffffu; }
+                if (kNodeExp) v = pack16<kBf16>(half_lo<kBf16>(v) * pow2(-kNodeExp), half_hi<kBf16>(v) * pow2(-kNodeExp));
               }
               my_chunk(x)[0] = my_chunk(x)[64 * 128 / 16] = w;      // (once for each part of the probabilities)
             }
@@ -917,8 +925,9 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
             info.valid[dw] = dw > 1 ? 0u : (uint32_t)(((bc.nodes >= 64 ? 0ull : 1ull << bc.nodes) - 1ull) >> (32 * dw));
             info.flags[dw] = 1 | (odd ? 4 : 0);
             if (dw == 0) {
-              info.key_scale = info.value_scale = 1.f;
-              info.value_exp = 0.f;
+              info.key_scale = 1.f;
+              info.value_exp = kNodeExp;
+              info.value_scale = pow2(-kNodeExp);
             }
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");

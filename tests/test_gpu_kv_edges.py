@@ -85,3 +85,44 @@ def test_large_hidden_nodes_change_nothing(m, hq, held, dtype, big):
     kn[:, 0], vn[:, 0] = big, -big                               # row 0 alone sees node 0
     got, gl = c.cache.attend(q, kn, vn, mask=mask)
     assert torch.equal(gl[:, 1:], wl[:, 1:]) and torch.equal(got[:, 1:], want[:, 1:])
+
+
+# ------------------------------------------- probabilities far below the largest ----
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("m,hq", [(10, 8), (40, 8)])
+@pytest.mark.parametrize("nats", [12.0, 17.5])
+def test_one_slot_far_above_the_others(nats, m, hq, dtype):
+    """An attention sink: one slot with a value of zero, `nats` above 32,768 others whose values
+    are alike, so that what each adds is small but all of it counts.  (As many sequences, over the
+    same pages, as leave every one whole to a block.)
+
+    A probability is an f16 operand: off by 2^-11 of itself, or, where it is small, by 2^-25 of
+    an operand of one.  Operands go up to 2^15, so that the largest probability is one of at least
+    2^7: 2^-32 absolute for each slot.  Values are rounded by 2^-11 of themselves at most."""
+    n, d, n_seq = 32768, 128, 320
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    u = torch.randn(d, generator=gen, device="cuda")
+    u /= u.norm()
+    like = torch.linspace(0.5, 1.0, d, device="cuda")[torch.randperm(d, generator=gen, device="cuda")]
+    keys = torch.randn(1, n + 1, 1, d, generator=gen, device="cuda") * 0.05
+    values = like + 0.01 * torch.randn(1, n + 1, 1, d, generator=gen, device="cuda")
+    keys[0, 777, 0], values[0, 777, 0] = u * 16, 0.0
+    c = custom(keys, values, d, 64, dtype)
+    many = B.KVCache.over(c.pages, c.weight, c.pos, c.table.repeat(n_seq, 1), c.seq_len.repeat(n_seq),
+                          c.n_pos.repeat(n_seq), dtype=KIND[dtype], workspace=c.cache.workspace)
+    q = (u * nats / 16 * d ** 0.5 + 0.01 * torch.randn(n_seq, m, hq, d, generator=gen, device="cuda")).to(KIND[dtype])
+    out, lse = many.attend(q)
+    k, v, _ = c.dense(0, 0)
+    top, step = np.abs(v).max(), np.ptp(k, -1).max() / 15
+    for s in (0, 131, 319):
+        row = f64(q[s], dtype).reshape(-1, d)
+        x = (row @ k.T) * d ** -0.5
+        p = np.exp(x - x.max(-1, keepdims=True))
+        p /= p.sum(-1, keepdims=True)
+        want, got = p @ v, f64(out[s], dtype).reshape(-1, d)
+        mag = d ** -0.5 * (np.abs(row) @ (np.abs(k).T + 2 * np.abs(k).max())).max()
+        # (the last term of e: keys as the sum of two f16 numbers, off by 2^-13 of the scale)
+        e = 2.0 ** -24 * (2 * d + 12) * mag + 2.0 ** -21 + 2.0 ** -13 * d ** -0.5 * np.abs(row).sum(-1).max() * step
+        tol = UNIT[dtype] * np.abs(want) + (p @ np.abs(v)) * (2 * 2.0 ** -11 + 2 * e) + n * 2.0 ** -32 * 2 * top + 2.0 ** -25
+        assert np.all(np.abs(got - want) <= tol), (np.abs(got - want).max(), tol.min(), np.abs(want).max())
