@@ -8,7 +8,8 @@
 // products run on the codes alone, as f16 numbers that are exact, and one fp32 multiply-add
 // per (slot, row, group) brings in scale and offset; the scores carry no rounding but fp32's.
 // For the values the scale joins the probability before it becomes an f16 operand (one
-// rounding, at most 2^-11 of each term).  All codes are positive, so over a long sequence their
+// rounding, at most 2^-11 of each term, in units that use f16's whole range: slots 17.5 nats below
+// another one still bring in their values, not their groups' middles alone).  All codes are positive, so over a long sequence their
 // sums would outgrow the result by far, and with them what the tensor cores cut off: half of the
 // slots therefore go in with 15 - code and a negative operand, and the groups' middles
 // (lo + 7.5 scale, in fp32) in place of the offsets make up the difference, with 7.5 times the
@@ -48,6 +49,9 @@ namespace oilbird {
 // 21 rows of 64 channels over 777 slots take 17.2 us there and 18.6 us as two blocks of 16 rows
 // here, which would read the cache twice; with 16 rows or fewer one reading is enough.
 constexpr int kFewRows = 16;
+// Probability times value scale is an f16 operand, in units in which the largest scale lies below
+// 2^7: with probabilities up to 2^8 f16 just holds it, and small probabilities keep their bits.
+constexpr int kRoom = 7;
 template <int D, int NT>
 struct Attend {
   static constexpr int kWarps = NT == 1 ? 6 : 4, kThreads = 32 * kWarps, kCtas = 2;
@@ -486,7 +490,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
             vtop = __reduce_max_sync(0xffffffffu, vtop);
           }
         }
-        const int etile = kBf16 ? min(max((int)(vtop >> 7) - 126, -120), 100) : (int)(vtop >> 10) - 14;
+        const int etile = kBf16 ? max((int)(vtop >> 7) - 126 - kRoom, -120) : (int)(vtop >> 10) - 14 - kRoom;
         float mx[NT][2];
         bool grow = etile > eref || fresh;
 #pragma unroll
@@ -513,7 +517,8 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
           for (int r = 0; r < NT; ++r)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float mn = fmaxf(m[r][e], mx[r][e]);
+              // (each row for itself: what its warp's other rows look at changes nothing)
+              const float mn = mx[r][e] > m[r][e] + 8.f ? mx[r][e] : m[r][e];
               const float down = mn == -INFINITY ? 1.f : exp2_approx(m[r][e] - mn);
               m[r][e] = mn;
               l[r][e] *= down;
@@ -613,7 +618,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
     list.owners(u0 + item_u0, n_tiles, n_cta, b0, b1);
     const bool whole = b0 == b1;
     float* my_part = parts + (size_t)(2 * blockIdx.x + (blockIdx.x == b0 ? 1 : 0)) * kPartFloats;
-    const float unit = pow2(min(eref + 24, 127));
+    const float unit = pow2(eref);
 
 #pragma unroll
     for (int r = 0; r < NT; ++r) {
@@ -634,9 +639,9 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
           float v[8];
 #pragma unroll
           for (int n = 0; n < 4; ++n) {
-            const float u = n & 1 ? unit * 0.0625f : unit;
-            v[2 * n] = fmaf(o[r][i * 4 + n][e], u, olo[r][i][e]);
-            v[2 * n + 1] = fmaf(o[r][i * 4 + n][e + 2], u, olo[r][i][e]);
+            const float u = n & 1 ? 0x1p20f : 0x1p24f;   // (with the unit it could pass fp32's range)
+            v[2 * n] = fmaf(o[r][i * 4 + n][e] * u, unit, olo[r][i][e]);
+            v[2 * n + 1] = fmaf(o[r][i * 4 + n][e + 2] * u, unit, olo[r][i][e]);
           }
           *reinterpret_cast<float4*>(dst + i * kKvGroup) = make_float4(v[0], v[1], v[2], v[3]);
           *reinterpret_cast<float4*>(dst + i * kKvGroup + 4) = make_float4(v[4], v[5], v[6], v[7]);

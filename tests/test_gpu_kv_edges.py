@@ -90,7 +90,7 @@ def test_large_hidden_nodes_change_nothing(m, hq, held, dtype, big):
 # ------------------------------------------- probabilities far below the largest ----
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("m,hq", [(10, 8), (40, 8)])
+@pytest.mark.parametrize("m,hq", [(1, 8), (2, 8), (10, 8), (40, 8)])
 @pytest.mark.parametrize("nats", [12.0, 17.5])
 def test_one_slot_far_above_the_others(nats, m, hq, dtype):
     """An attention sink: one slot with a value of zero, `nats` above 32,768 others whose values
