@@ -247,9 +247,10 @@ template <bool kBf16> __device__ __forceinline__ uint32_t meta_peak(uint32_t met
   const float x = fmaxf(fabsf(lo), fabsf(fmaf(15.f, sc, lo)));
   return x < INFINITY ? __float_as_uint(x) : 0u;
 }
-// exponent E with peak < 2^E, as far as sums over long sequences times 2^-E stay in range
+// exponent E with peak < 2^E, as far as 2^E and 2^-E are numbers (the largest peaks come to 4, which
+// f16 holds) and sums over long sequences times 2^-E stay in range
 __device__ __forceinline__ int peak_exp(uint32_t peak) {
-  return min(max((int)(peak >> 23) - 126, -90), 100);
+  return min(max((int)(peak >> 23) - 126, -90), 126);
 }
 __device__ __forceinline__ __half2 as_half2(uint32_t w) { return *reinterpret_cast<__half2*>(&w); }
 __device__ __forceinline__ uint32_t as_word(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
@@ -457,8 +458,9 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
           flags |= flags >> 16;
           flags |= flags >> 8;
           // (never zero, as f is not: zero times the -inf of what the row does not see is NaN; rows and
-          // keys this small have scores of zero either way)
-          const float g = fmaxf(f * info.key_scale, 1e-37f), ev = info.value_exp;
+          // keys this small have scores of zero either way.  Nor infinite: times a score of zero that
+          // is NaN too.)
+          const float g = fminf(fmaxf(f * info.key_scale, 1e-37f), 3e38f), ev = info.value_exp;
           // which slots count for this row
           uint32_t see[4];
           if (flags & 1) {

@@ -126,3 +126,24 @@ def test_one_slot_far_above_the_others(nats, m, hq, dtype):
         e = 2.0 ** -24 * (2 * d + 12) * mag + 2.0 ** -21 + 2.0 ** -13 * d ** -0.5 * np.abs(row).sum(-1).max() * step
         tol = UNIT[dtype] * np.abs(want) + (p @ np.abs(v)) * (2 * 2.0 ** -11 + 2 * e) + n * 2.0 ** -32 * 2 * top + 2.0 ** -25
         assert np.all(np.abs(got - want) <= tol), (np.abs(got - want).max(), tol.min(), np.abs(want).max())
+
+
+# ------------------------------------------------------------------- extreme values ----
+
+@pytest.mark.parametrize("m,hq", [(1, 4), (4, 4), (30, 4)])
+def test_values_near_the_largest_number(m, hq):
+    c = Made([200, 17], 1, 128, 64, "bf16", v_gain=2e35)
+    q = (c.rand(2, m, hq, 128) * 0.5).bfloat16()
+    out, lse = c.cache.attend(q)
+    check_attend(c, q, None, None, None, None, out, lse, 128 ** -0.5)
+
+
+@pytest.mark.parametrize("m,hq", [(1, 4), (30, 4)])
+def test_keys_near_the_largest_number(m, hq):
+    """Keys of 1e35 under queries of 1e-35: ordinary scores."""
+    c = Made([0, 0], 1, 64, 64, max_pages=3, spare=6)
+    c.table.copy_(torch.arange(6).int().view(2, 3))
+    c.cache.append((c.rand(2, 150, 1, 64) * 2e35).bfloat16(), c.rand(2, 150, 1, 64).bfloat16())
+    q = (c.rand(2, m, hq, 64) * 2e-35).bfloat16()
+    out, lse = c.cache.attend(q)
+    check_attend(c, q, None, None, None, None, out, lse, 64 ** -0.5)
