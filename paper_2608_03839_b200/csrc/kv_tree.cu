@@ -1015,18 +1015,19 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
       at += count;
       if (at < u1) list.advance(bc, count);
     }
-    // what was issued is done before the memory goes away: the softmax warps waited for the last
-    // products, unless somebody gave up
-    if (warp == kTrIssuer && *gave_up) {
-      const unsigned long long t0 = now_ns();
-      while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
-    }
   }
   fence_before();
   __syncthreads();
   fence_after();
-  if (warp == kTrIssuer)
+  if (warp == kTrIssuer) {
+    // What was issued is done before the memory goes away: the softmax warps waited for the last
+    // products, unless somebody gave up.  (Read behind the barrier, when nobody can any more.)
+    if (*gave_up) {
+      const unsigned long long t0 = now_ns();
+      while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
+    }
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  }
 }
 
 // The pieces of every item joined, in their order.  A block: 128 rows of an item, 16 channels;

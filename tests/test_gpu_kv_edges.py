@@ -147,3 +147,37 @@ def test_keys_near_the_largest_number(m, hq):
     q = (c.rand(2, m, hq, 64) * 2e-35).bfloat16()
     out, lse = c.cache.attend(q)
     check_attend(c, q, None, None, None, None, out, lse, 64 ** -0.5)
+
+
+# ------------------------------------------------------------- waits that run out ----
+
+def test_a_stall_is_reported():
+    """The flag that a bounded wait raises when it gives up, set here by hand."""
+    c = Made([40, 3], 1, 64, 16)
+    stalled = c.cache.workspace[16:20].view(torch.int32)
+    assert c.cache.dropped() == 0
+    stalled.fill_(1)
+    with pytest.raises(B.OilbirdError) as e:
+        c.cache.dropped()
+    assert e.value.code == B.ESTALL
+    stalled.zero_()
+    assert c.cache.dropped() == 0
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_waits_of_a_nanosecond_end_and_leave_everything_usable(d):
+    """With next to no patience the kernel may give up anywhere: it says so or its result is right,
+    and the next call with the usual limit is right again."""
+    c = Made([3000, 300, 1], 2, d, 32)
+    q, kn, vn = (c.rand(3, 40, h, d).bfloat16() for h in (8, 2, 2))
+    want, wl = c.cache.attend(q, kn, vn)
+    stalled, limit = c.cache.workspace[16:20].view(torch.int32), c.cache.workspace[24:32].view(torch.int64)
+    for _ in range(5):
+        limit.fill_(1)
+        out, lse = c.cache.attend(q, kn, vn)
+        if int(stalled) == 0:
+            assert torch.equal(out, want) and torch.equal(lse, wl)
+        limit.zero_()
+        stalled.zero_()
+        out, lse = c.cache.attend(q, kn, vn)
+        assert torch.equal(out, want) and torch.equal(lse, wl) and c.cache.dropped() == 0
