@@ -679,8 +679,9 @@ size_t  oilbird_kv_workspace_bytes(int32_t head_dim);
  * Append: of the m rows per sequence in k and v, the rows select[s, 0..n) (dev [n_seq, rows];
  * NULL: rows 0..n) are stored at slots seq_len[s].. with positions n_pos[s].., n = n_new[s] (dev;
  * NULL: `rows`).  weight: dev [n_seq, n_kv_heads, m] the rows' first weights, NULL: 0.  A row
- * that finds no page, or a select entry outside 0..m-1, is not stored (its slot counts) and is
- * counted in status().  rows at most 2^24, as is read()'s n.
+ * that finds no page is not stored (its slot counts) and is counted in status(); so is a select
+ * entry outside 0..m-1, whose slot reads as NaN and has weight 0.  rows at most 2^24, as is
+ * read()'s n.
  */
 int oilbird_kv_append(const oilbird_kv_cache* cache, const oilbird_kv_rows* k,
                       const oilbird_kv_rows* v, int32_t m, int32_t rows, const int32_t* n_new,

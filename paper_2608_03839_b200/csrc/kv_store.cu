@@ -129,25 +129,27 @@ kv_append_kernel(const KvView c, const KvAppendArgs a) {
   struct Row {
     uint4 v[kStTurns];
     float w;
-    int j, head0, p;                                     // p: the page; -1: not stored
+    int j, head0, p;                                     // p: the page; -1: none; -2 - page: no such row
   };
   auto ask = [&](Row& r, int task) {
     r.j = task / head_groups;
     r.head0 = (task - r.j * head_groups) * kHeads;
     r.p = -1;
     if (r.j < n) {
-      const int src = a.select ? a.select[(size_t)s * a.rows + r.j] : r.j;
-      if (src >= 0 && src < a.m) {
-        r.p = page_of(c, s, (long long)before + r.j);
-#pragma unroll
-        for (int t = 0; t < kStTurns; ++t) {
-          const int head = r.head0 + t * kHeadsATurn + unit / kUnits;
-          r.v[t] = make_uint4(0, 0, 0, 0);
-          if (head < c.n_kv) r.v[t] = *reinterpret_cast<const uint4*>(rows.at(s, src, head) + grp * kKvGroup + lane8 * 8);
-        }
-        r.w = a.weight && lane < kHeads && r.head0 + lane < c.n_kv
-                  ? a.weight[((size_t)s * c.n_kv + r.head0 + lane) * a.m + src] : 0.f;
+      int src = a.select ? a.select[(size_t)s * a.rows + r.j] : r.j;
+      r.p = page_of(c, s, (long long)before + r.j);
+      if (src < 0 || src >= a.m) {
+        if (r.p >= 0) r.p = -2 - r.p;
+        src = 0;
       }
+#pragma unroll
+      for (int t = 0; t < kStTurns; ++t) {
+        const int head = r.head0 + t * kHeadsATurn + unit / kUnits;
+        r.v[t] = make_uint4(0, 0, 0, 0);
+        if (head < c.n_kv) r.v[t] = *reinterpret_cast<const uint4*>(rows.at(s, src, head) + grp * kKvGroup + lane8 * 8);
+      }
+      r.w = a.weight && lane < kHeads && r.head0 + lane < c.n_kv
+                ? a.weight[((size_t)s * c.n_kv + r.head0 + lane) * a.m + src] : 0.f;
     }
   };
   int task = blockIdx.x * (kStThreads / 32) + (threadIdx.x >> 5);
@@ -157,7 +159,14 @@ kv_append_kernel(const KvView c, const KvAppendArgs a) {
     ask(next, task += stride);
     if (cur.p < 0) {
       if (cur.head0 == 0 && lane == 0) atomicAdd(&work->dropped, 1ull);
-    } else {
+      if (cur.p < -1) {                                  // its slot counts: NaN, not what lay there before
+        cur.p = -2 - cur.p;
+#pragma unroll
+        for (int t = 0; t < kStTurns; ++t) cur.v[t] = make_uint4(~0u, ~0u, ~0u, ~0u);
+        cur.w = 0.f;
+      }
+    }
+    if (cur.p >= 0) {
       const int in = (before + cur.j) & (page - 1);
 #pragma unroll
       for (int t = 0; t < kStTurns; ++t) {

@@ -149,6 +149,33 @@ def test_keys_near_the_largest_number(m, hq):
     check_attend(c, q, None, None, None, None, out, lse, 64 ** -0.5)
 
 
+# ---------------------------------------------------------- slots without content ----
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_append_of_rows_that_do_not_exist_leaves_nothing_stale(d, dtype):
+    """A select entry outside the rows: the slot counts, so it has content of its own: NaN, weight 0
+    and its position; what lay there before does not come back."""
+    c = custom(torch.randn(2, 20, 3, d, device="cuda"), torch.randn(2, 20, 3, d, device="cuda"), d, 16, dtype)
+    c.weight.fill_(9.0)
+    c.seq_len.fill_(10)
+    c.n_pos.copy_(torch.tensor([50, 10]))
+    k, v = (c.rand(2, 4, 3, d).to(KIND[dtype]) for _ in range(2))
+    sel = torch.tensor([[-1, 2, 4], [3, 99, -5]], dtype=torch.int32, device="cuda")
+    w = torch.full((2, 3, 4), 5.0, device="cuda")
+    c.cache.append(k, v, select=sel, weight=w)
+    assert c.seq_len.tolist() == [13, 13] and c.n_pos.tolist() == [53, 13] and c.cache.dropped() == 4
+    rk, rv = c.cache.read(3, start=torch.full((2,), 10, dtype=torch.int32, device="cuda"))
+    bad = torch.tensor([[True, False, True], [False, True, True]], device="cuda")
+    for r in (rk, rv):
+        assert torch.isnan(r[bad]).all() and torch.isfinite(r[~bad]).all()
+    for s in range(2):
+        for j in range(3):
+            page, cell = int(c.table[s, (10 + j) // 16]), (10 + j) % 16
+            assert c.pos[page, :, cell].tolist() == [[50, 10][s] + j] * 3
+            assert c.weight[page, :, cell].tolist() == [0.0 if bad[s, j] else 5.0] * 3
+
+
 # ------------------------------------------------------------- waits that run out ----
 
 def test_a_stall_is_reported():
