@@ -722,6 +722,7 @@ int oilbird_kv_weigh(const oilbird_kv_cache* cache, int32_t n_q_heads, int32_t m
  * ascending; a NaN weight counts as the lowest) up to `budget`.  (Should more than `budget`
  * slots have such positions, as append() never makes them, the lowest stay; ties of all these
  * go to the lowest slot.)  Slots are not put in order: the i-th slot below budget that was not kept takes the i-th kept slot from budget on.
+ * Slots below budget whose page is none keep their places, so that much fewer of the others stay.
  * sink + recent <= budget.
  */
 int oilbird_kv_evict(const oilbird_kv_cache* cache, int32_t budget, int32_t sink, int32_t recent,

@@ -4,7 +4,8 @@
 // `sink` or among the newest `recent`, then the others by (weight descending, position
 // ascending).  Attention does not depend on the order of the slots, so nothing is shifted:
 // the i-th slot below the budget that was not kept takes the i-th kept slot at or above it.
-// What moves is the smaller side, in steady state one row per appended token.
+// What moves is the smaller side, in steady state one row per appended token.  Slots whose page is
+// none hold their places below the budget, for a slot moved there would be lost.
 //
 // A cluster of one to eight blocks handles one (sequence, head), a run of its slots each.  The
 // weight of the last slot kept is found by radix selection on the weights' order-preserving
@@ -155,8 +156,11 @@ kv_evict_kernel(const KvView c, const KvEvictArgs a, int groups) {
       const bool have = (uint32_t)p < (uint32_t)c.n_pages;
       const size_t at = ((size_t)(have ? p : 0) * c.n_kv + head) * page + (slot & (page - 1));
       const float w = c.weight[at];
-      const int32_t x = c.pos[at];                       // (no page: below everything)
-      return have ? make_uint2(x < a.sink || x >= newest ? kEvStays : weight_order(w), (uint32_t)x) : make_uint2(0u, 2147483647u);
+      const int32_t x = c.pos[at];
+      // No page: nothing can be moved there, so below the budget the slot holds its place, and above
+      // it is behind everything.
+      if (!have) return slot < budget ? make_uint2(kEvStays, 0x80000000u) : make_uint2(0u, 0x7fffffffu);
+      return make_uint2(x < a.sink || x >= newest ? kEvStays : weight_order(w), (uint32_t)x);
     };
     if (a.held) {
 #pragma unroll 8

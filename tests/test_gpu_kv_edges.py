@@ -176,6 +176,45 @@ def test_append_of_rows_that_do_not_exist_leaves_nothing_stale(d, dtype):
             assert c.weight[page, :, cell].tolist() == [0.0 if bad[s, j] else 5.0] * 3
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,budget,none", [([100, 90], 64, [1]), ([70, 66], 64, [0, 3]), ([5000, 300], 128, [0, 2, 7]),
+                                              ([100, 100], 64, [1, 5]), ([64 + 16, 200], 64, [1, 2, 3])])
+def test_evict_moves_nothing_to_pages_that_name_nothing(lens, budget, none, d):
+    """Slots without a page hold their places, for nothing is stored there; the slots that are kept
+    are the best of the others, and all of them are still there afterwards."""
+    page, hkv = 16, 2
+    c = Made(lens, hkv, d, page, spare=2)
+    c.weight.copy_(torch.rand(c.weight.shape, generator=c.g, device="cuda"))
+    c.table[:, none] = -1
+    sink, recent = 2, 8
+    table = c.table.cpu().numpy()
+    before = [t.cpu().numpy().copy() for t in (c.pages, c.weight, c.pos)]
+    c.cache.evict(budget, sink=sink, recent=recent)
+    after = [t.cpu().numpy() for t in (c.pages, c.weight, c.pos)]
+    assert c.seq_len.tolist() == [min(n, budget) for n in lens]
+    for s, n in enumerate(lens):
+        here = [j for j in range(n) if table[s, j // page] >= 0]
+        room = [j for j in range(min(n, budget)) if table[s, j // page] >= 0]
+        for h in range(hkv):
+            cell = lambda arr, j: arr[table[s, j // page], h, j % page]
+            rank = sorted(here, key=lambda j: (not (cell(before[2], j) < sink or cell(before[2], j) >= n - recent),
+                                               -cell(before[1], j) if sink <= cell(before[2], j) < n - recent else 0.0,
+                                               cell(before[2], j)))
+            keep = set(rank[:len(room)]) if n > budget else set(here)
+            movers = [j for j in sorted(keep) if j >= budget]
+            old, new = ({name: {} for name in ("k_code", "v_code", "k_low", "v_scale")} for _ in range(2))
+            for j in here:
+                for store, arr in ((old, before[0]), (new, after[0])):
+                    blk = O.decode_block(arr[table[s, j // page], h], page, d, "bf16")
+                    for name in store:
+                        store[name][j] = blk[name][j % page]
+            for j in room:
+                src = j if j in keep else movers.pop(0)
+                assert cell(after[1], j) == cell(before[1], src) and cell(after[2], j) == cell(before[2], src), (s, h, j)
+                assert all(np.array_equal(new[name][j], old[name][src]) for name in old), (s, h, j)
+            assert not movers
+
+
 # ------------------------------------------------------------- waits that run out ----
 
 def test_a_stall_is_reported():
