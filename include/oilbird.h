@@ -687,7 +687,8 @@ int oilbird_kv_append(const oilbird_kv_cache* cache, const oilbird_kv_rows* k,
                       const oilbird_kv_rows* v, int32_t m, int32_t rows, const int32_t* n_new,
                       const int32_t* select, const float* weight, void* cuda_stream);
 /* Slots start[s].. (dev [n_seq]; NULL: 0) as 16-bit rows: k, v dev [n_seq, n, n_kv_heads,
- * head_dim]; zeros where there is no slot. */
+ * head_dim]; zeros where there is no slot, the type's largest number where an element stands for
+ * more (its group's scale was rounded up). */
 int oilbird_kv_read(const oilbird_kv_cache* cache, int32_t n, const int32_t* start, void* k,
                     void* v, void* cuda_stream);
 /*

@@ -235,6 +235,13 @@ kv_read_kernel(const KvView c, const KvReadArgs a) {
 #pragma unroll
       for (int n = 0; n < 4; ++n)
         out[n] = pack16<kBf16>(fmaf((float)(w[kv][g] >> (4 * n) & 15u), sc, lo), fmaf((float)(w[kv][g] >> (16 + 4 * n) & 15u), sc, lo));
+      // The scale was rounded, up perhaps, so the largest code may stand for more than the type
+      // holds: its largest number then, as the group's elements were finite.
+      if (half_hi<kBf16>(pack16<kBf16>(0.f, fmaf(15.f, sc, lo))) == INFINITY) {
+        constexpr uint32_t kInf = kBf16 ? 0x7f80u : 0x7c00u;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) out[n] -= ((out[n] & 0x7fffu) == kInf ? 1u : 0u) + ((out[n] >> 16 & 0x7fffu) == kInf ? 0x10000u : 0u);
+      }
       __stcs(reinterpret_cast<uint4*>((kv ? a.v : a.k) + at + g * kKvGroup), make_uint4(out[0], out[1], out[2], out[3]));
     }
 }

@@ -149,6 +149,27 @@ def test_keys_near_the_largest_number(m, hq):
     check_attend(c, q, None, None, None, None, out, lse, 64 ** -0.5)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_read_of_the_largest_numbers_is_finite(dtype):
+    """15 * scale + lo may pass the type's largest number, as the scale was rounded up: the largest
+    number it is then."""
+    top = float(torch.finfo(KIND[dtype]).max)
+    d = 128
+    k = torch.zeros(1, 6, 1, d, device="cuda")
+    k[0, 0, 0, 3] = top
+    k[0, 1, 0, 70] = -top
+    k[0, 2, 0, 0], k[0, 2, 0, 1] = top, -top
+    k[0, 3] = top
+    k[0, 4, 0, :64] = torch.linspace(0, 1, 64, device="cuda") * top
+    k[0, 5, 0, 5] = float("inf")
+    c = custom(k, -k, d, 16, dtype)
+    for got, want in zip(c.cache.read(6), (k, -k)):
+        got, want = got[0, :, 0].double(), want[0, :, 0].double()
+        assert torch.isfinite(got[:5]).all() and torch.isfinite(got[5, 64:]).all() and torch.isnan(got[5, :64]).all()
+        # half a step of 2 top / 15 at most, the scale's rounding over fifteen codes, the result's own
+        assert float((got[:5] - want[:5]).abs().max()) <= top * (1 / 15 + 15 * UNIT[dtype] + UNIT[dtype])
+
+
 # ---------------------------------------------------------- slots without content ----
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
