@@ -964,6 +964,10 @@ class KVCache:
         need = self._L.oilbird_kv_workspace_bytes(int(head_dim))
         if workspace is None:
             workspace = torch.zeros(need, dtype=torch.uint8, device=dev)
+        elif workspace.device != dev or workspace.dtype != torch.uint8 or not workspace.is_contiguous() or \
+                workspace.numel() < need or workspace.data_ptr() % 16:
+            raise ValueError(f"workspace: {need} bytes at least (uint8, contiguous, 16-byte aligned, zeroed once), "
+                             "on the cache's device")
         self.pages, self.weight, self.pos, self.page_table = pages, weight, pos, page_table
         self.seq_len, self.n_pos, self.workspace = seq_len, n_pos, workspace
         self.dtype, self.head_dim, self.n_kv_heads = dtype, int(head_dim), int(weight.shape[1])

@@ -268,3 +268,20 @@ def test_waits_of_a_nanosecond_end_and_leave_everything_usable(d):
         stalled.zero_()
         out, lse = c.cache.attend(q, kn, vn)
         assert torch.equal(out, want) and torch.equal(lse, wl) and c.cache.dropped() == 0
+
+
+# ------------------------------------------------------------- what the binding takes ----
+
+def test_workspaces_are_checked():
+    """What goes to the kernels as a device address is one: of the cache's device, large enough."""
+    c = Made([40, 3], 1, 64, 16)
+    need = B.lib().oilbird_kv_workspace_bytes(64)
+    dev = c.pages.device
+    over = lambda w: B.KVCache.over(c.pages, c.weight, c.pos, c.table, c.seq_len, c.n_pos, workspace=w)
+    for bad in (torch.zeros(need, dtype=torch.uint8), torch.zeros(need, dtype=torch.int8, device=dev),
+                torch.zeros(need - 1, dtype=torch.uint8, device=dev),
+                torch.zeros(need, 2, dtype=torch.uint8, device=dev)[:, 0],
+                torch.zeros(need + 16, dtype=torch.uint8, device=dev)[8:]):
+        with pytest.raises(ValueError, match="workspace"):
+            over(bad)
+    assert over(torch.zeros(need, dtype=torch.uint8, device=dev)).dropped() == 0
