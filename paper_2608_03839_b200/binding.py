@@ -985,25 +985,25 @@ class KVCache:
     # comparison for each property, and four integers in place of the struct of the same layout.)
     def _rows(self, t: torch.Tensor, heads: int, m: int):
         """The C view of a [n_seq, m, heads, head_dim] tensor (any strides but the last)."""
-        if t.dtype is self.dtype and t.shape == (self.n_seq, m, heads, self.head_dim) and t.is_cuda:
+        if t.dtype is self.dtype and t.shape == (self.n_seq, m, heads, self.head_dim) and t.get_device() == self._index:
             s0, s1, s2, s3 = t.stride()
             if s3 == 1:
                 return _KV_ROWS(t.data_ptr(), s0, s1, s2)
-        raise AssertionError(f"a CUDA {self.dtype} tensor [{self.n_seq}, {m}, {heads}, {self.head_dim}] "
+        raise AssertionError(f"a {self.dtype} tensor [{self.n_seq}, {m}, {heads}, {self.head_dim}] on {self._dev} "
                              "with contiguous channels")
 
     def _vec(self, t, dtype, shape):
         """Pointer of an optional contiguous tensor of that type and shape."""
         if t is None:
             return None
-        if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
-            raise AssertionError(f"a contiguous CUDA {dtype} tensor {list(shape)}")
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != self._index or not t.is_contiguous():
+            raise AssertionError(f"a contiguous {dtype} tensor {list(shape)} on {self._dev}")
         return t.data_ptr()
 
     def _lse(self, t, m, heads):
         """Pointer and strides of a [n_seq, m, heads] fp32 tensor."""
-        if t.dtype is not torch.float32 or t.shape != (self.n_seq, m, heads) or not t.is_cuda:
-            raise AssertionError(f"a CUDA fp32 tensor [{self.n_seq}, {m}, {heads}]")
+        if t.dtype is not torch.float32 or t.shape != (self.n_seq, m, heads) or t.get_device() != self._index:
+            raise AssertionError(f"an fp32 tensor [{self.n_seq}, {m}, {heads}] on {self._dev}")
         return t.data_ptr(), None if t.is_contiguous() else _KV_STRIDES(*t.stride())
 
     def _mask(self, mask, m):
@@ -1011,8 +1011,8 @@ class KVCache:
             return None, 0
         shape = mask.shape
         if mask.dtype not in _KV_MASKS or len(shape) != 2 or shape[0] != self.n_seq or shape[1] < m or \
-                not mask.is_cuda or mask.stride(1) != 1:
-            raise AssertionError(f"a CUDA int64 tensor [{self.n_seq}, {m} or more]")
+                mask.get_device() != self._index or mask.stride(1) != 1:
+            raise AssertionError(f"an int64 tensor [{self.n_seq}, {m} or more] on {self._dev}")
         return mask.data_ptr(), mask.stride(0)
 
     def _new(self, like: torch.Tensor, shape) -> torch.Tensor:

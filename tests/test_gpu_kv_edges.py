@@ -285,3 +285,21 @@ def test_workspaces_are_checked():
         with pytest.raises(ValueError, match="workspace"):
             over(bad)
     assert over(torch.zeros(need, dtype=torch.uint8, device=dev)).dropped() == 0
+
+
+def test_tensors_of_another_device_are_refused():
+    c = Made([40, 3], 1, 64, 16)
+    q, kn = c.rand(2, 2, 4, 64).bfloat16(), c.rand(2, 2, 1, 64).bfloat16()
+    out, lse = c.cache.attend(q, kn, kn)
+    ints = torch.ones(2, dtype=torch.int32, device="cuda")
+    words = torch.ones(2, 2, dtype=torch.int64, device="cuda")
+    calls = [lambda d: c.cache._rows(d(q), 4, 2), lambda d: c.cache._vec(d(ints), torch.int32, (2,)),
+             lambda d: c.cache._lse(d(lse), 2, 4), lambda d: c.cache._mask(d(words), 2)]
+    for call in calls:
+        call(lambda t: t)
+        with pytest.raises(AssertionError):
+            call(lambda t: t.cpu())
+    c.cache._index = 1                                           # as if the cache lay on the second GPU
+    for call in calls:
+        with pytest.raises(AssertionError):
+            call(lambda t: t)
