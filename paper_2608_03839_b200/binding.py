@@ -915,6 +915,7 @@ class KVCache:
     on tensors the caller holds: pages (uint8, the blocks of all pages), weight (fp32) and pos
     (int32) [n_pages, n_kv_heads, page_size], page_table (int32 [n_seq, max_pages]), seq_len and
     n_pos (int32 [n_seq]).  The workspace may be shared by caches that are used on one stream.
+    There is no backward pass: tensors that want a gradient are refused where one would be recorded.
     """
 
     def __init__(self, n_seq: int, n_kv_heads: int, head_dim: int, max_len: int, *,
@@ -986,6 +987,9 @@ class KVCache:
     def _rows(self, t: torch.Tensor, heads: int, m: int):
         """The C view of a [n_seq, m, heads, head_dim] tensor (any strides but the last)."""
         if t.dtype is self.dtype and t.shape == (self.n_seq, m, heads, self.head_dim) and t.get_device() == self._index:
+            if t.requires_grad and torch.is_grad_enabled():
+                raise RuntimeError("the key/value cache has no backward pass: detach the tensor, or call under "
+                                   "torch.no_grad()")
             s0, s1, s2, s3 = t.stride()
             if s3 == 1:
                 return _KV_ROWS(t.data_ptr(), s0, s1, s2)

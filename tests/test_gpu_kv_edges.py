@@ -303,3 +303,16 @@ def test_tensors_of_another_device_are_refused():
     for call in calls:
         with pytest.raises(AssertionError):
             call(lambda t: t)
+
+
+def test_tensors_that_want_a_gradient_are_refused():
+    c = Made([40, 3], 1, 64, 16)
+    q, kn = c.rand(2, 2, 4, 64).bfloat16().requires_grad_(), c.rand(2, 2, 1, 64).bfloat16()
+    with pytest.raises(RuntimeError, match="no backward"):
+        c.cache.attend(q, kn, kn)
+    with pytest.raises(RuntimeError, match="no backward"):
+        c.cache.append(kn, kn.clone().requires_grad_())
+    with torch.no_grad():
+        out, lse = c.cache.attend(q, kn, kn)
+    a, b = c.cache.attend(q.detach(), kn, kn)
+    assert torch.equal(out, a) and torch.equal(lse, b) and c.seq_len.tolist() == [40, 3]
