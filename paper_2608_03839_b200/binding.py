@@ -914,12 +914,14 @@ class KVCache:
     KVCache(...) allocates everything, max_len slots for each sequence.  KVCache.over(...) works
     on tensors the caller holds: pages (uint8, the blocks of all pages), weight (fp32) and pos
     (int32) [n_pages, n_kv_heads, page_size], page_table (int32 [n_seq, max_pages]), seq_len and
-    n_pos (int32 [n_seq]).  The workspace may be shared by caches that are used on one stream.
+    n_pos (int32 [n_seq]).  workspace (22 MB for heads of 64, 43 MB for 128; None: one of its own) may
+    be shared by caches that are used on one stream, as a model's layers are: pass another's .workspace.
     There is no backward pass: tensors that want a gradient are refused where one would be recorded.
     """
 
     def __init__(self, n_seq: int, n_kv_heads: int, head_dim: int, max_len: int, *,
-                 page_size: int = 64, dtype=torch.bfloat16, device: int = 0):
+                 page_size: int = 64, dtype=torch.bfloat16, device: int = 0,
+                 workspace: torch.Tensor | None = None):
         if not torch.cuda.is_available():
             raise RuntimeError("the key/value cache needs a CUDA device; there is no CPU fallback")
         dev = torch.device(f"cuda:{device}")
@@ -933,7 +935,7 @@ class KVCache:
                     torch.zeros(n_pages, n_kv_heads, page_size, dtype=torch.int32, device=dev),
                     torch.arange(n_pages, dtype=torch.int32, device=dev).view(n_seq, per),
                     torch.zeros(n_seq, dtype=torch.int32, device=dev),
-                    torch.zeros(n_seq, dtype=torch.int32, device=dev), dtype, head_dim, None)
+                    torch.zeros(n_seq, dtype=torch.int32, device=dev), dtype, head_dim, workspace)
 
     @classmethod
     def over(cls, pages: torch.Tensor, weight: torch.Tensor, pos: torch.Tensor,

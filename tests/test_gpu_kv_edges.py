@@ -316,3 +316,19 @@ def test_tensors_that_want_a_gradient_are_refused():
         out, lse = c.cache.attend(q, kn, kn)
     a, b = c.cache.attend(q.detach(), kn, kn)
     assert torch.equal(out, a) and torch.equal(lse, b) and c.seq_len.tolist() == [40, 3]
+
+
+def test_an_owned_cache_takes_a_workspace():
+    """Caches of one stream (a model's layers) share one."""
+    one = B.KVCache(2, 1, 64, 100, page_size=16)
+    two = B.KVCache(2, 1, 64, 100, page_size=16, workspace=one.workspace)
+    assert two.workspace.data_ptr() == one.workspace.data_ptr()
+    k = torch.randn(2, 90, 1, 64, device="cuda").bfloat16()
+    q = torch.randn(2, 1, 4, 64, device="cuda").bfloat16()
+    for c in (one, two, one, two):
+        c.append(k[:, :45], k[:, 45:])
+        c.attend(q)
+    a, b = one.attend(q), two.attend(q)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and one.seq_len.tolist() == [90, 90]
+    with pytest.raises(ValueError, match="workspace"):
+        B.KVCache(2, 1, 128, 100, workspace=one.workspace)       # smaller than heads of 128 need
