@@ -667,8 +667,8 @@ typedef struct {
   int32_t        dtype;        /* OILBIRD_KV_BF16 or OILBIRD_KV_F16                       */
   int32_t        device;       /* CUDA ordinal                                            */
 } oilbird_kv_cache;
-/* 16-bit elements [sequence, row, head, channel]; strides in elements, multiples of 8; channels
- * are contiguous; data 16-byte aligned. */
+/* 16-bit elements [sequence, row, head, channel]; strides in elements, multiples of 8 (anything
+ * where there is one sequence, row or head); channels are contiguous; data 16-byte aligned. */
 typedef struct {
   const void* data;
   int64_t seq_stride, row_stride, head_stride;
@@ -695,7 +695,8 @@ int oilbird_kv_read(const oilbird_kv_cache* cache, int32_t n, const int32_t* sta
  * Attention of m nodes per sequence: q [n_seq, m, n_q_heads, head_dim] (head h reads key/value
  * head h / (n_q_heads / n_kv_heads)), scores scale * q.k over every slot of the sequence and,
  * with k_new and v_new ([n_seq, m, n_kv_heads, head_dim], in 16 bits), over the nodes j whose
- * bit is set in the node's mask word (dev, mask_stride words per sequence; NULL: nodes 0..i).
+ * bit is set in the node's mask word (dev, mask_stride words per sequence, 0: the same for all;
+ * NULL: nodes 0..i).
  * n_new: nodes of each sequence (dev; NULL: m); what lies behind them gets out = 0, lse = -inf,
  * and so does a row that sees nothing.  out: like q, written; lse: dev fp32 [n_seq, m, n_q_heads],
  * natural logarithm of the sum of exponentials, may be NULL; lse_strides (host): its strides in

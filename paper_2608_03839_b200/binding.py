@@ -1017,7 +1017,7 @@ class KVCache:
             return None, 0
         shape = mask.shape
         if mask.dtype not in _KV_MASKS or len(shape) != 2 or shape[0] != self.n_seq or shape[1] < m or \
-                mask.get_device() != self._index or mask.stride(1) != 1:
+                mask.get_device() != self._index or (mask.stride(1) != 1 and shape[1] > 1):
             raise AssertionError(f"an int64 tensor [{self.n_seq}, {m} or more] on {self._dev}")
         return mask.data_ptr(), mask.stride(0)
 

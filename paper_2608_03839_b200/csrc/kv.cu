@@ -57,16 +57,22 @@ static int check_cache(const oilbird_kv_cache* c, KvView* v) {
   return OILBIRD_OK;
 }
 
-static int check_rows(const oilbird_kv_rows* r, const char* what, KvRows* out) {
+// n_seq, rows, heads: the extents; the stride of an extent of one is never used, so it may be anything.
+static int check_rows(const oilbird_kv_rows* r, const char* what, int n_seq, int rows, int heads, KvRows* out) {
   if (!r || !r->data) return kv_refuse(what);
-  if (!aligned(r->data, 16) || r->seq_stride % 8 || r->row_stride % 8 || r->head_stride % 8) {
+  out->p = (const uint16_t*)r->data;
+  out->seq = n_seq > 1 ? r->seq_stride : 0;
+  out->row = rows > 1 ? r->row_stride : 0;
+  out->head = heads > 1 ? r->head_stride : 0;
+  if (!aligned(r->data, 16) || out->seq % 8 || out->row % 8 || out->head % 8) {
     snprintf(g_kv_err, sizeof g_kv_err, "%s: 16-byte aligned, with strides that are multiples of 8 elements", what);
     return OILBIRD_EINVAL;
   }
-  out->p = (const uint16_t*)r->data;
-  out->seq = r->seq_stride;
-  out->row = r->row_stride;
-  out->head = r->head_stride;
+  return OILBIRD_OK;
+}
+static int check_mask(const oilbird_kv_cache* c, const uint64_t* mask, int64_t stride, int m) {
+  if (mask && (!aligned(mask, 8) || (c->n_seq > 1 && stride != 0 && stride < m)))
+    return kv_refuse("mask: 8-byte aligned, m words a sequence at least, or a stride of 0");
   return OILBIRD_OK;
 }
 
@@ -124,8 +130,8 @@ int oilbird_kv_append(const oilbird_kv_cache* cache, const oilbird_kv_rows* k, c
   if (m < 0 || rows < 0 || rows > (1 << 24)) return kv_refuse("m and rows: not negative, rows at most 2^24");
   if (m == 0 || rows == 0) return OILBIRD_OK;
   if (!select && rows > m) return kv_refuse("rows: m at most without select");
-  KTRY(check_rows(k, "k", &a.k));
-  KTRY(check_rows(v, "v", &a.v));
+  KTRY(check_rows(k, "k", c.n_seq, m, c.n_kv, &a.k));
+  KTRY(check_rows(v, "v", c.n_seq, m, c.n_kv, &a.v));
   a.n_new = n_new;
   a.select = select;
   a.weight = weight;
@@ -161,14 +167,14 @@ int oilbird_kv_attend(const oilbird_kv_cache* cache, int32_t n_q_heads, int32_t 
   memset(&a, 0, sizeof a);
   KTRY(check_cache(cache, &c));
   KTRY(check_heads(cache, n_q_heads, m));
-  KTRY(check_rows(q, "q", &a.q));
-  KTRY(check_rows(out, "out", &o));
+  KTRY(check_rows(q, "q", c.n_seq, m, n_q_heads, &a.q));
+  KTRY(check_rows(out, "out", c.n_seq, m, n_q_heads, &o));
   if (!k_new != !v_new) return kv_refuse("k_new and v_new: both or neither");
   if (k_new) {
-    KTRY(check_rows(k_new, "k_new", &a.k));
-    KTRY(check_rows(v_new, "v_new", &a.v));
+    KTRY(check_rows(k_new, "k_new", c.n_seq, m, c.n_kv, &a.k));
+    KTRY(check_rows(v_new, "v_new", c.n_seq, m, c.n_kv, &a.v));
   }
-  if (mask && (!aligned(mask, 8) || mask_stride < m)) return kv_refuse("mask: 8-byte aligned, m words a sequence at least");
+  KTRY(check_mask(cache, mask, mask_stride, m));
   if (!(scale == scale)) return kv_refuse("scale: a number");
   a.out = (uint16_t*)o.p;
   a.out_seq = o.seq;
@@ -199,11 +205,11 @@ int oilbird_kv_weigh(const oilbird_kv_cache* cache, int32_t n_q_heads, int32_t m
   memset(&a, 0, sizeof a);
   KTRY(check_cache(cache, &c));
   KTRY(check_heads(cache, n_q_heads, m));
-  KTRY(check_rows(q, "q", &a.q));
+  KTRY(check_rows(q, "q", c.n_seq, m, n_q_heads, &a.q));
   if (!lse || !aligned(lse, 4)) return kv_refuse("lse");
   if (!k_new != !node_weight) return kv_refuse("k_new and node_weight: both or neither");
-  if (k_new) KTRY(check_rows(k_new, "k_new", &a.k));
-  if (mask && (!aligned(mask, 8) || mask_stride < m)) return kv_refuse("mask: 8-byte aligned, m words a sequence at least");
+  if (k_new) KTRY(check_rows(k_new, "k_new", c.n_seq, m, c.n_kv, &a.k));
+  KTRY(check_mask(cache, mask, mask_stride, m));
   if (!(scale == scale)) return kv_refuse("scale: a number");
   a.node_weight = node_weight;
   a.lse = lse;

@@ -332,3 +332,30 @@ def test_an_owned_cache_takes_a_workspace():
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and one.seq_len.tolist() == [90, 90]
     with pytest.raises(ValueError, match="workspace"):
         B.KVCache(2, 1, 128, 100, workspace=one.workspace)       # smaller than heads of 128 need
+
+
+def test_strides_of_dimensions_of_one_do_not_matter():
+    """One sequence, one node: its row of a wider buffer whose rows are no multiple of 16 bytes."""
+    c = Made([40], 1, 64, 16)
+    wide = c.rand(1, 1, 4 * 64 + 2 * 64 + 4).bfloat16()
+    q, kn, vn = (torch.as_strided(wide, (1, 1, h, 64), (388, 388, 64, 1), at) for h, at in ((4, 0), (1, 256), (1, 320)))
+    assert q.stride()[:2] == (388, 388)
+    mask = torch.ones(1, 1, dtype=torch.int64, device="cuda")
+    out, lse = c.cache.attend(q, kn, vn, mask=mask)
+    a, b = c.cache.attend(q.contiguous(), kn.contiguous(), vn.contiguous(), mask=mask)
+    assert torch.equal(out, a) and torch.equal(lse, b)
+    nodes = c.cache.weigh(q, lse, kn, mask=mask)
+    c.cache.append(kn, vn, weight=nodes)
+    # masks: one request's as a column, every request's alike
+    m = 3
+    q, kn = c.rand(1, m, 4, 64).bfloat16(), c.rand(1, m, 1, 64).bfloat16()
+    column = torch.tensor([[1], [3], [5]], dtype=torch.int64, device="cuda").t()
+    assert column.stride() == (1, 1)
+    a, b = c.cache.attend(q, kn, kn, mask=column), c.cache.attend(q, kn, kn, mask=column.clone(memory_format=torch.contiguous_format))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    c = Made([40, 3, 0], 1, 64, 16)
+    q, kn = c.rand(3, m, 4, 64).bfloat16(), c.rand(3, m, 1, 64).bfloat16()
+    alike = column.expand(3, m)
+    assert alike.stride(0) == 0
+    a, b = c.cache.attend(q, kn, kn, mask=alike), c.cache.attend(q, kn, kn, mask=alike.contiguous())
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
