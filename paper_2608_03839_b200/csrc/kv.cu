@@ -3,6 +3,7 @@
 #include <string.h>
 
 #include <atomic>
+#include <initializer_list>
 
 #include "kv.cuh"
 
@@ -70,6 +71,15 @@ static int check_rows(const oilbird_kv_rows* r, const char* what, int n_seq, int
   }
   return OILBIRD_OK;
 }
+// Arrays of 32-bit elements, each of which may be missing.
+static int check_words(const char* what, std::initializer_list<const void*> arrays) {
+  for (const void* p : arrays)
+    if (!aligned(p, 4)) {
+      snprintf(g_kv_err, sizeof g_kv_err, "%s: 4-byte aligned", what);
+      return OILBIRD_EINVAL;
+    }
+  return OILBIRD_OK;
+}
 static int check_mask(const oilbird_kv_cache* c, const uint64_t* mask, int64_t stride, int m) {
   if (mask && (!aligned(mask, 8) || (c->n_seq > 1 && stride != 0 && stride < m)))
     return kv_refuse("mask: 8-byte aligned, m words a sequence at least, or a stride of 0");
@@ -132,6 +142,7 @@ int oilbird_kv_append(const oilbird_kv_cache* cache, const oilbird_kv_rows* k, c
   if (!select && rows > m) return kv_refuse("rows: m at most without select");
   KTRY(check_rows(k, "k", c.n_seq, m, c.n_kv, &a.k));
   KTRY(check_rows(v, "v", c.n_seq, m, c.n_kv, &a.v));
+  KTRY(check_words("n_new, select, weight", {n_new, select, weight}));
   a.n_new = n_new;
   a.select = select;
   a.weight = weight;
@@ -150,6 +161,7 @@ int oilbird_kv_read(const oilbird_kv_cache* cache, int32_t n, const int32_t* sta
   if (n < 0 || n > (1 << 24)) return kv_refuse("n: 0 to 2^24");
   if (n == 0) return OILBIRD_OK;
   if (!k || !v || !aligned(k, 16) || !aligned(v, 16)) return kv_refuse("k and v: 16-byte aligned");
+  KTRY(check_words("start", {start}));
   const KvReadArgs a = {(uint16_t*)k, (uint16_t*)v, start, n};
   int sms;
   KTRY(on_device(cache->device, &sms));
@@ -176,6 +188,7 @@ int oilbird_kv_attend(const oilbird_kv_cache* cache, int32_t n_q_heads, int32_t 
   }
   KTRY(check_mask(cache, mask, mask_stride, m));
   if (!(scale == scale)) return kv_refuse("scale: a number");
+  KTRY(check_words("lse, n_new", {lse, n_new}));
   a.out = (uint16_t*)o.p;
   a.out_seq = o.seq;
   a.out_row = o.row;
@@ -206,7 +219,8 @@ int oilbird_kv_weigh(const oilbird_kv_cache* cache, int32_t n_q_heads, int32_t m
   KTRY(check_cache(cache, &c));
   KTRY(check_heads(cache, n_q_heads, m));
   KTRY(check_rows(q, "q", c.n_seq, m, n_q_heads, &a.q));
-  if (!lse || !aligned(lse, 4)) return kv_refuse("lse");
+  if (!lse) return kv_refuse("lse");
+  KTRY(check_words("lse, n_new, row_weight, node_weight", {lse, n_new, row_weight, node_weight}));
   if (!k_new != !node_weight) return kv_refuse("k_new and node_weight: both or neither");
   if (k_new) KTRY(check_rows(k_new, "k_new", c.n_seq, m, c.n_kv, &a.k));
   KTRY(check_mask(cache, mask, mask_stride, m));
