@@ -40,7 +40,7 @@
 
 namespace oilbird {
 
-// Rows per block are 8 NT.  A warp holds its tile's keys and values in buffers of their own: the
+// A block takes all rows of a key head, 8 NT at most (16, so 16 new nodes at most).  A warp holds its tile's keys and values in buffers of their own: the
 // next tile's keys are asked for as soon as the scores are taken, its values after the products
 // with them, so that a single buffer of each keeps half a tile per warp in flight.
 // Eight rows leave registers (168 a thread) for twelve warps an SM, sixteen rows for eight.
@@ -62,7 +62,7 @@ struct Attend {
   static constexpr int kCum = (kKvMaxSeq + 1) * 8;
   static constexpr int kBytes = kRing + kObuf + kMl + kCum + kWarps * 8 + kKvMaxSeq * 5 + 64;
 };
-struct OpenItem { int b0, b1, s, head, row0, n_rows; };  // an item whose pieces are all there
+struct OpenItem { int b0, b1, s, head, n_rows; };  // an item whose pieces are all there
 
 template <int N> __device__ __forceinline__ void load_floats(const float* p, float (&v)[N]) {
   if (N == 4) { const float4 x = *reinterpret_cast<const float4*>(p); v[0] = x.x; v[1] = x.y; v[N - 2] = x.z; v[N - 1] = x.w; }
@@ -95,7 +95,6 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
   OpenItem* open = reinterpret_cast<OpenItem*>(n_open + 1);
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, g = lane >> 2, t4 = lane & 3;
-  const int rblocks = (a.m * a.group + kRows - 1) / kRows;
   if (tid == 0) *n_open = 0;                             // (barriers follow)
   pdl_enter();
 
@@ -103,7 +102,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
   list.cum = cum;
   list.len = len_s;
   list.nodes = nodes_s;
-  list.items = c.n_kv * rblocks;
+  list.items = c.n_kv;
   list.group = a.group;
   list.rows = kRows;
   list.build<kAtThreads>(c, a.n_new, a.m, scratch);
@@ -166,8 +165,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
     const int item = bc.item, tile0 = bc.tile;
     const int n_tiles = item < bc.live ? bc.tiles : 1;
     const int piece = min(n_tiles - tile0, u1 - at), item_u0 = at - tile0;
-    // live items: head fastest, then row block; the others follow in the same order
-    const int head = bc.head, row0 = item / c.n_kv * kRows;
+    const int head = bc.head;
     const int n_rows = bc.nodes * a.group;               // rows of the sequence that exist
     const int s = bc.s;
 
@@ -190,23 +188,19 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
       }
     }
 
-    if (item < bc.live && mu < at + piece && mu < item_u0 + kKvFront) {
-      // ---- the item's first round: new nodes, 16-bit keys and values, with the tree's mask ----
-      const int node0 = (mu - item_u0) * kKvNodeTile;
-      if (a.k.p && node0 < bc.nodes) {
+    if (item < bc.live && mu < at + piece && mu == item_u0) {
+      // ---- the item's first tile: new nodes, 16-bit keys and values, with the tree's mask ----
+      if (a.k.p) {
         had = true;
-        float sc[NT][2][4];
+        float sc[NT][4];
 #pragma unroll
         for (int r = 0; r < NT; ++r)
 #pragma unroll
-          for (int ch = 0; ch < 2; ++ch)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sc[r][ch][e] = 0.f;
-        const bool both = node0 + 16 < bc.nodes;         // the second sixteen exist
-        uint4 qw[NT][G][2];
+          for (int e = 0; e < 4; ++e) sc[r][e] = 0.f;
+        uint4 qw[NT][G][2], kw[2][G][2];
 #pragma unroll
         for (int r = 0; r < NT; ++r) {
-          const int row = row0 + r * 8 + g;
+          const int row = r * 8 + g;
           const int node = row < n_rows ? row / a.group : 0, sub = row < n_rows ? row % a.group : 0;
           const uint16_t* qp = a.q.at(s, node, head * a.group + sub) + t4 * 16;
 #pragma unroll
@@ -218,38 +212,33 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
             }
         }
 #pragma unroll
-        for (int ch = 0; ch < 2; ++ch) {
-          if (ch && !both) break;
-          uint4 kw[2][G][2];
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const int node = node0 + ch * 16 + g + 8 * k;
-            const uint16_t* kp = a.k.at(s, node < bc.nodes ? node : 0, head) + t4 * 16;
-#pragma unroll
-            for (int i = 0; i < G; ++i)
-#pragma unroll
-              for (int half = 0; half < 2; ++half) {
-                kw[k][i][half] = make_uint4(0, 0, 0, 0);
-                if (node < bc.nodes) kw[k][i][half] = *reinterpret_cast<const uint4*>(kp + i * kKvGroup + half * 8);
-              }
-          }
+        for (int k = 0; k < 2; ++k) {
+          const int node = g + 8 * k;
+          const uint16_t* kp = a.k.at(s, node < bc.nodes ? node : 0, head) + t4 * 16;
 #pragma unroll
           for (int i = 0; i < G; ++i)
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-              for (int r = 0; r < NT; ++r) {
-                const uint4 &x = kw[0][i][half], &y = kw[1][i][half], &z = qw[r][i][half];
-                mma16816<kBf16>(sc[r][ch], x.x, y.x, x.y, y.y, z.x, z.y);
-                mma16816<kBf16>(sc[r][ch], x.z, y.z, x.w, y.w, z.z, z.w);
-              }
+            for (int half = 0; half < 2; ++half) {
+              kw[k][i][half] = make_uint4(0, 0, 0, 0);
+              if (node < bc.nodes) kw[k][i][half] = *reinterpret_cast<const uint4*>(kp + i * kKvGroup + half * 8);
+            }
         }
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int r = 0; r < NT; ++r) {
+              const uint4 &x = kw[0][i][half], &y = kw[1][i][half], &z = qw[r][i][half];
+              mma16816<kBf16>(sc[r], x.x, y.x, x.y, y.y, z.x, z.y);
+              mma16816<kBf16>(sc[r], x.z, y.z, x.w, y.w, z.z, z.w);
+            }
         const float fs = a.scale * kLog2e;
 #pragma unroll
         for (int r = 0; r < NT; ++r)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const int row = row0 + r * 8 + 2 * t4 + e;
+            const int row = r * 8 + 2 * t4 + e;
             unsigned long long sees = 0;
             if (row < n_rows) {
               const int node = row / a.group;
@@ -257,15 +246,13 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
             }
             float mx = -INFINITY;
 #pragma unroll
-            for (int ch = 0; ch < 2; ++ch)
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const int node = node0 + ch * 16 + g + 8 * k;
-                const bool ok = node < bc.nodes && (sees >> node & 1ull);
-                float& x = sc[r][ch][e + 2 * k];
-                x = ok ? x * fs : -INFINITY;
-                mx = fmaxf(mx, x);
-              }
+            for (int k = 0; k < 2; ++k) {
+              const int node = g + 8 * k;
+              const bool ok = node < bc.nodes && (sees >> node & 1ull);
+              float& x = sc[r][e + 2 * k];
+              x = ok ? x * fs : -INFINITY;
+              mx = fmaxf(mx, x);
+            }
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
             m[r][e] = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
@@ -274,58 +261,54 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
         // the first cached tile chooses anew
         eref = 0;
         bool odd = false;
+        // p as the sum of two 16-bit numbers: with bf16 one alone would be as coarse as the
+        // result's own rounding
+        uint32_t hi[NT][2], lo[NT][2];
 #pragma unroll
-        for (int ch = 0; ch < 2; ++ch) {
-          if (ch && !both) break;
-          // p as the sum of two 16-bit numbers: with bf16 one alone would be as coarse as the
-          // result's own rounding
-          uint32_t hi[NT][2], lo[NT][2];
+        for (int r = 0; r < NT; ++r)
 #pragma unroll
-          for (int r = 0; r < NT; ++r)
+          for (int k = 0; k < 2; ++k) {
+            float p[2];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              float p[2];
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                p[e] = exp2_approx(sc[r][ch][e + 2 * k] - (m[r][e] == -INFINITY ? 0.f : m[r][e]));
-                l[r][e] += p[e];
-              }
-              const uint32_t h = pack16<kBf16>(p[0], p[1]);
-              hi[r][k] = transpose8x8(h);
-              lo[r][k] = transpose8x8(pack16<kBf16>(p[0] - half_lo<kBf16>(h), p[1] - half_hi<kBf16>(h)));
+            for (int e = 0; e < 2; ++e) {
+              p[e] = exp2_approx(sc[r][e + 2 * k] - (m[r][e] == -INFINITY ? 0.f : m[r][e]));
+              l[r][e] += p[e];
             }
-          uint4 w[G][4];                                 // nodes 2t, 2t+1, 2t+8, 2t+9; 8 channels
+            const uint32_t h = pack16<kBf16>(p[0], p[1]);
+            hi[r][k] = transpose8x8(h);
+            lo[r][k] = transpose8x8(pack16<kBf16>(p[0] - half_lo<kBf16>(h), p[1] - half_hi<kBf16>(h)));
+          }
+        uint4 w[G][4];                                   // nodes 2t, 2t+1, 2t+8, 2t+9; 8 channels
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int node = node0 + ch * 16 + 2 * t4 + (k & 1) + 8 * (k >> 1);
-            const uint16_t* vp = a.v.at(s, node < bc.nodes ? node : 0, head) + g * 8;
+        for (int k = 0; k < 4; ++k) {
+          const int node = 2 * t4 + (k & 1) + 8 * (k >> 1);
+          const uint16_t* vp = a.v.at(s, node < bc.nodes ? node : 0, head) + g * 8;
 #pragma unroll
-            for (int i = 0; i < G; ++i) {
-              w[i][k] = make_uint4(0, 0, 0, 0);
-              if (node < bc.nodes) w[i][k] = *reinterpret_cast<const uint4*>(vp + i * kKvGroup);
+          for (int i = 0; i < G; ++i) {
+            w[i][k] = make_uint4(0, 0, 0, 0);
+            if (node < bc.nodes) w[i][k] = *reinterpret_cast<const uint4*>(vp + i * kKvGroup);
 #pragma unroll
-              for (int x = 0; x < 4; ++x) {              // infinities and NaN: see below
-                uint32_t& v = (&w[i][k].x)[x];
-                constexpr uint32_t kInf = kBf16 ? 0x7f80u : 0x7c00u;
-                if ((v & kInf) == kInf) { odd = true; v &= 0xffff0000u; }
-                if ((v >> 16 & kInf) == kInf) { odd = true; v &= 0x0000ffffu; }
-              }
+            for (int x = 0; x < 4; ++x) {                // infinities and NaN: see below
+              uint32_t& v = (&w[i][k].x)[x];
+              constexpr uint32_t kInf = kBf16 ? 0x7f80u : 0x7c00u;
+              if ((v & kInf) == kInf) { odd = true; v &= 0xffff0000u; }
+              if ((v >> 16 & kInf) == kInf) { odd = true; v &= 0x0000ffffu; }
             }
           }
-#pragma unroll
-          for (int i = 0; i < G; ++i)
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-              const uint32_t x0 = (&w[i][0].x)[n], x1 = (&w[i][1].x)[n], x2 = (&w[i][2].x)[n], x3 = (&w[i][3].x)[n];
-              const uint32_t ea = __byte_perm(x0, x1, 0x5410), oa = __byte_perm(x0, x1, 0x7632);
-              const uint32_t eb = __byte_perm(x2, x3, 0x5410), ob = __byte_perm(x2, x3, 0x7632);
-#pragma unroll
-              for (int r = 0; r < NT; ++r) {
-                mma16816<kBf16>(o[r][i * 4 + n], ea, oa, eb, ob, hi[r][0], hi[r][1]);
-                mma16816<kBf16>(o[r][i * 4 + n], ea, oa, eb, ob, lo[r][0], lo[r][1]);
-              }
-            }
         }
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            const uint32_t x0 = (&w[i][0].x)[n], x1 = (&w[i][1].x)[n], x2 = (&w[i][2].x)[n], x3 = (&w[i][3].x)[n];
+            const uint32_t ea = __byte_perm(x0, x1, 0x5410), oa = __byte_perm(x0, x1, 0x7632);
+            const uint32_t eb = __byte_perm(x2, x3, 0x5410), ob = __byte_perm(x2, x3, 0x7632);
+#pragma unroll
+            for (int r = 0; r < NT; ++r) {
+              mma16816<kBf16>(o[r][i * 4 + n], ea, oa, eb, ob, hi[r][0], hi[r][1]);
+              mma16816<kBf16>(o[r][i * 4 + n], ea, oa, eb, ob, lo[r][0], lo[r][1]);
+            }
+          }
         if (__any_sync(0xffffffffu, odd)) {
           // values that are not finite stayed out of the products (0 times a hidden node's
           // would have reached every row): they are added to the rows that see them
@@ -333,11 +316,11 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
           for (int r = 0; r < NT; ++r)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const int row = row0 + r * 8 + 2 * t4 + e;
+              const int row = r * 8 + 2 * t4 + e;
               if (row >= n_rows) continue;
               const int node = row / a.group;
               const unsigned long long sees = a.mask ? a.mask[s * a.mask_stride + node] : (2ull << node) - 1ull;
-              for (int j = node0; j < min(node0 + kKvNodeTile, bc.nodes); ++j)
+              for (int j = 0; j < bc.nodes; ++j)
                 if (sees >> j & 1ull) {
                   const uint16_t* vp = a.v.at(s, j, head) + g * 8;
 #pragma unroll
@@ -373,7 +356,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
           loaded = had = true;
 #pragma unroll
           for (int r = 0; r < NT; ++r) {
-            const int row = row0 + r * 8 + g;
+            const int row = r * 8 + g;
             const bool have = row < n_rows;
             const int node = have ? row / a.group : 0;
             float sum[G];
@@ -668,7 +651,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
           }
         }
         if (whole) {
-          finish(s, head, row0 + r * 8 + rr, n_rows, big, sum, v);
+          finish(s, head, r * 8 + rr, n_rows, big, sum, v);
         } else {
           store_floats<kPer>(my_part + (size_t)(r * 8 + rr) * D + lane * kPer, v);
           if (lane == 0)
@@ -684,7 +667,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
       __threadfence();
       if (n == (unsigned)(b1 - b0)) {
         *ticket = 0u;                                    // for the next call
-        open[*n_open] = OpenItem{b0, b1, s, head, row0, n_rows};
+        open[*n_open] = OpenItem{b0, b1, s, head, n_rows};
         ++*n_open;                                       // its first and its last item, at most
       }
     }
@@ -730,7 +713,7 @@ kv_attend_kernel(const KvView c, const KvAttendArgs a) {
           }
         }
       }
-      finish(it.s, it.head, it.row0 + r, it.n_rows, big, sum, v);
+      finish(it.s, it.head, r, it.n_rows, big, sum, v);
     }
   }
 }
