@@ -359,3 +359,145 @@ def test_strides_of_dimensions_of_one_do_not_matter():
     assert alike.stride(0) == 0
     a, b = c.cache.attend(q, kn, kn, mask=alike), c.cache.attend(q, kn, kn, mask=alike.contiguous())
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+# ------------------------------------------------------------------ further ranges ----
+
+def score_error(row, k, d, scale, many):
+    """How far a score may be off.  Few rows: fp32 sums of the codes' products and the offsets' (see
+    test_gpu_kv).  Many: sums of 2 D products, 16 a step, each step cut off at 2^-23 of the sum; the
+    exponential's argument; keys as the sum of two f16 numbers, off by 2^-13 of their group's scale
+    (independent in the channels: five standard deviations) and 2^-23 of the largest element."""
+    size = scale * (np.abs(row) @ np.abs(k).T).max(initial=0)
+    top = np.abs(k).max(initial=0) * scale * np.abs(row).sum(-1).max()
+    if not many:
+        return 2.0 ** -24 * (d + 12) * (size + 2 * top) + 2.0 ** -21
+    step = np.ptp(k.reshape(-1, 64), -1).max(initial=0) / 15
+    return (2.0 ** -23 * (2 * d / 16 + 4) * size + 2.0 ** -21 + 5 * 2.0 ** -13 / 3 ** 0.5 * step * scale * np.sqrt((row ** 2).sum(-1)).max()
+            + 2.0 ** -23 * top)
+
+
+@pytest.mark.parametrize("d,dtype", [(128, "bf16"), (128, "f16"), (64, "bf16"), (64, "f16")])
+@pytest.mark.parametrize("m,hq", [(5, 4), (20, 8), (60, 4)])
+def test_scores_of_many_rows(m, hq, d, dtype):
+    """lse and out to what two-part keys give.  (f16 keys rounded once are off by three times the bound
+    on the short sequences; bf16 ones, whose scales have eight bits, mostly fit f16 as they are.)"""
+    lens = [1, 2, 3, 5, 40, 130, 3000, 0]
+    c = Made(lens, 1, d, 64, dtype, seed=11)
+    q, kn, vn = (c.rand(len(lens), m, h, d).to(KIND[dtype]) for h in (hq, 1, 1))
+    scale = d ** -0.5
+    for nodes in (False, True):
+        mask = tree_mask(len(lens), m, 2) if nodes else None
+        out, lse = c.cache.attend(q, kn if nodes else None, vn if nodes else None, mask=mask)
+        for s, n in enumerate(lens):
+            k, v, _ = c.dense(s, 0)
+            sees = np.ones((m, n), bool)
+            if nodes:
+                k, v = (np.concatenate([x, f64(y, dtype)[s, :, 0]]) for x, y in ((k, kn), (v, vn)))
+                sees = np.concatenate([sees, sees_of(mask, s, m, m)], 1)
+            for h in range(hq):
+                row = f64(q, dtype)[s, :, h]
+                want, wl = O.attend(row, k, v, sees, scale)
+                got, gl = f64(out, dtype)[s, :, h], lse[s, :, h].cpu().numpy().astype(np.float64)
+                if len(k) == 0:
+                    assert np.all(got == 0) and np.all(gl == -np.inf)
+                    continue
+                e, vmax = score_error(row, k, d, scale, True), np.abs(v).max()
+                assert np.all(np.abs(gl - wl) <= e + 2.0 ** -22 * (np.abs(wl) + 1)), (s, h, np.abs(gl - wl).max(), e)
+                assert np.all(np.abs(got - want) <= UNIT[dtype] * np.abs(want) + (2 * e + 2 * 2.0 ** -11) * vmax + len(k) * 2.0 ** -32 * 2 * vmax)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("m,hq", [(1, 8), (2, 8), (20, 8)])
+def test_a_long_sequence(m, hq, dtype):
+    """131,085 slots.  Roundings of different slots are independent, so eight standard deviations of
+    their sum are 8 |p| (2-norm) times one slot's: R 2^-11 and 2^-11 max |v| for the operands, 2 e max |v| for
+    the score.  Beside them 2^-31 R for each slot (operands below f16's normal range) and 2^-23 R for
+    each of 64 sums that the tensor cores cut off."""
+    n, d = 131085, 128
+    c = Made([n], 1, d, 64, dtype, seed=8, v_gain=1.0)
+    q = (c.rand(1, m, hq, d) * 2).to(KIND[dtype])
+    out, lse = c.cache.attend(q)
+    k, v, _ = c.dense(0, 0)
+    vmax, rng = np.abs(v).max(), np.ptp(v.reshape(-1, 64), -1).max()
+    for h in range(hq):
+        row = f64(q, dtype)[0, :, h]
+        x = (row @ k.T) * d ** -0.5
+        p = np.exp(x - x.max(-1, keepdims=True))
+        total = p.sum(-1, keepdims=True)
+        wl = np.log(total[:, 0]) + x.max(-1)
+        p /= total
+        want, got, gl = p @ v, f64(out, dtype)[0, :, h], lse[0, :, h].cpu().numpy().astype(np.float64)
+        e = score_error(row, k, d, d ** -0.5, m * hq > 16)
+        norm = np.sqrt((p ** 2).sum(-1, keepdims=True))
+        tol = UNIT[dtype] * np.abs(want) + 8 * norm * (2.0 ** -11 * (rng + vmax) + 2 * e * vmax) + n * 2.0 ** -31 * rng + 64 * 2.0 ** -23 * rng
+        assert np.all(np.abs(got - want) <= tol), (h, np.abs(got - want).max(), tol.min(), np.abs(want).max())
+        assert np.all(np.abs(gl - wl) <= e + 2.0 ** -22 * (np.abs(wl) + 1))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("m,hq,hkv", [(16, 1, 1), (8, 2, 1), (5, 3, 1), (9, 1, 1), (16, 2, 2), (17, 1, 1), (3, 12, 2)])
+def test_rows_up_to_the_change_of_kernels(m, hq, hkv, dtype):
+    c = Made([0, 1, 63, 200, 900], hkv, 128, 64, dtype)
+    q, kn, vn = (c.rand(5, m, h, 128).to(KIND[dtype]) for h in (hq, hkv, hkv))
+    mask = tree_mask(5, m, 6)
+    n_new = torch.tensor([m, 0, m - 1, 1, m], dtype=torch.int32, device="cuda")
+    out, lse = c.cache.attend(q, kn, vn, mask=mask, n_new=n_new)
+    check_attend(c, q, kn, vn, mask, n_new, out, lse, 128 ** -0.5)
+
+
+@pytest.mark.parametrize("lens", [[700, 1300, 129], [4000]])
+def test_f16_trees_over_long_heads(lens):
+    c = Made(lens, 2, 128, 32, "f16")
+    n = len(lens)
+    q, kn, vn = (c.rand(n, 60, h, 128).half() for h in (8, 2, 2))
+    mask = tree_mask(n, 60, 6)
+    out, lse = c.cache.attend(q, kn, vn, mask=mask)
+    check_attend(c, q, kn, vn, mask, None, out, lse, 128 ** -0.5)
+
+
+@pytest.mark.parametrize("n_seq", [300, 1024])
+def test_as_many_sequences_as_there_may_be(n_seq):
+    """attend (both kernels), weigh, append and evict over all of them."""
+    lens = [(7 * i) % 23 for i in range(n_seq)]
+    c = Made(lens, 1, 64, 16, "bf16", max_pages=2)
+    for m, hq in ((1, 2), (6, 4)):
+        q, kn, vn = (c.rand(n_seq, m, h, 64).bfloat16() for h in (hq, 1, 1))
+        out, lse = c.cache.attend(q, kn, vn)
+        check_attend(c, q, kn, vn, None, None, out, lse, 64 ** -0.5)
+        c.weight.zero_()
+        nodes = c.cache.weigh(q, lse, kn)
+        page, hold = c.table.clamp(min=0).long(), (c.table >= 0)
+        got = (c.weight[page, 0].sum(-1) * hold).sum(-1) + nodes.sum((1, 2))
+        assert torch.allclose(got, torch.full_like(got, float(m * hq)), rtol=1e-4)    # a softmax adds up to 1
+    weight = c.weight[:, 0].cpu().numpy()
+    table = c.table.cpu().numpy()
+    c.cache.evict(9, sink=1, recent=2)
+    after = c.weight[:, 0].cpu().numpy()
+    assert c.seq_len.tolist() == [min(n, 9) for n in lens]
+    for s, n in enumerate(lens):
+        if n > 9:
+            at = np.arange(n)
+            w = weight[table[s, at // 16], at % 16]
+            src = O.evict(w, at, n, 9, 1, 2)
+            assert np.array_equal(after[table[s, at[:9] // 16], at[:9] % 16], w[src])
+    k = c.rand(n_seq, 2, 1, 64).bfloat16()
+    before = c.seq_len.tolist()
+    c.cache.append(k, k, n_new=torch.arange(n_seq, device="cuda").int() % 3)
+    room = [16 if 0 < n <= 16 else 0 if n == 0 else 32 for n in lens]
+    lost = sum(max(0, b + i % 3 - r) for i, (b, r) in enumerate(zip(before, room)))
+    assert c.seq_len.tolist() == [b + i % 3 for i, b in enumerate(before)] and c.cache.dropped() == lost
+
+
+@pytest.mark.parametrize("m,hq", [(1, 4), (3, 4), (30, 4)])
+def test_a_negative_scale_is_the_queries_sign(m, hq):
+    c = Made([300, 0, 40], 1, 128, 64)
+    q, kn, vn = (c.rand(3, m, h, 128).bfloat16() for h in (hq, 1, 1))
+    a, b = c.cache.attend(q, kn, vn, scale=-0.1), c.cache.attend(-q, kn, vn, scale=0.1)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    c.weight.zero_()
+    na = c.cache.weigh(q, a[1], kn, scale=-0.1)
+    wa = c.weight.clone()
+    c.weight.zero_()
+    nb = c.cache.weigh(-q, b[1], kn, scale=0.1)
+    assert torch.equal(na, nb) and torch.equal(wa, c.weight) and float(wa.sum()) > 0
