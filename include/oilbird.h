@@ -631,7 +631,8 @@ const char* oilbird_query_static_error(void);   /* why the last call was rejecte
  *   pages       [n_pages, n_kv_heads] blocks of oilbird_kv_block_bytes(head_dim, page_size)
  *   weight      fp32 accumulated attention weight of each slot;  pos: its position
  *   page_table  pages of each sequence in order; an entry that names no page (negative, or
- *               n_pages and above) is a page without content: nothing is read or stored there
+ *               n_pages and above) is a page without content: nothing is read or stored there.
+ *               max_pages * page_size at most 2^31 - 1024
  *   seq_len     slots each sequence holds;  n_pos: positions it has seen (append and evict
  *               update them in stream order)
  *   workspace   zeroed once by the caller; one stream at a time

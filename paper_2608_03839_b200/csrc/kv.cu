@@ -34,8 +34,9 @@ static int check_cache(const oilbird_kv_cache* c, KvView* v) {
   if (c->n_seq < 1 || c->n_seq > OILBIRD_KV_MAX_SEQ) return kv_refuse("n_seq: 1 to OILBIRD_KV_MAX_SEQ");
   if (c->n_kv_heads < 1 || c->n_kv_heads > 1024) return kv_refuse("n_kv_heads: 1 to 1024");
   if (c->n_pages < 1 || c->n_pages > 2147483647LL) return kv_refuse("n_pages: 1 to 2^31 - 1");
-  if (c->max_pages < 1 || (int64_t)c->max_pages * c->page_size > 2147483647LL)
-    return kv_refuse("max_pages: at least 1, and max_pages * page_size below 2^31");
+  // (a tile's worth below 2^31, so that slots and tiles can be counted in 32 bits)
+  if (c->max_pages < 1 || (int64_t)c->max_pages * c->page_size > 2147483648LL - 1024)
+    return kv_refuse("max_pages: at least 1, and max_pages * page_size at most 2^31 - 1024");
   if (!c->pages || !c->weight || !c->pos || !c->page_table || !c->seq_len || !c->n_pos || !c->workspace)
     return kv_refuse("an array of the cache is missing");
   if (!aligned(c->pages, 16) || !aligned(c->workspace, 16)) return kv_refuse("pages and workspace: 16-byte aligned");

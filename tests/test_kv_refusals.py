@@ -51,3 +51,14 @@ def test_rows_and_masks(cache):
     refused(attend(mask=AT + 4, stride=4), "mask")
     refused(attend(mask=AT, stride=3), "mask")
     refused(attend(mask=AT, stride=-4), "mask")
+
+
+@pytest.mark.parametrize("page", [16, 32, 64])
+def test_sequences_end_a_tile_before_two_to_the_31(cache, page):
+    """The last tile's slots, rounded up to whole tiles, still count in 32 bits.  (A budget of zero is
+    refused next, so that nothing goes further.)"""
+    L, ref = B.lib(), ctypes.byref(cache)
+    cache.page_size = page
+    for slots, text in ((2 ** 31 - page, "max_pages"), (2 ** 31 - 1024 + page, "max_pages"), (2 ** 31 - 1024, "budget")):
+        cache.max_pages = slots // page
+        refused(L.oilbird_kv_evict(ref, 0, 0, 0, None), text)
