@@ -632,7 +632,10 @@ const char* oilbird_query_static_error(void);   /* why the last call was rejecte
  *   weight      fp32 accumulated attention weight of each slot;  pos: its position
  *   page_table  pages of each sequence in order; an entry that names no page (negative, or
  *               n_pages and above) is a page without content: nothing is read or stored there.
- *               max_pages * page_size at most 2^31 - 1024
+ *               max_pages * page_size at most 2^31 - 1024.  attend() and read() take pages that
+ *               several sequences name; weigh() adds to a shared slot for each of them, in an order
+ *               that is not fixed; append() and evict() need the pages they change to be one
+ *               sequence's
  *   seq_len     slots each sequence holds;  n_pos: positions it has seen (append and evict
  *               update them in stream order)
  *   workspace   zeroed once by the caller; one stream at a time

@@ -6,7 +6,8 @@
 // The keys' half of the cache is read once, with the products and the layout of the attention
 // kernel (exact codes as f16 operands, scale and offset in fp32); what follows the scores is
 // one exponential each and a sum over the rows.  A slot's sum is formed by one warp in a fixed
-// order and added once, so the result does not depend on which block ran when.  The rows that
+// order and added once, so the result does not depend on which block ran when (where every page is one
+// sequence's).  The rows that
 // take part are gathered per item, so a tree of sixty nodes of which five were accepted costs
 // five; their operands lie in shared memory and every tile is multiplied with all of them.
 //
@@ -234,7 +235,8 @@ kv_weigh_kernel(const KvView c, const KvWeighArgs a, int row_tiles) {
           if (n_tiles && (valid >> sl & 1)) {
             const int slot = slot0 + sl, page = 1 << c.page_shift;
             const int p = c.table[(size_t)s * c.max_pages + (slot >> c.page_shift)];
-            // nobody else adds to this slot in this launch: the result has no order to depend on
+            // nobody else adds to this slot in this launch (unless sequences share the page): the
+            // result has no order to depend on
             atomicAdd(c.weight + ((size_t)p * c.n_kv + head) * page + (slot & (page - 1)), mine);
           }
         }
