@@ -31,11 +31,11 @@
 // their order, whichever block that is.
 //
 // Measured, with 8 key/value heads of 128: 64 sequences of 4,096 to 8,192 slots, 444 MB of cache
-// under 32 query heads, in 108 us (4.1 TB/s; 68 us at the copy rate); 131,085 slots under 64
-// query heads in 44 us (23 us at the copy rate); 517 slots in 10 us.  The long ones are bound by
-// instructions (taking codes apart, 32 lanes' worth of exponentials and scales for each slot and
-// row) at half the issue slots, unevenly between the two blocks of an SM; the short one by the
-// latency of one tile, one join and one launch.
+// under 32 query heads, in 107 us (4.2 TB/s; 68 us at the copy rate); 131,085 slots under 64
+// query heads in 44 us (23 us at the copy rate); 517 slots in 10 us.  The long ones fill half the
+// issue slots (taking codes apart, 32 lanes' worth of exponentials and scales for each slot and
+// row) with twelve warps an SM that wait for their own results in between, unevenly between the two
+// blocks of an SM; the short one is bound by the latency of one tile, one join and one launch.
 #include "kv.cuh"
 
 namespace oilbird {
@@ -45,9 +45,15 @@ namespace oilbird {
 // with them, so that a single buffer of each keeps half a tile per warp in flight.
 // Eight rows leave registers (168 a thread) for twelve warps an SM, sixteen rows for eight.
 //
-// More rows go to kv_tree.cu, whose tensor core products cost the same for 17 rows as for 128:
-// 21 rows of 64 channels over 777 slots take 17.2 us there and 18.6 us as two blocks of 16 rows
-// here, which would read the cache twice; with 16 rows or fewer one reading is enough.
+// More rows go to kv_tree.cu, whose tensor core products cost the same for 17 rows as for 128.
+// With 16 rows or fewer one reading of the cache is enough here.  Measured beyond that, there
+// against as many calls of 16 rows here as it takes, 8 heads of 128 channels, f16 (bf16 within 2 %):
+//   slots          17..32 rows          33..48 rows          49..64 rows
+//   8 x 4,096      66 us against 58     66 against 87        67 against 116
+//   65,536         87 against 86        87 against 129       87 against 172
+//   32 x 8,192     366 against 209      367 against 313      367 against 417
+// and 21 rows of 64 channels over 777 slots 17.2 us against 18.6.  So up to 32 rows over long
+// sequences, where the GPU is full, two readings here would be faster; the change stands at 16.
 constexpr int kFewRows = 16;
 // Probability times value scale is an f16 operand, in units in which the largest scale lies below
 // 2^7: with probabilities up to 2^8 f16 just holds it, and small probabilities keep their bits.

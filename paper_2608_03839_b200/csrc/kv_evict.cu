@@ -16,8 +16,8 @@
 // over the words' prefix sums (in whichever block's shared memory it lies), and the moves are
 // dealt out to all blocks, eight lanes each.
 //
-// Measured, with 8 heads of 128: 8 sequences of 4,096 to 32,768 slots cut to 4,096 in 72 us
-// (selection 28 us, moves 27 us: rows of 32-byte pieces, at 60 % of the copy rate);
+// Measured, with 8 heads of 128: 8 sequences of 4,096 to 32,768 slots cut to 4,096 in 66 us
+// (9.5 us at the copy rate; selection 28 us, moves 27 us: rows of 32-byte pieces);
 // 16 sequences up to seven slots over a budget of 1,024 in 15 us: a launch, one reading, and a
 // chain of barriers.
 #include <cooperative_groups.h>

@@ -7,7 +7,7 @@
 // four slots at a time.  All loads of a warp are on their way before the first is used.
 //
 // Measured, with 8 heads of 128: 4 prompts of 2,048 to 4,096 rows (12,800 in all) are stored in
-// 31 us (68 MB, 2.2 TB/s; bound by the instructions of minima, quotients and packing) and read
+// 32 us (68 MB, 2.1 TB/s; bound by the instructions of minima, quotients and packing) and read
 // in 16 us (with the zeros behind the shorter ones 85 MB, 5.3 TB/s: memory); 16 paths of four to
 // seven rows in 7 and 4.6 us: latency of a launch and three dependent loads.
 //

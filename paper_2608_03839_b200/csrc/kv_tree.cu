@@ -1,5 +1,5 @@
-// Attention over the 4-bit cache for many query rows per key/value head (whole draft trees,
-// prompt chunks): tensor cores with accumulators in TMEM.
+// Attention over the 4-bit cache for many query rows per key/value head (whole draft trees):
+// tensor cores with accumulators in TMEM.
 //
 // The formulas are those of kv_attend.cu.  With 128 or 256 rows on a tile of 128 slots the
 // products decide (4 D flops for each row and slot), so keys and values are turned into f16 once per tile
@@ -42,8 +42,9 @@
 // read back in microseconds and one block would not.
 //
 // Measured, with 60-node trees under 32 query heads, 8 key/value heads of 128: 65,541 slots in
-// 99 us (64.4 GFLOP at 650 TFLOP/s; 39 us at the measured bf16 rate), 8 sequences of 2,048 to
-// 4,096 slots in 73 us with the join (11 us).  A tile takes about 5,700 cycles, of which the
+// 102 us (64.4 GFLOP at 630 TFLOP/s; 39 us at the measured bf16 rate), 8 sequences of 2,048 to
+// 4,096 slots in 75 us with the join (59 and 25 us each by itself with cold
+// caches).  The kernel spills some 200 bytes a thread.  A tile takes about 5,700 cycles, of which the
 // exponentials (2,048), the products (3,072 with both parts of the keys) and the shared
 // memory they read (3,300) each fill about half: what bounds it is their chain - products,
 // exponentials, products - with two groups to overlap and one place for the keys.
