@@ -1105,10 +1105,10 @@ class KVCache:
         """Cut every sequence to `budget` slots per head: positions below sink and the newest
         `recent` (None: half the budget, as far as sink leaves room) stay, then the slots of
         greatest weight."""
-        if recent is None:
-            recent = max(0, min(budget // 2, budget - sink))
-        _kv_check(self._L.oilbird_kv_evict(self._ref, int(budget), int(sink), int(recent),
-                                           self._stream(stream)), "oilbird_kv_evict")
+        # (the C call takes 32 bits, and a number beyond them would come out as another)
+        budget, sink = (max(-1, min(int(x), 2 ** 31 - 1)) for x in (budget, sink))
+        recent = max(0, min(budget // 2, budget - sink)) if recent is None else max(-1, min(int(recent), 2 ** 31 - 1))
+        _kv_check(self._L.oilbird_kv_evict(self._ref, budget, sink, recent, self._stream(stream)), "oilbird_kv_evict")
 
     def dropped(self, stream=None) -> int:
         """Rows append() could not store so far (synchronises)."""

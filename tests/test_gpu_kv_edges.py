@@ -501,3 +501,18 @@ def test_a_negative_scale_is_the_queries_sign(m, hq):
     c.weight.zero_()
     nb = c.cache.weigh(-q, b[1], kn, scale=0.1)
     assert torch.equal(na, nb) and torch.equal(wa, c.weight) and float(wa.sum()) > 0
+
+
+# ------------------------------------------------------------------ large budgets ----
+
+def test_budgets_beyond_32_bits_cut_nothing():
+    c = Made([40, 7], 1, 64, 16)
+    for budget in (2 ** 31 - 1, 2 ** 31, 2 ** 32 + 5, 2 ** 40):
+        c.cache.evict(budget)
+        c.cache.evict(budget, sink=2 ** 30, recent=3)
+        assert c.seq_len.tolist() == [40, 7]
+    for sink, recent in ((2 ** 32, 0), (0, 2 ** 32), (-2 ** 32, 0)):
+        with pytest.raises(B.OilbirdError):
+            c.cache.evict(30, sink=sink, recent=recent)
+    c.cache.evict(8)
+    assert c.seq_len.tolist() == [8, 7]
