@@ -738,6 +738,64 @@ int oilbird_kv_evict(const oilbird_kv_cache* cache, int32_t budget, int32_t sink
 int oilbird_kv_status(const oilbird_kv_cache* cache, int64_t* dropped, void* cuda_stream);
 const char* oilbird_kv_last_error(void);
 
+/*
+ * Whole prompts (not in the paper, whose verifier is a given): what happens to a prompt before its
+ * keys and values join the 4-bit cache.  attend() is its attention over itself, or of its next piece over
+ * all of it so far; weigh() is the attention weight that its keys receive, which append() takes as the
+ * slots' first weights and evict() goes by.  Keys and values are the 16-bit rows that append() stores.
+ *
+ * Each side (query rows; key and value rows) is packed or padded:
+ *   first   dev [n_seq + 1]: packed; sequence s has rows first[s] .. first[s + 1) of an array of `rows`
+ *           rows (its row views have no use for a sequence stride); rows of no sequence are neither
+ *           looked at nor written
+ *   count   dev [n_seq]: padded (first is NULL); sequence s has the first count[s] of `rows` rows of
+ *           its own (NULL: all of them)
+ * Offsets and counts that leave the array are cut to it.  Sequences must not overlap in what is written.
+ * With n query rows and c key rows, row i of a sequence sees the keys j <= i + c - n: its query rows are
+ * its last ones.  Query head h reads key/value head h / (n_q_heads / n_kv_heads).
+ * head_dim 64 or 128, bf16 or f16, up to OILBIRD_KV_MAX_SEQ sequences and OILBIRD_KV_MAX_GROUP query
+ * heads a key head.  Nothing synchronises (but status()) or allocates; there is no workspace, so calls
+ * on different streams do not meet; the calls can be captured in a CUDA graph after the first call on
+ * the device.  Refusals return OILBIRD_EINVAL and leave the reason in oilbird_prompt_last_error().
+ */
+typedef struct {
+  const int32_t* first;
+  const int32_t* count;
+  int64_t rows;                /* at most 2^31 - 1024                                     */
+} oilbird_prompt_side;
+typedef struct {
+  oilbird_prompt_side q, k;    /* k: keys and values                                      */
+  int32_t n_seq, n_q_heads, n_kv_heads, head_dim;
+  int32_t dtype;               /* OILBIRD_KV_BF16 or OILBIRD_KV_F16                       */
+  int32_t device;              /* CUDA ordinal                                            */
+} oilbird_prompt;
+/*
+ * out (like q) = softmax(scale * q.k) v over the keys each row sees; lse (dev fp32, may be NULL): the
+ * natural logarithm of the row's sum of exponentials; lse_strides (host): its strides in elements for
+ * sequence, row and head, NULL: contiguous [n_seq, rows, n_q_heads] or [rows, n_q_heads].  A row that
+ * sees nothing gets out = 0 and lse = -inf, and so do padded rows behind count[s].  Keys and values that a
+ * row does not see do not reach it, whatever they hold.  out overlaps no input.
+ */
+int oilbird_prompt_attend(const oilbird_prompt* prompt, const oilbird_kv_rows* q, const oilbird_kv_rows* k,
+                          const oilbird_kv_rows* v, float scale, const oilbird_kv_rows* out, float* lse,
+                          const int64_t* lse_strides, void* cuda_stream);
+/*
+ * weight (dev fp32 [n_seq, n_kv_heads, k.rows], packed [n_kv_heads, k.rows], written) = sum over the query
+ * rows i that see the key and the head's query heads of row_weight[i] * exp(scale * q.k - lse), with
+ * attend()'s arguments and its lse.  row_weight: dev fp32 [n_seq, q.rows] or [q.rows], NULL: 1; rows
+ * with weight 0 do not count, whatever they hold, and long runs of them cost next to nothing.  Padded keys
+ * behind count[s] get 0.
+ */
+int oilbird_prompt_weigh(const oilbird_prompt* prompt, const oilbird_kv_rows* q, const float* lse,
+                         const int64_t* lse_strides, const oilbird_kv_rows* k, const float* row_weight,
+                         float scale, float* weight, void* cuda_stream);
+/* Synchronises cuda_stream; OILBIRD_ESTALL if a bounded device-side wait of a prompt call on the device
+ * gave up since the last status() (which forgets it). */
+int oilbird_prompt_status(int32_t device, void* cuda_stream);
+/* How long those waits may take, in nanoseconds (0: two seconds); holds for the calls behind it. */
+int oilbird_prompt_set_wait_limit(int32_t device, uint64_t limit_ns, void* cuda_stream);
+const char* oilbird_prompt_last_error(void);
+
 const char* oilbird_strerror(int code);
 const char* oilbird_last_cuda_error(void);    /* text of the last failing CUDA call      */
 

@@ -184,6 +184,10 @@ SYMBOLS = {
     "oilbird_kv_evict": (ctypes.c_int, [ctypes.POINTER(CKVCache), _i32, _i32, _i32, _vp]),
     "oilbird_kv_status": (ctypes.c_int, [ctypes.POINTER(CKVCache), ctypes.POINTER(_i64), _vp]),
     "oilbird_kv_last_error": (ctypes.c_char_p, []),
+    "oilbird_prompt_attend": (ctypes.c_int, [_vp, _vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp]),
+    "oilbird_prompt_status": (ctypes.c_int, [_i32, _vp]),
+    "oilbird_prompt_set_wait_limit": (ctypes.c_int, [_i32, _u64, _vp]),
+    "oilbird_prompt_last_error": (ctypes.c_char_p, []),
     "oilbird_query_static": (ctypes.c_int, [ctypes.POINTER(StaticPool), _vp, _i32,
                                             ctypes.POINTER(CQueryParams),
                                             ctypes.POINTER(CQueryOut), _vp]),
@@ -1116,3 +1120,113 @@ class KVCache:
         _kv_check(self._L.oilbird_kv_status(self._ref, ctypes.byref(n), self._stream(stream)),
                   "oilbird_kv_status")
         return int(n.value)
+
+
+# ------------------------------------------------------------------ whole prompts ----
+_PROMPT = ctypes.c_int64 * 9         # oilbird_prompt: two sides of three words, six 32-bit numbers
+
+
+def _prompt_check(rc: int, where: str) -> None:
+    if rc != OK:
+        err = OilbirdError(rc, where)
+        err.args = (err.args[0] + ": " + lib().oilbird_prompt_last_error().decode(),)
+        raise err
+
+
+class _Prompt:
+    """Checked arguments of a prompt call: the C view of both sides, and of every tensor given."""
+
+    def __init__(self, q, k, first, n_new, first_k, n_k):
+        self.packed, self.packed_k = q.dim() == 3, k.dim() == 3
+        if (not self.packed and q.dim() != 4) or (not self.packed_k and k.dim() != 4):
+            raise AssertionError("q and k: [rows, heads, head_dim] packed, [n_seq, rows, heads, head_dim] padded")
+        if q.dtype not in _KV_DTYPES or not q.is_cuda:
+            raise AssertionError("q: a bf16 or f16 tensor on a CUDA device; there is no CPU fallback")
+        self.dtype, self.dev, self.index = q.dtype, q.device, q.get_device()
+        if self.packed and first is None or not self.packed and first is not None:
+            raise AssertionError("first goes with packed q [rows, heads, head_dim], and only with it")
+        if first_k is None and self.packed_k:
+            first_k = first
+        if self.packed_k != (first_k is not None):
+            raise AssertionError("first_k (or first) goes with packed k, and only with it")
+        if self.packed and n_new is not None or self.packed_k and n_k is not None:
+            raise AssertionError("n_new and n_k count the rows of padded sequences")
+        self.n_seq = first.shape[0] - 1 if self.packed else q.shape[0]
+        self.rows, self.heads, self.d = q.shape[-3:]
+        self.rows_k, self.kv_heads = k.shape[-3:-1]
+        if n_k is None and not self.packed and not self.packed_k and self.rows_k == self.rows:
+            n_k = n_new                  # a prompt over itself
+        self.lead = (self.rows,) if self.packed else (self.n_seq, self.rows)
+        self.lead_k = (self.rows_k,) if self.packed_k else (self.n_seq, self.rows_k)
+        offsets, counts = (self.n_seq + 1,), (self.n_seq,)
+        self.c = _PROMPT(self.vec(first, torch.int32, offsets) or 0, self.vec(n_new, torch.int32, counts) or 0, self.rows,
+                         self.vec(first_k, torch.int32, offsets) or 0, self.vec(n_k, torch.int32, counts) or 0, self.rows_k,
+                         self.n_seq | self.heads << 32, self.kv_heads | self.d << 32,
+                         _KV_DTYPES[self.dtype] | self.index << 32)
+
+    def vec(self, t, dtype, shape):
+        """Pointer of an optional contiguous tensor of that type and shape."""
+        if t is None:
+            return None
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != self.index or not t.is_contiguous():
+            raise AssertionError(f"a contiguous {dtype} tensor {list(shape)} on {self.dev}")
+        return t.data_ptr()
+
+    def view(self, t, lead, heads):
+        """The C view of a tensor [*lead, heads, head_dim] (any strides but the last)."""
+        if t.dtype is self.dtype and t.shape == (*lead, heads, self.d) and t.get_device() == self.index:
+            if t.requires_grad and torch.is_grad_enabled():
+                raise RuntimeError("prompt calls have no backward pass: detach the tensor, or call under torch.no_grad()")
+            stride = t.stride()
+            if stride[-1] == 1 or self.d == 1:
+                return _KV_ROWS(t.data_ptr(), stride[0] if len(lead) == 2 else 0, *stride[-3:-1])
+        raise AssertionError(f"a {self.dtype} tensor [{', '.join(map(str, lead))}, {heads}, {self.d}] on {self.dev} "
+                             "with contiguous channels")
+
+    def lse(self, t):
+        """Pointer and strides of an fp32 tensor [*lead, n_q_heads]."""
+        if t.dtype is not torch.float32 or t.shape != (*self.lead, self.heads) or t.get_device() != self.index:
+            raise AssertionError(f"an fp32 tensor [{', '.join(map(str, self.lead))}, {self.heads}] on {self.dev}")
+        if t.is_contiguous():
+            return t.data_ptr(), None
+        return t.data_ptr(), _KV_STRIDES(t.stride(0) if len(self.lead) == 2 else 0, *t.stride()[-2:])
+
+    def stream(self, stream) -> int:
+        return _raw_stream(self.index) if stream is None else stream.cuda_stream
+
+
+def prompt_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, first: torch.Tensor | None = None,
+                  n_new: torch.Tensor | None = None, first_k: torch.Tensor | None = None,
+                  n_k: torch.Tensor | None = None, scale: float | None = None, out: torch.Tensor | None = None,
+                  lse: torch.Tensor | None = None, stream=None):
+    """Causal attention over whole prompts (oilbird_prompt_attend).  Packed: q [rows, n_q_heads, head_dim], k and v
+    [rows_k, n_kv_heads, head_dim], first and first_k (int32 [n_seq + 1]; first_k None: first) say where
+    each sequence begins.  Padded: q [n_seq, rows, n_q_heads, head_dim], k and v likewise, n_new and n_k
+    (int32 [n_seq]; None: all rows, n_k: n_new where both have as many rows) count each sequence's rows.
+    The query rows are the last of their sequence's keys.  scale: None for 1 / sqrt(head_dim).
+    Returns (out, lse): out like q, lse fp32 [..., n_q_heads] (natural logarithm).  Packed rows of no sequence
+    are not written."""
+    p = _Prompt(q, k, first, n_new, first_k, n_k)
+    if out is None:
+        out = ALLOC((*p.lead, p.heads, p.d), p.dtype, p.dev)
+    if lse is None:
+        lse = ALLOC((*p.lead, p.heads), torch.float32, p.dev)
+    _prompt_check(lib().oilbird_prompt_attend(
+        p.c, p.view(q, p.lead, p.heads), p.view(k, p.lead_k, p.kv_heads), p.view(v, p.lead_k, p.kv_heads),
+        p.d ** -0.5 if scale is None else scale, p.view(out, p.lead, p.heads), *p.lse(lse), p.stream(stream)),
+        "oilbird_prompt_attend")
+    return out, lse
+
+
+def prompt_status(device: int = 0, stream=None) -> int:
+    """OK, or ESTALL if a bounded wait of a prompt call gave up since the last status (synchronises)."""
+    rc = lib().oilbird_prompt_status(device, _raw_stream(device) if stream is None else stream.cuda_stream)
+    if rc != ESTALL:
+        _prompt_check(rc, "oilbird_prompt_status")
+    return rc
+
+
+def prompt_set_wait_limit(limit_ns: int, device: int = 0, stream=None) -> None:
+    """How long the device-side waits of prompt calls may take (0: two seconds)."""
+    _prompt_check(lib().oilbird_prompt_set_wait_limit(device, limit_ns, _raw_stream(device) if stream is None
+                                                      else stream.cuda_stream), "oilbird_prompt_set_wait_limit")

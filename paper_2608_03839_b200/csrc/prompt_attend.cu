@@ -1,0 +1,560 @@
+// Attention over whole prompts: causal, grouped query heads, sequences of different lengths, on the
+// tensor cores with accumulators in TMEM.
+//
+//   out_i = sum_j exp(x_ij - lse_i) v_j,  lse_i = ln sum_j exp x_ij,  x_ij = scale q_i.k_j,  j <= i + c - n
+//
+// One pass over the keys with a running maximum.  A block takes items of 256 query rows of one key
+// head, in two groups A and B of 128.  `pack` query heads that share the key head lie side by side, so a
+// group is 128 / pack tokens: every tile of keys serves all of them, and fewer keys lie beyond the
+// diagonal.  Warps:
+//   0-3, 4-7   softmax of A and of B, one row a thread: scores from TMEM, maximum, exponentials, and
+//              the probabilities in 16 bits back over the scores
+//   8          loads: queries, then keys and values in turn into a ring, by tensor maps
+//   9          issues the products S = Q K^T and O += P V (P from TMEM)
+// While A's scores go through the exponentials the tensor core works for B, and the other way round.
+//
+// Numbers.  Scores, maxima, sums and accumulators are fp32.  Probabilities are rounded to the inputs'
+// type, as the product wants both operands alike (2^-9 of each in bf16, 2^-12 in f16); the sum takes
+// them unrounded.  m follows the row's maximum only when that has grown by 2^8 (the accumulators are
+// rescaled in TMEM then), so p reaches 2^8; f16 takes them 2^7 higher, where its range ends, as
+// what lies 17 below the maximum (in exp's units) would otherwise be rounded to nothing.
+//
+// Values that are not finite.  A masked key's probability is 0, and 0 times an infinity would reach
+// every row of the tile: a row whose output is not finite looks whether such a value lies among the keys of
+// its tiles that it does not see, and is then computed again by its warp from what it does see.
+//
+// Work.  Items by falling number of key tiles, so that the last ones are the short ones; block b takes
+// b, 2G-1-b, 2G+b, ... of G blocks.  The list is not stored: the loading warp finds an item by its number (a
+// search over the number of tiles, then over the sequences) while the one before it is worked on.
+//
+// Every wait is bounded (two seconds unless set otherwise): a wait that runs out raises `stalled`, all
+// roles leave, TMEM is freed.
+#include "prompt.cuh"
+#include "tensor.cuh"
+
+namespace oilbird {
+
+namespace {
+
+constexpr int kPaThreads = 384, kPaLoader = 8, kPaIssuer = 9;
+// registers a thread: launched with 168; the three warpgroups' shares add up to 3 x 168
+constexpr int kPaSoftRegs = 224, kPaRestRegs = 56;
+static_assert(2 * kPaSoftRegs + kPaRestRegs <= 3 * 168, "more registers than the block was launched with");
+constexpr float kPaLn2 = 0.6931471805599453f;
+constexpr int kPaSlack = 8;
+
+struct PaItem {
+  int s, tok, head, q_head;          // sequence, first token, key head, first query head
+  int n, c, q0, k0;
+  int tiles[2];                      // of A and of B
+  int live;                          // 0: no item is left
+};
+struct PaShared {
+  uint64_t full[16], free[16], qfull, qfree, sfull[2], pfull[2], ofull[2], item_full[2], item_free[2];
+  PaItem item[2];
+  uint32_t tmem;
+  int gave_up;
+};
+
+template <int D>
+struct Pa {
+  static constexpr int kBlocks = D / 64, kMat = kBlocks * kPrTile * 128;      // one tile of 128 rows
+  static constexpr int kStages = D == 128 ? 4 : 8;
+  static constexpr int kBytes = 1024 + (2 + kStages) * kMat + (int)sizeof(PaShared) + 16 + (int)sizeof(PromptList);
+  static_assert(kBytes <= 227 * 1024, "shared memory");
+};
+
+// Tiles (of `span` tokens) of a sequence whose last row sees more than `keys` keys.
+__device__ __forceinline__ int tiles_beyond(int n, int c, int span, long long keys) {
+  if (c <= keys) return 0;
+  const long long d = keys - ((long long)c - n);
+  const int tiles = (n + span - 1) / span, from = d > 0 ? (int)(d / span) : 0;
+  return max(tiles - from, 0);
+}
+
+struct PaFinder {
+  const PromptList* l;
+  int n_seq, span, padded_rows;      // padded_rows: rows to write for every sequence (0: packed)
+  int level;                         // key tiles of the last item found: the next one has no more
+  __device__ __forceinline__ int tiles_at(int s, int level) const {
+    if (level == 0) return padded_rows ? (padded_rows + span - 1) / span : (l->n[s] + span - 1) / span;
+    return tiles_beyond(l->n[s], l->c[s], span, (long long)(level - 1) * kPrTile);
+  }
+  // items (of one head) with `level` key tiles or more
+  __device__ __forceinline__ long long count(int level, int lane) const {
+    long long v = 0;
+    for (int s = lane; s < n_seq; s += 32) v += tiles_at(s, level);
+    return warp_sum_i64(v);
+  }
+  // item number i: sequence and tile
+  __device__ __forceinline__ bool find(long long i, int lane, int& s_out, int& t_out) {
+    int lo = 0, hi = level;
+    if (count(0, lane) <= i) return false;
+    while (lo < hi) {                                    // the largest level with more than i items
+      const int mid = (lo + hi + 1) >> 1;
+      if (count(mid, lane) > i) lo = mid; else hi = mid - 1;
+    }
+    level = lo;
+    long long left = i - count(lo + 1, lane);            // place among the items of this level
+    for (int s0 = 0; s0 < n_seq; s0 += 32) {
+      const int s = s0 + lane;
+      const int above = s < n_seq ? tiles_at(s, lo + 1) : 0, all = s < n_seq ? tiles_at(s, lo) : 0;
+      int here = all - above, sum = here;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += y;
+      }
+      const unsigned hit = __ballot_sync(0xffffffffu, left < sum);
+      if (hit) {
+        const int at = __ffs(hit) - 1;
+        s_out = s0 + at;
+        t_out = (int)(left - __shfl_sync(0xffffffffu, sum - here, at));
+        const int there = (l->n[s_out] + span - 1) / span;
+        if (lo > 0) t_out += there - __shfl_sync(0xffffffffu, all, at);
+        else {                                           // rows in front that see nothing, then padding
+          const int seeing = __shfl_sync(0xffffffffu, above, at);
+          if (t_out >= there - seeing) t_out += seeing;
+        }
+        return true;
+      }
+      left -= __shfl_sync(0xffffffffu, sum, 31);
+    }
+    return false;
+  }
+};
+
+// One row again, by a whole warp, from the keys it sees: what masked values were kept out of.
+template <int D, bool kBf16>
+__device__ __noinline__ void row_again(const PromptArgs& a, const PaItem& it, int tok, int head, int vis, float m, float l, int lane) {
+  constexpr int E = D / 64;                              // pairs of channels a lane
+  const uint16_t* qp = a.q.at(a.qs.first ? 0 : it.s, it.q0 + tok, head);
+  float2 q[E], o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(qp + e * 64 + 2 * lane);
+    q[e] = make_float2(half_lo<kBf16>(w), half_hi<kBf16>(w));
+    o[e] = make_float2(0.f, 0.f);
+  }
+  const float f = a.negate ? -a.factor : a.factor, inv = 1.f / l;
+  for (int j = 0; j < vis; ++j) {
+    const uint16_t* kp = a.k.at(a.ks.first ? 0 : it.s, it.k0 + j, it.head);
+    const uint16_t* vp = a.v.at(a.ks.first ? 0 : it.s, it.k0 + j, it.head);
+    float x = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const uint32_t w = *reinterpret_cast<const uint32_t*>(kp + e * 64 + 2 * lane);
+      x = fmaf(q[e].x, half_lo<kBf16>(w), fmaf(q[e].y, half_hi<kBf16>(w), x));
+    }
+    const float p = exp2_approx(fmaf(warp_sum(x), f, -m)) * inv;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const uint32_t w = *reinterpret_cast<const uint32_t*>(vp + e * 64 + 2 * lane);
+      o[e].x = fmaf(p, half_lo<kBf16>(w), o[e].x);
+      o[e].y = fmaf(p, half_hi<kBf16>(w), o[e].y);
+    }
+  }
+  uint16_t* op = a.out + (a.qs.first ? 0 : it.s) * a.out_seq + (long long)(it.q0 + tok) * a.out_row + head * a.out_head;
+#pragma unroll
+  for (int e = 0; e < E; ++e) *reinterpret_cast<uint32_t*>(op + e * 64 + 2 * lane) = pack16<kBf16>(o[e].x, o[e].y);
+}
+
+// Whether a value of keys [from, to) of the item's sequence (as far as the array goes) is not finite; a warp.
+template <int D, bool kBf16>
+__device__ __noinline__ bool odd_values(const PromptArgs& a, const PaItem& it, int from, int to, int lane) {
+  constexpr uint32_t kInf = kBf16 ? 0x7f80u : 0x7c00u;
+  bool odd = false;
+  to = min(to, a.ks.rows - it.k0);
+#pragma unroll 4
+  for (int j = max(from, 0); j < to; ++j)
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) {
+      const uint32_t w = *reinterpret_cast<const uint32_t*>(a.v.at(a.ks.first ? 0 : it.s, it.k0 + j, it.head) + e * 64 + 2 * lane);
+      odd |= (w & kInf) == kInf || (w >> 16 & kInf) == kInf;
+    }
+  return __any_sync(0xffffffffu, odd);
+}
+
+}  // namespace
+
+template <int D, bool kBf16>
+__global__ void __launch_bounds__(kPaThreads, 1)
+prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
+                     const __grid_constant__ CUtensorMap v_map, const __grid_constant__ PromptArgs a) {
+  using P = Pa<D>;
+  constexpr float kRoom = kBf16 ? 0.f : 7.f;
+  extern __shared__ unsigned char raw_smem[];
+  unsigned char* smem = raw_smem + ((1024 - (kv_smem(raw_smem) & 1023)) & 1023);
+  unsigned char* qmat = smem;                            // A, then B: [block of 64 channels][row]
+  unsigned char* ring = smem + 2 * P::kMat;
+  PaShared& sh = *reinterpret_cast<PaShared*>(ring + P::kStages * P::kMat);
+  PromptList& list = *reinterpret_cast<PromptList*>(ring + P::kStages * P::kMat + (sizeof(PaShared) + 15) / 16 * 16);
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  volatile int* gave_up = &sh.gave_up;
+
+  if (tid == 0) {
+    for (int i = 0; i < P::kStages; ++i) {
+      bar_init(&sh.full[i], 1);
+      bar_init(&sh.free[i], 1);
+    }
+    bar_init(&sh.qfull, 1);
+    bar_init(&sh.qfree, 1);
+    for (int i = 0; i < 2; ++i) {
+      bar_init(&sh.sfull[i], 1);
+      bar_init(&sh.pfull[i], 4);
+      bar_init(&sh.ofull[i], 1);
+      bar_init(&sh.item_full[i], 1);
+      bar_init(&sh.item_free[i], 9);
+    }
+    sh.gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kPaIssuer) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(kv_smem(&sh.tmem)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  pdl_enter();
+  prompt_extents(a, list);
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
+  const int span = kPrTile / a.pack;                     // tokens of a group
+
+  if (warp < 8) {
+    // ============================================================ softmax ========
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPaSoftRegs));
+    const int wg = warp >> 2, row = tid & 127;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+    const uint32_t s_tm = tmem + lanes + wg * 128, o_tm = tmem + lanes + 256 + wg * 128;
+    const int row_tok = wg * span + row / a.pack, row_head = row % a.pack;
+    const float2 g2 = make_float2(a.factor, a.factor);
+    uint32_t su = 0, ou = 0;
+    bool ok = true;
+    for (uint32_t iu = 0; ok; ++iu) {
+      if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, gave_up, a.stats)) break;
+      const PaItem it = sh.item[iu & 1];
+      __syncwarp();
+      if (lane == 0) bar_arrive(&sh.item_free[iu & 1]);
+      if (!it.live) break;
+      const int tok = it.tok + row_tok, head = it.q_head + row_head;
+      const bool have = tok < it.n;
+      const int vis = have ? min(it.c, it.c - it.n + tok + 1) : 0;       // keys the row sees (0 or less: none)
+      const int n_tiles = it.tiles[wg];
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < n_tiles; ++j, ++su) {
+        if (!warp_wait(&sh.sfull[wg], su & 1, gave_up, a.stats)) { ok = false; break; }
+        fence_after();
+        uint32_t x[128];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) tmem_ask32(s_tm + k * 32, x + k * 32);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) tmem_wait32(x + k * 32);
+        const int see = vis - j * kPrTile;
+        if (__any_sync(0xffffffffu, see < kPrTile)) {
+#pragma unroll
+          for (int e = 0; e < 128; ++e) x[e] = e < see ? x[e] : 0xff800000u;
+        }
+        float y[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int e = 0; e < 64; ++e) y[e & 3] = max3(y[e & 3], __uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1]));
+        const float mx = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])) * a.factor;
+        if (__any_sync(0xffffffffu, mx > m + kPaSlack)) {
+          // (each row for itself; the products so far are done, or there were no scores)
+          const float mn = mx > m + kPaSlack ? mx : m, down = mn == -INFINITY ? 1.f : exp2_approx(m - mn);
+          m = mn;
+          l *= down;
+          if (j > 0) {
+#pragma unroll 1
+            for (int k = 0; k < D; k += 16) {
+              uint32_t r[16];
+              tmem_ld16(o_tm + k, r);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * down);
+              tmem_st16(o_tm + k, r);
+            }
+          }
+        }
+        const float shift = kRoom - (m == -INFINITY ? 0.f : m);
+        const float2 shift2 = make_float2(shift, shift);
+        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint32_t w[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int i2 = k * 32 + 2 * e;
+            const float2 z = fma2(make_float2(__uint_as_float(x[i2]), __uint_as_float(x[i2 + 1])), g2, shift2);
+            const float2 pr = make_float2(exp2_approx(z.x), exp2_approx(z.y));
+            sum[e & 1] = add2(sum[e & 1], pr);
+            w[e] = pack16<kBf16>(pr.x, pr.y);
+          }
+          tmem_st16(s_tm + k * 16, w);                   // over the scores
+        }
+        sum[0] = add2(sum[0], sum[1]);
+        l += sum[0].x + sum[0].y;
+        tmem_wait_st();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(&sh.pfull[wg]);
+      }
+      if (!ok) break;
+      if (n_tiles > 0) {
+        if (!warp_wait(&sh.ofull[wg], ou++ & 1, gave_up, a.stats)) break;
+        fence_after();
+      }
+      // ---- out ----
+      const bool write = tok < (a.qs.first ? it.n : a.qs.rows);
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const long long seq = a.qs.first ? 0 : it.s, r = (long long)it.q0 + tok;
+      uint16_t* op = a.out + seq * a.out_seq + r * a.out_row + head * a.out_head;
+      bool odd = false;
+#pragma unroll 1
+      for (int k = 0; k < D; k += 32) {
+        float o[32];
+        if (n_tiles > 0) tmem_ld32(o_tm + k, o);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          uint32_t w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float u0 = o[8 * h + 2 * e] * inv, u1 = o[8 * h + 2 * e + 1] * inv;
+            odd |= !(fabsf(u0) < INFINITY) || !(fabsf(u1) < INFINITY);
+            w[e] = l == 0.f ? 0u : pack16<kBf16>(u0, u1);
+          }
+          if (write) *reinterpret_cast<uint4*>(op + k + 8 * h) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      }
+      if (write && a.lse)
+        a.lse[seq * a.lse_seq + r * a.lse_row + head * a.lse_head] = l == 0.f ? -INFINITY : (m - kRoom + log2f(l)) * kPaLn2;
+      odd = odd && have && l != 0.f && n_tiles > 0;
+      unsigned rows = __ballot_sync(0xffffffffu, odd);
+      if (rows) {
+        const int least = __reduce_min_sync(0xffffffffu, odd ? vis : 0x7fffffff);
+        if (!odd_values<D, kBf16>(a, it, least, n_tiles * kPrTile, lane)) rows = 0;
+        for (; rows; rows &= rows - 1) {
+          const int at = __ffs(rows) - 1;
+          row_again<D, kBf16>(a, it, __shfl_sync(0xffffffffu, tok, at), __shfl_sync(0xffffffffu, head, at),
+                              __shfl_sync(0xffffffffu, vis, at), __shfl_sync(0xffffffffu, m, at) - kRoom,
+                              __shfl_sync(0xffffffffu, l, at), lane);
+        }
+      }
+      fence_before();
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPaRestRegs));
+    if (warp == kPaLoader) {
+      // ========================================================== loads ==========
+      PaFinder finder;
+      finder.l = &list;
+      finder.n_seq = a.n_seq;
+      finder.span = 2 * span;
+      finder.padded_rows = a.qs.first ? 0 : a.qs.rows;
+      int most = 0;
+      for (int s = lane; s < a.n_seq; s += 32) most = max(most, list.c[s]);
+      finder.level = (__reduce_max_sync(0xffffffffu, most) + kPrTile - 1) / kPrTile;
+      const int heads = a.n_kv * (a.group / a.pack);
+      const bool leader = one_lane();
+      uint32_t u = 0, qu = 0;
+      bool ok = true;
+      for (uint32_t iu = 0; ok; ++iu) {
+        const long long i = (long long)iu * gridDim.x + (iu & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+        const int hd = (int)(i % heads);
+        int s = 0, t = 0;
+        const bool live = finder.find(i / heads, lane, s, t);
+        PaItem it;
+        it.live = live;
+        it.s = s;
+        it.tok = t * 2 * span;
+        it.head = hd / (a.group / a.pack);
+        it.q_head = hd * a.pack;
+        it.n = list.n[s];
+        it.c = list.c[s];
+        it.q0 = list.q0[s];
+        it.k0 = list.k0[s];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const int last = min(it.n, it.tok + (g + 1) * span) - 1;       // the group's last row that is there
+          const int vis = last >= it.tok + g * span ? min(it.c, it.c - it.n + last + 1) : 0;
+          it.tiles[g] = vis > 0 ? (vis + kPrTile - 1) / kPrTile : 0;
+        }
+        if (iu >= 2 && !warp_wait(&sh.item_free[iu & 1], ((iu >> 1) - 1) & 1, gave_up, a.stats)) break;
+        if (lane == 0) {
+          sh.item[iu & 1] = it;
+          bar_arrive(&sh.item_full[iu & 1]);
+        }
+        if (!live) break;
+        const int n_tiles = max(it.tiles[0], it.tiles[1]);
+        if (n_tiles == 0) continue;
+        const int qs = a.qs.first ? 0 : s, ks = a.ks.first ? 0 : s;
+        for (int j = 0; j < 2 * n_tiles && ok; ++j, ++u) {               // K0 (then Q), V0, K1, V1, ..
+          const uint32_t st = u % P::kStages, use = u / P::kStages;
+          if (use > 0 && !warp_wait(&sh.free[st], (use - 1) & 1, gave_up, a.stats)) { ok = false; break; }
+          if (leader) {
+            bar_expect(&sh.full[st], P::kMat);
+#pragma unroll
+            for (int b = 0; b < P::kBlocks; ++b)
+              map_load4(kv_smem(ring + st * P::kMat + b * (kPrTile * 128)), j & 1 ? &v_map : &k_map, b * 64, it.head,
+                        it.k0 + (j >> 1) * kPrTile, ks, &sh.full[st]);
+          }
+          __syncwarp();
+          if (j == 0) {
+            if (qu > 0 && !warp_wait(&sh.qfree, (qu - 1) & 1, gave_up, a.stats)) { ok = false; break; }
+            ++qu;
+            if (leader) {
+              bar_expect(&sh.qfull, 2 * P::kMat);
+#pragma unroll
+              for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int b = 0; b < P::kBlocks; ++b)
+                  map_load4(kv_smem(qmat + g * P::kMat + b * (kPrTile * 128)), &q_map, b * 64, it.q_head,
+                            it.q0 + it.tok + g * span, qs, &sh.qfull);
+            }
+            __syncwarp();
+          }
+        }
+      }
+    } else if (warp == kPaIssuer) {
+      // ========================================================== products =======
+      const uint32_t s_idesc = idesc_16(kPrTile, false, kBf16) | (a.negate ? kNegateA : 0u);
+      constexpr uint32_t o_idesc = idesc_16(D, true, kBf16);
+      const uint64_t q_desc = desc128(kv_smem(qmat), 16), k_desc = desc128(kv_smem(ring), 16),
+                     v_desc = desc128(kv_smem(ring), kPrTile * 128);
+      constexpr uint64_t kStage = P::kMat >> 4;
+      const bool leader = one_lane();
+      uint32_t u = 0, qu = 0, pu[2] = {0, 0};
+      bool ok = true;
+      for (uint32_t iu = 0; ok; ++iu) {
+        if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, gave_up, a.stats)) break;
+        const int live = sh.item[iu & 1].live, tiles0 = sh.item[iu & 1].tiles[0], tiles1 = sh.item[iu & 1].tiles[1];
+        __syncwarp();
+        if (lane == 0) bar_arrive(&sh.item_free[iu & 1]);
+        if (!live) break;
+        const int n_tiles = max(tiles0, tiles1);
+        if (n_tiles == 0) continue;
+        auto landed = [&](uint32_t v) { ok = ok && warp_wait(&sh.full[v % P::kStages], (v / P::kStages) & 1, gave_up, a.stats); };
+        auto scores = [&](int g, uint32_t kv) {          // of group g, keys in ring place kv
+          const uint64_t kd = k_desc + (kv % P::kStages) * kStage;
+          if (leader) {
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+              const uint64_t off = (uint64_t)((k >> 2) * (kPrTile * 128 >> 4) + (k & 3) * 2);
+              mma_ss(tmem + g * 128, q_desc + g * kStage + off, kd + off, s_idesc, k > 0);
+            }
+            commit(&sh.sfull[g]);
+          }
+          __syncwarp();
+        };
+        landed(u);
+        ok = ok && warp_wait(&sh.qfull, qu++ & 1, gave_up, a.stats);
+        if (!ok) break;
+        fence_after();
+        if (tiles0 > 0) scores(0, u);
+        if (tiles1 > 0) scores(1, u);
+        if (leader) {
+          commit(&sh.free[u % P::kStages]);
+          if (n_tiles == 1) commit(&sh.qfree);
+        }
+        __syncwarp();
+        for (int j = 0; j < n_tiles && ok; ++j) {
+          const uint32_t vu = u + 2 * j + 1, ku = vu + 1;
+          landed(vu);
+          if (j + 1 < n_tiles) landed(ku);
+          if (!ok) break;
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            const int mine = g ? tiles1 : tiles0;
+            if (j < mine) {
+              if (!warp_wait(&sh.pfull[g], pu[g]++ & 1, gave_up, a.stats)) { ok = false; break; }
+              fence_after();
+              const uint64_t vd = v_desc + (vu % P::kStages) * kStage;
+              if (leader) {
+#pragma unroll
+                for (int k = 0; k < kPrTile / 16; ++k)
+                  mma_ts(tmem + 256 + g * 128, tmem + g * 128 + k * 8, vd + (uint64_t)(k * 2048 >> 4), o_idesc, j > 0 || k > 0);
+                if (j + 1 == mine) commit(&sh.ofull[g]);
+              }
+              __syncwarp();
+              if (j + 1 < mine) scores(g, ku);
+            }
+          }
+          if (!ok) break;
+          if (leader) {
+            commit(&sh.free[vu % P::kStages]);
+            if (j + 1 < n_tiles) commit(&sh.free[ku % P::kStages]);
+            if (j + 2 == n_tiles) commit(&sh.qfree);
+          }
+          __syncwarp();
+        }
+        u += 2 * n_tiles;
+      }
+    }
+  }
+  fence_before();
+  __syncthreads();
+  if (warp == kPaIssuer) {
+    fence_after();
+    // The softmax warps waited for the last products, and the products for the last copies, unless
+    // somebody gave up: then what is in flight gets time to end.  (Read behind the barrier, when nobody
+    // can any more.)
+    if (*gave_up) {
+      const unsigned long long t0 = now_ns();
+      while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
+    }
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------ host side ---
+bool prompt_map(CUtensorMap* map, const KvRows& r, int head_dim, int heads, int rows, int n_seq, int box_heads, int box_rows, bool bf16) {
+  typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                             const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static const Encode encode = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult res;
+    const bool there = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &res) == cudaSuccess &&
+                       res == cudaDriverEntryPointSuccess;
+    return there ? (Encode)p : (Encode)nullptr;
+  }();
+  if (!encode) return false;
+  // (the stride of an extent of one is never used: any that the map takes)
+  const cuuint64_t dims[4] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)rows, (cuuint64_t)n_seq};
+  const cuuint64_t strides[3] = {(cuuint64_t)(heads > 1 ? r.head * 2 : 16), (cuuint64_t)(rows > 1 ? r.row * 2 : 16),
+                                 (cuuint64_t)(n_seq > 1 ? r.seq * 2 : 16)};
+  const cuuint32_t box[4] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows, 1}, step[4] = {1, 1, 1, 1};
+  return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, (void*)r.p, dims, strides,
+                box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, bool kBf16>
+static cudaError_t run_attend(const PromptArgs& a, int sms, cudaStream_t st) {
+  CUtensorMap qm, km, vm;
+  const int nq = a.qs.first ? 1 : a.n_seq, nk = a.ks.first ? 1 : a.n_seq;
+  // (without a key row nothing is loaded by the maps, but they have to be over something)
+  const bool keys = a.ks.rows > 0;
+  if (!prompt_map(&qm, a.q, D, a.n_kv * a.group, a.qs.rows, nq, a.pack, kPrTile / a.pack, kBf16) ||
+      !prompt_map(&km, keys ? a.k : a.q, D, a.n_kv, keys ? a.ks.rows : 1, keys ? nk : 1, 1, kPrTile, kBf16) ||
+      !prompt_map(&vm, keys ? a.v : a.q, D, a.n_kv, keys ? a.ks.rows : 1, keys ? nk : 1, 1, kPrTile, kBf16))
+    return cudaErrorInvalidValue;
+  // the most items there can be: a sequence's last one may be short
+  const long long span = 2 * kPrTile / a.pack;
+  const long long tiles = a.qs.first ? a.qs.rows / span + a.n_seq : (long long)a.n_seq * ((a.qs.rows + span - 1) / span);
+  const long long items = tiles * a.n_kv * (a.group / a.pack);
+  return launch_pdl(prompt_attend_kernel<D, kBf16>, dim3((unsigned)(items < sms ? items : sms)), dim3(kPaThreads), Pa<D>::kBytes, st,
+                    qm, km, vm, a);
+}
+cudaError_t launch_prompt_attend(const PromptArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st) {
+  if (head_dim == 64) return bf16 ? run_attend<64, true>(a, sms, st) : run_attend<64, false>(a, sms, st);
+  return bf16 ? run_attend<128, true>(a, sms, st) : run_attend<128, false>(a, sms, st);
+}
+cudaError_t preload_prompt_attend_kernels() {
+  cudaError_t e;
+  if ((e = preload_kernel(prompt_attend_kernel<64, true>, true)) != cudaSuccess) return e;
+  if ((e = preload_kernel(prompt_attend_kernel<64, false>, true)) != cudaSuccess) return e;
+  if ((e = preload_kernel(prompt_attend_kernel<128, true>, true)) != cudaSuccess) return e;
+  return preload_kernel(prompt_attend_kernel<128, false>, true);
+}
+
+}  // namespace oilbird
