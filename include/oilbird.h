@@ -783,8 +783,8 @@ int oilbird_prompt_attend(const oilbird_prompt* prompt, const oilbird_kv_rows* q
  * weight (dev fp32 [n_seq, n_kv_heads, k.rows], packed [n_kv_heads, k.rows], written) = sum over the query
  * rows i that see the key and the head's query heads of row_weight[i] * exp(scale * q.k - lse), with
  * attend()'s arguments and its lse.  row_weight: dev fp32 [n_seq, q.rows] or [q.rows], NULL: 1; rows
- * with weight 0 do not count, whatever they hold, and long runs of them cost next to nothing.  Padded keys
- * behind count[s] get 0.
+ * with weight 0 do not count, whatever they hold, and those in front of a sequence's first and behind
+ * its last other one cost next to nothing.  Padded keys behind count[s] get 0.
  */
 int oilbird_prompt_weigh(const oilbird_prompt* prompt, const oilbird_kv_rows* q, const float* lse,
                          const int64_t* lse_strides, const oilbird_kv_rows* k, const float* row_weight,

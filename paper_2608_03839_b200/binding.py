@@ -185,6 +185,7 @@ SYMBOLS = {
     "oilbird_kv_status": (ctypes.c_int, [ctypes.POINTER(CKVCache), ctypes.POINTER(_i64), _vp]),
     "oilbird_kv_last_error": (ctypes.c_char_p, []),
     "oilbird_prompt_attend": (ctypes.c_int, [_vp, _vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp]),
+    "oilbird_prompt_weigh": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_float, _vp, _vp]),
     "oilbird_prompt_status": (ctypes.c_int, [_i32, _vp]),
     "oilbird_prompt_set_wait_limit": (ctypes.c_int, [_i32, _u64, _vp]),
     "oilbird_prompt_last_error": (ctypes.c_char_p, []),
@@ -1216,6 +1217,24 @@ def prompt_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, first: torc
         p.d ** -0.5 if scale is None else scale, p.view(out, p.lead, p.heads), *p.lse(lse), p.stream(stream)),
         "oilbird_prompt_attend")
     return out, lse
+
+
+def prompt_weigh(q: torch.Tensor, lse: torch.Tensor, k: torch.Tensor, first: torch.Tensor | None = None,
+                 n_new: torch.Tensor | None = None, first_k: torch.Tensor | None = None,
+                 n_k: torch.Tensor | None = None, row_weight: torch.Tensor | None = None,
+                 scale: float | None = None, weight: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The attention weight that the rows with row_weight (fp32 [n_seq, rows] or [rows]; None: 1) gave each key in
+    prompt_attend (same arguments, and its lse; oilbird_prompt_weigh): fp32 [n_seq, n_kv_heads, rows_k], which
+    KVCache.append takes, packed [n_kv_heads, rows_k]."""
+    p = _Prompt(q, k, first, n_new, first_k, n_k)
+    shape = (*p.lead_k[:-1], p.kv_heads, p.rows_k)
+    if weight is None:
+        weight = ALLOC(shape, torch.float32, p.dev)
+    _prompt_check(lib().oilbird_prompt_weigh(
+        p.c, p.view(q, p.lead, p.heads), *p.lse(lse), p.view(k, p.lead_k, p.kv_heads),
+        p.vec(row_weight, torch.float32, p.lead), p.d ** -0.5 if scale is None else scale,
+        p.vec(weight, torch.float32, shape), p.stream(stream)), "oilbird_prompt_weigh")
+    return weight
 
 
 def prompt_status(device: int = 0, stream=None) -> int:

@@ -79,6 +79,7 @@ cudaError_t preload_kv_weigh_kernels();
 cudaError_t preload_merge_kernels();
 cudaError_t preload_merge_tree_kernels();
 cudaError_t preload_prompt_attend_kernels();
+cudaError_t preload_prompt_weigh_kernels();
 cudaError_t preload_quant8_kernels();
 cudaError_t preload_ring_kernels();
 cudaError_t preload_scan_gemv_kernels();

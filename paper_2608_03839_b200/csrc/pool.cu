@@ -58,6 +58,7 @@ cudaError_t preload_all_kernels() {
   if ((e = preload_merge_kernels()) != cudaSuccess) return e;
   if ((e = preload_merge_tree_kernels()) != cudaSuccess) return e;
   if ((e = preload_prompt_attend_kernels()) != cudaSuccess) return e;
+  if ((e = preload_prompt_weigh_kernels()) != cudaSuccess) return e;
   if ((e = preload_quant8_kernels()) != cudaSuccess) return e;
   if ((e = preload_ring_kernels()) != cudaSuccess) return e;
   if ((e = preload_scan_gemv_kernels()) != cudaSuccess) return e;

@@ -155,6 +155,30 @@ int oilbird_prompt_attend(const oilbird_prompt* prompt, const oilbird_kv_rows* q
   return OILBIRD_OK;
 }
 
+int oilbird_prompt_weigh(const oilbird_prompt* prompt, const oilbird_kv_rows* q, const float* lse,
+                         const int64_t* lse_strides, const oilbird_kv_rows* k, const float* row_weight, float scale,
+                         float* weight, void* cuda_stream) {
+  PromptArgs a;
+  PTRY(check_prompt(prompt, &a));
+  PTRY(check_rows(q, "q", a.qs, a.n_seq, prompt->n_q_heads, &a.q));
+  PTRY(check_rows(k, "k", a.ks, a.n_seq, a.n_kv, &a.k));
+  PTRY(check_scale(scale, &a));
+  if (!aligned(lse, 4) || !aligned(row_weight, 4) || !aligned(weight, 4)) return refuse("lse, row_weight, weight: 4-byte aligned");
+  if (a.ks.rows == 0) return OILBIRD_OK;
+  if (!weight || (!lse && a.qs.rows > 0)) return refuse("lse and weight: neither may be missing");
+  a.lse = const_cast<float*>(lse);
+  a.row_weight = row_weight;
+  a.weight = weight;
+  lse_layout(prompt, lse_strides, &a);
+  OnDevice dev(prompt->device);
+  int sms;
+  PTRY(dev.enter(&sms, &a.stats));
+  const cudaError_t e = launch_prompt_weigh(a, prompt->head_dim, prompt->dtype == OILBIRD_KV_BF16, sms, (cudaStream_t)cuda_stream);
+  if (e == cudaErrorInvalidValue) return refuse("q, k: strides that no tensor map takes");
+  PCU(e);
+  return OILBIRD_OK;
+}
+
 int oilbird_prompt_status(int32_t device, void* cuda_stream) {
   OnDevice dev(device);
   int sms;

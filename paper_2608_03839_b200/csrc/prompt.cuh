@@ -64,6 +64,47 @@ __device__ __forceinline__ long long warp_sum_i64(long long v) {
   return v;
 }
 
+// The list of work is not stored.  Items are numbered by falling level (tiles they have to go
+// through), so that the last ones are short; a warp finds number i by a search over the levels, then over
+// the sequences, while the item before it is worked on.  `level`: any that no item from i on passes; becomes the item's.
+template <class Order>
+__device__ __forceinline__ bool prompt_find(const Order& order, int n_seq, long long i, int lane, int& level, int& s_out, int& t_out) {
+  auto count = [&](int x) {
+    long long v = 0;
+    for (int s = lane; s < n_seq; s += 32) v += order.items(s, x);
+    return warp_sum_i64(v);
+  };
+  if (count(0) <= i) return false;
+  int lo = 0, hi = level;
+  while (lo < hi) {                                      // the largest level with more than i items
+    const int mid = lo + (hi - lo + 1) / 2;
+    if (count(mid) > i) lo = mid; else hi = mid - 1;
+  }
+  level = lo;
+  long long left = i - count(lo + 1);                    // place among the items of this level
+  for (int s0 = 0; s0 < n_seq; s0 += 32) {
+    const int s = s0 + lane;
+    const int above = s < n_seq ? order.items(s, lo + 1) : 0, all = s < n_seq ? order.items(s, lo) : 0;
+    const long long here = all - above;
+    long long sum = here;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += y;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, left < sum);
+    if (hit) {
+      const int at = __ffs(hit) - 1;
+      s_out = s0 + at;
+      t_out = order.item(s_out, lo, (int)(left - __shfl_sync(0xffffffffu, sum - here, at)), __shfl_sync(0xffffffffu, all, at),
+                         __shfl_sync(0xffffffffu, above, at));
+      return true;
+    }
+    left -= __shfl_sync(0xffffffffu, sum, 31);
+  }
+  return false;
+}
+
 cudaError_t launch_prompt_attend(const PromptArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st);
 cudaError_t launch_prompt_weigh(const PromptArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st);
 // The 4-dimensional map (channel, head, row, sequence) of one side; a box is 64 channels of `heads`

@@ -24,8 +24,7 @@
 // its tiles that it does not see, and is then computed again by its warp from what it does see.
 //
 // Work.  Items by falling number of key tiles, so that the last ones are the short ones; block b takes
-// b, 2G-1-b, 2G+b, ... of G blocks.  The list is not stored: the loading warp finds an item by its number (a
-// search over the number of tiles, then over the sequences) while the one before it is worked on.
+// b, 2G-1-b, 2G+b, ... of G blocks (see prompt_find).
 //
 // Every wait is bounded (two seconds unless set otherwise): a wait that runs out raises `stalled`, all
 // roles leave, TMEM is freed.
@@ -64,63 +63,24 @@ struct Pa {
   static_assert(kBytes <= 227 * 1024, "shared memory");
 };
 
-// Tiles (of `span` tokens) of a sequence whose last row sees more than `keys` keys.
-__device__ __forceinline__ int tiles_beyond(int n, int c, int span, long long keys) {
-  if (c <= keys) return 0;
-  const long long d = keys - ((long long)c - n);
-  const int tiles = (n + span - 1) / span, from = d > 0 ? (int)(d / span) : 0;
-  return max(tiles - from, 0);
-}
-
-struct PaFinder {
+// Items of 2 `span` tokens.  Those with more keys lie behind those with fewer; in the padded form what
+// lies behind a sequence's rows is written too.
+struct PaOrder {
   const PromptList* l;
-  int n_seq, span, padded_rows;      // padded_rows: rows to write for every sequence (0: packed)
-  int level;                         // key tiles of the last item found: the next one has no more
-  __device__ __forceinline__ int tiles_at(int s, int level) const {
-    if (level == 0) return padded_rows ? (padded_rows + span - 1) / span : (l->n[s] + span - 1) / span;
-    return tiles_beyond(l->n[s], l->c[s], span, (long long)(level - 1) * kPrTile);
+  int span, padded;                  // padded: rows to write for every sequence (0: packed)
+  __device__ __forceinline__ int there(int s) const { return (l->n[s] + span - 1) / span; }
+  // items of sequence s with `level` key tiles or more
+  __device__ __forceinline__ int items(int s, int level) const {
+    if (level == 0) return padded ? (padded + span - 1) / span : there(s);
+    const long long keys = (long long)(level - 1) * kPrTile;             // the last row of the item sees more than these
+    if (l->c[s] <= keys) return 0;
+    const long long d = keys - ((long long)l->c[s] - l->n[s]);
+    return max(there(s) - (d > 0 ? (int)min(d / span, (long long)there(s)) : 0), 0);
   }
-  // items (of one head) with `level` key tiles or more
-  __device__ __forceinline__ long long count(int level, int lane) const {
-    long long v = 0;
-    for (int s = lane; s < n_seq; s += 32) v += tiles_at(s, level);
-    return warp_sum_i64(v);
-  }
-  // item number i: sequence and tile
-  __device__ __forceinline__ bool find(long long i, int lane, int& s_out, int& t_out) {
-    int lo = 0, hi = level;
-    if (count(0, lane) <= i) return false;
-    while (lo < hi) {                                    // the largest level with more than i items
-      const int mid = (lo + hi + 1) >> 1;
-      if (count(mid, lane) > i) lo = mid; else hi = mid - 1;
-    }
-    level = lo;
-    long long left = i - count(lo + 1, lane);            // place among the items of this level
-    for (int s0 = 0; s0 < n_seq; s0 += 32) {
-      const int s = s0 + lane;
-      const int above = s < n_seq ? tiles_at(s, lo + 1) : 0, all = s < n_seq ? tiles_at(s, lo) : 0;
-      int here = all - above, sum = here;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, sum, o);
-        if (lane >= o) sum += y;
-      }
-      const unsigned hit = __ballot_sync(0xffffffffu, left < sum);
-      if (hit) {
-        const int at = __ffs(hit) - 1;
-        s_out = s0 + at;
-        t_out = (int)(left - __shfl_sync(0xffffffffu, sum - here, at));
-        const int there = (l->n[s_out] + span - 1) / span;
-        if (lo > 0) t_out += there - __shfl_sync(0xffffffffu, all, at);
-        else {                                           // rows in front that see nothing, then padding
-          const int seeing = __shfl_sync(0xffffffffu, above, at);
-          if (t_out >= there - seeing) t_out += seeing;
-        }
-        return true;
-      }
-      left -= __shfl_sync(0xffffffffu, sum, 31);
-    }
-    return false;
+  // the `at`-th item of sequence s among those of one level; `all` items have that level or more, `above` more
+  __device__ __forceinline__ int item(int s, int level, int at, int all, int above) const {
+    if (level > 0) return there(s) - all + at;
+    return at < there(s) - above ? at : at + above;      // rows in front that see nothing, then padding
   }
 };
 
@@ -345,14 +305,10 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPaRestRegs));
     if (warp == kPaLoader) {
       // ========================================================== loads ==========
-      PaFinder finder;
-      finder.l = &list;
-      finder.n_seq = a.n_seq;
-      finder.span = 2 * span;
-      finder.padded_rows = a.qs.first ? 0 : a.qs.rows;
-      int most = 0;
-      for (int s = lane; s < a.n_seq; s += 32) most = max(most, list.c[s]);
-      finder.level = (__reduce_max_sync(0xffffffffu, most) + kPrTile - 1) / kPrTile;
+      const PaOrder order = {&list, 2 * span, a.qs.first ? 0 : a.qs.rows};
+      int level = 0;                                     // of the last item found: the next one has no more
+      for (int s = lane; s < a.n_seq; s += 32) level = max(level, (list.c[s] + kPrTile - 1) / kPrTile);
+      level = __reduce_max_sync(0xffffffffu, level);
       const int heads = a.n_kv * (a.group / a.pack);
       const bool leader = one_lane();
       uint32_t u = 0, qu = 0;
@@ -361,7 +317,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         const long long i = (long long)iu * gridDim.x + (iu & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
         const int hd = (int)(i % heads);
         int s = 0, t = 0;
-        const bool live = finder.find(i / heads, lane, s, t);
+        const bool live = prompt_find(order, a.n_seq, i / heads, lane, level, s, t);
         PaItem it;
         it.live = live;
         it.s = s;

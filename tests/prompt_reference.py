@@ -66,3 +66,28 @@ def check_attend(got, lse, ref, dtype, d):
     assert torch.equal(lse > -math.inf, there)
     e = (lse.double() - rl)[there].abs()
     assert bool((e <= (drift + 2.0 ** -21 * rl.abs())[there]).all()), f"lse off by {e.max().item():.3g}"
+
+
+def weigh(q, lse, k, row_weight, scale):
+    """One sequence, in 64 bits: what each key receives, [hkv, c]; the same with |row_weight|, and the largest
+    of the sums |scale q k| + |lse| of what goes into it."""
+    n, hq, d = q.shape
+    c, hkv, _ = k.shape
+    q, lse, w = q.double(), lse.double(), row_weight.double()
+    k = k.double().repeat_interleave(hq // hkv, 1)
+    use = seen(n, c) & (w != 0)[:, None] & (lse.T > -math.inf)[..., None]
+    x = torch.einsum("nhd,chd->hnc", q, k) * scale - lse.T[..., None]
+    p = torch.where(use, x.exp() * w[:, None], 0.0)
+    size = torch.einsum("nhd,chd->hnc", q.abs(), k.abs()) * abs(scale) + lse.abs().T[..., None]
+    per = lambda y: y.unflatten(0, (hkv, -1)).sum((1, 2))
+    reach = torch.where(use, size, 0.0).unflatten(0, (hkv, -1)).amax((1, 2)) if n else p.new_zeros(hkv, c)
+    return per(p), per(p.abs()), reach
+
+
+def check_weigh(got, ref, n_terms, d):
+    """What the fp32 sums of d products and of a tile's 32 terms each may be off by; the sum over the tiles keeps what
+    it loses (two steps and a half in all)."""
+    w, mass, reach = ref
+    tol = ((d + 8) * 2.0 ** -24 * reach + (32 + 8) * 2.0 ** -24 + n_terms * 2.0 ** -46) * mass * 1.01 + 1e-37
+    err = (got.double() - w).abs()
+    assert bool((err <= tol).all()), f"off by {err.max().item():.3g}, {(err / tol).max().item():.3g} of the bound"
