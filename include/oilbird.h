@@ -796,6 +796,37 @@ int oilbird_prompt_status(int32_t device, void* cuda_stream);
 int oilbird_prompt_set_wait_limit(int32_t device, uint64_t limit_ns, void* cuda_stream);
 const char* oilbird_prompt_last_error(void);
 
+/*
+ * Scores of tokens from the verifier's logits (not in the paper, whose verifier is a given): what a draft's
+ * tokens are compared with.  For each row, over x_0 .. x_{vocab-1}:
+ *   lse      ln sum_j exp x_j
+ *   logp     x_t - lse for the row's n_tokens given tokens t; -inf for a t outside the vocabulary
+ *   entropy  -sum_j p_j ln p_j, p_j = exp(x_j - lse)
+ *   top_id, top_logp   the k tokens of largest logit, best first, equal ones by lowest token, and their
+ *            log probabilities; -1 and -inf where the row has fewer than k that are not NaN
+ * A logit of -inf has probability 0 (and is an alternative like any other).  A row of nothing else has lse
+ * -inf, logp -inf, entropy 0; a row holding NaN or +inf has NaN for its numbers.
+ * logits: dev [rows, vocab], row_stride elements apart, of any alignment that their elements have; tokens:
+ * dev [rows, n_tokens].  Results: dev [rows, n_tokens], [rows], [rows], [rows, k]; lse and entropy may be NULL,
+ * the others where there are none of them.  Enqueues one kernel; no allocation, no workspace; can be captured in a
+ * CUDA graph after the first call on the device.  Refusals return OILBIRD_EINVAL and leave the reason in
+ * oilbird_token_scores_error().
+ */
+#define OILBIRD_LOGITS_BF16 0
+#define OILBIRD_LOGITS_F16  1
+#define OILBIRD_LOGITS_F32  2
+#define OILBIRD_SCORES_MAX_VOCAB 16777216
+#define OILBIRD_SCORES_MAX_TOP   64
+typedef struct {
+  float *logp, *lse, *entropy;
+  int32_t* top_id;
+  float* top_logp;
+} oilbird_scores_out;
+int oilbird_token_scores(const void* logits, int64_t row_stride, int32_t rows, int32_t vocab,
+                         int32_t dtype, const int32_t* tokens, int32_t n_tokens, int32_t k,
+                         const oilbird_scores_out* out, int32_t device, void* cuda_stream);
+const char* oilbird_token_scores_error(void);
+
 const char* oilbird_strerror(int code);
 const char* oilbird_last_cuda_error(void);    /* text of the last failing CUDA call      */
 

@@ -189,6 +189,8 @@ SYMBOLS = {
     "oilbird_prompt_status": (ctypes.c_int, [_i32, _vp]),
     "oilbird_prompt_set_wait_limit": (ctypes.c_int, [_i32, _u64, _vp]),
     "oilbird_prompt_last_error": (ctypes.c_char_p, []),
+    "oilbird_token_scores": (ctypes.c_int, [_vp, _i64, _i32, _i32, _i32, _vp, _i32, _i32, _vp, _i32, _vp]),
+    "oilbird_token_scores_error": (ctypes.c_char_p, []),
     "oilbird_query_static": (ctypes.c_int, [ctypes.POINTER(StaticPool), _vp, _i32,
                                             ctypes.POINTER(CQueryParams),
                                             ctypes.POINTER(CQueryOut), _vp]),
@@ -1249,3 +1251,53 @@ def prompt_set_wait_limit(limit_ns: int, device: int = 0, stream=None) -> None:
     """How long the device-side waits of prompt calls may take (0: two seconds)."""
     _prompt_check(lib().oilbird_prompt_set_wait_limit(device, limit_ns, _raw_stream(device) if stream is None
                                                       else stream.cuda_stream), "oilbird_prompt_set_wait_limit")
+
+
+# ------------------------------------------------------------------ token scores ----
+LOGITS_BF16, LOGITS_F16, LOGITS_F32 = 0, 1, 2
+SCORES_MAX_VOCAB, SCORES_MAX_TOP = 16777216, 64
+_LOGITS_DTYPES = {torch.bfloat16: LOGITS_BF16, torch.float16: LOGITS_F16, torch.float32: LOGITS_F32}
+_SCORES_OUT = ctypes.c_int64 * 5     # oilbird_scores_out
+
+
+@dataclass
+class TokenScores:
+    logp: torch.Tensor | None   # [rows, n_tokens] fp32 (None without tokens)
+    lse: torch.Tensor           # [rows] fp32
+    entropy: torch.Tensor       # [rows] fp32
+    top_id: torch.Tensor        # [rows, top] int32
+    top_logp: torch.Tensor      # [rows, top] fp32
+
+
+def token_scores(logits: torch.Tensor, tokens: torch.Tensor | None = None, top: int = 0, stream=None) -> TokenScores:
+    """Log probabilities of the given tokens (int32 [rows, n_tokens]), entropy and the `top` best tokens of each row
+    of logits [rows, vocab] (bf16, f16 or fp32; rows of any stride), in one reading (oilbird_token_scores)."""
+    if logits.dtype not in _LOGITS_DTYPES or logits.dim() != 2 or not logits.is_cuda or \
+            (logits.stride(1) != 1 and logits.shape[1] > 1):
+        raise AssertionError("logits: a bf16, f16 or fp32 tensor [rows, vocab] on a CUDA device, with contiguous rows; "
+                             "there is no CPU fallback")
+    if logits.requires_grad and torch.is_grad_enabled():
+        raise RuntimeError("token scores have no backward pass: detach the logits, or call under torch.no_grad()")
+    rows, vocab = logits.shape
+    index, dev = logits.get_device(), logits.device
+    n = 0
+    if tokens is not None:
+        if tokens.dtype is not torch.int32 or tokens.dim() != 2 or tokens.shape[0] != rows or \
+                tokens.get_device() != index or not tokens.is_contiguous():
+            raise AssertionError(f"tokens: a contiguous int32 tensor [{rows}, n] on {dev}")
+        n = tokens.shape[1]
+    top = max(-1, min(int(top), 2 ** 31 - 1))
+    new = ALLOC
+    got = TokenScores(None if tokens is None else new((rows, n), torch.float32, dev), new((rows,), torch.float32, dev),
+                      new((rows,), torch.float32, dev), new((rows, max(0, min(top, SCORES_MAX_TOP))), torch.int32, dev),
+                      new((rows, max(0, min(top, SCORES_MAX_TOP))), torch.float32, dev))
+    out = _SCORES_OUT(got.logp.data_ptr() if n else 0, got.lse.data_ptr(), got.entropy.data_ptr(), got.top_id.data_ptr(),
+                      got.top_logp.data_ptr())
+    rc = lib().oilbird_token_scores(logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, rows, vocab,
+                                    _LOGITS_DTYPES[logits.dtype], tokens.data_ptr() if n else None, n, top, out, index,
+                                    _raw_stream(index) if stream is None else stream.cuda_stream)
+    if rc != OK:
+        err = OilbirdError(rc, "oilbird_token_scores")
+        err.args = (err.args[0] + ": " + lib().oilbird_token_scores_error().decode(),)
+        raise err
+    return got

@@ -86,6 +86,7 @@ cudaError_t preload_scan_gemv_kernels();
 cudaError_t preload_scan_mma_kernels();
 cudaError_t preload_scan_tc_kernels();
 cudaError_t preload_shard_kernels();
+cudaError_t preload_token_scores_kernels();
 // all of the above, once per device (the current device); thread-safe
 cudaError_t preload_all_kernels();
 

@@ -65,6 +65,7 @@ cudaError_t preload_all_kernels() {
   if ((e = preload_scan_mma_kernels()) != cudaSuccess) return e;
   if ((e = preload_scan_tc_kernels()) != cudaSuccess) return e;
   if ((e = preload_shard_kernels()) != cudaSuccess) return e;
+  if ((e = preload_token_scores_kernels()) != cudaSuccess) return e;
   if (dev >= 0 && dev < 64) done[dev] = true;
   return cudaSuccess;
 }
