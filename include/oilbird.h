@@ -690,6 +690,12 @@ size_t  oilbird_kv_workspace_bytes(int32_t head_dim);
 int oilbird_kv_append(const oilbird_kv_cache* cache, const oilbird_kv_rows* k,
                       const oilbird_kv_rows* v, int32_t m, int32_t rows, const int32_t* n_new,
                       const int32_t* select, const float* weight, void* cuda_stream);
+/* Append packed: the same for prompts that lie one after another, as the prompt calls below take them: of
+ * the m rows of k and v (no sequence stride; at most 2^24), rows first[s] .. first[s + 1) (dev [n_seq + 1];
+ * what leaves 0..m is cut) join sequence s.  weight: dev [n_kv_heads, m], NULL: 0. */
+int oilbird_kv_append_packed(const oilbird_kv_cache* cache, const oilbird_kv_rows* k,
+                             const oilbird_kv_rows* v, int32_t m, const int32_t* first,
+                             const float* weight, void* cuda_stream);
 /* Slots start[s].. (dev [n_seq]; NULL: 0) as 16-bit rows: k, v dev [n_seq, n, n_kv_heads,
  * head_dim]; zeros where there is no slot, the type's largest number where an element stands for
  * more (its group's scale was rounded up). */

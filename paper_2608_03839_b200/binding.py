@@ -176,6 +176,7 @@ SYMBOLS = {
     "oilbird_kv_workspace_bytes": (ctypes.c_size_t, [_i32]),
     "oilbird_kv_append": (ctypes.c_int, [ctypes.POINTER(CKVCache), _vp, _vp, _i32, _i32, _vp, _vp,
                                          _vp, _vp]),
+    "oilbird_kv_append_packed": (ctypes.c_int, [ctypes.POINTER(CKVCache), _vp, _vp, _i32, _vp, _vp, _vp]),
     "oilbird_kv_read": (ctypes.c_int, [ctypes.POINTER(CKVCache), _i32, _vp, _vp, _vp, _vp]),
     "oilbird_kv_attend": (ctypes.c_int, [ctypes.POINTER(CKVCache), _i32, _i32, _vp, _vp, _vp, _vp,
                                          _i64, _vp, ctypes.c_float, _vp, _vp, _vp, _vp]),
@@ -1005,6 +1006,12 @@ class KVCache:
         raise AssertionError(f"a {self.dtype} tensor [{self.n_seq}, {m}, {heads}, {self.head_dim}] on {self._dev} "
                              "with contiguous channels")
 
+    def _packed_rows(self, t: torch.Tensor, m: int):
+        """The C view of a [m, n_kv_heads, head_dim] tensor (any strides but the last)."""
+        if t.shape != (m, self.n_kv_heads, self.head_dim):
+            raise AssertionError(f"a tensor [{m}, {self.n_kv_heads}, {self.head_dim}]")
+        return self._rows(t.expand(self.n_seq, -1, -1, -1), self.n_kv_heads, m)
+
     def _vec(self, t, dtype, shape):
         """Pointer of an optional contiguous tensor of that type and shape."""
         if t is None:
@@ -1039,10 +1046,21 @@ class KVCache:
 
     def append(self, k: torch.Tensor, v: torch.Tensor, n_new: torch.Tensor | None = None,
                select: torch.Tensor | None = None, weight: torch.Tensor | None = None,
-               stream=None) -> None:
+               stream=None, first: torch.Tensor | None = None) -> None:
         """Store rows of k and v [n_seq, m, n_kv_heads, head_dim]: rows select[s, :n_new[s]]
         (int32 [n_seq, rows]; None: the first n_new[s], None: all).  weight: fp32
-        [n_seq, n_kv_heads, m], the rows' first weights (None: 0)."""
+        [n_seq, n_kv_heads, m], the rows' first weights (None: 0).  With first (int32 [n_seq + 1]) k and v are packed
+        [m, n_kv_heads, head_dim]: rows first[s] .. first[s + 1] - 1 join sequence s; weight [n_kv_heads, m]."""
+        if first is not None:
+            if n_new is not None or select is not None:
+                raise AssertionError("packed rows (first) take neither n_new nor select")
+            m = k.shape[0]
+            if m > 0:
+                _kv_check(self._L.oilbird_kv_append_packed(
+                    self._ref, self._packed_rows(k, m), self._packed_rows(v, m), m,
+                    self._vec(first, torch.int32, (self.n_seq + 1,)),
+                    self._vec(weight, torch.float32, (self.n_kv_heads, m)), self._stream(stream)), "oilbird_kv_append_packed")
+            return
         m = k.shape[1]
         if m == 0:
             return

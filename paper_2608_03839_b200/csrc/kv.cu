@@ -155,6 +155,27 @@ int oilbird_kv_append(const oilbird_kv_cache* cache, const oilbird_kv_rows* k, c
   return OILBIRD_OK;
 }
 
+int oilbird_kv_append_packed(const oilbird_kv_cache* cache, const oilbird_kv_rows* k, const oilbird_kv_rows* v, int32_t m,
+                             const int32_t* first, const float* weight, void* cuda_stream) {
+  KvView c;
+  KvAppendArgs a;
+  memset(&a, 0, sizeof a);
+  KTRY(check_cache(cache, &c));
+  if (m < 0 || m > (1 << 24)) return kv_refuse("m: 0 to 2^24");
+  if (m == 0) return OILBIRD_OK;
+  if (!first) return kv_refuse("first");
+  KTRY(check_rows(k, "k", 1, m, c.n_kv, &a.k));
+  KTRY(check_rows(v, "v", 1, m, c.n_kv, &a.v));
+  KTRY(check_words("first, weight", {first, weight}));
+  a.first = first;
+  a.weight = weight;
+  a.m = a.rows = m;
+  int sms;
+  KTRY(on_device(cache->device, &sms));
+  KCU(launch_kv_append(c, a, cache->head_dim, cache->dtype == OILBIRD_KV_BF16, sms, (cudaStream_t)cuda_stream));
+  return OILBIRD_OK;
+}
+
 int oilbird_kv_read(const oilbird_kv_cache* cache, int32_t n, const int32_t* start, void* k, void* v,
                     void* cuda_stream) {
   KvView c;

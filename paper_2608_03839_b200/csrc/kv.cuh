@@ -87,8 +87,16 @@ struct KvAppendArgs {
   KvRows k, v;               // [n_seq, m, n_kv, D]
   const int32_t* n_new;      // [n_seq] or nullptr: `rows` each
   const int32_t* select;     // [n_seq, rows] rows of k and v to take, or nullptr: 0, 1, ...
-  const float* weight;       // [n_seq, n_kv, m] or nullptr: 0
+  const int32_t* first;      // [n_seq + 1] packed: sequence s has rows first[s] .. first[s + 1) of the m; else nullptr
+  const float* weight;       // [n_seq, n_kv, m], packed [n_kv, m], or nullptr: 0
   int m, rows;
+  // rows that join sequence s, and the first of them
+  __device__ __forceinline__ int count(int s, int& base) const {
+    base = 0;
+    if (!first) return n_new ? min(max(n_new[s], 0), rows) : rows;
+    base = min(max(first[s], 0), m);
+    return min(max(first[s + 1], base), m) - base;
+  }
 };
 struct KvReadArgs {
   uint16_t *k, *v;           // [n_seq, n, n_kv, D]

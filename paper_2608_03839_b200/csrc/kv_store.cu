@@ -121,8 +121,8 @@ kv_append_kernel(const KvView c, const KvAppendArgs a) {
   const int page = 1 << c.page_shift;
   const size_t block = 2 * (size_t)kv_part_bytes(D, page);
   const int s = blockIdx.y;
-  int n = a.n_new ? a.n_new[s] : a.rows;
-  n = min(n, a.rows);
+  int base;
+  const int n = a.count(s, base);
   const int before = max(c.seq_len[s], 0), pos0 = c.n_pos[s];
   const int head_groups = (c.n_kv + kHeads - 1) / kHeads, stride = gridDim.x * (kStThreads / 32);
   const KvRows& rows = kv ? a.v : a.k;
@@ -136,7 +136,7 @@ kv_append_kernel(const KvView c, const KvAppendArgs a) {
     r.head0 = (task - r.j * head_groups) * kHeads;
     r.p = -1;
     if (r.j < n) {
-      int src = a.select ? a.select[(size_t)s * a.rows + r.j] : r.j;
+      int src = a.select ? a.select[(size_t)s * a.rows + r.j] : base + r.j;
       r.p = page_of(c, s, (long long)before + r.j);
       if (src < 0 || src >= a.m) {
         if (r.p >= 0) r.p = -2 - r.p;
@@ -149,7 +149,7 @@ kv_append_kernel(const KvView c, const KvAppendArgs a) {
         if (head < c.n_kv) r.v[t] = *reinterpret_cast<const uint4*>(rows.at(s, src, head) + grp * kKvGroup + lane8 * 8);
       }
       r.w = a.weight && lane < kHeads && r.head0 + lane < c.n_kv
-                ? a.weight[((size_t)s * c.n_kv + r.head0 + lane) * a.m + src] : 0.f;
+                ? a.weight[((size_t)(a.first ? 0 : s) * c.n_kv + r.head0 + lane) * a.m + src] : 0.f;
     }
   };
   int task = blockIdx.x * (kStThreads / 32) + (threadIdx.x >> 5);
@@ -190,8 +190,7 @@ kv_append_kernel(const KvView c, const KvAppendArgs a) {
   if (last_block(&work->arrivals, gridDim.x * gridDim.y)) {
     const long long room = (long long)c.max_pages << c.page_shift;
     for (int i = threadIdx.x; i < c.n_seq; i += kStThreads) {
-      int m = a.n_new ? a.n_new[i] : a.rows;
-      m = m < 0 ? 0 : (m > a.rows ? a.rows : m);
+      const int m = a.count(i, base);
       const long long after = (long long)max(c.seq_len[i], 0) + m;
       c.seq_len[i] = (int)(after > room ? room : after);
       c.n_pos[i] += m;
