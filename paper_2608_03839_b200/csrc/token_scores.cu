@@ -10,10 +10,14 @@
 // sums of its own under a maximum of its own: no thread waits for another to add up.  Exponentials are
 // 2^((x - m) log2 e): the difference first, as it is exact where it counts and stays a number for the largest and lowest ones.
 //
-// The k best.  A list in shared memory takes every element above a floor (a composite of value and token, so
-// that equal values are in order too).  The floor is at first the k-th best of 64 groups' best elements of what
-// the block holds at the moment, so that few pass it, and again where more than half of the threads would add
-// to the list (as behind a long run of masked tokens); when the list is full it is sorted and cut to k, and the floor is the k-th.
+// The k best.  A list in shared memory takes every element that reaches a floor: the k-th largest of 64 or
+// 128 groups' largest values so far, which k elements reach and few pass, found anew after the first,
+// fourth, sixteenth, .. load.  Otherwise nobody waits for anybody in that either; where the list turns out to have been too
+// short (long runs of equal or rising values), or too few are above -inf, the block goes through its part again, cutting the list to
+// its k best each time it is full and raising the floor to the k-th, a composite of value and token.  Cutting
+// counts for each entry how many are better, which is its place: no sort, and little code, as what runs
+// once a row is bound by fetching it (a bitonic sort and straight-line code for each of a thread's 32
+// elements took 15 us a row; a barrier a load 100 us on 2,048 rows).
 #include <cooperative_groups.h>
 #include <stdio.h>
 #include <string.h>
@@ -28,8 +32,9 @@ namespace oilbird {
 
 namespace {
 
-constexpr int kTsThreads = 256, kTsWarps = kTsThreads / 32, kTsUnroll = 4, kTsList = kTsWarps * 64;
+constexpr int kTsThreads = 256, kTsWarps = kTsThreads / 32, kTsUnroll = 4, kTsList = 1024;
 constexpr int kTsMaxParts = 8;
+static_assert(OILBIRD_SCORES_MAX_TOP <= kTsList / kTsMaxParts && OILBIRD_SCORES_MAX_TOP <= 64, "the lists of a row's blocks");
 constexpr float kTsLn2 = 0.6931471805599453f;
 enum { kTsBf16 = OILBIRD_LOGITS_BF16, kTsF16 = OILBIRD_LOGITS_F16, kTsF32 = OILBIRD_LOGITS_F32 };
 
@@ -45,19 +50,33 @@ struct TsSums {
   float m, s, e;                     // maximum; sums of 2^z and of 2^z z with z = (x - m) log2 e
 };
 struct TsShared {
-  u64 list[kTsList], scratch[kTsList];
-  u64 floor;
-  int count;
+  alignas(16) u64 list[kTsList];
+  alignas(16) float group[128];
+  u64 floor;                         // what is not above it is not among the k best (second reading)
+  float floor_x;                     // what is below it is not (first reading)
+  int count;                         // of the list's entries, and those that found no room
   TsSums sums[kTsWarps];
 };
 
 template <int kType> struct TsType {
   static constexpr int kBytes = kType == kTsF32 ? 4 : 2, kPer = 16 / kBytes, kAll = kPer * kTsUnroll;
   static constexpr uint32_t kNone = kType == kTsF32 ? 0xff800000u : kType == kTsF16 ? 0xfc00fc00u : 0xff80ff80u;   // -inf
-  static __device__ __forceinline__ float get(const uint4 (&v)[kTsUnroll], int i) {         // element i of the thread's
-    const uint32_t w = (&v[i / kPer].x)[i % kPer * kBytes / 4];
+  static __device__ __forceinline__ float get(const uint4& v, int i) {                      // element i of sixteen bytes
+    const uint32_t w = (&v.x)[i * kBytes / 4];
     if (kType == kTsF32) return __uint_as_float(w);
     return i & 1 ? half_hi<kType == kTsBf16>(w) : half_lo<kType == kTsBf16>(w);
+  }
+  // the largest of sixteen bytes' elements (NaN says nothing); pairs first where a word is one
+  static __device__ __forceinline__ float largest(const uint4& v) {
+    if (kType == kTsF32) return fmaxf(fmaxf(get(v, 0), get(v, 1)), fmaxf(get(v, 2), get(v, 3)));
+    uint32_t r = pair_max(pair_max(v.x, v.y), pair_max(v.z, v.w));
+    return fmaxf(half_lo<kType == kTsBf16>(r), half_hi<kType == kTsBf16>(r));
+  }
+  static __device__ __forceinline__ uint32_t pair_max(uint32_t a, uint32_t b) {
+    uint32_t r;
+    if (kType == kTsBf16) asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
   }
   static __device__ __forceinline__ float one(const unsigned char* p) {
     if (kType == kTsF32) return __ldg(reinterpret_cast<const float*>(p));
@@ -71,43 +90,139 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
-__device__ __forceinline__ TsSums joined(const TsSums& a, const TsSums& b) {
-  TsSums r;
-  r.m = fmaxf(a.m, b.m);
-  r.s = r.e = 0.f;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const TsSums& x = i ? b : a;
-    const float d = x.m == r.m ? 0.f : max_nan((x.m - r.m) * kLog2e, -400.f);       // (equal infinities are no distance)
-    const float f = exp2_approx(d);
-    r.s = fmaf(f, x.s, r.s);
-    r.e = fmaf(f, fmaf(x.s, d, x.e), r.e);
-  }
-  return r;
+// The same sums under a maximum that is not smaller.
+__device__ __forceinline__ TsSums brought_to(const TsSums& x, float m) {
+  const float d = x.m == m ? 0.f : max_nan((x.m - m) * kLog2e, -400.f);          // (equal infinities are no distance)
+  const float f = exp2_approx(d);
+  return TsSums{m, f * x.s, f * fmaf(x.s, d, x.e)};
 }
-// Sorts the list's first n (at most kTsList) entries and keeps the k best; every thread calls.  Ends with a barrier.
-__device__ __forceinline__ void cut_list(TsShared& sh, int n, int k) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  u64 v[2];
+__device__ __forceinline__ TsSums joined(const TsSums& a, const TsSums& b) {
+  const float m = fmaxf(a.m, b.m);
+  const TsSums x = brought_to(a, m), y = brought_to(b, m);
+  return TsSums{m, x.s + y.s, x.e + y.e};
+}
+// Keeps the k best of the list's first n (at most kTsList) entries, in order; every thread calls, behind a barrier.
+template <int kMine>
+__device__ __forceinline__ void cut_list_of(TsShared& sh, int n, int k) {
+  u64 key[kMine];
+  int place[kMine];
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    const int i = warp * 64 + r * 32 + lane;
-    v[r] = i < n ? sh.list[i] : 0ull;
+  for (int r = 0; r < kMine; ++r) {
+    const int i = r * kTsThreads + threadIdx.x;
+    key[r] = i < n ? sh.list[i] : 0ull;
+    place[r] = 0;
   }
-  if (warp * 64 < n || warp == 0) warp_sort_desc<2>(v, lane);
-  block_merge_desc<2>(v, sh.scratch, max(1, (n + 63) / 64));
+  const ulonglong2* pairs = reinterpret_cast<const ulonglong2*>(sh.list);
+  if (n & 1 && threadIdx.x == 0) sh.list[n] = 0ull;      // (an even place: kTsList is even)
   __syncthreads();
-  if (warp == 0) {
-    const u64 last = warp_list_get<2>(v, k - 1);
+  if (kMine > 1 || threadIdx.x / 32 * 32 < n) {
+#pragma unroll 4
+    for (int j = 0; j < (n + 1) / 2; ++j) {
+      const ulonglong2 y = pairs[j];
 #pragma unroll
-    for (int r = 0; r < 2; ++r)
-      if (r * 32 + lane < k) sh.list[r * 32 + lane] = v[r];
-    if (lane == 0) {
-      sh.count = min(n, k);
-      if (n >= k) sh.floor = last;
+      for (int r = 0; r < kMine; ++r) place[r] += (y.x > key[r]) + (y.y > key[r]);
     }
   }
   __syncthreads();
+#pragma unroll
+  for (int r = 0; r < kMine; ++r)
+    if (key[r] != 0ull && place[r] < k) {
+      sh.list[place[r]] = key[r];
+      if (place[r] == k - 1) sh.floor = key[r];
+    }
+  if (threadIdx.x == 0) sh.count = min(n, k);
+  __syncthreads();
+}
+__device__ __noinline__ void cut_list(TsShared& sh, int n, int k) {
+  if (n <= kTsThreads) cut_list_of<1>(sh, n, k);
+  else cut_list_of<kTsList / kTsThreads>(sh, n, k);
+}
+
+// The floor that the threads' largest values so far (m) allow, in sh.floor_x; every thread calls.  More groups:
+// fewer elements pass, more to count.
+__device__ __noinline__ void raise_floor(TsShared& sh, float m, int k) {
+  const int tid = threadIdx.x, shares = k <= 32 ? 4 : 2; // threads of a group, each of which counts its share of the groups
+  float g = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+  if (shares == 4) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
+  const int group = tid / shares, share = kTsThreads / shares / shares;
+  if (tid % shares == 0) sh.group[group] = g;
+  __syncthreads();
+  int better = 0;
+  const int j0 = tid % shares * share;
+#pragma unroll 4
+  for (int j = j0; j < j0 + share; j += 4) {
+    const float4 y = *reinterpret_cast<const float4*>(sh.group + j);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) better += (&y.x)[e] > g || ((&y.x)[e] == g && j + e < group);
+  }
+  better += __shfl_xor_sync(0xffffffffu, better, 1);
+  if (shares == 4) better += __shfl_xor_sync(0xffffffffu, better, 2);
+  if (better == k - 1) sh.floor_x = fmaxf(g, -3.402823466e38f);
+  __syncthreads();
+}
+// Leaves out of a list that holds all that reached earlier floors what does not reach the last one.
+__device__ __noinline__ void thin_list(TsShared& sh, float m, int k) {
+  constexpr int kMine = kTsList / kTsThreads;
+  raise_floor(sh, m, k);
+  const float floor_x = sh.floor_x;
+  const int n = sh.count;
+  u64 key[kMine];
+#pragma unroll
+  for (int r = 0; r < kMine; ++r) key[r] = r * kTsThreads + threadIdx.x < n ? sh.list[r * kTsThreads + threadIdx.x] : 0ull;
+  __syncthreads();
+  if (threadIdx.x == 0) sh.count = 0;
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < kMine; ++r)
+    if (key[r] != 0ull && candidate_score(key[r]) >= floor_x) sh.list[atomicAdd(&sh.count, 1)] = key[r];
+  __syncthreads();
+}
+
+// The list of a block's elements [lo, hi) from the beginning, for any order of them; every thread calls.
+template <int kType>
+__device__ __noinline__ void list_again(TsShared& sh, int k, const unsigned char* x0, const uint4* src, int lo, int hi, int first,
+                                        int vectors, int behind) {
+  using E = TsType<kType>;
+  const int tid = threadIdx.x;
+  __syncthreads();
+  if (tid == 0) { sh.count = 0; sh.floor = 0; }
+  __syncthreads();
+  // (a round more than there are vectors to go through: the elements in front and behind)
+  for (int at = -kTsThreads; at < vectors; at += kTsThreads) {
+    uint4 w = make_uint4(E::kNone, E::kNone, E::kNone, E::kNone);
+    int token = first + (at + tid) * E::kPer;
+    uint32_t wait = 0;
+    if (at < 0) {
+      const int one = tid < first - lo ? lo + tid : tid >= 32 && tid - 32 < hi - behind ? behind + tid - 32 : -1;
+      if (one >= 0) {
+        const float x = E::one(x0 + (long long)one * E::kBytes);
+        w.x = kType == kTsF32 ? __float_as_uint(x) : pack16<kType == kTsBf16>(x, x);
+        token = one;
+        wait = 1;
+      }
+    } else if (at + tid < vectors) {
+      w = ld_stream16(src + at + tid);
+      wait = (2u << (E::kPer - 1)) - 1u;
+    }
+    for (;;) {
+      const u64 floor = sh.floor;
+#pragma unroll
+      for (int e = 0; e < E::kPer; ++e) {
+        const float x = E::get(w, e);
+        const u64 key = x == x ? pack_candidate(x, token + e) : 0ull;
+        if (key <= floor) wait &= ~(1u << e);
+        if (wait >> e & 1u) {
+          const int to = atomicAdd(&sh.count, 1);
+          if (to < kTsList) {
+            sh.list[to] = key;
+            wait &= ~(1u << e);
+          }
+        }
+      }
+      if (!__syncthreads_or(wait != 0)) break;
+      cut_list(sh, kTsList, k);
+    }
+  }
 }
 
 }  // namespace
@@ -130,7 +245,7 @@ token_scores_kernel(const TsArgs a, int parts) {
   int single = -1;
   if (tid < first - lo) single = lo + tid;
   else if (tid >= 32 && tid - 32 < hi - behind) single = behind + tid - 32;
-  if (kTop && tid == 0) { sh.count = 0; sh.floor = 0; }
+  if (kTop && tid == 0) { sh.count = 0; sh.floor = 0; sh.floor_x = -INFINITY; }
 
   uint4 v[kTsUnroll];
   auto load = [&](uint4 (&to)[kTsUnroll], int at) {
@@ -145,14 +260,18 @@ token_scores_kernel(const TsArgs a, int parts) {
   float alone = -INFINITY;
   if (single >= 0) alone = E::one(x0 + (long long)single * E::kBytes);
 
-  int at = 0;
+  float floor_x = -INFINITY;
+  int at = 0, again = 0;
   do {
     uint4 next[kTsUnroll];
     load(next, at + kTsUnroll * kTsThreads);
     // ---- sums ----
-    float top = alone;
+    float high[kTsUnroll], top = alone;
 #pragma unroll
-    for (int i = 0; i < E::kAll; ++i) top = fmaxf(top, E::get(v, i));
+    for (int i = 0; i < kTsUnroll; ++i) {
+      high[i] = E::largest(v[i]);
+      top = fmaxf(top, high[i]);
+    }
     if (top > t.m) {
       const float d = max_nan((t.m - top) * kLog2e, -400.f), f = exp2_approx(d);
       t.e = f * fmaf(t.s, d, t.e);
@@ -165,12 +284,27 @@ token_scores_kernel(const TsArgs a, int parts) {
       float2 s = make_float2(0.f, 0.f), e = make_float2(0.f, 0.f);
 #pragma unroll
       for (int i = 0; i < E::kAll; i += 2) {
-        float2 z = mul2(add2(make_float2(E::get(v, i), E::get(v, i + 1)), b2), l2);
-        z.x = max_nan(z.x, -400.f);                      // (2^-400 is 0; so that 0 times z is, too)
-        z.y = max_nan(z.y, -400.f);
+        const uint4& w = v[i / E::kPer];
+        const float2 z = mul2(add2(make_float2(E::get(w, i % E::kPer), E::get(w, i % E::kPer + 1)), b2), l2);
         const float2 p = make_float2(exp2_approx(z.x), exp2_approx(z.y));
         s = add2(s, p);
         e = fma2(p, z, e);
+      }
+      if (!(e.x + e.y > -INFINITY)) {                    // 0 times -inf, or something is NaN: again, with care
+        s = e = make_float2(0.f, 0.f);
+#pragma unroll 1
+        for (int i = 0; i < kTsUnroll; ++i) {
+          uint4 w = v[0];
+#pragma unroll
+          for (int j = 1; j < kTsUnroll; ++j)
+            if (j == i) w = v[j];
+#pragma unroll
+          for (int k = 0; k < E::kPer; ++k) {
+            const float z = max_nan((E::get(w, k) + base) * kLog2e, -400.f), p = exp2_approx(z);     // (2^-400 is 0)
+            s.x += p;
+            e.x = fmaf(p, z, e.x);
+          }
+        }
       }
       t.s += s.x + s.y;
       t.e += e.x + e.y;
@@ -182,75 +316,41 @@ token_scores_kernel(const TsArgs a, int parts) {
     }
     // ---- the k best ----
     if (kTop) {
-      const int mine = (at + tid) * E::kPer + first;     // the token of the thread's first element
-      auto token = [&](int i) { return mine + i / E::kPer * kTsThreads * E::kPer + i % E::kPer; };
-      auto key_of = [&](int i) -> u64 {                  // 0: none (behind the row's end, or NaN)
-        const float x = E::get(v, i);
-        return token(i) < behind && x == x ? pack_candidate(x, token(i)) : 0ull;
+      if (at == again) {
+        again = 4 * at + 3 * kTsUnroll * kTsThreads;
+        raise_floor(sh, t.m, a.k);
+        floor_x = sh.floor_x;
+      }
+      auto add = [&](float x, int token) {
+        const int to = atomicAdd(&sh.count, 1);
+        if (to < kTsList) sh.list[to] = pack_candidate(x, token);
       };
-      auto key_alone = [&]() -> u64 { return single >= 0 && alone == alone ? pack_candidate(alone, single) : 0ull; };
-      __syncthreads();                                   // the floor of the round before; the list's beginning
-      u64 floor = sh.floor;
-      bool above = floor == 0ull || top >= candidate_score(floor);
-      const int many = __syncthreads_count(above);
-      if (many > 0) {
-        if (many > kTsThreads / 2) {
-          // the k-th best of 64 groups' best
-          float x = -INFINITY;
-          int tok = -1;
+      if (top >= floor_x) {
+        uint32_t hits = 0;                               // sixteen bytes that hold something for the list
 #pragma unroll
-          for (int i = 0; i < E::kAll; ++i) {            // (tokens ascend: the first of equal ones stays)
-            const float y = E::get(v, i);
-            if (token(i) < behind && (y > x || (tok < 0 && y == y))) { x = y; tok = token(i); }
-          }
-          u64 best = tok >= 0 ? pack_candidate(x, tok) : 0ull;
-          if (key_alone() > best) best = key_alone();
+        for (int i = 0; i < kTsUnroll; ++i) hits |= (uint32_t)(high[i] >= floor_x) << i;
+        for (; hits; hits &= hits - 1) {
+          const int i = __ffs(hits) - 1;
+          uint4 w = v[0];
 #pragma unroll
-          for (int o = 1; o < 4; o <<= 1) {
-            const u64 y = shfl_xor_u64(best, o);
-            best = y > best ? y : best;
+          for (int j = 1; j < kTsUnroll; ++j)
+            if (j == i) w = v[j];
+          // (what stands for elements behind the row's end is -inf, below every floor)
+          const int token = first + (at + i * kTsThreads + tid) * E::kPer;
+          uint32_t these = 0;
+#pragma unroll
+          for (int e = 0; e < E::kPer; ++e) these |= (uint32_t)(E::get(w, e) >= floor_x) << e;
+          for (; these; these &= these - 1) {
+            const int e = __ffs(these) - 1;
+            uint32_t x = w.x;
+#pragma unroll
+            for (int j = 1; j < 4; ++j)
+              if (j == e * E::kBytes / 4) x = (&w.x)[j];
+            if (kType != kTsF32 && e & 1) x >>= 16;
+            add(kType == kTsF32 ? __uint_as_float(x) : half_lo<kType == kTsBf16>(x), token + e);
           }
-          if ((lane & 3) == 0) sh.scratch[tid >> 2] = best;
-          __syncthreads();
-          if (warp == 0) {
-            u64 g[2] = {sh.scratch[lane], sh.scratch[32 + lane]};
-            warp_sort_desc<2>(g, lane);
-            const u64 kth = warp_list_get<2>(g, a.k - 1);
-            // (one below: the k-th itself belongs on the list)
-            if (lane == 0 && kth > 0ull && kth - 1 > sh.floor) sh.floor = kth - 1;
-          }
-          __syncthreads();
-          floor = sh.floor;
-          above = floor == 0ull || top >= candidate_score(floor);
         }
-        uint64_t wait = 0;                               // elements above the floor that are not on the list yet
-        if (above) {
-#pragma unroll
-          for (int i = 0; i < E::kAll; ++i) wait |= (uint64_t)(key_of(i) > floor) << i;
-          wait |= (uint64_t)(key_alone() > floor) << E::kAll;
-        }
-        for (;;) {
-          if (wait) {
-#pragma unroll
-            for (int i = 0; i <= E::kAll; ++i)
-              if (wait >> i & 1) {
-                const int to = atomicAdd(&sh.count, 1);
-                if (to < kTsList) {
-                  sh.list[to] = i < E::kAll ? key_of(i < E::kAll ? i : 0) : key_alone();
-                  wait &= ~(1ull << i);
-                }
-              }
-          }
-          if (!__syncthreads_or(wait != 0)) break;
-          cut_list(sh, kTsList, a.k);
-          floor = sh.floor;
-#pragma unroll
-          for (int i = 0; i <= E::kAll; ++i)
-            if (wait >> i & 1) {
-              const u64 key = i < E::kAll ? key_of(i < E::kAll ? i : 0) : key_alone();
-              if (key <= floor) wait &= ~(1ull << i);
-            }
-        }
+        if (single >= 0 && alone >= floor_x) add(alone, single);
       }
     }
     single = -1;
@@ -261,17 +361,24 @@ token_scores_kernel(const TsArgs a, int parts) {
   } while (at < vectors);
 
   // ---- joined: threads, warps, blocks ----
+  const float own = t.m;
+  {
+    float m = own;
 #pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    TsSums y;
-    y.m = __shfl_xor_sync(0xffffffffu, t.m, o);
-    y.s = __shfl_xor_sync(0xffffffffu, t.s, o);
-    y.e = __shfl_xor_sync(0xffffffffu, t.e, o);
-    t = joined(t, y);
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    t = brought_to(t, m);
+    t.s = warp_sum(t.s);
+    t.e = warp_sum(t.e);
   }
   if (lane == 0) sh.sums[warp] = t;
   __syncthreads();
-  if (kTop) cut_list(sh, min(sh.count, kTsList), a.k);
+  if (kTop) {
+    const int n = sh.count;                              // (all that follows has a barrier before its first change)
+    if (n > kTsList || n < min(a.k, hi - lo)) list_again<kType>(sh, a.k, x0, src, lo, hi, first, vectors, behind);
+    else if (n > kTsThreads / 2) thin_list(sh, own, a.k);
+    // (short lists of a row's blocks are cut together)
+    if (parts == 1 || sh.count * parts > kTsThreads) cut_list(sh, sh.count, a.k);
+  }
   t = sh.sums[0];
 #pragma unroll
   for (int w = 1; w < kTsWarps; ++w) t = joined(t, sh.sums[w]);
@@ -280,27 +387,18 @@ token_scores_kernel(const TsArgs a, int parts) {
     __syncthreads();
     if (tid == 0) sh.sums[0] = t;
     cluster.sync();
-    if (rank == 0 && warp == 0) {
-      u64 best[2];
-      if (kTop) {
-#pragma unroll
-        for (int r = 0; r < 2; ++r) best[r] = r * 32 + lane < sh.count ? sh.list[r * 32 + lane] : 0ull;
-      }
-      for (int p = 1; p < parts; ++p) {
-        const TsShared* other = cluster.map_shared_rank(&sh, p);
-        t = joined(t, other->sums[0]);
-        if (kTop) {
-          u64 y[2];
-          const int n = other->count;
-#pragma unroll
-          for (int r = 0; r < 2; ++r) y[r] = r * 32 + lane < n ? other->list[r * 32 + lane] : 0ull;
-          warp_merge_desc<2>(best, y, lane);
+    if (rank == 0) {
+      for (int p = 1; p < parts; ++p) t = joined(t, cluster.map_shared_rank(&sh, p)->sums[0]);
+      if (kTop) {                                        // of at most kTsList / kTsMaxParts each
+        int n = sh.count;
+        for (int p = 1; p < parts; ++p) {
+          const TsShared* other = cluster.map_shared_rank(&sh, p);
+          const int more = other->count;
+          for (int i = tid; i < more; i += kTsThreads) sh.list[n + i] = other->list[i];
+          n += more;
         }
-      }
-      if (kTop) {
-#pragma unroll
-        for (int r = 0; r < 2; ++r) sh.list[r * 32 + lane] = best[r];
-        if (lane == 0) sh.count = min(a.k, a.vocab);
+        __syncthreads();
+        cut_list(sh, n, a.k);
       }
     }
     cluster.sync();                                      // (nobody leaves while its shared memory is read)
