@@ -2,20 +2,25 @@
 //
 //   w_j = sum over rows i >= j - (c - n) and the key head's query heads of r_i exp(scale q_i.k_j - lse_i)
 //
-// A block takes items of 256 keys of one key head, in two groups A and B of 128 that stay in shared
-// memory, and goes through the query rows that see them in tiles of 128: 128 / pack tokens of `pack` query
-// heads.  S = Q K^T as in attention, a row of TMEM a query row: its lse and its weight are two numbers of the
-// thread's, and the thread adds its row's share to 128 sums in registers, one a key, over all tiles.
-// Only every sixteenth tile, and at the item's end, are the sums added up over the lanes, to totals that
-// carry along what each addition loses (a key may receive 10^5 terms).  (With a key a thread, S = K Q^T,
-// nothing would have to be added up, but every exponent needs its row's two numbers from shared memory,
-// and somebody to bring them there: 3,200 cycles a tile, where the exponentials take 1,024.)  Warps:
-//   0-3, 4-7   sums of A and of B
-//   8          loads by tensor maps: the next item's keys (two places), then this one's queries
-//   9          issues the products
-// Rows that do not count (behind the sequence's last one, weight 0, lse -inf) are not added, whatever
-// they hold.  Leading and trailing rows with weight 0 are left out of the tiles: all warps look for the first
-// and the last other one of each long sequence when the kernel begins.
+// The product is taken the other way round than in attention, S = K Q^T: a row of TMEM is a key, its columns
+// are query rows, so that a thread adds up one key's weight over all rows in registers and nothing is
+// joined between lanes.  A block takes items of 256 keys of one key head, in two groups A and B of 128 that
+// stay in shared memory, and goes through the query rows that see them in tiles of 128: 128 / pack tokens
+// of `pack` query heads.  Warps:
+//   0-3, 4-7, 8-11, 12-15   sums of A over the first and the last 64 columns, of B: a key a thread
+//   16         loads by tensor maps: the next item's keys (two places), then this one's queries
+//   17         issues the products
+//   18, 19     bring what a row's exponent begins with, -lse log2 e, and its weight r to shared memory
+// What counts is to have four warps an SM quarter: their chains of a load from TMEM, exponent, sum hide each other.
+// (With a query row a thread and 128 sums a thread there were registers for two, and a tile took 3,400 cycles,
+// where its exponentials take 2,048.)
+// Rows that do not count (behind the sequence's last one, weight 0, lse -inf) have -inf there, and their
+// scores are replaced, so that it does not matter what they hold.  Leading and trailing rows with weight 0
+// are left out of the tiles: all warps look for the first and the last other one of each long sequence
+// when the kernel begins.
+//
+// Sums are fp32: of a tile's 64 columns as four, and over the tiles with the part that each addition
+// loses carried along (a key may receive 10^5 terms).
 //
 // Where there are fewer items than SMs the rows of an item are shared by a cluster of blocks, whose
 // totals are added in order.
@@ -32,10 +37,12 @@ namespace oilbird {
 
 namespace {
 
-constexpr int kPwThreads = 384, kPwLoader = 8, kPwIssuer = 9;
-constexpr int kPwSumRegs = 224, kPwRestRegs = 56;
-static_assert(2 * kPwSumRegs + kPwRestRegs <= 3 * 168, "more registers than the block was launched with");
-constexpr int kPwTogether = 16;                          // tiles that are added up in one go
+constexpr int kPwThreads = 640, kPwSumWarps = 16, kPwLoader = 16, kPwIssuer = 17, kPwRows = 18;
+// registers a thread: launched with 96; the five warpgroups' shares add up to 5 x 96
+constexpr int kPwSumRegs = 104, kPwRestRegs = 64;
+static_assert(4 * kPwSumRegs + kPwRestRegs <= 5 * 96, "more registers than the block was launched with");
+constexpr int kPwHalf = 64;                              // a thread's columns of a tile
+constexpr int kPwAhead = 4;                              // places for the rows' numbers
 constexpr int kPwLong = 512;                             // rows of a sequence whose ends are looked at
 
 struct PwItem {
@@ -47,10 +54,13 @@ struct PwItem {
   int live;
 };
 struct PwShared {
-  uint64_t full[8], free[8], kfull[2], kfree[2], sfull[2][2], sfree[2][2], item_full[2], item_free[2], meet[2];
+  uint64_t full[8], free[8], kfull[2], kfree[2], sfull[2][2], sfree[2][2], item_full[2], item_free[2], meet;
+  uint64_t rows_full[kPwAhead], rows_free[kPwAhead];
   PwItem item[2];
-  float sums[2][2][4][kPrTile];                          // [item's parity][group][warp]: totals
-  float shared[2][kPrTile];                              // of the block, for the cluster
+  alignas(16) float bias[kPwAhead][kPrTile], weight[kPwAhead][kPrTile];      // of a tile's rows, read four at a time
+  int plain[kPwAhead][2];                                // all of a half count, with weight 1
+  float sums[2][2][2 * kPrTile];                         // [item's parity][half of the columns][key]
+  float shared[2 * kPrTile];                             // of the block, for the cluster
   int from[kPrMaxSeq], to[kPrMaxSeq];                    // rows of a sequence that count
   uint32_t tmem;
   int gave_up;
@@ -149,13 +159,17 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
       bar_init(&sh.kfree[i], 1);
       for (int b = 0; b < 2; ++b) {
         bar_init(&sh.sfull[i][b], 1);
-        bar_init(&sh.sfree[i][b], 4);
+        bar_init(&sh.sfree[i][b], 8);
       }
       bar_init(&sh.item_full[i], 1);
-      bar_init(&sh.item_free[i], 9);
-      bar_init(&sh.meet[i], 4);
+      bar_init(&sh.item_free[i], kPwSumWarps + 3);
       sh.item[i].live = 0;
     }
+    for (int i = 0; i < kPwAhead; ++i) {
+      bar_init(&sh.rows_full[i], 2);
+      bar_init(&sh.rows_free[i], kPwSumWarps);
+    }
+    bar_init(&sh.meet, kPwSumWarps);
     sh.gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -173,130 +187,98 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
   const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
   const int span = kPrTile / a.pack, packs = a.group / a.pack;
 
-  if (warp < 8) {
+  if (warp < kPwSumWarps) {
     // ============================================================ sums ===========
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPwSumRegs));
-    const int wg = warp >> 2, row = tid & 127;
-    const uint32_t s_tm = tmem + ((uint32_t)(warp & 3) << 21) + wg * 256;
-    const int row_tok = row / a.pack, row_head = row % a.pack;
-    uint32_t su = 0;
-    bool ok = true;
+    const int half = warp >> 2 & 1, wg = warp >> 3, row = tid & 127, col0 = half * kPwHalf;
+    const uint32_t s_tm = tmem + ((uint32_t)(warp & 3) << 21) + wg * 256 + col0;
+    const float2 f2 = make_float2(a.factor, a.factor);
+    uint32_t u = 0, su = 0;
     for (uint32_t iu = 0;; ++iu) {
       if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, gave_up, a.stats)) break;
-      const PwItem it = sh.item[iu & 1];
+      const PwItem& now = sh.item[iu & 1];
+      const int live = now.live, begin = now.begin, end = now.end, tiles = now.tiles, skip = wg ? now.skip : 0, from = now.from;
+      const int s = now.s, head = now.head, c = now.c, k0 = now.k0, key = now.key0 + wg * kPrTile + row;
+      const int first_row = key - (c - now.n);           // the first row that sees the key
       __syncwarp();
       if (lane == 0) bar_arrive(&sh.item_free[iu & 1]);
-      if (!it.live) break;
-      const int shift = it.c - it.n, key0 = it.key0 + wg * kPrTile;
-      const long long seq = a.qs.first ? 0 : it.s;
-      const float* lse = a.lse + seq * a.lse_seq + it.q0 * a.lse_row;
-      const float* rw = a.row_weight ? a.row_weight + seq * a.qs.rows + it.q0 : nullptr;
-      float total[4] = {0.f, 0.f, 0.f, 0.f}, lost[4] = {0.f, 0.f, 0.f, 0.f};
-      float2 acc[64];
+      if (!live) break;
+      float total = 0.f, lost = 0.f;
+      bool ok = true;
+      int t = tiles > 0 ? begin % tiles : 0;
+      for (int i = begin; i < end; ++i, ++u, t = t + 1 == tiles ? 0 : t + 1) {
+        const uint32_t rs = u % kPwAhead, b = su & 1;
+        // (also where nothing is done with the tile: its place is given back once each time it is full)
+        if (!warp_wait(&sh.rows_full[rs], (u / kPwAhead) & 1, gave_up, a.stats)) { ok = false; break; }
+        if (t >= skip) {
+          if (!warp_wait(&sh.sfull[wg][b], (su >> 1) & 1, gave_up, a.stats)) { ok = false; break; }
+          fence_after();
+          ++su;
+          // columns whose rows do not see the key
+          const int blind = min(max(first_row - (from + t * span), 0), span) * a.pack - col0;
+          const float4* bias = reinterpret_cast<const float4*>(sh.bias[rs] + col0);
+          const float4* weight = reinterpret_cast<const float4*>(sh.weight[rs] + col0);
+          const bool plain = sh.plain[rs][half] && __all_sync(0xffffffffu, blind <= 0);
+          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+          uint32_t x[2][16];
+          tmem_ask16(s_tm + b * 128, x[0]);
 #pragma unroll
-      for (int e = 0; e < 64; ++e) acc[e] = make_float2(0.f, 0.f);
-      // the lanes' sums of 128 keys: each step leaves half of the keys to either half of the lanes
-      auto add_up = [&]() {
-        float v[64];
-        const bool h16 = lane & 16;
+          for (int k = 0; k < kPwHalf / 16; ++k) {
+            uint32_t (&y)[16] = x[k & 1];
+            tmem_wait16(y);
+            if (k + 1 < kPwHalf / 16) tmem_ask16(s_tm + b * 128 + (k + 1) * 16, x[(k + 1) & 1]);
+            else {
+              fence_before();
+              __syncwarp();
+              if (lane == 0) bar_arrive(&sh.sfree[wg][b]);
+            }
+            if (plain) {
 #pragma unroll
-        for (int e = 0; e < 64; ++e) {
-          const float lo = e & 1 ? acc[e >> 1].y : acc[e >> 1].x, hi = e & 1 ? acc[32 + (e >> 1)].y : acc[32 + (e >> 1)].x;
-          v[e] = (h16 ? hi : lo) + __shfl_xor_sync(0xffffffffu, h16 ? lo : hi, 16);
-        }
+              for (int e = 0; e < 4; ++e) {
+                const float4 bb = bias[4 * k + e];
+                const float2 z0 = fma2(make_float2(__uint_as_float(y[4 * e]), __uint_as_float(y[4 * e + 1])), f2, make_float2(bb.x, bb.y));
+                const float2 z1 = fma2(make_float2(__uint_as_float(y[4 * e + 2]), __uint_as_float(y[4 * e + 3])), f2, make_float2(bb.z, bb.w));
+                sum[0] = add2(sum[0], make_float2(exp2_approx(z0.x), exp2_approx(z0.y)));
+                sum[1] = add2(sum[1], make_float2(exp2_approx(z1.x), exp2_approx(z1.y)));
+              }
+            } else {
 #pragma unroll
-        for (int o = 8, m = 32; o; o >>= 1, m >>= 1) {
-          const bool h = lane & o;
+              for (int e = 0; e < 4; ++e) {
+                const float4 bb = bias[4 * k + e], ww = weight[4 * k + e];
+                float z[4];
 #pragma unroll
-          for (int e = 0; e < m; ++e) v[e] = (h ? v[e + m] : v[e]) + __shfl_xor_sync(0xffffffffu, h ? v[e] : v[e + m], o);
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {                    // keys 4 lane ..
-          const float more = __fadd_rn(v[e], lost[e]), next = __fadd_rn(total[e], more);
+                for (int h = 0; h < 4; ++h)
+                  z[h] = 16 * k + 4 * e + h >= blind && (&bb.x)[h] > -INFINITY ? __uint_as_float(y[4 * e + h]) : -INFINITY;
+                const float2 z0 = fma2(make_float2(z[0], z[1]), f2, make_float2(bb.x, bb.y));
+                const float2 z1 = fma2(make_float2(z[2], z[3]), f2, make_float2(bb.z, bb.w));
+                sum[0] = fma2(make_float2(exp2_approx(z0.x), exp2_approx(z0.y)), make_float2(ww.x, ww.y), sum[0]);
+                sum[1] = fma2(make_float2(exp2_approx(z1.x), exp2_approx(z1.y)), make_float2(ww.z, ww.w), sum[1]);
+              }
+            }
+          }
+          sum[0] = add2(sum[0], sum[1]);
+          const float more = __fadd_rn(__fadd_rn(sum[0].x, sum[0].y), lost), next = __fadd_rn(total, more);
           // (what rounding to `next` lost; nothing once that is infinite or NaN)
-          lost[e] = fabsf(next) < INFINITY ? __fsub_rn(more, __fsub_rn(next, total[e])) : 0.f;
-          total[e] = next;
+          lost = fabsf(next) < INFINITY ? __fsub_rn(more, __fsub_rn(next, total)) : 0.f;
+          total = next;
         }
-#pragma unroll
-        for (int e = 0; e < 64; ++e) acc[e] = make_float2(0.f, 0.f);
-      };
-      // a row's numbers, asked for a tile ahead
-      float l = -INFINITY, w = 0.f;
-      auto ask = [&](int i) {
-        l = -INFINITY;
-        w = 0.f;
-        const int tok = it.from + i % it.tiles * span + row_tok, head = it.head * a.group + i / it.tiles * a.pack + row_head;
-        if (i < it.end && tok < it.to) {
-          l = __ldg(lse + tok * a.lse_row + head * a.lse_head);
-          w = rw ? __ldg(rw + tok) : 1.f;
-        }
-      };
-      int held = 0;
-      if (it.begin < it.end) ask(it.begin);
-      for (int i = it.begin; i < it.end; ++i) {
-        const float my_l = l, my_w = w;
-        ask(i + 1);
-        const int t = i % it.tiles;
-        if (wg && t < it.skip) continue;
-        const uint32_t b = su & 1;
-        if (!warp_wait(&sh.sfull[wg][b], (su >> 1) & 1, gave_up, a.stats)) { ok = false; break; }
-        fence_after();
-        ++su;
-        const bool counts = my_w != 0.f && my_l != -INFINITY;
-        const int see = it.from + t * span + row_tok + shift - key0 + 1;     // keys of the group that the row sees
-        const float2 f2 = make_float2(a.factor, a.factor), b2 = make_float2(-my_l * kLog2e, -my_l * kLog2e), w2 = make_float2(my_w, my_w);
-        const bool all = __all_sync(0xffffffffu, counts && see >= kPrTile), some = __any_sync(0xffffffffu, counts && see > 0);
-        uint32_t x[2][32];
-        if (some) tmem_ask32(s_tm + b * 128, x[0]);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (some) {
-            tmem_wait32(x[k & 1]);
-            if (k < 3) tmem_ask32(s_tm + b * 128 + (k + 1) * 32, x[(k + 1) & 1]);
-          }
-          if (k == 3) {
-            fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(&sh.sfree[wg][b]);
-          }
-          if (all) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float2 z = fma2(make_float2(__uint_as_float(x[k & 1][2 * e]), __uint_as_float(x[k & 1][2 * e + 1])), f2, b2);
-              acc[k * 16 + e] = fma2(make_float2(exp2_approx(z.x), exp2_approx(z.y)), w2, acc[k * 16 + e]);
-            }
-          } else if (counts && see > k * 32) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float z0 = 2 * e + k * 32 < see ? __uint_as_float(x[k & 1][2 * e]) : -INFINITY;
-              const float z1 = 2 * e + 1 + k * 32 < see ? __uint_as_float(x[k & 1][2 * e + 1]) : -INFINITY;
-              const float2 z = fma2(make_float2(z0, z1), f2, b2);
-              acc[k * 16 + e] = fma2(make_float2(exp2_approx(z.x), exp2_approx(z.y)), w2, acc[k * 16 + e]);
-            }
-          }
-          __syncwarp();
-        }
-        if (++held == kPwTogether) {
-          held = 0;
-          add_up();
-        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(&sh.rows_free[rs]);
       }
       if (!ok) break;
-      if (held) add_up();
-      float (&sums)[4][kPrTile] = sh.sums[iu & 1][wg];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sums[warp & 3][4 * lane + e] = total[e] + lost[e];
+      // both halves of the columns
+      float (&sums)[2][2 * kPrTile] = sh.sums[iu & 1];
+      sums[half][wg * kPrTile + row] = total + lost;
       __syncwarp();
-      if (lane == 0) bar_arrive(&sh.meet[wg]);
-      if (!warp_wait(&sh.meet[wg], iu & 1, gave_up, a.stats)) break;
-      const float sum = (sums[0][row] + sums[1][row]) + (sums[2][row] + sums[3][row]);
-      if (shares > 1) {
-        sh.shared[wg][row] = sum;
-        break;                                           // (a cluster has one item)
+      if (lane == 0) bar_arrive(&sh.meet);
+      if (!warp_wait(&sh.meet, iu & 1, gave_up, a.stats)) break;
+      if (half == 0) {
+        const float sum = sums[0][wg * kPrTile + row] + sums[1][wg * kPrTile + row];
+        if (shares > 1) sh.shared[wg * kPrTile + row] = sum;
+        else if (key < (a.ks.first ? c : a.ks.rows))
+          a.weight[((a.ks.first ? 0ll : (long long)s * a.n_kv) + head) * a.ks.rows + k0 + key] = key < c ? sum : 0.f;
       }
-      const int key = key0 + row, keys = a.ks.first ? it.c : a.ks.rows;
-      if (key < keys)
-        a.weight[((a.ks.first ? 0ll : (long long)it.s * a.n_kv) + it.head) * a.ks.rows + it.k0 + key] = key < it.c ? sum : 0.f;
+      if (shares > 1) break;                             // (a cluster has one item)
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPwRestRegs));
@@ -371,6 +353,57 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
         if (!next.live) break;
         cur = next;
       }
+    } else if (warp >= kPwRows) {
+      // ========================================================== the rows' numbers ====
+      const int half = warp - kPwRows, col = half * kPwHalf + 2 * lane;
+      uint32_t u = 0;
+      bool ok = true;
+      for (uint32_t iu = 0; ok; ++iu) {
+        if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, gave_up, a.stats)) break;
+        const PwItem& now = sh.item[iu & 1];
+        const int live = now.live, begin = now.begin, end = now.end, tiles = now.tiles, from = now.from, to = now.to;
+        const int s = a.qs.first ? 0 : now.s, q0 = now.q0, head0 = now.head * a.group;
+        __syncwarp();
+        if (lane == 0) bar_arrive(&sh.item_free[iu & 1]);
+        if (!live) break;
+        const float* lse = a.lse + s * a.lse_seq + q0 * a.lse_row;
+        const float* rw = a.row_weight ? a.row_weight + (long long)s * a.qs.rows + q0 : nullptr;
+        // two rows a lane, asked for a tile ahead
+        float l[2] = {-INFINITY, -INFINITY}, w[2] = {0.f, 0.f};
+        auto ask = [&](int i) {
+          const int pack = i / tiles, tok0 = from + (i - pack * tiles) * span;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int tok = tok0 + (col + e) / a.pack, hd = head0 + pack * a.pack + (col + e) % a.pack;
+            l[e] = -INFINITY;
+            w[e] = 0.f;
+            if (tok < to) {
+              l[e] = __ldg(lse + tok * a.lse_row + hd * a.lse_head);
+              w[e] = rw ? __ldg(rw + tok) : 1.f;
+            }
+          }
+        };
+        if (begin < end) ask(begin);
+        for (int i = begin; i < end; ++i, ++u) {
+          const uint32_t rs = u % kPwAhead, use = u / kPwAhead;
+          float2 bias, weight;
+          bool counts[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            counts[e] = w[e] != 0.f && l[e] != -INFINITY;
+            (&bias.x)[e] = counts[e] ? -l[e] * kLog2e : -INFINITY;
+            (&weight.x)[e] = counts[e] ? w[e] : 0.f;
+          }
+          if (i + 1 < end) ask(i + 1);
+          const bool plain = __all_sync(0xffffffffu, counts[0] && counts[1] && weight.x == 1.f && weight.y == 1.f);
+          if (use > 0 && !warp_wait(&sh.rows_free[rs], (use - 1) & 1, gave_up, a.stats)) { ok = false; break; }
+          *reinterpret_cast<float2*>(sh.bias[rs] + col) = bias;
+          *reinterpret_cast<float2*>(sh.weight[rs] + col) = weight;
+          if (lane == 0) sh.plain[rs][half] = plain;
+          __syncwarp();
+          if (lane == 0) bar_arrive(&sh.rows_full[rs]);
+        }
+      }
     } else if (warp == kPwIssuer) {
       // ========================================================== products =======
       const uint32_t idesc = idesc_16(kPrTile, false, kBf16) | (a.negate ? kNegateA : 0u);
@@ -406,7 +439,7 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
 #pragma unroll
               for (int k = 0; k < D / 16; ++k) {
                 const uint64_t off = (uint64_t)((k >> 2) * (kPrTile * 128 >> 4) + (k & 3) * 2);
-                mma_ss(tmem + g * 256 + b * 128, qd + off, kd + g * kStage + off, idesc, k > 0);
+                mma_ss(tmem + g * 256 + b * 128, kd + g * kStage + off, qd + off, idesc, k > 0);
               }
               commit(&sh.sfull[g][b]);
             }
@@ -436,12 +469,12 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
   if (shares > 1) {
     cg::cluster_group cluster = cg::this_cluster();
     cluster.sync();
-    if (rank == 0 && warp < 8) {
+    if (rank == 0 && tid < 2 * kPrTile) {                // a key a thread
       const PwItem& it = sh.item[0];
       if (it.live) {
-        const int wg = warp >> 2, row = tid & 127, key = it.key0 + tid, keys = a.ks.first ? it.c : a.ks.rows;
-        float sum = sh.shared[wg][row];
-        for (int r = 1; r < shares; ++r) sum += cluster.map_shared_rank(&sh, r)->shared[wg][row];
+        const int key = it.key0 + tid, keys = a.ks.first ? it.c : a.ks.rows;
+        float sum = sh.shared[tid];
+        for (int r = 1; r < shares; ++r) sum += cluster.map_shared_rank(&sh, r)->shared[tid];
         if (key < keys)
           a.weight[((a.ks.first ? 0ll : (long long)it.s * a.n_kv) + it.head) * a.ks.rows + it.k0 + key] = key < it.c ? sum : 0.f;
       }
