@@ -36,67 +36,72 @@ struct PromptArgs {
   bool negate;               // the scale is negative
 };
 
-// Extents of all sequences in shared memory.
+// Extents of all sequences, and the numbers of items by level (see prompt_levels), in shared memory.
+constexpr int kPrLevels = 256;
 struct PromptList {
-  int n[kPrMaxSeq], c[kPrMaxSeq], q0[kPrMaxSeq], k0[kPrMaxSeq];   // rows, keys, where they begin
+  int n[kPrMaxSeq], c[kPrMaxSeq];    // rows, keys
+  int count[kPrLevels + 2], unit, levels;
 };
 
 // Offsets and counts are the caller's: whatever they hold, rows stay inside the arrays.
-__device__ __forceinline__ void prompt_extent(const PromptSide& p, int s, int& at, int& n) {
-  if (p.first) {
-    at = min(max(p.first[s], 0), p.rows);
-    n = min(max(p.first[s + 1], at), p.rows) - at;
-  } else {
-    at = 0;
-    n = p.count ? min(max(p.count[s], 0), p.rows) : p.rows;
-  }
+__device__ __forceinline__ int prompt_begin(const PromptSide& p, int s) {
+  return p.first ? min(max(p.first[s], 0), p.rows) : 0;
+}
+__device__ __forceinline__ int prompt_rows(const PromptSide& p, int s) {
+  if (!p.first) return p.count ? min(max(p.count[s], 0), p.rows) : p.rows;
+  const int at = prompt_begin(p, s);
+  return min(max(p.first[s + 1], at), p.rows) - at;
 }
 __device__ __forceinline__ void prompt_extents(const PromptArgs& a, PromptList& l) {
   for (int s = threadIdx.x; s < a.n_seq; s += blockDim.x) {
-    prompt_extent(a.qs, s, l.q0[s], l.n[s]);
-    prompt_extent(a.ks, s, l.k0[s], l.c[s]);
+    l.n[s] = prompt_rows(a.qs, s);
+    l.c[s] = prompt_rows(a.ks, s);
   }
 }
 
-__device__ __forceinline__ long long warp_sum_i64(long long v) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-
-// The list of work is not stored.  Items are numbered by falling level (tiles they have to go
-// through), so that the last ones are short; a warp finds number i by a search over the levels, then over
-// the sequences, while the item before it is worked on.  `level`: any that no item from i on passes; becomes the item's.
+// The list of work is not stored.  Items are numbered by falling level (tiles they have to go through, in
+// units that make up to kPrLevels of them), so that the last ones are short.  How many items have a level
+// or more is counted once, when the kernel begins, by all threads; a warp then finds number i by going down
+// the levels from the last item's and through the sequences, while the item before it is worked on.  (A search
+// that counted anew for each item took 6 us an item, which short prompts waited for.)
 template <class Order>
-__device__ __forceinline__ bool prompt_find(const Order& order, int n_seq, long long i, int lane, int& level, int& s_out, int& t_out) {
-  auto count = [&](int x) {
-    long long v = 0;
-    for (int s = lane; s < n_seq; s += 32) v += order.items(s, x);
-    return warp_sum_i64(v);
-  };
-  if (count(0) <= i) return false;
-  int lo = 0, hi = level;
-  while (lo < hi) {                                      // the largest level with more than i items
-    const int mid = lo + (hi - lo + 1) / 2;
-    if (count(mid) > i) lo = mid; else hi = mid - 1;
+__device__ __forceinline__ void prompt_levels(const Order& order, int n_seq, PromptList& l) {
+  __shared__ int most;                                   // tiles of the longest item
+  if (threadIdx.x == 0) most = 0;
+  __syncthreads();
+  for (int s = threadIdx.x; s < n_seq; s += blockDim.x) atomicMax(&most, order.most_tiles(s));
+  __syncthreads();
+  const int unit = max(1, (most + kPrLevels - 1) / kPrLevels), levels = (most + unit - 1) / unit;
+  if (threadIdx.x == 0) { l.unit = unit; l.levels = levels; }
+  for (int x = threadIdx.x; x <= levels + 1; x += blockDim.x) {
+    int v = 0;
+    for (int s = 0; s < n_seq; ++s) v += order.items(s, x, unit);
+    l.count[x] = v;
   }
-  level = lo;
-  long long left = i - count(lo + 1);                    // place among the items of this level
+}
+// `level`: any that no item from i on passes (at first l.levels); becomes the item's.  A warp.
+template <class Order>
+__device__ __forceinline__ bool prompt_find(const Order& order, int n_seq, const PromptList& l, int i, int lane, int& level, int& s_out,
+                                            int& t_out) {
+  if (l.count[0] <= i) return false;
+  while (l.count[level] <= i) --level;                   // the largest level with more than i items
+  const int unit = l.unit;
+  int left = i - l.count[level + 1];                     // place among the items of this level
   for (int s0 = 0; s0 < n_seq; s0 += 32) {
     const int s = s0 + lane;
-    const int above = s < n_seq ? order.items(s, lo + 1) : 0, all = s < n_seq ? order.items(s, lo) : 0;
-    const long long here = all - above;
-    long long sum = here;
+    const int above = s < n_seq ? order.items(s, level + 1, unit) : 0, all = s < n_seq ? order.items(s, level, unit) : 0;
+    const int here = all - above;
+    int sum = here;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long y = __shfl_up_sync(0xffffffffu, sum, o);
+      const int y = __shfl_up_sync(0xffffffffu, sum, o);
       if (lane >= o) sum += y;
     }
     const unsigned hit = __ballot_sync(0xffffffffu, left < sum);
     if (hit) {
       const int at = __ffs(hit) - 1;
       s_out = s0 + at;
-      t_out = order.item(s_out, lo, (int)(left - __shfl_sync(0xffffffffu, sum - here, at)), __shfl_sync(0xffffffffu, all, at),
+      t_out = order.item(s_out, level, left - __shfl_sync(0xffffffffu, sum - here, at), __shfl_sync(0xffffffffu, all, at),
                          __shfl_sync(0xffffffffu, above, at));
       return true;
     }

@@ -7,10 +7,10 @@
 // head, in two groups A and B of 128.  `pack` query heads that share the key head lie side by side, so a
 // group is 128 / pack tokens: every tile of keys serves all of them, and fewer keys lie beyond the
 // diagonal.  Warps:
-//   0-3, 4-7   softmax of A and of B, one row a thread: scores from TMEM, maximum, exponentials, and
-//              the probabilities in 16 bits back over the scores
-//   8          loads: queries, then keys and values in turn into a ring, by tensor maps
-//   9          issues the products S = Q K^T and O += P V (P from TMEM)
+//   0-7, 8-15  softmax of A and of B, 16 rows a warp, four lanes to a row: scores from TMEM, maximum,
+//              exponentials, and the probabilities in 16 bits back over the scores
+//   16         loads: queries, then keys and values in turn into a ring, by tensor maps
+//   17         issues the products S = Q K^T and O += P V (P from TMEM)
 // While A's scores go through the exponentials the tensor core works for B, and the other way round.
 //
 // Numbers.  Scores, maxima, sums and accumulators are fp32.  Probabilities are rounded to the inputs'
@@ -35,10 +35,10 @@ namespace oilbird {
 
 namespace {
 
-constexpr int kPaThreads = 384, kPaLoader = 8, kPaIssuer = 9;
-// registers a thread: launched with 168; the three warpgroups' shares add up to 3 x 168
-constexpr int kPaSoftRegs = 224, kPaRestRegs = 56;
-static_assert(2 * kPaSoftRegs + kPaRestRegs <= 3 * 168, "more registers than the block was launched with");
+constexpr int kPaThreads = 640, kPaSoftWarps = 16, kPaLoader = 16, kPaIssuer = 17;
+// registers a thread: launched with 96; the five warpgroups' shares add up to 5 x 96
+constexpr int kPaSoftRegs = 112, kPaRestRegs = 32;
+static_assert(4 * kPaSoftRegs + kPaRestRegs <= 5 * 96, "more registers than the block was launched with");
 constexpr float kPaLn2 = 0.6931471805599453f;
 constexpr int kPaSlack = 8;
 
@@ -49,7 +49,7 @@ struct PaItem {
   int live;                          // 0: no item is left
 };
 struct PaShared {
-  uint64_t full[16], free[16], qfull, qfree, sfull[2], pfull[2], ofull[2], item_full[2], item_free[2];
+  uint64_t full[16], free[16], qfull, qfree, sfull[2], pfull[2][2], ofull[2], item_full[2], item_free[2];
   PaItem item[2];
   uint32_t tmem;
   int gave_up;
@@ -67,15 +67,18 @@ struct Pa {
 // lies behind a sequence's rows is written too.
 struct PaOrder {
   const PromptList* l;
-  int span, padded;                  // padded: rows to write for every sequence (0: packed)
-  __device__ __forceinline__ int there(int s) const { return (l->n[s] + span - 1) / span; }
-  // items of sequence s with `level` key tiles or more
-  __device__ __forceinline__ int items(int s, int level) const {
-    if (level == 0) return padded ? (padded + span - 1) / span : there(s);
-    const long long keys = (long long)(level - 1) * kPrTile;             // the last row of the item sees more than these
-    if (l->c[s] <= keys) return 0;
-    const long long d = keys - ((long long)l->c[s] - l->n[s]);
-    return max(there(s) - (d > 0 ? (int)min(d / span, (long long)there(s)) : 0), 0);
+  int log_span, padded;              // tokens of an item; rows to write for every sequence (0: packed)
+  __device__ __forceinline__ int ceil(int rows) const { return (int)(((unsigned)rows + (1u << log_span) - 1) >> log_span); }
+  __device__ __forceinline__ int there(int s) const { return ceil(l->n[s]); }
+  __device__ __forceinline__ int most_tiles(int s) const { return (l->c[s] + kPrTile - 1) / kPrTile; }
+  // items of sequence s with `level` units of key tiles or more
+  __device__ __forceinline__ int items(int s, int level, int unit) const {
+    if (level == 0) return padded ? ceil(padded) : there(s);
+    const int c = l->c[s], n = l->n[s];
+    const long long keys = (long long)(level - 1) * unit * kPrTile;      // the last row of the item sees more than these
+    if (c <= keys) return 0;
+    const long long d = (keys - c + n) >> log_span;
+    return d > 0 ? (int)max(there(s) - d, 0ll) : there(s);
   }
   // the `at`-th item of sequence s among those of one level; `all` items have that level or more, `above` more
   __device__ __forceinline__ int item(int s, int level, int at, int all, int above) const {
@@ -161,10 +164,10 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
     bar_init(&sh.qfree, 1);
     for (int i = 0; i < 2; ++i) {
       bar_init(&sh.sfull[i], 1);
-      bar_init(&sh.pfull[i], 4);
+      for (int h = 0; h < 2; ++h) bar_init(&sh.pfull[i][h], kPaSoftWarps / 2);
       bar_init(&sh.ofull[i], 1);
       bar_init(&sh.item_full[i], 1);
-      bar_init(&sh.item_free[i], 9);
+      bar_init(&sh.item_free[i], kPaSoftWarps + 1);
     }
     sh.gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -175,88 +178,121 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
   }
   pdl_enter();
   prompt_extents(a, list);
+  const PaOrder order = {&list, 31 - __clz(2 * kPrTile / a.pack), a.qs.first ? 0 : a.qs.rows};
+  __syncthreads();
+  prompt_levels(order, a.n_seq, list);
   fence_before();
   __syncthreads();
   fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
   const int span = kPrTile / a.pack;                     // tokens of a group
 
-  if (warp < 8) {
+  if (warp < kPaSoftWarps) {
     // ============================================================ softmax ========
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPaSoftRegs));
-    const int wg = warp >> 2, row = tid & 127;
-    const uint32_t lanes = (uint32_t)(warp & 3) << 21;
-    const uint32_t s_tm = tmem + lanes + wg * 128, o_tm = tmem + lanes + 256 + wg * 128;
-    const int row_tok = wg * span + row / a.pack, row_head = row % a.pack;
+    const int wg = warp >> 3, quad = lane & 3;
+    const int row0 = (warp & 3) * 32 + (warp >> 2 & 1) * 16 + (lane >> 2);       // the lane's rows: this one and 8 on
+    const uint32_t s_tm = tmem + ((uint32_t)((warp & 3) * 32 + (warp >> 2 & 1) * 16) << 16) + wg * 128, o_tm = s_tm + 256;
     const float2 g2 = make_float2(a.factor, a.factor);
     uint32_t su = 0, ou = 0;
     bool ok = true;
     for (uint32_t iu = 0; ok; ++iu) {
       if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, gave_up, a.stats)) break;
-      const PaItem it = sh.item[iu & 1];
-      __syncwarp();
-      if (lane == 0) bar_arrive(&sh.item_free[iu & 1]);
-      if (!it.live) break;
-      const int tok = it.tok + row_tok, head = it.q_head + row_head;
-      const bool have = tok < it.n;
-      const int vis = have ? min(it.c, it.c - it.n + tok + 1) : 0;       // keys the row sees (0 or less: none)
-      const int n_tiles = it.tiles[wg];
-      float m = -INFINITY, l = 0.f;
+      // (read again where the rows are written: there are no registers to keep it in)
+      volatile const PaItem& now = sh.item[iu & 1];
+      if (!now.live) break;
+      const int n_tiles = now.tiles[wg];
+      int vis[2];                                        // keys the row sees (0 or less: none)
+      float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int tok = now.tok + wg * span + (row0 + 8 * r) / a.pack, n = now.n, c = now.c;
+        vis[r] = tok < n ? min(c, c - n + tok + 1) : 0;
+      }
       for (int j = 0; j < n_tiles; ++j, ++su) {
         if (!warp_wait(&sh.sfull[wg], su & 1, gave_up, a.stats)) { ok = false; break; }
         fence_after();
-        uint32_t x[128];
+        uint32_t x[64];
+        tmem_ask_rows(s_tm, x);
+        tmem_wait_rows(x);
+        if (__any_sync(0xffffffffu, min(vis[0], vis[1]) < (j + 1) * kPrTile)) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) tmem_ask32(s_tm + k * 32, x + k * 32);
+          for (int r = 0; r < 2; ++r) {
+            const int see = vis[r] - j * kPrTile - 2 * quad;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) tmem_wait32(x + k * 32);
-        const int see = vis - j * kPrTile;
-        if (__any_sync(0xffffffffu, see < kPrTile)) {
-#pragma unroll
-          for (int e = 0; e < 128; ++e) x[e] = e < see ? x[e] : 0xff800000u;
-        }
-        float y[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int e = 0; e < 64; ++e) y[e & 3] = max3(y[e & 3], __uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1]));
-        const float mx = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])) * a.factor;
-        if (__any_sync(0xffffffffu, mx > m + kPaSlack)) {
-          // (each row for itself; the products so far are done, or there were no scores)
-          const float mn = mx > m + kPaSlack ? mx : m, down = mn == -INFINITY ? 1.f : exp2_approx(m - mn);
-          m = mn;
-          l *= down;
-          if (j > 0) {
-#pragma unroll 1
-            for (int k = 0; k < D; k += 16) {
-              uint32_t r[16];
-              tmem_ld16(o_tm + k, r);
-#pragma unroll
-              for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * down);
-              tmem_st16(o_tm + k, r);
+            for (int i = 0; i < 16; ++i) {
+              if (8 * i >= see) x[4 * i + 2 * r] = 0xff800000u;
+              if (8 * i + 1 >= see) x[4 * i + 2 * r + 1] = 0xff800000u;
             }
           }
         }
-        const float shift = kRoom - (m == -INFINITY ? 0.f : m);
-        const float2 shift2 = make_float2(shift, shift);
-        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        float mx[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float y[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+          for (int i = 0; i < 16; ++i) y[i & 1] = max3(y[i & 1], __uint_as_float(x[4 * i + 2 * r]), __uint_as_float(x[4 * i + 2 * r + 1]));
+          mx[r] = fmaxf(y[0], y[1]);
+        }
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+          mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], o));
+          mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], o));
+        }
+        mx[0] *= a.factor;
+        mx[1] *= a.factor;
+        if (__any_sync(0xffffffffu, mx[0] > m[0] + kPaSlack || mx[1] > m[1] + kPaSlack)) {
+          // (each row for itself; the products so far are done, or there were no scores)
+          float down[2];
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const float mn = mx[r] > m[r] + kPaSlack ? mx[r] : m[r];
+            down[r] = mn == -INFINITY ? 1.f : exp2_approx(m[r] - mn);
+            m[r] = mn;
+            l[r] *= down[r];
+          }
+          if (j > 0) {
+#pragma unroll 1
+            for (int k = 0; k < D; k += 32) {
+              uint32_t r[16];
+              tmem_ask_rows(o_tm + k, r);
+              tmem_wait_rows(r);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * down[e >> 1 & 1]);
+              tmem_st_rows(o_tm + k, r);
+            }
+          }
+        }
+        float2 shift2[2], sum[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float shift = kRoom - (m[r] == -INFINITY ? 0.f : m[r]);
+          shift2[r] = make_float2(shift, shift);
+          sum[r] = make_float2(0.f, 0.f);
+        }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          uint32_t w[16];
+          uint32_t w[8];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int i2 = k * 32 + 2 * e;
-            const float2 z = fma2(make_float2(__uint_as_float(x[i2]), __uint_as_float(x[i2 + 1])), g2, shift2);
-            const float2 pr = make_float2(exp2_approx(z.x), exp2_approx(z.y));
-            sum[e & 1] = add2(sum[e & 1], pr);
-            w[e] = pack16<kBf16>(pr.x, pr.y);
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const int e = 16 * k + 4 * i + 2 * r;
+              const float2 z = fma2(make_float2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), g2, shift2[r]);
+              const float2 pr = make_float2(exp2_approx(z.x), exp2_approx(z.y));
+              sum[r] = add2(sum[r], pr);
+              w[2 * i + r] = pack16<kBf16>(pr.x, pr.y);
+            }
+          tmem_st_pairs(s_tm + k * 16, w);               // over the scores
+          if (k & 1) {                                   // a half of the keys: their product can begin
+            tmem_wait_st();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(&sh.pfull[wg][k >> 1]);
           }
-          tmem_st16(s_tm + k * 16, w);                   // over the scores
         }
-        sum[0] = add2(sum[0], sum[1]);
-        l += sum[0].x + sum[0].y;
-        tmem_wait_st();
-        fence_before();
-        __syncwarp();
-        if (lane == 0) bar_arrive(&sh.pfull[wg]);
+        l[0] += sum[0].x + sum[0].y;
+        l[1] += sum[1].x + sum[1].y;
       }
       if (!ok) break;
       if (n_tiles > 0) {
@@ -264,51 +300,83 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         fence_after();
       }
       // ---- out ----
-      const bool write = tok < (a.qs.first ? it.n : a.qs.rows);
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      const long long seq = a.qs.first ? 0 : it.s, r = (long long)it.q0 + tok;
-      uint16_t* op = a.out + seq * a.out_seq + r * a.out_row + head * a.out_head;
-      bool odd = false;
+      const PaItem it = sh.item[iu & 1];
+      int tok[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) tok[r] = it.tok + wg * span + (row0 + 8 * r) / a.pack;
+      const long long seq = a.qs.first ? 0 : it.s;
+      float inv[2];
+      uint16_t* op[2];
+      bool write[2], odd[2] = {false, false};
+      int head[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+        inv[r] = l[r] == 0.f ? 0.f : 1.f / l[r];
+        write[r] = tok[r] < (a.qs.first ? it.n : a.qs.rows);
+        head[r] = it.q_head + (row0 + 8 * r) % a.pack;
+        op[r] = a.out + seq * a.out_seq + ((long long)it.q0 + tok[r]) * a.out_row + head[r] * a.out_head + 8 * quad;
+        if (write[r] && a.lse && quad == 0)
+          a.lse[seq * a.lse_seq + ((long long)it.q0 + tok[r]) * a.lse_row + head[r] * a.lse_head] =
+              l[r] == 0.f ? -INFINITY : (m[r] - kRoom + log2f(l[r])) * kPaLn2;
+      }
 #pragma unroll 1
       for (int k = 0; k < D; k += 32) {
-        float o[32];
-        if (n_tiles > 0) tmem_ld32(o_tm + k, o);
+        uint32_t o[16];
+        if (n_tiles > 0) {
+          tmem_ask_rows(o_tm + k, o);
+          tmem_wait_rows(o);
+        }
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          uint32_t w[4];
+        for (int r = 0; r < 2; ++r) {
+          uint32_t w[4];                                 // columns 8i + 2 quad, .. of the 32
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float u0 = o[8 * h + 2 * e] * inv, u1 = o[8 * h + 2 * e + 1] * inv;
-            odd |= !(fabsf(u0) < INFINITY) || !(fabsf(u1) < INFINITY);
-            w[e] = l == 0.f ? 0u : pack16<kBf16>(u0, u1);
+          for (int i = 0; i < 4; ++i) {
+            const float u0 = __uint_as_float(o[4 * i + 2 * r]) * inv[r], u1 = __uint_as_float(o[4 * i + 2 * r + 1]) * inv[r];
+            odd[r] |= !(fabsf(u0) < INFINITY) || !(fabsf(u1) < INFINITY);
+            w[i] = l[r] == 0.f ? 0u : pack16<kBf16>(u0, u1);
           }
-          if (write) *reinterpret_cast<uint4*>(op + k + 8 * h) = make_uint4(w[0], w[1], w[2], w[3]);
+          // the row's four lanes swap, so that each has eight columns that lie together
+          uint4 v;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int other = quad ^ x;
+            const uint32_t give = other == 0 ? w[0] : other == 1 ? w[1] : other == 2 ? w[2] : w[3];
+            const uint32_t take = x ? __shfl_xor_sync(0xffffffffu, give, x) : give;
+            if (other == 0) v.x = take;
+            else if (other == 1) v.y = take;
+            else if (other == 2) v.z = take;
+            else v.w = take;
+          }
+          if (write[r]) *reinterpret_cast<uint4*>(op[r] + k) = v;
         }
       }
-      if (write && a.lse)
-        a.lse[seq * a.lse_seq + r * a.lse_row + head * a.lse_head] = l == 0.f ? -INFINITY : (m - kRoom + log2f(l)) * kPaLn2;
-      odd = odd && have && l != 0.f && n_tiles > 0;
-      unsigned rows = __ballot_sync(0xffffffffu, odd);
-      if (rows) {
-        const int least = __reduce_min_sync(0xffffffffu, odd ? vis : 0x7fffffff);
-        if (!odd_values<D, kBf16>(a, it, least, n_tiles * kPrTile, lane)) rows = 0;
-        for (; rows; rows &= rows - 1) {
-          const int at = __ffs(rows) - 1;
-          row_again<D, kBf16>(a, it, __shfl_sync(0xffffffffu, tok, at), __shfl_sync(0xffffffffu, head, at),
-                              __shfl_sync(0xffffffffu, vis, at), __shfl_sync(0xffffffffu, m, at) - kRoom,
-                              __shfl_sync(0xffffffffu, l, at), lane);
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        unsigned rows = __ballot_sync(0xffffffffu, odd[r] && tok[r] < it.n && l[r] != 0.f && n_tiles > 0);
+        rows |= rows >> 1;
+        rows = (rows | rows >> 2) & 0x11111111u;         // a row's first lane
+        if (rows) {
+          const int least = __reduce_min_sync(0xffffffffu, vis[r]);
+          if (!odd_values<D, kBf16>(a, it, least, n_tiles * kPrTile, lane)) rows = 0;
+          for (; rows; rows &= rows - 1) {
+            const int at = __ffs(rows) - 1;
+            row_again<D, kBf16>(a, it, __shfl_sync(0xffffffffu, tok[r], at), __shfl_sync(0xffffffffu, head[r], at),
+                                __shfl_sync(0xffffffffu, vis[r], at), __shfl_sync(0xffffffffu, m[r], at) - kRoom,
+                                __shfl_sync(0xffffffffu, l[r], at), lane);
+          }
         }
       }
       fence_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(&sh.item_free[iu & 1]);
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPaRestRegs));
     if (warp == kPaLoader) {
       // ========================================================== loads ==========
-      const PaOrder order = {&list, 2 * span, a.qs.first ? 0 : a.qs.rows};
-      int level = 0;                                     // of the last item found: the next one has no more
-      for (int s = lane; s < a.n_seq; s += 32) level = max(level, (list.c[s] + kPrTile - 1) / kPrTile);
-      level = __reduce_max_sync(0xffffffffu, level);
+      int level = list.levels;                           // of the last item found: the next one has no more
       const int heads = a.n_kv * (a.group / a.pack);
       const bool leader = one_lane();
       uint32_t u = 0, qu = 0;
@@ -317,7 +385,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         const long long i = (long long)iu * gridDim.x + (iu & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
         const int hd = (int)(i % heads);
         int s = 0, t = 0;
-        const bool live = prompt_find(order, a.n_seq, i / heads, lane, level, s, t);
+        const bool live = prompt_find(order, a.n_seq, list, (int)(i / heads), lane, level, s, t);
         PaItem it;
         it.live = live;
         it.s = s;
@@ -326,8 +394,8 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         it.q_head = hd * a.pack;
         it.n = list.n[s];
         it.c = list.c[s];
-        it.q0 = list.q0[s];
-        it.k0 = list.k0[s];
+        it.q0 = prompt_begin(a.qs, s);
+        it.k0 = prompt_begin(a.ks, s);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
           const int last = min(it.n, it.tok + (g + 1) * span) - 1;       // the group's last row that is there
@@ -421,16 +489,21 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
           for (int g = 0; g < 2; ++g) {
             const int mine = g ? tiles1 : tiles0;
             if (j < mine) {
-              if (!warp_wait(&sh.pfull[g], pu[g]++ & 1, gave_up, a.stats)) { ok = false; break; }
-              fence_after();
               const uint64_t vd = v_desc + (vu % P::kStages) * kStage;
-              if (leader) {
 #pragma unroll
-                for (int k = 0; k < kPrTile / 16; ++k)
-                  mma_ts(tmem + 256 + g * 128, tmem + g * 128 + k * 8, vd + (uint64_t)(k * 2048 >> 4), o_idesc, j > 0 || k > 0);
-                if (j + 1 == mine) commit(&sh.ofull[g]);
+              for (int h = 0; h < 2 && ok; ++h) {        // half of the keys at a time, as the probabilities come
+                if (!warp_wait(&sh.pfull[g][h], pu[g] & 1, gave_up, a.stats)) { ok = false; break; }
+                fence_after();
+                if (leader) {
+#pragma unroll
+                  for (int k = h * kPrTile / 32; k < (h + 1) * kPrTile / 32; ++k)
+                    mma_ts(tmem + 256 + g * 128, tmem + g * 128 + k * 8, vd + (uint64_t)(k * 2048 >> 4), o_idesc, j > 0 || k > 0);
+                  if (h == 1 && j + 1 == mine) commit(&sh.ofull[g]);
+                }
+                __syncwarp();
               }
-              __syncwarp();
+              ++pu[g];
+              if (!ok) break;
               if (j + 1 < mine) scores(g, ku);
             }
           }

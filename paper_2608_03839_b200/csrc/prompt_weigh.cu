@@ -77,13 +77,13 @@ struct Pw {
 // Items of 256 keys; those with more rows lie in front.
 struct PwOrder {
   const PromptList* l;
-  int span, padded;                  // padded: keys to write for every sequence (0: packed)
-  __device__ __forceinline__ int items(int s, int level) const {
-    if (level == 0) return ((padded ? padded : l->c[s]) + 2 * kPrTile - 1) / (2 * kPrTile);
-    const long long rows = (long long)(level - 1) * span;                // the first key of the item is seen by more than these
-    if (l->n[s] <= rows) return 0;
-    const long long keys = l->c[s] - rows;
-    return keys > 0 ? (int)((keys + 2 * kPrTile - 1) / (2 * kPrTile)) : 0;
+  int log_span, padded;              // tokens of a tile; keys to write for every sequence (0: packed)
+  static __device__ __forceinline__ int ceil(int keys) { return (int)(((unsigned)keys + 2 * kPrTile - 1) / (2 * kPrTile)); }
+  __device__ __forceinline__ int most_tiles(int s) const { return (int)(((unsigned)l->n[s] + (1u << log_span) - 1) >> log_span); }
+  __device__ __forceinline__ int items(int s, int level, int unit) const {
+    if (level == 0) return ceil(padded ? padded : l->c[s]);
+    const long long rows = ((long long)(level - 1) * unit) << log_span;  // the first key of the item is seen by more than these
+    return l->n[s] <= rows || l->c[s] <= rows ? 0 : ceil((int)(l->c[s] - rows));
   }
   __device__ __forceinline__ int item(int, int, int at, int, int above) const { return above + at; }
 };
@@ -91,7 +91,7 @@ struct PwOrder {
 // The rows [from, to) of each long sequence outside which all weights are 0; every thread calls.
 __device__ __forceinline__ void live_rows(const PromptArgs& a, const PromptList& l, PwShared& sh) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  auto weights = [&](int s) { return a.row_weight + (a.qs.first ? 0ll : (long long)s * a.qs.rows) + l.q0[s]; };
+  auto weights = [&](int s) { return a.row_weight + (a.qs.first ? 0ll : (long long)s * a.qs.rows) + prompt_begin(a.qs, s); };
   for (int s = tid; s < a.n_seq; s += kPwThreads) {
     const int n = l.n[s];
     const bool look = a.row_weight && n > kPwLong && (weights(s)[0] == 0.f || weights(s)[n - 1] == 0.f);
@@ -180,6 +180,8 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
   pdl_enter();
   prompt_extents(a, list);
   __syncthreads();
+  const PwOrder order = {&list, 31 - __clz(kPrTile / a.pack), a.ks.first ? 0 : a.ks.rows};
+  prompt_levels(order, a.n_seq, list);
   live_rows(a, list, sh);
   fence_before();
   __syncthreads();
@@ -284,10 +286,7 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPwRestRegs));
     if (warp == kPwLoader) {
       // ========================================================== loads ==========
-      const PwOrder order = {&list, span, a.ks.first ? 0 : a.ks.rows};
-      int level = 0;
-      for (int s = lane; s < a.n_seq; s += 32) level = max(level, (list.n[s] + span - 1) / span);
-      level = __reduce_max_sync(0xffffffffu, level);
+      int level = list.levels;
       const bool leader = one_lane();
       const int crew = gridDim.x / shares, me = blockIdx.x / shares;
       uint32_t u = 0, ku = 0;
@@ -299,14 +298,14 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
         // ---- the next item, and its keys ----
         const long long i = (long long)iu * crew + (iu & 1 ? crew - 1 - me : me);
         int s = 0, t = 0;
-        next.live = (shares == 1 || iu == 0) && prompt_find(order, a.n_seq, i / a.n_kv, lane, level, s, t);
+        next.live = (shares == 1 || iu == 0) && prompt_find(order, a.n_seq, list, (int)(i / a.n_kv), lane, level, s, t);
         next.s = s;
         next.head = (int)(i % a.n_kv);
         next.key0 = t * 2 * kPrTile;
         next.n = list.n[s];
         next.c = list.c[s];
-        next.q0 = list.q0[s];
-        next.k0 = list.k0[s];
+        next.q0 = prompt_begin(a.qs, s);
+        next.k0 = prompt_begin(a.ks, s);
         const int shift = next.c - next.n;
         next.from = max(max(sh.from[s], next.key0 - shift), 0);
         next.to = sh.to[s];
