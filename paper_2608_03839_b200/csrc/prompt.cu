@@ -88,6 +88,7 @@ static int check_prompt(const oilbird_prompt* p, PromptArgs* a) {
   a->n_kv = p->n_kv_heads;
   a->group = p->n_q_heads / p->n_kv_heads;
   a->pack = a->group & -a->group;
+  while (1 << a->log_pack < a->pack) ++a->log_pack;
   return OILBIRD_OK;
 }
 // The stride of an extent of one is never used, so it may be anything; a packed side has no sequences.

@@ -31,7 +31,7 @@ struct PromptArgs {
   float* weight;             // weigh: [n_seq, n_kv, key rows] or [n_kv, key rows]
   DeviceStats* stats;
   int n_seq, n_kv, group;
-  int pack;                  // query heads that lie side by side in a tile: a power of two that divides group
+  int pack, log_pack;        // query heads that lie side by side in a tile: a power of two that divides group
   float factor;              // |scale| log2 e
   bool negate;               // the scale is negative
 };

@@ -178,14 +178,14 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
   }
   pdl_enter();
   prompt_extents(a, list);
-  const PaOrder order = {&list, 31 - __clz(2 * kPrTile / a.pack), a.qs.first ? 0 : a.qs.rows};
+  const PaOrder order = {&list, 8 - a.log_pack, a.qs.first ? 0 : a.qs.rows};
   __syncthreads();
   prompt_levels(order, a.n_seq, list);
   fence_before();
   __syncthreads();
   fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
-  const int span = kPrTile / a.pack;                     // tokens of a group
+  const int span = kPrTile >> a.log_pack;                    // tokens of a group
 
   if (warp < kPaSoftWarps) {
     // ============================================================ softmax ========
@@ -206,7 +206,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        const int tok = now.tok + wg * span + (row0 + 8 * r) / a.pack, n = now.n, c = now.c;
+        const int tok = now.tok + wg * span + ((row0 + 8 * r) >> a.log_pack), n = now.n, c = now.c;
         vis[r] = tok < n ? min(c, c - n + tok + 1) : 0;
       }
       for (int j = 0; j < n_tiles; ++j, ++su) {
@@ -300,26 +300,30 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         fence_after();
       }
       // ---- out ----
+      // (Once a tile of short prompts: every instruction counts.  A row's four lanes swap their words in two steps, so
+      // that each has eight columns that lie together.)
       const PaItem it = sh.item[iu & 1];
-      int tok[2];
-#pragma unroll
-      for (int r = 0; r < 2; ++r) tok[r] = it.tok + wg * span + (row0 + 8 * r) / a.pack;
       const long long seq = a.qs.first ? 0 : it.s;
-      float inv[2];
+      const float zero = 0.f;
+      float2 inv[2], odd2[2];
       uint16_t* op[2];
-      bool write[2], odd[2] = {false, false};
-      int head[2];
+      int tok[2], head[2];
+      bool write[2], odd[2];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
         l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-        inv[r] = l[r] == 0.f ? 0.f : 1.f / l[r];
+        const float i = l[r] == 0.f ? 0.f : __frcp_rn(l[r]);
+        inv[r] = make_float2(i, i);
+        odd2[r] = make_float2(0.f, 0.f);
+        tok[r] = it.tok + wg * span + ((row0 + 8 * r) >> a.log_pack);
+        head[r] = it.q_head + ((row0 + 8 * r) & (a.pack - 1));
         write[r] = tok[r] < (a.qs.first ? it.n : a.qs.rows);
-        head[r] = it.q_head + (row0 + 8 * r) % a.pack;
-        op[r] = a.out + seq * a.out_seq + ((long long)it.q0 + tok[r]) * a.out_row + head[r] * a.out_head + 8 * quad;
+        const long long row = (long long)it.q0 + tok[r];
+        op[r] = a.out + seq * a.out_seq + row * a.out_row + head[r] * a.out_head + 8 * quad;
         if (write[r] && a.lse && quad == 0)
-          a.lse[seq * a.lse_seq + ((long long)it.q0 + tok[r]) * a.lse_row + head[r] * a.lse_head] =
-              l[r] == 0.f ? -INFINITY : (m[r] - kRoom + log2f(l[r])) * kPaLn2;
+          a.lse[seq * a.lse_seq + row * a.lse_row + head[r] * a.lse_head] =
+              l[r] == 0.f ? -INFINITY : (m[r] - kRoom + __log2f(l[r])) * kPaLn2;
       }
 #pragma unroll 1
       for (int k = 0; k < D; k += 32) {
@@ -333,25 +337,26 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
           uint32_t w[4];                                 // columns 8i + 2 quad, .. of the 32
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float u0 = __uint_as_float(o[4 * i + 2 * r]) * inv[r], u1 = __uint_as_float(o[4 * i + 2 * r + 1]) * inv[r];
-            odd[r] |= !(fabsf(u0) < INFINITY) || !(fabsf(u1) < INFINITY);
-            w[i] = l[r] == 0.f ? 0u : pack16<kBf16>(u0, u1);
+            const float2 u = mul2(make_float2(__uint_as_float(o[4 * i + 2 * r]), __uint_as_float(o[4 * i + 2 * r + 1])), inv[r]);
+            odd2[r] = fma2(u, make_float2(zero, zero), odd2[r]);             // (NaN once one is not finite)
+            w[i] = l[r] == 0.f ? 0u : pack16<kBf16>(u.x, u.y);
           }
-          // the row's four lanes swap, so that each has eight columns that lie together
-          uint4 v;
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const int other = quad ^ x;
-            const uint32_t give = other == 0 ? w[0] : other == 1 ? w[1] : other == 2 ? w[2] : w[3];
-            const uint32_t take = x ? __shfl_xor_sync(0xffffffffu, give, x) : give;
-            if (other == 0) v.x = take;
-            else if (other == 1) v.y = take;
-            else if (other == 2) v.z = take;
-            else v.w = take;
+          for (int x = 2; x; x >>= 1) {
+            const bool up = quad & x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (!(i & x)) {
+                const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[i] : w[i + x], x);
+                w[i] = up ? got : w[i];
+                w[i + x] = up ? w[i + x] : got;
+              }
           }
-          if (write[r]) *reinterpret_cast<uint4*>(op[r] + k) = v;
+          if (write[r]) *reinterpret_cast<uint4*>(op[r] + k) = make_uint4(w[0], w[1], w[2], w[3]);
         }
       }
+#pragma unroll
+      for (int r = 0; r < 2; ++r) odd[r] = !(odd2[r].x + odd2[r].y == 0.f);
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         unsigned rows = __ballot_sync(0xffffffffu, odd[r] && tok[r] < it.n && l[r] != 0.f && n_tiles > 0);

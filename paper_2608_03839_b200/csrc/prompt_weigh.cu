@@ -180,14 +180,14 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
   pdl_enter();
   prompt_extents(a, list);
   __syncthreads();
-  const PwOrder order = {&list, 31 - __clz(kPrTile / a.pack), a.ks.first ? 0 : a.ks.rows};
+  const PwOrder order = {&list, 7 - a.log_pack, a.ks.first ? 0 : a.ks.rows};
   prompt_levels(order, a.n_seq, list);
   live_rows(a, list, sh);
   fence_before();
   __syncthreads();
   fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
-  const int span = kPrTile / a.pack, packs = a.group / a.pack;
+  const int span = kPrTile >> a.log_pack, packs = a.group >> a.log_pack;
 
   if (warp < kPwSumWarps) {
     // ============================================================ sums ===========
@@ -373,7 +373,7 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
           const int pack = i / tiles, tok0 = from + (i - pack * tiles) * span;
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const int tok = tok0 + (col + e) / a.pack, hd = head0 + pack * a.pack + (col + e) % a.pack;
+            const int tok = tok0 + ((col + e) >> a.log_pack), hd = head0 + pack * a.pack + ((col + e) & (a.pack - 1));
             l[e] = -INFINITY;
             w[e] = 0.f;
             if (tok < to) {
