@@ -26,10 +26,18 @@
 // Work.  Items by falling number of key tiles, so that the last ones are the short ones; block b takes
 // b, 2G-1-b, 2G+b, ... of G blocks (see prompt_find).
 //
+// Where there are fewer items than SMs (few rows, over many keys perhaps) the key tiles of an item are shared
+// by a cluster of blocks.  Each leaves its rows' maxima, sums and accumulators in its shared memory, and a
+// part of the rows is joined by each block, in the order of the keys.
+//
 // Every wait is bounded (two seconds unless set otherwise): a wait that runs out raises `stalled`, all
 // roles leave, TMEM is freed.
+#include <cooperative_groups.h>
+
 #include "prompt.cuh"
 #include "tensor.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace oilbird {
 
@@ -45,12 +53,15 @@ constexpr int kPaSlack = 8;
 struct PaItem {
   int s, tok, head, q_head;          // sequence, first token, key head, first query head
   int n, c, q0, k0;
-  int tiles[2];                      // of A and of B
+  int tiles[2];                      // of A and of B: all that their rows see
+  int begin;                         // this block's: from here on,
+  int end[2];                        // up to here
   int live;                          // 0: no item is left
 };
 struct PaShared {
-  uint64_t full[16], free[16], qfull, qfree, sfull[2], pfull[2][2], ofull[2], item_full[2], item_free[2];
+  uint64_t full[16], free[16], qfull, qfree, sfull[2], pfull[2][2], ofull[2], item_full[2], item_free[2], meet;
   PaItem item[2];
+  float2 ml[256];                                        // a cluster's: maxima and sums of A's rows and B's
   uint32_t tmem;
   int gave_up;
 };
@@ -61,6 +72,9 @@ struct Pa {
   static constexpr int kStages = D == 128 ? 4 : 8;
   static constexpr int kBytes = 1024 + (2 + kStages) * kMat + (int)sizeof(PaShared) + 16 + (int)sizeof(PromptList);
   static_assert(kBytes <= 227 * 1024, "shared memory");
+  // accumulators of a block of a cluster, over the tiles; rows spread over the banks
+  static constexpr int kRow = D + 8;
+  static_assert(256 * kRow * 4 <= (2 + kStages) * kMat, "accumulators in the tiles' place");
 };
 
 // Items of 2 `span` tokens.  Those with more keys lie behind those with fewer; in the padded form what
@@ -138,13 +152,83 @@ __device__ __noinline__ bool odd_values(const PromptArgs& a, const PaItem& it, i
   return __any_sync(0xffffffffu, odd);
 }
 
+// every thread of every block of the cluster
+__device__ __forceinline__ void meet_cluster() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The item of a cluster.  First every block leaves its accumulators in its shared memory (a softmax warp its 16 rows) ..
+template <int D>
+__device__ __forceinline__ void leave_rows(float* acc, uint32_t o_tm, int row0) {
+  const int quad = threadIdx.x & 3;
+#pragma unroll 1
+  for (int k = 0; k < D; k += 32) {
+    uint32_t o[16];
+    tmem_ask_rows(o_tm + k, o);
+    tmem_wait_rows(o);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+        *reinterpret_cast<float2*>(acc + (row0 + 8 * r) * Pa<D>::kRow + k + 8 * i + 2 * quad) =
+            make_float2(__uint_as_float(o[4 * i + 2 * r]), __uint_as_float(o[4 * i + 2 * r + 1]));
+  }
+}
+// .. then it joins its part of the 256 rows, a row a softmax warp.
+template <int D, bool kBf16>
+__device__ __noinline__ void join_rows(const PromptArgs& a, const PaItem& it, float* acc, float2* ml, int shares, int rank) {
+  constexpr float kRoom = kBf16 ? 0.f : 7.f;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  cg::cluster_group cluster = cg::this_cluster();
+  constexpr int E = D / 64;                            // pairs of channels a lane
+  const int rows = 256 / shares;
+  for (int i = warp; i < rows; i += kPaSoftWarps) {    // a row a warp
+    const int row = rank * rows + i, wg = row >> 7, tok = it.tok + (row >> a.log_pack), head = it.q_head + (row & (a.pack - 1));
+    if (tok >= (a.qs.first ? it.n : a.qs.rows)) continue;
+    float big = -INFINITY, sum = 0.f;
+    for (int s = 0; s < shares; ++s) big = fmaxf(big, cluster.map_shared_rank(ml, s)[row].x);
+    float2 o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = make_float2(0.f, 0.f);
+    for (int s = 0; s < shares; ++s) {
+      const float2 y = cluster.map_shared_rank(ml, s)[row];
+      if (y.x == -INFINITY && y.y == 0.f) continue;    // it saw nothing there
+      const float f = y.x == big ? 1.f : exp2_approx(y.x - big);
+      const float* from = cluster.map_shared_rank(acc, s) + row * Pa<D>::kRow + 2 * lane;
+      sum = fmaf(f, y.y, sum);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float2 x = *reinterpret_cast<const float2*>(from + 64 * e);
+        o[e].x = fmaf(f, x.x, o[e].x);
+        o[e].y = fmaf(f, x.y, o[e].y);
+      }
+    }
+    const float inv = sum == 0.f ? 0.f : __frcp_rn(sum);
+    const long long seq = a.qs.first ? 0 : it.s, at = (long long)it.q0 + tok;
+    uint16_t* op = a.out + seq * a.out_seq + at * a.out_row + head * a.out_head + 2 * lane;
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float u0 = o[e].x * inv, u1 = o[e].y * inv;
+      odd |= !(fabsf(u0) < INFINITY) || !(fabsf(u1) < INFINITY);
+      *reinterpret_cast<uint32_t*>(op + 64 * e) = sum == 0.f ? 0u : pack16<kBf16>(u0, u1);
+    }
+    if (lane == 0 && a.lse)
+      a.lse[seq * a.lse_seq + at * a.lse_row + head * a.lse_head] = sum == 0.f ? -INFINITY : (big - kRoom + __log2f(sum)) * kPaLn2;
+    const int vis = min(it.c, it.c - it.n + tok + 1);
+    if (__any_sync(0xffffffffu, odd && sum != 0.f) && odd_values<D, kBf16>(a, it, vis, it.tiles[wg] * kPrTile, lane))
+      row_again<D, kBf16>(a, it, tok, head, vis, big - kRoom, sum, lane);
+  }
+}
+
 }  // namespace
 
-template <int D, bool kBf16>
+template <int D, bool kBf16, bool kSplit>
 __global__ void __launch_bounds__(kPaThreads, 1)
 prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
-                     const __grid_constant__ CUtensorMap v_map, const __grid_constant__ PromptArgs a) {
+                     const __grid_constant__ CUtensorMap v_map, const __grid_constant__ PromptArgs a, int blocks) {
   using P = Pa<D>;
+  const int shares = kSplit ? blocks : 1;                // of an item, one a block of a cluster
   constexpr float kRoom = kBf16 ? 0.f : 7.f;
   extern __shared__ unsigned char raw_smem[];
   unsigned char* smem = raw_smem + ((1024 - (kv_smem(raw_smem) & 1023)) & 1023);
@@ -162,6 +246,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
     }
     bar_init(&sh.qfull, 1);
     bar_init(&sh.qfree, 1);
+    bar_init(&sh.meet, kPaSoftWarps);
     for (int i = 0; i < 2; ++i) {
       bar_init(&sh.sfull[i], 1);
       for (int h = 0; h < 2; ++h) bar_init(&sh.pfull[i][h], kPaSoftWarps / 2);
@@ -169,6 +254,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       bar_init(&sh.item_full[i], 1);
       bar_init(&sh.item_free[i], kPaSoftWarps + 1);
     }
+    sh.item[0].live = 0;
     sh.gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -185,7 +271,8 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
   __syncthreads();
   fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
-  const int span = kPrTile >> a.log_pack;                    // tokens of a group
+  const int span = kPrTile >> a.log_pack;                // tokens of a group
+  const int rank = kSplit ? blockIdx.x % shares : 0;     // in the cluster
 
   if (warp < kPaSoftWarps) {
     // ============================================================ softmax ========
@@ -201,7 +288,6 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       // (read again where the rows are written: there are no registers to keep it in)
       volatile const PaItem& now = sh.item[iu & 1];
       if (!now.live) break;
-      const int n_tiles = now.tiles[wg];
       int vis[2];                                        // keys the row sees (0 or less: none)
       float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
@@ -209,7 +295,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         const int tok = now.tok + wg * span + ((row0 + 8 * r) >> a.log_pack), n = now.n, c = now.c;
         vis[r] = tok < n ? min(c, c - n + tok + 1) : 0;
       }
-      for (int j = 0; j < n_tiles; ++j, ++su) {
+      for (int j = now.begin; j < now.end[wg]; ++j, ++su) {
         if (!warp_wait(&sh.sfull[wg], su & 1, gave_up, a.stats)) { ok = false; break; }
         fence_after();
         uint32_t x[64];
@@ -251,7 +337,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
             m[r] = mn;
             l[r] *= down[r];
           }
-          if (j > 0) {
+          if (j > now.begin) {
 #pragma unroll 1
             for (int k = 0; k < D; k += 32) {
               uint32_t r[16];
@@ -295,9 +381,22 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         l[1] += sum[1].x + sum[1].y;
       }
       if (!ok) break;
-      if (n_tiles > 0) {
+      const bool any = now.end[wg] > now.begin;
+      if (any) {
         if (!warp_wait(&sh.ofull[wg], ou++ & 1, gave_up, a.stats)) break;
         fence_after();
+      }
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+      }
+      if (kSplit) {                                      // (a cluster has one item, joined below)
+        if (quad == 0) {
+          sh.ml[wg * 128 + row0] = make_float2(m[0], l[0]);
+          sh.ml[wg * 128 + row0 + 8] = make_float2(m[1], l[1]);
+        }
+        break;
       }
       // ---- out ----
       // (Once a tile of short prompts: every instruction counts.  A row's four lanes swap their words in two steps, so
@@ -311,8 +410,6 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       bool write[2], odd[2];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
         const float i = l[r] == 0.f ? 0.f : __frcp_rn(l[r]);
         inv[r] = make_float2(i, i);
         odd2[r] = make_float2(0.f, 0.f);
@@ -328,7 +425,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
 #pragma unroll 1
       for (int k = 0; k < D; k += 32) {
         uint32_t o[16];
-        if (n_tiles > 0) {
+        if (any) {
           tmem_ask_rows(o_tm + k, o);
           tmem_wait_rows(o);
         }
@@ -359,12 +456,12 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       for (int r = 0; r < 2; ++r) odd[r] = !(odd2[r].x + odd2[r].y == 0.f);
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        unsigned rows = __ballot_sync(0xffffffffu, odd[r] && tok[r] < it.n && l[r] != 0.f && n_tiles > 0);
+        unsigned rows = __ballot_sync(0xffffffffu, odd[r] && tok[r] < it.n && l[r] != 0.f && any);
         rows |= rows >> 1;
         rows = (rows | rows >> 2) & 0x11111111u;         // a row's first lane
         if (rows) {
           const int least = __reduce_min_sync(0xffffffffu, vis[r]);
-          if (!odd_values<D, kBf16>(a, it, least, n_tiles * kPrTile, lane)) rows = 0;
+          if (!odd_values<D, kBf16>(a, it, least, it.tiles[wg] * kPrTile, lane)) rows = 0;
           for (; rows; rows &= rows - 1) {
             const int at = __ffs(rows) - 1;
             row_again<D, kBf16>(a, it, __shfl_sync(0xffffffffu, tok[r], at), __shfl_sync(0xffffffffu, head[r], at),
@@ -377,6 +474,18 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       __syncwarp();
       if (lane == 0) bar_arrive(&sh.item_free[iu & 1]);
     }
+    if (kSplit) {
+      // (the tiles' place is free when both groups have their last products)
+      float* acc = reinterpret_cast<float*>(smem);
+      const PaItem& it = sh.item[0];
+      __syncwarp();
+      if (lane == 0) bar_arrive(&sh.meet);
+      if (warp_wait(&sh.meet, 0, gave_up, a.stats) && it.live && it.end[wg] > it.begin) leave_rows<D>(acc, o_tm, wg * 128 + row0);
+      fence_before();
+      meet_cluster();
+      if (it.live) join_rows<D, kBf16>(a, it, acc, sh.ml, shares, rank);
+      meet_cluster();                                    // (nobody leaves while its shared memory is read)
+    }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPaRestRegs));
     if (warp == kPaLoader) {
@@ -384,13 +493,14 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       int level = list.levels;                           // of the last item found: the next one has no more
       const int heads = a.n_kv * (a.group / a.pack);
       const bool leader = one_lane();
+      const int crew = gridDim.x / shares, me = blockIdx.x / shares;
       uint32_t u = 0, qu = 0;
       bool ok = true;
       for (uint32_t iu = 0; ok; ++iu) {
-        const long long i = (long long)iu * gridDim.x + (iu & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+        const long long i = (long long)iu * crew + (iu & 1 ? crew - 1 - me : me);
         const int hd = (int)(i % heads);
         int s = 0, t = 0;
-        const bool live = prompt_find(order, a.n_seq, list, (int)(i / heads), lane, level, s, t);
+        const bool live = (!kSplit || iu == 0) && prompt_find(order, a.n_seq, list, (int)(i / heads), lane, level, s, t);
         PaItem it;
         it.live = live;
         it.s = s;
@@ -407,13 +517,18 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
           const int vis = last >= it.tok + g * span ? min(it.c, it.c - it.n + last + 1) : 0;
           it.tiles[g] = vis > 0 ? (vis + kPrTile - 1) / kPrTile : 0;
         }
+        const int all = max(it.tiles[0], it.tiles[1]);
+        it.begin = (int)((long long)all * rank / shares);
+        const int end = (int)((long long)all * (rank + 1) / shares);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) it.end[g] = max(min(end, it.tiles[g]), it.begin);
         if (iu >= 2 && !warp_wait(&sh.item_free[iu & 1], ((iu >> 1) - 1) & 1, gave_up, a.stats)) break;
         if (lane == 0) {
           sh.item[iu & 1] = it;
           bar_arrive(&sh.item_full[iu & 1]);
         }
         if (!live) break;
-        const int n_tiles = max(it.tiles[0], it.tiles[1]);
+        const int n_tiles = end - it.begin;
         if (n_tiles == 0) continue;
         const int qs = a.qs.first ? 0 : s, ks = a.ks.first ? 0 : s;
         for (int j = 0; j < 2 * n_tiles && ok; ++j, ++u) {               // K0 (then Q), V0, K1, V1, ..
@@ -424,7 +539,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
 #pragma unroll
             for (int b = 0; b < P::kBlocks; ++b)
               map_load4(kv_smem(ring + st * P::kMat + b * (kPrTile * 128)), j & 1 ? &v_map : &k_map, b * 64, it.head,
-                        it.k0 + (j >> 1) * kPrTile, ks, &sh.full[st]);
+                        it.k0 + (it.begin + (j >> 1)) * kPrTile, ks, &sh.full[st]);
           }
           __syncwarp();
           if (j == 0) {
@@ -455,7 +570,8 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       bool ok = true;
       for (uint32_t iu = 0; ok; ++iu) {
         if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, gave_up, a.stats)) break;
-        const int live = sh.item[iu & 1].live, tiles0 = sh.item[iu & 1].tiles[0], tiles1 = sh.item[iu & 1].tiles[1];
+        const int live = sh.item[iu & 1].live, begin = sh.item[iu & 1].begin, tiles0 = sh.item[iu & 1].end[0] - begin,
+                  tiles1 = sh.item[iu & 1].end[1] - begin;
         __syncwarp();
         if (lane == 0) bar_arrive(&sh.item_free[iu & 1]);
         if (!live) break;
@@ -524,19 +640,22 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       }
     }
   }
+  if (kSplit && warp >= kPaSoftWarps) {
+    __syncwarp();
+    meet_cluster();
+    meet_cluster();
+  }
   fence_before();
   __syncthreads();
-  if (warp == kPaIssuer) {
-    fence_after();
-    // The softmax warps waited for the last products, and the products for the last copies, unless
-    // somebody gave up: then what is in flight gets time to end.  (Read behind the barrier, when nobody
-    // can any more.)
-    if (*gave_up) {
-      const unsigned long long t0 = now_ns();
-      while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
-    }
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  fence_after();
+  // The softmax warps waited for the last products, and the products for the last copies, unless
+  // somebody gave up: then what is in flight gets time to end.  (Read behind the barrier, when nobody
+  // can any more.)
+  if (*gave_up) {
+    const unsigned long long t0 = now_ns();
+    while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
   }
+  if (warp == kPaIssuer) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
 // ------------------------------------------------------------------ host side ---
@@ -576,19 +695,28 @@ static cudaError_t run_attend(const PromptArgs& a, int sms, cudaStream_t st) {
   const long long span = 2 * kPrTile / a.pack;
   const long long tiles = a.qs.first ? a.qs.rows / span + a.n_seq : (long long)a.n_seq * ((a.qs.rows + span - 1) / span);
   const long long items = tiles * a.n_kv * (a.group / a.pack);
-  return launch_pdl(prompt_attend_kernel<D, kBf16>, dim3((unsigned)(items < sms ? items : sms)), dim3(kPaThreads), Pa<D>::kBytes, st,
-                    qm, km, vm, a);
+  // Fewer items than SMs: the keys of each are shared by a cluster (of tiles, as far as there can be some).
+  int shares = 1;
+  while (shares < 8 && items * shares * 2 <= sms && (long long)a.ks.rows > kPrTile * shares) shares *= 2;
+  const unsigned grid = (unsigned)(items < sms ? items * shares : sms);
+  return launch_cluster(shares > 1 ? prompt_attend_kernel<D, kBf16, true> : prompt_attend_kernel<D, kBf16, false>, grid, kPaThreads,
+                        Pa<D>::kBytes, shares, st, qm, km, vm, a, shares);
 }
 cudaError_t launch_prompt_attend(const PromptArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st) {
   if (head_dim == 64) return bf16 ? run_attend<64, true>(a, sms, st) : run_attend<64, false>(a, sms, st);
   return bf16 ? run_attend<128, true>(a, sms, st) : run_attend<128, false>(a, sms, st);
 }
+template <int D, bool kBf16>
+static cudaError_t preload_both() {
+  const cudaError_t e = preload_kernel(prompt_attend_kernel<D, kBf16, false>, true);
+  return e != cudaSuccess ? e : preload_kernel(prompt_attend_kernel<D, kBf16, true>, true);
+}
 cudaError_t preload_prompt_attend_kernels() {
   cudaError_t e;
-  if ((e = preload_kernel(prompt_attend_kernel<64, true>, true)) != cudaSuccess) return e;
-  if ((e = preload_kernel(prompt_attend_kernel<64, false>, true)) != cudaSuccess) return e;
-  if ((e = preload_kernel(prompt_attend_kernel<128, true>, true)) != cudaSuccess) return e;
-  return preload_kernel(prompt_attend_kernel<128, false>, true);
+  if ((e = preload_both<64, true>()) != cudaSuccess) return e;
+  if ((e = preload_both<64, false>()) != cudaSuccess) return e;
+  if ((e = preload_both<128, true>()) != cudaSuccess) return e;
+  return preload_both<128, false>();
 }
 
 }  // namespace oilbird

@@ -497,25 +497,8 @@ static cudaError_t run_weigh(const PromptArgs& a, int sms, cudaStream_t st) {
   // Fewer items than SMs: the rows of each are shared by a cluster.
   int shares = 1;
   while (shares < 8 && items * shares * 2 <= sms) shares *= 2;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(items < sms ? items * shares : sms));
-  cfg.blockDim = dim3(kPwThreads);
-  cfg.dynamicSmemBytes = Pw<D>::kBytes;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  if (shares > 1) {
-    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
-    attr[cfg.numAttrs].val.clusterDim.x = shares;
-    attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
-    ++cfg.numAttrs;
-  }
-  if (!tl_pdl_off && pdl_process_ok()) {
-    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
-    ++cfg.numAttrs;
-  }
-  cfg.attrs = attr;
-  return cudaLaunchKernelEx(&cfg, prompt_weigh_kernel<D, kBf16>, qm, km, a, shares);
+  return launch_cluster(prompt_weigh_kernel<D, kBf16>, (unsigned)(items < sms ? items * shares : sms), kPwThreads, Pw<D>::kBytes, shares,
+                        st, qm, km, a, shares);
 }
 cudaError_t launch_prompt_weigh(const PromptArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st) {
   if (head_dim == 64) return bf16 ? run_weigh<64, true>(a, sms, st) : run_weigh<64, false>(a, sms, st);

@@ -434,24 +434,7 @@ namespace {
 
 template <int kType, bool kTop>
 cudaError_t run_scores(const TsArgs& a, int rows, int parts, cudaStream_t st) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)rows * (unsigned)parts);
-  cfg.blockDim = dim3(kTsThreads);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  if (parts > 1) {
-    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
-    attr[cfg.numAttrs].val.clusterDim.x = parts;
-    attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
-    ++cfg.numAttrs;
-  }
-  if (!tl_pdl_off && pdl_process_ok()) {
-    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
-    ++cfg.numAttrs;
-  }
-  cfg.attrs = attr;
-  return cudaLaunchKernelEx(&cfg, token_scores_kernel<kType, kTop>, a, parts);
+  return launch_cluster(token_scores_kernel<kType, kTop>, (unsigned)rows * (unsigned)parts, kTsThreads, 0, parts, st, a, parts);
 }
 template <int kType>
 cudaError_t run_type(TsArgs a, int rows, int sms, cudaStream_t st) {
