@@ -34,6 +34,8 @@
 // roles leave, TMEM is freed.
 #include <cooperative_groups.h>
 
+#include <atomic>
+
 #include "prompt.cuh"
 #include "tensor.cuh"
 
@@ -681,6 +683,12 @@ bool prompt_map(CUtensorMap* map, const KvRows& r, int head_dim, int heads, int 
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// How many clusters of 16 blocks run at once (0 until it has been asked for, when the kernels are loaded).
+template <int D, bool kBf16>
+static std::atomic<int>& most_clusters() {
+  static std::atomic<int> n(0);
+  return n;
+}
 template <int D, bool kBf16>
 static cudaError_t run_attend(const PromptArgs& a, int sms, cudaStream_t st) {
   CUtensorMap qm, km, vm;
@@ -695,9 +703,11 @@ static cudaError_t run_attend(const PromptArgs& a, int sms, cudaStream_t st) {
   const long long span = 2 * kPrTile / a.pack;
   const long long tiles = a.qs.first ? a.qs.rows / span + a.n_seq : (long long)a.n_seq * ((a.qs.rows + span - 1) / span);
   const long long items = tiles * a.n_kv * (a.group / a.pack);
-  // Fewer items than SMs: the keys of each are shared by a cluster (of tiles, as far as there can be some).
+  // Fewer items than SMs: the keys of each are shared by a cluster (of tiles, as far as there can be some), of 16
+  // blocks where the device takes that many clusters of that size at once.
   int shares = 1;
-  while (shares < 8 && items * shares * 2 <= sms && (long long)a.ks.rows > kPrTile * shares) shares *= 2;
+  while (shares < 16 && items * shares * 2 <= sms && (long long)a.ks.rows > kPrTile * shares) shares *= 2;
+  if (shares == 16 && items > most_clusters<D, kBf16>()) shares = 8;
   const unsigned grid = (unsigned)(items < sms ? items * shares : sms);
   return launch_cluster(shares > 1 ? prompt_attend_kernel<D, kBf16, true> : prompt_attend_kernel<D, kBf16, false>, grid, kPaThreads,
                         Pa<D>::kBytes, shares, st, qm, km, vm, a, shares);
@@ -708,8 +718,25 @@ cudaError_t launch_prompt_attend(const PromptArgs& a, int head_dim, bool bf16, i
 }
 template <int D, bool kBf16>
 static cudaError_t preload_both() {
-  const cudaError_t e = preload_kernel(prompt_attend_kernel<D, kBf16, false>, true);
-  return e != cudaSuccess ? e : preload_kernel(prompt_attend_kernel<D, kBf16, true>, true);
+  auto split = prompt_attend_kernel<D, kBf16, true>;
+  cudaError_t e = preload_kernel(prompt_attend_kernel<D, kBf16, false>, true);
+  if (e == cudaSuccess) e = preload_kernel(split, true);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(split, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 16;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.gridDim = dim3(16);
+  cfg.blockDim = dim3(kPaThreads);
+  cfg.dynamicSmemBytes = Pa<D>::kBytes;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, split, &cfg) != cudaSuccess) { n = 0; (void)cudaGetLastError(); }
+  most_clusters<D, kBf16>().store(n);
+  return cudaSuccess;
 }
 cudaError_t preload_prompt_attend_kernels() {
   cudaError_t e;
