@@ -1229,9 +1229,9 @@ def prompt_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, first: torc
     are not written."""
     p = _Prompt(q, k, first, n_new, first_k, n_k)
     if out is None:
-        out = ALLOC((*p.lead, p.heads, p.d), p.dtype, p.dev)
+        out = q.new_empty(q.shape) if ALLOC is _torch_empty else ALLOC(q.shape, p.dtype, p.dev)
     if lse is None:
-        lse = ALLOC((*p.lead, p.heads), torch.float32, p.dev)
+        lse = ALLOC(q.shape[:-1], torch.float32, p.dev)
     _prompt_check(lib().oilbird_prompt_attend(
         p.c, p.view(q, p.lead, p.heads), p.view(k, p.lead_k, p.kv_heads), p.view(v, p.lead_k, p.kv_heads),
         p.d ** -0.5 if scale is None else scale, p.view(out, p.lead, p.heads), *p.lse(lse), p.stream(stream)),
@@ -1305,10 +1305,15 @@ def token_scores(logits: torch.Tensor, tokens: torch.Tensor | None = None, top: 
             raise AssertionError(f"tokens: a contiguous int32 tensor [{rows}, n] on {dev}")
         n = tokens.shape[1]
     top = max(-1, min(int(top), 2 ** 31 - 1))
-    new = ALLOC
-    got = TokenScores(None if tokens is None else new((rows, n), torch.float32, dev), new((rows,), torch.float32, dev),
-                      new((rows,), torch.float32, dev), new((rows, max(0, min(top, SCORES_MAX_TOP))), torch.int32, dev),
-                      new((rows, max(0, min(top, SCORES_MAX_TOP))), torch.float32, dev))
+    k = max(0, min(top, SCORES_MAX_TOP))
+    if ALLOC is _torch_empty:            # one allocation for all results: five take longer than the call
+        buf = torch.empty(rows * (2 + n + 2 * k), dtype=torch.float32, device=dev)
+        lse, entropy, logp, best, top_logp = buf.split_with_sizes((rows, rows, rows * n, rows * k, rows * k))
+        got = TokenScores(None if tokens is None else logp.view(rows, n), lse, entropy, best.view(torch.int32).view(rows, k),
+                          top_logp.view(rows, k))
+    else:
+        got = TokenScores(None if tokens is None else ALLOC((rows, n), torch.float32, dev), ALLOC((rows,), torch.float32, dev),
+                          ALLOC((rows,), torch.float32, dev), ALLOC((rows, k), torch.int32, dev), ALLOC((rows, k), torch.float32, dev))
     out = _SCORES_OUT(got.logp.data_ptr() if n else 0, got.lse.data_ptr(), got.entropy.data_ptr(), got.top_id.data_ptr(),
                       got.top_logp.data_ptr())
     rc = lib().oilbird_token_scores(logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, rows, vocab,

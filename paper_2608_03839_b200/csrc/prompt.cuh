@@ -73,10 +73,12 @@ __device__ __forceinline__ void prompt_levels(const Order& order, int n_seq, Pro
   __syncthreads();
   const int unit = max(1, (most + kPrLevels - 1) / kPrLevels), levels = (most + unit - 1) / unit;
   if (threadIdx.x == 0) { l.unit = unit; l.levels = levels; }
-  for (int x = threadIdx.x; x <= levels + 1; x += blockDim.x) {
+  const int lane = threadIdx.x & 31;                     // a warp a level, a lane a sequence
+  for (int x = threadIdx.x >> 5; x <= levels + 1; x += blockDim.x >> 5) {
     int v = 0;
-    for (int s = 0; s < n_seq; ++s) v += order.items(s, x, unit);
-    l.count[x] = v;
+    for (int s = lane; s < n_seq; s += 32) v += order.items(s, x, unit);
+    v = __reduce_add_sync(0xffffffffu, v);
+    if (lane == 0) l.count[x] = v;
   }
 }
 // `level`: any that no item from i on passes (at first l.levels); becomes the item's.  A warp.
