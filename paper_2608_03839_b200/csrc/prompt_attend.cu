@@ -154,11 +154,6 @@ __device__ __noinline__ bool odd_values(const PromptArgs& a, const PaItem& it, i
   return __any_sync(0xffffffffu, odd);
 }
 
-// every thread of every block of the cluster
-__device__ __forceinline__ void meet_cluster() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 // The item of a cluster.  First every block leaves its accumulators in its shared memory (a softmax warp its 16 rows) ..
 template <int D>
 __device__ __forceinline__ void leave_rows(float* acc, uint32_t o_tm, int row0) {
@@ -488,6 +483,9 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       if (it.live) join_rows<D, kBf16>(a, it, acc, sh.ml, shares, rank);
       meet_cluster();                                    // (nobody leaves while its shared memory is read)
     }
+    fence_before();
+    __syncthreads();
+    return;                                              // (see below)
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPaRestRegs));
     if (warp == kPaLoader) {
@@ -641,23 +639,27 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         u += 2 * n_tiles;
       }
     }
+    // Nothing follows the roles: code that all warps share may use any register that the block was launched with, and
+    // these warps have given most of theirs away.
+    if (kSplit) {
+      meet_cluster();
+      meet_cluster();
+    }
+    fence_before();
+    __syncthreads();
+    if (warp == kPaIssuer) {
+      fence_after();
+      // The softmax warps waited for the last products, and the products for the last copies, unless
+      // somebody gave up: then what is in flight gets time to end.  (Read behind the barrier, when nobody
+      // can any more.)
+      if (*gave_up) {
+        const unsigned long long t0 = now_ns();
+        while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
+      }
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+    return;
   }
-  if (kSplit && warp >= kPaSoftWarps) {
-    __syncwarp();
-    meet_cluster();
-    meet_cluster();
-  }
-  fence_before();
-  __syncthreads();
-  fence_after();
-  // The softmax warps waited for the last products, and the products for the last copies, unless
-  // somebody gave up: then what is in flight gets time to end.  (Read behind the barrier, when nobody
-  // can any more.)
-  if (*gave_up) {
-    const unsigned long long t0 = now_ns();
-    while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
-  }
-  if (warp == kPaIssuer) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
 // ------------------------------------------------------------------ host side ---

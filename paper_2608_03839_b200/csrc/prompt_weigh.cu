@@ -282,6 +282,23 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
       }
       if (shares > 1) break;                             // (a cluster has one item)
     }
+    fence_before();
+    __syncthreads();
+    if (shares > 1) {
+      meet_cluster();
+      if (rank == 0 && tid < 2 * kPrTile) {              // a key a thread
+        const PwItem& it = sh.item[0];
+        if (it.live) {
+          const int key = it.key0 + tid, keys = a.ks.first ? it.c : a.ks.rows;
+          float sum = sh.shared[tid];
+          for (int r = 1; r < shares; ++r) sum += cg::this_cluster().map_shared_rank(&sh, r)->shared[tid];
+          if (key < keys)
+            a.weight[((a.ks.first ? 0ll : (long long)it.s * a.n_kv) + it.head) * a.ks.rows + it.k0 + key] = key < it.c ? sum : 0.f;
+        }
+      }
+      meet_cluster();                                    // (nobody leaves while its shared memory is read)
+    }
+    return;
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPwRestRegs));
     if (warp == kPwLoader) {
@@ -453,32 +470,23 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
         }
       }
     }
-  }
-  fence_before();
-  __syncthreads();
-  if (warp == kPwIssuer) {
-    fence_after();
-    // (as in attention: the sums waited for all products, and those for all copies, unless somebody gave up)
-    if (*gave_up) {
-      const unsigned long long t0 = now_ns();
-      while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
-    }
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
-  }
-  if (shares > 1) {
-    cg::cluster_group cluster = cg::this_cluster();
-    cluster.sync();
-    if (rank == 0 && tid < 2 * kPrTile) {                // a key a thread
-      const PwItem& it = sh.item[0];
-      if (it.live) {
-        const int key = it.key0 + tid, keys = a.ks.first ? it.c : a.ks.rows;
-        float sum = sh.shared[tid];
-        for (int r = 1; r < shares; ++r) sum += cluster.map_shared_rank(&sh, r)->shared[tid];
-        if (key < keys)
-          a.weight[((a.ks.first ? 0ll : (long long)it.s * a.n_kv) + it.head) * a.ks.rows + it.k0 + key] = key < it.c ? sum : 0.f;
+    // (as in attention: nothing follows the roles)
+    fence_before();
+    __syncthreads();
+    if (warp == kPwIssuer) {
+      fence_after();
+      // (the sums waited for all products, and those for all copies, unless somebody gave up)
+      if (*gave_up) {
+        const unsigned long long t0 = now_ns();
+        while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
       }
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
-    cluster.sync();                                      // (nobody leaves while its shared memory is read)
+    if (shares > 1) {
+      meet_cluster();
+      meet_cluster();
+    }
+    return;
   }
 }
 

@@ -161,6 +161,12 @@ __device__ __forceinline__ constexpr uint32_t idesc_16(int n, bool transposed, b
 }
 constexpr uint32_t kNegateA = 1u << 13;              // idesc: A's elements with the other sign
 
+// every thread of every block of the cluster
+__device__ __forceinline__ void meet_cluster() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
 // Copies by tensor map into this block's shared memory; `bytes` of them are announced on the barrier first.
 __device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(kv_smem(b)), "r"(bytes) : "memory");
