@@ -11,10 +11,14 @@ that repeat phrases) runs the draft path and the cache together, as a serving lo
     KVCache.evict   cuts every sequence back to its budget, lightest slots first
     Pool.append     remembers the accepted positions for later drafts
 
+With --whole-prompts the prompts go through the prompt calls first: prompt_attend (their attention),
+prompt_weigh (the weight every one of their rows gave the keys, which goes into the cache with them) and
+token_scores (log probability of every prompt token); each pass then scores its trees' drafted tokens as well.
+
 and compares each pass's attention with attention in 64 bits over the exact 16-bit keys and
 values of the whole text, which shows what four bits and eviction cost together.
 
-    python examples/verify_passes.py [--requests 4] [--passes 40] [--budget 256] [--dtype bf16]
+    python examples/verify_passes.py [--requests 4] [--passes 40] [--budget 256] [--dtype bf16] [--whole-prompts]
 """
 import argparse
 import os
@@ -46,6 +50,10 @@ class Verifier:
         cut = lambda w, h: (x @ w).view(*tok.shape, h, self.d).to(self.dtype)
         return cut(self.wq, self.heads), cut(self.wk, self.kv_heads), cut(self.wv, self.kv_heads)
 
+    def logits(self, out):
+        """[rows, vocab] from attention's [rows, heads, head_dim]: the layer's way back to tokens."""
+        return (out.flatten(1).float() @ self.wq.T @ self.embed.T / self.wq.shape[0] ** 0.5).to(self.dtype)
+
 
 def make_texts(n, length, vocab, gen):
     """[n, length] tokens: phrases of 12 drawn again and again from a small common stock."""
@@ -74,7 +82,7 @@ def accepted_path(tok, parent, n_nodes, text, at):
 
 
 def run(requests=4, passes=40, budget=256, dtype=torch.bfloat16, prompt=200, max_nodes=32, seed=0,
-        log=print):
+        log=print, whole_prompts=False):
     gen = torch.Generator(device="cuda").manual_seed(seed)
     ver = Verifier(2048, 256, 8, 2, 64, dtype, gen)
     length = prompt + passes * max_nodes + 1
@@ -87,11 +95,19 @@ def run(requests=4, passes=40, budget=256, dtype=torch.bfloat16, prompt=200, max
     cache = B.KVCache(requests, ver.kv_heads, ver.d, max(prompt, budget) + max_nodes, dtype=dtype)
     params = B.QueryParams(k=4, theta=0.5, depth_mode=B.DEPTH_FIXED, cont_len=8)
 
-    # The prompts: stored, then weighed by the last positions' own queries, as any later pass is.
+    # The prompts: stored, then weighed by the last positions' own queries, as any later pass is; or attended to
+    # as a whole, with the weight that all of their positions gave.
     q, k, v = (x[:, :prompt] for x in everything)
-    cache.append(k, v)
-    look = q[:, prompt - 16:prompt]
-    cache.weigh(look, cache.attend(look)[1])
+    scores = {"tokens": 0, "logp": 0.0, "entropy": 0.0}
+    if whole_prompts:
+        out, lse = B.prompt_attend(q, k, v)
+        cache.append(k, v, weight=B.prompt_weigh(q, lse, k))
+        got = B.token_scores(ver.logits(out[:, :-1].flatten(0, 1)), texts[:, 1:prompt].int().reshape(-1, 1))
+        scores = {"tokens": got.logp.numel(), "logp": got.logp.sum().item(), "entropy": got.entropy.sum().item()}
+    else:
+        cache.append(k, v)
+        look = q[:, prompt - 16:prompt]
+        cache.weigh(look, cache.attend(look)[1])
     cache.evict(budget)
     for s in range(requests):
         pool.append(ver.state(texts[s, :prompt], prev[s, :prompt]), texts[s, :prompt].int())
@@ -116,6 +132,14 @@ def run(requests=4, passes=40, budget=256, dtype=torch.bfloat16, prompt=200, max
         up = torch.where(parent >= 0, node.gather(1, parent.clamp(min=0).long()), before[:, None])
         q, k, v = ver.qkv(node, up)
         out, lse = cache.attend(q, k, v, tree.mask, n_nodes)
+
+        if whole_prompts:                                    # every node's token, from its parent's logits
+            got = B.token_scores(ver.logits(out.gather(1, parent.clamp(min=0).long()[..., None, None].expand_as(out)).flatten(0, 1)),
+                                 tok.view(-1, 1), top=1)
+            live = (parent >= 0).view(-1) & (tok >= 0).view(-1)
+            scores["tokens"] += int(live.sum())
+            scores["logp"] += got.logp[live].sum().item()
+            scores["entropy"] += got.entropy[live].sum().item()
 
         # Which nodes the verifier agrees with: here, those that follow the request's text.
         path = [accepted_path(t, p, n, text_host[s], at[s]) for s, (t, p, n) in
@@ -146,9 +170,12 @@ def run(requests=4, passes=40, budget=256, dtype=torch.bfloat16, prompt=200, max
     assert cache.n_pos.tolist() == at, "every accepted position was stored once"
     assert cache.seq_len.tolist() == [min(budget, n) for n in at] and cache.dropped() == 0
     result = {"tokens_per_pass": taken / (passes * requests), "positions": at,
-              "slots": cache.seq_len.tolist(), "worst_error": worst}
+              "slots": cache.seq_len.tolist(), "worst_error": worst, "scores": scores}
     log(f"{requests} requests, {passes} passes: {result['tokens_per_pass']:.2f} tokens a pass; positions {at} in "
         f"{result['slots']} slots of 4 bits; attention off by at most {worst:.3f} of its norm")
+    if scores["tokens"]:
+        log(f"{scores['tokens']} tokens scored: {scores['logp'] / scores['tokens']:.2f} nats each, entropy "
+            f"{scores['entropy'] / scores['tokens']:.2f}")
     pool.close()
     return result
 
@@ -159,5 +186,6 @@ if __name__ == "__main__":
     ap.add_argument("--passes", type=int, default=40)
     ap.add_argument("--budget", type=int, default=256)
     ap.add_argument("--dtype", choices=("bf16", "f16"), default="bf16")
+    ap.add_argument("--whole-prompts", action="store_true")
     a = ap.parse_args()
-    run(a.requests, a.passes, a.budget, {"bf16": torch.bfloat16, "f16": torch.float16}[a.dtype])
+    run(a.requests, a.passes, a.budget, {"bf16": torch.bfloat16, "f16": torch.float16}[a.dtype], whole_prompts=a.whole_prompts)
