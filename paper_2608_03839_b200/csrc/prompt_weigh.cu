@@ -502,10 +502,14 @@ static cudaError_t run_weigh(const PromptArgs& a, int sms, cudaStream_t st) {
   constexpr long long kItem = 2 * kPrTile;
   const long long tiles = a.ks.first ? a.ks.rows / kItem + a.n_seq : (long long)a.n_seq * ((a.ks.rows + kItem - 1) / kItem);
   const long long items = tiles * a.n_kv;
-  // Fewer items than SMs: the rows of each are shared by a cluster.
+  // Fewer items than SMs: the rows of each are shared by a cluster.  So they are where the longest item (of the first
+  // keys of a prompt, twice the mean) would outlast the others: up to four blocks an SM one after another, while a block has
+  // eight tiles in the mean (one prompt of 4,096: 135 us, by whole items 180).  With weights of the rows nothing is known of that.
   int shares = 1;
-  while (shares < 8 && items * shares * 2 <= sms) shares *= 2;
-  return launch_cluster(prompt_weigh_kernel<D, kBf16>, (unsigned)(items < sms ? items * shares : sms), kPwThreads, Pw<D>::kBytes, shares,
+  const long long mean = (long long)a.qs.rows * a.group / kPrTile / (a.qs.first ? a.n_seq : 1) / 2;
+  while (shares < 8 && (items * shares * 2 <= sms || (!a.row_weight && items <= 2 * sms && items * shares * 2 <= 4 * sms && mean >= 16 * shares)))
+    shares *= 2;
+  return launch_cluster(prompt_weigh_kernel<D, kBf16>, (unsigned)(shares > 1 || items < sms ? items * shares : sms), kPwThreads, Pw<D>::kBytes, shares,
                         st, qm, km, a, shares);
 }
 cudaError_t launch_prompt_weigh(const PromptArgs& a, int head_dim, bool bf16, int sms, cudaStream_t st) {
