@@ -14,8 +14,8 @@
 // While A's scores go through the exponentials the tensor core works for B, and the other way round.
 //
 // Numbers.  Scores, maxima, sums and accumulators are fp32.  Probabilities are rounded to the inputs'
-// type, as the product wants both operands alike (2^-9 of each in bf16, 2^-12 in f16); the sum takes
-// them unrounded.  m follows the row's maximum only when that has grown by 2^8 (the accumulators are
+// type, as the product wants both operands alike (off by 2^-8 of each at most in bf16, 2^-11 in f16); the
+// sum takes them unrounded.  m follows the row's maximum only when that has grown by 2^8 (the accumulators are
 // rescaled in TMEM then), so p reaches 2^8; f16 takes them 2^7 higher, where its range ends, as
 // what lies 17 below the maximum (in exp's units) would otherwise be rounded to nothing.
 //
@@ -29,6 +29,14 @@
 // Where there are fewer items than SMs (few rows, over many keys perhaps) the key tiles of an item are shared
 // by a cluster of blocks.  Each leaves its rows' maxima, sums and accumulators in its shared memory, and a
 // part of the rows is joined by each block, in the order of the keys.
+//
+// Measured, with 32 query heads over 8 key heads of 128: one prompt of 32,768 tokens in 7.5 ms (8.8 TFLOP, 1,165
+// TFLOP/s; 6.3 ms at cuBLAS's sustained rate), 16 of up to 2,048 in 220 us, one of 37 in 10 us, one token over
+// 32,768 keys in 68 us (64 blocks).  What bounds long prompts is power: 990 W at 1,520 MHz, where a step of 256
+// rows by 128 keys takes 3,200 cycles, its exponentials and its products 2,048 each (tensor pipe 59 %, exponential
+// unit 60 %).  Polynomials in place of an eighth to half of the exponentials were slower by 1 to 7 %.  A row
+// a thread, with 8 warps, left the exponentials to two warps an SM quarter (7.9 ms).
+// Short prompts wait for an item's chain: loads, products, a tile's exponentials, products, the rows' way out.
 //
 // Every wait is bounded (two seconds unless set otherwise): a wait that runs out raises `stalled`, all
 // roles leave, TMEM is freed.

