@@ -1172,13 +1172,14 @@ class _Prompt:
             raise AssertionError("first_k (or first) goes with packed k, and only with it")
         if self.packed and n_new is not None or self.packed_k and n_k is not None:
             raise AssertionError("n_new and n_k count the rows of padded sequences")
-        self.n_seq = first.shape[0] - 1 if self.packed else q.shape[0]
-        self.rows, self.heads, self.d = q.shape[-3:]
-        self.rows_k, self.kv_heads = k.shape[-3:-1]
+        self.q_shape, self.k_shape = q.shape, k.shape
+        *lead, self.rows, self.heads, self.d = self.q_shape
+        *lead_k, self.rows_k, self.kv_heads, d = self.k_shape
+        self.n_seq = first.shape[0] - 1 if self.packed else lead[0]
+        if d != self.d or (lead_k and lead_k[0] != self.n_seq):
+            raise AssertionError(f"k: {'' if self.packed_k else f'{self.n_seq} sequences, '}head_dim {self.d}")
         if n_k is None and not self.packed and not self.packed_k and self.rows_k == self.rows:
             n_k = n_new                  # a prompt over itself
-        self.lead = (self.rows,) if self.packed else (self.n_seq, self.rows)
-        self.lead_k = (self.rows_k,) if self.packed_k else (self.n_seq, self.rows_k)
         offsets, counts = (self.n_seq + 1,), (self.n_seq,)
         self.c = _PROMPT(self.vec(first, torch.int32, offsets) or 0, self.vec(n_new, torch.int32, counts) or 0, self.rows,
                          self.vec(first_k, torch.int32, offsets) or 0, self.vec(n_k, torch.int32, counts) or 0, self.rows_k,
@@ -1193,24 +1194,30 @@ class _Prompt:
             raise AssertionError(f"a contiguous {dtype} tensor {list(shape)} on {self.dev}")
         return t.data_ptr()
 
-    def view(self, t, lead, heads):
-        """The C view of a tensor [*lead, heads, head_dim] (any strides but the last)."""
-        if t.dtype is self.dtype and t.shape == (*lead, heads, self.d) and t.get_device() == self.index:
+    # (what runs for every argument of every call bounds the smallest calls: see KVCache._rows)
+    def view(self, t, shape):
+        """The C view of a tensor of that shape (any strides but the last)."""
+        if t.dtype is self.dtype and t.shape == shape and t.get_device() == self.index:
             if t.requires_grad and torch.is_grad_enabled():
                 raise RuntimeError("prompt calls have no backward pass: detach the tensor, or call under torch.no_grad()")
             stride = t.stride()
-            if stride[-1] == 1 or self.d == 1:
-                return _KV_ROWS(t.data_ptr(), stride[0] if len(lead) == 2 else 0, *stride[-3:-1])
-        raise AssertionError(f"a {self.dtype} tensor [{', '.join(map(str, lead))}, {heads}, {self.d}] on {self.dev} "
-                             "with contiguous channels")
+            if stride[-1] == 1:
+                return _KV_ROWS(t.data_ptr(), *stride[:3]) if len(stride) == 4 else _KV_ROWS(t.data_ptr(), 0, *stride[:2])
+        raise AssertionError(f"a {self.dtype} tensor {list(shape)} on {self.dev} with contiguous channels")
+
+    def new(self, q):
+        """A fresh result like q, and its C view."""
+        t = q.new_empty(self.q_shape) if ALLOC is _torch_empty else ALLOC(self.q_shape, self.dtype, self.dev)
+        row = self.heads * self.d
+        return t, _KV_ROWS(t.data_ptr(), 0 if self.packed else self.rows * row, row, self.d)
 
     def lse(self, t):
-        """Pointer and strides of an fp32 tensor [*lead, n_q_heads]."""
-        if t.dtype is not torch.float32 or t.shape != (*self.lead, self.heads) or t.get_device() != self.index:
-            raise AssertionError(f"an fp32 tensor [{', '.join(map(str, self.lead))}, {self.heads}] on {self.dev}")
+        """Pointer and strides of an fp32 tensor [.., n_q_heads]."""
+        if t.dtype is not torch.float32 or t.shape != self.q_shape[:-1] or t.get_device() != self.index:
+            raise AssertionError(f"an fp32 tensor {list(self.q_shape[:-1])} on {self.dev}")
         if t.is_contiguous():
             return t.data_ptr(), None
-        return t.data_ptr(), _KV_STRIDES(t.stride(0) if len(self.lead) == 2 else 0, *t.stride()[-2:])
+        return t.data_ptr(), _KV_STRIDES(0 if self.packed else t.stride(0), *t.stride()[-2:])
 
     def stream(self, stream) -> int:
         return _raw_stream(self.index) if stream is None else stream.cuda_stream
@@ -1228,14 +1235,13 @@ def prompt_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, first: torc
     Returns (out, lse): out like q, lse fp32 [..., n_q_heads] (natural logarithm).  Packed rows of no sequence
     are not written."""
     p = _Prompt(q, k, first, n_new, first_k, n_k)
-    if out is None:
-        out = q.new_empty(q.shape) if ALLOC is _torch_empty else ALLOC(q.shape, p.dtype, p.dev)
+    out, out_view = p.new(q) if out is None else (out, p.view(out, p.q_shape))
     if lse is None:
-        lse = ALLOC(q.shape[:-1], torch.float32, p.dev)
+        lse = (q.new_empty(p.q_shape[:-1], dtype=torch.float32) if ALLOC is _torch_empty else
+               ALLOC(p.q_shape[:-1], torch.float32, p.dev))
     _prompt_check(lib().oilbird_prompt_attend(
-        p.c, p.view(q, p.lead, p.heads), p.view(k, p.lead_k, p.kv_heads), p.view(v, p.lead_k, p.kv_heads),
-        p.d ** -0.5 if scale is None else scale, p.view(out, p.lead, p.heads), *p.lse(lse), p.stream(stream)),
-        "oilbird_prompt_attend")
+        p.c, p.view(q, p.q_shape), p.view(k, p.k_shape), p.view(v, p.k_shape), p.d ** -0.5 if scale is None else scale, out_view,
+        *p.lse(lse), p.stream(stream)), "oilbird_prompt_attend")
     return out, lse
 
 
@@ -1247,13 +1253,12 @@ def prompt_weigh(q: torch.Tensor, lse: torch.Tensor, k: torch.Tensor, first: tor
     prompt_attend (same arguments, and its lse; oilbird_prompt_weigh): fp32 [n_seq, n_kv_heads, rows_k], which
     KVCache.append takes, packed [n_kv_heads, rows_k]."""
     p = _Prompt(q, k, first, n_new, first_k, n_k)
-    shape = (*p.lead_k[:-1], p.kv_heads, p.rows_k)
+    shape = (p.kv_heads, p.rows_k) if p.packed_k else (p.n_seq, p.kv_heads, p.rows_k)
     if weight is None:
         weight = ALLOC(shape, torch.float32, p.dev)
     _prompt_check(lib().oilbird_prompt_weigh(
-        p.c, p.view(q, p.lead, p.heads), *p.lse(lse), p.view(k, p.lead_k, p.kv_heads),
-        p.vec(row_weight, torch.float32, p.lead), p.d ** -0.5 if scale is None else scale,
-        p.vec(weight, torch.float32, shape), p.stream(stream)), "oilbird_prompt_weigh")
+        p.c, p.view(q, p.q_shape), *p.lse(lse), p.view(k, p.k_shape), p.vec(row_weight, torch.float32, p.q_shape[:-2]),
+        p.d ** -0.5 if scale is None else scale, p.vec(weight, torch.float32, shape), p.stream(stream)), "oilbird_prompt_weigh")
     return weight
 
 
