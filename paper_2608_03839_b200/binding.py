@@ -1312,7 +1312,7 @@ def token_scores(logits: torch.Tensor, tokens: torch.Tensor | None = None, top: 
     top = max(-1, min(int(top), 2 ** 31 - 1))
     k = max(0, min(top, SCORES_MAX_TOP))
     if ALLOC is _torch_empty:            # one allocation for all results: five take longer than the call
-        buf = torch.empty(rows * (2 + n + 2 * k), dtype=torch.float32, device=dev)
+        buf = logits.new_empty(rows * (2 + n + 2 * k), dtype=torch.float32)
         lse, entropy, logp, best, top_logp = buf.split_with_sizes((rows, rows, rows * n, rows * k, rows * k))
         got = TokenScores(None if tokens is None else logp.view(rows, n), lse, entropy, best.view(torch.int32).view(rows, k),
                           top_logp.view(rows, k))
