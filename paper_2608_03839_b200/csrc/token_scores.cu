@@ -10,17 +10,20 @@
 // sums of its own under a maximum of its own: no thread waits for another to add up.  Exponentials are
 // 2^((x - m) log2 e): the difference first, as it is exact where it counts and stays a number for the largest and lowest ones.
 //
-// The k best.  A list in shared memory takes every element that reaches a floor: the k-th largest of 64 or
-// 128 groups' largest values so far, which k elements reach and few pass, found anew after the first,
-// fourth, sixteenth, .. load.  Otherwise nobody waits for anybody in that either; where the list turns out to have been too
-// short (long runs of equal or rising values), or too few are above -inf, the block goes through its part again, cutting the list to
+// The k best.  What reaches a floor is among them or near: the k-th largest of 64 or 128 groups' largest values so far,
+// which k elements reach and few pass, found anew after 1, 3, 7, 15, .. loads.  A thread whose load holds something that
+// reaches it notes the load and goes on (taking elements out of registers there and then cost 5 us of 135); at the end the
+// noted loads are read once more, and their elements that reach the last floor make a list in shared memory.  Otherwise nobody
+// waits for anybody in that either; where there turn out to be too many notes or elements (long runs of equal or rising
+// values), or too few above -inf, the block goes through its part again, cutting the list to
 // its k best each time it is full and raising the floor to the k-th, a composite of value and token.  Cutting
 // counts for each entry how many are better, which is its place: no sort, and little code, as what runs
 // once a row is bound by fetching it (a bitonic sort and straight-line code for each of a thread's 32
-// elements took 15 us a row; a barrier a load 100 us on 2,048 rows).
+// elements took 15 us a row; a barrier a load 100 us on 2,048 rows).  Blocks that go from row to row, the next one's
+// first load under way meanwhile, took 170 us: registers.
 //
-// Measured, with bf16 logits: 2,048 rows of 152,064 with 5 alternatives in 133 us (623 MB, 4.7 TB/s; 112 us without
-// alternatives, 5.6 TB/s), 64 rows of 128,256 in 12 us, one row of 128,256 in fp32 with 20 alternatives in 14 us.  Many rows
+// Measured, with bf16 logits: 2,048 rows of 152,064 with 5 alternatives in 132 us (623 MB, 4.7 TB/s; 111 us without
+// alternatives, 5.6 TB/s), 64 rows of 128,256 in 12 us, one row of 128,256 in fp32 with 20 alternatives in 12 us.  Many rows
 // are bound by instructions (two thirds of the issue slots: taking pairs apart, exponentials, three sums) beside
 // the memory, few by the chain of a launch, loads, floor, list and join.
 #include <cooperative_groups.h>
@@ -57,9 +60,10 @@ struct TsSums {
 struct TsShared {
   alignas(16) u64 list[kTsList];
   alignas(16) float group[128];
+  int seen[kTsList];                 // first reading: which threads' loads hold something for the list
   u64 floor;                         // what is not above it is not among the k best (second reading)
   float floor_x;                     // what is below it is not (first reading)
-  int count;                         // of the list's entries, and those that found no room
+  int count;                         // of entries (of `seen`, then of the list), and those that found no room
   TsSums sums[kTsWarps];
 };
 
@@ -165,21 +169,41 @@ __device__ __noinline__ void raise_floor(TsShared& sh, float m, int k) {
   if (better == k - 1) sh.floor_x = fmaxf(g, -3.402823466e38f);
   __syncthreads();
 }
-// Leaves out of a list that holds all that reached earlier floors what does not reach the last one.
-__device__ __noinline__ void thin_list(TsShared& sh, float m, int k) {
-  constexpr int kMine = kTsList / kTsThreads;
-  raise_floor(sh, m, k);
+// The list, from the first n noted loads and the single elements: what reaches the last floor; every thread calls, behind a barrier.
+template <int kType>
+__device__ __noinline__ void collect(TsShared& sh, int n, float m, int k, const unsigned char* x0, int first, int vectors, int single) {
+  using E = TsType<kType>;
+  constexpr int kOnce = 2;
+  if (n > kTsThreads / 2) raise_floor(sh, m, k);
   const float floor_x = sh.floor_x;
-  const int n = sh.count;
-  u64 key[kMine];
-#pragma unroll
-  for (int r = 0; r < kMine; ++r) key[r] = r * kTsThreads + threadIdx.x < n ? sh.list[r * kTsThreads + threadIdx.x] : 0ull;
   __syncthreads();
   if (threadIdx.x == 0) sh.count = 0;
   __syncthreads();
+  auto add = [&](float x, int token) {
+    if (x >= floor_x) {
+      const int to = atomicAdd(&sh.count, 1);
+      if (to < kTsList) sh.list[to] = pack_candidate(x, token);
+    }
+  };
+  if (single >= 0) add(E::one(x0 + (long long)single * E::kBytes), single);
+  const uint4* src = reinterpret_cast<const uint4*>(x0 + (long long)first * E::kBytes);
+  for (int i0 = threadIdx.x; i0 < n * kTsUnroll; i0 += kOnce * kTsThreads) {
+    uint4 w[kOnce];
+    int place[kOnce];
 #pragma unroll
-  for (int r = 0; r < kMine; ++r)
-    if (key[r] != 0ull && candidate_score(key[r]) >= floor_x) sh.list[atomicAdd(&sh.count, 1)] = key[r];
+    for (int r = 0; r < kOnce; ++r) {
+      const int i = i0 + r * kTsThreads;
+      place[r] = i < n * kTsUnroll ? sh.seen[i / kTsUnroll] + i % kTsUnroll * kTsThreads : vectors;
+      w[r] = make_uint4(E::kNone, E::kNone, E::kNone, E::kNone);
+      if (place[r] < vectors) w[r] = __ldg(src + place[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < kOnce; ++r)
+      if (E::largest(w[r]) >= floor_x) {
+#pragma unroll
+        for (int e = 0; e < E::kPer; ++e) add(E::get(w[r], e), first + place[r] * E::kPer + e);
+      }
+  }
   __syncthreads();
 }
 
@@ -321,41 +345,14 @@ token_scores_kernel(const TsArgs a, int parts) {
     }
     // ---- the k best ----
     if (kTop) {
-      if (at == again) {
-        again = 4 * at + 3 * kTsUnroll * kTsThreads;
+      if (at == again && (at == 0 || vectors - at > at / 2)) {     // (a floor for little that is left does not pay)
+        again = 2 * (at + kTsUnroll * kTsThreads);
         raise_floor(sh, t.m, a.k);
         floor_x = sh.floor_x;
       }
-      auto add = [&](float x, int token) {
-        const int to = atomicAdd(&sh.count, 1);
-        if (to < kTsList) sh.list[to] = pack_candidate(x, token);
-      };
       if (top >= floor_x) {
-        uint32_t hits = 0;                               // sixteen bytes that hold something for the list
-#pragma unroll
-        for (int i = 0; i < kTsUnroll; ++i) hits |= (uint32_t)(high[i] >= floor_x) << i;
-        for (; hits; hits &= hits - 1) {
-          const int i = __ffs(hits) - 1;
-          uint4 w = v[0];
-#pragma unroll
-          for (int j = 1; j < kTsUnroll; ++j)
-            if (j == i) w = v[j];
-          // (what stands for elements behind the row's end is -inf, below every floor)
-          const int token = first + (at + i * kTsThreads + tid) * E::kPer;
-          uint32_t these = 0;
-#pragma unroll
-          for (int e = 0; e < E::kPer; ++e) these |= (uint32_t)(E::get(w, e) >= floor_x) << e;
-          for (; these; these &= these - 1) {
-            const int e = __ffs(these) - 1;
-            uint32_t x = w.x;
-#pragma unroll
-            for (int j = 1; j < 4; ++j)
-              if (j == e * E::kBytes / 4) x = (&w.x)[j];
-            if (kType != kTsF32 && e & 1) x >>= 16;
-            add(kType == kTsF32 ? __uint_as_float(x) : half_lo<kType == kTsBf16>(x), token + e);
-          }
-        }
-        if (single >= 0 && alone >= floor_x) add(alone, single);
+        const int to = atomicAdd(&sh.count, 1);
+        if (to < kTsList) sh.seen[to] = at + tid;
       }
     }
     single = -1;
@@ -378,9 +375,13 @@ token_scores_kernel(const TsArgs a, int parts) {
   if (lane == 0) sh.sums[warp] = t;
   __syncthreads();
   if (kTop) {
-    const int n = sh.count;                              // (all that follows has a barrier before its first change)
+    const int lone = tid < first - lo ? lo + tid : tid >= 32 && tid - 32 < hi - behind ? behind + tid - 32 : -1;
+    int n = sh.count;                                    // (all that follows has a barrier before its first change)
+    if (n <= kTsList) {
+      collect<kType>(sh, n, own, a.k, x0, first, vectors, lone);
+      n = sh.count;
+    }
     if (n > kTsList || n < min(a.k, hi - lo)) list_again<kType>(sh, a.k, x0, src, lo, hi, first, vectors, behind);
-    else if (n > kTsThreads / 2) thin_list(sh, own, a.k);
     // (short lists of a row's blocks are cut together)
     if (parts == 1 || sh.count * parts > kTsThreads) cut_list(sh, sh.count, a.k);
   }
