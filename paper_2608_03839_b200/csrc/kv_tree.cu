@@ -557,6 +557,11 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
       at += count;
       if (at < u1) list.advance(bc, count);
     }
+    // Every role ends in code of its own: what all warps share may use any register that the block was launched
+    // with, and the others have given some of theirs away.
+    fence_before();
+    __syncthreads();
+    return;
   } else if (warp < 8 + kTrDecWarps) {
     // ============================================================ decode =========
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTrDecRegs));
@@ -825,6 +830,9 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
       if (at < u1) list.advance(bc, count);
     }
     cp_async_wait<0>();
+    fence_before();
+    __syncthreads();
+    return;
   } else {
     // ============================================================ products =======
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTrIssueRegs));
@@ -895,18 +903,19 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
       at += count;
       if (at < u1) list.advance(bc, count);
     }
-  }
-  fence_before();
-  __syncthreads();
-  fence_after();
-  if (warp == kTrIssuer) {
-    // What was issued is done before the memory goes away: the softmax warps waited for the last
-    // products, unless somebody gave up.  (Read behind the barrier, when nobody can any more.)
-    if (*gave_up) {
-      const unsigned long long t0 = now_ns();
-      while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (warp == kTrIssuer) {
+      // What was issued is done before the memory goes away: the softmax warps waited for the last
+      // products, unless somebody gave up.  (Read behind the barrier, when nobody can any more.)
+      if (*gave_up) {
+        const unsigned long long t0 = now_ns();
+        while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
+      }
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    return;
   }
 }
 
