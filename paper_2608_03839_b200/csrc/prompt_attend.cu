@@ -465,6 +465,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         rows |= rows >> 1;
         rows = (rows | rows >> 2) & 0x11111111u;         // a row's first lane
         if (rows) {
+          __syncwarp();                                  // (other lanes wrote what row_again writes once more)
           const int least = __reduce_min_sync(0xffffffffu, vis[r]);
           if (!odd_values<D, kBf16>(a, it, least, it.tiles[wg] * kPrTile, lane)) rows = 0;
           for (; rows; rows &= rows - 1) {

@@ -1,0 +1,46 @@
+"""Attention over prompts where infinities and NaN lie among the values, at sizes that take every block
+through several items (no clusters share them)."""
+import math
+
+import pytest
+import torch
+
+from paper_2608_03839_b200 import binding as B
+from tests.prompt_reference import Side, attend, check_attend
+
+pytestmark = pytest.mark.gpu
+
+BF16, F16 = torch.bfloat16, torch.float16
+
+
+def make(s, hq, hkv, d, dtype, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    new = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    return ((new(*s.shape, hq, d) * 2).to(dtype), new(*s.shape, hkv, d).to(dtype), new(*s.shape, hkv, d).to(dtype))
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("packed", [True, False])
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(16, 16, 128, BF16), (16, 16, 64, F16), (32, 8, 64, BF16), (24, 8, 128, F16)])
+def test_values_that_are_not_finite_in_whole_items(bad, packed, hq, hkv, d, dtype):
+    """More items than twice the SMs: of sequence i, key j and what lies behind every sequence's last row."""
+    s = Side([700, 300, 690, 513, 450, 64] * 2, packed, tail=5)
+    q, k, v = make(s, hq, hkv, d, dtype)
+    refs = {n: attend(q[s.at(n)], k[s.at(n)], v[s.at(n)], d ** -0.5) for n in (0, 1, 3, 9)}
+    how = s.arguments(("first", "n_new"))
+    for i, j in ((0, 5), (0, 699), (1, 250), (9, 511)):
+        k2, v2 = k.clone(), v.clone()
+        for x in (k2, v2):
+            x[s.at(i)][j, :, 3] = bad
+            if packed:
+                x[s.rows - 5:] = bad
+            else:
+                for n, rows in enumerate(s.counts):
+                    x[n, rows:] = bad
+        out, lse = B.prompt_attend(q, k2, v2, **how)
+        assert B.prompt_status() == B.OK
+        for n, ref in refs.items():
+            a, clean = s.at(n), slice(0, j if n == i else None)
+            check_attend(out[a][clean], lse[a][clean], [x[clean] for x in ref], dtype, d)
+            if n == i:
+                assert not torch.isfinite(out[a][j:]).all(-1).any(), "what a row sees is not hidden"
