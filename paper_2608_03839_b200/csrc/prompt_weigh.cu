@@ -14,8 +14,8 @@
 // What counts is to have four warps an SM quarter: their chains of a load from TMEM, exponent, sum hide each other.
 // (With a query row a thread and 128 sums a thread there were registers for two, and a tile took 3,400 cycles,
 // where its exponentials take 2,048.)
-// Rows that do not count (behind the sequence's last one, weight 0, lse -inf) have -inf there, and their
-// scores are replaced, so that it does not matter what they hold.  Leading and trailing rows with weight 0
+// Rows that do not count (behind the sequence's last one, weight 0, lse -inf) have -inf there, and the exponents of
+// their columns and of those that do not see the key are replaced, so that it does not matter what they hold.  Leading and trailing rows with weight 0
 // are left out of the tiles: all warps look for the first and the last other one of each long sequence
 // when the kernel begins.
 //
@@ -253,14 +253,15 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
                 const float4 bb = bias[4 * k + e], ww = weight[4 * k + e];
-                float z[4];
+                const float2 z0 = fma2(make_float2(__uint_as_float(y[4 * e]), __uint_as_float(y[4 * e + 1])), f2, make_float2(bb.x, bb.y));
+                const float2 z1 = fma2(make_float2(__uint_as_float(y[4 * e + 2]), __uint_as_float(y[4 * e + 3])), f2, make_float2(bb.z, bb.w));
+                float z[4] = {z0.x, z0.y, z1.x, z1.y};
+                // (the exponent is replaced, not the score: a blind row's logarithm may be NaN)
 #pragma unroll
                 for (int h = 0; h < 4; ++h)
-                  z[h] = 16 * k + 4 * e + h >= blind && (&bb.x)[h] > -INFINITY ? __uint_as_float(y[4 * e + h]) : -INFINITY;
-                const float2 z0 = fma2(make_float2(z[0], z[1]), f2, make_float2(bb.x, bb.y));
-                const float2 z1 = fma2(make_float2(z[2], z[3]), f2, make_float2(bb.z, bb.w));
-                sum[0] = fma2(make_float2(exp2_approx(z0.x), exp2_approx(z0.y)), make_float2(ww.x, ww.y), sum[0]);
-                sum[1] = fma2(make_float2(exp2_approx(z1.x), exp2_approx(z1.y)), make_float2(ww.z, ww.w), sum[1]);
+                  if (16 * k + 4 * e + h < blind || (&bb.x)[h] == -INFINITY) z[h] = -INFINITY;
+                sum[0] = fma2(make_float2(exp2_approx(z[0]), exp2_approx(z[1])), make_float2(ww.x, ww.y), sum[0]);
+                sum[1] = fma2(make_float2(exp2_approx(z[2]), exp2_approx(z[3])), make_float2(ww.z, ww.w), sum[1]);
               }
             }
           }
@@ -415,6 +416,12 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
             counts[e] = w[e] != 0.f && l[e] != -INFINITY;
             (&bias.x)[e] = counts[e] ? -l[e] * kLog2e : -INFINITY;
             (&weight.x)[e] = counts[e] ? w[e] : 0.f;
+            // A weight that is not finite goes into the exponent, which columns that do not see the key leave out (0 times
+            // it would be NaN there); of a row that counts for nothing (lse +inf) it is NaN.
+            if (counts[e] && !(fabsf(w[e]) < INFINITY)) {
+              (&bias.x)[e] = w[e] == w[e] && l[e] < INFINITY ? INFINITY : __int_as_float(0x7fffffff);
+              (&weight.x)[e] = w[e] < 0.f ? -1.f : 1.f;
+            }
           }
           if (i + 1 < end) ask(i + 1);
           const bool plain = __all_sync(0xffffffffu, counts[0] && counts[1] && weight.x == 1.f && weight.y == 1.f);
