@@ -17,7 +17,8 @@
 // type, as the product wants both operands alike (off by 2^-8 of each at most in bf16, 2^-11 in f16); the
 // sum takes them unrounded.  m follows the row's maximum only when that has grown by 2^8 (the accumulators are
 // rescaled in TMEM then), so p reaches 2^8; f16 takes them 2^7 higher, where its range ends, as
-// what lies 17 below the maximum (in exp's units) would otherwise be rounded to nothing.
+// what lies 17 below the maximum (in exp's units) would otherwise be rounded to nothing.  bf16 takes them lower, as many
+// keys' large values would otherwise add up to more than fp32 holds (see room_of).
 //
 // Values that are not finite.  A masked key's probability is 0, and 0 times an infinity would reach
 // every row of the tile: a row whose output is not finite looks whether such a value lies among the keys of
@@ -66,8 +67,20 @@ struct PaItem {
   int tiles[2];                      // of A and of B: all that their rows see
   int begin;                         // this block's: from here on,
   int end[2];                        // up to here
+  float room;                        // probabilities are 2^room times as large
   int live;                          // 0: no item is left
 };
+// f16 probabilities use the type's whole range (see above).  In bf16, which ends where fp32 does, they are so small
+// that neither their sum over `tiles` of keys, each up to 2^kPaSlack, reaches 1, nor the sum of the values that they weigh
+// fp32's end: as far down as values of 2^-117 over 2,048 keys that costs no bit.
+template <bool kBf16>
+__device__ __forceinline__ float room_of(int tiles) {
+  return kBf16 ? -(float)(1 + kPaSlack + 7 + (tiles > 1 ? 32 - __clz(tiles - 1) : 0)) : 7.f;
+}
+// (the room is taken out of the sum, which is exact: as part of the logarithm it would cost its last bits)
+__device__ __forceinline__ float row_lse(float m, float l, float room) {
+  return (m + __log2f(l * __int_as_float((127 - (int)room) << 23))) * kPaLn2;
+}
 struct PaShared {
   uint64_t full[16], free[16], qfull, qfree, sfull[2], pfull[2][2], ofull[2], item_full[2], item_free[2], meet;
   PaItem item[2];
@@ -182,7 +195,6 @@ __device__ __forceinline__ void leave_rows(float* acc, uint32_t o_tm, int row0) 
 // .. then it joins its part of the 256 rows, a row a softmax warp.
 template <int D, bool kBf16>
 __device__ __noinline__ void join_rows(const PromptArgs& a, const PaItem& it, float* acc, float2* ml, int shares, int rank) {
-  constexpr float kRoom = kBf16 ? 0.f : 7.f;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   cg::cluster_group cluster = cg::this_cluster();
   constexpr int E = D / 64;                            // pairs of channels a lane
@@ -219,10 +231,10 @@ __device__ __noinline__ void join_rows(const PromptArgs& a, const PaItem& it, fl
       *reinterpret_cast<uint32_t*>(op + 64 * e) = sum == 0.f ? 0u : pack16<kBf16>(u0, u1);
     }
     if (lane == 0 && a.lse)
-      a.lse[seq * a.lse_seq + at * a.lse_row + head * a.lse_head] = sum == 0.f ? -INFINITY : (big - kRoom + __log2f(sum)) * kPaLn2;
+      a.lse[seq * a.lse_seq + at * a.lse_row + head * a.lse_head] = sum == 0.f ? -INFINITY : row_lse(big, sum, it.room);
     const int vis = min(it.c, it.c - it.n + tok + 1);
     if (__any_sync(0xffffffffu, odd && sum != 0.f) && odd_values<D, kBf16>(a, it, vis, it.tiles[wg] * kPrTile, lane))
-      row_again<D, kBf16>(a, it, tok, head, vis, big - kRoom, sum, lane);
+      row_again<D, kBf16>(a, it, tok, head, vis, big - it.room, sum, lane);
   }
 }
 
@@ -234,7 +246,6 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
                      const __grid_constant__ CUtensorMap v_map, const __grid_constant__ PromptArgs a, int blocks) {
   using P = Pa<D>;
   const int shares = kSplit ? blocks : 1;                // of an item, one a block of a cluster
-  constexpr float kRoom = kBf16 ? 0.f : 7.f;
   extern __shared__ unsigned char raw_smem[];
   unsigned char* smem = raw_smem + ((1024 - (kv_smem(raw_smem) & 1023)) & 1023);
   unsigned char* qmat = smem;                            // A, then B: [block of 64 channels][row]
@@ -357,7 +368,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         float2 shift2[2], sum[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const float shift = kRoom - (m[r] == -INFINITY ? 0.f : m[r]);
+          const float shift = (kBf16 ? now.room : 7.f) - (m[r] == -INFINITY ? 0.f : m[r]);
           shift2[r] = make_float2(shift, shift);
           sum[r] = make_float2(0.f, 0.f);
         }
@@ -425,7 +436,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         op[r] = a.out + seq * a.out_seq + row * a.out_row + head[r] * a.out_head + 8 * quad;
         if (write[r] && a.lse && quad == 0)
           a.lse[seq * a.lse_seq + row * a.lse_row + head[r] * a.lse_head] =
-              l[r] == 0.f ? -INFINITY : (m[r] - kRoom + __log2f(l[r])) * kPaLn2;
+              l[r] == 0.f ? -INFINITY : row_lse(m[r], l[r], it.room);
       }
 #pragma unroll 1
       for (int k = 0; k < D; k += 32) {
@@ -471,7 +482,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
           for (; rows; rows &= rows - 1) {
             const int at = __ffs(rows) - 1;
             row_again<D, kBf16>(a, it, __shfl_sync(0xffffffffu, tok[r], at), __shfl_sync(0xffffffffu, head[r], at),
-                                __shfl_sync(0xffffffffu, vis[r], at), __shfl_sync(0xffffffffu, m[r], at) - kRoom,
+                                __shfl_sync(0xffffffffu, vis[r], at), __shfl_sync(0xffffffffu, m[r], at) - it.room,
                                 __shfl_sync(0xffffffffu, l[r], at), lane);
           }
         }
@@ -527,6 +538,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
           it.tiles[g] = vis > 0 ? (vis + kPrTile - 1) / kPrTile : 0;
         }
         const int all = max(it.tiles[0], it.tiles[1]);
+        it.room = room_of<kBf16>(all);
         it.begin = (int)((long long)all * rank / shares);
         const int end = (int)((long long)all * (rank + 1) / shares);
 #pragma unroll
