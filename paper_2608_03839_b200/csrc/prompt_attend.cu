@@ -124,6 +124,22 @@ struct PaOrder {
   }
 };
 
+// Two results in the type: of finite accumulators o the largest number of the type where u, rounded, lies behind it (the
+// probabilities are rounded, the sum that divides them is not, so that a result may pass the largest value that it is
+// made of).
+template <bool kBf16>
+__device__ __forceinline__ uint32_t pack_finite(float lo, float hi) {
+  uint32_t r;
+  if (kBf16) asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+template <bool kBf16>
+__device__ __forceinline__ uint32_t pack_result(float o0, float o1, float u0, float u1) {
+  const uint32_t a = pack_finite<kBf16>(u0, u1), b = pack16<kBf16>(u0, u1);
+  return ((fabsf(o0) < INFINITY ? a : b) & 0xffffu) | ((fabsf(o1) < INFINITY ? a : b) & 0xffff0000u);
+}
+
 // One row again, by a whole warp, from the keys it sees: what masked values were kept out of.
 template <int D, bool kBf16>
 __device__ __noinline__ void row_again(const PromptArgs& a, const PaItem& it, int tok, int head, int vis, float m, float l, int lane) {
@@ -156,7 +172,7 @@ __device__ __noinline__ void row_again(const PromptArgs& a, const PaItem& it, in
   }
   uint16_t* op = a.out + (a.qs.first ? 0 : it.s) * a.out_seq + (long long)(it.q0 + tok) * a.out_row + head * a.out_head;
 #pragma unroll
-  for (int e = 0; e < E; ++e) *reinterpret_cast<uint32_t*>(op + e * 64 + 2 * lane) = pack16<kBf16>(o[e].x, o[e].y);
+  for (int e = 0; e < E; ++e) *reinterpret_cast<uint32_t*>(op + e * 64 + 2 * lane) = pack_result<kBf16>(o[e].x, o[e].y, o[e].x, o[e].y);
 }
 
 // Whether a value of keys [from, to) of the item's sequence (as far as the array goes) is not finite; a warp.
@@ -227,8 +243,8 @@ __device__ __noinline__ void join_rows(const PromptArgs& a, const PaItem& it, fl
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const float u0 = o[e].x * inv, u1 = o[e].y * inv;
-      odd |= !(fabsf(u0) < INFINITY) || !(fabsf(u1) < INFINITY);
-      *reinterpret_cast<uint32_t*>(op + 64 * e) = sum == 0.f ? 0u : pack16<kBf16>(u0, u1);
+      odd |= !(fabsf(o[e].x) < INFINITY) || !(fabsf(o[e].y) < INFINITY);
+      *reinterpret_cast<uint32_t*>(op + 64 * e) = sum == 0.f ? 0u : pack_result<kBf16>(o[e].x, o[e].y, u0, u1);
     }
     if (lane == 0 && a.lse)
       a.lse[seq * a.lse_seq + at * a.lse_row + head * a.lse_head] = sum == 0.f ? -INFINITY : row_lse(big, sum, it.room);
@@ -438,35 +454,39 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
           a.lse[seq * a.lse_seq + row * a.lse_row + head[r] * a.lse_head] =
               l[r] == 0.f ? -INFINITY : row_lse(m[r], l[r], it.room);
       }
+      // (a second time where a row has accumulators that are not finite: those results are infinite or NaN too)
+      for (bool exact = false;; exact = true) {
 #pragma unroll 1
-      for (int k = 0; k < D; k += 32) {
-        uint32_t o[16];
-        if (any) {
-          tmem_ask_rows(o_tm + k, o);
-          tmem_wait_rows(o);
-        }
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          uint32_t w[4];                                 // columns 8i + 2 quad, .. of the 32
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float2 u = mul2(make_float2(__uint_as_float(o[4 * i + 2 * r]), __uint_as_float(o[4 * i + 2 * r + 1])), inv[r]);
-            odd2[r] = fma2(u, make_float2(zero, zero), odd2[r]);             // (NaN once one is not finite)
-            w[i] = l[r] == 0.f ? 0u : pack16<kBf16>(u.x, u.y);
+        for (int k = 0; k < D; k += 32) {
+          uint32_t o[16];
+          if (any) {
+            tmem_ask_rows(o_tm + k, o);
+            tmem_wait_rows(o);
           }
 #pragma unroll
-          for (int x = 2; x; x >>= 1) {
-            const bool up = quad & x;
+          for (int r = 0; r < 2; ++r) {
+            uint32_t w[4];                               // columns 8i + 2 quad, .. of the 32
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (!(i & x)) {
-                const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[i] : w[i + x], x);
-                w[i] = up ? got : w[i];
-                w[i + x] = up ? w[i + x] : got;
-              }
+            for (int i = 0; i < 4; ++i) {
+              const float2 x = make_float2(__uint_as_float(o[4 * i + 2 * r]), __uint_as_float(o[4 * i + 2 * r + 1])), u = mul2(x, inv[r]);
+              odd2[r] = fma2(x, make_float2(zero, zero), odd2[r]);           // (NaN once one is not finite)
+              w[i] = l[r] == 0.f ? 0u : exact ? pack_result<kBf16>(x.x, x.y, u.x, u.y) : pack_finite<kBf16>(u.x, u.y);
+            }
+#pragma unroll
+            for (int x = 2; x; x >>= 1) {
+              const bool up = quad & x;
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (!(i & x)) {
+                  const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[i] : w[i + x], x);
+                  w[i] = up ? got : w[i];
+                  w[i + x] = up ? w[i + x] : got;
+                }
+            }
+            if (write[r]) *reinterpret_cast<uint4*>(op[r] + k) = make_uint4(w[0], w[1], w[2], w[3]);
           }
-          if (write[r]) *reinterpret_cast<uint4*>(op[r] + k) = make_uint4(w[0], w[1], w[2], w[3]);
         }
+        if (exact || !__any_sync(0xffffffffu, any && !(odd2[0].x + odd2[0].y + odd2[1].x + odd2[1].y == 0.f))) break;
       }
 #pragma unroll
       for (int r = 0; r < 2; ++r) odd[r] = !(odd2[r].x + odd2[r].y == 0.f);

@@ -61,3 +61,27 @@ def test_sums_of_small_values(size):
     out, _ = B.prompt_attend(q.bfloat16(), k.bfloat16(), v, scale=1.0, **how)
     want = v.double().cumsum(0) / torch.arange(1, 2001, device="cuda")[:, None, None]
     assert bool(((out.double() - want).abs() <= 2.0 ** -7 * want + 2.0 ** -126).all())
+
+
+@pytest.mark.parametrize("many", [FEW, MANY])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_results_next_to_the_types_largest_number(many, d, dtype):
+    """Rounded probabilities over a sum that is not: all of them may be rounded up (one key at 0, the others
+    where half a step is added), and the result lies above the values' size.  It ends at the type's largest number."""
+    s, q, k, v, how = prompts(1000, many, d, dtype)
+    half = 0.5 + 0.6 * torch.finfo(dtype).eps / 2          # (rounded to the next number up)
+    first = torch.tensor(math.log(half)).to(dtype).float()
+    q[..., :2] = 1.0
+    k[..., 0], k[..., 1] = first, (math.log(half) - first).to(dtype).float()
+    v[:] = torch.finfo(dtype).max
+    v[..., 1::2] *= -1
+    for i in range(len(s.counts)):
+        k[s.at(i)][0] = 0.0
+    out, _ = check(q, k, v, s, how, dtype, 1.0)
+    for i in (0, len(s.counts) - 1):                       # what a row sees is not hidden
+        v[s.at(i)][900, 0, 3] = math.inf
+    out, _ = B.prompt_attend(*(x.to(dtype) for x in (q, k, v)), scale=1.0, **how)
+    for i in (0, len(s.counts) - 1):
+        x = out[s.at(i)]
+        assert bool((x[900:, 0, 3] == math.inf).all()) and bool(torch.isfinite(x[:900]).all()) and bool(torch.isfinite(x[..., 4:]).all())
