@@ -113,8 +113,8 @@ static int check_rows(const oilbird_kv_rows* r, const char* what, const PromptSi
 }
 static int check_scale(float scale, PromptArgs* a) {
   if (!(fabsf(scale) < INFINITY)) return refuse("scale: a finite number");
-  // (never zero, as zero times the -inf of what a row does not see is NaN; scores times this are zero)
-  a->factor = fminf(fmaxf(fabsf(scale) * kLog2e, 1e-37f), 3e38f);
+  // (never zero, as zero times the -inf of what a row does not see is NaN; scores times fp32's smallest number are)
+  a->factor = fminf(fmaxf(fabsf(scale) * kLog2e, 1.5e-45f), 3e38f);
   a->negate = scale < 0.f;
   return OILBIRD_OK;
 }

@@ -77,9 +77,24 @@ template <bool kBf16>
 __device__ __forceinline__ float room_of(int tiles) {
   return kBf16 ? -(float)(1 + kPaSlack + 7 + (tiles > 1 ? 32 - __clz(tiles - 1) : 0)) : 7.f;
 }
+// A row's exponents are x f - m f + room with f = scale log2 e and m the running maximum of its scores x.  One fused
+// multiply-add does that while m f is small: what rounding m f loses is the same in every exponent.  Beyond 2^20
+// that would be worth something, beyond 2^24 whole powers of two, and m f may be infinite: there the difference x - m
+// comes first.
+constexpr float kPaFar = 1048576.f;
+__device__ __forceinline__ bool row_far(float m, float f) { return fabsf(m * f) > kPaFar && m != -INFINITY; }
+__device__ __forceinline__ float row_shift(float m, float f, float room) {
+  return fabsf(m * f) <= kPaFar ? fmaf(-m, f, room) : room;      // (no maximum yet: room)
+}
+// log2 of what sums and accumulators under the maximum `from` are multiplied with to be under `to`
+__device__ __forceinline__ float row_fall(float from, float to, float f, float room) {
+  if (from == -INFINITY || row_far(from, f) || row_far(to, f)) return (from - to) * f;
+  return row_shift(to, f, room) - row_shift(from, f, room);
+}
 // (the room is taken out of the sum, which is exact: as part of the logarithm it would cost its last bits)
-__device__ __forceinline__ float row_lse(float m, float l, float room) {
-  return (m + __log2f(l * __int_as_float((127 - (int)room) << 23))) * kPaLn2;
+__device__ __forceinline__ float row_lse(float m, float l, float f, float room) {
+  const float ls = __log2f(l * __int_as_float((127 - (int)room) << 23));
+  return row_far(m, f) ? fmaf(m, f * kPaLn2, ls * kPaLn2) : (ls - (row_shift(m, f, room) - room)) * kPaLn2;
 }
 struct PaShared {
   uint64_t full[16], free[16], qfull, qfree, sfull[2], pfull[2][2], ofull[2], item_full[2], item_free[2], meet;
@@ -142,7 +157,7 @@ __device__ __forceinline__ uint32_t pack_result(float o0, float o1, float u0, fl
 
 // One row again, by a whole warp, from the keys it sees: what masked values were kept out of.
 template <int D, bool kBf16>
-__device__ __noinline__ void row_again(const PromptArgs& a, const PaItem& it, int tok, int head, int vis, float m, float l, int lane) {
+__device__ __noinline__ void row_again(const PromptArgs& a, const PaItem& it, int tok, int head, int vis, float m, int lane) {
   constexpr int E = D / 64;                              // pairs of channels a lane
   const uint16_t* qp = a.q.at(a.qs.first ? 0 : it.s, it.q0 + tok, head);
   float2 q[E], o[E];
@@ -152,7 +167,8 @@ __device__ __noinline__ void row_again(const PromptArgs& a, const PaItem& it, in
     q[e] = make_float2(half_lo<kBf16>(w), half_hi<kBf16>(w));
     o[e] = make_float2(0.f, 0.f);
   }
-  const float f = a.negate ? -a.factor : a.factor, inv = 1.f / l;
+  const float f = a.factor, shift = row_shift(m, f, it.room), less = row_far(m, f) ? m : 0.f;
+  float l = 0.f;
   for (int j = 0; j < vis; ++j) {
     const uint16_t* kp = a.k.at(a.ks.first ? 0 : it.s, it.k0 + j, it.head);
     const uint16_t* vp = a.v.at(a.ks.first ? 0 : it.s, it.k0 + j, it.head);
@@ -162,7 +178,9 @@ __device__ __noinline__ void row_again(const PromptArgs& a, const PaItem& it, in
       const uint32_t w = *reinterpret_cast<const uint32_t*>(kp + e * 64 + 2 * lane);
       x = fmaf(q[e].x, half_lo<kBf16>(w), fmaf(q[e].y, half_hi<kBf16>(w), x));
     }
-    const float p = exp2_approx(fmaf(warp_sum(x), f, -m)) * inv;
+    x = warp_sum(x);
+    const float p = exp2_approx(fmaf((a.negate ? -x : x) - less, f, shift));
+    l += p;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const uint32_t w = *reinterpret_cast<const uint32_t*>(vp + e * 64 + 2 * lane);
@@ -170,9 +188,10 @@ __device__ __noinline__ void row_again(const PromptArgs& a, const PaItem& it, in
       o[e].y = fmaf(p, half_hi<kBf16>(w), o[e].y);
     }
   }
+  const float inv = 1.f / l;
   uint16_t* op = a.out + (a.qs.first ? 0 : it.s) * a.out_seq + (long long)(it.q0 + tok) * a.out_row + head * a.out_head;
 #pragma unroll
-  for (int e = 0; e < E; ++e) *reinterpret_cast<uint32_t*>(op + e * 64 + 2 * lane) = pack_result<kBf16>(o[e].x, o[e].y, o[e].x, o[e].y);
+  for (int e = 0; e < E; ++e) *reinterpret_cast<uint32_t*>(op + e * 64 + 2 * lane) = pack_result<kBf16>(o[e].x, o[e].y, o[e].x * inv, o[e].y * inv);
 }
 
 // Whether a value of keys [from, to) of the item's sequence (as far as the array goes) is not finite; a warp.
@@ -226,7 +245,7 @@ __device__ __noinline__ void join_rows(const PromptArgs& a, const PaItem& it, fl
     for (int s = 0; s < shares; ++s) {
       const float2 y = cluster.map_shared_rank(ml, s)[row];
       if (y.x == -INFINITY && y.y == 0.f) continue;    // it saw nothing there
-      const float f = y.x == big ? 1.f : exp2_approx(y.x - big);
+      const float f = y.x == big ? 1.f : exp2_approx(row_fall(y.x, big, a.factor, it.room));
       const float* from = cluster.map_shared_rank(acc, s) + row * Pa<D>::kRow + 2 * lane;
       sum = fmaf(f, y.y, sum);
 #pragma unroll
@@ -247,10 +266,10 @@ __device__ __noinline__ void join_rows(const PromptArgs& a, const PaItem& it, fl
       *reinterpret_cast<uint32_t*>(op + 64 * e) = sum == 0.f ? 0u : pack_result<kBf16>(o[e].x, o[e].y, u0, u1);
     }
     if (lane == 0 && a.lse)
-      a.lse[seq * a.lse_seq + at * a.lse_row + head * a.lse_head] = sum == 0.f ? -INFINITY : row_lse(big, sum, it.room);
+      a.lse[seq * a.lse_seq + at * a.lse_row + head * a.lse_head] = sum == 0.f ? -INFINITY : row_lse(big, sum, a.factor, it.room);
     const int vis = min(it.c, it.c - it.n + tok + 1);
     if (__any_sync(0xffffffffu, odd && sum != 0.f) && odd_values<D, kBf16>(a, it, vis, it.tiles[wg] * kPrTile, lane))
-      row_again<D, kBf16>(a, it, tok, head, vis, big - it.room, sum, lane);
+      row_again<D, kBf16>(a, it, tok, head, vis, big, lane);
   }
 }
 
@@ -357,15 +376,15 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
           mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], o));
           mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], o));
         }
-        mx[0] *= a.factor;
-        mx[1] *= a.factor;
-        if (__any_sync(0xffffffffu, mx[0] > m[0] + kPaSlack || mx[1] > m[1] + kPaSlack)) {
+        const float room = kBf16 ? now.room : 7.f;
+        // (differences of scores: as products with the factor both may be infinite)
+        if (__any_sync(0xffffffffu, (mx[0] - m[0]) * a.factor > kPaSlack || (mx[1] - m[1]) * a.factor > kPaSlack)) {
           // (each row for itself; the products so far are done, or there were no scores)
           float down[2];
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            const float mn = mx[r] > m[r] + kPaSlack ? mx[r] : m[r];
-            down[r] = mn == -INFINITY ? 1.f : exp2_approx(m[r] - mn);
+            const float mn = (mx[r] - m[r]) * a.factor > kPaSlack ? mx[r] : m[r];
+            down[r] = mn == m[r] ? 1.f : exp2_approx(row_fall(m[r], mn, a.factor, room));
             m[r] = mn;
             l[r] *= down[r];
           }
@@ -381,10 +400,21 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
             }
           }
         }
+        if (__any_sync(0xffffffffu, row_far(m[0], a.factor) || row_far(m[1], a.factor))) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const float less = row_far(m[r], a.factor) ? m[r] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              x[4 * i + 2 * r] = __float_as_uint(__uint_as_float(x[4 * i + 2 * r]) - less);
+              x[4 * i + 2 * r + 1] = __float_as_uint(__uint_as_float(x[4 * i + 2 * r + 1]) - less);
+            }
+          }
+        }
         float2 shift2[2], sum[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const float shift = (kBf16 ? now.room : 7.f) - (m[r] == -INFINITY ? 0.f : m[r]);
+          const float shift = row_shift(m[r], a.factor, room);
           shift2[r] = make_float2(shift, shift);
           sum[r] = make_float2(0.f, 0.f);
         }
@@ -452,7 +482,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         op[r] = a.out + seq * a.out_seq + row * a.out_row + head[r] * a.out_head + 8 * quad;
         if (write[r] && a.lse && quad == 0)
           a.lse[seq * a.lse_seq + row * a.lse_row + head[r] * a.lse_head] =
-              l[r] == 0.f ? -INFINITY : row_lse(m[r], l[r], it.room);
+              l[r] == 0.f ? -INFINITY : row_lse(m[r], l[r], a.factor, it.room);
       }
       // (a second time where a row has accumulators that are not finite: those results are infinite or NaN too)
       for (bool exact = false;; exact = true) {
@@ -502,8 +532,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
           for (; rows; rows &= rows - 1) {
             const int at = __ffs(rows) - 1;
             row_again<D, kBf16>(a, it, __shfl_sync(0xffffffffu, tok[r], at), __shfl_sync(0xffffffffu, head[r], at),
-                                __shfl_sync(0xffffffffu, vis[r], at), __shfl_sync(0xffffffffu, m[r], at) - it.room,
-                                __shfl_sync(0xffffffffu, l[r], at), lane);
+                                __shfl_sync(0xffffffffu, vis[r], at), __shfl_sync(0xffffffffu, m[r], at), lane);
           }
         }
       }

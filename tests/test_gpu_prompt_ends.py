@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2608_03839_b200 import binding as B
-from tests.prompt_reference import Side, attend, check_attend
+from tests.prompt_reference import Side, attend, check_attend, seen
 
 pytestmark = pytest.mark.gpu
 
@@ -85,3 +85,66 @@ def test_results_next_to_the_types_largest_number(many, d, dtype):
     for i in (0, len(s.counts) - 1):
         x = out[s.at(i)]
         assert bool((x[900:, 0, 3] == math.inf).all()) and bool(torch.isfinite(x[:900]).all()) and bool(torch.isfinite(x[..., 4:]).all())
+
+
+@pytest.mark.parametrize("many", [FEW, MANY])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("dtype,size,scale", [(F16, 3e4, 1.0), (F16, 3e4, 0.7), (F16, 5e4, 3.3), (BF16, 1.3e6, 0.123), (BF16, 1e18, 0.9),
+                                              (BF16, 7e18, 1.1), (F16, 4e3, 0.9)])
+def test_scores_of_any_size(many, sign, dtype, size, scale):
+    """Scores beside whose size a softmax's differences vanish: equal ones share, larger ones take all.  Each is one
+    product, exact in fp32."""
+    s, q, k, v, how = prompts(700, many, 64, dtype)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    v[:] = torch.randn(v.shape, generator=g, device="cuda")
+    q[..., 9], k[..., 9] = size, sign * size
+    for i in range(len(s.counts)):
+        k[s.at(i)][300:310, :, 9] = size * 1.125 * sign
+        k[s.at(i)][400:, :, 9] = size * 0.5 * sign
+        k[s.at(i)][500:505, :, 9] = size * 1.25 * sign
+    q, k, v = (x.to(dtype) for x in (q, k, v))
+    out, lse = B.prompt_attend(q, k, v, scale=scale, **how)
+    half = torch.finfo(dtype).eps / 2
+    for i in {0, len(s.counts) - 1}:
+        x, y, z = (t[s.at(i)].double() for t in (q, k, v))
+        scores = (torch.einsum("nhd,chd->hnc", x, y) * scale).masked_fill(~seen(700, 700), -math.inf)
+        p, rl = scores.softmax(-1), scores.logsumexp(-1).T  # (exp(x - lse) would miss what 64 bits have no room for in lse)
+        ref, mass = torch.einsum("hnc,chd->nhd", p, z), torch.einsum("hnc,chd->nhd", p, z.abs())
+        # equal scores have equal probabilities, whatever they are rounded to: half a step of the result, and of fp32
+        assert bool(((out[s.at(i)].double() - ref).abs() <= half * ref.abs() + (half + 2.0 ** -20) * mass).all())
+        assert bool(((lse[s.at(i)].double() - rl).abs() <= 2.0 ** -21 * rl.abs() + 2.0 ** -20).all())
+
+
+@pytest.mark.parametrize("many", [FEW, MANY])
+def test_scores_that_fp32_does_not_hold(many):
+    """scale q.k beyond 3e38, q.k itself not: the largest takes all, and the logarithm is infinite."""
+    s, q, k, v, how = prompts(300, many, 64, BF16)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    v[:] = torch.randn(v.shape, generator=g, device="cuda")
+    q[..., 9], k[..., 9] = 1e15, 1e15
+    for i in range(len(s.counts)):
+        k[s.at(i)][40, :, 9] = 2e15
+        k[s.at(i)][200, :, 9] = 4e15
+    q, k, v = (x.to(BF16) for x in (q, k, v))
+    out, lse = B.prompt_attend(q, k, v, scale=1e12, **how)
+    for i in {0, len(s.counts) - 1}:
+        x, y = out[s.at(i)], v[s.at(i)]
+        assert torch.equal(x[40:200], y[40:41].expand(160, -1, -1)) and torch.equal(x[200:], y[200:201].expand(100, -1, -1))
+    assert bool((lse == math.inf).all())
+    k.neg_()
+    out, lse = B.prompt_attend(q, k, v, scale=1e12, **how)
+    for i in {0, len(s.counts) - 1}:                       # all but two are equal
+        x, y = out[s.at(i)], v[s.at(i)].double()
+        want = (y[:300].sum(0) - y[40] - y[200]) / 298
+        assert bool(((x[299].double() - want).abs() <= 2.0 ** -8 * (want.abs() + y.abs().mean(0)) * 1.01).all())
+    assert bool((lse == -math.inf).all())                  # (its value is below fp32's lowest)
+
+
+def test_a_scale_of_zero_over_large_scores():
+    s, q, k, v, how = prompts(300, FEW, 64, BF16)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    v[:] = torch.randn(v.shape, generator=g, device="cuda")
+    q[..., 0] = 1e18
+    k[..., 0] = torch.linspace(-1e19, 1e19, 300, device="cuda")[:, None]
+    for scale in (0.0, 1e-40):
+        check(q, k, v, s, how, BF16, scale)
