@@ -798,7 +798,8 @@ int oilbird_prompt_weigh(const oilbird_prompt* prompt, const oilbird_kv_rows* q,
 /* Synchronises cuda_stream; OILBIRD_ESTALL if a bounded device-side wait of a prompt call on the device
  * gave up since the last status() (which forgets it). */
 int oilbird_prompt_status(int32_t device, void* cuda_stream);
-/* How long those waits may take, in nanoseconds (0: two seconds); holds for the calls behind it. */
+/* How long those waits may take, in nanoseconds (0: two seconds; 274 seconds at most, by steps of 64 ns); holds
+ * for the calls behind it. */
 int oilbird_prompt_set_wait_limit(int32_t device, uint64_t limit_ns, void* cuda_stream);
 const char* oilbird_prompt_last_error(void);
 

@@ -81,7 +81,7 @@ struct TreeShared {
   TileInfo info[4];
   uint32_t peak[4][kTrDecWarps][2];  // by tile: largest key and value bound each decoding warp saw
   uint32_t tmem;
-  int gave_up;
+  Waits waits;
   float2 ml[128];                    // group B's sums on their way to A
 };
 
@@ -199,7 +199,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
   long long* scratch = cum + kKvMaxSeq + 1;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   DeviceStats* stats = &reinterpret_cast<KvWork*>(c.work)->stats;
-  volatile int* gave_up = &sh.gave_up;
+  volatile Waits* waits = &sh.waits;
 
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
@@ -215,7 +215,6 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
     bar_init(&sh.kfree, 1);
     bar_init(&sh.qfull, 8);
     bar_init(&sh.meet, 8);
-    sh.gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kTrIssuer) {
@@ -227,6 +226,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
   fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
   pdl_enter();
+  if (tid == 0) waits_begin(sh.waits, stats);
 
   TreeList list;
   list.cum = cum;
@@ -257,7 +257,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
     auto meet = [&]() {                                  // of both groups
       __syncwarp();
       if (lane == 0) bar_arrive(&sh.meet);
-      ok = ok && warp_wait(&sh.meet, met++ & 1, gave_up, stats);
+      ok = ok && warp_wait(&sh.meet, met++ & 1, waits, stats);
       return ok;
     };
     for (int at = 0; at < u1 && ok;) {
@@ -330,8 +330,8 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
         const int mine = p.two ? p.n : (p.n + 1 - wg) / 2;
         for (int i = 0; i < mine; ++i, ++su) {
           const uint32_t t = kt + (p.two ? i : 2 * i + wg);
-          if (!warp_wait(&sh.info_full[t & 3], (t >> 2) & 1, gave_up, stats) ||
-              !warp_wait(&sh.sfull[wg], su & 1, gave_up, stats)) { ok = false; break; }
+          if (!warp_wait(&sh.info_full[t & 3], (t >> 2) & 1, waits, stats) ||
+              !warp_wait(&sh.sfull[wg], su & 1, waits, stats)) { ok = false; break; }
           fence_after();
           const TileInfo& info = sh.info[t & 3];
           uint32_t flags = *reinterpret_cast<const uint32_t*>(info.flags);
@@ -387,7 +387,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
             m = mn;
             l *= down;
             if (i > 0) {
-              if (!warp_wait(&sh.pvdone[wg], (su - 1) & 1, gave_up, stats)) { ok = false; break; }
+              if (!warp_wait(&sh.pvdone[wg], (su - 1) & 1, waits, stats)) { ok = false; break; }
               fence_after();
 #pragma unroll 1
               for (int k = 0; k < D; k += 16) {
@@ -445,7 +445,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
         if (!ok) break;
         kt += p.n;
         if (mine > 0) {
-          if (!warp_wait(&sh.pvdone[wg], (su - 1) & 1, gave_up, stats)) { ok = false; break; }
+          if (!warp_wait(&sh.pvdone[wg], (su - 1) & 1, waits, stats)) { ok = false; break; }
           fence_after();
         }
         if (mine == 0) { m = -INFINITY; l = 0.f; }
@@ -668,9 +668,9 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
             int which = part;
             asm volatile("" : "+r"(which));
             const bool values = which != 0;
-            ok = warp_wait(values ? &sh.vfree[st] : &sh.kfree, (values ? ph : kt & 1) ^ 1, gave_up, stats);
+            ok = warp_wait(values ? &sh.vfree[st] : &sh.kfree, (values ? ph : kt & 1) ^ 1, waits, stats);
             if (ok && !values) {
-              ok = warp_wait(&sh.peaks[st], ph, gave_up, stats);
+              ok = warp_wait(&sh.peaks[st], ph, waits, stats);
               peaks_of(kt, ek, ev);
               if (lane == 0) {
                 info.valid[dw] = ballot;
@@ -740,7 +740,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
           // turned into f16 in place, each by a power of two of its own, values stay as they are
           // (their products take the cache's type): a hidden node's numbers, however large, take no
           // bits from what the others hold.
-          if (!warp_wait(&sh.kfree, (kt & 1) ^ 1, gave_up, stats) || !warp_wait(&sh.vfree[st], ph ^ 1, gave_up, stats)) {
+          if (!warp_wait(&sh.kfree, (kt & 1) ^ 1, waits, stats) || !warp_wait(&sh.vfree[st], ph ^ 1, waits, stats)) {
             ok = false;
             break;
           }
@@ -759,7 +759,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
           // (nothing to agree on, but the count of tiles goes on)
           post(kt, 0u, 0u);
           if (cached > 0) post_meta(kt + 1, mc);
-          if (!warp_wait(&sh.peaks[st], ph, gave_up, stats)) { ok = false; break; }
+          if (!warp_wait(&sh.peaks[st], ph, waits, stats)) { ok = false; break; }
           auto my_chunk = [&](int x) {
             return reinterpret_cast<uint4*>(mat + (x >> 3) * (kTrTile * 128) + j * 128 + (((x & 7) ^ (j & 7)) << 4));
           };
@@ -852,12 +852,12 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
       const Piece p = piece_at(bc, count, c, a);
       if (p.n > 0) {
         const int steps = p.two ? 2 * p.n : p.n;
-        ok = warp_wait(&sh.qfull, np & 1, gave_up, stats);
+        ok = warp_wait(&sh.qfull, np & 1, waits, stats);
         ++np;
         auto scores = [&](int u) {
           const uint32_t t = kt + (p.two ? u >> 1 : u);
           const int wg = u & 1;
-          if (!p.two || wg == 0) ok = ok && warp_wait(&sh.kfull, t & 1, gave_up, stats);
+          if (!p.two || wg == 0) ok = ok && warp_wait(&sh.kfull, t & 1, waits, stats);
           if (!ok) return;
           fence_after();
           const uint64_t qd = q_desc + (p.two && wg ? (uint64_t)(128 * 128 >> 4) : 0);
@@ -880,8 +880,8 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
         for (int u = 0; u < steps && ok; ++u) {
           const uint32_t t = kt + (p.two ? u >> 1 : u);
           const int st = t & 1, wg = u & 1;
-          if (!p.two || wg == 0) ok = warp_wait(&sh.vfull[st], (t >> 1) & 1, gave_up, stats);
-          ok = ok && warp_wait(&sh.pfull[wg], pu[wg] & 1, gave_up, stats);
+          if (!p.two || wg == 0) ok = warp_wait(&sh.vfull[st], (t >> 1) & 1, waits, stats);
+          ok = ok && warp_wait(&sh.pfull[wg], pu[wg] & 1, waits, stats);
           if (!ok) break;
           const uint32_t pv_idesc = __shfl_sync(0xffffffffu, p.nodes && t == kt ? n_idesc : o_idesc, 0);
           ++pu[wg];
@@ -909,7 +909,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
     if (warp == kTrIssuer) {
       // What was issued is done before the memory goes away: the softmax warps waited for the last
       // products, unless somebody gave up.  (Read behind the barrier, when nobody can any more.)
-      if (*gave_up) {
+      if (waits->gave_up) {
         const unsigned long long t0 = now_ns();
         while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
       }

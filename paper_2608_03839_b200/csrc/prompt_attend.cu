@@ -101,7 +101,7 @@ struct PaShared {
   PaItem item[2];
   float2 ml[256];                                        // a cluster's: maxima and sums of A's rows and B's
   uint32_t tmem;
-  int gave_up;
+  Waits waits;
 };
 
 template <int D>
@@ -288,7 +288,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
   PaShared& sh = *reinterpret_cast<PaShared*>(ring + P::kStages * P::kMat);
   PromptList& list = *reinterpret_cast<PromptList*>(ring + P::kStages * P::kMat + (sizeof(PaShared) + 15) / 16 * 16);
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-  volatile int* gave_up = &sh.gave_up;
+  volatile Waits* waits = &sh.waits;
 
   if (tid == 0) {
     for (int i = 0; i < P::kStages; ++i) {
@@ -306,7 +306,6 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       bar_init(&sh.item_free[i], kPaSoftWarps + 1);
     }
     sh.item[0].live = 0;
-    sh.gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kPaIssuer) {
@@ -314,6 +313,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   pdl_enter();
+  if (tid == 0) waits_begin(sh.waits, a.stats);
   prompt_extents(a, list);
   const PaOrder order = {&list, 8 - a.log_pack, a.qs.first ? 0 : a.qs.rows};
   __syncthreads();
@@ -335,7 +335,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
     uint32_t su = 0, ou = 0;
     bool ok = true;
     for (uint32_t iu = 0; ok; ++iu) {
-      if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, gave_up, a.stats)) break;
+      if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, waits, a.stats)) break;
       // (read again where the rows are written: there are no registers to keep it in)
       volatile const PaItem& now = sh.item[iu & 1];
       if (!now.live) break;
@@ -347,7 +347,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         vis[r] = tok < n ? min(c, c - n + tok + 1) : 0;
       }
       for (int j = now.begin; j < now.end[wg]; ++j, ++su) {
-        if (!warp_wait(&sh.sfull[wg], su & 1, gave_up, a.stats)) { ok = false; break; }
+        if (!warp_wait(&sh.sfull[wg], su & 1, waits, a.stats)) { ok = false; break; }
         fence_after();
         uint32_t x[64];
         tmem_ask_rows(s_tm, x);
@@ -445,7 +445,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       if (!ok) break;
       const bool any = now.end[wg] > now.begin;
       if (any) {
-        if (!warp_wait(&sh.ofull[wg], ou++ & 1, gave_up, a.stats)) break;
+        if (!warp_wait(&sh.ofull[wg], ou++ & 1, waits, a.stats)) break;
         fence_after();
       }
 #pragma unroll
@@ -546,7 +546,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       const PaItem& it = sh.item[0];
       __syncwarp();
       if (lane == 0) bar_arrive(&sh.meet);
-      if (warp_wait(&sh.meet, 0, gave_up, a.stats) && it.live && it.end[wg] > it.begin) leave_rows<D>(acc, o_tm, wg * 128 + row0);
+      if (warp_wait(&sh.meet, 0, waits, a.stats) && it.live && it.end[wg] > it.begin) leave_rows<D>(acc, o_tm, wg * 128 + row0);
       fence_before();
       meet_cluster();
       if (it.live) join_rows<D, kBf16>(a, it, acc, sh.ml, shares, rank);
@@ -592,7 +592,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         const int end = (int)((long long)all * (rank + 1) / shares);
 #pragma unroll
         for (int g = 0; g < 2; ++g) it.end[g] = max(min(end, it.tiles[g]), it.begin);
-        if (iu >= 2 && !warp_wait(&sh.item_free[iu & 1], ((iu >> 1) - 1) & 1, gave_up, a.stats)) break;
+        if (iu >= 2 && !warp_wait(&sh.item_free[iu & 1], ((iu >> 1) - 1) & 1, waits, a.stats)) break;
         if (lane == 0) {
           sh.item[iu & 1] = it;
           bar_arrive(&sh.item_full[iu & 1]);
@@ -603,7 +603,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         const int qs = a.qs.first ? 0 : s, ks = a.ks.first ? 0 : s;
         for (int j = 0; j < 2 * n_tiles && ok; ++j, ++u) {               // K0 (then Q), V0, K1, V1, ..
           const uint32_t st = u % P::kStages, use = u / P::kStages;
-          if (use > 0 && !warp_wait(&sh.free[st], (use - 1) & 1, gave_up, a.stats)) { ok = false; break; }
+          if (use > 0 && !warp_wait(&sh.free[st], (use - 1) & 1, waits, a.stats)) { ok = false; break; }
           if (leader) {
             bar_expect(&sh.full[st], P::kMat);
 #pragma unroll
@@ -613,7 +613,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
           }
           __syncwarp();
           if (j == 0) {
-            if (qu > 0 && !warp_wait(&sh.qfree, (qu - 1) & 1, gave_up, a.stats)) { ok = false; break; }
+            if (qu > 0 && !warp_wait(&sh.qfree, (qu - 1) & 1, waits, a.stats)) { ok = false; break; }
             ++qu;
             if (leader) {
               bar_expect(&sh.qfull, 2 * P::kMat);
@@ -639,7 +639,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       uint32_t u = 0, qu = 0, pu[2] = {0, 0};
       bool ok = true;
       for (uint32_t iu = 0; ok; ++iu) {
-        if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, gave_up, a.stats)) break;
+        if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, waits, a.stats)) break;
         const int live = sh.item[iu & 1].live, begin = sh.item[iu & 1].begin, tiles0 = sh.item[iu & 1].end[0] - begin,
                   tiles1 = sh.item[iu & 1].end[1] - begin;
         __syncwarp();
@@ -647,7 +647,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         if (!live) break;
         const int n_tiles = max(tiles0, tiles1);
         if (n_tiles == 0) continue;
-        auto landed = [&](uint32_t v) { ok = ok && warp_wait(&sh.full[v % P::kStages], (v / P::kStages) & 1, gave_up, a.stats); };
+        auto landed = [&](uint32_t v) { ok = ok && warp_wait(&sh.full[v % P::kStages], (v / P::kStages) & 1, waits, a.stats); };
         auto scores = [&](int g, uint32_t kv) {          // of group g, keys in ring place kv
           const uint64_t kd = k_desc + (kv % P::kStages) * kStage;
           if (leader) {
@@ -661,7 +661,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
           __syncwarp();
         };
         landed(u);
-        ok = ok && warp_wait(&sh.qfull, qu++ & 1, gave_up, a.stats);
+        ok = ok && warp_wait(&sh.qfull, qu++ & 1, waits, a.stats);
         if (!ok) break;
         fence_after();
         if (tiles0 > 0) scores(0, u);
@@ -683,7 +683,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
               const uint64_t vd = v_desc + (vu % P::kStages) * kStage;
 #pragma unroll
               for (int h = 0; h < 2 && ok; ++h) {        // half of the keys at a time, as the probabilities come
-                if (!warp_wait(&sh.pfull[g][h], pu[g] & 1, gave_up, a.stats)) { ok = false; break; }
+                if (!warp_wait(&sh.pfull[g][h], pu[g] & 1, waits, a.stats)) { ok = false; break; }
                 fence_after();
                 if (leader) {
 #pragma unroll
@@ -722,7 +722,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       // The softmax warps waited for the last products, and the products for the last copies, unless
       // somebody gave up: then what is in flight gets time to end.  (Read behind the barrier, when nobody
       // can any more.)
-      if (*gave_up) {
+      if (waits->gave_up) {
         const unsigned long long t0 = now_ns();
         while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
       }

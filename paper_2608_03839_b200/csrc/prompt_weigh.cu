@@ -69,7 +69,7 @@ struct PwShared {
   float shared[2 * kPrTile];                             // of the block, for the cluster
   int from[kPrMaxSeq], to[kPrMaxSeq];                    // rows of a sequence that count
   uint32_t tmem;
-  int gave_up;
+  Waits waits;
 };
 
 template <int D>
@@ -153,7 +153,7 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
   PromptList& list = *reinterpret_cast<PromptList*>(ring + P::kStages * P::kMat + (sizeof(PwShared) + 15) / 16 * 16);
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int rank = blockIdx.x % shares;                  // in the cluster
-  volatile int* gave_up = &sh.gave_up;
+  volatile Waits* waits = &sh.waits;
 
   if (tid == 0) {
     for (int i = 0; i < P::kStages; ++i) {
@@ -176,7 +176,6 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
       bar_init(&sh.rows_free[i], kPwSumWarps);
     }
     bar_init(&sh.meet, kPwSumWarps);
-    sh.gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kPwIssuer) {
@@ -184,6 +183,7 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   pdl_enter();
+  if (tid == 0) waits_begin(sh.waits, a.stats);
   prompt_extents(a, list);
   __syncthreads();
   const PwOrder order = {&list, 7 - a.log_pack, a.ks.first ? 0 : a.ks.rows};
@@ -203,7 +203,7 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
     const float2 f2 = make_float2(a.factor, a.factor);
     uint32_t u = 0, su = 0;
     for (uint32_t iu = 0;; ++iu) {
-      if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, gave_up, a.stats)) break;
+      if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, waits, a.stats)) break;
       const PwItem& now = sh.item[iu & 1];
       const int live = now.live, begin = now.begin, end = now.end, tiles = now.tiles, skip = wg ? now.skip : 0, from = now.from;
       const int s = now.s, head = now.head, c = now.c, k0 = now.k0, key = now.key0 + wg * kPrTile + row;
@@ -217,9 +217,9 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
       for (int i = begin; i < end; ++i, ++u, t = t + 1 == tiles ? 0 : t + 1) {
         const uint32_t rs = u % kPwAhead, b = su & 1;
         // (also where nothing is done with the tile: its place is given back once each time it is full)
-        if (!warp_wait(&sh.rows_full[rs], (u / kPwAhead) & 1, gave_up, a.stats)) { ok = false; break; }
+        if (!warp_wait(&sh.rows_full[rs], (u / kPwAhead) & 1, waits, a.stats)) { ok = false; break; }
         if (t >= skip) {
-          if (!warp_wait(&sh.sfull[wg][b], (su >> 1) & 1, gave_up, a.stats)) { ok = false; break; }
+          if (!warp_wait(&sh.sfull[wg][b], (su >> 1) & 1, waits, a.stats)) { ok = false; break; }
           fence_after();
           ++su;
           // columns whose rows do not see the key
@@ -280,7 +280,7 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
       sums[half][wg * kPrTile + row] = total + lost;
       __syncwarp();
       if (lane == 0) bar_arrive(&sh.meet);
-      if (!warp_wait(&sh.meet, iu & 1, gave_up, a.stats)) break;
+      if (!warp_wait(&sh.meet, iu & 1, waits, a.stats)) break;
       if (half == 0) {
         const float sum = sums[0][wg * kPrTile + row] + sums[1][wg * kPrTile + row];
         if (shares > 1) sh.shared[wg * kPrTile + row] = sum;
@@ -339,14 +339,14 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
         const long long all = (long long)packs * next.tiles;
         next.begin = (int)(all * rank / shares);
         next.end = (int)(all * (rank + 1) / shares);
-        if (iu >= 2 && !warp_wait(&sh.item_free[iu & 1], ((iu >> 1) - 1) & 1, gave_up, a.stats)) break;
+        if (iu >= 2 && !warp_wait(&sh.item_free[iu & 1], ((iu >> 1) - 1) & 1, waits, a.stats)) break;
         if (lane == 0) {
           sh.item[iu & 1] = next;
           bar_arrive(&sh.item_full[iu & 1]);
         }
         if (next.begin < next.end) {
           const uint32_t place = ku & 1;
-          if (ku >= 2 && !warp_wait(&sh.kfree[place], ((ku >> 1) - 1) & 1, gave_up, a.stats)) break;
+          if (ku >= 2 && !warp_wait(&sh.kfree[place], ((ku >> 1) - 1) & 1, waits, a.stats)) break;
           ++ku;
           if (leader) {
             bar_expect(&sh.kfull[place], 2 * P::kMat);
@@ -362,7 +362,7 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
         // ---- this one's queries ----
         for (int j = cur.begin; j < cur.end; ++j, ++u) {
           const uint32_t st = u % P::kStages, use = u / P::kStages;
-          if (use > 0 && !warp_wait(&sh.free[st], (use - 1) & 1, gave_up, a.stats)) { ok = false; break; }
+          if (use > 0 && !warp_wait(&sh.free[st], (use - 1) & 1, waits, a.stats)) { ok = false; break; }
           if (leader) {
             bar_expect(&sh.full[st], P::kMat);
 #pragma unroll
@@ -382,7 +382,7 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
       uint32_t u = 0;
       bool ok = true;
       for (uint32_t iu = 0; ok; ++iu) {
-        if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, gave_up, a.stats)) break;
+        if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, waits, a.stats)) break;
         const PwItem& now = sh.item[iu & 1];
         const int live = now.live, begin = now.begin, end = now.end, tiles = now.tiles, from = now.from, to = now.to;
         const int s = a.qs.first ? 0 : now.s, q0 = now.q0, head0 = now.head * a.group;
@@ -425,7 +425,7 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
           }
           if (i + 1 < end) ask(i + 1);
           const bool plain = __all_sync(0xffffffffu, counts[0] && counts[1] && weight.x == 1.f && weight.y == 1.f);
-          if (use > 0 && !warp_wait(&sh.rows_free[rs], (use - 1) & 1, gave_up, a.stats)) { ok = false; break; }
+          if (use > 0 && !warp_wait(&sh.rows_free[rs], (use - 1) & 1, waits, a.stats)) { ok = false; break; }
           *reinterpret_cast<float2*>(sh.bias[rs] + col) = bias;
           *reinterpret_cast<float2*>(sh.weight[rs] + col) = weight;
           if (lane == 0) sh.plain[rs][half] = plain;
@@ -442,7 +442,7 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
       uint32_t u = 0, ku = 0, su[2] = {0, 0};
       bool ok = true;
       for (uint32_t iu = 0; ok; ++iu) {
-        if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, gave_up, a.stats)) break;
+        if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, waits, a.stats)) break;
         const PwItem& it = sh.item[iu & 1];
         const int live = it.live, tiles = it.tiles, skip = it.skip, begin = it.begin, end = it.end;
         __syncwarp();
@@ -450,18 +450,18 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
         if (!live) break;
         if (begin >= end) continue;
         const uint32_t place = ku & 1;
-        if (!warp_wait(&sh.kfull[place], (ku >> 1) & 1, gave_up, a.stats)) break;
+        if (!warp_wait(&sh.kfull[place], (ku >> 1) & 1, waits, a.stats)) break;
         ++ku;
         const uint64_t kd = k_desc + place * 2 * kStage;
         for (int i = begin; i < end && ok; ++i, ++u) {
           const uint32_t st = u % P::kStages;
-          if (!warp_wait(&sh.full[st], (u / P::kStages) & 1, gave_up, a.stats)) { ok = false; break; }
+          if (!warp_wait(&sh.full[st], (u / P::kStages) & 1, waits, a.stats)) { ok = false; break; }
           const uint64_t qd = q_desc + st * kStage;
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
             if (g && i % tiles < skip) continue;
             const uint32_t b = su[g] & 1, use = su[g] >> 1;
-            if (use > 0 && !warp_wait(&sh.sfree[g][b], (use - 1) & 1, gave_up, a.stats)) { ok = false; break; }
+            if (use > 0 && !warp_wait(&sh.sfree[g][b], (use - 1) & 1, waits, a.stats)) { ok = false; break; }
             ++su[g];
             fence_after();
             if (leader) {
@@ -489,7 +489,7 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
     if (warp == kPwIssuer) {
       fence_after();
       // (the sums waited for all products, and those for all copies, unless somebody gave up)
-      if (*gave_up) {
+      if (waits->gave_up) {
         const unsigned long long t0 = now_ns();
         while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
       }

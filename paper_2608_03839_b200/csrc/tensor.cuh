@@ -11,6 +11,26 @@ __device__ __forceinline__ void bar_init(uint64_t* b, uint32_t n) {
 __device__ __forceinline__ void bar_arrive(uint64_t* b) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(kv_smem(b)) : "memory");
 }
+// What a block's waits go by, in shared memory.
+struct Waits {
+  uint32_t limit;                        // steps of 64 ns (up to 274 s)
+  int gave_up;                           // a wait ran out: all roles leave
+};
+// one thread, in front of a barrier of the block
+__device__ __forceinline__ void waits_begin(Waits& w, const DeviceStats* stats) {
+  w.limit = (uint32_t)min(wait_limit_ns(stats) >> 6, 0xfffffffeull);
+  w.gave_up = 0;
+}
+__device__ __forceinline__ bool bar_test(uint64_t* b, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(kv_smem(b)), "r"(parity) : "memory");
+  return ok != 0;
+}
+// the same, asleep for as long as the device allows (some ten microseconds) or until the phase is complete
 __device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity) {
   uint32_t ok;
   asm volatile(
@@ -25,25 +45,24 @@ __device__ __forceinline__ unsigned long long now_ns() {
   asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
   return t;
 }
-// Bounded wait; false if it gave up or another role did.
-__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* gave_up, DeviceStats* stats) {
-  if (bar_try(b, parity)) return true;
-  const unsigned long long t0 = now_ns(), limit = wait_limit_ns(stats);
-  for (uint32_t spin = 0;; ++spin) {
-    if (bar_try(b, parity)) return true;
-    if ((spin & 63u) == 63u) {
-      if (*gave_up) return false;
-      if (now_ns() - t0 > limit) {
-        *gave_up = 1;
-        atomicExch(&stats->stalled, 1);
-        return false;
-      }
+// Bounded wait; false if it gave up or another role did.  (Where the limit is short nobody sleeps: with tries alone
+// waits of microseconds ended before they looked at the clock.)
+__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile Waits* w, DeviceStats* stats) {
+  if (bar_test(b, parity)) return true;
+  const uint32_t t0 = (uint32_t)(now_ns() >> 6);
+  for (;;) {
+    if (w->limit < 1024u ? bar_test(b, parity) : bar_try(b, parity)) return true;
+    if (w->gave_up) return false;
+    if ((uint32_t)(now_ns() >> 6) - t0 > w->limit) {
+      w->gave_up = 1;
+      atomicExch(&stats->stalled, 1);
+      return false;
     }
   }
 }
 // the same by a converged warp, one outcome for all lanes
-__device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, volatile int* gave_up, DeviceStats* stats) {
-  return __all_sync(0xffffffffu, bar_wait(b, parity, gave_up, stats));
+__device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, volatile Waits* w, DeviceStats* stats) {
+  return __all_sync(0xffffffffu, bar_wait(b, parity, w, stats));
 }
 __device__ __forceinline__ bool one_lane() {
   uint32_t p;
