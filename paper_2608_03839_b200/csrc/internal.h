@@ -119,7 +119,7 @@ cudaError_t preload_all_kernels();
 struct DeviceStats {
   unsigned long long degenerate_rows;
   unsigned long long nonfinite_queries;
-  int stalled;
+  int stalled;                            // not 0: a wait ran out (the tensor-core kernels over prompts and trees count)
   int pad;
   // how long a device-side wait may spin before it gives up, in nanoseconds of %globaltimer
   // (0 = kDefaultWaitNs); survives reset()

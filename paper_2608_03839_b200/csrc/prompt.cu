@@ -10,7 +10,7 @@
 
 using namespace oilbird;
 
-// One per device: where a wait that ran out is remembered, and the limit of the waits.
+// One per device: how often a wait ran out, and the limit of the waits.
 static __device__ DeviceStats g_prompt_stats;
 
 static thread_local char g_prompt_err[256] = "";
@@ -186,9 +186,14 @@ int oilbird_prompt_status(int32_t device, void* cuda_stream) {
   DeviceStats *stats, got;
   PTRY(dev.enter(&sms, &stats));
   PCU(cudaMemcpyAsync(&got, stats, sizeof got, cudaMemcpyDeviceToHost, (cudaStream_t)cuda_stream));
-  PCU(cudaMemsetAsync(&stats->stalled, 0, sizeof stats->stalled, (cudaStream_t)cuda_stream));
   PCU(cudaStreamSynchronize((cudaStream_t)cuda_stream));
-  return got.stalled ? OILBIRD_ESTALL : OILBIRD_OK;
+  // The device counts on and nothing is cleared (what another stream's call adds meanwhile would be lost); a count beyond
+  // the last one reported, by whichever thread, is news.
+  static std::atomic<int> reported[64];
+  int was = reported[device].load();
+  while ((int)((unsigned)got.stalled - (unsigned)was) > 0)
+    if (reported[device].compare_exchange_weak(was, got.stalled)) return OILBIRD_ESTALL;
+  return OILBIRD_OK;
 }
 
 int oilbird_prompt_set_wait_limit(int32_t device, uint64_t limit_ns, void* cuda_stream) {

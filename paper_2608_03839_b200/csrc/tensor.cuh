@@ -55,7 +55,7 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile 
     if (w->gave_up) return false;
     if ((uint32_t)(now_ns() >> 6) - t0 > w->limit) {
       w->gave_up = 1;
-      atomicExch(&stats->stalled, 1);
+      atomicAdd(&stats->stalled, 1);
       return false;
     }
   }

@@ -40,3 +40,48 @@ def test_waits_that_run_out_are_reported_once(d, lengths):
     for call in calls.values():
         call()
     assert B.prompt_status() == B.OK
+
+
+def test_a_status_elsewhere_loses_no_report():
+    """Another thread asks for the status all the time, on a stream of its own: a call that gives up is reported to
+    one of the two, whenever that happens."""
+    q, k, v, first = made([700, 2000], 128)
+    want = B.prompt_attend(q, k, v, first=first)[0]
+    torch.cuda.synchronize()
+    assert B.prompt_status() == B.OK
+    elsewhere, done = [0], threading.Event()
+
+    def ask():
+        stream = torch.cuda.Stream()
+        while not done.is_set():
+            elsewhere[0] += B.prompt_status(stream=stream) == B.ESTALL
+
+    thread = threading.Thread(target=ask)
+    gave_up = lost = 0
+    stream = torch.cuda.Stream()
+    try:
+        B.prompt_set_wait_limit(1)
+        torch.cuda.synchronize()
+        thread.start()
+        with torch.cuda.stream(stream):
+            for _ in range(200):
+                before = elsewhere[0]
+                out = torch.zeros_like(want)
+                B.prompt_attend(q, k, v, first=first, out=out)
+                stream.synchronize()
+                here = B.prompt_status() == B.ESTALL
+                if torch.equal(out, want):
+                    continue
+                gave_up += 1
+                if not here:                               # the other thread has it, or is about to
+                    for _ in range(100):
+                        if elsewhere[0] > before:
+                            break
+                        done.wait(0.001)
+                    lost += elsewhere[0] == before
+    finally:
+        done.set()
+        thread.join()
+        B.prompt_set_wait_limit(0)
+        B.prompt_status()
+    assert gave_up > 0 and lost == 0, (gave_up, lost)
