@@ -914,6 +914,12 @@ def _kv_check(rc: int, where: str) -> None:
         raise err
 
 
+def _no_backward(who: str) -> None:
+    """For a tensor that wants a gradient: results come without one."""
+    if torch.is_grad_enabled():
+        raise RuntimeError(f"{who} no backward pass: detach the tensor, or call under torch.no_grad()")
+
+
 class KVCache:
     """Keys and values of n_seq requests (one layer) in 4 bits, in pages, with the attention
     weight each slot has received (oilbird_kv_* of the C-ABI; see include/oilbird.h for the
@@ -997,9 +1003,8 @@ class KVCache:
     def _rows(self, t: torch.Tensor, heads: int, m: int):
         """The C view of a [n_seq, m, heads, head_dim] tensor (any strides but the last)."""
         if t.dtype is self.dtype and t.shape == (self.n_seq, m, heads, self.head_dim) and t.get_device() == self._index:
-            if t.requires_grad and torch.is_grad_enabled():
-                raise RuntimeError("the key/value cache has no backward pass: detach the tensor, or call under "
-                                   "torch.no_grad()")
+            if t.requires_grad:
+                _no_backward("the key/value cache has")
             s0, s1, s2, s3 = t.stride()
             if s3 == 1:
                 return _KV_ROWS(t.data_ptr(), s0, s1, s2)
@@ -1018,12 +1023,16 @@ class KVCache:
             return None
         if t.dtype is not dtype or t.shape != shape or t.get_device() != self._index or not t.is_contiguous():
             raise AssertionError(f"a contiguous {dtype} tensor {list(shape)} on {self._dev}")
+        if t.requires_grad:
+            _no_backward("the key/value cache has")
         return t.data_ptr()
 
     def _lse(self, t, m, heads):
         """Pointer and strides of a [n_seq, m, heads] fp32 tensor."""
         if t.dtype is not torch.float32 or t.shape != (self.n_seq, m, heads) or t.get_device() != self._index:
             raise AssertionError(f"an fp32 tensor [{self.n_seq}, {m}, {heads}] on {self._dev}")
+        if t.requires_grad:
+            _no_backward("the key/value cache has")
         return t.data_ptr(), None if t.is_contiguous() else _KV_STRIDES(*t.stride())
 
     def _mask(self, mask, m):
@@ -1192,14 +1201,16 @@ class _Prompt:
             return None
         if t.dtype is not dtype or t.shape != shape or t.get_device() != self.index or not t.is_contiguous():
             raise AssertionError(f"a contiguous {dtype} tensor {list(shape)} on {self.dev}")
+        if t.requires_grad:
+            _no_backward("prompt calls have")
         return t.data_ptr()
 
     # (what runs for every argument of every call bounds the smallest calls: see KVCache._rows)
     def view(self, t, shape):
         """The C view of a tensor of that shape (any strides but the last)."""
         if t.dtype is self.dtype and t.shape == shape and t.get_device() == self.index:
-            if t.requires_grad and torch.is_grad_enabled():
-                raise RuntimeError("prompt calls have no backward pass: detach the tensor, or call under torch.no_grad()")
+            if t.requires_grad:
+                _no_backward("prompt calls have")
             stride = t.stride()
             if stride[-1] == 1:
                 return _KV_ROWS(t.data_ptr(), *stride[:3]) if len(stride) == 4 else _KV_ROWS(t.data_ptr(), 0, *stride[:2])
@@ -1215,6 +1226,8 @@ class _Prompt:
         """Pointer and strides of an fp32 tensor [.., n_q_heads]."""
         if t.dtype is not torch.float32 or t.shape != self.q_shape[:-1] or t.get_device() != self.index:
             raise AssertionError(f"an fp32 tensor {list(self.q_shape[:-1])} on {self.dev}")
+        if t.requires_grad:
+            _no_backward("prompt calls have")
         if t.is_contiguous():
             return t.data_ptr(), None
         return t.data_ptr(), _KV_STRIDES(0 if self.packed else t.stride(0), *t.stride()[-2:])
@@ -1299,8 +1312,8 @@ def token_scores(logits: torch.Tensor, tokens: torch.Tensor | None = None, top: 
             (logits.stride(1) != 1 and logits.shape[1] > 1):
         raise AssertionError("logits: a bf16, f16 or fp32 tensor [rows, vocab] on a CUDA device, with contiguous rows; "
                              "there is no CPU fallback")
-    if logits.requires_grad and torch.is_grad_enabled():
-        raise RuntimeError("token scores have no backward pass: detach the logits, or call under torch.no_grad()")
+    if logits.requires_grad:
+        _no_backward("token scores have")
     rows, vocab = logits.shape
     index, dev = logits.get_device(), logits.device
     n = 0
