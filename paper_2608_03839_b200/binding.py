@@ -215,6 +215,20 @@ def _torch_empty(shape, dtype, device):
 ALLOC = _torch_empty
 
 
+def _results(stream, make):
+    """make(): the results of a call on `stream` (None: the current one).  Their memory is that stream's, as it is under
+    torch.cuda.stream(stream) - the current stream may still be at work on what lay there -, and once they are
+    dropped it waits for the current stream too."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        got = make()
+    for t in (got,) if isinstance(got, torch.Tensor) else vars(got).values() if isinstance(got, TokenScores) else got:
+        if t is not None:
+            t.record_stream(torch.cuda.current_stream(t.device))
+    return got
+
+
 def lib() -> ctypes.CDLL:
     """Load liboilbird.so (built by ``paper_2608_03839_b200.build``); raises if absent."""
     global _lib
@@ -297,12 +311,12 @@ class QueryOut:
     _c: CQueryOut = field(default=None, repr=False)
 
     @staticmethod
-    def empty(nq: int, k: int, L: int, device) -> "QueryOut":
-        o = QueryOut(ALLOC((nq, k), torch.int32, device),
-                     ALLOC((nq, k), torch.float32, device),
-                     ALLOC((nq,), torch.int32, device),
-                     ALLOC((nq, k), torch.int32, device),
-                     ALLOC((nq, k, L), torch.int32, device))
+    def empty(nq: int, k: int, L: int, device, stream=None) -> "QueryOut":
+        o = QueryOut(*_results(stream, lambda: (ALLOC((nq, k), torch.int32, device),
+                                                ALLOC((nq, k), torch.float32, device),
+                                                ALLOC((nq,), torch.int32, device),
+                                                ALLOC((nq, k), torch.int32, device),
+                                                ALLOC((nq, k, L), torch.int32, device))))
         o._c = CQueryOut(o.idx.data_ptr(), o.score.data_ptr(), o.fired.data_ptr(),
                          o.cont_len.data_ptr(), o.cont_tok.data_ptr())
         return o
@@ -330,7 +344,7 @@ def query_static(keys: torch.Tensor, tokens: torch.Tensor, trace_id: torch.Tenso
     q = q.reshape(-1, d)
     nq = q.shape[0]
     if out is None:
-        out = QueryOut.empty(nq, params.k, params.cont_len, keys.device)
+        out = QueryOut.empty(nq, params.k, params.cont_len, keys.device, stream)
     sp = StaticPool(keys.data_ptr(), tokens.data_ptr(), trace_id.data_ptr(), trace_end.data_ptr(),
                     n, d, keys.device.index or 0)
     cp = params.to_c(None)
@@ -466,7 +480,7 @@ class Pool:
         """Local rows (int32) -> global positions (int64); -1 stays -1."""
         assert idx.is_cuda and idx.dtype == torch.int32 and idx.is_contiguous()
         if out is None:
-            out = ALLOC(tuple(idx.shape), torch.int64, idx.device)
+            out, = _results(stream, lambda: (ALLOC(tuple(idx.shape), torch.int64, idx.device),))
         _check(self._L.oilbird_pool_to_global(self._h, idx.data_ptr(), out.data_ptr(),
                                               idx.numel(), _stream_ptr(stream)),
                "oilbird_pool_to_global")
@@ -484,7 +498,7 @@ class Pool:
             assert ex.is_cuda and ex.dtype in (torch.int64, torch.uint64) and ex.numel() == nq
             ex_ptr = ex.data_ptr()
         if out is None:
-            out = QueryOut.empty(nq, pr.k, pr.cont_len, self._dev)
+            out = QueryOut.empty(nq, pr.k, pr.cont_len, self._dev, stream)
         cp = pr.to_c(ex_ptr)
         _check(self._L.oilbird_pool_query(self._h, q.data_ptr(), nq, ctypes.byref(cp),
                                           ctypes.byref(out._c), _stream_ptr(stream)),
@@ -518,7 +532,7 @@ class Pool:
             assert ex.is_cuda and ex.dtype in (torch.int64, torch.uint64) and ex.numel() == nq
             ex_ptr = ex.data_ptr()
         if out is None:
-            out = QueryOut.empty(nq, pr.k, pr.cont_len, self._dev)
+            out = QueryOut.empty(nq, pr.k, pr.cont_len, self._dev, stream)
         cp = pr.to_c(ex_ptr)
         _check(self._L.oilbird_pool_step(
             self._h, states.data_ptr(), tokens.data_ptr(), n, int(tag),
@@ -530,7 +544,7 @@ class Pool:
                stream=None) -> QueryOut:
         assert idx.is_cuda and idx.dtype == torch.int32 and score.dtype == torch.float32
         nq = idx.shape[0]
-        out = QueryOut.empty(nq, params.k, params.cont_len, self._dev)
+        out = QueryOut.empty(nq, params.k, params.cont_len, self._dev, stream)
         out.idx, out.score = idx, score
         cp = params.to_c(None)
         co = CQueryOut(None, None, out.fired.data_ptr(), out.cont_len.data_ptr(),
@@ -704,7 +718,7 @@ class Index:
             assert ex.is_cuda and ex.dtype in (torch.int64, torch.uint64) and ex.numel() == nq
             ex_ptr = ex.data_ptr()
         if out is None:
-            out = QueryOut.empty(nq, pr.k, pr.cont_len, self.pool._dev)
+            out = QueryOut.empty(nq, pr.k, pr.cont_len, self.pool._dev, stream)
         cp = pr.to_c(ex_ptr)
         _check(self._L.oilbird_index_query(self._h, q.data_ptr(), nq, int(n_probe), ctypes.byref(cp),
                                            ctypes.byref(out._c), _stream_ptr(stream)),
@@ -780,6 +794,13 @@ class Ring:
                                            rollouts.data_ptr(), n, _stream_ptr(stream)),
                "oilbird_ring_append")
 
+    def _out(self, nq: int, m: int, stream) -> RingOut:
+        return RingOut(*_results(stream, lambda: (ALLOC((nq, m), torch.int32, self._dev),
+                                                  ALLOC((nq, m), torch.float32, self._dev),
+                                                  ALLOC((nq,), torch.int32, self._dev),
+                                                  ALLOC((nq, m, self.max_rollout), torch.int32, self._dev),
+                                                  ALLOC((nq, m), torch.int32, self._dev))))
+
     def query(self, q: torch.Tensor, anchors: torch.Tensor, m: int = 4, floor: float = 0.8,
               out: RingOut | None = None, stream=None) -> RingOut:
         assert q.is_cuda and q.dtype == torch.bfloat16 and q.is_contiguous()
@@ -787,11 +808,7 @@ class Ring:
         nq = q.shape[0]
         assert anchors.is_cuda and anchors.dtype == torch.int32 and anchors.numel() == nq
         if out is None:
-            out = RingOut(ALLOC((nq, m), torch.int32, self._dev),
-                          ALLOC((nq, m), torch.float32, self._dev),
-                          ALLOC((nq,), torch.int32, self._dev),
-                          ALLOC((nq, m, self.max_rollout), torch.int32, self._dev),
-                          ALLOC((nq, m), torch.int32, self._dev))
+            out = self._out(nq, m, stream)
         co = CRingOut(out.slot.data_ptr(), out.score.data_ptr(), out.count.data_ptr(),
                       out.rollout.data_ptr(), out.rollout_len.data_ptr())
         _check(self._L.oilbird_ring_query(self._h, q.data_ptr(), anchors.data_ptr(), nq, int(m),
@@ -813,11 +830,7 @@ class Ring:
         nq = q.shape[0]
         assert q_anchors.is_cuda and q_anchors.dtype == torch.int32 and q_anchors.numel() == nq
         if out is None:
-            out = RingOut(ALLOC((nq, m), torch.int32, self._dev),
-                          ALLOC((nq, m), torch.float32, self._dev),
-                          ALLOC((nq,), torch.int32, self._dev),
-                          ALLOC((nq, m, self.max_rollout), torch.int32, self._dev),
-                          ALLOC((nq, m), torch.int32, self._dev))
+            out = self._out(nq, m, stream)
         co = CRingOut(out.slot.data_ptr(), out.score.data_ptr(), out.count.data_ptr(),
                       out.rollout.data_ptr(), out.rollout_len.data_ptr())
         _check(self._L.oilbird_ring_step(self._h, states.data_ptr(), anchors.data_ptr(),
@@ -873,11 +886,9 @@ def merge_chains(tree_tok: torch.Tensor, tree_parent: torch.Tensor, n_nodes: tor
         depth, mask, status, bought, walked = out.depth, out.mask, out.status, out.bought, out.walked
         assert depth.shape == (nq, max_nodes) and status.shape == (nq, k + ne)
     else:
-        depth = ALLOC((nq, max_nodes), torch.int32, dev)
-        mask = ALLOC((nq, max_nodes), torch.int64, dev)
-        status = ALLOC((nq, k + ne), torch.int32, dev)
-        bought = ALLOC((nq, k + ne), torch.int32, dev)
-        walked = ALLOC((nq, k + ne), torch.int32, dev)
+        depth, mask, status, bought, walked = _results(stream, lambda: (
+            ALLOC((nq, max_nodes), torch.int32, dev), ALLOC((nq, max_nodes), torch.int64, dev),
+            *(ALLOC((nq, k + ne), torch.int32, dev) for _ in range(3))))
     mp = MergeParams(budget, max_nodes, min_len, int(bool(root_attached)))
     ptr = lambda t: None if t is None else t.data_ptr()
     _check(lib().oilbird_merge_chains(nq, ptr(sem_tok), ptr(sem_len), k, L, ptr(extra_tok),
@@ -1044,7 +1055,9 @@ class KVCache:
             raise AssertionError(f"an int64 tensor [{self.n_seq}, {m} or more] on {self._dev}")
         return mask.data_ptr(), mask.stride(0)
 
-    def _new(self, like: torch.Tensor, shape) -> torch.Tensor:
+    def _new(self, like: torch.Tensor, shape, stream) -> torch.Tensor:
+        if stream is not None:
+            return _results(stream, lambda: (self._new(like, shape, None),))[0]
         # (new_empty takes half the time of torch.empty with a type and a device)
         return like.new_empty(shape) if ALLOC is _torch_empty else ALLOC(shape, like.dtype, self._dev)
 
@@ -1085,7 +1098,7 @@ class KVCache:
         """Slots start[s] .. start[s] + n - 1 (int32 [n_seq]; None: from 0) in 16 bits: (k, v), each
         [n_seq, n, n_kv_heads, head_dim]; zeros where a sequence has no slot."""
         shape = (self.n_seq, n, self.n_kv_heads, self.head_dim)
-        k, v = ALLOC(shape, self.dtype, self._dev), ALLOC(shape, self.dtype, self._dev)
+        k, v = _results(stream, lambda: (ALLOC(shape, self.dtype, self._dev), ALLOC(shape, self.dtype, self._dev)))
         _kv_check(self._L.oilbird_kv_read(self._ref, n, self._vec(start, torch.int32, self._seqs),
                                           k.data_ptr(), v.data_ptr(), self._stream(stream)),
                   "oilbird_kv_read")
@@ -1101,9 +1114,9 @@ class KVCache:
         Returns (out, lse): out like q, lse fp32 [n_seq, m, n_q_heads] (natural logarithm)."""
         _, m, heads, _ = q.shape
         if out is None:
-            out = self._new(q, (self.n_seq, m, heads, self.head_dim))
+            out = self._new(q, (self.n_seq, m, heads, self.head_dim), stream)
         if lse is None:
-            lse = self._new(self.weight, (self.n_seq, m, heads))
+            lse = self._new(self.weight, (self.n_seq, m, heads), stream)
         mp, ms = self._mask(mask, m)
         _kv_check(self._L.oilbird_kv_attend(
             self._ref, heads, m, self._rows(q, heads, m),
@@ -1123,7 +1136,7 @@ class KVCache:
         _, m, heads, _ = q.shape
         nodes = None
         if k_new is not None:
-            nodes = self._new(self.weight, (self.n_seq, self.n_kv_heads, m))
+            nodes = self._new(self.weight, (self.n_seq, self.n_kv_heads, m), stream)
         mp, ms = self._mask(mask, m)
         _kv_check(self._L.oilbird_kv_weigh(
             self._ref, heads, m, self._rows(q, heads, m),
@@ -1153,6 +1166,12 @@ class KVCache:
 
 
 # ------------------------------------------------------------------ whole prompts ----
+def _stream_of(stream, t: torch.Tensor):
+    if stream.device != t.device:
+        raise AssertionError(f"a stream of {t.device}")
+    return stream
+
+
 _PROMPT = ctypes.c_int64 * 9         # oilbird_prompt: two sides of three words, six 32-bit numbers
 
 
@@ -1232,9 +1251,6 @@ class _Prompt:
             return t.data_ptr(), None
         return t.data_ptr(), _KV_STRIDES(0 if self.packed else t.stride(0), *t.stride()[-2:])
 
-    def stream(self, stream) -> int:
-        return _raw_stream(self.index) if stream is None else stream.cuda_stream
-
 
 def prompt_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, first: torch.Tensor | None = None,
                   n_new: torch.Tensor | None = None, first_k: torch.Tensor | None = None,
@@ -1247,6 +1263,8 @@ def prompt_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, first: torc
     The query rows are the last of their sequence's keys.  scale: None for 1 / sqrt(head_dim).
     Returns (out, lse): out like q, lse fp32 [..., n_q_heads] (natural logarithm).  Packed rows of no sequence
     are not written."""
+    if stream is not None:
+        return _results(_stream_of(stream, q), lambda: prompt_attend(q, k, v, first, n_new, first_k, n_k, scale, out, lse))
     p = _Prompt(q, k, first, n_new, first_k, n_k)
     out, out_view = p.new(q) if out is None else (out, p.view(out, p.q_shape))
     if lse is None:
@@ -1254,7 +1272,7 @@ def prompt_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, first: torc
                ALLOC(p.q_shape[:-1], torch.float32, p.dev))
     _prompt_check(lib().oilbird_prompt_attend(
         p.c, p.view(q, p.q_shape), p.view(k, p.k_shape), p.view(v, p.k_shape), p.d ** -0.5 if scale is None else scale, out_view,
-        *p.lse(lse), p.stream(stream)), "oilbird_prompt_attend")
+        *p.lse(lse), _raw_stream(p.index)), "oilbird_prompt_attend")
     return out, lse
 
 
@@ -1265,13 +1283,16 @@ def prompt_weigh(q: torch.Tensor, lse: torch.Tensor, k: torch.Tensor, first: tor
     """The attention weight that the rows with row_weight (fp32 [n_seq, rows] or [rows]; None: 1) gave each key in
     prompt_attend (same arguments, and its lse; oilbird_prompt_weigh): fp32 [n_seq, n_kv_heads, rows_k], which
     KVCache.append takes, packed [n_kv_heads, rows_k]."""
+    if stream is not None:
+        return _results(_stream_of(stream, q),
+                        lambda: prompt_weigh(q, lse, k, first, n_new, first_k, n_k, row_weight, scale, weight))
     p = _Prompt(q, k, first, n_new, first_k, n_k)
     shape = (p.kv_heads, p.rows_k) if p.packed_k else (p.n_seq, p.kv_heads, p.rows_k)
     if weight is None:
         weight = ALLOC(shape, torch.float32, p.dev)
     _prompt_check(lib().oilbird_prompt_weigh(
         p.c, p.view(q, p.q_shape), *p.lse(lse), p.view(k, p.k_shape), p.vec(row_weight, torch.float32, p.q_shape[:-2]),
-        p.d ** -0.5 if scale is None else scale, p.vec(weight, torch.float32, shape), p.stream(stream)), "oilbird_prompt_weigh")
+        p.d ** -0.5 if scale is None else scale, p.vec(weight, torch.float32, shape), _raw_stream(p.index)), "oilbird_prompt_weigh")
     return weight
 
 
@@ -1314,6 +1335,8 @@ def token_scores(logits: torch.Tensor, tokens: torch.Tensor | None = None, top: 
                              "there is no CPU fallback")
     if logits.requires_grad:
         _no_backward("token scores have")
+    if stream is not None:
+        return _results(_stream_of(stream, logits), lambda: token_scores(logits, tokens, top))
     rows, vocab = logits.shape
     index, dev = logits.get_device(), logits.device
     n = 0
@@ -1336,7 +1359,7 @@ def token_scores(logits: torch.Tensor, tokens: torch.Tensor | None = None, top: 
                       got.top_logp.data_ptr())
     rc = lib().oilbird_token_scores(logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, rows, vocab,
                                     _LOGITS_DTYPES[logits.dtype], tokens.data_ptr() if n else None, n, top, out, index,
-                                    _raw_stream(index) if stream is None else stream.cuda_stream)
+                                    _raw_stream(index))
     if rc != OK:
         err = OilbirdError(rc, "oilbird_token_scores")
         err.args = (err.args[0] + ": " + lib().oilbird_token_scores_error().decode(),)

@@ -104,11 +104,11 @@ def merge_gathered(gathered: torch.Tensor, lay: RecordLayout, theta: float, stre
     n_shards = gathered.shape[0]
     dev = gathered.device
     nq, k, L = lay.nq, lay.k, lay.L
-    out = ShardedOut(B.ALLOC((nq, k), torch.int64, dev),
-                     B.ALLOC((nq, k), torch.float32, dev),
-                     B.ALLOC((nq,), torch.int32, dev),
-                     B.ALLOC((nq, k), torch.int32, dev),
-                     B.ALLOC((nq, k, L), torch.int32, dev))
+    out = ShardedOut(*B._results(stream, lambda: (B.ALLOC((nq, k), torch.int64, dev),
+                                                  B.ALLOC((nq, k), torch.float32, dev),
+                                                  B.ALLOC((nq,), torch.int32, dev),
+                                                  B.ALLOC((nq, k), torch.int32, dev),
+                                                  B.ALLOC((nq, k, L), torch.int32, dev))))
     B._check(B.lib().oilbird_merge_shards(
         n_shards, nq, k, L, float(theta), gathered.data_ptr(), gathered.stride(0), lay.off_gidx,
         lay.off_score, lay.off_len, lay.off_tok, out.gidx.data_ptr(), out.score.data_ptr(),
