@@ -11,6 +11,7 @@
 //              exponentials, and the probabilities in 16 bits back over the scores
 //   16         loads: queries, then keys and values in turn into a ring, by tensor maps
 //   17         issues the products S = Q K^T and O += P V (P from TMEM)
+//   18, 19     take what is not finite out of values that not every row sees
 // While A's scores go through the exponentials the tensor core works for B, and the other way round.
 //
 // Numbers.  Scores, maxima, sums and accumulators are fp32.  Probabilities are rounded to the inputs'
@@ -20,9 +21,12 @@
 // what lies 17 below the maximum (in exp's units) would otherwise be rounded to nothing.  bf16 takes them lower, as many
 // keys' large values would otherwise add up to more than fp32 holds (see room_of).
 //
-// Values that are not finite.  A masked key's probability is 0, and 0 times an infinity would reach
-// every row of the tile: a row whose output is not finite looks whether such a value lies among the keys of
-// its tiles that it does not see, and is then computed again by its warp from what it does see.
+// Values that are not finite.  A masked key's probability is 0, and 0 times an infinity would reach every row of the
+// tile.  An item with a row whose accumulators are not finite is done once more: of its tiles the last ones, up to
+// three, hold keys that one of its rows does not see (of later tokens, or behind the sequence's last), and there two warps
+// put zeros in place of infinities and NaN before the tile's product.  The rows that do see such a key have its value
+// added when they are written.  (In clusters, which have one item, the tiles are cleaned at once.  Done for every item
+// that took 16 prompts from 225 to 243 us.)
 //
 // Work.  Items by falling number of key tiles, so that the last ones are the short ones; block b takes
 // b, 2G-1-b, 2G+b, ... of G blocks (see prompt_find).
@@ -54,7 +58,7 @@ namespace oilbird {
 
 namespace {
 
-constexpr int kPaThreads = 640, kPaSoftWarps = 16, kPaLoader = 16, kPaIssuer = 17;
+constexpr int kPaThreads = 640, kPaSoftWarps = 16, kPaLoader = 16, kPaIssuer = 17, kPaCleaner = 18, kPaCleaners = 2;
 // registers a thread: launched with 96; the five warpgroups' shares add up to 5 x 96
 constexpr int kPaSoftRegs = 112, kPaRestRegs = 32;
 static_assert(4 * kPaSoftRegs + kPaRestRegs <= 5 * 96, "more registers than the block was launched with");
@@ -65,6 +69,8 @@ struct PaItem {
   int s, tok, head, q_head;          // sequence, first token, key head, first query head
   int n, c, q0, k0;
   int tiles[2];                      // of A and of B: all that their rows see
+  int part;                          // from this tile on there are keys that not every row sees
+  int clean;                         // from this tile on values are cleaned: part, or none
   int begin;                         // this block's: from here on,
   int end[2];                        // up to here
   float room;                        // probabilities are 2^room times as large
@@ -98,8 +104,12 @@ __device__ __forceinline__ float row_lse(float m, float l, float f, float room) 
 }
 struct PaShared {
   uint64_t full[16], free[16], qfull, qfree, sfull[2], pfull[2][2], ofull[2], item_full[2], item_free[2], meet;
+  uint64_t ask, clean, found, written;
   PaItem item[2];
-  float2 ml[256];                                        // a cluster's: maxima and sums of A's rows and B's
+  int again[2];                                          // the item has to be done again, with clean values
+  uint32_t asked;                                        // the use of the ring whose values are to be cleaned
+  struct Odd { int from, to; } odd[kPaCleaners];         // keys among which values were taken out
+  float2 ml[256];                                        // maxima and sums of A's rows and B's, of items that are cleaned
   uint32_t tmem;
   Waits waits;
 };
@@ -155,59 +165,51 @@ __device__ __forceinline__ uint32_t pack_result(float o0, float o1, float u0, fl
   return ((fabsf(o0) < INFINITY ? a : b) & 0xffffu) | ((fabsf(o1) < INFINITY ? a : b) & 0xffff0000u);
 }
 
-// One row again, by a whole warp, from the keys it sees: what masked values were kept out of.
-template <int D, bool kBf16>
-__device__ __noinline__ void row_again(const PromptArgs& a, const PaItem& it, int tok, int head, int vis, float m, int lane) {
-  constexpr int E = D / 64;                              // pairs of channels a lane
-  const uint16_t* qp = a.q.at(a.qs.first ? 0 : it.s, it.q0 + tok, head);
-  float2 q[E], o[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(qp + e * 64 + 2 * lane);
-    q[e] = make_float2(half_lo<kBf16>(w), half_hi<kBf16>(w));
-    o[e] = make_float2(0.f, 0.f);
-  }
-  const float f = a.factor, shift = row_shift(m, f, it.room), less = row_far(m, f) ? m : 0.f;
-  float l = 0.f;
-  for (int j = 0; j < vis; ++j) {
-    const uint16_t* kp = a.k.at(a.ks.first ? 0 : it.s, it.k0 + j, it.head);
-    const uint16_t* vp = a.v.at(a.ks.first ? 0 : it.s, it.k0 + j, it.head);
-    float x = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const uint32_t w = *reinterpret_cast<const uint32_t*>(kp + e * 64 + 2 * lane);
-      x = fmaf(q[e].x, half_lo<kBf16>(w), fmaf(q[e].y, half_hi<kBf16>(w), x));
-    }
-    x = warp_sum(x);
-    const float p = exp2_approx(fmaf((a.negate ? -x : x) - less, f, shift));
-    l += p;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const uint32_t w = *reinterpret_cast<const uint32_t*>(vp + e * 64 + 2 * lane);
-      o[e].x = fmaf(p, half_lo<kBf16>(w), o[e].x);
-      o[e].y = fmaf(p, half_hi<kBf16>(w), o[e].y);
-    }
-  }
-  const float inv = 1.f / l;
-  uint16_t* op = a.out + (a.qs.first ? 0 : it.s) * a.out_seq + (long long)(it.q0 + tok) * a.out_row + head * a.out_head;
-#pragma unroll
-  for (int e = 0; e < E; ++e) *reinterpret_cast<uint32_t*>(op + e * 64 + 2 * lane) = pack_result<kBf16>(o[e].x, o[e].y, o[e].x * inv, o[e].y * inv);
+// The sign bits of those halves of a word that are not finite.
+template <bool kBf16>
+__device__ __forceinline__ uint32_t odd_halves(uint32_t w) {
+  return ((w & (kBf16 ? 0x7f807f80u : 0x7c007c00u)) + (kBf16 ? 0x00800080u : 0x04000400u)) & 0x80008000u;
 }
-
-// Whether a value of keys [from, to) of the item's sequence (as far as the array goes) is not finite; a warp.
+// Adds a lane's channels (pairs, 64 apart) of values [from, to) that are not finite.
 template <int D, bool kBf16>
-__device__ __noinline__ bool odd_values(const PromptArgs& a, const PaItem& it, int from, int to, int lane) {
-  constexpr uint32_t kInf = kBf16 ? 0x7f80u : 0x7c00u;
-  bool odd = false;
-  to = min(to, a.ks.rows - it.k0);
-#pragma unroll 4
-  for (int j = max(from, 0); j < to; ++j)
+__device__ __forceinline__ void add_odd(const PromptArgs& a, const PaItem& it, int from, int to, int lane, float2 (&sum)[D / 64]) {
+#pragma unroll 2
+  for (int j = from; j < to; ++j)
 #pragma unroll
     for (int e = 0; e < D / 64; ++e) {
       const uint32_t w = *reinterpret_cast<const uint32_t*>(a.v.at(a.ks.first ? 0 : it.s, it.k0 + j, it.head) + e * 64 + 2 * lane);
-      odd |= (w & kInf) == kInf || (w >> 16 & kInf) == kInf;
+      const uint32_t odd = odd_halves<kBf16>(w);
+      if (odd & 0xffffu) sum[e].x += half_lo<kBf16>(w);
+      if (odd >> 16) sum[e].y += half_hi<kBf16>(w);
     }
-  return __any_sync(0xffffffffu, odd);
+}
+// The values among keys [from, to) that were taken out, added to those of an item's rows [row0, row0 + 128) that see them; a
+// warp.  The rows' tokens rise, and so does what they see.
+template <int D, bool kBf16>
+__device__ __forceinline__ void odd_rows(const PromptArgs& a, const PaItem& it, const float2* ml, int row0, int from, int to, int lane) {
+  float2 sum[D / 64];
+#pragma unroll
+  for (int e = 0; e < D / 64; ++e) sum[e] = make_float2(0.f, 0.f);
+  int at = from;
+#pragma unroll 1
+  for (int row = row0; row < row0 + 128; ++row) {
+    const int tok = it.tok + (row >> a.log_pack), stop = min(min(it.c, it.c - it.n + tok + 1), to);
+    if (tok >= it.n) break;
+    if (stop <= from) continue;                          // it sees none of them
+    add_odd<D, kBf16>(a, it, at, stop, lane, sum);
+    at = max(at, stop);
+    if (ml[row].y == 0.f) continue;                      // it sees nothing
+    uint16_t* op = a.out + (a.qs.first ? 0 : it.s) * a.out_seq + (long long)(it.q0 + tok) * a.out_row +
+                   (it.q_head + (row & (a.pack - 1))) * a.out_head + 2 * lane;
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) {
+      const bool x = !(fabsf(sum[e].x) < INFINITY), y = !(fabsf(sum[e].y) < INFINITY);
+      if (!x && !y) continue;
+      uint32_t* at_e = reinterpret_cast<uint32_t*>(op + e * 64);
+      const uint32_t was = *at_e, w = pack16<kBf16>(half_lo<kBf16>(was) + sum[e].x, half_hi<kBf16>(was) + sum[e].y);
+      *at_e = ((x ? w : was) & 0xffffu) | ((y ? w : was) & 0xffff0000u);
+    }
+  }
 }
 
 // The item of a cluster.  First every block leaves its accumulators in its shared memory (a softmax warp its 16 rows) ..
@@ -229,13 +231,22 @@ __device__ __forceinline__ void leave_rows(float* acc, uint32_t o_tm, int row0) 
 }
 // .. then it joins its part of the 256 rows, a row a softmax warp.
 template <int D, bool kBf16>
-__device__ __noinline__ void join_rows(const PromptArgs& a, const PaItem& it, float* acc, float2* ml, int shares, int rank) {
+__device__ __noinline__ void join_rows(const PromptArgs& a, PaShared& sh, float* acc, int shares, int rank) {
+  const PaItem& it = sh.item[0];
+  float2* ml = sh.ml;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   cg::cluster_group cluster = cg::this_cluster();
   constexpr int E = D / 64;                            // pairs of channels a lane
   const int rows = 256 / shares;
+  int odd_from = 0x7fffffff, odd_to = 0;
+  for (int s = 0; s < shares; ++s)
+    for (int x = 0; x < kPaCleaners; ++x) {
+      const PaShared::Odd o = cluster.map_shared_rank(&sh, s)->odd[x];
+      odd_from = min(odd_from, o.from);
+      odd_to = max(odd_to, o.to);
+    }
   for (int i = warp; i < rows; i += kPaSoftWarps) {    // a row a warp
-    const int row = rank * rows + i, wg = row >> 7, tok = it.tok + (row >> a.log_pack), head = it.q_head + (row & (a.pack - 1));
+    const int row = rank * rows + i, tok = it.tok + (row >> a.log_pack), head = it.q_head + (row & (a.pack - 1));
     if (tok >= (a.qs.first ? it.n : a.qs.rows)) continue;
     float big = -INFINITY, sum = 0.f;
     for (int s = 0; s < shares; ++s) big = fmaxf(big, cluster.map_shared_rank(ml, s)[row].x);
@@ -255,21 +266,15 @@ __device__ __noinline__ void join_rows(const PromptArgs& a, const PaItem& it, fl
         o[e].y = fmaf(f, x.y, o[e].y);
       }
     }
+    add_odd<D, kBf16>(a, it, odd_from, min(odd_to, min(it.c, it.c - it.n + tok + 1)), lane, o);
     const float inv = sum == 0.f ? 0.f : __frcp_rn(sum);
     const long long seq = a.qs.first ? 0 : it.s, at = (long long)it.q0 + tok;
     uint16_t* op = a.out + seq * a.out_seq + at * a.out_row + head * a.out_head + 2 * lane;
-    bool odd = false;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float u0 = o[e].x * inv, u1 = o[e].y * inv;
-      odd |= !(fabsf(o[e].x) < INFINITY) || !(fabsf(o[e].y) < INFINITY);
-      *reinterpret_cast<uint32_t*>(op + 64 * e) = sum == 0.f ? 0u : pack_result<kBf16>(o[e].x, o[e].y, u0, u1);
-    }
+    for (int e = 0; e < E; ++e)
+      *reinterpret_cast<uint32_t*>(op + 64 * e) = sum == 0.f ? 0u : pack_result<kBf16>(o[e].x, o[e].y, o[e].x * inv, o[e].y * inv);
     if (lane == 0 && a.lse)
       a.lse[seq * a.lse_seq + at * a.lse_row + head * a.lse_head] = sum == 0.f ? -INFINITY : row_lse(big, sum, a.factor, it.room);
-    const int vis = min(it.c, it.c - it.n + tok + 1);
-    if (__any_sync(0xffffffffu, odd && sum != 0.f) && odd_values<D, kBf16>(a, it, vis, it.tiles[wg] * kPrTile, lane))
-      row_again<D, kBf16>(a, it, tok, head, vis, big, lane);
   }
 }
 
@@ -303,8 +308,14 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       for (int h = 0; h < 2; ++h) bar_init(&sh.pfull[i][h], kPaSoftWarps / 2);
       bar_init(&sh.ofull[i], 1);
       bar_init(&sh.item_full[i], 1);
-      bar_init(&sh.item_free[i], kPaSoftWarps + 1);
+      bar_init(&sh.item_free[i], kPaSoftWarps + 1 + kPaCleaners);
+      sh.again[i] = 0;
     }
+    bar_init(&sh.ask, 1);
+    bar_init(&sh.clean, kPaCleaners);
+    bar_init(&sh.found, kPaCleaners);
+    bar_init(&sh.written, kPaSoftWarps);
+    for (int x = 0; x < kPaCleaners; ++x) sh.odd[x] = {0x7fffffff, 0};
     sh.item[0].live = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -463,13 +474,13 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       // ---- out ----
       // (Once a tile of short prompts: every instruction counts.  A row's four lanes swap their words in two steps, so
       // that each has eight columns that lie together.)
-      const PaItem it = sh.item[iu & 1];
+      const PaItem& it = sh.item[iu & 1];
       const long long seq = a.qs.first ? 0 : it.s;
       const float zero = 0.f;
       float2 inv[2], odd2[2];
       uint16_t* op[2];
       int tok[2], head[2];
-      bool write[2], odd[2];
+      bool write[2];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const float i = l[r] == 0.f ? 0.f : __frcp_rn(l[r]);
@@ -516,25 +527,20 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
             if (write[r]) *reinterpret_cast<uint4*>(op[r] + k) = make_uint4(w[0], w[1], w[2], w[3]);
           }
         }
-        if (exact || !__any_sync(0xffffffffu, any && !(odd2[0].x + odd2[0].y + odd2[1].x + odd2[1].y == 0.f))) break;
-      }
-#pragma unroll
-      for (int r = 0; r < 2; ++r) odd[r] = !(odd2[r].x + odd2[r].y == 0.f);
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        unsigned rows = __ballot_sync(0xffffffffu, odd[r] && tok[r] < it.n && l[r] != 0.f && any);
-        rows |= rows >> 1;
-        rows = (rows | rows >> 2) & 0x11111111u;         // a row's first lane
-        if (rows) {
-          __syncwarp();                                  // (other lanes wrote what row_again writes once more)
-          const int least = __reduce_min_sync(0xffffffffu, vis[r]);
-          if (!odd_values<D, kBf16>(a, it, least, it.tiles[wg] * kPrTile, lane)) rows = 0;
-          for (; rows; rows &= rows - 1) {
-            const int at = __ffs(rows) - 1;
-            row_again<D, kBf16>(a, it, __shfl_sync(0xffffffffu, tok[r], at), __shfl_sync(0xffffffffu, head[r], at),
-                                __shfl_sync(0xffffffffu, vis[r], at), __shfl_sync(0xffffffffu, m[r], at), lane);
-          }
+        const bool odd = (l[0] != 0.f && !(odd2[0].x + odd2[0].y == 0.f)) || (l[1] != 0.f && !(odd2[1].x + odd2[1].y == 0.f));
+        if (exact || !__any_sync(0xffffffffu, any && odd)) break;
+        if (it.clean != it.part && it.part < max(it.tiles[0], it.tiles[1])) {
+          if (lane == 0) sh.again[iu & 1] = 1;
+          break;
         }
+      }
+      if (it.clean == it.part) {                         // (warps 18 and 19 add what they have taken out)
+        if (quad == 0) {
+          sh.ml[wg * 128 + row0] = make_float2(m[0], l[0]);
+          sh.ml[wg * 128 + row0 + 8] = make_float2(m[1], l[1]);
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(&sh.written);
       }
       fence_before();
       __syncwarp();
@@ -549,7 +555,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       if (warp_wait(&sh.meet, 0, waits, a.stats) && it.live && it.end[wg] > it.begin) leave_rows<D>(acc, o_tm, wg * 128 + row0);
       fence_before();
       meet_cluster();
-      if (it.live) join_rows<D, kBf16>(a, it, acc, sh.ml, shares, rank);
+      if (it.live) join_rows<D, kBf16>(a, sh, acc, shares, rank);
       meet_cluster();                                    // (nobody leaves while its shared memory is read)
     }
     fence_before();
@@ -563,44 +569,71 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       const int heads = a.n_kv * (a.group / a.pack);
       const bool leader = one_lane();
       const int crew = gridDim.x / shares, me = blockIdx.x / shares;
-      uint32_t u = 0, qu = 0;
-      bool ok = true;
+      uint32_t u = 0, qu = 0, no = 0;
+      int s = 0, t = 0, hd = 0;
+      bool ok = true, live = false, used = true;         // the item found last: there is one; it has been posted
       for (uint32_t iu = 0; ok; ++iu) {
-        const long long i = (long long)iu * crew + (iu & 1 ? crew - 1 - me : me);
-        const int hd = (int)(i % heads);
-        int s = 0, t = 0;
-        const bool live = (!kSplit || iu == 0) && prompt_find(order, a.n_seq, list, (int)(i / heads), lane, level, s, t);
-        PaItem it;
-        it.live = live;
-        it.s = s;
-        it.tok = t * 2 * span;
-        it.head = hd / (a.group / a.pack);
-        it.q_head = hd * a.pack;
-        it.n = list.n[s];
-        it.c = list.c[s];
-        it.q0 = prompt_begin(a.qs, s);
-        it.k0 = prompt_begin(a.ks, s);
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const int last = min(it.n, it.tok + (g + 1) * span) - 1;       // the group's last row that is there
-          const int vis = last >= it.tok + g * span ? min(it.c, it.c - it.n + last + 1) : 0;
-          it.tiles[g] = vis > 0 ? (vis + kPrTile - 1) / kPrTile : 0;
+        if (used) {
+          const long long i = (long long)no * crew + (no & 1 ? crew - 1 - me : me);
+          hd = (int)(i % heads);
+          live = (!kSplit || no == 0) && prompt_find(order, a.n_seq, list, (int)(i / heads), lane, level, s, t);
+          ++no;
         }
-        const int all = max(it.tiles[0], it.tiles[1]);
-        it.room = room_of<kBf16>(all);
-        it.begin = (int)((long long)all * rank / shares);
-        const int end = (int)((long long)all * (rank + 1) / shares);
+        // An item that has to be done again goes first: the one whose place this is, or with nothing left to do the last one.
+        int old = iu & 1;
+        if (iu >= 2 && !warp_wait(&sh.item_free[old], ((iu >> 1) - 1) & 1, waits, a.stats)) break;
+        used = kSplit || !*const_cast<volatile int*>(&sh.again[old]);
+        if (!kSplit && used && !live && iu >= 1) {
+          old ^= 1;
+          if (!warp_wait(&sh.item_free[old], ((iu - 1) >> 1) & 1, waits, a.stats)) break;
+          used = !*const_cast<volatile int*>(&sh.again[old]);
+        }
+        PaItem& it = sh.item[iu & 1];
+        if (used) {
+          const int head = hd / (a.group / a.pack), tok = t * 2 * span, n = list.n[s], c = list.c[s];
+          int tiles[2];
 #pragma unroll
-        for (int g = 0; g < 2; ++g) it.end[g] = max(min(end, it.tiles[g]), it.begin);
-        if (iu >= 2 && !warp_wait(&sh.item_free[iu & 1], ((iu >> 1) - 1) & 1, waits, a.stats)) break;
+          for (int g = 0; g < 2; ++g) {
+            const int last = min(n, tok + (g + 1) * span) - 1;           // the group's last row that is there
+            const int vis = last >= tok + g * span ? min(c, c - n + last + 1) : 0;
+            tiles[g] = vis > 0 ? (vis + kPrTile - 1) / kPrTile : 0;
+          }
+          const int all = max(tiles[0], tiles[1]), part = max(min(c, c - n + tok + 1), 0) / kPrTile;
+          const int begin = (int)((long long)all * rank / shares), end = (int)((long long)all * (rank + 1) / shares);
+          if (lane == 0) {
+            it.live = live;
+            it.s = s;
+            it.tok = tok;
+            it.head = head;
+            it.q_head = hd * a.pack;
+            it.n = n;
+            it.c = c;
+            it.q0 = prompt_begin(a.qs, s);
+            it.k0 = prompt_begin(a.ks, s);
+            it.room = room_of<kBf16>(all);
+            it.part = part;
+            it.clean = kSplit ? part : 0x7fffffff;
+            it.begin = begin;
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+              it.tiles[g] = tiles[g];
+              it.end[g] = max(min(end, tiles[g]), begin);
+            }
+          }
+        } else if (lane == 0) {
+          if (old != (iu & 1)) it = sh.item[old];
+          it.clean = it.part;
+        }
         if (lane == 0) {
-          sh.item[iu & 1] = it;
+          sh.again[old] = 0;
           bar_arrive(&sh.item_full[iu & 1]);
         }
-        if (!live) break;
+        __syncwarp();
+        if (!it.live) break;
+        const int end = max(it.end[0], it.end[1]);
         const int n_tiles = end - it.begin;
         if (n_tiles == 0) continue;
-        const int qs = a.qs.first ? 0 : s, ks = a.ks.first ? 0 : s;
+        const int qs = a.qs.first ? 0 : it.s, ks = a.ks.first ? 0 : it.s;
         for (int j = 0; j < 2 * n_tiles && ok; ++j, ++u) {               // K0 (then Q), V0, K1, V1, ..
           const uint32_t st = u % P::kStages, use = u / P::kStages;
           if (use > 0 && !warp_wait(&sh.free[st], (use - 1) & 1, waits, a.stats)) { ok = false; break; }
@@ -636,12 +669,12 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
                      v_desc = desc128(kv_smem(ring), kPrTile * 128);
       constexpr uint64_t kStage = P::kMat >> 4;
       const bool leader = one_lane();
-      uint32_t u = 0, qu = 0, pu[2] = {0, 0};
+      uint32_t u = 0, qu = 0, cu = 0, pu[2] = {0, 0};
       bool ok = true;
       for (uint32_t iu = 0; ok; ++iu) {
         if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, waits, a.stats)) break;
         const int live = sh.item[iu & 1].live, begin = sh.item[iu & 1].begin, tiles0 = sh.item[iu & 1].end[0] - begin,
-                  tiles1 = sh.item[iu & 1].end[1] - begin;
+                  tiles1 = sh.item[iu & 1].end[1] - begin, clean = sh.item[iu & 1].clean - begin;
         __syncwarp();
         if (lane == 0) bar_arrive(&sh.item_free[iu & 1]);
         if (!live) break;
@@ -674,7 +707,15 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         for (int j = 0; j < n_tiles && ok; ++j) {
           const uint32_t vu = u + 2 * j + 1, ku = vu + 1;
           landed(vu);
+          if (ok && j >= clean) {                        // (while the softmax warps are at work on the scores)
+            if (lane == 0) {
+              sh.asked = vu;
+              bar_arrive(&sh.ask);
+            }
+            __syncwarp();
+          }
           if (j + 1 < n_tiles) landed(ku);
+          if (ok && j >= clean) ok = warp_wait(&sh.clean, cu++ & 1, waits, a.stats);
           if (!ok) break;
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
@@ -707,6 +748,63 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
           __syncwarp();
         }
         u += 2 * n_tiles;
+      }
+    } else {
+      // ========================================================== values =========
+      const int who = warp - kPaCleaner;
+      uint32_t au = 0, cleaned = 0;
+      bool ok = true;
+      for (uint32_t iu = 0; ok; ++iu) {
+        if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, waits, a.stats)) break;
+        const PaItem& now = sh.item[iu & 1];
+        if (!now.live) break;
+        const int c = now.c, end = max(now.end[0], now.end[1]);
+        int from = 0x7fffffff, to = 0;
+        for (int j = max(now.begin, now.clean); j < end; ++j, ++au) {
+          if (!warp_wait(&sh.ask, au & 1, waits, a.stats)) { ok = false; break; }
+          const uint32_t vu = *const_cast<volatile uint32_t*>(&sh.asked);
+          // (it has landed, and stays until these warps are through with it)
+          if (!warp_wait(&sh.full[vu % P::kStages], (vu / P::kStages) & 1, waits, a.stats)) { ok = false; break; }
+          uint4* tile = reinterpret_cast<uint4*>(ring + vu % P::kStages * P::kMat);
+#pragma unroll 2
+          for (int i = who * 32 + lane; i < P::kMat / 16; i += 32 * kPaCleaners) {
+            uint4 w = tile[i];
+            const uint32_t x = odd_halves<kBf16>(w.x), y = odd_halves<kBf16>(w.y), z = odd_halves<kBf16>(w.z), q = odd_halves<kBf16>(w.w);
+            if (x | y | z | q) {
+              w.x &= ~((x >> 15) * 0xffffu);
+              w.y &= ~((y >> 15) * 0xffffu);
+              w.z &= ~((z >> 15) * 0xffffu);
+              w.w &= ~((q >> 15) * 0xffffu);
+              tile[i] = w;
+              const int key = j * kPrTile + (i >> 3 & 127);              // rows of 128 bytes, whatever their swizzle
+              if (key < c) {
+                from = min(from, key);
+                to = max(to, key + 1);
+              }
+            }
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) bar_arrive(&sh.clean);
+        }
+        if (!ok) break;
+        if (now.clean == now.part) {
+          from = __reduce_min_sync(0xffffffffu, from);
+          to = __reduce_max_sync(0xffffffffu, to);
+          if (lane == 0) {
+            sh.odd[who] = {from, to};
+            bar_arrive(&sh.found);
+          }
+          if (!kSplit) {                                 // (a cluster's rows are joined with them)
+            if (!warp_wait(&sh.found, cleaned & 1, waits, a.stats) || !warp_wait(&sh.written, cleaned & 1, waits, a.stats)) break;
+            ++cleaned;
+            from = min(sh.odd[0].from, sh.odd[1].from);
+            to = max(sh.odd[0].to, sh.odd[1].to);
+            if (from < to) odd_rows<D, kBf16>(a, now, sh.ml, who * 128, from, to, lane);
+          }
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(&sh.item_free[iu & 1]);
       }
     }
     // Nothing follows the roles: code that all warps share may use any register that the block was launched with, and

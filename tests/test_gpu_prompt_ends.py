@@ -148,3 +148,30 @@ def test_a_scale_of_zero_over_large_scores():
     k[..., 0] = torch.linspace(-1e19, 1e19, 300, device="cuda")[:, None]
     for scale in (0.0, 1e-40):
         check(q, k, v, s, how, BF16, scale)
+
+
+@pytest.mark.parametrize("where", ["padding", "inside", "everywhere"])
+def test_values_that_are_not_finite_take_no_time(where):
+    """8,192 keys with NaN behind a sequence's last row, at one key inside, at all of them: rows that do not see them are
+    right, and no wait of five milliseconds runs out (the whole call takes less than one)."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    new = lambda h: torch.randn(2, 8256, h, 64, generator=g, device="cuda").bfloat16()
+    q, k, v = new(8), new(2), new(2)
+    n = torch.tensor([8191, 8000], dtype=torch.int32, device="cuda")
+    bad = {"padding": slice(8256, None), "inside": slice(8100, 8101), "everywhere": slice(0, None)}[where]
+    want, wl = B.prompt_attend(q, k, v, n_new=n)
+    dirty = v.clone()
+    for i in range(2):
+        dirty[i, int(n[i]):] = math.nan
+        dirty[i, bad] = math.nan
+    try:
+        B.prompt_set_wait_limit(5_000_000)
+        out, lse = B.prompt_attend(q, k, dirty, n_new=n)
+        assert B.prompt_status() == B.OK
+    finally:
+        B.prompt_set_wait_limit(0)
+    assert torch.equal(lse, wl)
+    for i in range(2):
+        clean = min(int(n[i]), bad.start)
+        assert torch.equal(out[i, :clean], want[i, :clean]) and bool(torch.isnan(out[i, clean:int(n[i])]).all())
+        assert bool((out[i, int(n[i]):] == 0).all())

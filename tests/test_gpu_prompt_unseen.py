@@ -44,3 +44,21 @@ def test_values_that_are_not_finite_in_whole_items(bad, packed, hq, hkv, d, dtyp
             check_attend(out[a][clean], lse[a][clean], [x[clean] for x in ref], dtype, d)
             if n == i:
                 assert not torch.isfinite(out[a][j:]).all(-1).any(), "what a row sees is not hidden"
+
+
+@pytest.mark.parametrize("packed", [True, False])
+def test_infinite_values_reach_the_rows_that_see_them(packed):
+    """A channel with an infinity is infinite from that key on, one with both signs NaN; the others stay."""
+    s = Side([600, 300, 500] * 4, packed)
+    q, k, v = make(s, 16, 16, 64, BF16)
+    how = s.arguments(("first", "n_new"))
+    want, wl = B.prompt_attend(q, k, v, **how)
+    v2 = v.clone()
+    x = v2[s.at(4)]
+    x[50, 3, 7], x[60, 3, 7], x[70, 3, 9], x[70, 4, 9] = math.inf, math.inf, -math.inf, math.nan
+    x[75, 3, 9], x[299, 5, 63] = math.inf, -math.inf
+    out, lse = B.prompt_attend(q, k, v2, **how)
+    expect = want.clone()
+    y = expect[s.at(4)]
+    y[50:, 3, 7], y[70:75, 3, 9], y[75:, 3, 9], y[70:, 4, 9], y[299, 5, 63] = math.inf, -math.inf, math.nan, math.nan, -math.inf
+    assert torch.equal(out.nan_to_num(2.0 ** 100), expect.nan_to_num(2.0 ** 100)) and torch.equal(lse, wl)
