@@ -11,7 +11,7 @@
 //              exponentials, and the probabilities in 16 bits back over the scores
 //   16         loads: queries, then keys and values in turn into a ring, by tensor maps
 //   17         issues the products S = Q K^T and O += P V (P from TMEM)
-//   18, 19     take what is not finite out of values that not every row sees
+//   18, 19     put zeros over values behind a sequence's last and, where they matter, over those that are not finite
 // While A's scores go through the exponentials the tensor core works for B, and the other way round.
 //
 // Numbers.  Scores, maxima, sums and accumulators are fp32.  Probabilities are rounded to the inputs'
@@ -22,11 +22,11 @@
 // keys' large values would otherwise add up to more than fp32 holds (see room_of).
 //
 // Values that are not finite.  A masked key's probability is 0, and 0 times an infinity would reach every row of the
-// tile.  An item with a row whose accumulators are not finite is done once more: of its tiles the last ones, up to
-// three, hold keys that one of its rows does not see (of later tokens, or behind the sequence's last), and there two warps
-// put zeros in place of infinities and NaN before the tile's product.  The rows that do see such a key have its value
-// added when they are written.  (In clusters, which have one item, the tiles are cleaned at once.  Done for every item
-// that took 16 prompts from 225 to 243 us.)
+// tile.  Before the product of a tile that passes the sequence's last key two warps put zeros there (padding may hold
+// anything).  And an item with a row whose accumulators are not finite is done once more: of its tiles the last ones, up
+// to three, hold keys of tokens behind one of its rows, and for those keys the two warps now put zeros in place of
+// infinities and NaN.  The rows that do see such a key have its value added when they are written.  (In clusters, which have one
+// item, that is done at once.  For every item it took 16 prompts from 225 to 243 us.)
 //
 // Work.  Items by falling number of key tiles, so that the last ones are the short ones; block b takes
 // b, 2G-1-b, 2G+b, ... of G blocks (see prompt_find).
@@ -69,7 +69,7 @@ struct PaItem {
   int s, tok, head, q_head;          // sequence, first token, key head, first query head
   int n, c, q0, k0;
   int tiles[2];                      // of A and of B: all that their rows see
-  int part;                          // from this tile on there are keys that not every row sees
+  int seen, part;                    // keys that every row sees; the tile in which they end
   int clean;                         // from this tile on values are cleaned: part, or none
   int begin;                         // this block's: from here on,
   int end[2];                        // up to here
@@ -238,13 +238,11 @@ __device__ __noinline__ void join_rows(const PromptArgs& a, PaShared& sh, float*
   cg::cluster_group cluster = cg::this_cluster();
   constexpr int E = D / 64;                            // pairs of channels a lane
   const int rows = 256 / shares;
-  int odd_from = 0x7fffffff, odd_to = 0;
-  for (int s = 0; s < shares; ++s)
-    for (int x = 0; x < kPaCleaners; ++x) {
-      const PaShared::Odd o = cluster.map_shared_rank(&sh, s)->odd[x];
-      odd_from = min(odd_from, o.from);
-      odd_to = max(odd_to, o.to);
-    }
+  PaShared::Odd odd = {0x7fffffff, 0};
+  static_assert(16 * kPaCleaners <= 32, "a lane for each of a cluster's");
+  if (lane < shares * kPaCleaners) odd = cluster.map_shared_rank(&sh, lane / kPaCleaners)->odd[lane % kPaCleaners];
+  odd.from = __reduce_min_sync(0xffffffffu, odd.from);
+  odd.to = __reduce_max_sync(0xffffffffu, odd.to);
   for (int i = warp; i < rows; i += kPaSoftWarps) {    // a row a warp
     const int row = rank * rows + i, tok = it.tok + (row >> a.log_pack), head = it.q_head + (row & (a.pack - 1));
     if (tok >= (a.qs.first ? it.n : a.qs.rows)) continue;
@@ -266,7 +264,7 @@ __device__ __noinline__ void join_rows(const PromptArgs& a, PaShared& sh, float*
         o[e].y = fmaf(f, x.y, o[e].y);
       }
     }
-    add_odd<D, kBf16>(a, it, odd_from, min(odd_to, min(it.c, it.c - it.n + tok + 1)), lane, o);
+    if (odd.from < odd.to) add_odd<D, kBf16>(a, it, odd.from, min(odd.to, min(it.c, it.c - it.n + tok + 1)), lane, o);
     const float inv = sum == 0.f ? 0.f : __frcp_rn(sum);
     const long long seq = a.qs.first ? 0 : it.s, at = (long long)it.q0 + tok;
     uint16_t* op = a.out + seq * a.out_seq + at * a.out_row + head * a.out_head + 2 * lane;
@@ -598,7 +596,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
             const int vis = last >= tok + g * span ? min(c, c - n + last + 1) : 0;
             tiles[g] = vis > 0 ? (vis + kPrTile - 1) / kPrTile : 0;
           }
-          const int all = max(tiles[0], tiles[1]), part = max(min(c, c - n + tok + 1), 0) / kPrTile;
+          const int all = max(tiles[0], tiles[1]), seen = max(min(c, c - n + tok + 1), 0), part = seen / kPrTile;
           const int begin = (int)((long long)all * rank / shares), end = (int)((long long)all * (rank + 1) / shares);
           if (lane == 0) {
             it.live = live;
@@ -611,6 +609,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
             it.q0 = prompt_begin(a.qs, s);
             it.k0 = prompt_begin(a.ks, s);
             it.room = room_of<kBf16>(all);
+            it.seen = seen;
             it.part = part;
             it.clean = kSplit ? part : 0x7fffffff;
             it.begin = begin;
@@ -674,7 +673,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       for (uint32_t iu = 0; ok; ++iu) {
         if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, waits, a.stats)) break;
         const int live = sh.item[iu & 1].live, begin = sh.item[iu & 1].begin, tiles0 = sh.item[iu & 1].end[0] - begin,
-                  tiles1 = sh.item[iu & 1].end[1] - begin, clean = sh.item[iu & 1].clean - begin;
+                  tiles1 = sh.item[iu & 1].end[1] - begin, clean = min(sh.item[iu & 1].clean, sh.item[iu & 1].c / kPrTile) - begin;
         __syncwarp();
         if (lane == 0) bar_arrive(&sh.item_free[iu & 1]);
         if (!live) break;
@@ -760,26 +759,35 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         if (!now.live) break;
         const int c = now.c, end = max(now.end[0], now.end[1]);
         int from = 0x7fffffff, to = 0;
-        for (int j = max(now.begin, now.clean); j < end; ++j, ++au) {
+        for (int j = max(now.begin, min(now.clean, c / kPrTile)); j < end; ++j, ++au) {
           if (!warp_wait(&sh.ask, au & 1, waits, a.stats)) { ok = false; break; }
           const uint32_t vu = *const_cast<volatile uint32_t*>(&sh.asked);
           // (it has landed, and stays until these warps are through with it)
           if (!warp_wait(&sh.full[vu % P::kStages], (vu / P::kStages) & 1, waits, a.stats)) { ok = false; break; }
           uint4* tile = reinterpret_cast<uint4*>(ring + vu % P::kStages * P::kMat);
+          // (a block of 64 channels: rows of 128 bytes, whatever their swizzle)
+          const bool zero = j < now.clean;               // behind the last key; the other values as they are
+          const int first = max((zero ? c : now.seen) - j * kPrTile, 0) * 8 + who * 32 + lane;
+          for (int b = 0; b < P::kBlocks; ++b, tile += kPrTile * 8) {
+            if (zero) {
+              for (int i = first; i < kPrTile * 8; i += 32 * kPaCleaners) tile[i] = make_uint4(0u, 0u, 0u, 0u);
+              continue;
+            }
 #pragma unroll 2
-          for (int i = who * 32 + lane; i < P::kMat / 16; i += 32 * kPaCleaners) {
-            uint4 w = tile[i];
-            const uint32_t x = odd_halves<kBf16>(w.x), y = odd_halves<kBf16>(w.y), z = odd_halves<kBf16>(w.z), q = odd_halves<kBf16>(w.w);
-            if (x | y | z | q) {
-              w.x &= ~((x >> 15) * 0xffffu);
-              w.y &= ~((y >> 15) * 0xffffu);
-              w.z &= ~((z >> 15) * 0xffffu);
-              w.w &= ~((q >> 15) * 0xffffu);
-              tile[i] = w;
-              const int key = j * kPrTile + (i >> 3 & 127);              // rows of 128 bytes, whatever their swizzle
-              if (key < c) {
-                from = min(from, key);
-                to = max(to, key + 1);
+            for (int i = first; i < kPrTile * 8; i += 32 * kPaCleaners) {
+              uint4 w = tile[i];
+              const uint32_t x = odd_halves<kBf16>(w.x), y = odd_halves<kBf16>(w.y), z = odd_halves<kBf16>(w.z), q = odd_halves<kBf16>(w.w);
+              if (x | y | z | q) {
+                w.x &= ~((x >> 15) * 0xffffu);
+                w.y &= ~((y >> 15) * 0xffffu);
+                w.z &= ~((z >> 15) * 0xffffu);
+                w.w &= ~((q >> 15) * 0xffffu);
+                tile[i] = w;
+                const int key = j * kPrTile + (i >> 3);
+                if (key < c) {
+                  from = min(from, key);
+                  to = max(to, key + 1);
+                }
               }
             }
           }
