@@ -226,7 +226,7 @@ kv_tree_kernel(const KvView c, const KvAttendArgs a) {
   fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
   pdl_enter();
-  if (tid == 0) waits_begin(sh.waits, stats);
+  if (tid == 0) waits_begin(sh.waits, &stats->wait_limit_ns);
 
   TreeList list;
   list.cum = cum;

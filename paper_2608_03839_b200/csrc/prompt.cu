@@ -150,6 +150,7 @@ int oilbird_prompt_attend(const oilbird_prompt* prompt, const oilbird_kv_rows* q
   OnDevice dev(prompt->device);
   int sms;
   PTRY(dev.enter(&sms, &a.stats));
+  a.wait_limit = &a.stats->wait_limit_ns;
   const cudaError_t e = launch_prompt_attend(a, prompt->head_dim, prompt->dtype == OILBIRD_KV_BF16, sms, (cudaStream_t)cuda_stream);
   if (e == cudaErrorInvalidValue) return refuse("q, k, v: strides that no tensor map takes");
   PCU(e);
@@ -174,6 +175,7 @@ int oilbird_prompt_weigh(const oilbird_prompt* prompt, const oilbird_kv_rows* q,
   OnDevice dev(prompt->device);
   int sms;
   PTRY(dev.enter(&sms, &a.stats));
+  a.wait_limit = &a.stats->wait_limit_ns;
   const cudaError_t e = launch_prompt_weigh(a, prompt->head_dim, prompt->dtype == OILBIRD_KV_BF16, sms, (cudaStream_t)cuda_stream);
   if (e == cudaErrorInvalidValue) return refuse("q, k: strides that no tensor map takes");
   PCU(e);

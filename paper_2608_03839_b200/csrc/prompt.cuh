@@ -30,6 +30,7 @@ struct PromptArgs {
   const float* row_weight;   // weigh: [n_seq, rows] or [rows]; null: 1
   float* weight;             // weigh: [n_seq, n_kv, key rows] or [n_kv, key rows]
   DeviceStats* stats;
+  const unsigned long long* wait_limit;      // in stats
   int n_seq, n_kv, group;
   int pack, log_pack;        // query heads that lie side by side in a tile: a power of two that divides group
   float factor;              // |scale| log2 e

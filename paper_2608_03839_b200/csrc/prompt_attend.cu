@@ -322,7 +322,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   pdl_enter();
-  if (tid == 0) waits_begin(sh.waits, a.stats);
+  if (tid == 0) waits_begin(sh.waits, &a.stats->wait_limit_ns);
   prompt_extents(a, list);
   const PaOrder order = {&list, 8 - a.log_pack, a.qs.first ? 0 : a.qs.rows};
   __syncthreads();

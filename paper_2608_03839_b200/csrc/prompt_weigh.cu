@@ -183,7 +183,7 @@ prompt_weigh_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   pdl_enter();
-  if (tid == 0) waits_begin(sh.waits, a.stats);
+  if (tid == 0) waits_begin(sh.waits, a.wait_limit);
   prompt_extents(a, list);
   __syncthreads();
   const PwOrder order = {&list, 7 - a.log_pack, a.ks.first ? 0 : a.ks.rows};

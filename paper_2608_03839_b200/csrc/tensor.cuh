@@ -16,9 +16,11 @@ struct Waits {
   uint32_t limit;                        // steps of 64 ns (up to 274 s)
   int gave_up;                           // a wait ran out: all roles leave
 };
-// one thread, in front of a barrier of the block
-__device__ __forceinline__ void waits_begin(Waits& w, const DeviceStats* stats) {
-  w.limit = (uint32_t)min(wait_limit_ns(stats) >> 6, 0xfffffffeull);
+// one thread, in front of a barrier of the block; ns: DeviceStats::wait_limit_ns.  (A pointer of its own: read through the
+// statistics' it took registers from the loops of the weights' kernel, 53 us for 51.)
+__device__ __forceinline__ void waits_begin(Waits& w, const volatile unsigned long long* ns) {
+  const unsigned long long limit = *ns;
+  w.limit = (uint32_t)min((limit ? limit : kDefaultWaitNs) >> 6, 0xfffffffeull);
   w.gave_up = 0;
 }
 __device__ __forceinline__ bool bar_test(uint64_t* b, uint32_t parity) {
