@@ -334,6 +334,15 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
   const int span = kPrTile >> a.log_pack;                // tokens of a group
   const int rank = kSplit ? blockIdx.x % shares : 0;     // in the cluster
 
+  // The roles leave when no item is left.  They meet then, and go on if the last one has to be done again, with the number
+  // behind that of the item that was none.  (Only behind the barrier is it known for good whether somebody gave up.)
+  auto over = [&](uint32_t iu) {
+    if (kSplit) return true;
+    fence_before();
+    __syncthreads();
+    return waits->gave_up || !*const_cast<volatile int*>(&sh.again[(iu + 1) & 1]);
+  };
+
   if (warp < kPaSoftWarps) {
     // ============================================================ softmax ========
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPaSoftRegs));
@@ -343,207 +352,210 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
     const float2 g2 = make_float2(a.factor, a.factor);
     uint32_t su = 0, ou = 0;
     bool ok = true;
-    for (uint32_t iu = 0; ok; ++iu) {
-      if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, waits, a.stats)) break;
-      // (read again where the rows are written: there are no registers to keep it in)
-      volatile const PaItem& now = sh.item[iu & 1];
-      if (!now.live) break;
-      int vis[2];                                        // keys the row sees (0 or less: none)
-      float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int tok = now.tok + wg * span + ((row0 + 8 * r) >> a.log_pack), n = now.n, c = now.c;
-        vis[r] = tok < n ? min(c, c - n + tok + 1) : 0;
-      }
-      for (int j = now.begin; j < now.end[wg]; ++j, ++su) {
-        if (!warp_wait(&sh.sfull[wg], su & 1, waits, a.stats)) { ok = false; break; }
-        fence_after();
-        uint32_t x[64];
-        tmem_ask_rows(s_tm, x);
-        tmem_wait_rows(x);
-        if (__any_sync(0xffffffffu, min(vis[0], vis[1]) < (j + 1) * kPrTile)) {
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const int see = vis[r] - j * kPrTile - 2 * quad;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              if (8 * i >= see) x[4 * i + 2 * r] = 0xff800000u;
-              if (8 * i + 1 >= see) x[4 * i + 2 * r + 1] = 0xff800000u;
-            }
-          }
-        }
-        float mx[2];
+    uint32_t iu = 0;
+    do {
+      for (; ok; ++iu) {
+        if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, waits, a.stats)) break;
+        // (read again where the rows are written: there are no registers to keep it in)
+        volatile const PaItem& now = sh.item[iu & 1];
+        if (!now.live) break;
+        int vis[2];                                        // keys the row sees (0 or less: none)
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          float y[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-          for (int i = 0; i < 16; ++i) y[i & 1] = max3(y[i & 1], __uint_as_float(x[4 * i + 2 * r]), __uint_as_float(x[4 * i + 2 * r + 1]));
-          mx[r] = fmaxf(y[0], y[1]);
+          const int tok = now.tok + wg * span + ((row0 + 8 * r) >> a.log_pack), n = now.n, c = now.c;
+          vis[r] = tok < n ? min(c, c - n + tok + 1) : 0;
         }
-#pragma unroll
-        for (int o = 1; o < 4; o <<= 1) {
-          mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], o));
-          mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], o));
-        }
-        const float room = kBf16 ? now.room : 7.f;
-        // (differences of scores: as products with the factor both may be infinite)
-        if (__any_sync(0xffffffffu, (mx[0] - m[0]) * a.factor > kPaSlack || (mx[1] - m[1]) * a.factor > kPaSlack)) {
-          // (each row for itself; the products so far are done, or there were no scores)
-          float down[2];
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const float mn = (mx[r] - m[r]) * a.factor > kPaSlack ? mx[r] : m[r];
-            down[r] = mn == m[r] ? 1.f : exp2_approx(row_fall(m[r], mn, a.factor, room));
-            m[r] = mn;
-            l[r] *= down[r];
-          }
-          if (j > now.begin) {
-#pragma unroll 1
-            for (int k = 0; k < D; k += 32) {
-              uint32_t r[16];
-              tmem_ask_rows(o_tm + k, r);
-              tmem_wait_rows(r);
-#pragma unroll
-              for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * down[e >> 1 & 1]);
-              tmem_st_rows(o_tm + k, r);
-            }
-          }
-        }
-        if (__any_sync(0xffffffffu, row_far(m[0], a.factor) || row_far(m[1], a.factor))) {
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const float less = row_far(m[r], a.factor) ? m[r] : 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              x[4 * i + 2 * r] = __float_as_uint(__uint_as_float(x[4 * i + 2 * r]) - less);
-              x[4 * i + 2 * r + 1] = __float_as_uint(__uint_as_float(x[4 * i + 2 * r + 1]) - less);
-            }
-          }
-        }
-        float2 shift2[2], sum[2];
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const float shift = row_shift(m[r], a.factor, room);
-          shift2[r] = make_float2(shift, shift);
-          sum[r] = make_float2(0.f, 0.f);
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          uint32_t w[8];
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
+        for (int j = now.begin; j < now.end[wg]; ++j, ++su) {
+          if (!warp_wait(&sh.sfull[wg], su & 1, waits, a.stats)) { ok = false; break; }
+          fence_after();
+          uint32_t x[64];
+          tmem_ask_rows(s_tm, x);
+          tmem_wait_rows(x);
+          if (__any_sync(0xffffffffu, min(vis[0], vis[1]) < (j + 1) * kPrTile)) {
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-              const int e = 16 * k + 4 * i + 2 * r;
-              const float2 z = fma2(make_float2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), g2, shift2[r]);
-              const float2 pr = make_float2(exp2_approx(z.x), exp2_approx(z.y));
-              sum[r] = add2(sum[r], pr);
-              w[2 * i + r] = pack16<kBf16>(pr.x, pr.y);
+              const int see = vis[r] - j * kPrTile - 2 * quad;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                if (8 * i >= see) x[4 * i + 2 * r] = 0xff800000u;
+                if (8 * i + 1 >= see) x[4 * i + 2 * r + 1] = 0xff800000u;
+              }
             }
-          tmem_st_pairs(s_tm + k * 16, w);               // over the scores
-          if (k & 1) {                                   // a half of the keys: their product can begin
-            tmem_wait_st();
-            fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(&sh.pfull[wg][k >> 1]);
           }
-        }
-        l[0] += sum[0].x + sum[0].y;
-        l[1] += sum[1].x + sum[1].y;
-      }
-      if (!ok) break;
-      const bool any = now.end[wg] > now.begin;
-      if (any) {
-        if (!warp_wait(&sh.ofull[wg], ou++ & 1, waits, a.stats)) break;
-        fence_after();
-      }
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-      }
-      if (kSplit) {                                      // (a cluster has one item, joined below)
-        if (quad == 0) {
-          sh.ml[wg * 128 + row0] = make_float2(m[0], l[0]);
-          sh.ml[wg * 128 + row0 + 8] = make_float2(m[1], l[1]);
-        }
-        break;
-      }
-      // ---- out ----
-      // (Once a tile of short prompts: every instruction counts.  A row's four lanes swap their words in two steps, so
-      // that each has eight columns that lie together.)
-      const PaItem& it = sh.item[iu & 1];
-      const long long seq = a.qs.first ? 0 : it.s;
-      const float zero = 0.f;
-      float2 inv[2], odd2[2];
-      uint16_t* op[2];
-      int tok[2], head[2];
-      bool write[2];
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const float i = l[r] == 0.f ? 0.f : __frcp_rn(l[r]);
-        inv[r] = make_float2(i, i);
-        odd2[r] = make_float2(0.f, 0.f);
-        tok[r] = it.tok + wg * span + ((row0 + 8 * r) >> a.log_pack);
-        head[r] = it.q_head + ((row0 + 8 * r) & (a.pack - 1));
-        write[r] = tok[r] < (a.qs.first ? it.n : a.qs.rows);
-        const long long row = (long long)it.q0 + tok[r];
-        op[r] = a.out + seq * a.out_seq + row * a.out_row + head[r] * a.out_head + 8 * quad;
-        if (write[r] && a.lse && quad == 0)
-          a.lse[seq * a.lse_seq + row * a.lse_row + head[r] * a.lse_head] =
-              l[r] == 0.f ? -INFINITY : row_lse(m[r], l[r], a.factor, it.room);
-      }
-      // (a second time where a row has accumulators that are not finite: those results are infinite or NaN too)
-      for (bool exact = false;; exact = true) {
-#pragma unroll 1
-        for (int k = 0; k < D; k += 32) {
-          uint32_t o[16];
-          if (any) {
-            tmem_ask_rows(o_tm + k, o);
-            tmem_wait_rows(o);
-          }
+          float mx[2];
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            uint32_t w[4];                               // columns 8i + 2 quad, .. of the 32
+            float y[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float2 x = make_float2(__uint_as_float(o[4 * i + 2 * r]), __uint_as_float(o[4 * i + 2 * r + 1])), u = mul2(x, inv[r]);
-              odd2[r] = fma2(x, make_float2(zero, zero), odd2[r]);           // (NaN once one is not finite)
-              w[i] = l[r] == 0.f ? 0u : exact ? pack_result<kBf16>(x.x, x.y, u.x, u.y) : pack_finite<kBf16>(u.x, u.y);
-            }
-#pragma unroll
-            for (int x = 2; x; x >>= 1) {
-              const bool up = quad & x;
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (!(i & x)) {
-                  const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[i] : w[i + x], x);
-                  w[i] = up ? got : w[i];
-                  w[i + x] = up ? w[i + x] : got;
-                }
-            }
-            if (write[r]) *reinterpret_cast<uint4*>(op[r] + k) = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int i = 0; i < 16; ++i) y[i & 1] = max3(y[i & 1], __uint_as_float(x[4 * i + 2 * r]), __uint_as_float(x[4 * i + 2 * r + 1]));
+            mx[r] = fmaxf(y[0], y[1]);
           }
+#pragma unroll
+          for (int o = 1; o < 4; o <<= 1) {
+            mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], o));
+            mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], o));
+          }
+          const float room = kBf16 ? now.room : 7.f;
+          // (differences of scores: as products with the factor both may be infinite)
+          if (__any_sync(0xffffffffu, (mx[0] - m[0]) * a.factor > kPaSlack || (mx[1] - m[1]) * a.factor > kPaSlack)) {
+            // (each row for itself; the products so far are done, or there were no scores)
+            float down[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const float mn = (mx[r] - m[r]) * a.factor > kPaSlack ? mx[r] : m[r];
+              down[r] = mn == m[r] ? 1.f : exp2_approx(row_fall(m[r], mn, a.factor, room));
+              m[r] = mn;
+              l[r] *= down[r];
+            }
+            if (j > now.begin) {
+#pragma unroll 1
+              for (int k = 0; k < D; k += 32) {
+                uint32_t r[16];
+                tmem_ask_rows(o_tm + k, r);
+                tmem_wait_rows(r);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * down[e >> 1 & 1]);
+                tmem_st_rows(o_tm + k, r);
+              }
+            }
+          }
+          if (__any_sync(0xffffffffu, row_far(m[0], a.factor) || row_far(m[1], a.factor))) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const float less = row_far(m[r], a.factor) ? m[r] : 0.f;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                x[4 * i + 2 * r] = __float_as_uint(__uint_as_float(x[4 * i + 2 * r]) - less);
+                x[4 * i + 2 * r + 1] = __float_as_uint(__uint_as_float(x[4 * i + 2 * r + 1]) - less);
+              }
+            }
+          }
+          float2 shift2[2], sum[2];
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const float shift = row_shift(m[r], a.factor, room);
+            shift2[r] = make_float2(shift, shift);
+            sum[r] = make_float2(0.f, 0.f);
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int r = 0; r < 2; ++r) {
+                const int e = 16 * k + 4 * i + 2 * r;
+                const float2 z = fma2(make_float2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), g2, shift2[r]);
+                const float2 pr = make_float2(exp2_approx(z.x), exp2_approx(z.y));
+                sum[r] = add2(sum[r], pr);
+                w[2 * i + r] = pack16<kBf16>(pr.x, pr.y);
+              }
+            tmem_st_pairs(s_tm + k * 16, w);               // over the scores
+            if (k & 1) {                                   // a half of the keys: their product can begin
+              tmem_wait_st();
+              fence_before();
+              __syncwarp();
+              if (lane == 0) bar_arrive(&sh.pfull[wg][k >> 1]);
+            }
+          }
+          l[0] += sum[0].x + sum[0].y;
+          l[1] += sum[1].x + sum[1].y;
         }
-        const bool odd = (l[0] != 0.f && !(odd2[0].x + odd2[0].y == 0.f)) || (l[1] != 0.f && !(odd2[1].x + odd2[1].y == 0.f));
-        if (exact || !__any_sync(0xffffffffu, any && odd)) break;
-        if (it.clean != it.part && it.part < max(it.tiles[0], it.tiles[1])) {
-          if (lane == 0) sh.again[iu & 1] = 1;
+        if (!ok) break;
+        const bool any = now.end[wg] > now.begin;
+        if (any) {
+          if (!warp_wait(&sh.ofull[wg], ou++ & 1, waits, a.stats)) break;
+          fence_after();
+        }
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+          l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+        }
+        if (kSplit) {                                      // (a cluster has one item, joined below)
+          if (quad == 0) {
+            sh.ml[wg * 128 + row0] = make_float2(m[0], l[0]);
+            sh.ml[wg * 128 + row0 + 8] = make_float2(m[1], l[1]);
+          }
           break;
         }
-      }
-      if (it.clean == it.part) {                         // (warps 18 and 19 add what they have taken out)
-        if (quad == 0) {
-          sh.ml[wg * 128 + row0] = make_float2(m[0], l[0]);
-          sh.ml[wg * 128 + row0 + 8] = make_float2(m[1], l[1]);
+        // ---- out ----
+        // (Once a tile of short prompts: every instruction counts.  A row's four lanes swap their words in two steps, so
+        // that each has eight columns that lie together.)
+        const PaItem& it = sh.item[iu & 1];
+        const long long seq = a.qs.first ? 0 : it.s;
+        const float zero = 0.f;
+        float2 inv[2], odd2[2];
+        uint16_t* op[2];
+        int tok[2], head[2];
+        bool write[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float i = l[r] == 0.f ? 0.f : __frcp_rn(l[r]);
+          inv[r] = make_float2(i, i);
+          odd2[r] = make_float2(0.f, 0.f);
+          tok[r] = it.tok + wg * span + ((row0 + 8 * r) >> a.log_pack);
+          head[r] = it.q_head + ((row0 + 8 * r) & (a.pack - 1));
+          write[r] = tok[r] < (a.qs.first ? it.n : a.qs.rows);
+          const long long row = (long long)it.q0 + tok[r];
+          op[r] = a.out + seq * a.out_seq + row * a.out_row + head[r] * a.out_head + 8 * quad;
+          if (write[r] && a.lse && quad == 0)
+            a.lse[seq * a.lse_seq + row * a.lse_row + head[r] * a.lse_head] =
+                l[r] == 0.f ? -INFINITY : row_lse(m[r], l[r], a.factor, it.room);
         }
+        // (a second time where a row has accumulators that are not finite: those results are infinite or NaN too)
+        for (bool exact = false;; exact = true) {
+#pragma unroll 1
+          for (int k = 0; k < D; k += 32) {
+            uint32_t o[16];
+            if (any) {
+              tmem_ask_rows(o_tm + k, o);
+              tmem_wait_rows(o);
+            }
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              uint32_t w[4];                               // columns 8i + 2 quad, .. of the 32
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float2 x = make_float2(__uint_as_float(o[4 * i + 2 * r]), __uint_as_float(o[4 * i + 2 * r + 1])), u = mul2(x, inv[r]);
+                odd2[r] = fma2(x, make_float2(zero, zero), odd2[r]);           // (NaN once one is not finite)
+                w[i] = l[r] == 0.f ? 0u : exact ? pack_result<kBf16>(x.x, x.y, u.x, u.y) : pack_finite<kBf16>(u.x, u.y);
+              }
+#pragma unroll
+              for (int x = 2; x; x >>= 1) {
+                const bool up = quad & x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  if (!(i & x)) {
+                    const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[i] : w[i + x], x);
+                    w[i] = up ? got : w[i];
+                    w[i + x] = up ? w[i + x] : got;
+                  }
+              }
+              if (write[r]) *reinterpret_cast<uint4*>(op[r] + k) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          }
+          const bool odd = (l[0] != 0.f && !(odd2[0].x + odd2[0].y == 0.f)) || (l[1] != 0.f && !(odd2[1].x + odd2[1].y == 0.f));
+          if (exact || !__any_sync(0xffffffffu, any && odd)) break;
+          if (it.clean != it.part && it.part < max(it.tiles[0], it.tiles[1])) {
+            if (lane == 0) sh.again[iu & 1] = 1;
+            break;
+          }
+        }
+        if (it.clean == it.part) {                         // (warps 18 and 19 add what they have taken out)
+          if (quad == 0) {
+            sh.ml[wg * 128 + row0] = make_float2(m[0], l[0]);
+            sh.ml[wg * 128 + row0 + 8] = make_float2(m[1], l[1]);
+          }
+          __syncwarp();
+          if (lane == 0) bar_arrive(&sh.written);
+        }
+        fence_before();
         __syncwarp();
-        if (lane == 0) bar_arrive(&sh.written);
+        if (lane == 0) bar_arrive(&sh.item_free[iu & 1]);
       }
-      fence_before();
-      __syncwarp();
-      if (lane == 0) bar_arrive(&sh.item_free[iu & 1]);
-    }
+    } while (!over(iu++));
     if (kSplit) {
       // (the tiles' place is free when both groups have their last products)
       float* acc = reinterpret_cast<float*>(smem);
@@ -555,9 +567,9 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       meet_cluster();
       if (it.live) join_rows<D, kBf16>(a, sh, acc, shares, rank);
       meet_cluster();                                    // (nobody leaves while its shared memory is read)
+      fence_before();
+      __syncthreads();
     }
-    fence_before();
-    __syncthreads();
     return;                                              // (see below)
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPaRestRegs));
@@ -570,96 +582,93 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       uint32_t u = 0, qu = 0, no = 0;
       int s = 0, t = 0, hd = 0;
       bool ok = true, live = false, used = true;         // the item found last: there is one; it has been posted
-      for (uint32_t iu = 0; ok; ++iu) {
-        if (used) {
-          const long long i = (long long)no * crew + (no & 1 ? crew - 1 - me : me);
-          hd = (int)(i % heads);
-          live = (!kSplit || no == 0) && prompt_find(order, a.n_seq, list, (int)(i / heads), lane, level, s, t);
-          ++no;
-        }
-        // An item that has to be done again goes first: the one whose place this is, or with nothing left to do the last one.
-        int old = iu & 1;
-        if (iu >= 2 && !warp_wait(&sh.item_free[old], ((iu >> 1) - 1) & 1, waits, a.stats)) break;
-        used = kSplit || !*const_cast<volatile int*>(&sh.again[old]);
-        if (!kSplit && used && !live && iu >= 1) {
-          old ^= 1;
-          if (!warp_wait(&sh.item_free[old], ((iu - 1) >> 1) & 1, waits, a.stats)) break;
-          used = !*const_cast<volatile int*>(&sh.again[old]);
-        }
-        PaItem& it = sh.item[iu & 1];
-        if (used) {
-          const int head = hd / (a.group / a.pack), tok = t * 2 * span, n = list.n[s], c = list.c[s];
-          int tiles[2];
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            const int last = min(n, tok + (g + 1) * span) - 1;           // the group's last row that is there
-            const int vis = last >= tok + g * span ? min(c, c - n + last + 1) : 0;
-            tiles[g] = vis > 0 ? (vis + kPrTile - 1) / kPrTile : 0;
+      uint32_t iu = 0;
+      bool ended = false;
+      do {
+        for (; ok; ++iu) {
+          if (used) {
+            const long long i = (long long)no * crew + (no & 1 ? crew - 1 - me : me);
+            hd = (int)(i % heads);
+            live = (!kSplit || no == 0) && prompt_find(order, a.n_seq, list, (int)(i / heads), lane, level, s, t);
+            ++no;
           }
-          const int all = max(tiles[0], tiles[1]), seen = max(min(c, c - n + tok + 1), 0), part = seen / kPrTile;
-          const int begin = (int)((long long)all * rank / shares), end = (int)((long long)all * (rank + 1) / shares);
-          if (lane == 0) {
-            it.live = live;
-            it.s = s;
-            it.tok = tok;
-            it.head = head;
-            it.q_head = hd * a.pack;
-            it.n = n;
-            it.c = c;
-            it.q0 = prompt_begin(a.qs, s);
-            it.k0 = prompt_begin(a.ks, s);
-            it.room = room_of<kBf16>(all);
-            it.seen = seen;
-            it.part = part;
-            it.clean = kSplit ? part : 0x7fffffff;
-            it.begin = begin;
+          // An item that has to be done again goes first, in the place that it had.  (Once the roles have met all are free.)
+          if (iu >= 2 && !ended && !warp_wait(&sh.item_free[iu & 1], ((iu >> 1) - 1) & 1, waits, a.stats)) break;
+          used = kSplit || !*const_cast<volatile int*>(&sh.again[iu & 1]);
+          PaItem& it = sh.item[iu & 1];
+          if (used) {
+            const int head = hd / (a.group / a.pack), tok = t * 2 * span, n = list.n[s], c = list.c[s];
+            int tiles[2];
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
-              it.tiles[g] = tiles[g];
-              it.end[g] = max(min(end, tiles[g]), begin);
+              const int last = min(n, tok + (g + 1) * span) - 1;           // the group's last row that is there
+              const int vis = last >= tok + g * span ? min(c, c - n + last + 1) : 0;
+              tiles[g] = vis > 0 ? (vis + kPrTile - 1) / kPrTile : 0;
             }
-          }
-        } else if (lane == 0) {
-          if (old != (iu & 1)) it = sh.item[old];
-          it.clean = it.part;
-        }
-        if (lane == 0) {
-          sh.again[old] = 0;
-          bar_arrive(&sh.item_full[iu & 1]);
-        }
-        __syncwarp();
-        if (!it.live) break;
-        const int end = max(it.end[0], it.end[1]);
-        const int n_tiles = end - it.begin;
-        if (n_tiles == 0) continue;
-        const int qs = a.qs.first ? 0 : it.s, ks = a.ks.first ? 0 : it.s;
-        for (int j = 0; j < 2 * n_tiles && ok; ++j, ++u) {               // K0 (then Q), V0, K1, V1, ..
-          const uint32_t st = u % P::kStages, use = u / P::kStages;
-          if (use > 0 && !warp_wait(&sh.free[st], (use - 1) & 1, waits, a.stats)) { ok = false; break; }
-          if (leader) {
-            bar_expect(&sh.full[st], P::kMat);
+            const int all = max(tiles[0], tiles[1]), seen = max(min(c, c - n + tok + 1), 0), part = seen / kPrTile;
+            const int begin = (int)((long long)all * rank / shares), end = (int)((long long)all * (rank + 1) / shares);
+            if (lane == 0) {
+              it.live = live;
+              it.s = s;
+              it.tok = tok;
+              it.head = head;
+              it.q_head = hd * a.pack;
+              it.n = n;
+              it.c = c;
+              it.q0 = prompt_begin(a.qs, s);
+              it.k0 = prompt_begin(a.ks, s);
+              it.room = room_of<kBf16>(all);
+              it.seen = seen;
+              it.part = part;
+              it.clean = kSplit ? part : 0x7fffffff;
+              it.begin = begin;
 #pragma unroll
-            for (int b = 0; b < P::kBlocks; ++b)
-              map_load4(kv_smem(ring + st * P::kMat + b * (kPrTile * 128)), j & 1 ? &v_map : &k_map, b * 64, it.head,
-                        it.k0 + (it.begin + (j >> 1)) * kPrTile, ks, &sh.full[st]);
+              for (int g = 0; g < 2; ++g) {
+                it.tiles[g] = tiles[g];
+                it.end[g] = max(min(end, tiles[g]), begin);
+              }
+            }
+          } else if (lane == 0) {
+            it.clean = it.part;
+          }
+          if (lane == 0) {
+            sh.again[iu & 1] = 0;
+            bar_arrive(&sh.item_full[iu & 1]);
           }
           __syncwarp();
-          if (j == 0) {
-            if (qu > 0 && !warp_wait(&sh.qfree, (qu - 1) & 1, waits, a.stats)) { ok = false; break; }
-            ++qu;
+          if (!it.live) { ended = true; break; }
+          const int end = max(it.end[0], it.end[1]);
+          const int n_tiles = end - it.begin;
+          if (n_tiles == 0) continue;
+          const int qs = a.qs.first ? 0 : it.s, ks = a.ks.first ? 0 : it.s;
+          for (int j = 0; j < 2 * n_tiles && ok; ++j, ++u) {               // K0 (then Q), V0, K1, V1, ..
+            const uint32_t st = u % P::kStages, use = u / P::kStages;
+            if (use > 0 && !warp_wait(&sh.free[st], (use - 1) & 1, waits, a.stats)) { ok = false; break; }
             if (leader) {
-              bar_expect(&sh.qfull, 2 * P::kMat);
+              bar_expect(&sh.full[st], P::kMat);
 #pragma unroll
-              for (int g = 0; g < 2; ++g)
-#pragma unroll
-                for (int b = 0; b < P::kBlocks; ++b)
-                  map_load4(kv_smem(qmat + g * P::kMat + b * (kPrTile * 128)), &q_map, b * 64, it.q_head,
-                            it.q0 + it.tok + g * span, qs, &sh.qfull);
+              for (int b = 0; b < P::kBlocks; ++b)
+                map_load4(kv_smem(ring + st * P::kMat + b * (kPrTile * 128)), j & 1 ? &v_map : &k_map, b * 64, it.head,
+                          it.k0 + (it.begin + (j >> 1)) * kPrTile, ks, &sh.full[st]);
             }
             __syncwarp();
+            if (j == 0) {
+              if (qu > 0 && !warp_wait(&sh.qfree, (qu - 1) & 1, waits, a.stats)) { ok = false; break; }
+              ++qu;
+              if (leader) {
+                bar_expect(&sh.qfull, 2 * P::kMat);
+#pragma unroll
+                for (int g = 0; g < 2; ++g)
+#pragma unroll
+                  for (int b = 0; b < P::kBlocks; ++b)
+                    map_load4(kv_smem(qmat + g * P::kMat + b * (kPrTile * 128)), &q_map, b * 64, it.q_head,
+                              it.q0 + it.tok + g * span, qs, &sh.qfull);
+              }
+              __syncwarp();
+            }
           }
         }
-      }
+      } while (!over(iu++));
     } else if (warp == kPaIssuer) {
       // ========================================================== products =======
       const uint32_t s_idesc = idesc_16(kPrTile, false, kBf16) | (a.negate ? kNegateA : 0u);
@@ -670,159 +679,165 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       const bool leader = one_lane();
       uint32_t u = 0, qu = 0, cu = 0, pu[2] = {0, 0};
       bool ok = true;
-      for (uint32_t iu = 0; ok; ++iu) {
-        if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, waits, a.stats)) break;
-        const int live = sh.item[iu & 1].live, begin = sh.item[iu & 1].begin, tiles0 = sh.item[iu & 1].end[0] - begin,
-                  tiles1 = sh.item[iu & 1].end[1] - begin, clean = min(sh.item[iu & 1].clean, sh.item[iu & 1].c / kPrTile) - begin;
-        __syncwarp();
-        if (lane == 0) bar_arrive(&sh.item_free[iu & 1]);
-        if (!live) break;
-        const int n_tiles = max(tiles0, tiles1);
-        if (n_tiles == 0) continue;
-        auto landed = [&](uint32_t v) { ok = ok && warp_wait(&sh.full[v % P::kStages], (v / P::kStages) & 1, waits, a.stats); };
-        auto scores = [&](int g, uint32_t kv) {          // of group g, keys in ring place kv
-          const uint64_t kd = k_desc + (kv % P::kStages) * kStage;
-          if (leader) {
+      uint32_t iu = 0;
+      do {
+        for (; ok; ++iu) {
+          if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, waits, a.stats)) break;
+          const int live = sh.item[iu & 1].live, begin = sh.item[iu & 1].begin, tiles0 = sh.item[iu & 1].end[0] - begin,
+                    tiles1 = sh.item[iu & 1].end[1] - begin, clean = min(sh.item[iu & 1].clean, sh.item[iu & 1].c / kPrTile) - begin;
+          __syncwarp();
+          if (lane == 0) bar_arrive(&sh.item_free[iu & 1]);
+          if (!live) break;
+          const int n_tiles = max(tiles0, tiles1);
+          if (n_tiles == 0) continue;
+          auto landed = [&](uint32_t v) { ok = ok && warp_wait(&sh.full[v % P::kStages], (v / P::kStages) & 1, waits, a.stats); };
+          auto scores = [&](int g, uint32_t kv) {          // of group g, keys in ring place kv
+            const uint64_t kd = k_desc + (kv % P::kStages) * kStage;
+            if (leader) {
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-              const uint64_t off = (uint64_t)((k >> 2) * (kPrTile * 128 >> 4) + (k & 3) * 2);
-              mma_ss(tmem + g * 128, q_desc + g * kStage + off, kd + off, s_idesc, k > 0);
+              for (int k = 0; k < D / 16; ++k) {
+                const uint64_t off = (uint64_t)((k >> 2) * (kPrTile * 128 >> 4) + (k & 3) * 2);
+                mma_ss(tmem + g * 128, q_desc + g * kStage + off, kd + off, s_idesc, k > 0);
+              }
+              commit(&sh.sfull[g]);
             }
-            commit(&sh.sfull[g]);
+            __syncwarp();
+          };
+          landed(u);
+          ok = ok && warp_wait(&sh.qfull, qu++ & 1, waits, a.stats);
+          if (!ok) break;
+          fence_after();
+          if (tiles0 > 0) scores(0, u);
+          if (tiles1 > 0) scores(1, u);
+          if (leader) {
+            commit(&sh.free[u % P::kStages]);
+            if (n_tiles == 1) commit(&sh.qfree);
           }
           __syncwarp();
-        };
-        landed(u);
-        ok = ok && warp_wait(&sh.qfull, qu++ & 1, waits, a.stats);
-        if (!ok) break;
-        fence_after();
-        if (tiles0 > 0) scores(0, u);
-        if (tiles1 > 0) scores(1, u);
-        if (leader) {
-          commit(&sh.free[u % P::kStages]);
-          if (n_tiles == 1) commit(&sh.qfree);
-        }
-        __syncwarp();
-        for (int j = 0; j < n_tiles && ok; ++j) {
-          const uint32_t vu = u + 2 * j + 1, ku = vu + 1;
-          landed(vu);
-          if (ok && j >= clean) {                        // (while the softmax warps are at work on the scores)
-            if (lane == 0) {
-              sh.asked = vu;
-              bar_arrive(&sh.ask);
+          for (int j = 0; j < n_tiles && ok; ++j) {
+            const uint32_t vu = u + 2 * j + 1, ku = vu + 1;
+            landed(vu);
+            if (ok && j >= clean) {                        // (while the softmax warps are at work on the scores)
+              if (lane == 0) {
+                sh.asked = vu;
+                bar_arrive(&sh.ask);
+              }
+              __syncwarp();
+            }
+            if (j + 1 < n_tiles) landed(ku);
+            if (ok && j >= clean) ok = warp_wait(&sh.clean, cu++ & 1, waits, a.stats);
+            if (!ok) break;
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+              const int mine = g ? tiles1 : tiles0;
+              if (j < mine) {
+                const uint64_t vd = v_desc + (vu % P::kStages) * kStage;
+#pragma unroll
+                for (int h = 0; h < 2 && ok; ++h) {        // half of the keys at a time, as the probabilities come
+                  if (!warp_wait(&sh.pfull[g][h], pu[g] & 1, waits, a.stats)) { ok = false; break; }
+                  fence_after();
+                  if (leader) {
+#pragma unroll
+                    for (int k = h * kPrTile / 32; k < (h + 1) * kPrTile / 32; ++k)
+                      mma_ts(tmem + 256 + g * 128, tmem + g * 128 + k * 8, vd + (uint64_t)(k * 2048 >> 4), o_idesc, j > 0 || k > 0);
+                    if (h == 1 && j + 1 == mine) commit(&sh.ofull[g]);
+                  }
+                  __syncwarp();
+                }
+                ++pu[g];
+                if (!ok) break;
+                if (j + 1 < mine) scores(g, ku);
+              }
+            }
+            if (!ok) break;
+            if (leader) {
+              commit(&sh.free[vu % P::kStages]);
+              if (j + 1 < n_tiles) commit(&sh.free[ku % P::kStages]);
+              if (j + 2 == n_tiles) commit(&sh.qfree);
             }
             __syncwarp();
           }
-          if (j + 1 < n_tiles) landed(ku);
-          if (ok && j >= clean) ok = warp_wait(&sh.clean, cu++ & 1, waits, a.stats);
-          if (!ok) break;
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            const int mine = g ? tiles1 : tiles0;
-            if (j < mine) {
-              const uint64_t vd = v_desc + (vu % P::kStages) * kStage;
-#pragma unroll
-              for (int h = 0; h < 2 && ok; ++h) {        // half of the keys at a time, as the probabilities come
-                if (!warp_wait(&sh.pfull[g][h], pu[g] & 1, waits, a.stats)) { ok = false; break; }
-                fence_after();
-                if (leader) {
-#pragma unroll
-                  for (int k = h * kPrTile / 32; k < (h + 1) * kPrTile / 32; ++k)
-                    mma_ts(tmem + 256 + g * 128, tmem + g * 128 + k * 8, vd + (uint64_t)(k * 2048 >> 4), o_idesc, j > 0 || k > 0);
-                  if (h == 1 && j + 1 == mine) commit(&sh.ofull[g]);
-                }
-                __syncwarp();
-              }
-              ++pu[g];
-              if (!ok) break;
-              if (j + 1 < mine) scores(g, ku);
-            }
-          }
-          if (!ok) break;
-          if (leader) {
-            commit(&sh.free[vu % P::kStages]);
-            if (j + 1 < n_tiles) commit(&sh.free[ku % P::kStages]);
-            if (j + 2 == n_tiles) commit(&sh.qfree);
-          }
-          __syncwarp();
+          u += 2 * n_tiles;
         }
-        u += 2 * n_tiles;
-      }
+      } while (!over(iu++));
     } else {
       // ========================================================== values =========
       const int who = warp - kPaCleaner;
       uint32_t au = 0, cleaned = 0;
       bool ok = true;
-      for (uint32_t iu = 0; ok; ++iu) {
-        if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, waits, a.stats)) break;
-        const PaItem& now = sh.item[iu & 1];
-        if (!now.live) break;
-        const int c = now.c, end = max(now.end[0], now.end[1]);
-        int from = 0x7fffffff, to = 0;
-        for (int j = max(now.begin, min(now.clean, c / kPrTile)); j < end; ++j, ++au) {
-          if (!warp_wait(&sh.ask, au & 1, waits, a.stats)) { ok = false; break; }
-          const uint32_t vu = *const_cast<volatile uint32_t*>(&sh.asked);
-          // (it has landed, and stays until these warps are through with it)
-          if (!warp_wait(&sh.full[vu % P::kStages], (vu / P::kStages) & 1, waits, a.stats)) { ok = false; break; }
-          uint4* tile = reinterpret_cast<uint4*>(ring + vu % P::kStages * P::kMat);
-          // (a block of 64 channels: rows of 128 bytes, whatever their swizzle)
-          const bool zero = j < now.clean;               // behind the last key; the other values as they are
-          const int first = max((zero ? c : now.seen) - j * kPrTile, 0) * 8 + who * 32 + lane;
-          for (int b = 0; b < P::kBlocks; ++b, tile += kPrTile * 8) {
-            if (zero) {
-              for (int i = first; i < kPrTile * 8; i += 32 * kPaCleaners) tile[i] = make_uint4(0u, 0u, 0u, 0u);
-              continue;
-            }
+      uint32_t iu = 0;
+      do {
+        for (; ok; ++iu) {
+          if (!warp_wait(&sh.item_full[iu & 1], (iu >> 1) & 1, waits, a.stats)) break;
+          const PaItem& now = sh.item[iu & 1];
+          if (!now.live) break;
+          const int c = now.c, end = max(now.end[0], now.end[1]);
+          int from = 0x7fffffff, to = 0;
+          for (int j = max(now.begin, min(now.clean, c / kPrTile)); j < end; ++j, ++au) {
+            if (!warp_wait(&sh.ask, au & 1, waits, a.stats)) { ok = false; break; }
+            const uint32_t vu = *const_cast<volatile uint32_t*>(&sh.asked);
+            // (it has landed, and stays until these warps are through with it)
+            if (!warp_wait(&sh.full[vu % P::kStages], (vu / P::kStages) & 1, waits, a.stats)) { ok = false; break; }
+            uint4* tile = reinterpret_cast<uint4*>(ring + vu % P::kStages * P::kMat);
+            // (a block of 64 channels: rows of 128 bytes, whatever their swizzle)
+            const bool zero = j < now.clean;               // behind the last key; the other values as they are
+            const int first = max((zero ? c : now.seen) - j * kPrTile, 0) * 8 + who * 32 + lane;
+            for (int b = 0; b < P::kBlocks; ++b, tile += kPrTile * 8) {
+              if (zero) {
+                for (int i = first; i < kPrTile * 8; i += 32 * kPaCleaners) tile[i] = make_uint4(0u, 0u, 0u, 0u);
+                continue;
+              }
 #pragma unroll 2
-            for (int i = first; i < kPrTile * 8; i += 32 * kPaCleaners) {
-              uint4 w = tile[i];
-              const uint32_t x = odd_halves<kBf16>(w.x), y = odd_halves<kBf16>(w.y), z = odd_halves<kBf16>(w.z), q = odd_halves<kBf16>(w.w);
-              if (x | y | z | q) {
-                w.x &= ~((x >> 15) * 0xffffu);
-                w.y &= ~((y >> 15) * 0xffffu);
-                w.z &= ~((z >> 15) * 0xffffu);
-                w.w &= ~((q >> 15) * 0xffffu);
-                tile[i] = w;
-                const int key = j * kPrTile + (i >> 3);
-                if (key < c) {
-                  from = min(from, key);
-                  to = max(to, key + 1);
+              for (int i = first; i < kPrTile * 8; i += 32 * kPaCleaners) {
+                uint4 w = tile[i];
+                const uint32_t x = odd_halves<kBf16>(w.x), y = odd_halves<kBf16>(w.y), z = odd_halves<kBf16>(w.z), q = odd_halves<kBf16>(w.w);
+                if (x | y | z | q) {
+                  w.x &= ~((x >> 15) * 0xffffu);
+                  w.y &= ~((y >> 15) * 0xffffu);
+                  w.z &= ~((z >> 15) * 0xffffu);
+                  w.w &= ~((q >> 15) * 0xffffu);
+                  tile[i] = w;
+                  const int key = j * kPrTile + (i >> 3);
+                  if (key < c) {
+                    from = min(from, key);
+                    to = max(to, key + 1);
+                  }
                 }
               }
             }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) bar_arrive(&sh.clean);
           }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          if (!ok) break;
+          if (now.clean == now.part) {
+            from = __reduce_min_sync(0xffffffffu, from);
+            to = __reduce_max_sync(0xffffffffu, to);
+            if (lane == 0) {
+              sh.odd[who] = {from, to};
+              bar_arrive(&sh.found);
+            }
+            if (!kSplit) {                                 // (a cluster's rows are joined with them)
+              if (!warp_wait(&sh.found, cleaned & 1, waits, a.stats) || !warp_wait(&sh.written, cleaned & 1, waits, a.stats)) break;
+              ++cleaned;
+              from = min(sh.odd[0].from, sh.odd[1].from);
+              to = max(sh.odd[0].to, sh.odd[1].to);
+              if (from < to) odd_rows<D, kBf16>(a, now, sh.ml, who * 128, from, to, lane);
+            }
+          }
           __syncwarp();
-          if (lane == 0) bar_arrive(&sh.clean);
+          if (lane == 0) bar_arrive(&sh.item_free[iu & 1]);
         }
-        if (!ok) break;
-        if (now.clean == now.part) {
-          from = __reduce_min_sync(0xffffffffu, from);
-          to = __reduce_max_sync(0xffffffffu, to);
-          if (lane == 0) {
-            sh.odd[who] = {from, to};
-            bar_arrive(&sh.found);
-          }
-          if (!kSplit) {                                 // (a cluster's rows are joined with them)
-            if (!warp_wait(&sh.found, cleaned & 1, waits, a.stats) || !warp_wait(&sh.written, cleaned & 1, waits, a.stats)) break;
-            ++cleaned;
-            from = min(sh.odd[0].from, sh.odd[1].from);
-            to = max(sh.odd[0].to, sh.odd[1].to);
-            if (from < to) odd_rows<D, kBf16>(a, now, sh.ml, who * 128, from, to, lane);
-          }
-        }
-        __syncwarp();
-        if (lane == 0) bar_arrive(&sh.item_free[iu & 1]);
-      }
+      } while (!over(iu++));
     }
     // Nothing follows the roles: code that all warps share may use any register that the block was launched with, and
     // these warps have given most of theirs away.
     if (kSplit) {
       meet_cluster();
       meet_cluster();
+      fence_before();
+      __syncthreads();
     }
-    fence_before();
-    __syncthreads();
     if (warp == kPaIssuer) {
       fence_after();
       // The softmax warps waited for the last products, and the products for the last copies, unless
