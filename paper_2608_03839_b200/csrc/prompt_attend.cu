@@ -94,8 +94,8 @@ __device__ __forceinline__ float row_shift(float m, float f, float room) {
 }
 // log2 of what sums and accumulators under the maximum `from` are multiplied with to be under `to`
 __device__ __forceinline__ float row_fall(float from, float to, float f, float room) {
-  if (from == -INFINITY || row_far(from, f) || row_far(to, f)) return (from - to) * f;
-  return row_shift(to, f, room) - row_shift(from, f, room);
+  const float far = (from - to) * f, near = row_shift(to, f, room) - row_shift(from, f, room);
+  return fabsf(from * f) <= kPaFar && fabsf(to * f) <= kPaFar ? near : far;      // (branches here took a microsecond an item)
 }
 // (the room is taken out of the sum, which is exact: as part of the logarithm it would cost its last bits)
 __device__ __forceinline__ float row_lse(float m, float l, float f, float room) {
