@@ -780,7 +780,9 @@ typedef struct {
  * natural logarithm of the row's sum of exponentials; lse_strides (host): its strides in elements for
  * sequence, row and head, NULL: contiguous [n_seq, rows, n_q_heads] or [rows, n_q_heads].  A row that
  * sees nothing gets out = 0 and lse = -inf, and so do padded rows behind count[s].  Keys and values that a
- * row does not see do not reach it, whatever they hold.  out overlaps no input.
+ * row does not see do not reach it, whatever they hold; infinities and NaN among the values that it sees do (rows near
+ * them are computed twice).  Where those are finite out is, too: it ends at the type's largest number.  Scores may be of any
+ * size that fp32 holds as q.k; lse is infinite where scale * q.k is more.  out overlaps no input.
  */
 int oilbird_prompt_attend(const oilbird_prompt* prompt, const oilbird_kv_rows* q, const oilbird_kv_rows* k,
                           const oilbird_kv_rows* v, float scale, const oilbird_kv_rows* out, float* lse,
@@ -788,7 +790,8 @@ int oilbird_prompt_attend(const oilbird_prompt* prompt, const oilbird_kv_rows* q
 /*
  * weight (dev fp32 [n_seq, n_kv_heads, k.rows], packed [n_kv_heads, k.rows], written) = sum over the query
  * rows i that see the key and the head's query heads of row_weight[i] * exp(scale * q.k - lse), with
- * attend()'s arguments and its lse.  row_weight: dev fp32 [n_seq, q.rows] or [q.rows], NULL: 1; rows
+ * attend()'s arguments and its lse (a row of NaN, or of a weight that is not finite, reaches the keys that it sees and no
+ * others; one of lse +inf counts for nothing).  row_weight: dev fp32 [n_seq, q.rows] or [q.rows], NULL: 1; rows
  * with weight 0 do not count, whatever they hold, and those in front of a sequence's first and behind
  * its last other one cost next to nothing.  Padded keys behind count[s] get 0.
  */
