@@ -38,9 +38,9 @@
 // Measured, with 32 query heads over 8 key heads of 128: one prompt of 32,768 tokens in 7.57 ms (8.8 TFLOP, 1,162
 // TFLOP/s; 6.3 ms at cuBLAS's sustained rate), 16 of up to 2,048 in 219 us (an infinity that all their rows see, so that
 // every item is done twice: 2.4 times as long), one of 37 in 10.8 us, one token over 32,768 keys in 71 us (64
-// blocks, and half of each idles: an item of few rows has none for group B).  Heads of 64: 8,192 tokens in 345 us.  What bounds long prompts is power: 990 W at 1,520 MHz, where a step of 256
-// rows by 128 keys takes 3,200 cycles, its exponentials and its products 2,048 each (tensor pipe 59 %, exponential
-// unit 60 %).  Polynomials in place of an eighth to half of the exponentials were slower by 1 to 7 %.  A row
+// blocks, and half of each idles: an item of few rows has none for group B).  Heads of 64: 8,192 tokens in 345 us.
+// What bounds long prompts is power: 990 W at 1,520 MHz, where a step of 256 rows by 128 keys takes 3,200 cycles, its
+// exponentials and its products 2,048 each (tensor pipe 59 %, exponential unit 60 %).  Polynomials in place of an eighth to half of the exponentials were slower by 1 to 7 %.  A row
 // a thread, with 8 warps, left the exponentials to two warps an SM quarter (7.9 ms).
 // Short prompts wait for an item's chain: loads, products, a tile's exponentials, products, the rows' way out.
 //
@@ -105,12 +105,12 @@ __device__ __forceinline__ float row_lse(float m, float l, float f, float room) 
 }
 struct PaShared {
   uint64_t full[16], free[16], qfull, qfree, sfull[2], pfull[2][2], ofull[2], item_full[2], item_free[2], meet;
-  uint64_t ask, clean, found, written;
+  uint64_t ask, clean, found, written[2];
   PaItem item[2];
   int again[2];                                          // the item has to be done again, with clean values
   uint32_t asked;                                        // the use of the ring whose values are to be cleaned
   struct Odd { int from, to; } odd[kPaCleaners];         // keys among which values were taken out
-  float2 ml[256];                                        // maxima and sums of A's rows and B's, of items that are cleaned
+  float2 ml[2][256];                                     // maxima and sums of A's rows and B's, of items that are cleaned
   uint32_t tmem;
   Waits waits;
 };
@@ -187,7 +187,8 @@ __device__ __forceinline__ void add_odd(const PromptArgs& a, const PaItem& it, i
 // The values among keys [from, to) that were taken out, added to those of an item's rows [row0, row0 + 128) that see them; a
 // warp.  The rows' tokens rise, and so does what they see.
 template <int D, bool kBf16>
-__device__ __forceinline__ void odd_rows(const PromptArgs& a, const PaItem& it, const float2* ml, int row0, int from, int to, int lane) {
+__device__ __forceinline__ void odd_rows(const PromptArgs& a, const PaItem& it, const float2* ml, int row0, int from, int to,
+                                         int lane) {
   float2 sum[D / 64];
 #pragma unroll
   for (int e = 0; e < D / 64; ++e) sum[e] = make_float2(0.f, 0.f);
@@ -234,7 +235,7 @@ __device__ __forceinline__ void leave_rows(float* acc, uint32_t o_tm, int row0) 
 template <int D, bool kBf16>
 __device__ __noinline__ void join_rows(const PromptArgs& a, PaShared& sh, float* acc, int shares, int rank) {
   const PaItem& it = sh.item[0];
-  float2* ml = sh.ml;
+  float2* ml = sh.ml[0];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   cg::cluster_group cluster = cg::this_cluster();
   constexpr int E = D / 64;                            // pairs of channels a lane
@@ -308,12 +309,12 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
       bar_init(&sh.ofull[i], 1);
       bar_init(&sh.item_full[i], 1);
       bar_init(&sh.item_free[i], kPaSoftWarps + 1 + kPaCleaners);
+      bar_init(&sh.written[i], kPaSoftWarps);
       sh.again[i] = 0;
     }
     bar_init(&sh.ask, 1);
     bar_init(&sh.clean, kPaCleaners);
     bar_init(&sh.found, kPaCleaners);
-    bar_init(&sh.written, kPaSoftWarps);
     for (int x = 0; x < kPaCleaners; ++x) sh.odd[x] = {0x7fffffff, 0};
     sh.item[0].live = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -389,7 +390,8 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
           for (int r = 0; r < 2; ++r) {
             float y[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-            for (int i = 0; i < 16; ++i) y[i & 1] = max3(y[i & 1], __uint_as_float(x[4 * i + 2 * r]), __uint_as_float(x[4 * i + 2 * r + 1]));
+            for (int i = 0; i < 16; ++i)
+              y[i & 1] = max3(y[i & 1], __uint_as_float(x[4 * i + 2 * r]), __uint_as_float(x[4 * i + 2 * r + 1]));
             mx[r] = fmaxf(y[0], y[1]);
           }
 #pragma unroll
@@ -476,8 +478,8 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
         }
         if (kSplit) {                                      // (a cluster has one item, joined below)
           if (quad == 0) {
-            sh.ml[wg * 128 + row0] = make_float2(m[0], l[0]);
-            sh.ml[wg * 128 + row0 + 8] = make_float2(m[1], l[1]);
+            sh.ml[0][wg * 128 + row0] = make_float2(m[0], l[0]);
+            sh.ml[0][wg * 128 + row0 + 8] = make_float2(m[1], l[1]);
           }
           break;
         }
@@ -519,7 +521,8 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
               uint32_t w[4];                               // columns 8i + 2 quad, .. of the 32
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const float2 x = make_float2(__uint_as_float(o[4 * i + 2 * r]), __uint_as_float(o[4 * i + 2 * r + 1])), u = mul2(x, inv[r]);
+                const float2 x = make_float2(__uint_as_float(o[4 * i + 2 * r]), __uint_as_float(o[4 * i + 2 * r + 1]));
+                const float2 u = mul2(x, inv[r]);
                 odd2[r] = fma2(x, make_float2(zero, zero), odd2[r]);           // (NaN once one is not finite)
                 w[i] = l[r] == 0.f ? 0u : exact ? pack_result<kBf16>(x.x, x.y, u.x, u.y) : pack_finite<kBf16>(u.x, u.y);
               }
@@ -544,13 +547,15 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
             break;
           }
         }
-        if (it.clean == it.part) {                         // (warps 18 and 19 add what they have taken out)
+        // Warps 18 and 19 add what they have taken out.  (A group without tiles may be here while they are still at the item
+        // before: each place has sums and a barrier of its own, and they give it back when they are through.)
+        if (it.clean == it.part) {
           if (quad == 0) {
-            sh.ml[wg * 128 + row0] = make_float2(m[0], l[0]);
-            sh.ml[wg * 128 + row0 + 8] = make_float2(m[1], l[1]);
+            sh.ml[iu & 1][wg * 128 + row0] = make_float2(m[0], l[0]);
+            sh.ml[iu & 1][wg * 128 + row0 + 8] = make_float2(m[1], l[1]);
           }
           __syncwarp();
-          if (lane == 0) bar_arrive(&sh.written);
+          if (lane == 0) bar_arrive(&sh.written[iu & 1]);
         }
         fence_before();
         __syncwarp();
@@ -764,7 +769,7 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
     } else {
       // ========================================================== values =========
       const int who = warp - kPaCleaner;
-      uint32_t au = 0, cleaned = 0;
+      uint32_t au = 0, cu = 0, places = 0;               // places: parities of the items cleaned in either so far
       bool ok = true;
       uint32_t iu = 0;
       do {
@@ -791,7 +796,8 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
 #pragma unroll 2
               for (int i = first; i < kPrTile * 8; i += 32 * kPaCleaners) {
                 uint4 w = tile[i];
-                const uint32_t x = odd_halves<kBf16>(w.x), y = odd_halves<kBf16>(w.y), z = odd_halves<kBf16>(w.z), q = odd_halves<kBf16>(w.w);
+                const uint32_t x = odd_halves<kBf16>(w.x), y = odd_halves<kBf16>(w.y);
+                const uint32_t z = odd_halves<kBf16>(w.z), q = odd_halves<kBf16>(w.w);
                 if (x | y | z | q) {
                   w.x &= ~((x >> 15) * 0xffffu);
                   w.y &= ~((y >> 15) * 0xffffu);
@@ -819,11 +825,12 @@ prompt_attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_con
               bar_arrive(&sh.found);
             }
             if (!kSplit) {                                 // (a cluster's rows are joined with them)
-              if (!warp_wait(&sh.found, cleaned & 1, waits, a.stats) || !warp_wait(&sh.written, cleaned & 1, waits, a.stats)) break;
-              ++cleaned;
+              if (!warp_wait(&sh.found, cu++ & 1, waits, a.stats)) break;
+              if (!warp_wait(&sh.written[iu & 1], places >> (iu & 1) & 1, waits, a.stats)) break;
+              places ^= 1u << (iu & 1);
               from = min(sh.odd[0].from, sh.odd[1].from);
               to = max(sh.odd[0].to, sh.odd[1].to);
-              if (from < to) odd_rows<D, kBf16>(a, now, sh.ml, who * 128, from, to, lane);
+              if (from < to) odd_rows<D, kBf16>(a, now, sh.ml[iu & 1], who * 128, from, to, lane);
             }
           }
           __syncwarp();

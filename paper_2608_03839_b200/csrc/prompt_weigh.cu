@@ -15,9 +15,9 @@
 // (With a query row a thread and 128 sums a thread there were registers for two, and a tile took 3,400 cycles,
 // where its exponentials take 2,048.)
 // Rows that do not count (behind the sequence's last one, weight 0, lse -inf) have -inf there, and the exponents of
-// their columns and of those that do not see the key are replaced, so that it does not matter what they hold.  Leading and trailing rows with weight 0
-// are left out of the tiles: all warps look for the first and the last other one of each long sequence
-// when the kernel begins.
+// their columns and of those that do not see the key are replaced, so that it does not matter what they hold.  Leading
+// and trailing rows with weight 0 are left out of the tiles: all warps look for the first and the
+// last other one of each long sequence when the kernel begins.
 //
 // Sums are fp32: of a tile's 64 columns as four, and over the tiles with the part that each addition
 // loses carried along (a key may receive 10^5 terms).
@@ -29,8 +29,8 @@
 // TFLOP/s; their exponentials at the unit's rate take 88), one of 8,192 in 358 us, the last 64 rows of 4 x 16,384 in 52 us (74
 // MB; eight items a block of two tiles each, 6 us an item, of which the tiles' own time is less than half).  In
 // whole items a tile of 256 keys by 128 rows takes 2,500 cycles, the exponentials 2,048 of them; shared by a cluster (one
-// prompt of 4,096) the unit is busy 55 % of the time that a block runs.  A polynomial in place of an eighth of the exponentials gave 4 %, more of them
-// less; not kept.
+// prompt of 4,096) the unit is busy 55 % of the time that a block runs.  A polynomial in place of an eighth of the
+// exponentials gave 4 %, more of them less; not kept.
 //
 // Every wait is bounded, as in attention.
 #include <cooperative_groups.h>
