@@ -35,9 +35,9 @@
 // by a cluster of blocks.  Each leaves its rows' maxima, sums and accumulators in its shared memory, and a
 // part of the rows is joined by each block, in the order of the keys.
 //
-// Measured, with 32 query heads over 8 key heads of 128: one prompt of 32,768 tokens in 7.57 ms (8.8 TFLOP, 1,162
+// Measured, with 32 query heads over 8 key heads of 128: one prompt of 32,768 tokens in 7.5 ms (8.8 TFLOP, 1,174
 // TFLOP/s; 6.3 ms at cuBLAS's sustained rate), 16 of up to 2,048 in 219 us (an infinity that all their rows see, so that
-// every item is done twice: 2.4 times as long), one of 37 in 10.8 us, one token over 32,768 keys in 71 us (64
+// every item is done twice: 2.4 times as long), one of 37 in 10.4 us, one token over 32,768 keys in 71 us (64
 // blocks, and half of each idles: an item of few rows has none for group B).  Heads of 64: 8,192 tokens in 345 us.
 // What bounds long prompts is power: 990 W at 1,520 MHz, where a step of 256 rows by 128 keys takes 3,200 cycles, its
 // exponentials and its products 2,048 each (tensor pipe 59 %, exponential unit 60 %).  Polynomials in place of an eighth to half of the exponentials were slower by 1 to 7 %.  A row

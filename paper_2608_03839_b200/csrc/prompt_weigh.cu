@@ -25,7 +25,7 @@
 // Where there are fewer items than SMs the rows of an item are shared by a cluster of blocks, whose
 // totals are added in order.
 //
-// Measured, with 32 query heads over 8 key heads of 128: 16 prompts of up to 2,048 rows in 155 us (101 GFLOP, 650
+// Measured, with 32 query heads over 8 key heads of 128: 16 prompts of up to 2,048 rows in 153 us (101 GFLOP, 660
 // TFLOP/s; their exponentials at the unit's rate take 88), one of 8,192 in 358 us, the last 64 rows of 4 x 16,384 in 52 us (74
 // MB; eight items a block of two tiles each, 6 us an item, of which the tiles' own time is less than half).  In
 // whole items a tile of 256 keys by 128 rows takes 2,500 cycles, the exponentials 2,048 of them; shared by a cluster (one
